@@ -264,7 +264,7 @@ def _own(s):
     if "p" not in s:                                             # what a program keeps: the parameters, the scratch, the outputs' buffers
         s["cache"] = B.PagedCache(s["k"], s["v"], s["table"], s["lens"])
         s["p"] = B.make_paged_params(s["cache"], s["rows"], c["h_q"], causal=c["causal"])
-        s["ws"] = B.alloc_paged_workspace(s["p"], DEV)
+        s["ws"] = B.alloc_paged_workspace(s["p"], DEV, evict=c["kind"] == "evict")
         if c["kind"] == "attend":
             s["o"] = torch.empty_like(s["q"])
             s["lse_out"] = torch.empty((s["rows"], c["h_q"]), dtype=torch.float32, device=DEV)
