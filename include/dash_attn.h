@@ -299,6 +299,89 @@ int dash_kbar_summarize_backward(const dash_params* p, const void* k, const floa
                                  const int64_t* qbar_stride, const float* dkbar, void* dk,
                                  float* dqbar, void* stream);
 
+/* ---- Paged cache: keys and values in pages, shared by sequences of any length ----------
+ *
+ * What a serving program does around the calls above: its dense layers' keys and values lie in
+ * pages of a pool, prompts enter in chunks beside sequences that decode, and caches are held to
+ * a budget by dropping the tokens that attention gives the least weight.
+ *
+ * Layout
+ *   k_pages, v_pages  [n_pages, h_kv, page_size, d], d contiguous, the other strides in elements (k_stride, v_stride)
+ *   table     int32 [batch, max_pages] contiguous: page i of sequence b holds its tokens i*page_size ...;
+ *             entries behind a sequence's last token are not used
+ *   lens      int32 [batch]: tokens in the cache of each sequence, its new ones included; clamped to
+ *             [0, max_pages*page_size] by the kernels
+ *   row_start int32 [batch+1], ascending: the new tokens of sequence b are the packed rows row_start[b] ..
+ *             row_start[b+1]-1 of q, o, k_new, v_new, in order, and its last tokens: the t-th of m sits at slot
+ *             lens[b]-m+t.  A sequence may have none.  Rows of no sequence are neither read nor written.
+ *   weights   fp32, pos int32, both [n_pages, h_kv, page_size] contiguous: the attention weight every token
+ *             has received and its position in the sequence.  Only evicting callers need them.
+ * All of these are device pointers; nothing about the lengths is known to the host, so a captured graph
+ * serves any lengths that fit its n_rows, batch and max_pages.  A table entry outside [0, n_pages) is never
+ * followed: reads take some page of the pool, writes leave the token out.
+ * Limits: head_dim 64 or 128; h_q / h_kv in {1, 2, 4, 8, 16}; page_size a power of two from 16 to 1024;
+ * max_pages * page_size <= 2^24; a page's slice of one head below 2 GiB (DASH_EUNSUPPORTED beyond them).
+ * NaN and infinities: as above, and what the pages hold behind a sequence's last token reaches nothing. */
+typedef struct dash_paged_params {
+  int32_t batch;       /* sequences, >= 1                                             */
+  int32_t h_q, h_kv;   /* query and key/value heads                                   */
+  int32_t head_dim;    /* 64 or 128                                                   */
+  int32_t dtype;       /* DASH_F32 or DASH_BF16: element type of q, k, v, o           */
+  int32_t causal;      /* 1: a new token sees the tokens up to itself; 0: all of its sequence */
+  int32_t page_size;   /* tokens of a page                                            */
+  int32_t n_pages;     /* pages of the pool                                           */
+  int32_t max_pages;   /* entries of a table row                                      */
+  int32_t n_rows;      /* packed rows, >= 1                                           */
+  float scale;         /* logit scale; <= 0 selects 1/sqrt(head_dim)                  */
+  int32_t reserved;    /* 0                                                           */
+  int64_t q_stride[2]; /* row, head strides of q, in elements                         */
+  int64_t o_stride[2];
+  int64_t k_new_stride[2];
+  int64_t v_new_stride[2];
+  int64_t k_stride[3]; /* page, head, token strides of k_pages, in elements           */
+  int64_t v_stride[3];
+} dash_paged_params;
+
+/* Bytes of scratch for dash_paged_attend and dash_paged_weigh, and for dash_paged_evict (host computation
+ * only), whatever n_rows is.  256-byte aligned; of one call at a time, as above. */
+int dash_paged_workspace_bytes(const dash_paged_params* p, size_t* out_bytes);
+int dash_paged_evict_workspace_bytes(const dash_paged_params* p, size_t* out_bytes);
+
+/* Writes the new tokens' keys and values [n_rows, h_kv, d] into the pages of their sequences.  weights (optional):
+ * a new token's is set to 0.  pos (optional): a new token's is set to seen[b]-m+t, or to its slot where seen is NULL;
+ * seen int32 [batch]: tokens of the sequence so far, the evicted and the new ones included. */
+int dash_paged_append(const dash_paged_params* p, const void* k_new, const void* v_new, void* k_pages, void* v_pages,
+                      const int32_t* row_start, const int32_t* lens, const int32_t* table, float* weights, int32_t* pos,
+                      const int32_t* seen, void* stream);
+
+/* Attention of the new tokens over the cache (Eq. 1), which holds their own keys and values already:
+ *   o   out [n_rows, h_q, d]
+ *   lse out, optional, fp32 [n_rows, h_q] contiguous: log of the sum of e^logit over what the row sees
+ * A row that sees nothing gets o = 0 and lse = -inf.  The result of a row does not depend on what else is in flight, but
+ * its last bits may on the lengths beside it (they decide how long caches are cut). */
+int dash_paged_attend(const dash_paged_params* p, const void* q, const void* k_pages, const void* v_pages,
+                      const int32_t* row_start, const int32_t* lens, const int32_t* table, void* o, float* lse,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Adds the weight that the new tokens' attention gives to every cached token of their sequences: weights[token, kv-head] +=
+ * the sum over the rows that see it and the heads of its group of e^(logit - lse), lse as dash_paged_attend wrote it.
+ * last > 0: only the last `last` new tokens of each sequence weigh (an observation window); 0: all. */
+int dash_paged_weigh(const dash_paged_params* p, const void* q, const void* k_pages, const int32_t* row_start,
+                     const int32_t* lens, const int32_t* table, const float* lse, int32_t last, float* weights,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* Cuts every sequence that holds more than `budget` tokens to the budget, for each kv-head by itself: of its tokens
+ * those stay that are protected (pos < sinks, or pos >= seen[b] - recent), then those with the largest weights; among equals
+ * the lowest slots; NaN counts as less than anything.  Kept tokens behind the budget move, in ascending order, into the slots before it that
+ * were freed, with their weights and positions; all others stay where they are.  lens (in/out) becomes
+ * min(lens, budget); pages behind it may be given to others.  n_rows and the strides of q, o, k_new, v_new are not used.
+ *   src  out, optional, int32 [batch, h_kv, budget]: the slot each kept token was at; -1 behind the sequence's end
+ * budget >= 1, 0 <= sinks, 0 <= recent, sinks + recent <= budget.  Two sequences that share pages must not both be
+ * cut, nor one be read by the other afterwards. */
+int dash_paged_evict(const dash_paged_params* p, void* k_pages, void* v_pages, int32_t* lens, const int32_t* seen,
+                     const int32_t* table, float* weights, int32_t* pos, int32_t budget, int32_t sinks, int32_t recent,
+                     int32_t* src, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Static, NUL-terminated description of a dash_status. */
 const char* dash_strerror(int code);
 

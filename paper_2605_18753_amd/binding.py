@@ -37,9 +37,19 @@ class dash_params(ctypes.Structure):
     ]
 
 
+class dash_paged_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "h_q", "h_kv", "head_dim", "dtype", "causal", "page_size", "n_pages",
+                                              "max_pages", "n_rows")]
+    _fields_ += [("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
+    _fields_ += [(n, ctypes.c_int64 * k) for n, k in (("q_stride", 2), ("o_stride", 2), ("k_new_stride", 2), ("v_new_stride", 2),
+                                                      ("k_stride", 3), ("v_stride", 3))]
+
+
 _lib = None
 _P = ctypes.POINTER(dash_params)
+_PP = ctypes.POINTER(dash_paged_params)
 _V = ctypes.c_void_p
+_I = ctypes.c_int32
 _SIGNATURES = {
     "dash_list_stride": (ctypes.c_int32, [_P]),
     "dash_mask_words": (ctypes.c_int32, [_P]),
@@ -58,6 +68,12 @@ _SIGNATURES = {
     "dash_attn_backward_workspace_bytes": (ctypes.c_int, [_P, ctypes.POINTER(ctypes.c_size_t)]),
     "dash_attn_backward": (ctypes.c_int, [_P] + [_V] * 13 + [ctypes.c_size_t, _V]),
     "dash_kbar_summarize_backward": (ctypes.c_int, [_P, _V, _V, ctypes.POINTER(ctypes.c_int64), _V, _V, _V, _V]),
+    "dash_paged_workspace_bytes": (ctypes.c_int, [_PP, ctypes.POINTER(ctypes.c_size_t)]),
+    "dash_paged_evict_workspace_bytes": (ctypes.c_int, [_PP, ctypes.POINTER(ctypes.c_size_t)]),
+    "dash_paged_append": (ctypes.c_int, [_PP] + [_V] * 11),
+    "dash_paged_attend": (ctypes.c_int, [_PP] + [_V] * 9 + [ctypes.c_size_t, _V]),
+    "dash_paged_weigh": (ctypes.c_int, [_PP] + [_V] * 6 + [_I, _V, _V, ctypes.c_size_t, _V]),
+    "dash_paged_evict": (ctypes.c_int, [_PP] + [_V] * 7 + [_I, _I, _I, _V, _V, ctypes.c_size_t, _V]),
     "dash_strerror": (ctypes.c_char_p, [ctypes.c_int]),
 }
 
@@ -287,3 +303,127 @@ def dash_kbar_summarize_backward(p, k, qbar: torch.Tensor, dkbar: torch.Tensor, 
 
 def kbar_shape(p: dash_params):
     return (p.batch, p.h_kv, p.n_kv // p.block_size, p.head_dim)
+
+
+# ---- paged cache -----------------------------------------------------------------------------------------------------
+@dataclass
+class PagedCache:
+    """Keys and values of several sequences in pages of a pool (see the header's section on the paged cache).
+    k, v [n_pages, h_kv, page_size, d]; table int32 [batch, max_pages]; lens int32 [batch]; for evicting callers
+    weights (fp32) and pos (int32), both [n_pages, h_kv, page_size], and seen int32 [batch]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    table: torch.Tensor
+    lens: torch.Tensor
+    weights: Optional[torch.Tensor] = None
+    pos: Optional[torch.Tensor] = None
+    seen: Optional[torch.Tensor] = None
+
+    @staticmethod
+    def allocate(batch: int, h_kv: int, n_pages: int, page_size: int, head_dim: int, max_pages: int, device,
+                 dtype=torch.bfloat16, evicting: bool = False) -> "PagedCache":
+        """An empty cache without pages (table entries -1)."""
+        whole = lambda *s: torch.zeros(s, dtype=torch.int32, device=device)  # noqa: E731
+        kv = [torch.zeros((n_pages, h_kv, page_size, head_dim), dtype=dtype, device=device) for _ in range(2)]
+        c = PagedCache(*kv, whole(batch, max_pages).fill_(-1), whole(batch))
+        if evicting:
+            c.weights = torch.zeros((n_pages, h_kv, page_size), dtype=torch.float32, device=device)
+            c.pos, c.seen = whole(n_pages, h_kv, page_size), whole(batch)
+        return c
+
+
+def make_paged_params(cache: PagedCache, n_rows: int, h_q: int, causal: bool = True, scale: float = 0.0) -> dash_paged_params:
+    """Checks the cache's tensors once; the calls below look at their own arguments only.  The strides of q, o, k_new and
+    v_new are those of the tensors each call is given."""
+    k, v, t, n = cache.k, cache.v, cache.table, cache.lens
+    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in (torch.bfloat16, torch.float32):
+        raise DashError("k and v pages: two tensors [n_pages, h_kv, page_size, d] of one type, bf16 or fp32")
+    if k.stride(3) != 1 or v.stride(3) != 1:
+        raise DashError("k and v pages: head_dim must be contiguous")
+    if t.dim() != 2 or n.shape != t.shape[:1] or t.dtype != torch.int32 or n.dtype != torch.int32 or not (t.is_contiguous() and n.is_contiguous()):
+        raise DashError("table [batch, max_pages] and lens [batch]: contiguous int32 tensors")
+    p = dash_paged_params()
+    p.batch, p.max_pages = t.shape
+    p.n_pages, p.h_kv, p.page_size, p.head_dim = k.shape
+    p.h_q, p.n_rows, p.causal, p.scale = h_q, n_rows, int(causal), scale
+    p.dtype = DASH_BF16 if k.dtype == torch.bfloat16 else DASH_F32
+    p.k_stride[:] = k.stride()[:3]
+    p.v_stride[:] = v.stride()[:3]
+    if v.device != k.device:
+        raise DashError("the tensors of a call lie on one device")
+    return p
+
+
+def _paged_call(p: dash_paged_params, cache: PagedCache, row_start, rows, extra=()) -> dash_paged_params:
+    """The call's own copy of p, with the strides of its packed tensors; rows: (tensor, heads, field of its strides)."""
+    p = dash_paged_params.from_buffer_copy(p)
+    if row_start is not None and (row_start.dtype != torch.int32 or not row_start.is_contiguous() or row_start.numel() != p.batch + 1):
+        raise DashError("row_start: a contiguous int32 tensor of batch + 1 elements")
+    for t, heads, field in rows:
+        if t.shape != (p.n_rows, heads, p.head_dim) or t.dtype != cache.k.dtype or t.stride(2) != 1:
+            raise DashError(f"packed rows: [{p.n_rows}, {heads}, {p.head_dim}] of the cache's type, head_dim contiguous")
+        getattr(p, field)[:] = t.stride()[:2]
+    for t, dtype, shape in extra:
+        if t is not None and (t.dtype != dtype or t.shape != shape or not t.is_contiguous()):
+            raise DashError(f"expected a contiguous {dtype} tensor of shape {tuple(shape)}")
+    d = cache.k.device
+    for t in (cache.table, cache.lens, row_start, *(x[0] for x in rows), *(x[0] for x in extra)):
+        if t is not None and t.device != d:
+            raise DashError("the tensors of a call lie on one device")
+    if d.index is not None and _device is not None and torch.cuda.is_initialized() and d.index != _device():
+        raise DashError(f"the cache lies on {d}, which is not the current device")
+    return p
+
+
+def paged_workspace_bytes(p: dash_paged_params, evict: bool = False) -> int:
+    n = ctypes.c_size_t(0)
+    name = "dash_paged_evict_workspace_bytes" if evict else "dash_paged_workspace_bytes"
+    _check(getattr(load_library(), name)(ctypes.byref(p), ctypes.byref(n)), name)
+    return n.value
+
+
+def alloc_paged_workspace(p: dash_paged_params, device, evict: bool = False) -> torch.Tensor:
+    """Scratch of dash_paged_attend and dash_paged_weigh, or with evict=True of dash_paged_evict."""
+    return torch.empty(paged_workspace_bytes(p, evict) + 256, dtype=torch.uint8, device=device)
+
+
+def dash_paged_append(p: dash_paged_params, cache: PagedCache, k_new, v_new, row_start) -> None:
+    """k_new, v_new [n_rows, h_kv, d]; cache.weights, pos and seen as far as they are there."""
+    tok = cache.k.shape[:3]
+    p = _paged_call(p, cache, row_start, ((k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride")),
+                ((cache.weights, torch.float32, tok), (cache.pos, torch.int32, tok), (cache.seen, torch.int32, cache.lens.shape)))
+    _check(load_library().dash_paged_append(p, _ptr(k_new), _ptr(v_new), _ptr(cache.k), _ptr(cache.v), _ptr(row_start), _ptr(cache.lens),
+                                            _ptr(cache.table), _ptr(cache.weights), _ptr(cache.pos), _ptr(cache.seen), _stream()),
+           "dash_paged_append")
+
+
+def dash_paged_attend(p: dash_paged_params, cache: PagedCache, q, row_start, o, ws: torch.Tensor, lse=None) -> None:
+    """q, o [n_rows, h_q, d]; lse fp32 [n_rows, h_q] or None."""
+    p = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"), (o, p.h_q, "o_stride")), ((lse, torch.float32, (p.n_rows, p.h_q)),))
+    wp, wn = _ws_ptr(ws)
+    _check(load_library().dash_paged_attend(p, _ptr(q), _ptr(cache.k), _ptr(cache.v), _ptr(row_start), _ptr(cache.lens), _ptr(cache.table),
+                                            _ptr(o), _ptr(lse), wp, wn, _stream()), "dash_paged_attend")
+
+
+def dash_paged_weigh(p: dash_paged_params, cache: PagedCache, q, row_start, lse, ws: torch.Tensor, last: int = 0) -> None:
+    """Adds to cache.weights; lse as dash_paged_attend wrote it."""
+    if cache.weights is None or lse is None:
+        raise DashError("dash_paged_weigh needs the cache's weights and the rows' lse")
+    p = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"),),
+                ((lse, torch.float32, (p.n_rows, p.h_q)), (cache.weights, torch.float32, cache.k.shape[:3])))
+    wp, wn = _ws_ptr(ws)
+    _check(load_library().dash_paged_weigh(p, _ptr(q), _ptr(cache.k), _ptr(row_start), _ptr(cache.lens), _ptr(cache.table), _ptr(lse), last,
+                                           _ptr(cache.weights), wp, wn, _stream()), "dash_paged_weigh")
+
+
+def dash_paged_evict(p: dash_paged_params, cache: PagedCache, budget: int, ws: torch.Tensor, sinks: int = 0, recent: int = 0, src=None) -> None:
+    """ws from alloc_paged_workspace(p, device, evict=True); src int32 [batch, h_kv, budget] or None."""
+    if cache.weights is None or cache.pos is None or cache.seen is None:
+        raise DashError("dash_paged_evict needs the cache's weights, pos and seen")
+    tok = cache.k.shape[:3]
+    p = _paged_call(p, cache, None, (), ((cache.weights, torch.float32, tok), (cache.pos, torch.int32, tok),
+                                     (cache.seen, torch.int32, cache.lens.shape), (src, torch.int32, (p.batch, p.h_kv, budget))))
+    wp, wn = _ws_ptr(ws)
+    _check(load_library().dash_paged_evict(p, _ptr(cache.k), _ptr(cache.v), _ptr(cache.lens), _ptr(cache.seen), _ptr(cache.table),
+                                           _ptr(cache.weights), _ptr(cache.pos), budget, sinks, recent, _ptr(src), wp, wn, _stream()),
+           "dash_paged_evict")
