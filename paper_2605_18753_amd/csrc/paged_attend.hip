@@ -7,6 +7,8 @@
 // its own in LDS (two tiles deep, global -> LDS copies), without a barrier until the four add up at the end.
 #include <math.h>
 
+#include <type_traits>
+
 #include "f32_tiles.h"
 #include "lds_copy.h"
 #include "paged.h"
@@ -25,6 +27,21 @@ template <int D> __device__ __forceinline__ int pv_swz(int row) { return D == 12
 __device__ __forceinline__ int paged_last_key(const PagedArgs& a, const PagedItem& it, int t) {
   return a.causal ? min(it.n - it.m + t, it.n - 1) : it.n - 1;
 }
+
+// tiles of ROWS rows of a sequence; cost: steps of 128 keys (16 rows), or of 64
+template <int ROWS> __device__ __forceinline__ int2 tile_shape(const PagedArgs& a, int m, int n) {
+  const int T = ROWS / a.g;
+  return make_int2((m + T - 1) / T, max(ROWS == 16 ? (n + 127) >> 7 : (n + 63) >> 6, 1));
+}
+
+// 4 values of an output row
+__device__ __forceinline__ void put_row4(uint16_t* p, f32x4 o, float inv) {
+  uint2 y;
+  y.x = cvt_bf16x2(o[0] * inv, o[1] * inv);
+  y.y = cvt_bf16x2(o[2] * inv, o[3] * inv);
+  *reinterpret_cast<uint2*>(p) = y;
+}
+__device__ __forceinline__ void put_row4(float* p, f32x4 o, float inv) { *reinterpret_cast<f32x4*>(p) = o * inv; }
 
 template <int D> struct FewCfg {
   static constexpr int NCH = D / 8, ROW_BYTES = D * 2;
@@ -75,24 +92,11 @@ __device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const Paged
   const float inv = den > 0.f ? 1.f / den : den == 0.f ? 0.f : den;     // NaN stays
   T* op = (T*)a.o + (it.r0 + t) * a.o_t + head * a.o_h;
 #pragma unroll
-  for (int j = 0; j < D / 64; j++) {
-    if constexpr (sizeof(T) == 2) {
-      uint2 y;
-      y.x = cvt_bf16x2(o[j * 4] * inv, o[j * 4 + 1] * inv);
-      y.y = cvt_bf16x2(o[j * 4 + 2] * inv, o[j * 4 + 3] * inv);
-      *reinterpret_cast<uint2*>(op + j * 64 + c * 4) = y;
-    } else {
-      *reinterpret_cast<f32x4*>(op + j * 64 + c * 4) = f32x4{o[j * 4] * inv, o[j * 4 + 1] * inv, o[j * 4 + 2] * inv, o[j * 4 + 3] * inv};
-    }
-  }
+  for (int j = 0; j < D / 64; j++)
+    put_row4(op + j * 64 + c * 4, f32x4{o[j * 4], o[j * 4 + 1], o[j * 4 + 2], o[j * 4 + 3]}, inv);
   if (a.lse && c == 0) a.lse[(int64_t)(it.r0 + t) * a.h_q + head] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
 }
 
-// tiles of 16 rows of a sequence; cost: its 128-key steps
-__device__ __forceinline__ int2 few_shape(const PagedArgs& a, int m, int n) {
-  const int T = 16 / a.g;
-  return make_int2((m + T - 1) / T, max((n + 127) >> 7, 1));
-}
 
 template <int D>
 __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void paged_few_kernel(PagedArgs a) {
@@ -101,7 +105,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void paged_few_kernel(PagedA
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x % a.h_kv;
   PagedItem it;
-  if (!paged_find(a, blockIdx.x / a.h_kv, [&](int m, int n) { return few_shape(a, m, n); }, it)) return;
+  if (!paged_find(a, blockIdx.x / a.h_kv, [&](int m, int n) { return tile_shape<16>(a, m, n); }, it)) return;
   const int T = 16 / a.g, t0 = it.tile * T;
   const int n = lane & 15, kq = lane >> 4;
   const int t = t0 + n / a.g;
@@ -253,7 +257,7 @@ __global__ __launch_bounds__(256) void paged_few_f32_kernel(PagedArgs a) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x % a.h_kv;
   PagedItem it;
-  if (!paged_find(a, blockIdx.x / a.h_kv, [&](int m, int n) { return few_shape(a, m, n); }, it)) return;
+  if (!paged_find(a, blockIdx.x / a.h_kv, [&](int m, int n) { return tile_shape<16>(a, m, n); }, it)) return;
   const int T = 16 / a.g, t0 = it.tile * T;
   const int n = lane & 15, kq = lane >> 4;
   const int t = t0 + n / a.g;
@@ -319,19 +323,297 @@ __global__ __launch_bounds__(256) void paged_few_f32_kernel(PagedArgs a) {
   paged_few_finish<float, D>(a, it, r, t0, x, ml);
 }
 
-// Adds the parts of cut items: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  Eight packed (token, head) rows a workgroup,
-// 32 threads each.
-template <typename T, int D>
+// Many rows (pieces of prompts): a tile is 128 (token, head) rows, 32 of them a wave's: all heads of the group for 32 / g tokens.
+// 64-key tiles of K and V are copied from their pages straight into LDS, two stages deep, and shared by the four waves.
+// The first product is S^T[key, row] = K Q^T (A = K from LDS, B = Q in registers), the second O^T[d, row] += V^T P^T (A = V^T by
+// transposing reads, B = P): in the 32x32 accumulator layout lane (n = lane % 32, h = lane / 32) holds, for row n, keys 8 q + 4 h + i,
+// which are its slots of operand B once the contraction runs in that order, so nothing moves between the products.
+// A wave pipelines its tiles: the first product of tile i runs with the exponentials of tile i - 1, the second product of
+// tile i - 1 with the row maxima of tile i.
+template <int D> struct RowsCfg {
+  static constexpr int NCH = D / 8, ROW_BYTES = D * 2;
+  static constexpr int TILE_BYTES = 64 * ROW_BYTES;
+  static constexpr int COPIES = TILE_BYTES / 4096;       // copy instructions of a wave per tile and tensor
+  static constexpr int RPC = 256 / NCH, RPW = RPC / 4;   // rows that the workgroup's, and a wave's, copy instruction covers
+  static constexpr int LDS_BYTES = 4 * TILE_BYTES;       // K ring [2], V ring [2]
+};
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
+  using C = RowsCfg<D>;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, h = lane >> 5;
+  // kv-heads are the fast index: with 8 of them each XCD's L2 sees the pages of one
+  const int r = blockIdx.x % a.h_kv;
+  PagedItem it;
+  if (!paged_find(a, blockIdx.x / a.h_kv, [&](int m, int n) { return tile_shape<128>(a, m, n); }, it)) return;
+  const int T = 128 / a.g, t0 = it.tile * T, Tw = 32 / a.g, tw0 = t0 + wave * Tw;
+  const int t = tw0 + n / a.g, head = r * a.g + n % a.g;
+  const bool row_ok = t < it.m;
+  bf16x8 qf[D / 16];
+  {
+    const uint16_t* qp = (const uint16_t*)a.q + (it.r0 + min(t, it.m - 1)) * a.q_t + head * a.q_h + h * 8;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ks++) qf[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16);
+  }
+  const int last = paged_last_key(a, it, min(t, it.m - 1));
+  // keys that the tile, and the wave, sees; up to where the wave's first token does
+  const int end = max(paged_last_key(a, it, min(t0 + T, it.m) - 1) + 1, 0);
+  const int wave_end = tw0 < it.m ? paged_last_key(a, it, min(tw0 + Tw, it.m) - 1) + 1 : 0;
+  const int low = paged_last_key(a, it, min(tw0, it.m - 1));
+  const int kt = (end + 63) >> 6, per = (kt + it.parts - 1) / it.parts;
+  const int first = min(it.part * per, kt), n_it = min(per, kt - first);       // the part's tiles
+
+  // ---- pages: 64 entries of the table a lane each, the next 64 behind them ----------------------------------
+  const int32_t* table = a.table + (int64_t)it.b * a.max_pages;
+  auto window = [&](int i) { return paged_clamp(a, table[min(i + lane, a.max_pages - 1)]); };
+  int wbase = (first * 64) >> a.page_log;
+  int win = window(wbase), win_next = window(wbase + 64);
+
+  // ---- global -> LDS copies -----------------------------------------------------------------------------------
+  const uint32_t kt2 = (uint32_t)a.kp_t * 2u, vt2 = (uint32_t)a.vp_t * 2u;
+  const char* kb = (const char*)a.k + r * a.kp_h * 2;
+  const char* vb = (const char*)a.v + r * a.vp_h * 2;
+  const int64_t kp2 = a.kp_p * 2, vp2 = a.vp_p * 2;
+  const int pm = (1 << a.page_log) - 1;
+  const uint32_t lds0 = lds_addr_of(lds);
+  const int c_x = lane / C::NCH, c_pos = lane % C::NCH, c_row = wave * C::RPW + c_x;
+  const uint32_t k_off = (uint32_t)c_x * kt2 + (uint32_t)((c_pos ^ pk_swz<D>(c_row)) << 4);
+  const uint32_t v_off = (uint32_t)c_x * vt2 + (uint32_t)((c_pos ^ pv_swz<D>(c_row)) << 4);
+  // Rows [key, key + RPW) of page id: a resource of their own, which ends with the sequence's last token (rows behind it read as zeros,
+  // whatever the page holds)
+  auto copy = [&](const char* base, int64_t page_bytes, uint32_t row_bytes, uint32_t off, int id, int key, int stop, uint32_t to) {
+    const int left = min(max(stop - key, 0), C::RPW);
+    const char* p = base + (int64_t)id * page_bytes + (uint32_t)(key & pm) * row_bytes;
+    copy16_to_lds(make_rsrc(p, left ? (int64_t)(left - 1) * row_bytes + C::ROW_BYTES : 0), to, off, 0);
+  };
+  int id_v[C::COPIES], id_k[C::COPIES];                       // pages of tile i (its V is copied) and of tile i + 1 (its K)
+  auto ids_of = [&](int tile, int (&id)[C::COPIES]) {
+#pragma unroll
+    for (int c = 0; c < C::COPIES; c++)
+      id[c] = __builtin_amdgcn_readlane(win, (((tile * 64 + c * C::RPC + wave * C::RPW) >> a.page_log) - wbase) & 63);
+  };
+  auto copy_k = [&](int tile, int c, int slot) {              // behind the part's last tile: nothing is read
+    const int stop = tile < first + n_it ? it.n : 0;
+    copy(kb, kp2, kt2, k_off, id_k[c], tile * 64 + c * C::RPC + wave * C::RPW, stop, lds0 + slot * C::TILE_BYTES + c * 4096 + wave * 1024);
+  };
+  auto copy_v = [&](int tile, int c, int slot) {
+    copy(vb, vp2, vt2, v_off, id_v[c], tile * 64 + c * C::RPC + wave * C::RPW, it.n, lds0 + (2 + slot) * C::TILE_BYTES + c * 4096 + wave * 1024);
+  };
+  // ---- operand addresses in LDS, of slot 0 --------------------------------------------------------------------
+  uint32_t k_rd[D / 16], v_rd[D / 32];
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ks++) k_rd[ks] = lds0 + (uint32_t)(n * C::ROW_BYTES + (((2 * ks + h) ^ pk_swz<D>(n)) << 4));
+  const int s16 = lane & 15, a16 = (lane >> 4) & 1;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; dt++)
+    v_rd[dt] = lds0 + (uint32_t)((4 * h + (s16 >> 2)) * C::ROW_BYTES +
+                                 ((((4 * dt) ^ pv_swz<D>(s16 >> 2)) + 2 * a16 + ((s16 & 3) >> 1)) << 4) + ((s16 & 1) << 3));
+
+  float m_run = -INFINITY, l_run = 0.f;
+  constexpr int NDT = D / 32;
+  f32x16 oacc[NDT];
+#pragma unroll
+  for (int dt = 0; dt < NDT; dt++)
+#pragma unroll
+    for (int j = 0; j < 16; j++) oacc[dt][j] = 0.f;
+  // all loads so far are complete, and known to be, before the copies are in flight
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ks++) asm volatile("" : "+v"(qf[ks]));
+  asm volatile("" : "+v"(win), "+v"(win_next));
+  ids_of(first, id_k);
+  if (n_it > 0) {
+#pragma unroll
+    for (int c = 0; c < C::COPIES; c++) copy_k(first, c, 0);
+  }
+  // Iteration i, LDS: tile i lives in slot i & 1 of both rings, V one iteration behind K.  At its top a wave waits for its own
+  // copies (K of tile i, V of tile i - 1); the barrier makes everybody's visible and retires the reads of iteration i - 1, whose slots this
+  // iteration's copies (K of tile i + 1, V of tile i) overwrite, one at a time between the MFMAs.
+  int pend = 0;
+  float tmax_old = 0.f;
+  auto iteration = [&](auto p_tag, int i, f32x16 (&s)[2], f32x16 (&so)[2]) __attribute__((always_inline)) {
+    constexpr int P = decltype(p_tag)::value;
+    constexpr int NS = D / 8, KAHEAD = 4, VAHEAD = 2, EQ = 12, E0 = 2;
+    const bool cur = i < n_it;
+    const int tile = first + i;
+    const bool on = cur && tile * 64 < wave_end;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    asm volatile("" : "+v"(win_next));                         // asked for iterations ago
+#pragma unroll
+    for (int c = 0; c < C::COPIES; c++) id_v[c] = id_k[c];
+    if (((tile + 1) * 64 >> a.page_log) - wbase >= 64) {
+      wbase += 64;
+      win = win_next;
+      win_next = window(wbase + 64);
+    }
+    ids_of(tile + 1, id_k);
+    if (pend && __builtin_expect(__any(tmax_old > m_run + kPagedLazy), 0)) {
+      const float m_new = fmaxf(m_run, fmaxf(tmax_old, __shfl_xor(tmax_old, 32)));
+      const float use = m_new == -INFINITY ? 0.f : m_new;
+      const float corr = __builtin_amdgcn_exp2f(m_run - use);
+      m_run = m_new;
+      l_run *= corr;
+#pragma unroll
+      for (int dt = 0; dt < NDT; dt++)
+#pragma unroll
+        for (int j = 0; j < 16; j++) oacc[dt][j] *= corr;
+    }
+    const float off = m_run == -INFINITY ? 0.f : -m_run;
+    asm volatile("s_barrier" ::: "memory");
+    auto k_read = [&](int x) -> bf16x8 {   // slot x: d slice x / 2, key half x % 2
+      return lds_read_b128(k_rd[x >> 1] + (uint32_t)(P * C::TILE_BYTES + (x & 1) * 32 * C::ROW_BYTES));
+    };
+    auto v_read = [&](int x) -> bf16x8 {   // slot x: contraction step x / NDT, d-tile x % NDT
+      const uint32_t at = v_rd[x % NDT] + (uint32_t)((2 + (P ^ 1)) * C::TILE_BYTES + 16 * (x / NDT) * C::ROW_BYTES);
+      return lds_read_tr_pair(at, at + 8 * C::ROW_BYTES);
+    };
+    u32x4 pb[4];
+    float l_tile = 0.f;
+    // Pair k of tile i - 1: P^T slots 2 (k % 4), + 1 of contraction step k / 4.  P in bf16, the matrix cores' operand type; the row sum takes the
+    // unrounded values.
+    auto e_pair = [&](int k) {
+      const int g = k >> 2, x = g >> 1, j = 8 * (g & 1) + 2 * (k & 3);
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(so[x][j], a.c1, off));
+      const float p1 = __builtin_amdgcn_exp2f(fmaf(so[x][j + 1], a.c1, off));
+      l_tile += p0 + p1;
+      uint32_t w = cvt_bf16x2(p0, p1);
+      asm volatile("" : "+v"(l_tile), "+v"(w));
+      pb[g][k & 3] = w;
+    };
+    auto copies = [&](int c) {
+      if (c < C::COPIES) copy_k(tile + 1, c, P ^ 1);
+      else if (c < 2 * C::COPIES) copy_v(tile, c - C::COPIES, P);
+    };
+    bf16x8 vf[NS];
+    auto first_product = [&](auto e_tag) {
+      constexpr bool EXPS = decltype(e_tag)::value;
+      bf16x8 kf[NS];
+#pragma unroll
+      for (int x = 0; x < KAHEAD; x++) kf[x] = k_read(x);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (EXPS) {
+#pragma unroll
+        for (int k = 0; k < E0; k++) e_pair(k);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int x = 0; x < NS; x++) {
+        if (x + KAHEAD < NS) kf[x + KAHEAD] = k_read(x + KAHEAD);
+        if ((x & 1) == 0) copies(x >> 1);
+        const f32x16 z = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        s[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x], qf[x >> 1], x < 2 ? z : s[x & 1], 0, 0, 0);
+        if constexpr (EXPS) {
+#pragma unroll
+          for (int k = E0 + x * (EQ - E0) / NS; k < E0 + (x + 1) * (EQ - E0) / NS; k++) e_pair(k);
+          if (x >= NS - VAHEAD) vf[x - (NS - VAHEAD)] = v_read(x - (NS - VAHEAD));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    auto mask_keys = [&]() {
+      if (__builtin_expect(tile * 64 + 63 > low, 0)) {
+        int lim = last - (tile * 64 + 4 * h);
+        asm volatile("" : "+v"(lim));
+#pragma unroll
+        for (int x = 0; x < 2; x++)
+#pragma unroll
+          for (int j = 0; j < 16; j++) s[x][j] = x * 32 + (j >> 2) * 8 + (j & 3) > lim ? -INFINITY : s[x][j];
+      }
+    };
+    float mloc = -INFINITY;
+    auto max_quad = [&](int q) {
+      const int x = q >> 2, j = 4 * (q & 3);
+      mloc = fmaxf(fmaxf(mloc, s[x][j]), s[x][j + 1]);
+      mloc = fmaxf(fmaxf(mloc, s[x][j + 2]), s[x][j + 3]);
+    };
+    auto second_product = [&]() {
+#pragma unroll
+      for (int x = 0; x < NS; x++) {
+        if (x + VAHEAD < NS) vf[x + VAHEAD] = v_read(x + VAHEAD);
+        oacc[x % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x], __builtin_bit_cast(bf16x8, pb[x / NDT]), oacc[x % NDT], 0, 0, 0);
+        if (EQ + x < 16) e_pair(EQ + x);
+        if constexpr (NS == 16) { if (x >= 4 && x < 12) max_quad(x - 4); }
+        else if (x >= 4) { max_quad(2 * (x - 4)); max_quad(2 * (x - 4) + 1); }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      l_run += l_tile;
+    };
+    if (on) {
+      if (pend) first_product(std::true_type{});
+      else first_product(std::false_type{});
+      mask_keys();
+    } else {
+      asm volatile("" : "=v"(s[0]), "=v"(s[1]));               // nobody reads them
+      if (cur) {
+#pragma unroll
+        for (int c = 0; c < 2 * C::COPIES; c++) copies(c);
+      }
+      if (pend) {
+#pragma unroll
+        for (int x = 0; x < VAHEAD; x++) vf[x] = v_read(x);
+#pragma unroll
+        for (int k = 0; k < EQ; k++) e_pair(k);
+      }
+    }
+    if (pend) {
+      __builtin_amdgcn_sched_barrier(0);
+      second_product();
+    }
+    if (!pend && on) {
+#pragma unroll
+      for (int q = 0; q < 8; q++) max_quad(q);
+    }
+    tmax_old = mloc * a.c1;                                    // this lane half's; a.c1 > 0
+    pend = on;
+  };
+  if (n_it > 0) {
+    f32x16 sa[2], sb[2];
+    for (int i = 0;;) {
+      iteration(std::integral_constant<int, 0>{}, i, sa, sb);
+      if (++i > n_it) break;
+      iteration(std::integral_constant<int, 1>{}, i, sb, sa);
+      if (++i > n_it) break;
+    }
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // no copy outlives the workgroup's LDS
+  const float l_tot = l_run + __shfl_xor(l_run, 32);
+  if (!row_ok) return;
+  if (it.parts > 1) {
+    // record: O^T unnormalised as [d / 4][row][4], maximum and sum per row
+    const int64_t rec = (int64_t)r * a.part_stride + it.rec0 + it.part;
+    const int row = wave * 32 + n;
+    f32x4* po = reinterpret_cast<f32x4*>(a.part_o) + rec * (D / 4) * 128 + row;
+#pragma unroll
+    for (int dt = 0; dt < NDT; dt++)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; q4++)
+        po[(dt * 8 + q4 * 2 + h) * 128] = f32x4{oacc[dt][q4 * 4], oacc[dt][q4 * 4 + 1], oacc[dt][q4 * 4 + 2], oacc[dt][q4 * 4 + 3]};
+    if (h == 0) reinterpret_cast<float2*>(a.part_ml)[rec * 128 + row] = make_float2(m_run, l_tot);
+    return;
+  }
+  const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot == 0.f ? 0.f : l_tot;
+  uint16_t* op = (uint16_t*)a.o + (it.r0 + t) * a.o_t + head * a.o_h + h * 4;
+#pragma unroll
+  for (int dt = 0; dt < NDT; dt++)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; q4++)
+      put_row4(op + dt * 32 + q4 * 8, f32x4{oacc[dt][q4 * 4], oacc[dt][q4 * 4 + 1], oacc[dt][q4 * 4 + 2], oacc[dt][q4 * 4 + 3]}, inv);
+  if (a.lse && h == 0) a.lse[(int64_t)(it.r0 + t) * a.h_q + head] = l_tot == 0.f ? -INFINITY : (m_run + log2f(l_tot)) * kLn2;
+}
+
+// Adds the parts of cut items: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  D / 4 threads a (token, head) row.  ROWS: of a
+// tile (16 or 128), whose records are laid out accordingly.
+template <typename T, int D, int ROWS>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int heads = a.h_q;
-  const int64_t gr0 = (int64_t)blockIdx.x * 8;
-  const int sub = threadIdx.x >> 5, c = threadIdx.x & 31;
-  // the rows of a workgroup may belong to several sequences: each half wave finds its own
-  const int64_t gr = gr0 + sub;
-  const int row = (int)min(gr / heads, (int64_t)a.n_rows - 1), head = (int)(gr % heads);
+  constexpr int TPR = D / 4, RPW = 64 / TPR;               // threads of a row, rows of a wave
+  const int lane = threadIdx.x & 63, c = lane % TPR;
+  // rows in the order kv-head, token, head of the group: neighbours lie side by side in the records
+  const int64_t per = (int64_t)a.n_rows * a.g;
+  const int64_t gr = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * RPW + lane / TPR;
+  const int r = (int)min(gr / per, (int64_t)a.h_kv - 1), row = (int)(gr % per) / a.g, hg = (int)(gr % per) % a.g;
   // the dealing of the launch before, for a given row
-  const auto shape = [&](int m, int n) { return few_shape(a, m, n); };
+  const auto shape = [&](int m, int n) { return tile_shape<ROWS>(a, m, n); };
   const int S = paged_part_size(a, shape);
   int first = 0, parts = 0, tiles = 0, r0 = 0, base = 0;
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
@@ -342,90 +624,99 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
     }
     const int np = (s.y + S - 1) / S, incl = wave_scan(s.x * np);
 #pragma unroll
-    for (int half = 0; half < 2; half++) {
-      const int want = __builtin_amdgcn_readlane(row, half * 32);
+    for (int k = 0; k < RPW; k++) {
+      const int want = __builtin_amdgcn_readlane(row, k * TPR);
       const uint64_t hit = __ballot(want >= rm.x && want < rm.x + rm.y);
       if (hit) {
         const int l = __builtin_ctzll(hit);
         const int np_l = __builtin_amdgcn_readlane(np, l), tiles_l = __builtin_amdgcn_readlane(s.x, l);
         const int first_l = base + __builtin_amdgcn_readlane(incl, l) - tiles_l * np_l, r0_l = __builtin_amdgcn_readlane(rm.x, l);
-        if ((lane >> 5) == half) { parts = np_l; tiles = tiles_l; first = first_l; r0 = r0_l; }
+        if (lane / TPR == k) { parts = np_l; tiles = tiles_l; first = first_l; r0 = r0_l; }
       }
     }
     base += __builtin_amdgcn_readlane(incl, 63);
   }
-  if (parts <= 1 || gr >= (int64_t)a.n_rows * heads) return;
-  const int Tt = 16 / a.g, t = row - r0, tile = t / Tt, in = (t % Tt) * a.g + head % a.g;
-  const int64_t rec = (int64_t)(head / a.g) * a.part_stride + first + (tiles - 1 - tile) * parts;
-  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + rec * 16 + in;
+  if (parts <= 1 || gr >= per * a.h_kv) return;
+  const int Tt = ROWS / a.g, t = row - r0, tile = t / Tt, in = (t % Tt) * a.g + hg;
+  const int64_t rec = (int64_t)r * a.part_stride + first + (tiles - 1 - tile) * parts;
+  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + rec * ROWS + in;
   float M = -INFINITY, den = 0.f;
-  for (int p = 0; p < parts; p++) M = fmaxf(M, ml[p * 16].x);
+#pragma unroll 8
+  for (int p = 0; p < parts; p++) M = fmaxf(M, ml[p * ROWS].x);
   const float use = M == -INFINITY ? 0.f : M;
-  constexpr int V = D / 32;
-  float o[V];
-#pragma unroll
-  for (int i = 0; i < V; i++) o[i] = 0.f;
-  const float* po = a.part_o + (rec * 16 + in) * D + c * V;
-#pragma unroll 4
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o) + (ROWS == 16 ? (rec * ROWS + in) * (D / 4) + c : (rec * (D / 4) + c) * ROWS + in);
+#pragma unroll 8
   for (int p = 0; p < parts; p++) {
-    const float2 y = ml[p * 16];
+    const float2 y = ml[p * ROWS];
     const float w = __builtin_amdgcn_exp2f(y.x - use);
+    const f32x4 x = po[(int64_t)p * ROWS * (D / 4)];
     den = fmaf(w, y.y, den);
 #pragma unroll
-    for (int i = 0; i < V; i++) o[i] = fmaf(w, po[(int64_t)p * 16 * D + i], o[i]);
+    for (int e = 0; e < 4; e++) o[e] = fmaf(w, x[e], o[e]);
   }
   const float inv = den > 0.f ? 1.f / den : den == 0.f ? 0.f : den;
-  T* op = (T*)a.o + row * a.o_t + head * a.o_h + c * V;
-#pragma unroll
-  for (int i = 0; i < V; i += 2) {
-    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(op + i) = cvt_bf16x2(o[i] * inv, o[i + 1] * inv);
-    else { op[i] = o[i] * inv; op[i + 1] = o[i + 1] * inv; }
-  }
-  if (a.lse && c == 0) a.lse[(int64_t)row * heads + head] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
+  const int head = r * a.g + hg;
+  put_row4((T*)a.o + row * a.o_t + head * a.o_h + c * 4, o, inv);
+  if (a.lse && c == 0) a.lse[(int64_t)row * a.h_q + head] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
-static int few_items(const PagedArgs& a) {   // most items of a kv-head
-  const int T = 16 / a.g;
-  const int64_t n = (int64_t)a.n_rows / T + min(a.batch, a.n_rows);
-  return (int)(n < a.n_rows ? n : a.n_rows);
+// The kernel for a call: tiles of 128 rows where the sequences bring more than 16 rows each on the average, tiles of 16 otherwise.
+static bool use_rows(const PagedArgs& a, int dtype) { return dtype == DASH_BF16 && (int64_t)a.n_rows * a.g > (int64_t)a.batch * 16; }
+static int64_t most_items(const PagedArgs& a, int rows) {   // of a kv-head
+  const int T = rows / a.g;
+  return min((int64_t)a.n_rows / T + min(a.batch, a.n_rows), (int64_t)a.n_rows);
 }
+// workgroups that are resident at once, for a kv-head: what items are cut for
 static int few_target(const PagedArgs& a) { return max(256 / a.h_kv, 1); }
-static int few_wgs(const PagedArgs& a) { return few_items(a) < few_target(a) ? few_target(a) : 0; }
+static int rows_target(const PagedArgs& a) { return max(512 / a.h_kv, 1); }
 static size_t ws_align(size_t x) { return (x + 255) & ~(size_t)255; }
 
 size_t paged_attend_ws(const PagedArgs& a, int dtype, int d) {
-  const size_t recs = (size_t)few_target(a) * a.h_kv * 16;
+  const size_t few = (size_t)few_target(a) * a.h_kv * 16, rows = dtype == DASH_BF16 ? (size_t)rows_target(a) * a.h_kv * 128 : 0;
+  const size_t recs = few > rows ? few : rows;              // rows of records
   return ws_align(recs * 8) + recs * d * 4;
 }
 
+template <typename T, int D, int ROWS>
+static hipError_t launch_merge(const PagedArgs& a, hipStream_t st) {
+  const int64_t rows = (int64_t)a.n_rows * a.h_q;
+  constexpr int per = 256 / (D / 4);
+  hipLaunchKernelGGL((paged_merge_kernel<T, D, ROWS>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
 template <int D>
-static hipError_t launch_few(PagedArgs a, int dtype, char* ws, hipStream_t st) {
-  using C = FewCfg<D>;
-  a.wgs = few_wgs(a);
-  a.min_part = 1;
+static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st) {
+  const bool big = use_rows(a, dtype);
+  const int rows = big ? 128 : 16, target = big ? rows_target(a) : few_target(a);
+  const int64_t items = most_items(a, rows);
+  a.wgs = items < target ? target : 0;
+  a.min_part = big ? 4 : 1;
   a.part_stride = a.wgs;
-  const size_t recs = (size_t)a.wgs * a.h_kv * 16;
   a.part_ml = (float*)ws;
-  a.part_o = (float*)(ws + ws_align(recs * 8));
-  const dim3 grid((unsigned)(max(a.wgs, few_items(a)) * a.h_kv)), blk(256);
-  if (dtype == DASH_BF16) {
+  a.part_o = (float*)(ws + ws_align((size_t)a.wgs * a.h_kv * rows * 8));
+  const dim3 grid((unsigned)((a.wgs ? a.wgs : items) * a.h_kv)), blk(256);
+  if (big) {
     static LdsOptIn opt_in;
-    if (hipError_t e = allow_dyn_lds((const void*)paged_few_kernel<D>, C::LDS_BYTES, opt_in); e != hipSuccess) return e;
-    hipLaunchKernelGGL(paged_few_kernel<D>, grid, blk, C::LDS_BYTES, st, a);
+    if (hipError_t e = allow_dyn_lds((const void*)paged_rows_kernel<D>, RowsCfg<D>::LDS_BYTES, opt_in); e != hipSuccess) return e;
+    hipLaunchKernelGGL(paged_rows_kernel<D>, grid, blk, RowsCfg<D>::LDS_BYTES, st, a);
+  } else if (dtype == DASH_BF16) {
+    static LdsOptIn opt_in;
+    if (hipError_t e = allow_dyn_lds((const void*)paged_few_kernel<D>, FewCfg<D>::LDS_BYTES, opt_in); e != hipSuccess) return e;
+    hipLaunchKernelGGL(paged_few_kernel<D>, grid, blk, FewCfg<D>::LDS_BYTES, st, a);
   } else {
     hipLaunchKernelGGL(paged_few_f32_kernel<D>, grid, blk, 0, st, a);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.wgs == 0) return e;
-  const dim3 mgrid((unsigned)(((int64_t)a.n_rows * a.h_q + 7) / 8));
-  if (dtype == DASH_BF16) hipLaunchKernelGGL((paged_merge_kernel<uint16_t, D>), mgrid, blk, 0, st, a);
-  else hipLaunchKernelGGL((paged_merge_kernel<float, D>), mgrid, blk, 0, st, a);
-  return hipGetLastError();
+  if (dtype == DASH_F32) return launch_merge<float, D, 16>(a, st);
+  return big ? launch_merge<uint16_t, D, 128>(a, st) : launch_merge<uint16_t, D, 16>(a, st);
 }
 
 hipError_t launch_paged_attend(const PagedArgs& a, int dtype, int d, char* ws, hipStream_t st) {
-  return d == 128 ? launch_few<128>(a, dtype, ws, st) : launch_few<64>(a, dtype, ws, st);
+  return d == 128 ? launch_attend<128>(a, dtype, ws, st) : launch_attend<64>(a, dtype, ws, st);
 }
 
 }  // namespace dash
