@@ -70,25 +70,33 @@ __device__ __forceinline__ uint32_t evict_key(float w, int pos, int sinks, int f
 }
 
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
+constexpr int kSelRows = 32;                               // keys a thread holds in registers at most: sequences of up to 32768 tokens
+constexpr int kBins = 2048;                                // 11, 11 and 10 bits of a key
 
-// sum of a value over the workgroup, to all of it (two barriers)
-__device__ __forceinline__ int wg_sum(int v, int* xch) {
-  const int s = __builtin_amdgcn_readlane(wave_scan(v), 63);
+// sum of `v`, the same in a wave's lanes, over the waves before one's own, and over all
+__device__ __forceinline__ int2 waves_before(int v, int wave, int* xch) {
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) xch[threadIdx.x >> 6] = s;
+  if ((threadIdx.x & 63) == 0) xch[wave] = v;
   __syncthreads();
-  int t = 0;
+  int2 s = make_int2(0, 0);
 #pragma unroll
-  for (int i = 0; i < kSelWaves; i++) t += xch[i];
-  return t;
+  for (int w = 0; w < kSelWaves; w++) {
+    const int c = xch[w];
+    s.x += w < wave ? c : 0;
+    s.y += c;
+  }
+  return s;
 }
 
+// A workgroup per pair.  Wave w owns rows of 64 slots [w rows, (w + 1) rows), so that ranks in slot order need one exchange between
+// the waves.  The keys stay in registers (sequences of more than 32768 tokens: in the scratch); the budget-th largest is found by
+// counting its 11 leading bits, of those that share them the next 11, then the last 10.
 __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e) {
   const PagedArgs& a = e.a;
-  __shared__ int hist[256];
-  __shared__ int xch[kSelWaves], xch2[kSelWaves], chosen[2];
+  __shared__ int hist[kBins];
+  __shared__ int xch[kSelWaves], chosen[2];
   const int pair = blockIdx.x, h = pair % a.h_kv, b = pair / a.h_kv;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = paged_len(a, b), left = min(n, e.budget);
   int32_t* src = e.src ? e.src + (int64_t)pair * e.budget : nullptr;
   if (src)
@@ -97,78 +105,119 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e) 
     if (tid == 0) e.counts[pair] = 0;
     return;
   }
+  const int first_recent = a.seen[b] - e.recent, pm = (1 << a.page_log) - 1;
+  const int rows = (n + kSelThreads - 1) / kSelThreads;    // of 64 slots, a wave's
+  const int slot0 = wave * rows * 64 + lane;
   uint32_t* keys = e.keys + (int64_t)pair * a.cap;
-  const int first_recent = a.seen[b] - e.recent;
-  for (int i = tid; i < n; i += kSelThreads) {
-    const int64_t at = (((int64_t)paged_page_lane(a, b, i >> a.page_log) * a.h_kv + h) << a.page_log) + (i & ((1 << a.page_log) - 1));
-    keys[i] = evict_key(a.weights[at], a.pos[at], e.sinks, first_recent);
-  }
-  // the budget-th largest key, eight bits at a time
+  auto key_of = [&](int i) -> uint32_t {
+    const int64_t at = (((int64_t)paged_page_lane(a, b, i >> a.page_log) * a.h_kv + h) << a.page_log) + (i & pm);
+    return evict_key(a.weights[at], a.pos[at], e.sinks, first_recent);
+  };
   uint32_t prefix = 0, mask = 0;
   int want = e.budget;                                     // of the keys that begin with prefix
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += kSelThreads) hist[i] = 0;
-    __syncthreads();
-    for (int i = tid; i < n; i += kSelThreads) {
-      const uint32_t k = keys[i];
-      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1);
+  // each(f): f(key, slot) for every row of the wave, all lanes; slots behind the end among them
+  auto select = [&](auto&& each) {
+    for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+    for (int step = 0; step < 3; step++) {
+      const int shift = step == 0 ? 21 : step == 1 ? 10 : 0, bits = step == 2 ? 1023 : 2047;
+      __syncthreads();
+      each([&](uint32_t k, int i) {
+        if (i < n && (k & mask) == prefix) atomicAdd(&hist[(k >> shift) & bits], 1);
+      });
+      __syncthreads();
+      const int b1 = hist[kBins - 1 - 2 * tid], b0 = hist[kBins - 2 - 2 * tid];      // this thread's two bins, from the largest
+      hist[kBins - 1 - 2 * tid] = 0;
+      hist[kBins - 2 - 2 * tid] = 0;
+      const int incl = wave_scan(b1 + b0);
+      const int before = waves_before(__builtin_amdgcn_readlane(incl, 63), wave, xch).x + incl - b1 - b0;
+      if (before < want && before + b1 >= want) { chosen[0] = kBins - 1 - 2 * tid; chosen[1] = want - before; }
+      else if (before + b1 < want && before + b1 + b0 >= want) { chosen[0] = kBins - 2 - 2 * tid; chosen[1] = want - before - b1; }
+      __syncthreads();
+      prefix |= (uint32_t)chosen[0] << shift;
+      mask |= (uint32_t)bits << shift;
+      want = chosen[1];
     }
-    __syncthreads();
-    if (wave == 0) {                                       // lane l: bins 255 - 4 l .. 252 - 4 l, from the largest
-      int c[4], own = 0;
+    // of the keys equal to the last one kept, the first `want` stay
+    const uint64_t below = (1ull << lane) - 1ull;
+    int ties = 0;
+    each([&](uint32_t k, int i) { ties += __popcll(__ballot(i < n && k == prefix)); });
+    const int2 tw = waves_before(ties, wave, xch);
+    const bool all_ties = tw.y == want;
+    int t = tw.x, holes = 0, movers = 0;
+    auto kept_of = [&](uint32_t k, int i) {
+      const bool tie = i < n && k == prefix;
+      bool kept = i < n && (k > prefix || tie);
+      if (!all_ties) {
+        const uint64_t tb = __ballot(tie);
+        if (tie && t + __popcll(tb & below) >= want) kept = false;
+        t += __popcll(tb);
+      }
+      return kept;
+    };
+    each([&](uint32_t k, int i) {
+      const bool kept = kept_of(k, i);
+      holes += __popcll(__ballot(!kept && i < left));
+      movers += __popcll(__ballot(kept && i >= left));
+    });
+    const int2 hw = waves_before(holes, wave, xch);
+    int at_hole = hw.x, at_mover = a.cap - 1 - waves_before(movers, wave, xch).x;
+    int32_t* moves = e.moves + (int64_t)pair * a.cap;
+    t = tw.x;
+    each([&](uint32_t k, int i) {
+      const bool kept = kept_of(k, i), hole = !kept && i < left, mover = kept && i >= left;
+      const uint64_t hb = __ballot(hole), mb = __ballot(mover);
+      if (hole) moves[at_hole + __popcll(hb & below)] = i;
+      if (mover) moves[at_mover - __popcll(mb & below)] = i;
+      at_hole += __popcll(hb);
+      at_mover -= __popcll(mb);
+    });
+    if (tid == 0) e.counts[pair] = hw.y;
+  };
+  if (rows <= kSelRows) {
+    uint32_t key[kSelRows];
 #pragma unroll
-      for (int j = 0; j < 4; j++) own += c[j] = hist[255 - 4 * lane - j];
-      int before = wave_scan(own) - own;
+    for (int j0 = 0; j0 < kSelRows; j0 += 16) {            // sixteen rows in flight
+      if (j0 < rows) {
+        float w[16];
+        int p[16];
 #pragma unroll
-      for (int j = 0; j < 4; j++) {
-        if (before < want && before + c[j] >= want) { chosen[0] = 255 - 4 * lane - j; chosen[1] = want - before; }
-        before += c[j];
+        for (int j = 0; j < 16; j++) {
+          const int i = min(slot0 + (j0 + j) * 64, n - 1);
+          const int64_t at = (((int64_t)paged_page_lane(a, b, i >> a.page_log) * a.h_kv + h) << a.page_log) + (i & pm);
+          w[j] = a.weights[at];
+          p[j] = a.pos[at];
+        }
+#pragma unroll
+        for (int j = 0; j < 16; j++) key[j0 + j] = evict_key(w[j], p[j], e.sinks, first_recent);
       }
     }
-    __syncthreads();
-    prefix |= (uint32_t)chosen[0] << shift;
-    mask |= 255u << shift;
-    want = chosen[1];
-  }
-  // In slot order: of the keys equal to the last one kept, the first `want` stay.
-  int32_t* moves = e.moves + (int64_t)pair * a.cap;
-  int ties = 0, holes = 0, movers = 0;                     // before this row of 1024 slots
-  for (int i0 = 0; i0 < n; i0 += kSelThreads) {
-    const int i = i0 + tid;
-    const uint32_t k = i < n ? keys[i] : 0u;
-    const bool tie = i < n && k == prefix;
-    const uint64_t tb = __ballot(tie);
-    __syncthreads();
-    if (lane == 0) xch[wave] = __popcll(tb);
-    __syncthreads();
-    int t = ties;
+    select([&](auto&& f) {
 #pragma unroll
-    for (int w = 0; w < kSelWaves; w++) { if (w < wave) t += xch[w]; ties += xch[w]; }
-    const bool kept = i < n && (k > prefix || (tie && t + __popcll(tb & ((1ull << lane) - 1ull)) < want));
-    const bool hole = !kept && i < left, mover = kept && i >= left;
-    const uint64_t hb = __ballot(hole), mb = __ballot(mover);
-    if (lane == 0) xch2[wave] = __popcll(hb) | __popcll(mb) << 16;
-    __syncthreads();
-    int hh = holes, mm = movers;
-#pragma unroll
-    for (int w = 0; w < kSelWaves; w++) {
-      const int c = xch2[w];
-      if (w < wave) { hh += c & 0xffff; mm += c >> 16; }
-      holes += c & 0xffff; movers += c >> 16;
+      for (int j = 0; j < kSelRows; j++) {
+        if (j < rows) f(key[j], slot0 + j * 64);
+      }
+    });
+  } else {
+#pragma unroll 8
+    for (int j = 0; j < rows; j++) {
+      const int i = slot0 + j * 64;
+      if (i < n) keys[i] = key_of(i);
     }
-    if (hole) moves[hh + __popcll(hb & ((1ull << lane) - 1ull))] = i;
-    if (mover) moves[a.cap - 1 - (mm + __popcll(mb & ((1ull << lane) - 1ull)))] = i;
+    select([&](auto&& f) {
+#pragma unroll 8
+      for (int j = 0; j < rows; j++) {
+        const int i = slot0 + j * 64;
+        f(i < n ? keys[i] : 0u, i);
+      }
+    });
   }
-  if (tid == 0) e.counts[pair] = holes;
 }
 
-constexpr int kMoveWgs = 4;   // workgroups of a pair
-
 template <int ES, int D>
-__global__ __launch_bounds__(256) void paged_move_kernel(EvictArgs e) {
+__global__ __launch_bounds__(256) void paged_move_kernel(EvictArgs e, int wgs) {   // wgs: workgroups of a pair
   const PagedArgs& a = e.a;
   constexpr int C = D * ES / 16, PER = 256 / (2 * C);      // 16-byte pieces of a row; moves a workgroup makes at a time
-  const int pair = blockIdx.x / kMoveWgs, part = blockIdx.x % kMoveWgs, h = pair % a.h_kv, b = pair / a.h_kv;
+  const int pair = blockIdx.x / wgs, part = blockIdx.x % wgs, h = pair % a.h_kv, b = pair / a.h_kv;
   const int n_moves = e.counts[pair];
   if (h == 0 && part == 0 && threadIdx.x == 0) e.lens[b] = min(max(e.lens[b], 0), min(a.cap, e.budget));
   const int32_t* moves = e.moves + (int64_t)pair * a.cap;
@@ -178,7 +227,7 @@ __global__ __launch_bounds__(256) void paged_move_kernel(EvictArgs e) {
   const int pm = (1 << a.page_log) - 1;
   char* base = (char*)(is_v ? a.v : a.k) + h * (is_v ? a.vp_h : a.kp_h) * ES;
   const int64_t sp = (is_v ? a.vp_p : a.kp_p) * ES, st = (is_v ? a.vp_t : a.kp_t) * ES;
-  for (int j = part * PER + sub; j < n_moves; j += kMoveWgs * PER) {
+  for (int j = part * PER + sub; j < n_moves; j += wgs * PER) {
     const int to = moves[j], from = moves[a.cap - 1 - j];
     const uint32_t pt = (uint32_t)a.table[(int64_t)b * a.max_pages + (to >> a.page_log)];
     const int pf = paged_page_lane(a, b, from >> a.page_log);
@@ -209,11 +258,13 @@ hipError_t launch_paged_evict(const PagedArgs& a, int elem, int d, int32_t* lens
   e.moves = (int32_t*)(ws + evict_align(pairs * 4) + evict_align(pairs * a.cap * 4));
   hipLaunchKernelGGL(paged_select_kernel, dim3((unsigned)pairs), dim3(kSelThreads), 0, st, e);
   if (hipError_t r = hipGetLastError(); r != hipSuccess) return r;
-  const dim3 grid((unsigned)(pairs * kMoveWgs)), blk(256);
-  if (elem == 2 && d == 128) hipLaunchKernelGGL((paged_move_kernel<2, 128>), grid, blk, 0, st, e);
-  else if (elem == 2) hipLaunchKernelGGL((paged_move_kernel<2, 64>), grid, blk, 0, st, e);
-  else if (d == 128) hipLaunchKernelGGL((paged_move_kernel<4, 128>), grid, blk, 0, st, e);
-  else hipLaunchKernelGGL((paged_move_kernel<4, 64>), grid, blk, 0, st, e);
+  // eight workgroups per CU are resident at once; how many tokens move is not known here
+  const int wgs = pairs < 2048 ? (int)(2048 / pairs < 64 ? 2048 / pairs : 64) : 1;
+  const dim3 grid((unsigned)(pairs * wgs)), blk(256);
+  if (elem == 2 && d == 128) hipLaunchKernelGGL((paged_move_kernel<2, 128>), grid, blk, 0, st, e, wgs);
+  else if (elem == 2) hipLaunchKernelGGL((paged_move_kernel<2, 64>), grid, blk, 0, st, e, wgs);
+  else if (d == 128) hipLaunchKernelGGL((paged_move_kernel<4, 128>), grid, blk, 0, st, e, wgs);
+  else hipLaunchKernelGGL((paged_move_kernel<4, 64>), grid, blk, 0, st, e, wgs);
   return hipGetLastError();
 }
 
