@@ -24,6 +24,8 @@ static int paged_args(const dash_paged_params* p, PagedArgs* a, bool rows, bool 
   if (rows && (bad(p->q_stride, 2) || bad(p->o_stride, 2))) return DASH_EINVAL;
   if (fresh && (bad(p->k_new_stride, 2) || bad(p->v_new_stride, 2))) return DASH_EINVAL;
   if (d != 64 && d != 128) return DASH_EUNSUPPORTED;
+  // offsets between the 16 rows of a tile are 32-bit numbers
+  if (rows && (p->q_stride[0] > (1 << 25) || p->q_stride[1] > (1 << 25) || p->o_stride[0] > (1 << 25) || p->o_stride[1] > (1 << 25))) return DASH_EUNSUPPORTED;
   const int g = p->h_q / p->h_kv;
   if (g != 1 && g != 2 && g != 4 && g != 8 && g != 16) return DASH_EUNSUPPORTED;
   int log = 4;

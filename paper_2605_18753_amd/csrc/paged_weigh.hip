@@ -7,8 +7,8 @@
 // A single token: K is read once, HBM bounds it.  Many: an exponential, an FMA and an addition per pair, 24 clocks of a SIMD for 64
 // pairs, against 16 (head dimension 128; 64: 8) of matrix work.
 //
-// The keys of all sequences are dealt evenly: items of 4 waves' keys, a contiguous run of them to each of a fixed number of
-// workgroups; fewer items than workgroups have their rows cut into parts instead, added up by a second launch.
+// (block of keys, row tile) pairs of all sequences are dealt evenly to a fixed number of workgroups; blocks cut between two of them
+// are added up by a second launch, in a fixed order.
 #include "f32_tiles.h"
 #include "lds_copy.h"
 #include "paged.h"
@@ -48,71 +48,88 @@ template <int D> struct WeighTile<float, D> {
 
 template <typename T> constexpr int kWeighKeys = sizeof(T) == 2 ? 256 : 128;   // keys of an item
 
-// rows of a sequence that weigh, from t0 on
-__device__ __forceinline__ int weigh_first(const PagedArgs& a, int m) { return a.last > 0 ? max(m - a.last, 0) : 0; }
-
-// items of a sequence; none without rows
-template <typename T> __device__ __forceinline__ int weigh_items(int m, int n) { return m > 0 ? (n + kWeighKeys<T> - 1) / kWeighKeys<T> : 0; }
-
-template <typename T> __device__ __forceinline__ int weigh_total(const PagedArgs& a) {
+// The work of a kv-head: items (blocks of keys) times the row tiles of their sequence, one after the other, dealt in equal runs
+// [w F / G, (w + 1) F / G) to G workgroups.
+struct WeighSeq { int items, tiles, x0; };                 // blocks of keys, row tiles each, the first of these
+template <typename T> __device__ __forceinline__ WeighSeq weigh_seq(const PagedArgs& a, int m, int n) {
+  const int Tt = 16 / a.g, x0 = (a.last > 0 ? max(m - a.last, 0) : 0) / Tt;
+  return {m > 0 ? (n + kWeighKeys<T> - 1) / kWeighKeys<T> : 0, (m + Tt - 1) / Tt - x0, x0};
+}
+__device__ __forceinline__ int64_t scan64(int64_t v) {     // inclusive, over the lanes up to one's own
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t u = __shfl_up((long long)v, o);
+    if ((int)lane_id() >= o) v += u;
+  }
+  return v;
+}
+__device__ __forceinline__ int64_t lane64(int64_t v, int l) {   // lane l's, as a scalar
+  return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)((uint64_t)v >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, l));
+}
+// whole: places are items, which are not cut
+template <typename T> __device__ __forceinline__ int64_t weigh_total(const PagedArgs& a, bool whole = false) {
   const int lane = lane_id();
-  int total = 0;
-  for (int i0 = 0; i0 < a.batch; i0 += 64)
-    total += __builtin_amdgcn_readlane(
-        wave_scan(i0 + lane < a.batch ? weigh_items<T>(paged_rows(a, i0 + lane).y, paged_len(a, i0 + lane)) : 0), 63);
+  int64_t total = 0;
+  for (int i0 = 0; i0 < a.batch; i0 += 64) {
+    int64_t v = 0;
+    if (i0 + lane < a.batch) {
+      const WeighSeq s = weigh_seq<T>(a, paged_rows(a, i0 + lane).y, paged_len(a, i0 + lane));
+      v = whole ? s.items : (int64_t)s.items * s.tiles;
+    }
+    total += lane64(scan64(v), 63);
+  }
   return total;
 }
-struct WeighItem { int b, block, blocks, r0, m, n; };
-template <typename T> __device__ __forceinline__ void weigh_find(const PagedArgs& a, int idx, WeighItem& it) {
+struct WeighItem { int b, block, x, r0, m, n; WeighSeq s; };   // x: row tiles of the item before the place
+// the item at place f < weigh_total
+template <typename T> __device__ __forceinline__ void weigh_find(const PagedArgs& a, int64_t f, WeighItem& it, bool whole = false) {
   const int lane = lane_id();
-  int base = 0;
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
     int2 rm = make_int2(0, 0);
     int n = 0;
+    WeighSeq s = {0, 0, 0};
     if (i0 + lane < a.batch) {
       rm = paged_rows(a, i0 + lane);
       n = paged_len(a, i0 + lane);
+      s = weigh_seq<T>(a, rm.y, n);
     }
-    const int x = weigh_items<T>(rm.y, n), incl = wave_scan(x);
-    const uint64_t hit = __ballot(base + incl > idx);
+    const int64_t v = whole ? s.items : (int64_t)s.items * s.tiles, incl = scan64(v);
+    const uint64_t hit = __ballot(incl > f);
     if (hit) {
       const int l = __builtin_ctzll(hit);
       it.b = i0 + l;
-      it.blocks = __builtin_amdgcn_readlane(x, l);
-      it.block = idx - (base + __builtin_amdgcn_readlane(incl, l) - it.blocks);
+      it.s = {__builtin_amdgcn_readlane(s.items, l), __builtin_amdgcn_readlane(s.tiles, l), __builtin_amdgcn_readlane(s.x0, l)};
       it.r0 = __builtin_amdgcn_readlane(rm.x, l);
       it.m = __builtin_amdgcn_readlane(rm.y, l);
       it.n = __builtin_amdgcn_readlane(n, l);
+      const int64_t in = f - lane64(incl - v, l);
+      it.block = whole ? (int)in : __builtin_amdgcn_readfirstlane((int)(in / it.s.tiles));
+      it.x = whole ? 0 : __builtin_amdgcn_readfirstlane((int)(in - (int64_t)it.block * it.s.tiles));
       return;
     }
-    base += __builtin_amdgcn_readlane(incl, 63);
+    f -= lane64(incl, 63);
   }
 }
-
-// parts that an item's rows are cut into; one where the host gave no room for records
-__device__ __forceinline__ int weigh_parts(const PagedArgs& a, int total) { return a.part_o ? min(max(a.wgs / total, 1), 64) : 1; }
+__device__ __forceinline__ int64_t weigh_bound(const PagedArgs& a, int64_t total, int w) {
+  return total / a.wgs * w + total % a.wgs * w / a.wgs;
+}
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_weigh_kernel(PagedArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : D == 128 ? 3 : 4) void paged_weigh_kernel(PagedArgs a) {
   constexpr int SUBS = WeighTile<T, D>::SUBS;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv;
-  const int total = weigh_total<T>(a);
-  if (total == 0) return;
-  // parts > 1: one item each, its rows cut; else a run of whole items
-  const int parts = weigh_parts(a, total);
-  int i0, i1, part = 0;
-  if (parts > 1) {
-    i0 = wg / parts; part = wg % parts; i1 = min(i0 + 1, total);
-  } else {
-    i0 = (int)((int64_t)wg * total / a.wgs); i1 = (int)((int64_t)(wg + 1) * total / a.wgs);
-  }
+  const int64_t total = weigh_total<T>(a);
+  const int64_t f0 = weigh_bound(a, total, wg);
+  int64_t todo = weigh_bound(a, total, wg + 1) - f0;
+  if (todo <= 0) return;
   const int Tt = 16 / a.g, n = lane & 15, kq = lane >> 4, pm = (1 << a.page_log) - 1;
-  const int head = r * a.g + n % a.g;
+  const int tl = n / a.g;
+  const uint32_t q_lane = (uint32_t)(tl * (int)a.q_t + n % a.g * (int)a.q_h) * (uint32_t)sizeof(T) + kq * 16;
+  const uint32_t l_lane = (uint32_t)(tl * a.h_q + n % a.g) * 4u;
   WeighItem it;
-  it.block = it.blocks = 0;
-  for (int i = i0; i < i1; i++) {
-    if (++it.block >= it.blocks) weigh_find<T>(a, i, it);
+  weigh_find<T>(a, f0, it);
+  while (true) {
     const int key0 = it.block * kWeighKeys<T> + wave * SUBS * 16;
     WeighTile<T, D> kf[SUBS];
     int page[SUBS];
@@ -125,34 +142,47 @@ __global__ __launch_bounds__(256) void paged_weigh_kernel(PagedArgs a) {
       kf[s].load((const T*)a.k + (int64_t)paged_clamp(a, page[s]) * a.kp_p + r * a.kp_h + (int64_t)(key & pm) * a.kp_t, kq);
       acc[s] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    // row tiles: from the first that sees one of the wave's keys
-    const int first = weigh_first(a, it.m), back = it.n - it.m;
-    const int x0 = first / Tt, x1 = (it.m + Tt - 1) / Tt, per = (x1 - x0 + parts - 1) / parts;
-    int x = x0 + part * per;
-    const int xe = min(x + per, x1);
-    if (a.causal) x = max(x, (key0 - back) / Tt);              // its token sees keys up to back + t
+    // this run's row tiles of the item, those before the first that sees one of the wave's keys left out
+    const int take = (int)min((int64_t)(it.s.tiles - it.x), todo), back = it.n - it.m;
+    const int first = a.last > 0 ? max(it.m - a.last, 0) : 0;
+    int x = it.s.x0 + it.x;
+    const int xe = x + take;
+    if (a.causal) x = min(max(x, (key0 - back) / Tt), xe);     // its token sees keys up to back + t
     if (key0 >= it.n) x = xe;
+    // A tile's rows lie at constant offsets of a lane from its first row's address, a scalar; lanes behind the last row repeat it.
     WeighTile<T, D> qf;
-    float off = -INFINITY;
+    float l = 0.f;
+    const char* q_at = (const char*)((const T*)a.q + (int64_t)(it.r0 + x * Tt) * a.q_t + (int64_t)(r * a.g) * a.q_h);
+    const char* l_at = (const char*)(a.lse_in + (int64_t)(it.r0 + x * Tt) * a.h_q + r * a.g);
     auto ask = [&](int y) {
-      const int t = y * Tt + n / a.g, tc = min(t, it.m - 1);
-      qf.load((const T*)a.q + (it.r0 + tc) * a.q_t + head * a.q_h, kq);
-      const float l = a.lse_in[(int64_t)(it.r0 + tc) * a.h_q + head];
-      const bool live = t < it.m && t >= first && l != -INFINITY;
-      off = live ? -l * kLog2e : -INFINITY;
-      if (!live) qf.clear();                                   // whatever the row holds
+      uint32_t q_off = q_lane, l_off = l_lane;
+      if (__builtin_expect((y + 1) * Tt > it.m, 0)) {
+        const int back_rows = max(tl - (it.m - 1 - y * Tt), 0);
+        q_off -= (uint32_t)back_rows * (uint32_t)a.q_t * (uint32_t)sizeof(T);
+        l_off -= (uint32_t)(back_rows * a.h_q) * 4u;
+      }
+      qf.load((const T*)(q_at + q_off), 0);
+      l = *(const float*)(l_at + l_off);
+      q_at += (int64_t)Tt * a.q_t * sizeof(T);
+      l_at += (int64_t)Tt * a.h_q * 4;
     };
     if (x < xe) ask(x);
     for (; x < xe; x++) {
+      const int t = x * Tt + tl;
+      float off = l == -INFINITY ? -INFINITY : -l * kLog2e;
+      if (__builtin_expect(x * Tt < first || (x + 1) * Tt > it.m, 0)) {        // rows that do not weigh, whatever they hold
+        if (t < first || t >= it.m) {
+          qf.clear();
+          off = -INFINITY;
+        }
+        asm volatile("" : "+v"(off));
+      }
       f32x4 s[SUBS];
 #pragma unroll
       for (int j = 0; j < SUBS; j++) s[j] = kf[j].dot(qf);
-      const float o = off;
-      const int t0 = x * Tt;
       if (x + 1 < xe) ask(x + 1);
-      const int low = a.causal ? back + t0 : it.n - 1;         // the tile's first token sees keys up to here
-      if (key0 + SUBS * 16 - 1 > low) {
-        const int lim = (a.causal ? min(back + t0 + n / a.g, it.n - 1) : it.n - 1) - key0 - 4 * kq;
+      if (key0 + SUBS * 16 - 1 > (a.causal ? back + x * Tt : it.n - 1)) {       // the tile's first token sees keys up to there
+        const int lim = (a.causal ? min(back + t, it.n - 1) : it.n - 1) - key0 - 4 * kq;
 #pragma unroll
         for (int j = 0; j < SUBS; j++)
 #pragma unroll
@@ -161,9 +191,11 @@ __global__ __launch_bounds__(256) void paged_weigh_kernel(PagedArgs a) {
 #pragma unroll
       for (int j = 0; j < SUBS; j++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) acc[j][e] += __builtin_amdgcn_exp2f(fmaf(s[j][e], a.c1, o));
+        for (int e = 0; e < 4; e++) acc[j][e] += __builtin_amdgcn_exp2f(fmaf(s[j][e], a.c1, off));
     }
     // over the 16 rows of a key; lane (n, kq), n < 4, takes key 4 kq + n
+    const bool whole = take == it.s.tiles;
+    float* rec = a.part_o + (((int64_t)r * a.wgs + wg) * 2 + (it.x == 0)) * kWeighKeys<T> + wave * SUBS * 16 + 4 * kq + n;
 #pragma unroll
     for (int j = 0; j < SUBS; j++) {
 #pragma unroll
@@ -171,50 +203,179 @@ __global__ __launch_bounds__(256) void paged_weigh_kernel(PagedArgs a) {
       const float w = n == 0 ? acc[j][0] : n == 1 ? acc[j][1] : n == 2 ? acc[j][2] : acc[j][3];
       const int key = key0 + 16 * j + 4 * kq + n;
       if (n < 4) {
-        if (parts > 1) a.part_o[((int64_t)r * a.wgs + wg) * kWeighKeys<T> + wave * SUBS * 16 + 16 * j + 4 * kq + n] = w;
+        if (!whole) rec[16 * j] = w;                           // an item cut between runs
         else if (key < it.n && (uint32_t)page[j] < (uint32_t)a.n_pages) a.weights[(((int64_t)page[j] * a.h_kv + r) << a.page_log) + (key & pm)] += w;
       }
     }
+    if ((todo -= take) <= 0) return;
+    it.x = 0;
+    if (++it.block >= it.s.items) weigh_find<T>(a, weigh_bound(a, total, wg + 1) - todo, it);
   }
 }
 
-// the parts of items whose rows were cut: a thread per key
+// Items cut between runs.  The end of run wg - 1 lies inside an item whose first piece is that run's: its last record.  Of the runs
+// behind it that begin inside the item, the first records follow.  A thread per key.
 template <typename T>
 __global__ __launch_bounds__(kWeighKeys<T>) void paged_weigh_sum_kernel(PagedArgs a) {
-  const int r = blockIdx.x % a.h_kv, i = blockIdx.x / a.h_kv;
-  const int total = weigh_total<T>(a);
-  if (i >= total) return;
-  const int parts = weigh_parts(a, total);
-  if (parts <= 1) return;
+  const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv + 1;
+  const int64_t total = weigh_total<T>(a), f = weigh_bound(a, total, wg);
+  if (f >= total || f == weigh_bound(a, total, wg - 1)) return;
   WeighItem it;
-  weigh_find<T>(a, i, it);
+  weigh_find<T>(a, f, it);
+  const int64_t begin = f - it.x, end = begin + it.s.tiles;
+  if (it.x == 0 || weigh_bound(a, total, wg - 1) > begin) return;              // not cut here, or not for the first time
+  const float* p = a.part_o + ((int64_t)r * a.wgs + wg - 1) * 2 * kWeighKeys<T> + threadIdx.x;
+  float w = p[kWeighKeys<T>];
+  for (int k = wg; k < a.wgs; k++) {
+    const int64_t at = weigh_bound(a, total, k);
+    if (at >= end) break;
+    p += 2 * kWeighKeys<T>;
+    if (at < weigh_bound(a, total, k + 1)) w += *p;
+  }
   const int key = it.block * kWeighKeys<T> + threadIdx.x;
   if (key >= it.n) return;
-  const float* p = a.part_o + ((int64_t)r * a.wgs + (int64_t)i * parts) * kWeighKeys<T> + threadIdx.x;
-  float w = 0.f;
-#pragma unroll 4
-  for (int j = 0; j < parts; j++) w += p[(int64_t)j * kWeighKeys<T>];
   const uint32_t page = (uint32_t)a.table[(int64_t)it.b * a.max_pages + (key >> a.page_log)];
-  if (page >= (uint32_t)a.n_pages) return;
-  a.weights[(((int64_t)page * a.h_kv + r) << a.page_log) + (key & ((1 << a.page_log) - 1))] += w;
+  if (page < (uint32_t)a.n_pages) a.weights[(((int64_t)page * a.h_kv + r) << a.page_log) + (key & ((1 << a.page_log) - 1))] += w;
+}
+
+// Few rows a sequence (decode): K is streamed once, the next block's keys asked for before the present one's are used.  Whole blocks
+// only, in equal runs.
+template <int D>
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void paged_weigh_stream_kernel(PagedArgs a) {
+  using T = uint16_t;
+  using Tile = WeighTile<T, D>;
+  constexpr int SUBS = Tile::SUBS;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv;
+  const int Tt = 16 / a.g, n = lane & 15, kq = lane >> 4, pm = (1 << a.page_log) - 1, tl = n / a.g;
+  const uint32_t q_lane = (uint32_t)(tl * (int)a.q_t + n % a.g * (int)a.q_h) * 2u + kq * 16;
+  const uint32_t l_lane = (uint32_t)(tl * a.h_q + n % a.g) * 4u;
+  // blocks of all sequences, and the run's
+  const int64_t total = weigh_total<T>(a, true);
+  int64_t f = weigh_bound(a, total, wg);
+  int todo = (int)(weigh_bound(a, total, wg + 1) - f);
+  if (todo <= 0) return;
+  WeighItem it, next;
+  weigh_find<T>(a, f, it, true);
+  auto advance = [&](WeighItem& x) {
+    f++;
+    if (++x.block >= x.s.items) weigh_find<T>(a, f, x, true);
+  };
+  // lane (n, kq), n < 4, takes key 4 kq + n of 16 (the others, and those behind the end, some key of the page)
+  auto place = [&](const WeighItem& x, int page, int key16) {
+    return (((int64_t)paged_clamp(a, page) * a.h_kv + r) << a.page_log) + ((key16 + 4 * kq + (n & 3)) & pm);
+  };
+  // A block's keys, and what its keys weigh so far: asked for behind the keys of the next block, that would be waited for with them.
+  auto load_keys = [&](const WeighItem& x, Tile (&kf)[SUBS], int (&page)[SUBS], float (&was)[SUBS]) {
+    const int key0 = x.block * kWeighKeys<T> + wave * SUBS * 16;
+#pragma unroll
+    for (int s = 0; s < SUBS; s++) page[s] = paged_entry(a, x.b, min(key0 + 16 * s, (x.n - 1) & ~15) >> a.page_log);
+#pragma unroll
+    for (int s = 0; s < SUBS; s++) {
+      const int key = min(min(key0 + 16 * s, (x.n - 1) & ~15) + n, x.n - 1);
+      kf[s].load((const T*)a.k + (int64_t)paged_clamp(a, page[s]) * a.kp_p + r * a.kp_h + (int64_t)(key & pm) * a.kp_t, kq);
+    }
+#pragma unroll
+    for (int s = 0; s < SUBS; s++) was[s] = a.weights[place(x, page[s], key0 + 16 * s)];
+  };
+  Tile qf;
+  float off = 0.f;
+  int q_of = -1;                                             // the sequence whose only row tile qf and off hold
+  auto load_rows = [&](const WeighItem& x, int y) {
+    const int t = y * Tt + tl, up = max(t - (x.m - 1), 0);   // a lane behind the last row repeats it
+    const int first = a.last > 0 ? max(x.m - a.last, 0) : 0;
+    const char* q_at = (const char*)((const T*)a.q + (int64_t)(x.r0 + y * Tt) * a.q_t + (int64_t)(r * a.g) * a.q_h);
+    const char* l_at = (const char*)(a.lse_in + (int64_t)(x.r0 + y * Tt) * a.h_q + r * a.g);
+    qf.load((const T*)(q_at + (q_lane - (uint32_t)up * (uint32_t)a.q_t * 2u)), 0);
+    const float l = *(const float*)(l_at + (l_lane - (uint32_t)(up * a.h_q) * 4u));
+    off = l == -INFINITY ? -INFINITY : -l * kLog2e;
+    if (t < first || t >= x.m) {                             // does not weigh, whatever it holds
+      qf.clear();
+      off = -INFINITY;
+    }
+  };
+  auto work = [&](const WeighItem& x, const Tile (&kf)[SUBS], const int (&page)[SUBS], const float (&was)[SUBS]) {
+    const int key0 = x.block * kWeighKeys<T> + wave * SUBS * 16, back = x.n - x.m;
+    f32x4 acc[SUBS];
+#pragma unroll
+    for (int j = 0; j < SUBS; j++) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int y = x.s.x0; y < x.s.x0 + x.s.tiles; y++) {
+      if (q_of != x.b) load_rows(x, y);
+      q_of = x.s.tiles == 1 ? x.b : -1;
+      f32x4 s[SUBS];
+#pragma unroll
+      for (int j = 0; j < SUBS; j++) s[j] = kf[j].dot(qf);
+      if (key0 + SUBS * 16 - 1 > (a.causal ? back + y * Tt : x.n - 1)) {
+        const int lim = (a.causal ? min(back + y * Tt + tl, x.n - 1) : x.n - 1) - key0 - 4 * kq;
+#pragma unroll
+        for (int j = 0; j < SUBS; j++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) s[j][e] = 16 * j + e > lim ? -INFINITY : s[j][e];
+      }
+#pragma unroll
+      for (int j = 0; j < SUBS; j++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) acc[j][e] += __builtin_amdgcn_exp2f(fmaf(s[j][e], a.c1, off));
+    }
+#pragma unroll
+    for (int j = 0; j < SUBS; j++) {
+#pragma unroll
+      for (int e = 0; e < 4; e++) acc[j][e] = row16_sum(acc[j][e]);
+      const float w = n == 0 ? acc[j][0] : n == 1 ? acc[j][1] : n == 2 ? acc[j][2] : acc[j][3];
+      const int key = key0 + 16 * j + 4 * kq + n;
+      if (n < 4 && key < x.n && (uint32_t)page[j] < (uint32_t)a.n_pages) a.weights[place(x, page[j], key0 + 16 * j)] = was[j] + w;
+    }
+  };
+  Tile ka[SUBS], kb[SUBS];
+  int pa[SUBS], pb[SUBS];
+  float wa[SUBS], wb[SUBS];
+  load_keys(it, ka, pa, wa);
+  while (true) {
+    next = it;
+    if (todo > 1) {
+      advance(next);
+      load_keys(next, kb, pb, wb);
+    }
+    work(it, ka, pa, wa);
+    if (--todo == 0) return;
+    it = next;
+    if (todo > 1) {
+      advance(next);
+      load_keys(next, ka, pa, wa);
+    }
+    work(it, kb, pb, wb);
+    if (--todo == 0) return;
+    it = next;
+  }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
-static int weigh_wgs(const PagedArgs& a) { return max(768 / a.h_kv, 1); }
-// whether cutting rows into parts can pay: more than two tiles of them
-static bool weigh_may_cut(const PagedArgs& a) { return (int64_t)a.n_rows * a.g > 32; }
+// resident workgroups of a kv-head: three per CU at head dimension 128, four at 64
+static int weigh_wgs(const PagedArgs& a, int d) { return max((d == 128 ? 768 : 1024) / a.h_kv, 1); }
 
-size_t paged_weigh_ws(const PagedArgs& a, int dtype, int) {
-  return (size_t)weigh_wgs(a) * a.h_kv * (dtype == DASH_BF16 ? kWeighKeys<uint16_t> : kWeighKeys<float>) * 4;
+// K is streamed where the sequences bring no more than 16 rows each on the average
+static bool weigh_stream(const PagedArgs& a) { return (int64_t)a.n_rows * a.g <= (int64_t)a.batch * 16; }
+
+size_t paged_weigh_ws(const PagedArgs& a, int dtype, int d) {
+  return (size_t)weigh_wgs(a, d) * a.h_kv * 2 * (dtype == DASH_BF16 ? kWeighKeys<uint16_t> : kWeighKeys<float>) * 4;
 }
 
 template <typename T, int D>
 static hipError_t launch_weigh_t(PagedArgs a, char* ws, hipStream_t st) {
-  a.part_o = weigh_may_cut(a) ? (float*)ws : nullptr;
-  a.wgs = weigh_wgs(a);
+  if constexpr (sizeof(T) == 2) {
+    if (weigh_stream(a)) {
+      a.wgs = max((D == 128 ? 512 : 768) / a.h_kv, 1);
+      hipLaunchKernelGGL(paged_weigh_stream_kernel<D>, dim3((unsigned)(a.wgs * a.h_kv)), dim3(256), 0, st, a);
+      return hipGetLastError();
+    }
+  }
+  a.part_o = (float*)ws;
+  a.wgs = weigh_wgs(a, D);
   hipLaunchKernelGGL((paged_weigh_kernel<T, D>), dim3((unsigned)(a.wgs * a.h_kv)), dim3(256), 0, st, a);
-  if (hipError_t e = hipGetLastError(); e != hipSuccess || !a.part_o) return e;
-  hipLaunchKernelGGL(paged_weigh_sum_kernel<T>, dim3((unsigned)((a.wgs / 2 + 1) * a.h_kv)), dim3(kWeighKeys<T>), 0, st, a);
+  hipError_t e = hipGetLastError();
+  // a single tile of rows is not cut
+  if (e != hipSuccess || a.n_rows * (int64_t)a.g <= 16 || a.wgs == 1) return e;
+  hipLaunchKernelGGL(paged_weigh_sum_kernel<T>, dim3((unsigned)((a.wgs - 1) * a.h_kv)), dim3(kWeighKeys<T>), 0, st, a);
   return hipGetLastError();
 }
 
