@@ -357,21 +357,23 @@ def make_paged_params(cache: PagedCache, n_rows: int, h_q: int, causal: bool = T
 def _paged_call(p: dash_paged_params, cache: PagedCache, row_start, rows, extra=()) -> dash_paged_params:
     """The call's own copy of p, with the strides of its packed tensors; rows: (tensor, heads, field of its strides)."""
     p = dash_paged_params.from_buffer_copy(p)
-    if row_start is not None and (row_start.dtype != torch.int32 or not row_start.is_contiguous() or row_start.numel() != p.batch + 1):
-        raise DashError("row_start: a contiguous int32 tensor of batch + 1 elements")
+    n_rows, head_dim, dtype, dev = p.n_rows, p.head_dim, cache.k.dtype, cache.k.get_device()
+    if row_start is not None and (row_start.dtype is not torch.int32 or row_start.numel() != p.batch + 1 or not row_start.is_contiguous()
+                                  or row_start.get_device() != dev):
+        raise DashError("row_start: a contiguous int32 tensor of batch + 1 elements on the cache's device")
     for t, heads, field in rows:
-        if t.shape != (p.n_rows, heads, p.head_dim) or t.dtype != cache.k.dtype or t.stride(2) != 1:
-            raise DashError(f"packed rows: [{p.n_rows}, {heads}, {p.head_dim}] of the cache's type, head_dim contiguous")
-        getattr(p, field)[:] = t.stride()[:2]
-    for t, dtype, shape in extra:
-        if t is not None and (t.dtype != dtype or t.shape != shape or not t.is_contiguous()):
-            raise DashError(f"expected a contiguous {dtype} tensor of shape {tuple(shape)}")
-    d = cache.k.device
-    for t in (cache.table, cache.lens, row_start, *(x[0] for x in rows), *(x[0] for x in extra)):
-        if t is not None and t.device != d:
-            raise DashError("the tensors of a call lie on one device")
-    if d.index is not None and _device is not None and torch.cuda.is_initialized() and d.index != _device():
-        raise DashError(f"the cache lies on {d}, which is not the current device")
+        s = t.stride()
+        if t.dtype is not dtype or t.shape != (n_rows, heads, head_dim) or s[2] != 1 or t.get_device() != dev:
+            raise DashError(f"packed rows: [{n_rows}, {heads}, {head_dim}] of the cache's type and device, head_dim contiguous")
+        f = getattr(p, field)
+        f[0], f[1] = s[0], s[1]
+    for t, want, shape in extra:
+        if t is not None and (t.dtype is not want or t.shape != shape or not t.is_contiguous() or t.get_device() != dev):
+            raise DashError(f"expected a contiguous {want} tensor of shape {tuple(shape)} on the cache's device")
+    if cache.table.get_device() != dev or cache.lens.get_device() != dev:
+        raise DashError("the cache's tensors lie on one device")
+    if dev >= 0 and _device is not None and dev != _device():
+        raise DashError(f"the cache lies on cuda:{dev}, which is not the current device")
     return p
 
 

@@ -602,15 +602,17 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
   if (a.lse && h == 0) a.lse[(int64_t)(it.r0 + t) * a.h_q + head] = l_tot == 0.f ? -INFINITY : (m_run + log2f(l_tot)) * kLn2;
 }
 
-// Adds the parts of cut items: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  D / 4 threads a (token, head) row.  ROWS: of a
-// tile (16 or 128), whose records are laid out accordingly.
-template <typename T, int D, int ROWS>
+// Adds the parts of cut items: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  A workgroup adds 256 / (D / 4) / SLICES (token, head)
+// rows: D / 4 threads a row, 4 values each, in SLICES groups that take every SLICES-th part.  ROWS: of a tile (16 or 128), whose
+// records are laid out accordingly.
+template <typename T, int D, int ROWS, int SLICES>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
-  constexpr int TPR = D / 4, RPW = 64 / TPR;               // threads of a row, rows of a wave
-  const int lane = threadIdx.x & 63, c = lane % TPR;
+  constexpr int TPR = D / 4, PER = 256 / TPR / SLICES;     // threads of a row's slice, rows of a workgroup
+  __shared__ f32x4 xo[SLICES > 1 ? 256 : 1];
+  __shared__ float xd[SLICES > 1 ? 256 / TPR : 1];
+  const int lane = threadIdx.x & 63, c = threadIdx.x % TPR, unit = threadIdx.x / TPR, slice = unit / PER;
   // rows in the order kv-head, token, head of the group: neighbours lie side by side in the records
-  const int64_t per = (int64_t)a.n_rows * a.g;
-  const int64_t gr = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * RPW + lane / TPR;
+  const int64_t per = (int64_t)a.n_rows * a.g, gr = (int64_t)blockIdx.x * PER + unit % PER;
   const int r = (int)min(gr / per, (int64_t)a.h_kv - 1), row = (int)(gr % per) / a.g, hg = (int)(gr % per) % a.g;
   // the dealing of the launch before, for a given row
   const auto shape = [&](int m, int n) { return tile_shape<ROWS>(a, m, n); };
@@ -624,7 +626,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
     }
     const int np = (s.y + S - 1) / S, incl = wave_scan(s.x * np);
 #pragma unroll
-    for (int k = 0; k < RPW; k++) {
+    for (int k = 0; k < 64 / TPR; k++) {
       const int want = __builtin_amdgcn_readlane(row, k * TPR);
       const uint64_t hit = __ballot(want >= rm.x && want < rm.x + rm.y);
       if (hit) {
@@ -636,25 +638,41 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
     }
     base += __builtin_amdgcn_readlane(incl, 63);
   }
-  if (parts <= 1 || gr >= per * a.h_kv) return;
-  const int Tt = ROWS / a.g, t = row - r0, tile = t / Tt, in = (t % Tt) * a.g + hg;
-  const int64_t rec = (int64_t)r * a.part_stride + first + (tiles - 1 - tile) * parts;
-  const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + rec * ROWS + in;
+  const bool mine = parts > 1 && gr < per * a.h_kv;
   float M = -INFINITY, den = 0.f;
-#pragma unroll 8
-  for (int p = 0; p < parts; p++) M = fmaxf(M, ml[p * ROWS].x);
-  const float use = M == -INFINITY ? 0.f : M;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o) + (ROWS == 16 ? (rec * ROWS + in) * (D / 4) + c : (rec * (D / 4) + c) * ROWS + in);
+  if (mine) {
+    const int Tt = ROWS / a.g, t = row - r0, tile = t / Tt, in = (t % Tt) * a.g + hg;
+    const int64_t rec = (int64_t)r * a.part_stride + first + (tiles - 1 - tile) * parts;
+    const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + rec * ROWS + in;
+    // the maximum over all parts, c-th part of TPR a thread's; every slice finds the same
+    for (int p = c; p < parts; p += TPR) M = fmaxf(M, ml[p * ROWS].x);
+    M = row16_reduce(M, OpMax());
+    if constexpr (TPR == 32) M = fmaxf(M, __shfl_xor(M, 16));
+    const float use = M == -INFINITY ? 0.f : M;
+    const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o) + (ROWS == 16 ? (rec * ROWS + in) * (D / 4) + c : (rec * (D / 4) + c) * ROWS + in);
 #pragma unroll 8
-  for (int p = 0; p < parts; p++) {
-    const float2 y = ml[p * ROWS];
-    const float w = __builtin_amdgcn_exp2f(y.x - use);
-    const f32x4 x = po[(int64_t)p * ROWS * (D / 4)];
-    den = fmaf(w, y.y, den);
+    for (int p = slice; p < parts; p += SLICES) {
+      const float2 y = ml[p * ROWS];
+      const float w = __builtin_amdgcn_exp2f(y.x - use);
+      const f32x4 x = po[(int64_t)p * ROWS * (D / 4)];
+      den = fmaf(w, y.y, den);
 #pragma unroll
-    for (int e = 0; e < 4; e++) o[e] = fmaf(w, x[e], o[e]);
+      for (int e = 0; e < 4; e++) o[e] = fmaf(w, x[e], o[e]);
+    }
   }
+  if constexpr (SLICES > 1) {
+    xo[threadIdx.x] = o;
+    if (c == 0) xd[unit] = den;
+    __syncthreads();
+    if (slice > 0) return;
+#pragma unroll
+    for (int k = 1; k < SLICES; k++) {
+      o += xo[threadIdx.x + k * PER * TPR];
+      den += xd[unit + k * PER];
+    }
+  }
+  if (!mine) return;
   const float inv = den > 0.f ? 1.f / den : den == 0.f ? 0.f : den;
   const int head = r * a.g + hg;
   put_row4((T*)a.o + row * a.o_t + head * a.o_h + c * 4, o, inv);
@@ -679,11 +697,13 @@ size_t paged_attend_ws(const PagedArgs& a, int dtype, int d) {
   return ws_align(recs * 8) + recs * d * 4;
 }
 
+// Few rows leave the chip idle unless several groups of threads share a row's parts.
 template <typename T, int D, int ROWS>
 static hipError_t launch_merge(const PagedArgs& a, hipStream_t st) {
   const int64_t rows = (int64_t)a.n_rows * a.h_q;
-  constexpr int per = 256 / (D / 4);
-  hipLaunchKernelGGL((paged_merge_kernel<T, D, ROWS>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, a);
+  constexpr int units = 256 / (D / 4), slices = 4, per = units / slices;
+  if (rows <= 8192) hipLaunchKernelGGL((paged_merge_kernel<T, D, ROWS, slices>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((paged_merge_kernel<T, D, ROWS, 1>), dim3((unsigned)((rows + units - 1) / units)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

@@ -1,51 +1,76 @@
 // The paged cache itself: new tokens into their pages, and the eviction of the tokens with the least weight.
+#include <type_traits>
+
 #include "paged.h"
 
 namespace dash {
 
 // ---- append ----------------------------------------------------------------------------------------------------------
-// A workgroup writes kAppendRows packed rows: every row's keys and values of all kv-heads, 16 bytes a thread at a time.  Bound by
-// HBM: each byte is read once and written once.
-constexpr int kAppendRows = 4;
-
-template <int ES>   // bytes of an element
-__global__ __launch_bounds__(256) void paged_append_kernel(PagedArgs a, int chunks) {   // chunks: 16-byte pieces of a row
-  const int tid = threadIdx.x, lane = tid & 63;
-  for (int i = 0; i < kAppendRows; i++) {
-    const int row = blockIdx.x * kAppendRows + i;
-    if (row >= a.n_rows) return;
-    // the sequence the row belongs to: as many as end at or before it
-    int b = 0;
-    for (int i0 = 0; i0 < a.batch; i0 += 64)
-      b += __popcll(__ballot(i0 + lane < a.batch && a.row_start[i0 + lane + 1] <= row));
-    b = __builtin_amdgcn_readfirstlane(b);
-    if (b >= a.batch) continue;
-    const int2 rm = paged_rows(a, b);
-    const int back = rm.x + rm.y - row, n = paged_len(a, b), slot = n - back;   // back: 1 for the newest token
-    if (row < rm.x || back < 1 || slot < 0) continue;
-    const uint32_t page = (uint32_t)a.table[(int64_t)b * a.max_pages + (slot >> a.page_log)];
-    if (page >= (uint32_t)a.n_pages) continue;             // no page: nothing is written
-    const int off = slot & ((1 << a.page_log) - 1);
-    for (int x = tid; x < 2 * a.h_kv * chunks; x += 256) {
-      const int c = x % chunks, y = x / chunks, h = y >> 1;
-      const bool is_v = y & 1;
-      const char* from = (const char*)(is_v ? a.v_new : a.k_new) + (row * (is_v ? a.vn_t : a.kn_t) + h * (is_v ? a.vn_h : a.kn_h)) * ES;
-      char* to = (char*)(is_v ? a.v : a.k) + ((int64_t)page * (is_v ? a.vp_p : a.kp_p) + h * (is_v ? a.vp_h : a.kp_h) + off * (is_v ? a.vp_t : a.kp_t)) * ES;
-      reinterpret_cast<u32x4*>(to)[c] = reinterpret_cast<const u32x4*>(from)[c];
+// A wave writes a packed row: its keys and values of all kv-heads, 16 bytes a lane at a time.  Bound by HBM where there are many rows (each
+// byte is read once and written once), by the chain of dependent loads where there are few: what a row holds, and the starts,
+// lengths and positions of 64 sequences, are asked for together; only the page waits for them.
+template <int ES, int D>   // bytes of an element
+__global__ __launch_bounds__(256) void paged_append_kernel(PagedArgs a) {
+  constexpr int CHUNKS = D * ES / 16, AHEAD = 4;             // 16-byte pieces of a row; pieces of a lane in flight
+  const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (row >= a.n_rows) return;
+  const int pieces = 2 * a.h_kv * CHUNKS;
+  const char* kn = (const char*)a.k_new + row * a.kn_t * ES;
+  const char* vn = (const char*)a.v_new + row * a.vn_t * ES;
+  u32x4 w[AHEAD];
+  auto load = [&](int x0) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; i++) {
+      const int x = x0 + 64 * i, c = x % CHUNKS, h = x / CHUNKS >> 1;
+      const char* from = x / CHUNKS & 1 ? vn + h * a.vn_h * ES : kn + h * a.kn_h * ES;
+      if (x < pieces) w[i] = reinterpret_cast<const u32x4*>(from)[c];
     }
-    if (a.weights || a.pos)
-      for (int h = tid; h < a.h_kv; h += 256) {
-        const int64_t at = (((int64_t)page * a.h_kv + h) << a.page_log) + off;
-        if (a.weights) a.weights[at] = 0.f;
-        if (a.pos) a.pos[at] = (a.seen ? a.seen[b] : n) - back;
-      }
+  };
+  load(lane);
+  // the sequence that the row belongs to: as many as end at or before it
+  int b = -1, end = 0, n = 0, seen = 0;
+  for (int i0 = 0; i0 < a.batch && b < 0; i0 += 64) {
+    const int i = min(i0 + lane, a.batch - 1);
+    const int s0 = a.row_start[i], s1 = a.row_start[i + 1], len = a.lens[i], sn = a.seen ? a.seen[i] : 0;
+    const uint64_t on = __ballot(i0 + lane < a.batch && s1 > row);
+    if (on) {
+      const int l = __builtin_ctzll(on);
+      if (__builtin_amdgcn_readlane(s0, l) > row) return;    // a row of no sequence
+      b = i0 + l;
+      end = min(__builtin_amdgcn_readlane(s1, l), a.n_rows);
+      n = min(max(__builtin_amdgcn_readlane(len, l), 0), a.cap);
+      seen = a.seen ? __builtin_amdgcn_readlane(sn, l) : n;
+    }
+  }
+  const int back = end - row, slot = n - back;               // back: 1 for the newest token
+  if (b < 0 || slot < 0) return;
+  const uint32_t page = (uint32_t)paged_entry(a, b, slot >> a.page_log);
+  if (page >= (uint32_t)a.n_pages) return;                   // no page: nothing is written
+  const int off = slot & ((1 << a.page_log) - 1);
+  char* kp = (char*)a.k + ((int64_t)page * a.kp_p + off * a.kp_t) * ES;
+  char* vp = (char*)a.v + ((int64_t)page * a.vp_p + off * a.vp_t) * ES;
+  for (int x0 = lane; x0 - lane < pieces; x0 += 64 * AHEAD) {
+    if (x0 != lane) load(x0);
+#pragma unroll
+    for (int i = 0; i < AHEAD; i++) {
+      const int x = x0 + 64 * i, c = x % CHUNKS, h = x / CHUNKS >> 1;
+      char* to = x / CHUNKS & 1 ? vp + h * a.vp_h * ES : kp + h * a.kp_h * ES;
+      if (x < pieces) reinterpret_cast<u32x4*>(to)[c] = w[i];
+    }
+  }
+  for (int h = lane; h < a.h_kv; h += 64) {
+    const int64_t at = (((int64_t)page * a.h_kv + h) << a.page_log) + off;
+    if (a.weights) a.weights[at] = 0.f;
+    if (a.pos) a.pos[at] = seen - back;
   }
 }
 
 hipError_t launch_paged_append(const PagedArgs& a, int elem, int d, hipStream_t st) {
-  const dim3 grid((unsigned)((a.n_rows + kAppendRows - 1) / kAppendRows)), blk(256);
-  if (elem == 2) hipLaunchKernelGGL(paged_append_kernel<2>, grid, blk, 0, st, a, d * 2 / 16);
-  else hipLaunchKernelGGL(paged_append_kernel<4>, grid, blk, 0, st, a, d * 4 / 16);
+  const dim3 grid((unsigned)(((int64_t)a.n_rows + 3) / 4)), blk(256);
+  if (elem == 2 && d == 128) hipLaunchKernelGGL((paged_append_kernel<2, 128>), grid, blk, 0, st, a);
+  else if (elem == 2) hipLaunchKernelGGL((paged_append_kernel<2, 64>), grid, blk, 0, st, a);
+  else if (d == 128) hipLaunchKernelGGL((paged_append_kernel<4, 128>), grid, blk, 0, st, a);
+  else hipLaunchKernelGGL((paged_append_kernel<4, 64>), grid, blk, 0, st, a);
   return hipGetLastError();
 }
 
@@ -173,30 +198,44 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e) 
     });
     if (tid == 0) e.counts[pair] = hw.y;
   };
-  if (rows <= kSelRows) {
-    uint32_t key[kSelRows];
+  // keys in registers, in blocks of four rows; a row past the wave's last counts as behind the end
+  auto in_registers = [&](auto rows_tag) {
+    constexpr int ROWS = decltype(rows_tag)::value, AHEAD = ROWS < 16 ? ROWS : 16;
+    uint32_t key[ROWS];
 #pragma unroll
-    for (int j0 = 0; j0 < kSelRows; j0 += 16) {            // sixteen rows in flight
+    for (int j0 = 0; j0 < ROWS; j0 += AHEAD) {
       if (j0 < rows) {
-        float w[16];
-        int p[16];
+        int64_t at[AHEAD];
+        float w[AHEAD];
+        int p[AHEAD];
 #pragma unroll
-        for (int j = 0; j < 16; j++) {
+        for (int j = 0; j < AHEAD; j++) {
           const int i = min(slot0 + (j0 + j) * 64, n - 1);
-          const int64_t at = (((int64_t)paged_page_lane(a, b, i >> a.page_log) * a.h_kv + h) << a.page_log) + (i & pm);
-          w[j] = a.weights[at];
-          p[j] = a.pos[at];
+          at[j] = (((int64_t)paged_page_lane(a, b, i >> a.page_log) * a.h_kv + h) << a.page_log) + (i & pm);
         }
 #pragma unroll
-        for (int j = 0; j < 16; j++) key[j0 + j] = evict_key(w[j], p[j], e.sinks, first_recent);
+        for (int j = 0; j < AHEAD; j++) {
+          w[j] = a.weights[at[j]];
+          p[j] = a.pos[at[j]];
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; j++) key[j0 + j] = evict_key(w[j], p[j], e.sinks, first_recent);
       }
     }
     select([&](auto&& f) {
 #pragma unroll
-      for (int j = 0; j < kSelRows; j++) {
-        if (j < rows) f(key[j], slot0 + j * 64);
+      for (int j0 = 0; j0 < ROWS; j0 += 4) {
+        if (j0 < rows) {
+#pragma unroll
+          for (int j = j0; j < j0 + 4; j++) f(key[j], j < rows ? slot0 + j * 64 : n);
+        }
       }
     });
+  };
+  if (rows <= 8) {                                           // its own code: the longer one's would be fetched for nothing
+    in_registers(std::integral_constant<int, 8>{});
+  } else if (rows <= kSelRows) {
+    in_registers(std::integral_constant<int, kSelRows>{});
   } else {
 #pragma unroll 8
     for (int j = 0; j < rows; j++) {
@@ -213,31 +252,49 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e) 
   }
 }
 
+// A wave moves kMoves tokens at a time: their places first, a lane each, then all their rows at once.
 template <int ES, int D>
 __global__ __launch_bounds__(256) void paged_move_kernel(EvictArgs e, int wgs) {   // wgs: workgroups of a pair
   const PagedArgs& a = e.a;
-  constexpr int C = D * ES / 16, PER = 256 / (2 * C);      // 16-byte pieces of a row; moves a workgroup makes at a time
-  const int pair = blockIdx.x / wgs, part = blockIdx.x % wgs, h = pair % a.h_kv, b = pair / a.h_kv;
+  constexpr int C = D * ES / 16, PER = 64 / C > 0 ? 64 / C : 1, MOVES = 8;        // 16-byte pieces of a row; rows a wave's load covers
+  const int pair = blockIdx.x / wgs, h = pair % a.h_kv, b = pair / a.h_kv;
+  const int lane = threadIdx.x & 63, wave = (blockIdx.x % wgs) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n_moves = e.counts[pair];
-  if (h == 0 && part == 0 && threadIdx.x == 0) e.lens[b] = min(max(e.lens[b], 0), min(a.cap, e.budget));
+  if (h == 0 && wave == 0 && lane == 0) e.lens[b] = min(max(e.lens[b], 0), min(a.cap, e.budget));
   const int32_t* moves = e.moves + (int64_t)pair * a.cap;
-  int32_t* src = e.src ? e.src + (int64_t)pair * e.budget : nullptr;
-  const int sub = threadIdx.x / (2 * C), x = threadIdx.x % (2 * C), c = x % C;
-  const bool is_v = x >= C;
-  const int pm = (1 << a.page_log) - 1;
-  char* base = (char*)(is_v ? a.v : a.k) + h * (is_v ? a.vp_h : a.kp_h) * ES;
-  const int64_t sp = (is_v ? a.vp_p : a.kp_p) * ES, st = (is_v ? a.vp_t : a.kp_t) * ES;
-  for (int j = part * PER + sub; j < n_moves; j += wgs * PER) {
+  const int pm = (1 << a.page_log) - 1, c = lane % C;
+  char* kb = (char*)a.k + h * a.kp_h * ES;
+  char* vb = (char*)a.v + h * a.vp_h * ES;
+  for (int j0 = wave * MOVES; j0 < n_moves; j0 += wgs * 4 * MOVES) {
+    const int j = min(j0 + (lane & (MOVES - 1)), n_moves - 1);
     const int to = moves[j], from = moves[a.cap - 1 - j];
-    const uint32_t pt = (uint32_t)a.table[(int64_t)b * a.max_pages + (to >> a.page_log)];
-    const int pf = paged_page_lane(a, b, from >> a.page_log);
-    if (src && x == 0) src[to] = from;
-    if (pt >= (uint32_t)a.n_pages) continue;
-    reinterpret_cast<u32x4*>(base + pt * sp + (to & pm) * st)[c] = reinterpret_cast<const u32x4*>(base + pf * sp + (from & pm) * st)[c];
-    if (x < 2) {
-      const int64_t it = (((int64_t)pt * a.h_kv + h) << a.page_log) + (to & pm), jf = (((int64_t)pf * a.h_kv + h) << a.page_log) + (from & pm);
-      if (x == 0) a.weights[it] = a.weights[jf];
-      else a.pos[it] = a.pos[jf];
+    const int pt = a.table[(int64_t)b * a.max_pages + (to >> a.page_log)], pf = paged_page_lane(a, b, from >> a.page_log);
+    const bool ok = (uint32_t)pt < (uint32_t)a.n_pages && j0 + (lane & (MOVES - 1)) < n_moves;
+    if (lane < MOVES && j0 + lane < n_moves) {
+      if (e.src) e.src[(int64_t)pair * e.budget + to] = from;
+      if (ok) {
+        const int64_t x = (((int64_t)pt * a.h_kv + h) << a.page_log) + (to & pm), y = (((int64_t)pf * a.h_kv + h) << a.page_log) + (from & pm);
+        const float w = a.weights[y];
+        const int p = a.pos[y];
+        a.weights[x] = w;
+        a.pos[x] = p;
+      }
+    }
+    constexpr int N = MOVES / PER;
+    u32x4 kw[N], vw[N];
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const int m = i * PER + lane / C, f = __shfl(from, m), g = __shfl(pf, m);
+      kw[i] = reinterpret_cast<const u32x4*>(kb + ((int64_t)g * a.kp_p + (int64_t)(f & pm) * a.kp_t) * ES)[c];
+      vw[i] = reinterpret_cast<const u32x4*>(vb + ((int64_t)g * a.vp_p + (int64_t)(f & pm) * a.vp_t) * ES)[c];
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+      const int m = i * PER + lane / C, t = __shfl(to, m), g = __shfl(pt, m);
+      if (__shfl((int)ok, m)) {
+        reinterpret_cast<u32x4*>(kb + ((int64_t)g * a.kp_p + (int64_t)(t & pm) * a.kp_t) * ES)[c] = kw[i];
+        reinterpret_cast<u32x4*>(vb + ((int64_t)g * a.vp_p + (int64_t)(t & pm) * a.vp_t) * ES)[c] = vw[i];
+      }
     }
   }
 }

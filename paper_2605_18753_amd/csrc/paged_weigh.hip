@@ -51,9 +51,9 @@ template <typename T> constexpr int kWeighKeys = sizeof(T) == 2 ? 256 : 128;   /
 // The work of a kv-head: items (blocks of keys) times the row tiles of their sequence, one after the other, dealt in equal runs
 // [w F / G, (w + 1) F / G) to G workgroups.
 struct WeighSeq { int items, tiles, x0; };                 // blocks of keys, row tiles each, the first of these
-template <typename T> __device__ __forceinline__ WeighSeq weigh_seq(const PagedArgs& a, int m, int n) {
+template <int KEYS> __device__ __forceinline__ WeighSeq weigh_seq(const PagedArgs& a, int m, int n) {
   const int Tt = 16 / a.g, x0 = (a.last > 0 ? max(m - a.last, 0) : 0) / Tt;
-  return {m > 0 ? (n + kWeighKeys<T> - 1) / kWeighKeys<T> : 0, (m + Tt - 1) / Tt - x0, x0};
+  return {m > 0 ? (n + KEYS - 1) / KEYS : 0, (m + Tt - 1) / Tt - x0, x0};
 }
 __device__ __forceinline__ int64_t scan64(int64_t v) {     // inclusive, over the lanes up to one's own
 #pragma unroll
@@ -67,13 +67,13 @@ __device__ __forceinline__ int64_t lane64(int64_t v, int l) {   // lane l's, as 
   return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)((uint64_t)v >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, l));
 }
 // whole: places are items, which are not cut
-template <typename T> __device__ __forceinline__ int64_t weigh_total(const PagedArgs& a, bool whole = false) {
+template <int KEYS> __device__ __forceinline__ int64_t weigh_total(const PagedArgs& a, bool whole = false) {
   const int lane = lane_id();
   int64_t total = 0;
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
     int64_t v = 0;
     if (i0 + lane < a.batch) {
-      const WeighSeq s = weigh_seq<T>(a, paged_rows(a, i0 + lane).y, paged_len(a, i0 + lane));
+      const WeighSeq s = weigh_seq<KEYS>(a, paged_rows(a, i0 + lane).y, paged_len(a, i0 + lane));
       v = whole ? s.items : (int64_t)s.items * s.tiles;
     }
     total += lane64(scan64(v), 63);
@@ -82,7 +82,7 @@ template <typename T> __device__ __forceinline__ int64_t weigh_total(const Paged
 }
 struct WeighItem { int b, block, x, r0, m, n; WeighSeq s; };   // x: row tiles of the item before the place
 // the item at place f < weigh_total
-template <typename T> __device__ __forceinline__ void weigh_find(const PagedArgs& a, int64_t f, WeighItem& it, bool whole = false) {
+template <int KEYS> __device__ __forceinline__ void weigh_find(const PagedArgs& a, int64_t f, WeighItem& it, bool whole = false) {
   const int lane = lane_id();
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
     int2 rm = make_int2(0, 0);
@@ -91,7 +91,7 @@ template <typename T> __device__ __forceinline__ void weigh_find(const PagedArgs
     if (i0 + lane < a.batch) {
       rm = paged_rows(a, i0 + lane);
       n = paged_len(a, i0 + lane);
-      s = weigh_seq<T>(a, rm.y, n);
+      s = weigh_seq<KEYS>(a, rm.y, n);
     }
     const int64_t v = whole ? s.items : (int64_t)s.items * s.tiles, incl = scan64(v);
     const uint64_t hit = __ballot(incl > f);
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : D == 128 ? 3 : 4) void pa
   constexpr int SUBS = WeighTile<T, D>::SUBS;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv;
-  const int64_t total = weigh_total<T>(a);
+  const int64_t total = weigh_total<kWeighKeys<T>>(a);
   const int64_t f0 = weigh_bound(a, total, wg);
   int64_t todo = weigh_bound(a, total, wg + 1) - f0;
   if (todo <= 0) return;
@@ -128,7 +128,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : D == 128 ? 3 : 4) void pa
   const uint32_t q_lane = (uint32_t)(tl * (int)a.q_t + n % a.g * (int)a.q_h) * (uint32_t)sizeof(T) + kq * 16;
   const uint32_t l_lane = (uint32_t)(tl * a.h_q + n % a.g) * 4u;
   WeighItem it;
-  weigh_find<T>(a, f0, it);
+  weigh_find<kWeighKeys<T>>(a, f0, it);
   while (true) {
     const int key0 = it.block * kWeighKeys<T> + wave * SUBS * 16;
     WeighTile<T, D> kf[SUBS];
@@ -209,7 +209,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : D == 128 ? 3 : 4) void pa
     }
     if ((todo -= take) <= 0) return;
     it.x = 0;
-    if (++it.block >= it.s.items) weigh_find<T>(a, weigh_bound(a, total, wg + 1) - todo, it);
+    if (++it.block >= it.s.items) weigh_find<kWeighKeys<T>>(a, weigh_bound(a, total, wg + 1) - todo, it);
   }
 }
 
@@ -218,10 +218,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : D == 128 ? 3 : 4) void pa
 template <typename T>
 __global__ __launch_bounds__(kWeighKeys<T>) void paged_weigh_sum_kernel(PagedArgs a) {
   const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv + 1;
-  const int64_t total = weigh_total<T>(a), f = weigh_bound(a, total, wg);
+  const int64_t total = weigh_total<kWeighKeys<T>>(a), f = weigh_bound(a, total, wg);
   if (f >= total || f == weigh_bound(a, total, wg - 1)) return;
   WeighItem it;
-  weigh_find<T>(a, f, it);
+  weigh_find<kWeighKeys<T>>(a, f, it);
   const int64_t begin = f - it.x, end = begin + it.s.tiles;
   if (it.x == 0 || weigh_bound(a, total, wg - 1) > begin) return;              // not cut here, or not for the first time
   const float* p = a.part_o + ((int64_t)r * a.wgs + wg - 1) * 2 * kWeighKeys<T> + threadIdx.x;
@@ -240,26 +240,27 @@ __global__ __launch_bounds__(kWeighKeys<T>) void paged_weigh_sum_kernel(PagedArg
 
 // Few rows a sequence (decode): K is streamed once, the next block's keys asked for before the present one's are used.  Whole blocks
 // only, in equal runs.
+constexpr int kStreamSubs = 1;
 template <int D>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void paged_weigh_stream_kernel(PagedArgs a) {
+__global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a) {
   using T = uint16_t;
   using Tile = WeighTile<T, D>;
-  constexpr int SUBS = Tile::SUBS;
+  constexpr int SUBS = kStreamSubs, KEYS = 64 * SUBS;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv;
   const int Tt = 16 / a.g, n = lane & 15, kq = lane >> 4, pm = (1 << a.page_log) - 1, tl = n / a.g;
   const uint32_t q_lane = (uint32_t)(tl * (int)a.q_t + n % a.g * (int)a.q_h) * 2u + kq * 16;
   const uint32_t l_lane = (uint32_t)(tl * a.h_q + n % a.g) * 4u;
   // blocks of all sequences, and the run's
-  const int64_t total = weigh_total<T>(a, true);
+  const int64_t total = weigh_total<KEYS>(a, true);
   int64_t f = weigh_bound(a, total, wg);
   int todo = (int)(weigh_bound(a, total, wg + 1) - f);
   if (todo <= 0) return;
   WeighItem it, next;
-  weigh_find<T>(a, f, it, true);
+  weigh_find<KEYS>(a, f, it, true);
   auto advance = [&](WeighItem& x) {
     f++;
-    if (++x.block >= x.s.items) weigh_find<T>(a, f, x, true);
+    if (++x.block >= x.s.items) weigh_find<KEYS>(a, f, x, true);
   };
   // lane (n, kq), n < 4, takes key 4 kq + n of 16 (the others, and those behind the end, some key of the page)
   auto place = [&](const WeighItem& x, int page, int key16) {
@@ -267,7 +268,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void paged_weigh_stream_kern
   };
   // A block's keys, and what its keys weigh so far: asked for behind the keys of the next block, that would be waited for with them.
   auto load_keys = [&](const WeighItem& x, Tile (&kf)[SUBS], int (&page)[SUBS], float (&was)[SUBS]) {
-    const int key0 = x.block * kWeighKeys<T> + wave * SUBS * 16;
+    const int key0 = x.block * KEYS + wave * SUBS * 16;
 #pragma unroll
     for (int s = 0; s < SUBS; s++) page[s] = paged_entry(a, x.b, min(key0 + 16 * s, (x.n - 1) & ~15) >> a.page_log);
 #pragma unroll
@@ -295,7 +296,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void paged_weigh_stream_kern
     }
   };
   auto work = [&](const WeighItem& x, const Tile (&kf)[SUBS], const int (&page)[SUBS], const float (&was)[SUBS]) {
-    const int key0 = x.block * kWeighKeys<T> + wave * SUBS * 16, back = x.n - x.m;
+    const int key0 = x.block * KEYS + wave * SUBS * 16, back = x.n - x.m;
     f32x4 acc[SUBS];
 #pragma unroll
     for (int j = 0; j < SUBS; j++) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -364,7 +365,7 @@ template <typename T, int D>
 static hipError_t launch_weigh_t(PagedArgs a, char* ws, hipStream_t st) {
   if constexpr (sizeof(T) == 2) {
     if (weigh_stream(a)) {
-      a.wgs = max((D == 128 ? 512 : 768) / a.h_kv, 1);
+      a.wgs = max(1024 / a.h_kv, 1);
       hipLaunchKernelGGL(paged_weigh_stream_kernel<D>, dim3((unsigned)(a.wgs * a.h_kv)), dim3(256), 0, st, a);
       return hipGetLastError();
     }
