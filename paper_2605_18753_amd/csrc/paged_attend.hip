@@ -335,10 +335,12 @@ template <int D> struct RowsCfg {
   static constexpr int TILE_BYTES = 64 * ROW_BYTES;
   static constexpr int COPIES = TILE_BYTES / 4096;       // copy instructions of a wave per tile and tensor
   static constexpr int RPC = 256 / NCH, RPW = RPC / 4;   // rows that the workgroup's, and a wave's, copy instruction covers
-  static constexpr int LDS_BYTES = 4 * TILE_BYTES;       // K ring [2], V ring [2]
+  static constexpr int OUT_BYTES = 128 * (D + 4) * 4;    // a tile's rows in fp32, behind the walk
+  static constexpr int LDS_BYTES = 4 * TILE_BYTES > OUT_BYTES ? 4 * TILE_BYTES : OUT_BYTES;   // K ring [2], V ring [2]
 };
 
-template <int D>
+// SMALL: pages of fewer than 64 tokens, several to a tile.
+template <int D, bool SMALL>
 __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
   using C = RowsCfg<D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -381,25 +383,39 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
   const int c_x = lane / C::NCH, c_pos = lane % C::NCH, c_row = wave * C::RPW + c_x;
   const uint32_t k_off = (uint32_t)c_x * kt2 + (uint32_t)((c_pos ^ pk_swz<D>(c_row)) << 4);
   const uint32_t v_off = (uint32_t)c_x * vt2 + (uint32_t)((c_pos ^ pv_swz<D>(c_row)) << 4);
-  // Rows [key, key + RPW) of page id: a resource of their own, which ends with the sequence's last token (rows behind it read as zeros,
-  // whatever the page holds)
-  auto copy = [&](const char* base, int64_t page_bytes, uint32_t row_bytes, uint32_t off, int id, int key, int stop, uint32_t to) {
-    const int left = min(max(stop - key, 0), C::RPW);
-    const char* p = base + (int64_t)id * page_bytes + (uint32_t)(key & pm) * row_bytes;
-    copy16_to_lds(make_rsrc(p, left ? (int64_t)(left - 1) * row_bytes + C::ROW_BYTES : 0), to, off, 0);
+  // Rows [key, key + RPW) of page id onwards, up to key `stop` of the sequence: behind it a resource ends, and the rows read as
+  // zeros, whatever the page holds.  A tile in one page has one resource for all copies, otherwise each copy has its own.
+  auto rows_from = [&](const char* base, int64_t page_bytes, uint32_t row_bytes, int id, int key, int stop, int most) {
+    const int left = min(max(stop - key, 0), most);
+    const int64_t bytes = (int64_t)left * row_bytes - (int64_t)(row_bytes - C::ROW_BYTES);
+    return make_rsrc(base + (int64_t)id * page_bytes + (uint32_t)(key & pm) * row_bytes, bytes < 0 ? 0 : bytes);
   };
-  int id_v[C::COPIES], id_k[C::COPIES];                       // pages of tile i (its V is copied) and of tile i + 1 (its K)
-  auto ids_of = [&](int tile, int (&id)[C::COPIES]) {
+  constexpr int NID = SMALL ? C::COPIES : 1;
+  int id_v[NID], id_k[NID];                                   // pages of tile i (its V is copied) and of tile i + 1 (its K)
+  u32x4 k_rs = {}, v_rs = {};
+  auto ids_of = [&](int tile, int (&id)[NID]) {
 #pragma unroll
-    for (int c = 0; c < C::COPIES; c++)
-      id[c] = __builtin_amdgcn_readlane(win, (((tile * 64 + c * C::RPC + wave * C::RPW) >> a.page_log) - wbase) & 63);
+    for (int c = 0; c < NID; c++)
+      id[c] = __builtin_amdgcn_readlane(win, (((tile * 64 + (SMALL ? c * C::RPC + wave * C::RPW : 0)) >> a.page_log) - wbase) & 63);
   };
-  auto copy_k = [&](int tile, int c, int slot) {              // behind the part's last tile: nothing is read
-    const int stop = tile < first + n_it ? it.n : 0;
-    copy(kb, kp2, kt2, k_off, id_k[c], tile * 64 + c * C::RPC + wave * C::RPW, stop, lds0 + slot * C::TILE_BYTES + c * 4096 + wave * 1024);
+  const int part_end = first + n_it;
+  auto aim_k = [&](int tile) {                                // behind the part's last tile: nothing is read
+    if constexpr (!SMALL) k_rs = rows_from(kb, kp2, kt2, id_k[0], tile * 64 + wave * C::RPW, tile < part_end ? it.n : 0, 64 - wave * C::RPW);
+  };
+  auto aim_v = [&](int tile) {
+    if constexpr (!SMALL) v_rs = rows_from(vb, vp2, vt2, id_v[0], tile * 64 + wave * C::RPW, it.n, 64 - wave * C::RPW);
+  };
+  auto copy_k = [&](int tile, int c, int slot) {
+    const uint32_t to = lds0 + slot * C::TILE_BYTES + c * 4096 + wave * 1024;
+    if constexpr (SMALL)
+      copy16_to_lds(rows_from(kb, kp2, kt2, id_k[c], tile * 64 + c * C::RPC + wave * C::RPW, tile < part_end ? it.n : 0, C::RPW), to, k_off, 0);
+    else
+      copy16_to_lds(k_rs, to, k_off, (uint32_t)(c * C::RPC) * kt2);
   };
   auto copy_v = [&](int tile, int c, int slot) {
-    copy(vb, vp2, vt2, v_off, id_v[c], tile * 64 + c * C::RPC + wave * C::RPW, it.n, lds0 + (2 + slot) * C::TILE_BYTES + c * 4096 + wave * 1024);
+    const uint32_t to = lds0 + (2 + slot) * C::TILE_BYTES + c * 4096 + wave * 1024;
+    if constexpr (SMALL) copy16_to_lds(rows_from(vb, vp2, vt2, id_v[c], tile * 64 + c * C::RPC + wave * C::RPW, it.n, C::RPW), to, v_off, 0);
+    else copy16_to_lds(v_rs, to, v_off, (uint32_t)(c * C::RPC) * vt2);
   };
   // ---- operand addresses in LDS, of slot 0 --------------------------------------------------------------------
   uint32_t k_rd[D / 16], v_rd[D / 32];
@@ -423,6 +439,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
   for (int ks = 0; ks < D / 16; ks++) asm volatile("" : "+v"(qf[ks]));
   asm volatile("" : "+v"(win), "+v"(win_next));
   ids_of(first, id_k);
+  aim_k(first);
   if (n_it > 0) {
 #pragma unroll
     for (int c = 0; c < C::COPIES; c++) copy_k(first, c, 0);
@@ -441,13 +458,15 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     asm volatile("" : "+v"(win_next));                         // asked for iterations ago
 #pragma unroll
-    for (int c = 0; c < C::COPIES; c++) id_v[c] = id_k[c];
+    for (int c = 0; c < NID; c++) id_v[c] = id_k[c];
     if (((tile + 1) * 64 >> a.page_log) - wbase >= 64) {
       wbase += 64;
       win = win_next;
       win_next = window(wbase + 64);
     }
     ids_of(tile + 1, id_k);
+    aim_k(tile + 1);
+    aim_v(tile);
     if (pend && __builtin_expect(__any(tmax_old > m_run + kPagedLazy), 0)) {
       const float m_new = fmaxf(m_run, fmaxf(tmax_old, __shfl_xor(tmax_old, 32)));
       const float use = m_new == -INFINITY ? 0.f : m_new;
@@ -578,33 +597,40 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // no copy outlives the workgroup's LDS
   const float l_tot = l_run + __shfl_xor(l_run, 32);
-  if (!row_ok) return;
-  if (it.parts > 1) {
-    // record: O^T unnormalised as [d / 4][row][4], maximum and sum per row
-    const int64_t rec = (int64_t)r * a.part_stride + it.rec0 + it.part;
-    const int row = wave * 32 + n;
-    f32x4* po = reinterpret_cast<f32x4*>(a.part_o) + rec * (D / 4) * 128 + row;
-#pragma unroll
-    for (int dt = 0; dt < NDT; dt++)
-#pragma unroll
-      for (int q4 = 0; q4 < 4; q4++)
-        po[(dt * 8 + q4 * 2 + h) * 128] = f32x4{oacc[dt][q4 * 4], oacc[dt][q4 * 4 + 1], oacc[dt][q4 * 4 + 2], oacc[dt][q4 * 4 + 3]};
-    if (h == 0) reinterpret_cast<float2*>(a.part_ml)[rec * 128 + row] = make_float2(m_run, l_tot);
-    return;
-  }
-  const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot == 0.f ? 0.f : l_tot;
-  uint16_t* op = (uint16_t*)a.o + (it.r0 + t) * a.o_t + head * a.o_h + h * 4;
+  // The rows go through LDS, each wave's on its own, so that they are written in whole lines: as the output, or unnormalised as a
+  // record of the part.
+  constexpr int LD = D + 4;
+  const bool cut = it.parts > 1;
+  const int64_t rec = (int64_t)r * a.part_stride + it.rec0 + it.part;
+  const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot == 0.f ? 0.f : l_tot;    // NaN stays
+  __syncthreads();                                             // nobody reads the tiles any more
+  float* x = reinterpret_cast<float*>(lds) + wave * 32 * LD;
 #pragma unroll
   for (int dt = 0; dt < NDT; dt++)
 #pragma unroll
     for (int q4 = 0; q4 < 4; q4++)
-      put_row4(op + dt * 32 + q4 * 8, f32x4{oacc[dt][q4 * 4], oacc[dt][q4 * 4 + 1], oacc[dt][q4 * 4 + 2], oacc[dt][q4 * 4 + 3]}, inv);
-  if (a.lse && h == 0) a.lse[(int64_t)(it.r0 + t) * a.h_q + head] = l_tot == 0.f ? -INFINITY : (m_run + log2f(l_tot)) * kLn2;
+      *reinterpret_cast<f32x4*>(x + n * LD + dt * 32 + q4 * 8 + h * 4) =
+          f32x4{oacc[dt][q4 * 4], oacc[dt][q4 * 4 + 1], oacc[dt][q4 * 4 + 2], oacc[dt][q4 * 4 + 3]};
+  if (h == 0) {
+    x[n * LD + D] = inv;
+    if (row_ok) {
+      if (cut) reinterpret_cast<float2*>(a.part_ml)[rec * 128 + wave * 32 + n] = make_float2(m_run, l_tot);
+      else if (a.lse) a.lse[(int64_t)(it.r0 + t) * a.h_q + head] = l_tot == 0.f ? -INFINITY : (m_run + log2f(l_tot)) * kLn2;
+    }
+  }
+  asm volatile("" ::: "memory");                               // a wave's LDS operations complete in order
+  constexpr int TPR = D / 4;
+  const int c = lane % TPR, rows = min(max(it.m - tw0, 0), Tw) * a.g;
+  for (int i = lane / TPR; i < rows; i += 64 / TPR) {
+    const f32x4 y = *reinterpret_cast<const f32x4*>(x + i * LD + c * 4);
+    if (cut) *reinterpret_cast<f32x4*>(a.part_o + (rec * 128 + wave * 32 + i) * D + c * 4) = y;
+    else put_row4((uint16_t*)a.o + (it.r0 + tw0 + i / a.g) * a.o_t + (r * a.g + i % a.g) * a.o_h + c * 4, y, x[i * LD + D]);
+  }
 }
 
 // Adds the parts of cut items: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  A workgroup adds 256 / (D / 4) / SLICES (token, head)
-// rows: D / 4 threads a row, 4 values each, in SLICES groups that take every SLICES-th part.  ROWS: of a tile (16 or 128), whose
-// records are laid out accordingly.
+// rows: D / 4 threads a row, 4 values each, in SLICES groups that take every SLICES-th part.  ROWS: of a tile, 16 or
+// 128.
 template <typename T, int D, int ROWS, int SLICES>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
   constexpr int TPR = D / 4, PER = 256 / TPR / SLICES;     // threads of a row's slice, rows of a workgroup
@@ -650,7 +676,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
     M = row16_reduce(M, OpMax());
     if constexpr (TPR == 32) M = fmaxf(M, __shfl_xor(M, 16));
     const float use = M == -INFINITY ? 0.f : M;
-    const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o) + (ROWS == 16 ? (rec * ROWS + in) * (D / 4) + c : (rec * (D / 4) + c) * ROWS + in);
+    const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o) + (rec * ROWS + in) * (D / 4) + c;
 #pragma unroll 8
     for (int p = slice; p < parts; p += SLICES) {
       const float2 y = ml[p * ROWS];
@@ -719,9 +745,11 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
   a.part_o = (float*)(ws + ws_align((size_t)a.wgs * a.h_kv * rows * 8));
   const dim3 grid((unsigned)((a.wgs ? a.wgs : items) * a.h_kv)), blk(256);
   if (big) {
-    static LdsOptIn opt_in;
-    if (hipError_t e = allow_dyn_lds((const void*)paged_rows_kernel<D>, RowsCfg<D>::LDS_BYTES, opt_in); e != hipSuccess) return e;
-    hipLaunchKernelGGL(paged_rows_kernel<D>, grid, blk, RowsCfg<D>::LDS_BYTES, st, a);
+    static LdsOptIn opt_in[2];
+    const bool small = a.page_log < 6;
+    auto kern = small ? paged_rows_kernel<D, true> : paged_rows_kernel<D, false>;
+    if (hipError_t e = allow_dyn_lds((const void*)kern, RowsCfg<D>::LDS_BYTES, opt_in[small]); e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, grid, blk, RowsCfg<D>::LDS_BYTES, st, a);
   } else if (dtype == DASH_BF16) {
     static LdsOptIn opt_in;
     if (hipError_t e = allow_dyn_lds((const void*)paged_few_kernel<D>, FewCfg<D>::LDS_BYTES, opt_in); e != hipSuccess) return e;
