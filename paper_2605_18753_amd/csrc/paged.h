@@ -2,10 +2,15 @@
 // launchers each file exports.
 //
 // Dealing.  The host knows the number of packed rows and sequences, not their lengths, which lie on the device.  A launch has
-// a fixed grid; every workgroup finds its own item from row_start and lens (one pass over them, 64 sequences at a time).  An
-// item is a tile of a sequence's rows (attention) or of its keys (weights) of one kv-head; its walk over the other axis is
-// cut into parts where the items alone would leave the chip idle.  With n items of costs c_i and W > n workgroups, parts of
-// S = ceil(sum c_i / (W - n)) give sum ceil(c_i / S) <= W of them.
+// a fixed grid; every workgroup finds its own work from row_start and lens (one pass over them, 64 sequences at a time).  An item of the
+// attention is a tile of a sequence's rows for one kv-head; its cost is the steps of keys that it walks.
+//   Tiles of 16 rows: the steps of all items of a kv-head lie one behind the other, and G workgroups take equal runs
+//   [w F / G, (w + 1) F / G) of them: whatever the lengths, every CU streams as many keys.
+//   Tiles of 128 rows: one item a workgroup; items that leave the chip idle are cut into parts.  With n items of costs c_i and W > n
+//   workgroups, parts of S = ceil(sum c_i / (W - n)) give sum ceil(c_i / S) <= W of them.  (Equal runs for these as well: a run begins anew for every
+//   piece of an item, and most are cut.  1501 tokens beside seven decoding sequences of up to 12k 305 -> 309 us and the records to add
+//   up, 2048 tokens against 32k 995 -> 1088.)
+// Cut items leave records, which a second launch adds up.
 #pragma once
 #include "common.h"
 #include "dash_internal.h"
@@ -21,10 +26,8 @@ struct PagedArgs {
   int batch, h_q, h_kv, g, page_log, n_pages, max_pages, cap, n_rows, causal, last;
   int64_t q_t, q_h, o_t, o_h, kn_t, kn_h, vn_t, vn_h, kp_p, kp_h, kp_t, vp_p, vp_h, vp_t;
   float c1;                              // scale * log2(e)
-  int wgs;                               // workgroups of a kv-head that items may be cut for; 0: none is cut
-  int min_part;                          // smallest part
-  float* part_o; float* part_ml;         // records of cut items: [kv-head][part][row][d], [kv-head][part][row][2]
-  int part_stride;                       // records of a kv-head
+  int wgs;                               // runs of a kv-head; 0: an item a workgroup.  Tiles of 128 rows: parts of a kv-head at most; 0: none is cut
+  float* part_o; float* part_ml;         // records of cut items: two of each run (the item it begins in, the one it ends in), one of each part
 };
 
 __device__ __forceinline__ int paged_len(const PagedArgs& a, int b) { return min(max(a.lens[b], 0), a.cap); }
@@ -46,9 +49,11 @@ __device__ __forceinline__ int paged_page_lane(const PagedArgs& a, int b, int i)
   return paged_clamp(a, a.table[(int64_t)b * a.max_pages + min(i, a.max_pages - 1)]);
 }
 
-struct PagedItem { int b, tile, part, parts, rec0, r0, m, n; };   // rec0: the item's first part among those of the kv-head
+// ---- parts (tiles of 128 rows) ----------------------------------------------------------------------------------------
+constexpr int kMinPart = 4;                                // steps a part has at least
+struct PagedPart { int b, tile, part, parts, rec0, r0, m, n; };   // rec0: the item's first part among those of the kv-head
 
-// The size S of a part; a wave's lanes together.
+// The size S of a part; a wave's lanes together.  shape(m, n) gives a sequence's tiles and the cost of one (at least 1).
 template <typename F> __device__ __forceinline__ int paged_part_size(const PagedArgs& a, F&& shape) {
   if (a.wgs <= 0) return 0x3fffffff;
   const int lane = lane_id();
@@ -61,11 +66,11 @@ template <typename F> __device__ __forceinline__ int paged_part_size(const Paged
     cost += wave_sum((float)s.x * (float)s.y);
   }
   if (items >= a.wgs) return 0x3fffffff;
-  return max((int)fminf(cost * 1.0001f / (float)(a.wgs - items), 1e9f) + 1, a.min_part);   // the factor covers the sum's rounding
+  return max((int)fminf(cost * 1.0001f / (float)(a.wgs - items), 1e9f) + 1, kMinPart);   // the factor covers the sum's rounding
 }
 
-// Every lane of a wave: item `idx` of a kv-head.  shape(m, n) gives a sequence's tiles and the cost of one (at least 1).
-template <typename F> __device__ __forceinline__ bool paged_find(const PagedArgs& a, int idx, F&& shape, PagedItem& it) {
+// Every lane of a wave: part `idx` of a kv-head.
+template <typename F> __device__ __forceinline__ bool paged_find_part(const PagedArgs& a, int idx, F&& shape, PagedPart& it) {
   const int lane = lane_id();
   const int S = paged_part_size(a, shape);
   int base = 0;
@@ -98,6 +103,138 @@ template <typename F> __device__ __forceinline__ bool paged_find(const PagedArgs
   }
   return false;
 }
+
+// ---- runs (tiles of 16 rows) ------------------------------------------------------------------------------------------
+// Steps are of 128 keys.  With m new tokens behind `old`, tile t of a causal call, T = 16 / g tokens, walks ceil((old + (t + 1) T) / 128) =
+// ceil((u + t + 1) / k) steps, u = ceil(old / T), k = 128 / T, and the tiles before it H(u + t) - H(u), H(x) = sum of ceil(y / k) over
+// y = 1 .. x.  Runs are used for fewer than 4096 items, of at most 2^17 steps each: 32 bits (H may wrap, its differences do not).
+constexpr int kStep = 128;
+struct PagedSeq { int tiles, u, flat; };                   // flat > 0: steps of every tile (no causal mask)
+struct PagedItem { int b, tile, r0, m, n; PagedSeq s; };
+struct PagedDeal {
+  int T, k_log;                                            // tokens of a tile, log2 of k
+  __device__ __forceinline__ PagedDeal(const PagedArgs& a) : T(16 / a.g), k_log(31 - __builtin_clz(kStep / (16 / a.g))) {}
+  __device__ __forceinline__ PagedSeq seq(const PagedArgs& a, int m, int n) const {
+    return {(m + T - 1) / T, (max(n - m, 0) + T - 1) / T, a.causal ? 0 : max((n + kStep - 1) / kStep, 1)};
+  }
+  __device__ __forceinline__ uint32_t h(int x) const {
+    const uint32_t c = (uint32_t)x >> k_log, r = (uint32_t)x & ((1u << k_log) - 1u);
+    return ((c & 1 ? c * ((c + 1) / 2) : (c / 2) * (c + 1)) << k_log) + (c + 1) * r;
+  }
+  __device__ __forceinline__ int before(const PagedSeq& s, int t) const { return s.flat ? s.flat * t : (int)(h(s.u + t) - h(s.u)); }
+  __device__ __forceinline__ int steps(const PagedSeq& s, int t) const { return s.flat ? s.flat : ((s.u + t) >> k_log) + 1; }
+  // the steps of all items of a kv-head; a wave's lanes together
+  __device__ __forceinline__ int total(const PagedArgs& a) const {
+    int f = 0;
+    for (int i0 = 0; i0 < a.batch; i0 += 64) {
+      int v = 0;
+      if (i0 + (int)lane_id() < a.batch) {
+        const PagedSeq s = seq(a, paged_rows(a, i0 + lane_id()).y, paged_len(a, i0 + lane_id()));
+        v = before(s, s.tiles);
+      }
+      f += __builtin_amdgcn_readlane(wave_scan(v), 63);
+    }
+    return f;
+  }
+  // the item at step f (by_steps), or item number f; returns the steps of the item before f, -1 where there is none
+  __device__ __forceinline__ int find(const PagedArgs& a, int f, bool by_steps, PagedItem& it) const {
+    const int lane = lane_id();
+    for (int i0 = 0; i0 < a.batch; i0 += 64) {
+      int2 rm = make_int2(0, 0);
+      int n = 0;
+      PagedSeq s = {0, 0, 0};
+      if (i0 + lane < a.batch) {
+        rm = paged_rows(a, i0 + lane);
+        n = paged_len(a, i0 + lane);
+        s = seq(a, rm.y, n);
+      }
+      const int v = by_steps ? before(s, s.tiles) : s.tiles, incl = wave_scan(v);
+      const uint64_t hit = __ballot(incl > f);
+      if (hit) {
+        const int l = __builtin_ctzll(hit);
+        it.b = i0 + l;
+        it.r0 = __builtin_amdgcn_readlane(rm.x, l);
+        it.m = __builtin_amdgcn_readlane(rm.y, l);
+        it.n = __builtin_amdgcn_readlane(n, l);
+        it.s = {__builtin_amdgcn_readlane(s.tiles, l), __builtin_amdgcn_readlane(s.u, l), __builtin_amdgcn_readlane(s.flat, l)};
+        const int in = f - __builtin_amdgcn_readlane(incl - v, l);
+        if (!by_steps) {
+          it.tile = it.s.tiles - 1 - in;                   // the last tiles first: of a causal prompt they are the longest
+          return 0;
+        }
+        int lo = 0, hi = it.s.tiles;                       // before(lo) <= in < before(hi)
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (before(it.s, mid) <= in) lo = mid;
+          else hi = mid;
+        }
+        it.tile = lo;
+        return in - before(it.s, lo);
+      }
+      f -= __builtin_amdgcn_readlane(incl, 63);
+    }
+    return -1;
+  }
+};
+
+// Where run w of G <= 1024 begins: floor(w F / G), the fraction's part in floats (a numerator below 2^20 and a half, whose quotient is
+// nearer than 2^-12 to exact and not nearer than 2^-11 to a whole number).
+struct PagedBounds {
+  uint32_t q, rem; float inv;
+  __device__ __forceinline__ PagedBounds(const PagedArgs& a, int total)
+      : q((uint32_t)total / (uint32_t)a.wgs), rem((uint32_t)total % (uint32_t)a.wgs), inv(1.f / (float)a.wgs) {}
+  __device__ __forceinline__ int at(int w) const { return (int)(q * (uint32_t)w + (uint32_t)(((float)(rem * (uint32_t)w) + 0.5f) * inv)); }
+};
+
+// The kernel's arguments (its first and only parameter) and thread index, asked for anew: what follows from them is not kept in registers
+// from piece to piece, for which the walks have none left.
+__device__ __forceinline__ PagedArgs paged_reload() {
+  auto p = (const __attribute__((address_space(4))) PagedArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const PagedArgs*)p;
+}
+__device__ __forceinline__ int paged_thread() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
+// A workgroup's pieces of items, one after the other: steps [x0, x1) of item `it`.
+struct PagedRun {
+  PagedDeal deal;
+  PagedItem it;
+  int x0, x1, cost;
+  int next, end;                                           // the step behind this piece, the run's end
+  __device__ __forceinline__ PagedRun(const PagedArgs& a) : deal(a) {}
+  __device__ __forceinline__ bool begin(const PagedArgs& a, int wg) {
+    if (a.wgs == 0) {
+      if (deal.find(a, wg, false, it) < 0) return false;
+      x0 = next = end = 0;
+      x1 = cost = deal.steps(it.s, it.tile);
+      return true;
+    }
+    const PagedBounds b(a, deal.total(a));
+    next = __builtin_amdgcn_readfirstlane(b.at(wg));
+    end = __builtin_amdgcn_readfirstlane(b.at(wg + 1));
+    if (next >= end) return false;
+    x0 = deal.find(a, next, true, it);
+    cost = deal.steps(it.s, it.tile);
+    return piece();
+  }
+  __device__ __forceinline__ bool piece() {
+    x1 = min(cost, x0 + end - next);
+    next += x1 - x0;
+    return true;
+  }
+  __device__ __forceinline__ bool advance(const PagedArgs& a) {
+    if (next >= end) return false;
+    x0 = 0;
+    if (++it.tile >= it.s.tiles) deal.find(a, next, true, it);
+    cost = deal.steps(it.s, it.tile);
+    return piece();
+  }
+  __device__ __forceinline__ bool whole() const { return x0 == 0 && x1 == cost; }
+};
 
 hipError_t launch_paged_append(const PagedArgs& a, int elem, int d, hipStream_t st);
 hipError_t launch_paged_attend(const PagedArgs& a, int dtype, int d, char* ws, hipStream_t st);

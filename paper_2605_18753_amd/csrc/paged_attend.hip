@@ -24,14 +24,8 @@ template <int D> __device__ __forceinline__ int pk_swz(int row) { return D == 12
 template <int D> __device__ __forceinline__ int pv_swz(int row) { return D == 128 ? ((row & 3) << 2) : (((row >> 1) & 1) << 2); }
 
 // a row's last visible slot, -1: none
-__device__ __forceinline__ int paged_last_key(const PagedArgs& a, const PagedItem& it, int t) {
+template <typename I> __device__ __forceinline__ int paged_last_key(const PagedArgs& a, const I& it, int t) {
   return a.causal ? min(it.n - it.m + t, it.n - 1) : it.n - 1;
-}
-
-// tiles of ROWS rows of a sequence; cost: steps of 128 keys (16 rows), or of 64
-template <int ROWS> __device__ __forceinline__ int2 tile_shape(const PagedArgs& a, int m, int n) {
-  const int T = ROWS / a.g;
-  return make_int2((m + T - 1) / T, max(ROWS == 16 ? (n + 127) >> 7 : (n + 63) >> 6, 1));
 }
 
 // 4 values of an output row
@@ -55,7 +49,8 @@ template <int D> struct FewCfg {
 // What the four waves hold of a tile's 16 rows is added up in LDS, and written as the output or as a record of the part.
 // x: [4][16][D + 4] floats, ml: [4][16][2] behind it.  Threads 16 i .. + 15 hold row i.
 template <typename T, int D>
-__device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const PagedItem& it, int r, int t0, const float* x, const float* ml) {
+__device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const PagedRun& run, int r, int64_t rec, int t0, const float* x, const float* ml) {
+  const PagedItem& it = run.it;
   const int row = threadIdx.x >> 4, c = threadIdx.x & 15;
   float M = -INFINITY, den = 0.f, w[4];
 #pragma unroll
@@ -79,8 +74,7 @@ __device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const Paged
 #pragma unroll
     for (int e = 0; e < 4; e++) o[j * 4 + e] = s[e];
   }
-  if (it.parts > 1) {
-    const int64_t rec = (int64_t)r * a.part_stride + it.rec0 + it.part;
+  if (!run.whole()) {
     float* po = a.part_o + (rec * 16 + row) * D;
 #pragma unroll
     for (int j = 0; j < D / 64; j++) *reinterpret_cast<f32x4*>(po + j * 64 + c * 4) = f32x4{o[j * 4], o[j * 4 + 1], o[j * 4 + 2], o[j * 4 + 3]};
@@ -99,14 +93,18 @@ __device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const Paged
 
 
 template <int D>
-__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void paged_few_kernel(PagedArgs a) {
+__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void paged_few_kernel(PagedArgs args) {
   using C = FewCfg<D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = blockIdx.x % a.h_kv;
-  PagedItem it;
-  if (!paged_find(a, blockIdx.x / a.h_kv, [&](int m, int n) { return tile_shape<16>(a, m, n); }, it)) return;
-  const int T = 16 / a.g, t0 = it.tile * T;
+  const int r = blockIdx.x % args.h_kv, wg = blockIdx.x / args.h_kv;
+  PagedRun run(args);
+  if (!run.begin(args, wg)) return;
+  const PagedItem& it = run.it;
+  do {
+  const PagedArgs a = paged_reload();
+  const int tid = paged_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int T = 16 / a.g;
+  const int t0 = it.tile * T;
   const int n = lane & 15, kq = lane >> 4;
   const int t = t0 + n / a.g;
   const bool row_ok = t < it.m;
@@ -119,10 +117,9 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void paged_few_kernel(PagedA
   const int last = row_ok ? paged_last_key(a, it, t) : -1;
   const int first_last = paged_last_key(a, it, t0);                              // of the tile's first token
   const int end = max(paged_last_key(a, it, min(t0 + T, it.m) - 1) + 1, 0);      // keys that a row of the tile sees
-  // this part's 128-key steps; the wave's 32-key tiles among them
-  const int steps = (end + 127) >> 7, per = (steps + it.parts - 1) / it.parts;
-  const int j1 = min((it.part + 1) * per * 4, (end + 31) >> 5);
-  int j = it.part * per * 4 + wave;
+  // the wave's 32-key tiles of the piece's 128-key steps
+  const int j1 = min(run.x1 * 4, (end + 31) >> 5);
+  int j = run.x0 * 4 + wave;
 
   const uint32_t ring = lds_addr_of(lds) + wave * C::WAVE_BYTES;
   const int c_row = lane / C::NCH, c_pos = lane % C::NCH;
@@ -246,27 +243,32 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void paged_few_kernel(PagedA
     ml[(wave * 16 + n) * 2 + 1] = l_tot;
   }
   __syncthreads();
-  paged_few_finish<uint16_t, D>(a, it, r, t0, x, ml);
+  paged_few_finish<uint16_t, D>(a, run, r, ((int64_t)r * a.wgs + wg) * 2 + (run.x0 == 0), t0, x, ml);
+  __syncthreads();
+  } while (run.advance(args));
 }
 
 // fp32: the same walk with the fp32 matrix cores, operands straight from the pages, 16 keys at a time.  A token's NaN or infinity
 // reaches the rows that see it and no other.
 template <int D>
-__global__ __launch_bounds__(256) void paged_few_f32_kernel(PagedArgs a) {
+__global__ __launch_bounds__(256) void paged_few_f32_kernel(PagedArgs args) {
   __shared__ __attribute__((aligned(16))) float x[4 * 16 * (D + 4) + 4 * 16 * 2];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int r = blockIdx.x % a.h_kv;
-  PagedItem it;
-  if (!paged_find(a, blockIdx.x / a.h_kv, [&](int m, int n) { return tile_shape<16>(a, m, n); }, it)) return;
-  const int T = 16 / a.g, t0 = it.tile * T;
+  const int r = blockIdx.x % args.h_kv, wg = blockIdx.x / args.h_kv;
+  PagedRun run(args);
+  if (!run.begin(args, wg)) return;
+  const PagedItem& it = run.it;
+  do {
+  const PagedArgs a = paged_reload();
+  const int tid = paged_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int T = 16 / a.g;
+  const int t0 = it.tile * T;
   const int n = lane & 15, kq = lane >> 4;
   const int t = t0 + n / a.g;
   f32x4 qv[D / 16];
   load_row<D>((const float*)a.q + (it.r0 + min(t, it.m - 1)) * a.q_t + (r * a.g + n % a.g) * a.q_h, kq, qv);
   const int last = t < it.m ? paged_last_key(a, it, t) : -1;
   const int end = max(paged_last_key(a, it, min(t0 + T, it.m) - 1) + 1, 0);
-  const int steps = (end + 127) >> 7, per = (steps + it.parts - 1) / it.parts;
-  const int j0 = it.part * per * 8 + wave, j1 = min((it.part + 1) * per * 8, (end + 15) >> 4);   // 16-key tiles
+  const int j0 = run.x0 * 8 + wave, j1 = min(run.x1 * 8, (end + 15) >> 4);       // 16-key tiles
   const int pm = (1 << a.page_log) - 1;
   const float* kb = (const float*)a.k + r * a.kp_h;
   const float* vb = (const float*)a.v + r * a.vp_h;
@@ -320,7 +322,9 @@ __global__ __launch_bounds__(256) void paged_few_f32_kernel(PagedArgs a) {
     ml[(wave * 16 + n) * 2 + 1] = l_tot;
   }
   __syncthreads();
-  paged_few_finish<float, D>(a, it, r, t0, x, ml);
+  paged_few_finish<float, D>(a, run, r, ((int64_t)r * a.wgs + wg) * 2 + (run.x0 == 0), t0, x, ml);
+  __syncthreads();
+  } while (run.advance(args));
 }
 
 // Many rows (pieces of prompts): a tile is 128 (token, head) rows, 32 of them a wave's: all heads of the group for 32 / g tokens.
@@ -339,6 +343,12 @@ template <int D> struct RowsCfg {
   static constexpr int LDS_BYTES = 4 * TILE_BYTES > OUT_BYTES ? 4 * TILE_BYTES : OUT_BYTES;   // K ring [2], V ring [2]
 };
 
+// tiles of 128 rows of a sequence; cost: their steps of 64 keys
+__device__ __forceinline__ int2 rows_shape(const PagedArgs& a, int m, int n) {
+  const int T = 128 / a.g;
+  return make_int2((m + T - 1) / T, max((n + 63) >> 6, 1));
+}
+
 // SMALL: pages of fewer than 64 tokens, several to a tile.
 template <int D, bool SMALL>
 __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
@@ -348,8 +358,8 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
   const int n = lane & 31, h = lane >> 5;
   // kv-heads are the fast index: with 8 of them each XCD's L2 sees the pages of one
   const int r = blockIdx.x % a.h_kv;
-  PagedItem it;
-  if (!paged_find(a, blockIdx.x / a.h_kv, [&](int m, int n) { return tile_shape<128>(a, m, n); }, it)) return;
+  PagedPart it;
+  if (!paged_find_part(a, blockIdx.x / a.h_kv, [&](int m, int n) { return rows_shape(a, m, n); }, it)) return;
   const int T = 128 / a.g, t0 = it.tile * T, Tw = 32 / a.g, tw0 = t0 + wave * Tw;
   const int t = tw0 + n / a.g, head = r * a.g + n % a.g;
   const bool row_ok = t < it.m;
@@ -601,7 +611,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
   // record of the part.
   constexpr int LD = D + 4;
   const bool cut = it.parts > 1;
-  const int64_t rec = (int64_t)r * a.part_stride + it.rec0 + it.part;
+  const int64_t rec = (int64_t)r * a.wgs + it.rec0 + it.part;
   const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot == 0.f ? 0.f : l_tot;    // NaN stays
   __syncthreads();                                             // nobody reads the tiles any more
   float* x = reinterpret_cast<float*>(lds) + wave * 32 * LD;
@@ -628,81 +638,160 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
   }
 }
 
-// Adds the parts of cut items: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  A workgroup adds 256 / (D / 4) / SLICES (token, head)
-// rows: D / 4 threads a row, 4 values each, in SLICES groups that take every SLICES-th part.  ROWS: of a tile, 16 or
-// 128.
-template <typename T, int D, int ROWS, int SLICES>
+// Adds up items cut between runs: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  The begin of run w lies inside an item whose first
+// piece is run w - 1's (its second record); the pieces of the runs behind it that begin inside the item follow (their first records).
+// D / 4 threads a row, 4 values each, and where the item has few rows several groups of threads that take every so manieth piece.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
+  constexpr int TPR = D / 4, UNITS = 256 / TPR;            // threads of a row; rows at a time
+  __shared__ f32x4 xo[256];
+  __shared__ float xd[UNITS];
+  const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv + 1, lane = threadIdx.x & 63;
+  const PagedDeal deal(a);
+  const int total = deal.total(a);
+  const PagedBounds bounds(a, total);
+  const int f = __builtin_amdgcn_readfirstlane(bounds.at(wg));
+  if (f >= total) return;
+  PagedItem it;
+  const int x = deal.find(a, f, true, it), begin = f - x, end = begin + deal.steps(it.s, it.tile);
+  if (x == 0 || bounds.at(wg - 1) > begin) return;         // not cut here, or not for the first time
+  int pieces = 1;                                          // runs wg - 1 .. wg - 2 + pieces
+  for (int k0 = wg; k0 < a.wgs; k0 += 64) {
+    const int more = __popcll(__ballot(k0 + lane < a.wgs && bounds.at(k0 + lane) < end));
+    pieces += more;
+    if (more < 64) break;
+  }
+  const int64_t rec0 = ((int64_t)r * a.wgs + wg - 1) * 2;
+  // (with fewer steps than runs some runs are empty and wrote no record)
+  const bool holes = bounds.q == 0;
+  auto record = [&](int p) -> int64_t {
+    if (holes && p > 0 && bounds.at(wg - 1 + p) == bounds.at(wg + p)) return -1;
+    return p == 0 ? rec0 + 1 : rec0 + 2 * p;
+  };
+  const int rows = min(deal.T, it.m - it.tile * deal.T) * a.g;
+  const int slices = rows * 4 <= UNITS ? 4 : rows * 2 <= UNITS ? 2 : 1, per = UNITS / slices;
+  const int c = threadIdx.x % TPR, unit = threadIdx.x / TPR, slice = unit / per;
+  for (int i0 = 0; i0 < rows; i0 += per) {
+    const int in = min(i0 + unit % per, rows - 1);
+    const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + in;
+    float M = -INFINITY, den = 0.f;
+    for (int p = c; p < pieces; p += TPR)                  // c-th piece of TPR a thread's
+      if (const int64_t rec = record(p); rec >= 0) M = fmaxf(M, ml[rec * 16].x);
+    M = row16_reduce(M, OpMax());
+    if constexpr (TPR == 32) M = fmaxf(M, __shfl_xor(M, 16));
+    const float use = M == -INFINITY ? 0.f : M;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o) + in * (D / 4) + c;
+#pragma unroll 8
+    for (int p = slice; p < pieces; p += slices) {
+      const int64_t rec = record(p);
+      if (rec < 0) continue;
+      const float2 y = ml[rec * 16];
+      const f32x4 v = po[rec * 16 * (D / 4)];
+      const float w = __builtin_amdgcn_exp2f(y.x - use);
+      den = fmaf(w, y.y, den);
+#pragma unroll
+      for (int e = 0; e < 4; e++) o[e] = fmaf(w, v[e], o[e]);
+    }
+    if (slices > 1) {
+      __syncthreads();
+      xo[threadIdx.x] = o;
+      if (c == 0) xd[unit] = den;
+      __syncthreads();
+      for (int k = 1; k < slices && slice == 0; k++) {
+        o += xo[threadIdx.x + k * per * TPR];
+        den += xd[unit + k * per];
+      }
+    }
+    if (slice > 0 || i0 + unit >= rows) continue;
+    const float inv = den > 0.f ? 1.f / den : den == 0.f ? 0.f : den;
+    const int row = it.r0 + it.tile * deal.T + in / a.g, head = r * a.g + in % a.g;
+    put_row4((T*)a.o + row * a.o_t + head * a.o_h + c * 4, o, inv);
+    if (a.lse && c == 0) a.lse[(int64_t)row * a.h_q + head] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
+  }
+}
+
+// The same for tiles of 128 rows cut into parts.  A workgroup adds 256 / (D / 4) / SLICES (token, head) rows at a time, SLICES groups of threads
+// each taking every SLICES-th part.
+template <int D, int SLICES>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
   constexpr int TPR = D / 4, PER = 256 / TPR / SLICES;     // threads of a row's slice, rows of a workgroup
   __shared__ f32x4 xo[SLICES > 1 ? 256 : 1];
   __shared__ float xd[SLICES > 1 ? 256 / TPR : 1];
   const int lane = threadIdx.x & 63, c = threadIdx.x % TPR, unit = threadIdx.x / TPR, slice = unit / PER;
-  // rows in the order kv-head, token, head of the group: neighbours lie side by side in the records
-  const int64_t per = (int64_t)a.n_rows * a.g, gr = (int64_t)blockIdx.x * PER + unit % PER;
-  const int r = (int)min(gr / per, (int64_t)a.h_kv - 1), row = (int)(gr % per) / a.g, hg = (int)(gr % per) % a.g;
-  // the dealing of the launch before, for a given row
-  const auto shape = [&](int m, int n) { return tile_shape<ROWS>(a, m, n); };
+  const auto shape = [&](int m, int n) { return rows_shape(a, m, n); };
   const int S = paged_part_size(a, shape);
-  int first = 0, parts = 0, tiles = 0, r0 = 0, base = 0;
-  for (int i0 = 0; i0 < a.batch; i0 += 64) {
-    int2 s = make_int2(0, 0), rm = make_int2(0, 0);
-    if (i0 + lane < a.batch) {
-      rm = paged_rows(a, i0 + lane);
-      s = shape(rm.y, paged_len(a, i0 + lane));
-    }
-    const int np = (s.y + S - 1) / S, incl = wave_scan(s.x * np);
+  // rows in the order kv-head, token, head of the group: neighbours lie side by side in the records
+  const int64_t per = (int64_t)a.n_rows * a.g, all = per * a.h_kv;
+  for (int64_t g0 = (int64_t)blockIdx.x * PER; g0 < all; g0 += (int64_t)gridDim.x * PER) {
+    const int64_t gr = min(g0 + unit % PER, all - 1);
+    const int r = (int)(gr / per), row = (int)(gr % per) / a.g, hg = (int)(gr % per) % a.g;
+    // the dealing of the launch before, for a given row
+    int first = 0, parts = 0, tiles = 0, r0 = 0, base = 0;
+    bool any = false;                                      // whether an item of the call is cut
+    for (int i0 = 0; i0 < a.batch; i0 += 64) {
+      int2 s = make_int2(0, 0), rm = make_int2(0, 0);
+      if (i0 + lane < a.batch) {
+        rm = paged_rows(a, i0 + lane);
+        s = shape(rm.y, paged_len(a, i0 + lane));
+      }
+      const int np = (s.y + S - 1) / S, incl = wave_scan(s.x * np);
+      any |= __any(s.x > 0 && np > 1);
 #pragma unroll
-    for (int k = 0; k < 64 / TPR; k++) {
-      const int want = __builtin_amdgcn_readlane(row, k * TPR);
-      const uint64_t hit = __ballot(want >= rm.x && want < rm.x + rm.y);
-      if (hit) {
-        const int l = __builtin_ctzll(hit);
-        const int np_l = __builtin_amdgcn_readlane(np, l), tiles_l = __builtin_amdgcn_readlane(s.x, l);
-        const int first_l = base + __builtin_amdgcn_readlane(incl, l) - tiles_l * np_l, r0_l = __builtin_amdgcn_readlane(rm.x, l);
-        if (lane / TPR == k) { parts = np_l; tiles = tiles_l; first = first_l; r0 = r0_l; }
+      for (int k = 0; k < 64 / TPR; k++) {
+        const int want = __builtin_amdgcn_readlane(row, k * TPR);
+        const uint64_t hit = __ballot(want >= rm.x && want < rm.x + rm.y);
+        if (hit) {
+          const int l = __builtin_ctzll(hit);
+          const int np_l = __builtin_amdgcn_readlane(np, l), tiles_l = __builtin_amdgcn_readlane(s.x, l);
+          const int first_l = base + __builtin_amdgcn_readlane(incl, l) - tiles_l * np_l, r0_l = __builtin_amdgcn_readlane(rm.x, l);
+          if (lane / TPR == k) { parts = np_l; tiles = tiles_l; first = first_l; r0 = r0_l; }
+        }
+      }
+      base += __builtin_amdgcn_readlane(incl, 63);
+    }
+    if (!any) return;
+    const bool mine = parts > 1 && g0 + unit % PER < all;
+    float M = -INFINITY, den = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    if (mine) {
+      const int Tt = 128 / a.g, t = row - r0, tile = t / Tt, in = (t % Tt) * a.g + hg;
+      const int64_t rec = (int64_t)r * a.wgs + first + (tiles - 1 - tile) * parts;
+      const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + rec * 128 + in;
+      // the maximum over all parts, c-th part of TPR a thread's; every slice finds the same
+      for (int p = c; p < parts; p += TPR) M = fmaxf(M, ml[p * 128].x);
+      M = row16_reduce(M, OpMax());
+      if constexpr (TPR == 32) M = fmaxf(M, __shfl_xor(M, 16));
+      const float use = M == -INFINITY ? 0.f : M;
+      const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o) + (rec * 128 + in) * (D / 4) + c;
+#pragma unroll 8
+      for (int p = slice; p < parts; p += SLICES) {
+        const float2 y = ml[p * 128];
+        const float w = __builtin_amdgcn_exp2f(y.x - use);
+        const f32x4 x = po[(int64_t)p * 128 * (D / 4)];
+        den = fmaf(w, y.y, den);
+#pragma unroll
+        for (int e = 0; e < 4; e++) o[e] = fmaf(w, x[e], o[e]);
       }
     }
-    base += __builtin_amdgcn_readlane(incl, 63);
-  }
-  const bool mine = parts > 1 && gr < per * a.h_kv;
-  float M = -INFINITY, den = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  if (mine) {
-    const int Tt = ROWS / a.g, t = row - r0, tile = t / Tt, in = (t % Tt) * a.g + hg;
-    const int64_t rec = (int64_t)r * a.part_stride + first + (tiles - 1 - tile) * parts;
-    const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + rec * ROWS + in;
-    // the maximum over all parts, c-th part of TPR a thread's; every slice finds the same
-    for (int p = c; p < parts; p += TPR) M = fmaxf(M, ml[p * ROWS].x);
-    M = row16_reduce(M, OpMax());
-    if constexpr (TPR == 32) M = fmaxf(M, __shfl_xor(M, 16));
-    const float use = M == -INFINITY ? 0.f : M;
-    const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o) + (rec * ROWS + in) * (D / 4) + c;
-#pragma unroll 8
-    for (int p = slice; p < parts; p += SLICES) {
-      const float2 y = ml[p * ROWS];
-      const float w = __builtin_amdgcn_exp2f(y.x - use);
-      const f32x4 x = po[(int64_t)p * ROWS * (D / 4)];
-      den = fmaf(w, y.y, den);
+    if constexpr (SLICES > 1) {
+      __syncthreads();
+      xo[threadIdx.x] = o;
+      if (c == 0) xd[unit] = den;
+      __syncthreads();
 #pragma unroll
-      for (int e = 0; e < 4; e++) o[e] = fmaf(w, x[e], o[e]);
+      for (int k = 1; k < SLICES; k++) {
+        if (slice > 0) break;
+        o += xo[threadIdx.x + k * PER * TPR];
+        den += xd[unit + k * PER];
+      }
     }
+    if (!mine || slice > 0) continue;
+    const float inv = den > 0.f ? 1.f / den : den == 0.f ? 0.f : den;
+    const int head = r * a.g + hg;
+    put_row4((uint16_t*)a.o + row * a.o_t + head * a.o_h + c * 4, o, inv);
+    if (a.lse && c == 0) a.lse[(int64_t)row * a.h_q + head] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
   }
-  if constexpr (SLICES > 1) {
-    xo[threadIdx.x] = o;
-    if (c == 0) xd[unit] = den;
-    __syncthreads();
-    if (slice > 0) return;
-#pragma unroll
-    for (int k = 1; k < SLICES; k++) {
-      o += xo[threadIdx.x + k * PER * TPR];
-      den += xd[unit + k * PER];
-    }
-  }
-  if (!mine) return;
-  const float inv = den > 0.f ? 1.f / den : den == 0.f ? 0.f : den;
-  const int head = r * a.g + hg;
-  put_row4((T*)a.o + row * a.o_t + head * a.o_h + c * 4, o, inv);
-  if (a.lse && c == 0) a.lse[(int64_t)row * a.h_q + head] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
@@ -712,37 +801,26 @@ static int64_t most_items(const PagedArgs& a, int rows) {   // of a kv-head
   const int T = rows / a.g;
   return min((int64_t)a.n_rows / T + min(a.batch, a.n_rows), (int64_t)a.n_rows);
 }
-// workgroups that are resident at once, for a kv-head: what items are cut for
-static int few_target(const PagedArgs& a) { return max(256 / a.h_kv, 1); }
-static int rows_target(const PagedArgs& a) { return max(512 / a.h_kv, 1); }
+// Workgroups of a kv-head that are resident at once: one a CU for the 128 KB ring of 16-row tiles, two otherwise.
+static int runs_of(const PagedArgs& a, int dtype, int d, bool big) { return max((!big && dtype == DASH_BF16 && d == 128 ? 256 : 512) / a.h_kv, 1); }
 static size_t ws_align(size_t x) { return (x + 255) & ~(size_t)255; }
 
 size_t paged_attend_ws(const PagedArgs& a, int dtype, int d) {
-  const size_t few = (size_t)few_target(a) * a.h_kv * 16, rows = dtype == DASH_BF16 ? (size_t)rows_target(a) * a.h_kv * 128 : 0;
-  const size_t recs = few > rows ? few : rows;              // rows of records
+  const size_t few = (size_t)runs_of(a, dtype, d, false) * a.h_kv * 2 * 16;    // rows of records
+  const size_t rows = dtype == DASH_BF16 ? (size_t)runs_of(a, dtype, d, true) * a.h_kv * 128 : 0, recs = few > rows ? few : rows;
   return ws_align(recs * 8) + recs * d * 4;
-}
-
-// Few rows leave the chip idle unless several groups of threads share a row's parts.
-template <typename T, int D, int ROWS>
-static hipError_t launch_merge(const PagedArgs& a, hipStream_t st) {
-  const int64_t rows = (int64_t)a.n_rows * a.h_q;
-  constexpr int units = 256 / (D / 4), slices = 4, per = units / slices;
-  if (rows <= 8192) hipLaunchKernelGGL((paged_merge_kernel<T, D, ROWS, slices>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((paged_merge_kernel<T, D, ROWS, 1>), dim3((unsigned)((rows + units - 1) / units)), dim3(256), 0, st, a);
-  return hipGetLastError();
 }
 
 template <int D>
 static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st) {
   const bool big = use_rows(a, dtype);
-  const int rows = big ? 128 : 16, target = big ? rows_target(a) : few_target(a);
-  const int64_t items = most_items(a, rows);
-  a.wgs = items < target ? target : 0;
-  a.min_part = big ? 4 : 1;
-  a.part_stride = a.wgs;
+  const int runs = runs_of(a, dtype, D, big);
+  const int64_t items = most_items(a, big ? 128 : 16);
+  // Runs of small tiles cost little (a record is 16 rows) and even out the lengths of a batch; with many items a workgroup each evens them out as well.
+  a.wgs = items < (big ? 1 : 8) * (int64_t)runs ? runs : 0;
+  const size_t recs = (size_t)a.wgs * a.h_kv * (big ? 128 : 2 * 16);
   a.part_ml = (float*)ws;
-  a.part_o = (float*)(ws + ws_align((size_t)a.wgs * a.h_kv * rows * 8));
+  a.part_o = (float*)(ws + ws_align(recs * 8));
   const dim3 grid((unsigned)((a.wgs ? a.wgs : items) * a.h_kv)), blk(256);
   if (big) {
     static LdsOptIn opt_in[2];
@@ -758,9 +836,19 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
     hipLaunchKernelGGL(paged_few_f32_kernel<D>, grid, blk, 0, st, a);
   }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.wgs == 0) return e;
-  if (dtype == DASH_F32) return launch_merge<float, D, 16>(a, st);
-  return big ? launch_merge<uint16_t, D, 128>(a, st) : launch_merge<uint16_t, D, 16>(a, st);
+  if (e != hipSuccess || a.wgs <= 1) return e;
+  if (big) {
+    // few rows leave the chip idle unless several groups of threads share a row's parts
+    const int64_t out = (int64_t)a.n_rows * a.h_q;
+    constexpr int units = 256 / (D / 4);
+    if (out <= 8192) hipLaunchKernelGGL((paged_merge_kernel<D, 4>), dim3((unsigned)((out + units / 4 - 1) / (units / 4))), blk, 0, st, a);
+    else hipLaunchKernelGGL((paged_merge_kernel<D, 1>), dim3(2048), blk, 0, st, a);
+  } else {
+    const dim3 joins((unsigned)((a.wgs - 1) * a.h_kv));
+    if (dtype == DASH_BF16) hipLaunchKernelGGL((paged_join_kernel<uint16_t, D>), joins, blk, 0, st, a);
+    else hipLaunchKernelGGL((paged_join_kernel<float, D>), joins, blk, 0, st, a);
+  }
+  return hipGetLastError();
 }
 
 hipError_t launch_paged_attend(const PagedArgs& a, int dtype, int d, char* ws, hipStream_t st) {
