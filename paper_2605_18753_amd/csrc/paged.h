@@ -177,13 +177,20 @@ struct PagedDeal {
   }
 };
 
-// Where run w of G <= 1024 begins: floor(w F / G), the fraction's part in floats (a numerator below 2^20 and a half, whose quotient is
-// nearer than 2^-12 to exact and not nearer than 2^-11 to a whole number).
+// Where run w of G = min(a.wgs, F) begins: floor(w F / G), the fraction's part in floats (a numerator below 2^20 and a half, whose
+// quotient is nearer than 2^-12 to exact and not nearer than 2^-11 to a whole number).  No run is empty.
 struct PagedBounds {
-  uint32_t q, rem; float inv;
-  __device__ __forceinline__ PagedBounds(const PagedArgs& a, int total)
-      : q((uint32_t)total / (uint32_t)a.wgs), rem((uint32_t)total % (uint32_t)a.wgs), inv(1.f / (float)a.wgs) {}
-  __device__ __forceinline__ int at(int w) const { return (int)(q * (uint32_t)w + (uint32_t)(((float)(rem * (uint32_t)w) + 0.5f) * inv)); }
+  uint32_t q, rem;
+  int runs, total;
+  float inv;
+  __device__ __forceinline__ PagedBounds(const PagedArgs& a, int f) : runs(max(min(a.wgs, f), 1)), total(f) {
+    q = (uint32_t)f / (uint32_t)runs;
+    rem = (uint32_t)f % (uint32_t)runs;
+    inv = 1.f / (float)runs;
+  }
+  __device__ __forceinline__ int at(int w) const {
+    return w >= runs ? total : (int)(q * (uint32_t)w + (uint32_t)(((float)(rem * (uint32_t)w) + 0.5f) * inv));
+  }
 };
 
 // The kernel's arguments (its first and only parameter) and thread index, asked for anew: what follows from them is not kept in registers

@@ -46,18 +46,19 @@ template <int D> struct FewCfg {
   static constexpr int LDS_BYTES = 4 * WAVE_BYTES;
 };
 
-// What the four waves hold of a tile's 16 rows is added up in LDS, and written as the output or as a record of the part.
-// x: [4][16][D + 4] floats, ml: [4][16][2] behind it.  Threads 16 i .. + 15 hold row i.
-template <typename T, int D>
+// What the waves hold of a tile's 16 rows is added up in LDS, and written as the output or as a record of the piece.
+// x: [WAVES][16][D + 4] floats, ml: [WAVES][16][2].  Of the first 256 threads, 16 i .. + 15 hold row i.
+template <typename T, int D, int WAVES>
 __device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const PagedRun& run, int r, int64_t rec, int t0, const float* x, const float* ml) {
   const PagedItem& it = run.it;
   const int row = threadIdx.x >> 4, c = threadIdx.x & 15;
-  float M = -INFINITY, den = 0.f, w[4];
+  if (WAVES > 4 && row >= 16) return;
+  float M = -INFINITY, den = 0.f, w[WAVES];
 #pragma unroll
-  for (int i = 0; i < 4; i++) M = fmaxf(M, ml[(i * 16 + row) * 2]);
+  for (int i = 0; i < WAVES; i++) M = fmaxf(M, ml[(i * 16 + row) * 2]);
   const float use = M == -INFINITY ? 0.f : M;
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
+  for (int i = 0; i < WAVES; i++) {
     w[i] = __builtin_amdgcn_exp2f(ml[(i * 16 + row) * 2] - use);
     den = fmaf(w[i], ml[(i * 16 + row) * 2 + 1], den);
   }
@@ -66,7 +67,7 @@ __device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const Paged
   for (int j = 0; j < D / 64; j++) {
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
+    for (int i = 0; i < WAVES; i++) {
       const f32x4 y = *reinterpret_cast<const f32x4*>(x + (i * 16 + row) * (D + 4) + j * 64 + c * 4);
 #pragma unroll
       for (int e = 0; e < 4; e++) s[e] = fmaf(w[i], y[e], s[e]);
@@ -93,7 +94,7 @@ __device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const Paged
 
 
 template <int D>
-__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void paged_few_kernel(PagedArgs args) {
+__global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs args) {
   using C = FewCfg<D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int r = blockIdx.x % args.h_kv, wg = blockIdx.x / args.h_kv;
@@ -243,16 +244,19 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void paged_few_kernel(PagedA
     ml[(wave * 16 + n) * 2 + 1] = l_tot;
   }
   __syncthreads();
-  paged_few_finish<uint16_t, D>(a, run, r, ((int64_t)r * a.wgs + wg) * 2 + (run.x0 == 0), t0, x, ml);
+  paged_few_finish<uint16_t, D, 4>(a, run, r, ((int64_t)r * a.wgs + wg) * 2 + (run.x0 == 0), t0, x, ml);
   __syncthreads();
   } while (run.advance(args));
 }
 
 // fp32: the same walk with the fp32 matrix cores, operands straight from the pages, 16 keys at a time.  A token's NaN or infinity
-// reaches the rows that see it and no other.
+// reaches the rows that see it and no other.  Eight waves, one of each step's eight tiles each: the matrix cores' fp32 rate
+// bounds a wave (1024 clocks a tile at head dimension 64), and items are few.  (Four waves, 333 tokens of two sequences of up to 1024, 4 / 2
+// heads of 64: 19.0 us; eight: 17.4.)
 template <int D>
-__global__ __launch_bounds__(256) void paged_few_f32_kernel(PagedArgs args) {
-  __shared__ __attribute__((aligned(16))) float x[4 * 16 * (D + 4) + 4 * 16 * 2];
+__global__ __launch_bounds__(512) void paged_few_f32_kernel(PagedArgs args) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  float* x = reinterpret_cast<float*>(lds);                                      // [8][16][D + 4], [8][16][2]
   const int r = blockIdx.x % args.h_kv, wg = blockIdx.x / args.h_kv;
   PagedRun run(args);
   if (!run.begin(args, wg)) return;
@@ -276,16 +280,26 @@ __global__ __launch_bounds__(256) void paged_few_f32_kernel(PagedArgs args) {
   f32x4 acc[D / 16];
 #pragma unroll
   for (int i = 0; i < D / 16; i++) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int j = j0; j < j1; j += 4) {
-    // rows behind the sequence's last token repeat it
+  // the next tile's rows are asked for before the present one's are used; rows behind the sequence's last token repeat it
+  f32x4 kv[D / 16], vv[1][4][D / 64], kn[D / 16], vn[4][D / 64];
+  auto ask = [&](int j) {
     const int64_t id = paged_page(a, it.b, (j * 16) >> a.page_log);
     const int top = it.n - 1 - j * 16;
     const float* kp = kb + id * a.kp_p + (int64_t)(j * 16 & pm) * a.kp_t;
     const float* vp = vb + id * a.vp_p + (int64_t)(j * 16 & pm) * a.vp_t;
-    f32x4 kv[D / 16], vv[1][4][D / 64];
-    load_row<D>(kp + min(n, top) * a.kp_t, kq, kv);
+    load_row<D>(kp + min(n, top) * a.kp_t, kq, kn);
 #pragma unroll
-    for (int i = 0; i < 4; i++) load_row2<D>(vp + min(4 * kq + i, top) * a.vp_t, n, vv[0][i]);
+    for (int i = 0; i < 4; i++) load_row2<D>(vp + min(4 * kq + i, top) * a.vp_t, n, vn[i]);
+  };
+  if (j0 < j1) ask(j0);
+  for (int j = j0; j < j1; j += 8) {
+#pragma unroll
+    for (int i = 0; i < D / 16; i++) kv[i] = kn[i];
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+#pragma unroll
+      for (int e = 0; e < D / 64; e++) vv[0][i][e] = vn[i][e];
+    if (j + 8 < j1) ask(j + 8);
     f32x4 s[1] = {mma_dot<D>(kv, qv)};                                           // lane (row n, kq): keys 4 kq + i
     const int lim = last - (j * 16 + 4 * kq);
     float mx = -INFINITY;
@@ -310,7 +324,7 @@ __global__ __launch_bounds__(256) void paged_few_f32_kernel(PagedArgs args) {
     mma_outer_keys<D, 1>(vv, s, lim, min(T, it.m - t0), a.g, lane, acc);
   }
   const float l_tot = quad_rows_sum(l_run);
-  float* ml = x + 4 * 16 * (D + 4);
+  float* ml = x + 8 * 16 * (D + 4);
 #pragma unroll
   for (int nv = 0; nv < D / 64; nv++)
 #pragma unroll
@@ -322,7 +336,7 @@ __global__ __launch_bounds__(256) void paged_few_f32_kernel(PagedArgs args) {
     ml[(wave * 16 + n) * 2 + 1] = l_tot;
   }
   __syncthreads();
-  paged_few_finish<float, D>(a, run, r, ((int64_t)r * a.wgs + wg) * 2 + (run.x0 == 0), t0, x, ml);
+  paged_few_finish<float, D, 8>(a, run, r, ((int64_t)r * a.wgs + wg) * 2 + (run.x0 == 0), t0, x, ml);
   __syncthreads();
   } while (run.advance(args));
 }
@@ -656,18 +670,13 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
   const int x = deal.find(a, f, true, it), begin = f - x, end = begin + deal.steps(it.s, it.tile);
   if (x == 0 || bounds.at(wg - 1) > begin) return;         // not cut here, or not for the first time
   int pieces = 1;                                          // runs wg - 1 .. wg - 2 + pieces
-  for (int k0 = wg; k0 < a.wgs; k0 += 64) {
-    const int more = __popcll(__ballot(k0 + lane < a.wgs && bounds.at(k0 + lane) < end));
+  for (int k0 = wg; k0 < bounds.runs; k0 += 64) {
+    const int more = __popcll(__ballot(k0 + lane < bounds.runs && bounds.at(k0 + lane) < end));
     pieces += more;
     if (more < 64) break;
   }
   const int64_t rec0 = ((int64_t)r * a.wgs + wg - 1) * 2;
-  // (with fewer steps than runs some runs are empty and wrote no record)
-  const bool holes = bounds.q == 0;
-  auto record = [&](int p) -> int64_t {
-    if (holes && p > 0 && bounds.at(wg - 1 + p) == bounds.at(wg + p)) return -1;
-    return p == 0 ? rec0 + 1 : rec0 + 2 * p;
-  };
+  auto record = [&](int p) { return p == 0 ? rec0 + 1 : rec0 + 2 * p; };
   const int rows = min(deal.T, it.m - it.tile * deal.T) * a.g;
   const int slices = rows * 4 <= UNITS ? 4 : rows * 2 <= UNITS ? 2 : 1, per = UNITS / slices;
   const int c = threadIdx.x % TPR, unit = threadIdx.x / TPR, slice = unit / per;
@@ -676,7 +685,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
     const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + in;
     float M = -INFINITY, den = 0.f;
     for (int p = c; p < pieces; p += TPR)                  // c-th piece of TPR a thread's
-      if (const int64_t rec = record(p); rec >= 0) M = fmaxf(M, ml[rec * 16].x);
+      M = fmaxf(M, ml[record(p) * 16].x);
     M = row16_reduce(M, OpMax());
     if constexpr (TPR == 32) M = fmaxf(M, __shfl_xor(M, 16));
     const float use = M == -INFINITY ? 0.f : M;
@@ -684,10 +693,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
     const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o) + in * (D / 4) + c;
 #pragma unroll 8
     for (int p = slice; p < pieces; p += slices) {
-      const int64_t rec = record(p);
-      if (rec < 0) continue;
-      const float2 y = ml[rec * 16];
-      const f32x4 v = po[rec * 16 * (D / 4)];
+      const float2 y = ml[record(p) * 16];
+      const f32x4 v = po[record(p) * 16 * (D / 4)];
       const float w = __builtin_amdgcn_exp2f(y.x - use);
       den = fmaf(w, y.y, den);
 #pragma unroll
@@ -801,8 +808,8 @@ static int64_t most_items(const PagedArgs& a, int rows) {   // of a kv-head
   const int T = rows / a.g;
   return min((int64_t)a.n_rows / T + min(a.batch, a.n_rows), (int64_t)a.n_rows);
 }
-// Workgroups of a kv-head that are resident at once: one a CU for the 128 KB ring of 16-row tiles, two otherwise.
-static int runs_of(const PagedArgs& a, int dtype, int d, bool big) { return max((!big && dtype == DASH_BF16 && d == 128 ? 256 : 512) / a.h_kv, 1); }
+// Workgroups of a kv-head that are resident at once: one a CU for the 128 KB ring of 16-row tiles and the fp32 kernel, two otherwise.
+static int runs_of(const PagedArgs& a, int dtype, int d, bool big) { return max((!big && (dtype == DASH_F32 || d == 128) ? 256 : 512) / a.h_kv, 1); }
 static size_t ws_align(size_t x) { return (x + 255) & ~(size_t)255; }
 
 size_t paged_attend_ws(const PagedArgs& a, int dtype, int d) {
@@ -818,6 +825,8 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
   const int64_t items = most_items(a, big ? 128 : 16);
   // Runs of small tiles cost little (a record is 16 rows) and even out the lengths of a batch; with many items a workgroup each evens them out as well.
   a.wgs = items < (big ? 1 : 8) * (int64_t)runs ? runs : 0;
+  // Items of up to eight steps are not worth a launch that adds them up, if there is one for every other CU.
+  if (!big && a.cap <= 8 * kStep && items * a.h_kv >= 128) a.wgs = 0;
   const size_t recs = (size_t)a.wgs * a.h_kv * (big ? 128 : 2 * 16);
   a.part_ml = (float*)ws;
   a.part_o = (float*)(ws + ws_align(recs * 8));
@@ -833,7 +842,10 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
     if (hipError_t e = allow_dyn_lds((const void*)paged_few_kernel<D>, FewCfg<D>::LDS_BYTES, opt_in); e != hipSuccess) return e;
     hipLaunchKernelGGL(paged_few_kernel<D>, grid, blk, FewCfg<D>::LDS_BYTES, st, a);
   } else {
-    hipLaunchKernelGGL(paged_few_f32_kernel<D>, grid, blk, 0, st, a);
+    constexpr int lds = 8 * 16 * (D + 6) * 4;
+    static LdsOptIn opt_in;
+    if (hipError_t e = allow_dyn_lds((const void*)paged_few_f32_kernel<D>, lds, opt_in); e != hipSuccess) return e;
+    hipLaunchKernelGGL(paged_few_f32_kernel<D>, grid, dim3(512), lds, st, a);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.wgs <= 1) return e;
