@@ -178,18 +178,19 @@ struct PagedDeal {
 };
 
 // Where run w of G = min(a.wgs, F) begins: floor(w F / G), the fraction's part in floats (a numerator below 2^20 and a half, whose
-// quotient is nearer than 2^-12 to exact and not nearer than 2^-11 to a whole number).  No run is empty.
-struct PagedBounds {
-  uint32_t q, rem;
-  int runs, total;
+// quotient is nearer than 2^-12 to exact and not nearer than 2^-11 to a whole number).  No run is empty.  I: type of a place.
+template <typename I> struct PagedBounds {
+  I q, total;
+  uint32_t rem;
+  int runs;
   float inv;
-  __device__ __forceinline__ PagedBounds(const PagedArgs& a, int f) : runs(max(min(a.wgs, f), 1)), total(f) {
-    q = (uint32_t)f / (uint32_t)runs;
-    rem = (uint32_t)f % (uint32_t)runs;
+  __device__ __forceinline__ PagedBounds(const PagedArgs& a, I f) : total(f), runs((int)max(min((I)a.wgs, f), (I)1)) {
+    q = f / runs;
+    rem = (uint32_t)(f - q * runs);
     inv = 1.f / (float)runs;
   }
-  __device__ __forceinline__ int at(int w) const {
-    return w >= runs ? total : (int)(q * (uint32_t)w + (uint32_t)(((float)(rem * (uint32_t)w) + 0.5f) * inv));
+  __device__ __forceinline__ I at(int w) const {
+    return w >= runs ? total : q * w + (I)(uint32_t)(((float)(rem * (uint32_t)w) + 0.5f) * inv);
   }
 };
 
@@ -220,7 +221,7 @@ struct PagedRun {
       x1 = cost = deal.steps(it.s, it.tile);
       return true;
     }
-    const PagedBounds b(a, deal.total(a));
+    const PagedBounds<int> b(a, deal.total(a));
     next = __builtin_amdgcn_readfirstlane(b.at(wg));
     end = __builtin_amdgcn_readfirstlane(b.at(wg + 1));
     if (next >= end) return false;

@@ -663,7 +663,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
   const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv + 1, lane = threadIdx.x & 63;
   const PagedDeal deal(a);
   const int total = deal.total(a);
-  const PagedBounds bounds(a, total);
+  const PagedBounds<int> bounds(a, total);
   const int f = __builtin_amdgcn_readfirstlane(bounds.at(wg));
   if (f >= total) return;
   PagedItem it;

@@ -94,35 +94,42 @@ __device__ __forceinline__ uint32_t evict_key(float w, int pos, int sinks, int f
   return u ^ ((int32_t)u < 0 ? 0xffffffffu : 0x80000000u);
 }
 
-constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
-constexpr int kSelRows = 32;                               // keys a thread holds in registers at most: sequences of up to 32768 tokens
-constexpr int kBins = 2048;                                // 11, 11 and 10 bits of a key
+constexpr int kSelThreads = 1024;
+constexpr int kSelKeys = 32768;                            // keys that are kept in LDS at most
+constexpr int kBins = 2048;                                // 11 bits of a key
+constexpr int kCands = 2048, kRanked = 256;                // keys that are picked out; that are ranked against each other
 
-// sum of `v`, the same in a wave's lanes, over the waves before one's own, and over all
-__device__ __forceinline__ int2 waves_before(int v, int wave, int* xch) {
+// For two counts of a thread: their sums over the threads before it (x, y) and over all (z, w).
+__device__ __forceinline__ int4 threads_before(int u, int v, int2* xch) {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, us = wave_scan(u), vs = wave_scan(v);
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) xch[wave] = v;
+  if (lane == 63) xch[wave] = make_int2(us, vs);
   __syncthreads();
-  int2 s = make_int2(0, 0);
-#pragma unroll
-  for (int w = 0; w < kSelWaves; w++) {
-    const int c = xch[w];
-    s.x += w < wave ? c : 0;
-    s.y += c;
-  }
-  return s;
+  const int2 c = lane < kSelThreads / 64 ? xch[lane] : make_int2(0, 0);
+  const int cu = wave_scan(c.x), cv = wave_scan(c.y);
+  const int bu = wave ? __builtin_amdgcn_readlane(cu, wave - 1) : 0, bv = wave ? __builtin_amdgcn_readlane(cv, wave - 1) : 0;
+  return make_int4(us - u + bu, vs - v + bv, __builtin_amdgcn_readlane(cu, 63), __builtin_amdgcn_readlane(cv, 63));
 }
 
-// A workgroup per pair.  Wave w owns rows of 64 slots [w rows, (w + 1) rows), so that ranks in slot order need one exchange between
-// the waves.  The keys stay in registers (sequences of more than 32768 tokens: in the scratch); the budget-th largest is found by
-// counting its 11 leading bits, of those that share them the next 11, then the last 10.
-__global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e) {
+// A workgroup per pair.  The keys stay in LDS (of more than 32768 tokens: in the scratch).  The budget-th largest: the keys are counted by
+// their 11 leading bits; those that share the ones of the key looked for are picked out and ranked against each other (more than 256 of
+// them: counted by the next 11 bits, and the last 10; more than 2048 are not picked out).  Then a thread takes an odd number of consecutive slots, so that ranks in slot order need
+// one scan over the threads, and its reads meet no other's bank.
+// What bounds it: the chain of loads (lengths, pages, weights), then LDS and some fifteen barriers one after the other: 32 caches of 4352
+// tokens x 8 15 us (256 threads instead of 1024: 20), two of 20 and 32k 33.
+__global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e, int room) {   // room: keys that LDS has room for
   const PagedArgs& a = e.a;
+  extern __shared__ uint32_t lds_keys[];
   __shared__ int hist[kBins];
-  __shared__ int xch[kSelWaves], chosen[2];
+  __shared__ int2 xch[kSelThreads / 64], rank[kRanked];
+  __shared__ uint32_t cand[kCands];
+  __shared__ int chosen[3], n_cand;
   const int pair = blockIdx.x, h = pair % a.h_kv, b = pair / a.h_kv;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = paged_len(a, b), left = min(n, e.budget);
+  for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+  if (tid < kRanked) rank[tid] = make_int2(0, 0);
+  if (tid == 0) n_cand = 0;
   int32_t* src = e.src ? e.src + (int64_t)pair * e.budget : nullptr;
   if (src)
     for (int i = tid; i < e.budget; i += kSelThreads) src[i] = i < left ? i : -1;   // the moves change theirs
@@ -131,128 +138,180 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e) 
     return;
   }
   const int first_recent = a.seen[b] - e.recent, pm = (1 << a.page_log) - 1;
-  const int rows = (n + kSelThreads - 1) / kSelThreads;    // of 64 slots, a wave's
-  const int slot0 = wave * rows * 64 + lane;
-  uint32_t* keys = e.keys + (int64_t)pair * a.cap;
-  auto key_of = [&](int i) -> uint32_t {
-    const int64_t at = (((int64_t)paged_page_lane(a, b, i >> a.page_log) * a.h_kv + h) << a.page_log) + (i & pm);
-    return evict_key(a.weights[at], a.pos[at], e.sinks, first_recent);
-  };
-  uint32_t prefix = 0, mask = 0;
-  int want = e.budget;                                     // of the keys that begin with prefix
-  // each(f): f(key, slot) for every row of the wave, all lanes; slots behind the end among them
-  auto select = [&](auto&& each) {
-    for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
-    for (int step = 0; step < 3; step++) {
-      const int shift = step == 0 ? 21 : step == 1 ? 10 : 0, bits = step == 2 ? 1023 : 2047;
-      __syncthreads();
-      each([&](uint32_t k, int i) {
-        if (i < n && (k & mask) == prefix) atomicAdd(&hist[(k >> shift) & bits], 1);
-      });
-      __syncthreads();
-      const int b1 = hist[kBins - 1 - 2 * tid], b0 = hist[kBins - 2 - 2 * tid];      // this thread's two bins, from the largest
-      hist[kBins - 1 - 2 * tid] = 0;
-      hist[kBins - 2 - 2 * tid] = 0;
-      const int incl = wave_scan(b1 + b0);
-      const int before = waves_before(__builtin_amdgcn_readlane(incl, 63), wave, xch).x + incl - b1 - b0;
-      if (before < want && before + b1 >= want) { chosen[0] = kBins - 1 - 2 * tid; chosen[1] = want - before; }
-      else if (before + b1 < want && before + b1 + b0 >= want) { chosen[0] = kBins - 2 - 2 * tid; chosen[1] = want - before - b1; }
-      __syncthreads();
-      prefix |= (uint32_t)chosen[0] << shift;
-      mask |= (uint32_t)bits << shift;
-      want = chosen[1];
-    }
-    // of the keys equal to the last one kept, the first `want` stay
-    const uint64_t below = (1ull << lane) - 1ull;
-    int ties = 0;
-    each([&](uint32_t k, int i) { ties += __popcll(__ballot(i < n && k == prefix)); });
-    const int2 tw = waves_before(ties, wave, xch);
-    const bool all_ties = tw.y == want;
-    int t = tw.x, holes = 0, movers = 0;
-    auto kept_of = [&](uint32_t k, int i) {
-      const bool tie = i < n && k == prefix;
-      bool kept = i < n && (k > prefix || tie);
-      if (!all_ties) {
-        const uint64_t tb = __ballot(tie);
-        if (tie && t + __popcll(tb & below) >= want) kept = false;
-        t += __popcll(tb);
+  auto select = [&](uint32_t* keys) __attribute__((always_inline)) {
+    // Load: wave w owns rows of 64 slots [w rows, (w + 1) rows), sixteen at a time: their pages, a lane for each 16 slots, then all weights
+    // and positions.
+    const int rows = (n + kSelThreads - 1) / kSelThreads, base = wave * rows * 64;
+    for (int j0 = 0; j0 < rows; j0 += 16) {
+      const int pages = paged_page_lane(a, b, min(base + (j0 * 4 + lane) * 16, n - 1) >> a.page_log);
+      float w[16];
+      int p[16];
+      auto load = [&](int j) {
+        const int64_t at = (((int64_t)__shfl(pages, 4 * j + (lane >> 4)) * a.h_kv + h) << a.page_log) + ((base + (j0 + j) * 64 + lane) & pm);
+        w[j] = a.weights[at];
+        p[j] = a.pos[at];
+      };
+      auto use = [&](int j) {
+        const int i = base + (j0 + j) * 64 + lane;
+        if (j0 + j < rows && i < n) {
+          const uint32_t k = evict_key(w[j], p[j], e.sinks, first_recent);
+          keys[i] = k;
+          atomicAdd(&hist[k >> 21], 1);
+        }
+      };
+#pragma unroll
+      for (int j = 0; j < 8; j++) load(j);
+      if (j0 + 8 < rows) {
+#pragma unroll
+        for (int j = 8; j < 16; j++) load(j);
       }
-      return kept;
+      if (j0 == 0) __syncthreads();                          // the counts are zero
+#pragma unroll
+      for (int j = 0; j < 8; j++) use(j);
+      if (j0 + 8 < rows) {
+#pragma unroll
+        for (int j = 8; j < 16; j++) use(j);
+      }
+    }
+    __syncthreads();
+    // f(key, slot) for the thread's slots
+    const int own = rows | 1, slot0 = tid * own;
+    auto each = [&](auto&& f) {
+      int i = slot0;
+      const int end = min(slot0 + own, n);
+      for (; i + 4 <= end; i += 4) {
+        const uint32_t k0 = keys[i], k1 = keys[i + 1], k2 = keys[i + 2], k3 = keys[i + 3];
+        f(k0, i); f(k1, i + 1); f(k2, i + 2); f(k3, i + 3);
+      }
+      for (; i < end; i++) f(keys[i], i);
     };
+    // the bin that holds the want-th largest of the keys counted: how many of its keys stay, and all
+    auto find_bin = [&](int want) {
+      constexpr int OWN = kBins / kSelThreads;                   // bins of a thread, from the largest
+      int c[OWN], sum = 0;
+#pragma unroll
+      for (int q = 0; q < OWN; q++) sum += c[q] = hist[kBins - 1 - OWN * tid - q];
+      int before = threads_before(sum, 0, xch).x;
+      if (before < want && before + sum >= want) {
+#pragma unroll
+        for (int q = 0; q < OWN; q++) {
+          if (before < want && before + c[q] >= want) { chosen[0] = kBins - 1 - OWN * tid - q; chosen[1] = want - before; chosen[2] = c[q]; }
+          before += c[q];
+        }
+      }
+      __syncthreads();
+    };
+    find_bin(e.budget);
+    uint32_t last = (uint32_t)chosen[0] << 21;               // the smallest key that stays, from its leading bits on
+    int want = chosen[1], ties = chosen[2];                  // of the keys that share them, those that stay, and all
+    const int picked = ties <= kCands ? ties : 0;
+    if (picked) {
+      const uint32_t bin = last >> 21;
+      int mine = 0;
+      each([&](uint32_t k, int) { mine += k >> 21 == bin; });
+      if (mine) {
+        int at = atomicAdd(&n_cand, mine);
+        each([&](uint32_t k, int) { if (k >> 21 == bin) cand[at++] = k; });
+      }
+      __syncthreads();
+    }
+    if (ties <= kRanked) {
+      // thread t ranks candidate t % M among a share of them
+      int m_log = 0;
+      while ((1 << m_log) < ties) m_log++;
+      const int me = tid & ((1 << m_log) - 1), share = kSelThreads >> m_log;
+      if (me < ties) {
+        const uint32_t k = cand[me];
+        int more = 0, same = 0;
+        for (int i = tid >> m_log; i < ties; i += share) {
+          const uint32_t x = cand[i];
+          more += x > k;
+          same += x == k;
+        }
+        atomicAdd(&rank[me].x, more);
+        atomicAdd(&rank[me].y, same);
+      }
+      __syncthreads();
+      if (tid < ties) {
+        const int2 y = rank[tid];
+        if (y.x < want && y.x + y.y >= want) {               // those that find it are equal and write the same
+          chosen[0] = (int)(cand[tid] & 0x1fffff);
+          chosen[1] = want - y.x;
+          chosen[2] = y.y;
+        }
+      }
+      __syncthreads();
+      last |= (uint32_t)chosen[0];
+      want = chosen[1];
+      ties = chosen[2];
+    } else {
+#pragma unroll 1
+      for (int step = 0; step < 2; step++) {
+        const int shift = step ? 0 : 10, known = step ? 10 : 21, bits = step ? 1023 : 2047;
+        __syncthreads();
+        for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+        __syncthreads();
+        auto count = [&](uint32_t k) { if (k >> known == last >> known) atomicAdd(&hist[(k >> shift) & bits], 1); };
+        if (picked) {
+          for (int i = tid; i < picked; i += kSelThreads) count(cand[i]);
+        } else {
+          each([&](uint32_t k, int) { count(k); });
+        }
+        __syncthreads();
+        find_bin(want);
+        last |= (uint32_t)chosen[0] << shift;
+        want = chosen[1];
+        ties = chosen[2];
+      }
+    }
+    // Of the keys equal to the last one kept, the first `want` stay.
+    int tied = 0;
+    if (want < ties) {
+      each([&](uint32_t k, int) { tied += k == last; });
+      tied = threads_before(tied, 0, xch).x;
+    }
+    const int spare = want < ties ? want - tied : 0x7fffffff;   // equal keys that stay, from the thread's first on
+    int holes = 0, movers = 0, same = 0;
     each([&](uint32_t k, int i) {
-      const bool kept = kept_of(k, i);
-      holes += __popcll(__ballot(!kept && i < left));
-      movers += __popcll(__ballot(kept && i >= left));
+      const bool kept = k > last || (k == last && same++ < spare);
+      holes += !kept && i < left;
+      movers += kept && i >= left;
     });
-    const int2 hw = waves_before(holes, wave, xch);
-    int at_hole = hw.x, at_mover = a.cap - 1 - waves_before(movers, wave, xch).x;
+    const int4 hw = threads_before(holes, movers, xch);
     int32_t* moves = e.moves + (int64_t)pair * a.cap;
-    t = tw.x;
-    each([&](uint32_t k, int i) {
-      const bool kept = kept_of(k, i), hole = !kept && i < left, mover = kept && i >= left;
-      const uint64_t hb = __ballot(hole), mb = __ballot(mover);
-      if (hole) moves[at_hole + __popcll(hb & below)] = i;
-      if (mover) moves[at_mover - __popcll(mb & below)] = i;
-      at_hole += __popcll(hb);
-      at_mover -= __popcll(mb);
-    });
-    if (tid == 0) e.counts[pair] = hw.y;
-  };
-  // keys in registers, in blocks of four rows; a row past the wave's last counts as behind the end
-  auto in_registers = [&](auto rows_tag) {
-    constexpr int ROWS = decltype(rows_tag)::value, AHEAD = ROWS < 16 ? ROWS : 16;
-    uint32_t key[ROWS];
-#pragma unroll
-    for (int j0 = 0; j0 < ROWS; j0 += AHEAD) {
-      if (j0 < rows) {
-        int64_t at[AHEAD];
-        float w[AHEAD];
-        int p[AHEAD];
-#pragma unroll
-        for (int j = 0; j < AHEAD; j++) {
-          const int i = min(slot0 + (j0 + j) * 64, n - 1);
-          at[j] = (((int64_t)paged_page_lane(a, b, i >> a.page_log) * a.h_kv + h) << a.page_log) + (i & pm);
-        }
-#pragma unroll
-        for (int j = 0; j < AHEAD; j++) {
-          w[j] = a.weights[at[j]];
-          p[j] = a.pos[at[j]];
-        }
-#pragma unroll
-        for (int j = 0; j < AHEAD; j++) key[j0 + j] = evict_key(w[j], p[j], e.sinks, first_recent);
+    same = 0;
+    if (keys == lds_keys) {
+      // The lists take the keys' place (they hold each slot once at most) before they are written out in whole lines: what a thread keeps of its
+      // 33 slots at most is a mask by then.
+      uint64_t stay = 0;
+      each([&](uint32_t k, int i) { stay |= (uint64_t)(k > last || (k == last && same++ < spare)) << (i - slot0); });
+      __syncthreads();
+      int at = hw.x, am = hw.z + hw.y;
+      for (int i = slot0; i < min(slot0 + own, n); i++) {
+        const bool kept = (stay >> (i - slot0)) & 1;
+        if (!kept && i < left) keys[at++] = (uint32_t)i;
+        if (kept && i >= left) keys[am++] = (uint32_t)i;
       }
+      __syncthreads();
+      for (int i = tid; i < hw.z; i += kSelThreads) {
+        moves[i] = (int)keys[i];
+        moves[a.cap - 1 - i] = (int)keys[hw.z + i];
+      }
+    } else {
+      int at = hw.x, am = a.cap - 1 - hw.y;
+      each([&](uint32_t k, int i) {
+        const bool kept = k > last || (k == last && same++ < spare);
+        if (!kept && i < left) moves[at++] = i;
+        if (kept && i >= left) moves[am--] = i;
+      });
     }
-    select([&](auto&& f) {
-#pragma unroll
-      for (int j0 = 0; j0 < ROWS; j0 += 4) {
-        if (j0 < rows) {
-#pragma unroll
-          for (int j = j0; j < j0 + 4; j++) f(key[j], j < rows ? slot0 + j * 64 : n);
-        }
-      }
-    });
+    if (tid == 0) e.counts[pair] = hw.z;
   };
-  if (rows <= 8) {                                           // its own code: the longer one's would be fetched for nothing
-    in_registers(std::integral_constant<int, 8>{});
-  } else if (rows <= kSelRows) {
-    in_registers(std::integral_constant<int, kSelRows>{});
-  } else {
-#pragma unroll 8
-    for (int j = 0; j < rows; j++) {
-      const int i = slot0 + j * 64;
-      if (i < n) keys[i] = key_of(i);
-    }
-    select([&](auto&& f) {
-#pragma unroll 8
-      for (int j = 0; j < rows; j++) {
-        const int i = slot0 + j * 64;
-        f(i < n ? keys[i] : 0u, i);
-      }
-    });
-  }
+  if (n <= room) select(lds_keys);
+  else select(e.keys + (int64_t)pair * a.cap);
 }
 
-// A wave moves kMoves tokens at a time: their places first, a lane each, then all their rows at once.
+// A wave moves eight tokens at a time: their places first, a lane each, then all their rows at once.
 template <int ES, int D>
 __global__ __launch_bounds__(256) void paged_move_kernel(EvictArgs e, int wgs) {   // wgs: workgroups of a pair
   const PagedArgs& a = e.a;
@@ -313,7 +372,10 @@ hipError_t launch_paged_evict(const PagedArgs& a, int elem, int d, int32_t* lens
   e.counts = (int32_t*)ws;
   e.keys = (uint32_t*)(ws + evict_align(pairs * 4));
   e.moves = (int32_t*)(ws + evict_align(pairs * 4) + evict_align(pairs * a.cap * 4));
-  hipLaunchKernelGGL(paged_select_kernel, dim3((unsigned)pairs), dim3(kSelThreads), 0, st, e);
+  const int room = a.cap < kSelKeys ? a.cap : kSelKeys;
+  static LdsOptIn opt_in;
+  if (hipError_t r = allow_dyn_lds((const void*)paged_select_kernel, (size_t)room * 4, opt_in); r != hipSuccess) return r;
+  hipLaunchKernelGGL(paged_select_kernel, dim3((unsigned)pairs), dim3(kSelThreads), (size_t)room * 4, st, e, room);
   if (hipError_t r = hipGetLastError(); r != hipSuccess) return r;
   // eight workgroups per CU are resident at once; how many tokens move is not known here
   const int wgs = pairs < 2048 ? (int)(2048 / pairs < 64 ? 2048 / pairs : 64) : 1;

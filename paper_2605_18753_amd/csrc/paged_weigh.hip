@@ -66,11 +66,6 @@ __device__ __forceinline__ int64_t scan64(int64_t v) {     // inclusive, over th
 __device__ __forceinline__ int64_t lane64(int64_t v, int l) {   // lane l's, as a scalar
   return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)((uint64_t)v >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, l));
 }
-// where run w of a.wgs begins
-__device__ __forceinline__ int64_t run_bound(const PagedArgs& a, int64_t total, int w) {
-  return total / a.wgs * w + total % a.wgs * w / a.wgs;
-}
-
 // whole: places are items, which are not cut
 template <int KEYS> __device__ __forceinline__ int64_t weigh_total(const PagedArgs& a, bool whole = false) {
   const int lane = lane_id();
@@ -121,8 +116,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : D == 128 ? 3 : 4) void pa
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv;
   const int64_t total = weigh_total<kWeighKeys<T>>(a);
-  const int64_t f0 = run_bound(a, total, wg);
-  int64_t todo = run_bound(a, total, wg + 1) - f0;
+  const PagedBounds<int64_t> bounds(a, total);
+  const int64_t f0 = bounds.at(wg), f1 = bounds.at(wg + 1);
+  int64_t todo = f1 - f0;
   if (todo <= 0) return;
   const int Tt = 16 / a.g, n = lane & 15, kq = lane >> 4, pm = (1 << a.page_log) - 1;
   const int tl = n / a.g;
@@ -210,7 +206,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : D == 128 ? 3 : 4) void pa
     }
     if ((todo -= take) <= 0) return;
     it.x = 0;
-    if (++it.block >= it.s.items) weigh_find<kWeighKeys<T>>(a, run_bound(a, total, wg + 1) - todo, it);
+    if (++it.block >= it.s.items) weigh_find<kWeighKeys<T>>(a, f1 - todo, it);
   }
 }
 
@@ -219,20 +215,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : D == 128 ? 3 : 4) void pa
 template <typename T>
 __global__ __launch_bounds__(kWeighKeys<T>) void paged_weigh_sum_kernel(PagedArgs a) {
   const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv + 1;
-  const int64_t total = weigh_total<kWeighKeys<T>>(a), f = run_bound(a, total, wg);
-  if (f >= total || f == run_bound(a, total, wg - 1)) return;
+  const int64_t total = weigh_total<kWeighKeys<T>>(a);
+  const PagedBounds<int64_t> bounds(a, total);
+  const int64_t f = bounds.at(wg);
+  if (f >= total) return;
   WeighItem it;
   weigh_find<kWeighKeys<T>>(a, f, it);
   const int64_t begin = f - it.x, end = begin + it.s.tiles;
-  if (it.x == 0 || run_bound(a, total, wg - 1) > begin) return;              // not cut here, or not for the first time
+  if (it.x == 0 || bounds.at(wg - 1) > begin) return;              // not cut here, or not for the first time
   const float* p = a.part_o + ((int64_t)r * a.wgs + wg - 1) * 2 * kWeighKeys<T> + threadIdx.x;
   float w = p[kWeighKeys<T>];
-  for (int k = wg; k < a.wgs; k++) {
-    const int64_t at = run_bound(a, total, k);
-    if (at >= end) break;
-    p += 2 * kWeighKeys<T>;
-    if (at < run_bound(a, total, k + 1)) w += *p;
-  }
+  for (int k = wg; k < bounds.runs && bounds.at(k) < end; k++) w += *(p += 2 * kWeighKeys<T>);
   const int key = it.block * kWeighKeys<T> + threadIdx.x;
   if (key >= it.n) return;
   const uint32_t page = (uint32_t)a.table[(int64_t)it.b * a.max_pages + (key >> a.page_log)];
@@ -254,8 +247,9 @@ __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a)
   const uint32_t l_lane = (uint32_t)(tl * a.h_q + n % a.g) * 4u;
   // blocks of all sequences, and the run's
   const int64_t total = weigh_total<KEYS>(a, true);
-  int64_t f = run_bound(a, total, wg);
-  int todo = (int)(run_bound(a, total, wg + 1) - f);
+  const PagedBounds<int64_t> bounds(a, total);
+  int64_t f = bounds.at(wg);
+  int todo = (int)(bounds.at(wg + 1) - f);
   if (todo <= 0) return;
   WeighItem it, next;
   weigh_find<KEYS>(a, f, it, true);
