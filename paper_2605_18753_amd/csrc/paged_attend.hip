@@ -352,7 +352,7 @@ template <int D> struct RowsCfg {
   static constexpr int NCH = D / 8, ROW_BYTES = D * 2;
   static constexpr int TILE_BYTES = 64 * ROW_BYTES;
   static constexpr int COPIES = TILE_BYTES / 4096;       // copy instructions of a wave per tile and tensor
-  static constexpr int RPC = 256 / NCH, RPW = RPC / 4;   // rows that the workgroup's, and a wave's, copy instruction covers
+  static constexpr int RPC = 64 / NCH;                   // rows that a copy instruction covers
   static constexpr int OUT_BYTES = 128 * (D + 4) * 4;    // a tile's rows in fp32, behind the walk
   static constexpr int LDS_BYTES = 4 * TILE_BYTES > OUT_BYTES ? 4 * TILE_BYTES : OUT_BYTES;   // K ring [2], V ring [2]
 };
@@ -363,8 +363,7 @@ __device__ __forceinline__ int2 rows_shape(const PagedArgs& a, int m, int n) {
   return make_int2((m + T - 1) / T, max((n + 63) >> 6, 1));
 }
 
-// SMALL: pages of fewer than 64 tokens, several to a tile.
-template <int D, bool SMALL>
+template <int D>
 __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
   using C = RowsCfg<D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -404,42 +403,31 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
   const int64_t kp2 = a.kp_p * 2, vp2 = a.vp_p * 2;
   const int pm = (1 << a.page_log) - 1;
   const uint32_t lds0 = lds_addr_of(lds);
-  const int c_x = lane / C::NCH, c_pos = lane % C::NCH, c_row = wave * C::RPW + c_x;
-  const uint32_t k_off = (uint32_t)c_x * kt2 + (uint32_t)((c_pos ^ pk_swz<D>(c_row)) << 4);
-  const uint32_t v_off = (uint32_t)c_x * vt2 + (uint32_t)((c_pos ^ pv_swz<D>(c_row)) << 4);
-  // Rows [key, key + RPW) of page id onwards, up to key `stop` of the sequence: behind it a resource ends, and the rows read as
-  // zeros, whatever the page holds.  A tile in one page has one resource for all copies, otherwise each copy has its own.
-  auto rows_from = [&](const char* base, int64_t page_bytes, uint32_t row_bytes, int id, int key, int stop, int most) {
-    const int left = min(max(stop - key, 0), most);
+  // A wave copies 16 rows of a tile, which lie in one page: one resource, which ends with the sequence's last token (rows behind it
+  // read as zeros, whatever the page holds).  Copy c: rows RPC c + c_row of them.  The part of K's permutation that depends on c is a
+  // flip of chunk bits 2 (and 3).
+  const int c_row = lane / C::NCH, c_pos = lane % C::NCH, row0 = wave * 16;
+  uint32_t k_off[C::COPIES];
+#pragma unroll
+  for (int c = 0; c < C::COPIES; c++) k_off[c] = (uint32_t)c_row * kt2 + (uint32_t)((c_pos ^ pk_swz<D>(C::RPC * c + c_row)) << 4);
+  const uint32_t v_off = (uint32_t)c_row * vt2 + (uint32_t)((c_pos ^ pv_swz<D>(c_row)) << 4);
+  auto rows_from = [&](const char* base, int64_t page_bytes, uint32_t row_bytes, int id, int key, int stop) {
+    const int left = min(max(stop - key, 0), 16);
     const int64_t bytes = (int64_t)left * row_bytes - (int64_t)(row_bytes - C::ROW_BYTES);
     return make_rsrc(base + (int64_t)id * page_bytes + (uint32_t)(key & pm) * row_bytes, bytes < 0 ? 0 : bytes);
   };
-  constexpr int NID = SMALL ? C::COPIES : 1;
-  int id_v[NID], id_k[NID];                                   // pages of tile i (its V is copied) and of tile i + 1 (its K)
+  int id_v = 0, id_k = 0;                                     // pages of tile i (its V is copied) and of tile i + 1 (its K)
   u32x4 k_rs = {}, v_rs = {};
-  auto ids_of = [&](int tile, int (&id)[NID]) {
-#pragma unroll
-    for (int c = 0; c < NID; c++)
-      id[c] = __builtin_amdgcn_readlane(win, (((tile * 64 + (SMALL ? c * C::RPC + wave * C::RPW : 0)) >> a.page_log) - wbase) & 63);
-  };
+  auto id_of = [&](int tile) { return __builtin_amdgcn_readlane(win, (((tile * 64 + row0) >> a.page_log) - wbase) & 63); };
   const int part_end = first + n_it;
   auto aim_k = [&](int tile) {                                // behind the part's last tile: nothing is read
-    if constexpr (!SMALL) k_rs = rows_from(kb, kp2, kt2, id_k[0], tile * 64 + wave * C::RPW, tile < part_end ? it.n : 0, 64 - wave * C::RPW);
+    k_rs = rows_from(kb, kp2, kt2, id_k, tile * 64 + row0, tile < part_end ? it.n : 0);
   };
-  auto aim_v = [&](int tile) {
-    if constexpr (!SMALL) v_rs = rows_from(vb, vp2, vt2, id_v[0], tile * 64 + wave * C::RPW, it.n, 64 - wave * C::RPW);
+  auto copy_k = [&](int c, int slot) {
+    copy16_to_lds(k_rs, lds0 + slot * C::TILE_BYTES + wave * (C::TILE_BYTES / 4) + c * 1024, k_off[c], (uint32_t)(c * C::RPC) * kt2);
   };
-  auto copy_k = [&](int tile, int c, int slot) {
-    const uint32_t to = lds0 + slot * C::TILE_BYTES + c * 4096 + wave * 1024;
-    if constexpr (SMALL)
-      copy16_to_lds(rows_from(kb, kp2, kt2, id_k[c], tile * 64 + c * C::RPC + wave * C::RPW, tile < part_end ? it.n : 0, C::RPW), to, k_off, 0);
-    else
-      copy16_to_lds(k_rs, to, k_off, (uint32_t)(c * C::RPC) * kt2);
-  };
-  auto copy_v = [&](int tile, int c, int slot) {
-    const uint32_t to = lds0 + (2 + slot) * C::TILE_BYTES + c * 4096 + wave * 1024;
-    if constexpr (SMALL) copy16_to_lds(rows_from(vb, vp2, vt2, id_v[c], tile * 64 + c * C::RPC + wave * C::RPW, it.n, C::RPW), to, v_off, 0);
-    else copy16_to_lds(v_rs, to, v_off, (uint32_t)(c * C::RPC) * vt2);
+  auto copy_v = [&](int c, int slot) {
+    copy16_to_lds(v_rs, lds0 + (2 + slot) * C::TILE_BYTES + wave * (C::TILE_BYTES / 4) + c * 1024, v_off, (uint32_t)(c * C::RPC) * vt2);
   };
   // ---- operand addresses in LDS, of slot 0 --------------------------------------------------------------------
   uint32_t k_rd[D / 16], v_rd[D / 32];
@@ -462,11 +450,11 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
 #pragma unroll
   for (int ks = 0; ks < D / 16; ks++) asm volatile("" : "+v"(qf[ks]));
   asm volatile("" : "+v"(win), "+v"(win_next));
-  ids_of(first, id_k);
+  id_k = id_of(first);
   aim_k(first);
   if (n_it > 0) {
 #pragma unroll
-    for (int c = 0; c < C::COPIES; c++) copy_k(first, c, 0);
+    for (int c = 0; c < C::COPIES; c++) copy_k(c, 0);
   }
   // Iteration i, LDS: tile i lives in slot i & 1 of both rings, V one iteration behind K.  At its top a wave waits for its own
   // copies (K of tile i, V of tile i - 1); the barrier makes everybody's visible and retires the reads of iteration i - 1, whose slots this
@@ -481,16 +469,15 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
     const bool on = cur && tile * 64 < wave_end;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     asm volatile("" : "+v"(win_next));                         // asked for iterations ago
-#pragma unroll
-    for (int c = 0; c < NID; c++) id_v[c] = id_k[c];
+    id_v = id_k;
     if (((tile + 1) * 64 >> a.page_log) - wbase >= 64) {
       wbase += 64;
       win = win_next;
       win_next = window(wbase + 64);
     }
-    ids_of(tile + 1, id_k);
+    id_k = id_of(tile + 1);
     aim_k(tile + 1);
-    aim_v(tile);
+    v_rs = rows_from(vb, vp2, vt2, id_v, tile * 64 + row0, it.n);
     if (pend && __builtin_expect(__any(tmax_old > m_run + kPagedLazy), 0)) {
       const float m_new = fmaxf(m_run, fmaxf(tmax_old, __shfl_xor(tmax_old, 32)));
       const float use = m_new == -INFINITY ? 0.f : m_new;
@@ -525,8 +512,8 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
       pb[g][k & 3] = w;
     };
     auto copies = [&](int c) {
-      if (c < C::COPIES) copy_k(tile + 1, c, P ^ 1);
-      else if (c < 2 * C::COPIES) copy_v(tile, c - C::COPIES, P);
+      if (c < C::COPIES) copy_k(c, P ^ 1);
+      else if (c < 2 * C::COPIES) copy_v(c - C::COPIES, P);
     };
     bf16x8 vf[NS];
     auto first_product = [&](auto e_tag) {
@@ -832,11 +819,9 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
   a.part_o = (float*)(ws + ws_align(recs * 8));
   const dim3 grid((unsigned)((a.wgs ? a.wgs : items) * a.h_kv)), blk(256);
   if (big) {
-    static LdsOptIn opt_in[2];
-    const bool small = a.page_log < 6;
-    auto kern = small ? paged_rows_kernel<D, true> : paged_rows_kernel<D, false>;
-    if (hipError_t e = allow_dyn_lds((const void*)kern, RowsCfg<D>::LDS_BYTES, opt_in[small]); e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, grid, blk, RowsCfg<D>::LDS_BYTES, st, a);
+    static LdsOptIn opt_in;
+    if (hipError_t e = allow_dyn_lds((const void*)paged_rows_kernel<D>, RowsCfg<D>::LDS_BYTES, opt_in); e != hipSuccess) return e;
+    hipLaunchKernelGGL(paged_rows_kernel<D>, grid, blk, RowsCfg<D>::LDS_BYTES, st, a);
   } else if (dtype == DASH_BF16) {
     static LdsOptIn opt_in;
     if (hipError_t e = allow_dyn_lds((const void*)paged_few_kernel<D>, FewCfg<D>::LDS_BYTES, opt_in); e != hipSuccess) return e;
