@@ -102,6 +102,16 @@ __device__ __forceinline__ int wave_scan(int v) {
   return v;
 }
 
+// agent-scope accesses to the split records (8 bytes at a time): they bypass the caches that
+// are not shared by the whole device
+__device__ __forceinline__ void agent_store(float* p, float a, float b) {
+  const uint64_t w = (uint64_t)__float_as_uint(a) | ((uint64_t)__float_as_uint(b) << 32);
+  __hip_atomic_store(reinterpret_cast<uint64_t*>(p), w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t agent_load(const void* p) {
+  return __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
 __device__ __forceinline__ uint32_t lane_id() { return threadIdx.x & 63u; }
 
 // One wave: ORs the mask rows of consecutive tokens (n = tokens * words consecutive words) into

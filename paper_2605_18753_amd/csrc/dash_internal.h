@@ -99,6 +99,7 @@ hipError_t launch_kbar_summarize_bwd(const dash_params& p, const Layout& L, cons
 hipError_t launch_decode_s2(const dash_params& p, const Layout& L, const void* q, const void* k,
                             const void* v, void* o, const uint32_t* mask, const float* bias,
                             char* ws, bool dense, hipStream_t st);
+uint64_t next_nonce();     // a number that no other call of this process uses, for split flags
 bool decode_scores_apart(const dash_params& p, const Layout& L);
 int decode_scores_ld(const Layout& L);
 bool decode_route_applicable(const dash_params& p, const Layout& L, size_t ws_bytes);

@@ -10,7 +10,8 @@
 //   workgroups, parts of S = ceil(sum c_i / (W - n)) give sum ceil(c_i / S) <= W of them.  (Equal runs for these as well: a run begins anew for every
 //   piece of an item, and most are cut.  1501 tokens beside seven decoding sequences of up to 12k 305 -> 309 us and the records to add
 //   up, 2048 tokens against 32k 995 -> 1088.)
-// Cut items leave records, which a second launch adds up.
+// Cut items leave records.  Of parts a second launch adds them up; of runs the workgroup whose record of an item is complete last, which
+// sees the flags of all (stored past the caches, as in decode_body.h; who merges clears them, so a captured launch can be replayed).
 #pragma once
 #include "common.h"
 #include "dash_internal.h"
@@ -28,6 +29,7 @@ struct PagedArgs {
   float c1;                              // scale * log2(e)
   int wgs;                               // runs of a kv-head; 0: an item a workgroup.  Tiles of 128 rows: parts of a kv-head at most; 0: none is cut
   float* part_o; float* part_ml;         // records of cut items: two of each run (the item it begins in, the one it ends in), one of each part
+  uint64_t* flags; uint64_t nonce;       // runs: of each record, and the number that says that it is complete
 };
 
 __device__ __forceinline__ int paged_len(const PagedArgs& a, int b) { return min(max(a.lens[b], 0), a.cap); }
@@ -212,7 +214,7 @@ struct PagedRun {
   PagedDeal deal;
   PagedItem it;
   int x0, x1, cost;
-  int next, end;                                           // the step behind this piece, the run's end
+  int next, end, total;                                    // the step behind this piece, the run's end, the steps of the kv-head
   __device__ __forceinline__ PagedRun(const PagedArgs& a) : deal(a) {}
   __device__ __forceinline__ bool begin(const PagedArgs& a, int wg) {
     if (a.wgs == 0) {
@@ -221,7 +223,8 @@ struct PagedRun {
       x1 = cost = deal.steps(it.s, it.tile);
       return true;
     }
-    const PagedBounds<int> b(a, deal.total(a));
+    total = deal.total(a);
+    const PagedBounds<int> b(a, total);
     next = __builtin_amdgcn_readfirstlane(b.at(wg));
     end = __builtin_amdgcn_readfirstlane(b.at(wg + 1));
     if (next >= end) return false;

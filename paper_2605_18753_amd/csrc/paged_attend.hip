@@ -75,15 +75,18 @@ __device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const Paged
 #pragma unroll
     for (int e = 0; e < 4; e++) o[j * 4 + e] = s[e];
   }
-  if (!run.whole()) {
-    float* po = a.part_o + (rec * 16 + row) * D;
-#pragma unroll
-    for (int j = 0; j < D / 64; j++) *reinterpret_cast<f32x4*>(po + j * 64 + c * 4) = f32x4{o[j * 4], o[j * 4 + 1], o[j * 4 + 2], o[j * 4 + 3]};
-    if (c == 0) reinterpret_cast<float2*>(a.part_ml)[rec * 16 + row] = make_float2(M, den);
-    return;
-  }
   const int t = t0 + row / a.g, head = r * a.g + row % a.g;
   if (t >= it.m) return;
+  if (!run.whole()) {
+    float* po = a.part_o + (rec * 16 + row) * D + c * 4;
+#pragma unroll
+    for (int j = 0; j < D / 64; j++) {
+      agent_store(po + j * 64, o[j * 4], o[j * 4 + 1]);
+      agent_store(po + j * 64 + 2, o[j * 4 + 2], o[j * 4 + 3]);
+    }
+    if (c == 0) agent_store(a.part_ml + (rec * 16 + row) * 2, M, den);
+    return;
+  }
   const float inv = den > 0.f ? 1.f / den : den == 0.f ? 0.f : den;     // NaN stays
   T* op = (T*)a.o + (it.r0 + t) * a.o_t + head * a.o_h;
 #pragma unroll
@@ -92,6 +95,87 @@ __device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const Paged
   if (a.lse && c == 0) a.lse[(int64_t)(it.r0 + t) * a.h_q + head] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
 }
 
+// Behind a piece of an item that is cut between runs: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p, by the workgroup that sees the flags
+// of all its pieces.  They are those of runs w1, w1 + 1, ..; the first left its run's second record, the others their runs' first.  D / 4 threads
+// a row, 4 values each, and where the item has few rows several groups of threads that take every so manieth piece.  (A launch of its
+// own for this: one sequence of 1000 tokens, 32 / 8 heads, 11.1 us a step instead of 9.7.)
+template <typename T, int D, int THREADS>
+__device__ __forceinline__ void paged_few_join(const PagedArgs& a, const PagedRun& run, int r, int wg, char* lds) {
+  constexpr int TPR = D / 4, UNITS = THREADS / TPR;        // threads of a row; rows at a time
+  const PagedItem& it = run.it;
+  f32x4* xo = reinterpret_cast<f32x4*>(lds);               // [THREADS], [UNITS], [1]
+  float* xd = reinterpret_cast<float*>(xo + THREADS);
+  int* all = reinterpret_cast<int*>(xd + UNITS);
+  const int lane = threadIdx.x & 63, begin = run.next - run.x1, end = begin + run.cost;
+  const PagedBounds<int> bounds(a, run.total);
+  int w1 = wg, pieces = 1;
+  for (int k0 = wg; k0 > 0; k0 -= 64) {
+    const int more = __popcll(__ballot(k0 - lane > 0 && bounds.at(max(k0 - lane, 0)) > begin));
+    w1 -= more;
+    pieces += more;
+    if (more < 64) break;
+  }
+  for (int k0 = wg + 1; k0 < bounds.runs; k0 += 64) {
+    const int more = __popcll(__ballot(k0 + lane < bounds.runs && bounds.at(k0 + lane) < end));
+    pieces += more;
+    if (more < 64) break;
+  }
+  const int64_t rec0 = ((int64_t)r * a.wgs + w1) * 2;
+  auto record = [&](int p) { return p == 0 ? rec0 + 1 : rec0 + 2 * p; };
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // the record is in memory ...
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    if (lane == 0) __hip_atomic_store(a.flags + record(wg - w1), a.nonce, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // ... before its flag, and that before the flags are read
+    bool seen = true;
+    for (int p = lane; p < pieces; p += 64) seen &= agent_load(a.flags + record(p)) == a.nonce;
+    const bool ok = __all(seen);
+    if (lane == 0) *all = ok;
+  }
+  __syncthreads();
+  if (!*all) return;
+  const int rows = min(run.deal.T, it.m - it.tile * run.deal.T) * a.g;
+  const int slices = rows * 4 <= UNITS ? 4 : rows * 2 <= UNITS ? 2 : 1, per = UNITS / slices;
+  const int c = threadIdx.x % TPR, unit = threadIdx.x / TPR, slice = unit / per;
+  for (int i0 = 0; i0 < rows; i0 += per) {
+    const int in = min(i0 + unit % per, rows - 1);
+    const float* ml = a.part_ml + in * 2;
+    float M = -INFINITY, den = 0.f;
+    for (int p = c; p < pieces; p += TPR)                  // c-th piece of TPR a thread's
+      M = fmaxf(M, __uint_as_float((uint32_t)agent_load(ml + record(p) * 32)));
+    M = row16_reduce(M, OpMax());
+    if constexpr (TPR == 32) M = fmaxf(M, __shfl_xor(M, 16));
+    const float use = M == -INFINITY ? 0.f : M;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    const float* po = a.part_o + in * D + c * 4;
+#pragma unroll 4
+    for (int p = slice; p < pieces; p += slices) {
+      const uint64_t y = agent_load(ml + record(p) * 32), v0 = agent_load(po + record(p) * (16 * D)), v1 = agent_load(po + record(p) * (16 * D) + 2);
+      const float w = __builtin_amdgcn_exp2f(__uint_as_float((uint32_t)y) - use);
+      den = fmaf(w, __uint_as_float((uint32_t)(y >> 32)), den);
+      o[0] = fmaf(w, __uint_as_float((uint32_t)v0), o[0]);
+      o[1] = fmaf(w, __uint_as_float((uint32_t)(v0 >> 32)), o[1]);
+      o[2] = fmaf(w, __uint_as_float((uint32_t)v1), o[2]);
+      o[3] = fmaf(w, __uint_as_float((uint32_t)(v1 >> 32)), o[3]);
+    }
+    if (slices > 1) {
+      __syncthreads();
+      xo[threadIdx.x] = o;
+      if (c == 0) xd[unit] = den;
+      __syncthreads();
+      for (int k = 1; k < slices && slice == 0; k++) {
+        o += xo[threadIdx.x + k * per * TPR];
+        den += xd[unit + k * per];
+      }
+    }
+    if (slice > 0 || i0 + unit >= rows) continue;
+    const float inv = den > 0.f ? 1.f / den : den == 0.f ? 0.f : den;
+    const int row = it.r0 + it.tile * run.deal.T + in / a.g, head = r * a.g + in % a.g;
+    put_row4((T*)a.o + row * a.o_t + head * a.o_h + c * 4, o, inv);
+    if (a.lse && c == 0) a.lse[(int64_t)row * a.h_q + head] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
+  }
+  for (int p = threadIdx.x; p < pieces; p += THREADS) __hip_atomic_store(a.flags + record(p), (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
 
 template <int D>
 __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs args) {
@@ -245,6 +329,7 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs args) {
   }
   __syncthreads();
   paged_few_finish<uint16_t, D, 4>(a, run, r, ((int64_t)r * a.wgs + wg) * 2 + (run.x0 == 0), t0, x, ml);
+  if (!run.whole()) paged_few_join<uint16_t, D, 256>(a, run, r, wg, lds);
   __syncthreads();
   } while (run.advance(args));
 }
@@ -337,6 +422,7 @@ __global__ __launch_bounds__(512) void paged_few_f32_kernel(PagedArgs args) {
   }
   __syncthreads();
   paged_few_finish<float, D, 8>(a, run, r, ((int64_t)r * a.wgs + wg) * 2 + (run.x0 == 0), t0, x, ml);
+  if (!run.whole()) paged_few_join<float, D, 512>(a, run, r, wg, lds);
   __syncthreads();
   } while (run.advance(args));
 }
@@ -639,73 +725,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
   }
 }
 
-// Adds up items cut between runs: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  The begin of run w lies inside an item whose first
-// piece is run w - 1's (its second record); the pieces of the runs behind it that begin inside the item follow (their first records).
-// D / 4 threads a row, 4 values each, and where the item has few rows several groups of threads that take every so manieth piece.
-template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedArgs a) {
-  constexpr int TPR = D / 4, UNITS = 256 / TPR;            // threads of a row; rows at a time
-  __shared__ f32x4 xo[256];
-  __shared__ float xd[UNITS];
-  const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv + 1, lane = threadIdx.x & 63;
-  const PagedDeal deal(a);
-  const int total = deal.total(a);
-  const PagedBounds<int> bounds(a, total);
-  const int f = __builtin_amdgcn_readfirstlane(bounds.at(wg));
-  if (f >= total) return;
-  PagedItem it;
-  const int x = deal.find(a, f, true, it), begin = f - x, end = begin + deal.steps(it.s, it.tile);
-  if (x == 0 || bounds.at(wg - 1) > begin) return;         // not cut here, or not for the first time
-  int pieces = 1;                                          // runs wg - 1 .. wg - 2 + pieces
-  for (int k0 = wg; k0 < bounds.runs; k0 += 64) {
-    const int more = __popcll(__ballot(k0 + lane < bounds.runs && bounds.at(k0 + lane) < end));
-    pieces += more;
-    if (more < 64) break;
-  }
-  const int64_t rec0 = ((int64_t)r * a.wgs + wg - 1) * 2;
-  auto record = [&](int p) { return p == 0 ? rec0 + 1 : rec0 + 2 * p; };
-  const int rows = min(deal.T, it.m - it.tile * deal.T) * a.g;
-  const int slices = rows * 4 <= UNITS ? 4 : rows * 2 <= UNITS ? 2 : 1, per = UNITS / slices;
-  const int c = threadIdx.x % TPR, unit = threadIdx.x / TPR, slice = unit / per;
-  for (int i0 = 0; i0 < rows; i0 += per) {
-    const int in = min(i0 + unit % per, rows - 1);
-    const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + in;
-    float M = -INFINITY, den = 0.f;
-    for (int p = c; p < pieces; p += TPR)                  // c-th piece of TPR a thread's
-      M = fmaxf(M, ml[record(p) * 16].x);
-    M = row16_reduce(M, OpMax());
-    if constexpr (TPR == 32) M = fmaxf(M, __shfl_xor(M, 16));
-    const float use = M == -INFINITY ? 0.f : M;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o) + in * (D / 4) + c;
-#pragma unroll 8
-    for (int p = slice; p < pieces; p += slices) {
-      const float2 y = ml[record(p) * 16];
-      const f32x4 v = po[record(p) * 16 * (D / 4)];
-      const float w = __builtin_amdgcn_exp2f(y.x - use);
-      den = fmaf(w, y.y, den);
-#pragma unroll
-      for (int e = 0; e < 4; e++) o[e] = fmaf(w, v[e], o[e]);
-    }
-    if (slices > 1) {
-      __syncthreads();
-      xo[threadIdx.x] = o;
-      if (c == 0) xd[unit] = den;
-      __syncthreads();
-      for (int k = 1; k < slices && slice == 0; k++) {
-        o += xo[threadIdx.x + k * per * TPR];
-        den += xd[unit + k * per];
-      }
-    }
-    if (slice > 0 || i0 + unit >= rows) continue;
-    const float inv = den > 0.f ? 1.f / den : den == 0.f ? 0.f : den;
-    const int row = it.r0 + it.tile * deal.T + in / a.g, head = r * a.g + in % a.g;
-    put_row4((T*)a.o + row * a.o_t + head * a.o_h + c * 4, o, inv);
-    if (a.lse && c == 0) a.lse[(int64_t)row * a.h_q + head] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
-  }
-}
-
-// The same for tiles of 128 rows cut into parts.  A workgroup adds 256 / (D / 4) / SLICES (token, head) rows at a time, SLICES groups of threads
+// Adds up the parts of tiles of 128 rows: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  A workgroup adds 256 / (D / 4) / SLICES (token, head) rows at a time, SLICES groups of threads
 // each taking every SLICES-th part.
 template <int D, int SLICES>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
@@ -802,7 +822,7 @@ static size_t ws_align(size_t x) { return (x + 255) & ~(size_t)255; }
 size_t paged_attend_ws(const PagedArgs& a, int dtype, int d) {
   const size_t few = (size_t)runs_of(a, dtype, d, false) * a.h_kv * 2 * 16;    // rows of records
   const size_t rows = dtype == DASH_BF16 ? (size_t)runs_of(a, dtype, d, true) * a.h_kv * 128 : 0, recs = few > rows ? few : rows;
-  return ws_align(recs * 8) + recs * d * 4;
+  return ws_align(recs * 8) + recs * d * 4 + few / 16 * 8;
 }
 
 template <int D>
@@ -817,6 +837,8 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
   const size_t recs = (size_t)a.wgs * a.h_kv * (big ? 128 : 2 * 16);
   a.part_ml = (float*)ws;
   a.part_o = (float*)(ws + ws_align(recs * 8));
+  a.flags = (uint64_t*)((char*)a.part_o + recs * D * 4);     // runs only
+  a.nonce = big ? 0 : next_nonce();
   const dim3 grid((unsigned)((a.wgs ? a.wgs : items) * a.h_kv)), blk(256);
   if (big) {
     static LdsOptIn opt_in;
@@ -833,18 +855,12 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
     hipLaunchKernelGGL(paged_few_f32_kernel<D>, grid, dim3(512), lds, st, a);
   }
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.wgs <= 1) return e;
-  if (big) {
-    // few rows leave the chip idle unless several groups of threads share a row's parts
-    const int64_t out = (int64_t)a.n_rows * a.h_q;
-    constexpr int units = 256 / (D / 4);
-    if (out <= 8192) hipLaunchKernelGGL((paged_merge_kernel<D, 4>), dim3((unsigned)((out + units / 4 - 1) / (units / 4))), blk, 0, st, a);
-    else hipLaunchKernelGGL((paged_merge_kernel<D, 1>), dim3(2048), blk, 0, st, a);
-  } else {
-    const dim3 joins((unsigned)((a.wgs - 1) * a.h_kv));
-    if (dtype == DASH_BF16) hipLaunchKernelGGL((paged_join_kernel<uint16_t, D>), joins, blk, 0, st, a);
-    else hipLaunchKernelGGL((paged_join_kernel<float, D>), joins, blk, 0, st, a);
-  }
+  if (e != hipSuccess || a.wgs <= 1 || !big) return e;
+  // few rows leave the chip idle unless several groups of threads share a row's parts
+  const int64_t out = (int64_t)a.n_rows * a.h_q;
+  constexpr int units = 256 / (D / 4);
+  if (out <= 8192) hipLaunchKernelGGL((paged_merge_kernel<D, 4>), dim3((unsigned)((out + units / 4 - 1) / (units / 4))), blk, 0, st, a);
+  else hipLaunchKernelGGL((paged_merge_kernel<D, 1>), dim3(2048), blk, 0, st, a);
   return hipGetLastError();
 }
 

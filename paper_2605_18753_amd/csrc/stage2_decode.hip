@@ -18,7 +18,7 @@ hipError_t launch_decode_route_m4(const DecArgs& a, int head_dim, unsigned grid,
 
 // A number for the split flags that no other call of this process uses and that left-over
 // memory does not hold: a counter started from the clock, mixed (splitmix64).
-static uint64_t next_nonce() {
+uint64_t next_nonce() {
   static std::atomic<uint64_t> count{(uint64_t)std::chrono::steady_clock::now().time_since_epoch().count() << 20};
   uint64_t z = count.fetch_add(1, std::memory_order_relaxed) * 0x9e3779b97f4a7c15ull + 0x9e3779b97f4a7c15ull;
   z = (z ^ (z >> 30)) * 0xbf58476d1ce4e5b9ull;
