@@ -55,20 +55,24 @@ __device__ __forceinline__ int paged_page_lane(const PagedArgs& a, int b, int i)
 constexpr int kMinPart = 4;                                // steps a part has at least
 struct PagedPart { int b, tile, part, parts, rec0, r0, m, n; };   // rec0: the item's first part among those of the kv-head
 
-// The size S of a part; a wave's lanes together.  shape(m, n) gives a sequence's tiles and the cost of one (at least 1).
+// The size S of a part, no item costing more: none is cut; a wave's lanes together.  shape(m, n) gives a sequence's tiles and the cost
+// of one (at least 1).
+constexpr int kUncut = 0x3fffffff;
 template <typename F> __device__ __forceinline__ int paged_part_size(const PagedArgs& a, F&& shape) {
-  if (a.wgs <= 0) return 0x3fffffff;
+  if (a.wgs <= 0) return kUncut;
   const int lane = lane_id();
   int items = 0;
-  float cost = 0.f;
+  float cost = 0.f, most = 0.f;
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
     int2 s = make_int2(0, 0);
     if (i0 + lane < a.batch) s = shape(paged_rows(a, i0 + lane).y, paged_len(a, i0 + lane));
     items += __builtin_amdgcn_readlane(wave_scan(s.x), 63);
     cost += wave_sum((float)s.x * (float)s.y);
+    most = fmaxf(most, wave_max(s.x > 0 ? (float)s.y : 0.f));
   }
-  if (items >= a.wgs) return 0x3fffffff;
-  return max((int)fminf(cost * 1.0001f / (float)(a.wgs - items), 1e9f) + 1, kMinPart);   // the factor covers the sum's rounding
+  if (items >= a.wgs) return kUncut;
+  const int S = max((int)fminf(cost * 1.0001f / (float)(a.wgs - items), 1e9f) + 1, kMinPart);   // the factor covers the sum's rounding
+  return (float)S >= most ? kUncut : S;
 }
 
 // Every lane of a wave: part `idx` of a kv-head.

@@ -735,6 +735,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
   const int lane = threadIdx.x & 63, c = threadIdx.x % TPR, unit = threadIdx.x / TPR, slice = unit / PER;
   const auto shape = [&](int m, int n) { return rows_shape(a, m, n); };
   const int S = paged_part_size(a, shape);
+  if (S == kUncut) return;
   // rows in the order kv-head, token, head of the group: neighbours lie side by side in the records
   const int64_t per = (int64_t)a.n_rows * a.g, all = per * a.h_kv;
   for (int64_t g0 = (int64_t)blockIdx.x * PER; g0 < all; g0 += (int64_t)gridDim.x * PER) {
@@ -742,7 +743,6 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
     const int r = (int)(gr / per), row = (int)(gr % per) / a.g, hg = (int)(gr % per) % a.g;
     // the dealing of the launch before, for a given row
     int first = 0, parts = 0, tiles = 0, r0 = 0, base = 0;
-    bool any = false;                                      // whether an item of the call is cut
     for (int i0 = 0; i0 < a.batch; i0 += 64) {
       int2 s = make_int2(0, 0), rm = make_int2(0, 0);
       if (i0 + lane < a.batch) {
@@ -750,7 +750,6 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
         s = shape(rm.y, paged_len(a, i0 + lane));
       }
       const int np = (s.y + S - 1) / S, incl = wave_scan(s.x * np);
-      any |= __any(s.x > 0 && np > 1);
 #pragma unroll
       for (int k = 0; k < 64 / TPR; k++) {
         const int want = __builtin_amdgcn_readlane(row, k * TPR);
@@ -764,7 +763,6 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
       }
       base += __builtin_amdgcn_readlane(incl, 63);
     }
-    if (!any) return;
     const bool mine = parts > 1 && g0 + unit % PER < all;
     float M = -INFINITY, den = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -860,7 +858,7 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
   const int64_t out = (int64_t)a.n_rows * a.h_q;
   constexpr int units = 256 / (D / 4);
   if (out <= 8192) hipLaunchKernelGGL((paged_merge_kernel<D, 4>), dim3((unsigned)((out + units / 4 - 1) / (units / 4))), blk, 0, st, a);
-  else hipLaunchKernelGGL((paged_merge_kernel<D, 1>), dim3(2048), blk, 0, st, a);
+  else hipLaunchKernelGGL((paged_merge_kernel<D, 1>), dim3(1024), blk, 0, st, a);
   return hipGetLastError();
 }
 
