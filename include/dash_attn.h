@@ -366,7 +366,8 @@ int dash_paged_attend(const dash_paged_params* p, const void* q, const void* k_p
 
 /* Adds the weight that the new tokens' attention gives to every cached token of their sequences: weights[token, kv-head] +=
  * the sum over the rows that see it and the heads of its group of e^(logit - lse), lse as dash_paged_attend wrote it.
- * last > 0: only the last `last` new tokens of each sequence weigh (an observation window); 0: all. */
+ * last > 0: only the last `last` new tokens of each sequence weigh (an observation window); 0: all.  Pages that several
+ * sequences of the call share get the weight of all of them, added in no fixed order. */
 int dash_paged_weigh(const dash_paged_params* p, const void* q, const void* k_pages, const int32_t* row_start,
                      const int32_t* lens, const int32_t* table, const float* lse, int32_t last, float* weights,
                      void* workspace, size_t workspace_bytes, void* stream);

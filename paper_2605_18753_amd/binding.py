@@ -354,7 +354,7 @@ def make_paged_params(cache: PagedCache, n_rows: int, h_q: int, causal: bool = T
     return p
 
 
-def _paged_call(p: dash_paged_params, cache: PagedCache, row_start, rows, extra=()) -> dash_paged_params:
+def _paged_call(p: dash_paged_params, cache: PagedCache, row_start, rows, extra=(), ws=None) -> dash_paged_params:
     """The call's own copy of p, with the strides of its packed tensors; rows: (tensor, heads, field of its strides)."""
     p = dash_paged_params.from_buffer_copy(p)
     n_rows, head_dim, dtype, dev = p.n_rows, p.head_dim, cache.k.dtype, cache.k.get_device()
@@ -372,7 +372,9 @@ def _paged_call(p: dash_paged_params, cache: PagedCache, row_start, rows, extra=
             raise DashError(f"expected a contiguous {want} tensor of shape {tuple(shape)} on the cache's device")
     if cache.table.get_device() != dev or cache.lens.get_device() != dev:
         raise DashError("the cache's tensors lie on one device")
-    if dev >= 0 and _device is not None and dev != _device():
+    if dev < 0 or (ws is not None and ws.get_device() != dev):
+        raise DashError("the cache and the workspace lie on one GPU")
+    if _device is not None and dev != _device():
         raise DashError(f"the cache lies on cuda:{dev}, which is not the current device")
     return p
 
@@ -401,7 +403,7 @@ def dash_paged_append(p: dash_paged_params, cache: PagedCache, k_new, v_new, row
 
 def dash_paged_attend(p: dash_paged_params, cache: PagedCache, q, row_start, o, ws: torch.Tensor, lse=None) -> None:
     """q, o [n_rows, h_q, d]; lse fp32 [n_rows, h_q] or None."""
-    p = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"), (o, p.h_q, "o_stride")), ((lse, torch.float32, (p.n_rows, p.h_q)),))
+    p = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"), (o, p.h_q, "o_stride")), ((lse, torch.float32, (p.n_rows, p.h_q)),), ws)
     wp, wn = _ws_ptr(ws)
     _check(load_library().dash_paged_attend(p, _ptr(q), _ptr(cache.k), _ptr(cache.v), _ptr(row_start), _ptr(cache.lens), _ptr(cache.table),
                                             _ptr(o), _ptr(lse), wp, wn, _stream()), "dash_paged_attend")
@@ -412,7 +414,7 @@ def dash_paged_weigh(p: dash_paged_params, cache: PagedCache, q, row_start, lse,
     if cache.weights is None or lse is None:
         raise DashError("dash_paged_weigh needs the cache's weights and the rows' lse")
     p = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"),),
-                ((lse, torch.float32, (p.n_rows, p.h_q)), (cache.weights, torch.float32, cache.k.shape[:3])))
+                ((lse, torch.float32, (p.n_rows, p.h_q)), (cache.weights, torch.float32, cache.k.shape[:3])), ws)
     wp, wn = _ws_ptr(ws)
     _check(load_library().dash_paged_weigh(p, _ptr(q), _ptr(cache.k), _ptr(row_start), _ptr(cache.lens), _ptr(cache.table), _ptr(lse), last,
                                            _ptr(cache.weights), wp, wn, _stream()), "dash_paged_weigh")
@@ -424,7 +426,7 @@ def dash_paged_evict(p: dash_paged_params, cache: PagedCache, budget: int, ws: t
         raise DashError("dash_paged_evict needs the cache's weights, pos and seen")
     tok = cache.k.shape[:3]
     p = _paged_call(p, cache, None, (), ((cache.weights, torch.float32, tok), (cache.pos, torch.int32, tok),
-                                     (cache.seen, torch.int32, cache.lens.shape), (src, torch.int32, (p.batch, p.h_kv, budget))))
+                                     (cache.seen, torch.int32, cache.lens.shape), (src, torch.int32, (p.batch, p.h_kv, budget))), ws)
     wp, wn = _ws_ptr(ws)
     _check(load_library().dash_paged_evict(p, _ptr(cache.k), _ptr(cache.v), _ptr(cache.lens), _ptr(cache.seen), _ptr(cache.table),
                                            _ptr(cache.weights), _ptr(cache.pos), budget, sinks, recent, _ptr(src), wp, wn, _stream()),

@@ -82,7 +82,7 @@ struct EvictArgs {
   PagedArgs a;
   int budget, sinks, recent;
   int32_t* lens; int32_t* src;
-  uint32_t* keys;      // [pair][cap]
+  uint32_t* keys;      // [pair][cap], caches of more than kSelKeys slots only
   int32_t* moves;      // [pair][cap]: the targets from the front, the sources from the back
   int32_t* counts;     // [pair]
 };
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(256) void paged_move_kernel(EvictArgs e, int wgs) {
 static size_t evict_align(size_t x) { return (x + 255) & ~(size_t)255; }
 size_t paged_evict_ws(const PagedArgs& a) {
   const size_t pairs = (size_t)a.batch * a.h_kv;
-  return evict_align(pairs * 4) + 2 * evict_align(pairs * a.cap * 4);
+  return evict_align(pairs * 4) + evict_align(pairs * a.cap * 4) * (a.cap > kSelKeys ? 2 : 1);
 }
 
 hipError_t launch_paged_evict(const PagedArgs& a, int elem, int d, int32_t* lens, int budget, int sinks, int recent, int32_t* src,
@@ -370,8 +370,8 @@ hipError_t launch_paged_evict(const PagedArgs& a, int elem, int d, int32_t* lens
   e.a = a; e.budget = budget; e.sinks = sinks; e.recent = recent; e.lens = lens; e.src = src;
   const size_t pairs = (size_t)a.batch * a.h_kv;
   e.counts = (int32_t*)ws;
-  e.keys = (uint32_t*)(ws + evict_align(pairs * 4));
-  e.moves = (int32_t*)(ws + evict_align(pairs * 4) + evict_align(pairs * a.cap * 4));
+  e.moves = (int32_t*)(ws + evict_align(pairs * 4));
+  e.keys = (uint32_t*)(ws + evict_align(pairs * 4) + evict_align(pairs * a.cap * 4));   // of caches that LDS may have no room for
   const int room = a.cap < kSelKeys ? a.cap : kSelKeys;
   static LdsOptIn opt_in;
   if (hipError_t r = allow_dyn_lds((const void*)paged_select_kernel, (size_t)room * 4, opt_in); r != hipSuccess) return r;

@@ -9,6 +9,8 @@
 //
 // (block of keys, row tile) pairs of all sequences are dealt evenly to a fixed number of workgroups; blocks cut between two of them
 // are added up by a second launch, in a fixed order.
+// A token's weight gets one addition a call, atomic without a result: nothing waits for the old value, and pages that several sequences
+// share get the weight of all of them (only then in no fixed order).
 #include "f32_tiles.h"
 #include "lds_copy.h"
 #include "paged.h"
@@ -201,7 +203,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : D == 128 ? 3 : 4) void pa
       const int key = key0 + 16 * j + 4 * kq + n;
       if (n < 4) {
         if (!whole) rec[16 * j] = w;                           // an item cut between runs
-        else if (key < it.n && (uint32_t)page[j] < (uint32_t)a.n_pages) a.weights[(((int64_t)page[j] * a.h_kv + r) << a.page_log) + (key & pm)] += w;
+        else if (key < it.n && (uint32_t)page[j] < (uint32_t)a.n_pages) unsafeAtomicAdd(a.weights + ((((int64_t)page[j] * a.h_kv + r) << a.page_log) + (key & pm)), w);
       }
     }
     if ((todo -= take) <= 0) return;
@@ -229,7 +231,7 @@ __global__ __launch_bounds__(kWeighKeys<T>) void paged_weigh_sum_kernel(PagedArg
   const int key = it.block * kWeighKeys<T> + threadIdx.x;
   if (key >= it.n) return;
   const uint32_t page = (uint32_t)a.table[(int64_t)it.b * a.max_pages + (key >> a.page_log)];
-  if (page < (uint32_t)a.n_pages) a.weights[(((int64_t)page * a.h_kv + r) << a.page_log) + (key & ((1 << a.page_log) - 1))] += w;
+  if (page < (uint32_t)a.n_pages) unsafeAtomicAdd(a.weights + ((((int64_t)page * a.h_kv + r) << a.page_log) + (key & ((1 << a.page_log) - 1))), w);
 }
 
 // Few rows a sequence (decode): K is streamed once, the next block's keys asked for before the present one's are used.  Whole blocks
@@ -257,12 +259,7 @@ __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a)
     f++;
     if (++x.block >= x.s.items) weigh_find<KEYS>(a, f, x, true);
   };
-  // lane (n, kq), n < 4, takes key 4 kq + n of 16 (the others, and those behind the end, some key of the page)
-  auto place = [&](const WeighItem& x, int page, int key16) {
-    return (((int64_t)paged_clamp(a, page) * a.h_kv + r) << a.page_log) + ((key16 + 4 * kq + (n & 3)) & pm);
-  };
-  // A block's keys, and what its keys weigh so far: asked for behind the keys of the next block, that would be waited for with them.
-  auto load_keys = [&](const WeighItem& x, Tile (&kf)[SUBS], int (&page)[SUBS], float (&was)[SUBS]) {
+  auto load_keys = [&](const WeighItem& x, Tile (&kf)[SUBS], int (&page)[SUBS]) {
     const int key0 = x.block * KEYS + wave * SUBS * 16;
 #pragma unroll
     for (int s = 0; s < SUBS; s++) page[s] = paged_entry(a, x.b, min(key0 + 16 * s, (x.n - 1) & ~15) >> a.page_log);
@@ -271,8 +268,6 @@ __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a)
       const int key = min(min(key0 + 16 * s, (x.n - 1) & ~15) + n, x.n - 1);
       kf[s].load((const T*)a.k + (int64_t)paged_clamp(a, page[s]) * a.kp_p + r * a.kp_h + (int64_t)(key & pm) * a.kp_t, kq);
     }
-#pragma unroll
-    for (int s = 0; s < SUBS; s++) was[s] = a.weights[place(x, page[s], key0 + 16 * s)];
   };
   Tile qf;
   float off = 0.f;
@@ -290,7 +285,7 @@ __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a)
       off = -INFINITY;
     }
   };
-  auto work = [&](const WeighItem& x, const Tile (&kf)[SUBS], const int (&page)[SUBS], const float (&was)[SUBS]) {
+  auto work = [&](const WeighItem& x, const Tile (&kf)[SUBS], const int (&page)[SUBS]) {
     const int key0 = x.block * KEYS + wave * SUBS * 16, back = x.n - x.m;
     f32x4 acc[SUBS];
 #pragma unroll
@@ -319,27 +314,26 @@ __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a)
       for (int e = 0; e < 4; e++) acc[j][e] = row16_sum(acc[j][e]);
       const float w = n == 0 ? acc[j][0] : n == 1 ? acc[j][1] : n == 2 ? acc[j][2] : acc[j][3];
       const int key = key0 + 16 * j + 4 * kq + n;
-      if (n < 4 && key < x.n && (uint32_t)page[j] < (uint32_t)a.n_pages) a.weights[place(x, page[j], key0 + 16 * j)] = was[j] + w;
+      if (n < 4 && key < x.n && (uint32_t)page[j] < (uint32_t)a.n_pages) unsafeAtomicAdd(a.weights + ((((int64_t)page[j] * a.h_kv + r) << a.page_log) + (key & pm)), w);
     }
   };
   Tile ka[SUBS], kb[SUBS];
   int pa[SUBS], pb[SUBS];
-  float wa[SUBS], wb[SUBS];
-  load_keys(it, ka, pa, wa);
+  load_keys(it, ka, pa);
   while (true) {
     next = it;
     if (todo > 1) {
       advance(next);
-      load_keys(next, kb, pb, wb);
+      load_keys(next, kb, pb);
     }
-    work(it, ka, pa, wa);
+    work(it, ka, pa);
     if (--todo == 0) return;
     it = next;
     if (todo > 1) {
       advance(next);
-      load_keys(next, ka, pa, wa);
+      load_keys(next, ka, pa);
     }
-    work(it, kb, pb, wb);
+    work(it, kb, pb);
     if (--todo == 0) return;
     it = next;
   }

@@ -292,6 +292,13 @@ def test_the_rows_outside_the_window_weigh_nothing_whatever_they_hold(dtype):
     assert torch.equal(s.gpu.weights.cpu(), want)
 
 
+def test_weights_of_pages_that_sequences_share():
+    s = Setup([300, 280], [1, 2], page=16, seed=28)
+    s.ref.table[1, :17] = s.ref.table[0, :17]                   # 272 tokens in common
+    s.gpu.table.copy_(s.ref.table)
+    check_weigh(s)
+
+
 def test_a_bad_page_gets_no_weights():
     s = Setup([100, 90], [2, 2], seed=27)
     lse = R.attend(s.ref, s.q, s.row_start, 2)[1].float()

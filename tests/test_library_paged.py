@@ -88,8 +88,10 @@ def test_workspaces():
     for name, need in (("attend", n), ("weigh", B.paged_workspace_bytes(params())), ("evict", e)):
         assert call(name, params(), ws=None) == -3 and call(name, params(), ws=4097) == -3
     assert call("attend", params(), n=0) == -3 and call("evict", params(), n=e - 1) == -3 and call("weigh", params(), n=0) == -3
-    # the eviction's lists: two numbers a slot
-    assert 4 * 2 * 20 * 64 * 8 <= e <= 4 * 2 * 20 * 64 * 8 + 4096
+    # the eviction's lists: a number a slot, two where the keys do not fit in LDS
+    assert 4 * 2 * 20 * 64 * 4 <= e <= 4 * 2 * 20 * 64 * 4 + 4096
+    big = B.paged_workspace_bytes(params(max_pages=513), evict=True)
+    assert 4 * 2 * 513 * 64 * 8 <= big <= 4 * 2 * 513 * 64 * 8 + 4096
     # one workspace serves every number of rows
     assert all(B.paged_workspace_bytes(params(n_rows=r)) == n for r in (1, 64, 5000, 1 << 20))
 
@@ -125,6 +127,8 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
                        (c.k, c.v, c.table, c.lens[:1]), (c.k[..., ::2], c.v[..., ::2], c.table, c.lens), (c.k, c.v[:4], c.table, c.lens)):
         with pytest.raises(B.DashError):
             B.make_paged_params(B.PagedCache(k, v, t, n), 3, 4)
+    with pytest.raises(B.DashError, match="GPU"):               # nothing wrong but where the tensors lie
+        B.dash_paged_attend(p, c, q, start, q.clone(), ws, lse=lse)
     assert list(p.q_stride) == [0, 0]                           # a call leaves the caller's parameters alone
 
 
