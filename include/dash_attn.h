@@ -10,7 +10,7 @@
  *   Stage 2  block-sparse softmax attention over the kept  (Sec. 3.3, Eq. 5-6 in the
  *            chunks with the bias added to the logits       bias form of Prop. 1; Alg. 3)
  *   plus a split-KV decode variant of Stage 2 (Sec. 3.5) and a dense reference
- *   attention (Eq. 1).
+ *   attention (Eq. 1); and the calls of a paged cache for dense layers (dash_paged_*).
  *
  * Conventions shared by every entry point
  *   - Every tensor pointer is a DEVICE pointer owned by the caller.  The library
@@ -21,7 +21,7 @@
  *     one-time opt-in to a large dynamic LDS size has been made (thread-safe) and the
  *     addresses of two arrays of its own (the scratch of dash_attn_decode_static; the records, 96 KB, in
  *     which large bf16 prefills choose between two Stage-2 kernels on the device, any number of them at once),
- *     and, per process, two counters that give the split flags of a decode step and such a choice numbers of their own.
+ *     and, per process, two counters that give the split flags of a decode step (dash_paged_attend's too) and such a choice numbers of their own.
  *     Entry points may be called from several threads.  A workspace belongs to one call at a time: calls that are in
  *     flight together (several streams) need one each, or must not use it.  dash_stage2_attend of a bf16 prefill uses
  *     it for lists that are not given, and for parts where few rows meet a long cache.

@@ -111,15 +111,16 @@ __device__ __forceinline__ int4 threads_before(int u, int v, int2* xch) {
   return make_int4(us - u + bu, vs - v + bv, __builtin_amdgcn_readlane(cu, 63), __builtin_amdgcn_readlane(cv, 63));
 }
 
-// A workgroup per pair.  The keys stay in LDS (of more than 32768 tokens: in the scratch).  The budget-th largest: the keys are counted by
-// their 11 leading bits; those that share the ones of the key looked for are picked out and ranked against each other (more than 256 of
-// them: counted by the next 11 bits, and the last 10; more than 2048 are not picked out).  Then a thread takes an odd number of consecutive slots, so that ranks in slot order need
-// one scan over the threads, and its reads meet no other's bank.
+// A workgroup per pair.  The keys stay in LDS (more than 32768 of them: in the scratch, and come back in chunks).  The budget-th
+// largest: the keys are counted by their 11 leading bits; those that share the ones of the key looked for are picked out and ranked
+// against each other (more than 256 of them: counted by the next 11 bits, and the last 10; more than 2048 are not picked out).  Then a thread
+// takes an odd number of consecutive slots, so that ranks in slot order need one scan over the threads, and its reads meet no
+// other's bank.
 // What bounds it: the chain of loads (lengths, pages, weights), then LDS and some fifteen barriers one after the other: 32 caches of 4352
 // tokens x 8 15 us (256 threads instead of 1024: 20), two of 20 and 32k 33.
 __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e, int room) {   // room: keys that LDS has room for
   const PagedArgs& a = e.a;
-  extern __shared__ uint32_t lds_keys[];
+  extern __shared__ uint32_t keys[];
   __shared__ int hist[kBins];
   __shared__ int2 xch[kSelThreads / 64], rank[kRanked];
   __shared__ uint32_t cand[kCands];
@@ -138,10 +139,13 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e, 
     return;
   }
   const int first_recent = a.seen[b] - e.recent, pm = (1 << a.page_log) - 1;
-  auto select = [&](uint32_t* keys) __attribute__((always_inline)) {
-    // Load: wave w owns rows of 64 slots [w rows, (w + 1) rows), sixteen at a time: their pages, a lane for each 16 slots, then all weights
-    // and positions.
-    const int rows = (n + kSelThreads - 1) / kSelThreads, base = wave * rows * 64;
+  uint32_t* far = e.keys + (int64_t)pair * a.cap;
+  const bool one = n <= room;                                // chunk
+  __syncthreads();                                           // the counts are zero
+  for (int c0 = 0; c0 < n; c0 += room) {
+    // Wave w loads rows of 64 slots [w rows, (w + 1) rows) of the chunk, sixteen at a time: their pages, a lane for each 16 slots, then all
+    // weights and positions.
+    const int end = min(c0 + room, n), rows = (end - c0 + kSelThreads - 1) / kSelThreads, base = c0 + wave * rows * 64;
     for (int j0 = 0; j0 < rows; j0 += 16) {
       const int pages = paged_page_lane(a, b, min(base + (j0 * 4 + lane) * 16, n - 1) >> a.page_log);
       float w[16];
@@ -153,9 +157,10 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e, 
       };
       auto use = [&](int j) {
         const int i = base + (j0 + j) * 64 + lane;
-        if (j0 + j < rows && i < n) {
+        if (j0 + j < rows && i < end) {
           const uint32_t k = evict_key(w[j], p[j], e.sinks, first_recent);
-          keys[i] = k;
+          if (one) keys[i] = k;
+          else far[i] = k;
           atomicAdd(&hist[k >> 21], 1);
         }
       };
@@ -165,7 +170,6 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e, 
 #pragma unroll
         for (int j = 8; j < 16; j++) load(j);
       }
-      if (j0 == 0) __syncthreads();                          // the counts are zero
 #pragma unroll
       for (int j = 0; j < 8; j++) use(j);
       if (j0 + 8 < rows) {
@@ -173,142 +177,147 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e, 
         for (int j = 8; j < 16; j++) use(j);
       }
     }
+  }
+  __syncthreads();
+  // body(c0, own): the chunk that begins at slot c0 is in LDS, `own` slots a thread
+  auto chunks = [&](auto&& body) {
+    for (int c0 = 0; c0 < n; c0 += room) {
+      const int len = min(room, n - c0);
+      if (!one) {
+        __syncthreads();
+        for (int i = tid; i < len; i += kSelThreads) keys[i] = far[c0 + i];
+        __syncthreads();
+      }
+      body(c0, ((len + kSelThreads - 1) / kSelThreads) | 1);
+    }
+  };
+  // f(key, slot) for the thread's slots of a chunk
+  auto each = [&](int c0, int own, auto&& f) {
+    const int end = min((tid + 1) * own, min(room, n - c0));
+    int i = tid * own;
+    for (; i + 4 <= end; i += 4) {
+      const uint32_t k0 = keys[i], k1 = keys[i + 1], k2 = keys[i + 2], k3 = keys[i + 3];
+      f(k0, c0 + i); f(k1, c0 + i + 1); f(k2, c0 + i + 2); f(k3, c0 + i + 3);
+    }
+    for (; i < end; i++) f(keys[i], c0 + i);
+  };
+  // the bin that holds the want-th largest of the keys counted: how many of its keys stay, and all
+  auto find_bin = [&](int want) {
+    constexpr int OWN = kBins / kSelThreads;                 // bins of a thread, from the largest
+    int c[OWN], sum = 0;
+#pragma unroll
+    for (int q = 0; q < OWN; q++) sum += c[q] = hist[kBins - 1 - OWN * tid - q];
+    int before = threads_before(sum, 0, xch).x;
+    if (before < want && before + sum >= want) {
+#pragma unroll
+      for (int q = 0; q < OWN; q++) {
+        if (before < want && before + c[q] >= want) { chosen[0] = kBins - 1 - OWN * tid - q; chosen[1] = want - before; chosen[2] = c[q]; }
+        before += c[q];
+      }
+    }
     __syncthreads();
-    // f(key, slot) for the thread's slots
-    const int own = rows | 1, slot0 = tid * own;
-    auto each = [&](auto&& f) {
-      int i = slot0;
-      const int end = min(slot0 + own, n);
-      for (; i + 4 <= end; i += 4) {
-        const uint32_t k0 = keys[i], k1 = keys[i + 1], k2 = keys[i + 2], k3 = keys[i + 3];
-        f(k0, i); f(k1, i + 1); f(k2, i + 2); f(k3, i + 3);
-      }
-      for (; i < end; i++) f(keys[i], i);
-    };
-    // the bin that holds the want-th largest of the keys counted: how many of its keys stay, and all
-    auto find_bin = [&](int want) {
-      constexpr int OWN = kBins / kSelThreads;                   // bins of a thread, from the largest
-      int c[OWN], sum = 0;
-#pragma unroll
-      for (int q = 0; q < OWN; q++) sum += c[q] = hist[kBins - 1 - OWN * tid - q];
-      int before = threads_before(sum, 0, xch).x;
-      if (before < want && before + sum >= want) {
-#pragma unroll
-        for (int q = 0; q < OWN; q++) {
-          if (before < want && before + c[q] >= want) { chosen[0] = kBins - 1 - OWN * tid - q; chosen[1] = want - before; chosen[2] = c[q]; }
-          before += c[q];
-        }
-      }
-      __syncthreads();
-    };
-    find_bin(e.budget);
-    uint32_t last = (uint32_t)chosen[0] << 21;               // the smallest key that stays, from its leading bits on
-    int want = chosen[1], ties = chosen[2];                  // of the keys that share them, those that stay, and all
-    const int picked = ties <= kCands ? ties : 0;
-    if (picked) {
-      const uint32_t bin = last >> 21;
+  };
+  find_bin(e.budget);
+  uint32_t last = (uint32_t)chosen[0] << 21;                 // the smallest key that stays, from its leading bits on
+  int want = chosen[1], ties = chosen[2];                    // of the keys that share them, those that stay, and all
+  const int picked = ties <= kCands ? ties : 0;
+  if (picked) {
+    const uint32_t bin = last >> 21;
+    chunks([&](int c0, int own) {
       int mine = 0;
-      each([&](uint32_t k, int) { mine += k >> 21 == bin; });
+      each(c0, own, [&](uint32_t k, int) { mine += k >> 21 == bin; });
       if (mine) {
         int at = atomicAdd(&n_cand, mine);
-        each([&](uint32_t k, int) { if (k >> 21 == bin) cand[at++] = k; });
+        each(c0, own, [&](uint32_t k, int) { if (k >> 21 == bin) cand[at++] = k; });
       }
-      __syncthreads();
+    });
+    __syncthreads();
+  }
+  if (ties <= kRanked) {
+    // thread t ranks candidate t % M among a share of them
+    int m_log = 0;
+    while ((1 << m_log) < ties) m_log++;
+    const int me = tid & ((1 << m_log) - 1), share = kSelThreads >> m_log;
+    if (me < ties) {
+      const uint32_t k = cand[me];
+      int more = 0, same = 0;
+      for (int i = tid >> m_log; i < ties; i += share) {
+        const uint32_t x = cand[i];
+        more += x > k;
+        same += x == k;
+      }
+      atomicAdd(&rank[me].x, more);
+      atomicAdd(&rank[me].y, same);
     }
-    if (ties <= kRanked) {
-      // thread t ranks candidate t % M among a share of them
-      int m_log = 0;
-      while ((1 << m_log) < ties) m_log++;
-      const int me = tid & ((1 << m_log) - 1), share = kSelThreads >> m_log;
-      if (me < ties) {
-        const uint32_t k = cand[me];
-        int more = 0, same = 0;
-        for (int i = tid >> m_log; i < ties; i += share) {
-          const uint32_t x = cand[i];
-          more += x > k;
-          same += x == k;
-        }
-        atomicAdd(&rank[me].x, more);
-        atomicAdd(&rank[me].y, same);
+    __syncthreads();
+    if (tid < ties) {
+      const int2 y = rank[tid];
+      if (y.x < want && y.x + y.y >= want) {                 // those that find it are equal and write the same
+        chosen[0] = (int)(cand[tid] & 0x1fffff);
+        chosen[1] = want - y.x;
+        chosen[2] = y.y;
+      }
+    }
+    __syncthreads();
+    last |= (uint32_t)chosen[0];
+    want = chosen[1];
+    ties = chosen[2];
+  } else {
+#pragma unroll 1
+    for (int step = 0; step < 2; step++) {
+      const int shift = step ? 0 : 10, known = step ? 10 : 21, bits = step ? 1023 : 2047;
+      __syncthreads();
+      for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
+      __syncthreads();
+      auto count = [&](uint32_t k) { if (k >> known == last >> known) atomicAdd(&hist[(k >> shift) & bits], 1); };
+      if (picked) {
+        for (int i = tid; i < picked; i += kSelThreads) count(cand[i]);
+      } else {
+        chunks([&](int c0, int own) { each(c0, own, [&](uint32_t k, int) { count(k); }); });
       }
       __syncthreads();
-      if (tid < ties) {
-        const int2 y = rank[tid];
-        if (y.x < want && y.x + y.y >= want) {               // those that find it are equal and write the same
-          chosen[0] = (int)(cand[tid] & 0x1fffff);
-          chosen[1] = want - y.x;
-          chosen[2] = y.y;
-        }
-      }
-      __syncthreads();
-      last |= (uint32_t)chosen[0];
+      find_bin(want);
+      last |= (uint32_t)chosen[0] << shift;
       want = chosen[1];
       ties = chosen[2];
-    } else {
-#pragma unroll 1
-      for (int step = 0; step < 2; step++) {
-        const int shift = step ? 0 : 10, known = step ? 10 : 21, bits = step ? 1023 : 2047;
-        __syncthreads();
-        for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
-        __syncthreads();
-        auto count = [&](uint32_t k) { if (k >> known == last >> known) atomicAdd(&hist[(k >> shift) & bits], 1); };
-        if (picked) {
-          for (int i = tid; i < picked; i += kSelThreads) count(cand[i]);
-        } else {
-          each([&](uint32_t k, int) { count(k); });
-        }
-        __syncthreads();
-        find_bin(want);
-        last |= (uint32_t)chosen[0] << shift;
-        want = chosen[1];
-        ties = chosen[2];
-      }
     }
-    // Of the keys equal to the last one kept, the first `want` stay.
-    int tied = 0;
+  }
+  // Of the keys equal to the last one kept, the first `want` stay.
+  int32_t* moves = e.moves + (int64_t)pair * a.cap;
+  int tied = 0, holes = 0, movers = 0;                       // in the chunks before
+  chunks([&](int c0, int own) {
+    int spare = 0x7fffffff;                                  // equal keys that stay, from the thread's first on
     if (want < ties) {
-      each([&](uint32_t k, int) { tied += k == last; });
-      tied = threads_before(tied, 0, xch).x;
+      int mine = 0;
+      each(c0, own, [&](uint32_t k, int) { mine += k == last; });
+      const int4 s = threads_before(mine, 0, xch);
+      spare = want - tied - s.x;
+      tied += s.z;
     }
-    const int spare = want < ties ? want - tied : 0x7fffffff;   // equal keys that stay, from the thread's first on
-    int holes = 0, movers = 0, same = 0;
-    each([&](uint32_t k, int i) {
+    uint64_t stay = 0;                                       // of the thread's 33 slots at most
+    int freed = 0, moved = 0, same = 0;
+    each(c0, own, [&](uint32_t k, int i) {
       const bool kept = k > last || (k == last && same++ < spare);
-      holes += !kept && i < left;
-      movers += kept && i >= left;
+      stay |= (uint64_t)kept << (i - c0 - tid * own);
+      freed += !kept && i < left;
+      moved += kept && i >= left;
     });
-    const int4 hw = threads_before(holes, movers, xch);
-    int32_t* moves = e.moves + (int64_t)pair * a.cap;
-    same = 0;
-    if (keys == lds_keys) {
-      // The lists take the keys' place (they hold each slot once at most) before they are written out in whole lines: what a thread keeps of its
-      // 33 slots at most is a mask by then.
-      uint64_t stay = 0;
-      each([&](uint32_t k, int i) { stay |= (uint64_t)(k > last || (k == last && same++ < spare)) << (i - slot0); });
-      __syncthreads();
-      int at = hw.x, am = hw.z + hw.y;
-      for (int i = slot0; i < min(slot0 + own, n); i++) {
-        const bool kept = (stay >> (i - slot0)) & 1;
-        if (!kept && i < left) keys[at++] = (uint32_t)i;
-        if (kept && i >= left) keys[am++] = (uint32_t)i;
-      }
-      __syncthreads();
-      for (int i = tid; i < hw.z; i += kSelThreads) {
-        moves[i] = (int)keys[i];
-        moves[a.cap - 1 - i] = (int)keys[hw.z + i];
-      }
-    } else {
-      int at = hw.x, am = a.cap - 1 - hw.y;
-      each([&](uint32_t k, int i) {
-        const bool kept = k > last || (k == last && same++ < spare);
-        if (!kept && i < left) moves[at++] = i;
-        if (kept && i >= left) moves[am--] = i;
-      });
+    const int4 s = threads_before(freed, moved, xch);        // (every thread has read its keys by then)
+    // the lists take the keys' place, each slot of the chunk once at most, before they are written out in whole lines
+    const int end = min((tid + 1) * own, min(room, n - c0));
+    int at = s.x, am = s.z + s.y;
+    for (int i = tid * own; i < end; i++) {
+      const bool kept = (stay >> (i - tid * own)) & 1;
+      if (!kept && c0 + i < left) keys[at++] = (uint32_t)(c0 + i);
+      if (kept && c0 + i >= left) keys[am++] = (uint32_t)(c0 + i);
     }
-    if (tid == 0) e.counts[pair] = hw.z;
-  };
-  if (n <= room) select(lds_keys);
-  else select(e.keys + (int64_t)pair * a.cap);
+    __syncthreads();
+    for (int i = tid; i < s.z; i += kSelThreads) moves[holes + i] = (int)keys[i];
+    for (int i = tid; i < s.w; i += kSelThreads) moves[a.cap - 1 - movers - i] = (int)keys[s.z + i];
+    holes += s.z;
+    movers += s.w;
+  });
+  if (tid == 0) e.counts[pair] = holes;
 }
 
 // A wave moves eight tokens at a time: their places first, a lane each, then all their rows at once.
