@@ -38,6 +38,17 @@ __device__ __forceinline__ int2 paged_rows(const PagedArgs& a, int b) {
   const int r0 = min(max(a.row_start[b], 0), a.n_rows);
   return make_int2(r0, min(max(a.row_start[b + 1], r0), a.n_rows) - r0);
 }
+// A lane's sequence of 64: its rows and length (none behind the batch).  The first 64 are loaded once and kept.
+struct PagedLane { int2 rm; int n; };
+__device__ __forceinline__ PagedLane paged_lane(const PagedArgs& a, int b) {
+  PagedLane l = {make_int2(0, 0), 0};
+  if (b < a.batch) {
+    l.rm = paged_rows(a, b);
+    l.n = paged_len(a, b);
+  }
+  return l;
+}
+
 // Entry i of a sequence's table, read as a scalar: the caller's index is uniform.  Reads take a page of the pool, whatever the
 // entry says; writes look at it first.
 __device__ __forceinline__ int paged_entry(const PagedArgs& a, int b, int i) {
@@ -53,19 +64,17 @@ __device__ __forceinline__ int paged_page_lane(const PagedArgs& a, int b, int i)
 
 // ---- parts (tiles of 128 rows) ----------------------------------------------------------------------------------------
 constexpr int kMinPart = 4;                                // steps a part has at least
-struct PagedPart { int b, tile, part, parts, rec0, r0, m, n; };   // rec0: the item's first part among those of the kv-head
-
 // The size S of a part, no item costing more: none is cut; a wave's lanes together.  shape(m, n) gives a sequence's tiles and the cost
-// of one (at least 1).
+// of one (at least 1); l0: the first 64 sequences.
 constexpr int kUncut = 0x3fffffff;
-template <typename F> __device__ __forceinline__ int paged_part_size(const PagedArgs& a, F&& shape) {
+template <typename F> __device__ __forceinline__ int paged_part_size(const PagedArgs& a, const PagedLane& l0, F&& shape) {
   if (a.wgs <= 0) return kUncut;
   const int lane = lane_id();
   int items = 0;
   float cost = 0.f, most = 0.f;
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
-    int2 s = make_int2(0, 0);
-    if (i0 + lane < a.batch) s = shape(paged_rows(a, i0 + lane).y, paged_len(a, i0 + lane));
+    const PagedLane l = i0 ? paged_lane(a, i0 + lane) : l0;
+    const int2 s = shape(l.rm.y, l.n);
     items += __builtin_amdgcn_readlane(wave_scan(s.x), 63);
     cost += wave_sum((float)s.x * (float)s.y);
     most = fmaxf(most, wave_max(s.x > 0 ? (float)s.y : 0.f));
@@ -75,19 +84,16 @@ template <typename F> __device__ __forceinline__ int paged_part_size(const Paged
   return (float)S >= most ? kUncut : S;
 }
 
+struct PagedPart { int b, tile, part, parts, rec0, r0, m, n; };   // rec0: the item's first part among those of the kv-head
 // Every lane of a wave: part `idx` of a kv-head.
 template <typename F> __device__ __forceinline__ bool paged_find_part(const PagedArgs& a, int idx, F&& shape, PagedPart& it) {
   const int lane = lane_id();
-  const int S = paged_part_size(a, shape);
+  const PagedLane l0 = paged_lane(a, lane);
+  const int S = paged_part_size(a, l0, shape);
   int base = 0;
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
-    int2 s = make_int2(0, 0), rm = make_int2(0, 0);
-    int n = 0;
-    if (i0 + lane < a.batch) {
-      rm = paged_rows(a, i0 + lane);
-      n = paged_len(a, i0 + lane);
-      s = shape(rm.y, n);
-    }
+    const PagedLane p = i0 ? paged_lane(a, i0 + lane) : l0;
+    const int2 s = shape(p.rm.y, p.n);
     const int parts = (s.y + S - 1) / S;
     const int incl = wave_scan(s.x * parts);
     const uint64_t hit = __ballot(base + incl > idx);
@@ -100,9 +106,9 @@ template <typename F> __device__ __forceinline__ bool paged_find_part(const Page
       it.tile = __builtin_amdgcn_readlane(s.x, l) - 1 - (idx - first) / it.parts;
       it.part = (idx - first) % it.parts;
       it.rec0 = idx - it.part;
-      it.r0 = __builtin_amdgcn_readlane(rm.x, l);
-      it.m = __builtin_amdgcn_readlane(rm.y, l);
-      it.n = __builtin_amdgcn_readlane(n, l);
+      it.r0 = __builtin_amdgcn_readlane(p.rm.x, l);
+      it.m = __builtin_amdgcn_readlane(p.rm.y, l);
+      it.n = __builtin_amdgcn_readlane(p.n, l);
       return true;
     }
     base += __builtin_amdgcn_readlane(incl, 63);
@@ -129,39 +135,30 @@ struct PagedDeal {
   }
   __device__ __forceinline__ int before(const PagedSeq& s, int t) const { return s.flat ? s.flat * t : (int)(h(s.u + t) - h(s.u)); }
   __device__ __forceinline__ int steps(const PagedSeq& s, int t) const { return s.flat ? s.flat : ((s.u + t) >> k_log) + 1; }
-  // the steps of all items of a kv-head; a wave's lanes together
-  __device__ __forceinline__ int total(const PagedArgs& a) const {
+  // the steps of all items of a kv-head; a wave's lanes together; l0: the first 64 sequences
+  __device__ __forceinline__ int total(const PagedArgs& a, const PagedLane& l0) const {
     int f = 0;
     for (int i0 = 0; i0 < a.batch; i0 += 64) {
-      int v = 0;
-      if (i0 + (int)lane_id() < a.batch) {
-        const PagedSeq s = seq(a, paged_rows(a, i0 + lane_id()).y, paged_len(a, i0 + lane_id()));
-        v = before(s, s.tiles);
-      }
-      f += __builtin_amdgcn_readlane(wave_scan(v), 63);
+      const PagedLane l = i0 ? paged_lane(a, i0 + lane_id()) : l0;
+      const PagedSeq s = seq(a, l.rm.y, l.n);
+      f += __builtin_amdgcn_readlane(wave_scan(before(s, s.tiles)), 63);
     }
     return f;
   }
   // the item at step f (by_steps), or item number f; returns the steps of the item before f, -1 where there is none
-  __device__ __forceinline__ int find(const PagedArgs& a, int f, bool by_steps, PagedItem& it) const {
+  __device__ __forceinline__ int find(const PagedArgs& a, const PagedLane& l0, int f, bool by_steps, PagedItem& it) const {
     const int lane = lane_id();
     for (int i0 = 0; i0 < a.batch; i0 += 64) {
-      int2 rm = make_int2(0, 0);
-      int n = 0;
-      PagedSeq s = {0, 0, 0};
-      if (i0 + lane < a.batch) {
-        rm = paged_rows(a, i0 + lane);
-        n = paged_len(a, i0 + lane);
-        s = seq(a, rm.y, n);
-      }
+      const PagedLane p = i0 ? paged_lane(a, i0 + lane) : l0;
+      const PagedSeq s = seq(a, p.rm.y, p.n);
       const int v = by_steps ? before(s, s.tiles) : s.tiles, incl = wave_scan(v);
       const uint64_t hit = __ballot(incl > f);
       if (hit) {
         const int l = __builtin_ctzll(hit);
         it.b = i0 + l;
-        it.r0 = __builtin_amdgcn_readlane(rm.x, l);
-        it.m = __builtin_amdgcn_readlane(rm.y, l);
-        it.n = __builtin_amdgcn_readlane(n, l);
+        it.r0 = __builtin_amdgcn_readlane(p.rm.x, l);
+        it.m = __builtin_amdgcn_readlane(p.rm.y, l);
+        it.n = __builtin_amdgcn_readlane(p.n, l);
         it.s = {__builtin_amdgcn_readlane(s.tiles, l), __builtin_amdgcn_readlane(s.u, l), __builtin_amdgcn_readlane(s.flat, l)};
         const int in = f - __builtin_amdgcn_readlane(incl - v, l);
         if (!by_steps) {
@@ -221,18 +218,19 @@ struct PagedRun {
   int next, end, total;                                    // the step behind this piece, the run's end, the steps of the kv-head
   __device__ __forceinline__ PagedRun(const PagedArgs& a) : deal(a) {}
   __device__ __forceinline__ bool begin(const PagedArgs& a, int wg) {
+    const PagedLane l0 = paged_lane(a, lane_id());
     if (a.wgs == 0) {
-      if (deal.find(a, wg, false, it) < 0) return false;
+      if (deal.find(a, l0, wg, false, it) < 0) return false;
       x0 = next = end = 0;
       x1 = cost = deal.steps(it.s, it.tile);
       return true;
     }
-    total = deal.total(a);
+    total = deal.total(a, l0);
     const PagedBounds<int> b(a, total);
     next = __builtin_amdgcn_readfirstlane(b.at(wg));
     end = __builtin_amdgcn_readfirstlane(b.at(wg + 1));
     if (next >= end) return false;
-    x0 = deal.find(a, next, true, it);
+    x0 = deal.find(a, l0, next, true, it);
     cost = deal.steps(it.s, it.tile);
     return piece();
   }
@@ -244,7 +242,7 @@ struct PagedRun {
   __device__ __forceinline__ bool advance(const PagedArgs& a) {
     if (next >= end) return false;
     x0 = 0;
-    if (++it.tile >= it.s.tiles) deal.find(a, next, true, it);
+    if (++it.tile >= it.s.tiles) deal.find(a, paged_lane(a, lane_id()), next, true, it);
     cost = deal.steps(it.s, it.tile);
     return piece();
   }

@@ -95,6 +95,21 @@ __device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const Paged
   if (a.lse && c == 0) a.lse[(int64_t)(it.r0 + t) * a.h_q + head] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
 }
 
+// Partial results of a row (maximum m of the base-2 logits, sum, 4 values of the product) added one by one: what has to be loaded of
+// them can be asked for together.
+struct PagedSum {
+  float m = -INFINITY, den = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void add(float m2, float den2, f32x4 o2) {
+    const float top = fmaxf(m, m2), use = top == -INFINITY ? 0.f : top;
+    const float w = __builtin_amdgcn_exp2f(m - use), w2 = __builtin_amdgcn_exp2f(m2 - use);
+    m = top;
+    den = fmaf(w2, den2, w * den);
+#pragma unroll
+    for (int e = 0; e < 4; e++) o[e] = fmaf(w2, o2[e], w * o[e]);
+  }
+};
+
 // Behind a piece of an item that is cut between runs: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p, by the workgroup that sees the flags
 // of all its pieces.  They are those of runs w1, w1 + 1, ..; the first left its run's second record, the others their runs' first.  D / 4 threads
 // a row, 4 values each, and where the item has few rows several groups of threads that take every so manieth piece.  (A launch of its
@@ -103,9 +118,9 @@ template <typename T, int D, int THREADS>
 __device__ __forceinline__ void paged_few_join(const PagedArgs& a, const PagedRun& run, int r, int wg, char* lds) {
   constexpr int TPR = D / 4, UNITS = THREADS / TPR;        // threads of a row; rows at a time
   const PagedItem& it = run.it;
-  f32x4* xo = reinterpret_cast<f32x4*>(lds);               // [THREADS], [UNITS], [1]
+  f32x4* xo = reinterpret_cast<f32x4*>(lds);               // [THREADS], [UNITS][2], [1]
   float* xd = reinterpret_cast<float*>(xo + THREADS);
-  int* all = reinterpret_cast<int*>(xd + UNITS);
+  int* all = reinterpret_cast<int*>(xd + 2 * UNITS);
   const int lane = threadIdx.x & 63, begin = run.next - run.x1, end = begin + run.cost;
   const PagedBounds<int> bounds(a, run.total);
   int w1 = wg, pieces = 1;
@@ -140,34 +155,23 @@ __device__ __forceinline__ void paged_few_join(const PagedArgs& a, const PagedRu
   for (int i0 = 0; i0 < rows; i0 += per) {
     const int in = min(i0 + unit % per, rows - 1);
     const float* ml = a.part_ml + in * 2;
-    float M = -INFINITY, den = 0.f;
-    for (int p = c; p < pieces; p += TPR)                  // c-th piece of TPR a thread's
-      M = fmaxf(M, __uint_as_float((uint32_t)agent_load(ml + record(p) * 32)));
-    M = row16_reduce(M, OpMax());
-    if constexpr (TPR == 32) M = fmaxf(M, __shfl_xor(M, 16));
-    const float use = M == -INFINITY ? 0.f : M;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    PagedSum sum;
     const float* po = a.part_o + in * D + c * 4;
 #pragma unroll 4
     for (int p = slice; p < pieces; p += slices) {
       const uint64_t y = agent_load(ml + record(p) * 32), v0 = agent_load(po + record(p) * (16 * D)), v1 = agent_load(po + record(p) * (16 * D) + 2);
-      const float w = __builtin_amdgcn_exp2f(__uint_as_float((uint32_t)y) - use);
-      den = fmaf(w, __uint_as_float((uint32_t)(y >> 32)), den);
-      o[0] = fmaf(w, __uint_as_float((uint32_t)v0), o[0]);
-      o[1] = fmaf(w, __uint_as_float((uint32_t)(v0 >> 32)), o[1]);
-      o[2] = fmaf(w, __uint_as_float((uint32_t)v1), o[2]);
-      o[3] = fmaf(w, __uint_as_float((uint32_t)(v1 >> 32)), o[3]);
+      sum.add(__uint_as_float((uint32_t)y), __uint_as_float((uint32_t)(y >> 32)),
+              f32x4{__uint_as_float((uint32_t)v0), __uint_as_float((uint32_t)(v0 >> 32)), __uint_as_float((uint32_t)v1), __uint_as_float((uint32_t)(v1 >> 32))});
     }
     if (slices > 1) {
       __syncthreads();
-      xo[threadIdx.x] = o;
-      if (c == 0) xd[unit] = den;
+      xo[threadIdx.x] = sum.o;
+      if (c == 0) { xd[2 * unit] = sum.m; xd[2 * unit + 1] = sum.den; }
       __syncthreads();
-      for (int k = 1; k < slices && slice == 0; k++) {
-        o += xo[threadIdx.x + k * per * TPR];
-        den += xd[unit + k * per];
-      }
+      for (int k = 1; k < slices && slice == 0; k++) sum.add(xd[2 * (unit + k * per)], xd[2 * (unit + k * per) + 1], xo[threadIdx.x + k * per * TPR]);
     }
+    const float M = sum.m, den = sum.den;
+    const f32x4 o = sum.o;
     if (slice > 0 || i0 + unit >= rows) continue;
     const float inv = den > 0.f ? 1.f / den : den == 0.f ? 0.f : den;
     const int row = it.r0 + it.tile * run.deal.T + in / a.g, head = r * a.g + in % a.g;
@@ -731,10 +735,11 @@ template <int D, int SLICES>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
   constexpr int TPR = D / 4, PER = 256 / TPR / SLICES;     // threads of a row's slice, rows of a workgroup
   __shared__ f32x4 xo[SLICES > 1 ? 256 : 1];
-  __shared__ float xd[SLICES > 1 ? 256 / TPR : 1];
+  __shared__ float xd[SLICES > 1 ? 2 * (256 / TPR) : 1];
   const int lane = threadIdx.x & 63, c = threadIdx.x % TPR, unit = threadIdx.x / TPR, slice = unit / PER;
   const auto shape = [&](int m, int n) { return rows_shape(a, m, n); };
-  const int S = paged_part_size(a, shape);
+  const PagedLane l0 = paged_lane(a, lane);
+  const int S = paged_part_size(a, l0, shape);
   if (S == kUncut) return;
   // rows in the order kv-head, token, head of the group: neighbours lie side by side in the records
   const int64_t per = (int64_t)a.n_rows * a.g, all = per * a.h_kv;
@@ -744,11 +749,8 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
     // the dealing of the launch before, for a given row
     int first = 0, parts = 0, tiles = 0, r0 = 0, base = 0;
     for (int i0 = 0; i0 < a.batch; i0 += 64) {
-      int2 s = make_int2(0, 0), rm = make_int2(0, 0);
-      if (i0 + lane < a.batch) {
-        rm = paged_rows(a, i0 + lane);
-        s = shape(rm.y, paged_len(a, i0 + lane));
-      }
+      const PagedLane p = i0 ? paged_lane(a, i0 + lane) : l0;
+      const int2 rm = p.rm, s = shape(rm.y, p.n);
       const int np = (s.y + S - 1) / S, incl = wave_scan(s.x * np);
 #pragma unroll
       for (int k = 0; k < 64 / TPR; k++) {
@@ -764,41 +766,32 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
       base += __builtin_amdgcn_readlane(incl, 63);
     }
     const bool mine = parts > 1 && g0 + unit % PER < all;
-    float M = -INFINITY, den = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    PagedSum sum;
     if (mine) {
       const int Tt = 128 / a.g, t = row - r0, tile = t / Tt, in = (t % Tt) * a.g + hg;
       const int64_t rec = (int64_t)r * a.wgs + first + (tiles - 1 - tile) * parts;
       const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + rec * 128 + in;
-      // the maximum over all parts, c-th part of TPR a thread's; every slice finds the same
-      for (int p = c; p < parts; p += TPR) M = fmaxf(M, ml[p * 128].x);
-      M = row16_reduce(M, OpMax());
-      if constexpr (TPR == 32) M = fmaxf(M, __shfl_xor(M, 16));
-      const float use = M == -INFINITY ? 0.f : M;
       const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o) + (rec * 128 + in) * (D / 4) + c;
 #pragma unroll 8
       for (int p = slice; p < parts; p += SLICES) {
         const float2 y = ml[p * 128];
-        const float w = __builtin_amdgcn_exp2f(y.x - use);
-        const f32x4 x = po[(int64_t)p * 128 * (D / 4)];
-        den = fmaf(w, y.y, den);
-#pragma unroll
-        for (int e = 0; e < 4; e++) o[e] = fmaf(w, x[e], o[e]);
+        sum.add(y.x, y.y, po[(int64_t)p * 128 * (D / 4)]);
       }
     }
     if constexpr (SLICES > 1) {
       __syncthreads();
-      xo[threadIdx.x] = o;
-      if (c == 0) xd[unit] = den;
+      xo[threadIdx.x] = sum.o;
+      if (c == 0) { xd[2 * unit] = sum.m; xd[2 * unit + 1] = sum.den; }
       __syncthreads();
 #pragma unroll
       for (int k = 1; k < SLICES; k++) {
         if (slice > 0) break;
-        o += xo[threadIdx.x + k * PER * TPR];
-        den += xd[unit + k * PER];
+        sum.add(xd[2 * (unit + k * PER)], xd[2 * (unit + k * PER) + 1], xo[threadIdx.x + k * PER * TPR]);
       }
     }
     if (!mine || slice > 0) continue;
+    const float M = sum.m, den = sum.den;
+    const f32x4 o = sum.o;
     const float inv = den > 0.f ? 1.f / den : den == 0.f ? 0.f : den;
     const int head = r * a.g + hg;
     put_row4((uint16_t*)a.o + row * a.o_t + head * a.o_h + c * 4, o, inv);
