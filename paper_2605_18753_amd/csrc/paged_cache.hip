@@ -82,9 +82,15 @@ struct EvictArgs {
   PagedArgs a;
   int budget, sinks, recent;
   int32_t* lens; int32_t* src;
-  uint32_t* keys;      // [pair][cap], caches of more than kSelKeys slots only
   int32_t* moves;      // [pair][cap]: the targets from the front, the sources from the back
   int32_t* counts;     // [pair]
+  // long caches only
+  int chunks;          // chunks of a pair at most
+  uint32_t* keys;      // [pair][cap]
+  int32_t* cand;       // [pair][cap]: slots of the keys that share their leading bits with the one looked for
+  int32_t* hists;      // [pair][chunk][kBins]
+  int32_t* above;      // [pair][chunk]: keys with larger leading bits
+  int32_t* heads;      // [pair][4]: the leading bits looked for, how many keys that share them stay, and all; slots picked out so far
 };
 
 __device__ __forceinline__ uint32_t evict_key(float w, int pos, int sinks, int first_recent) {
@@ -94,31 +100,128 @@ __device__ __forceinline__ uint32_t evict_key(float w, int pos, int sinks, int f
   return u ^ ((int32_t)u < 0 ? 0xffffffffu : 0x80000000u);
 }
 
-constexpr int kSelThreads = 1024;
-constexpr int kSelKeys = 32768;                            // keys that are kept in LDS at most
 constexpr int kBins = 2048;                                // 11 bits of a key
+constexpr int kSelThreads = 1024, kSelKeys = 8192;         // caches of up to so many slots: a workgroup per pair, keys in LDS
 constexpr int kCands = 2048, kRanked = 256;                // keys that are picked out; that are ranked against each other
+constexpr int kChunk = 4096, kChunkThreads = 256;          // longer ones: slots and threads of a workgroup
 
 // For two counts of a thread: their sums over the threads before it (x, y) and over all (z, w).
-__device__ __forceinline__ int4 threads_before(int u, int v, int2* xch) {
+template <int THREADS> __device__ __forceinline__ int4 threads_before(int u, int v, int2* xch) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, us = wave_scan(u), vs = wave_scan(v);
   __syncthreads();
   if (lane == 63) xch[wave] = make_int2(us, vs);
   __syncthreads();
-  const int2 c = lane < kSelThreads / 64 ? xch[lane] : make_int2(0, 0);
+  const int2 c = lane < THREADS / 64 ? xch[lane] : make_int2(0, 0);
   const int cu = wave_scan(c.x), cv = wave_scan(c.y);
   const int bu = wave ? __builtin_amdgcn_readlane(cu, wave - 1) : 0, bv = wave ? __builtin_amdgcn_readlane(cv, wave - 1) : 0;
   return make_int4(us - u + bu, vs - v + bv, __builtin_amdgcn_readlane(cu, 63), __builtin_amdgcn_readlane(cv, 63));
 }
+// Of counts c of a thread's bins (from the largest: the thread's first is bin kBins - 1 - OWN tid): the bin that holds the want-th largest key, how
+// many of its keys stay, and all, into chosen[3] (complete behind the barrier).
+template <int THREADS> __device__ __forceinline__ void find_bin(const int (&c)[kBins / THREADS], int want, int2* xch, int* chosen) {
+  constexpr int OWN = kBins / THREADS;
+  int sum = 0;
+#pragma unroll
+  for (int q = 0; q < OWN; q++) sum += c[q];
+  int before = threads_before<THREADS>(sum, 0, xch).x;
+  if (before < want && before + sum >= want) {
+#pragma unroll
+    for (int q = 0; q < OWN; q++) {
+      if (before < want && before + c[q] >= want) { chosen[0] = kBins - 1 - OWN * (int)threadIdx.x - q; chosen[1] = want - before; chosen[2] = c[q]; }
+      before += c[q];
+    }
+  }
+  __syncthreads();
+}
+template <int THREADS> __device__ __forceinline__ void find_bin_of(const int* hist, int want, int2* xch, int* chosen) {
+  int c[kBins / THREADS];
+#pragma unroll
+  for (int q = 0; q < kBins / THREADS; q++) c[q] = hist[kBins - 1 - kBins / THREADS * (int)threadIdx.x - q];
+  find_bin<THREADS>(c, want, xch, chosen);
+}
+// Sixteen rows of 64 slots of a wave, from slot `base` on, a multiple of 16 (those before `end`): their pages, a lane for each 16 slots, then all weights
+// and positions, eight rows at least in flight; use(key, slot) of each.
+template <typename F> __device__ __forceinline__ void evict_keys16(const EvictArgs& e, int b, int h, int first_recent, int base, int rows, int end, F&& use) {
+  const PagedArgs& a = e.a;
+  const int lane = threadIdx.x & 63, pm = (1 << a.page_log) - 1;
+  const int pages = paged_page_lane(a, b, min(base + lane * 16, end - 1) >> a.page_log);
+  float w[16];
+  int p[16];
+  auto load = [&](int j) {
+    const int64_t at = (((int64_t)__shfl(pages, 4 * j + (lane >> 4)) * a.h_kv + h) << a.page_log) + ((base + j * 64 + lane) & pm);
+    w[j] = a.weights[at];
+    p[j] = a.pos[at];
+  };
+  auto take = [&](int j) {
+    const int i = base + j * 64 + lane;
+    if (j < rows && i < end) use(evict_key(w[j], p[j], e.sinks, first_recent), i);
+  };
+#pragma unroll
+  for (int j = 0; j < 8; j++) load(j);
+  if (8 < rows) {
+#pragma unroll
+    for (int j = 8; j < 16; j++) load(j);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; j++) take(j);
+  if (8 < rows) {
+#pragma unroll
+    for (int j = 8; j < 16; j++) take(j);
+  }
+}
+// f(key, slot) for a thread's `own` consecutive slots of the `len` whose keys are in LDS, the first of them slot c0.  An odd number of them: no
+// two lanes' reads meet in a bank.
+template <typename F> __device__ __forceinline__ void each_own(const uint32_t* keys, int c0, int own, int len, F&& f) {
+  int i = threadIdx.x * own;
+  const int end = min(i + own, len);
+  for (; i + 4 <= end; i += 4) {
+    const uint32_t k0 = keys[i], k1 = keys[i + 1], k2 = keys[i + 2], k3 = keys[i + 3];
+    f(k0, c0 + i); f(k1, c0 + i + 1); f(k2, c0 + i + 2); f(k3, c0 + i + 3);
+  }
+  for (; i < end; i++) f(keys[i], c0 + i);
+}
+// Of the slots [c0, c0 + len) whose keys are in LDS, those that are freed before `left` and those that move from behind it, behind the
+// `holes` and `movers` of the slots before them, into the lists.  Keys above `last` stay, and of those equal to it as many as
+// `spare` says, in slot order; ties: whether some of them go.  Returns the counts.
+template <int THREADS>
+__device__ __forceinline__ int2 list_moves(uint32_t* keys, int c0, int len, int left, uint32_t last, bool ties, int spare, int holes, int movers,
+                                           int32_t* moves, int cap, int2* xch) {
+  const int own = ((len + THREADS - 1) / THREADS) | 1, i0 = threadIdx.x * own;
+  int stays = 0x7fffffff;                                    // equal keys that stay, from the thread's first on
+  if (ties) {
+    int mine = 0;
+    each_own(keys, c0, own, len, [&](uint32_t k, int) { mine += k == last; });
+    stays = spare - threads_before<THREADS>(mine, 0, xch).x;
+  }
+  uint64_t stay = 0;                                         // of the thread's 17 slots at most
+  int freed = 0, moved = 0, same = 0;
+  each_own(keys, c0, own, len, [&](uint32_t k, int i) {
+    const bool kept = k > last || (k == last && same++ < stays);
+    stay |= (uint64_t)kept << (i - c0 - i0);
+    freed += !kept && i < left;
+    moved += kept && i >= left;
+  });
+  const int4 s = threads_before<THREADS>(freed, moved, xch);   // (every thread has read its keys by then)
+  // the lists take the keys' place, each slot once at most, before they are written out in whole lines
+  const int end = min(i0 + own, len);
+  int at = s.x, am = s.z + s.y;
+  for (int i = i0; i < end; i++) {
+    const bool kept = (stay >> (i - i0)) & 1;
+    if (!kept && c0 + i < left) keys[at++] = (uint32_t)(c0 + i);
+    if (kept && c0 + i >= left) keys[am++] = (uint32_t)(c0 + i);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < s.z; i += THREADS) moves[holes + i] = (int)keys[i];
+  for (int i = threadIdx.x; i < s.w; i += THREADS) moves[cap - 1 - movers - i] = (int)keys[s.z + i];
+  return make_int2(s.z, s.w);
+}
 
-// A workgroup per pair.  The keys stay in LDS (more than 32768 of them: in the scratch, and come back in chunks).  The budget-th
-// largest: the keys are counted by their 11 leading bits; those that share the ones of the key looked for are picked out and ranked
-// against each other (more than 256 of them: counted by the next 11 bits, and the last 10; more than 2048 are not picked out).  Then a thread
-// takes an odd number of consecutive slots, so that ranks in slot order need one scan over the threads, and its reads meet no
-// other's bank.
+// Caches of up to 8192 slots: a workgroup per pair, keys in LDS.  The budget-th largest: the keys are counted by their 11 leading bits;
+// those that share the ones of the key looked for are picked out and ranked against each other (more than 256 of them: counted by the next 11
+// bits, and the last 10; more than 2048 are not picked out).
 // What bounds it: the chain of loads (lengths, pages, weights), then LDS and some fifteen barriers one after the other: 32 caches of 4352
-// tokens x 8 15 us (256 threads instead of 1024: 20), two of 20 and 32k 33.
-__global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e, int room) {   // room: keys that LDS has room for
+// tokens x 8 15 us (256 threads instead of 1024: 20).
+__global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e) {
   const PagedArgs& a = e.a;
   extern __shared__ uint32_t keys[];
   __shared__ int hist[kBins];
@@ -126,7 +229,7 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e, 
   __shared__ uint32_t cand[kCands];
   __shared__ int chosen[3], n_cand;
   const int pair = blockIdx.x, h = pair % a.h_kv, b = pair / a.h_kv;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = paged_len(a, b), left = min(n, e.budget);
   for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
   if (tid < kRanked) rank[tid] = make_int2(0, 0);
@@ -138,99 +241,26 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e, 
     if (tid == 0) e.counts[pair] = 0;
     return;
   }
-  const int first_recent = a.seen[b] - e.recent, pm = (1 << a.page_log) - 1;
-  uint32_t* far = e.keys + (int64_t)pair * a.cap;
-  const bool one = n <= room;                                // chunk
+  const int first_recent = a.seen[b] - e.recent;
   __syncthreads();                                           // the counts are zero
-  for (int c0 = 0; c0 < n; c0 += room) {
-    // Wave w loads rows of 64 slots [w rows, (w + 1) rows) of the chunk, sixteen at a time: their pages, a lane for each 16 slots, then all
-    // weights and positions.
-    const int end = min(c0 + room, n), rows = (end - c0 + kSelThreads - 1) / kSelThreads, base = c0 + wave * rows * 64;
-    for (int j0 = 0; j0 < rows; j0 += 16) {
-      const int pages = paged_page_lane(a, b, min(base + (j0 * 4 + lane) * 16, n - 1) >> a.page_log);
-      float w[16];
-      int p[16];
-      auto load = [&](int j) {
-        const int64_t at = (((int64_t)__shfl(pages, 4 * j + (lane >> 4)) * a.h_kv + h) << a.page_log) + ((base + (j0 + j) * 64 + lane) & pm);
-        w[j] = a.weights[at];
-        p[j] = a.pos[at];
-      };
-      auto use = [&](int j) {
-        const int i = base + (j0 + j) * 64 + lane;
-        if (j0 + j < rows && i < end) {
-          const uint32_t k = evict_key(w[j], p[j], e.sinks, first_recent);
-          if (one) keys[i] = k;
-          else far[i] = k;
-          atomicAdd(&hist[k >> 21], 1);
-        }
-      };
-#pragma unroll
-      for (int j = 0; j < 8; j++) load(j);
-      if (j0 + 8 < rows) {
-#pragma unroll
-        for (int j = 8; j < 16; j++) load(j);
-      }
-#pragma unroll
-      for (int j = 0; j < 8; j++) use(j);
-      if (j0 + 8 < rows) {
-#pragma unroll
-        for (int j = 8; j < 16; j++) use(j);
-      }
-    }
-  }
+  const int rows = (n + kSelThreads - 1) / kSelThreads, base = wave * rows * 64;   // rows of 64 slots, at most eight
+  evict_keys16(e, b, h, first_recent, base, rows, n, [&](uint32_t k, int i) {
+    keys[i] = k;
+    atomicAdd(&hist[k >> 21], 1);
+  });
   __syncthreads();
-  // body(c0, own): the chunk that begins at slot c0 is in LDS, `own` slots a thread
-  auto chunks = [&](auto&& body) {
-    for (int c0 = 0; c0 < n; c0 += room) {
-      const int len = min(room, n - c0);
-      if (!one) {
-        __syncthreads();
-        for (int i = tid; i < len; i += kSelThreads) keys[i] = far[c0 + i];
-        __syncthreads();
-      }
-      body(c0, ((len + kSelThreads - 1) / kSelThreads) | 1);
-    }
-  };
-  // f(key, slot) for the thread's slots of a chunk
-  auto each = [&](int c0, int own, auto&& f) {
-    const int end = min((tid + 1) * own, min(room, n - c0));
-    int i = tid * own;
-    for (; i + 4 <= end; i += 4) {
-      const uint32_t k0 = keys[i], k1 = keys[i + 1], k2 = keys[i + 2], k3 = keys[i + 3];
-      f(k0, c0 + i); f(k1, c0 + i + 1); f(k2, c0 + i + 2); f(k3, c0 + i + 3);
-    }
-    for (; i < end; i++) f(keys[i], c0 + i);
-  };
-  // the bin that holds the want-th largest of the keys counted: how many of its keys stay, and all
-  auto find_bin = [&](int want) {
-    constexpr int OWN = kBins / kSelThreads;                 // bins of a thread, from the largest
-    int c[OWN], sum = 0;
-#pragma unroll
-    for (int q = 0; q < OWN; q++) sum += c[q] = hist[kBins - 1 - OWN * tid - q];
-    int before = threads_before(sum, 0, xch).x;
-    if (before < want && before + sum >= want) {
-#pragma unroll
-      for (int q = 0; q < OWN; q++) {
-        if (before < want && before + c[q] >= want) { chosen[0] = kBins - 1 - OWN * tid - q; chosen[1] = want - before; chosen[2] = c[q]; }
-        before += c[q];
-      }
-    }
-    __syncthreads();
-  };
-  find_bin(e.budget);
+  find_bin_of<kSelThreads>(hist, e.budget, xch, chosen);
   uint32_t last = (uint32_t)chosen[0] << 21;                 // the smallest key that stays, from its leading bits on
   int want = chosen[1], ties = chosen[2];                    // of the keys that share them, those that stay, and all
-  const int picked = ties <= kCands ? ties : 0;
+  const int picked = ties <= kCands ? ties : 0, own = rows | 1;
   if (picked) {
     const uint32_t bin = last >> 21;
-    chunks([&](int c0, int own) {
-      int mine = 0;
-      each(c0, own, [&](uint32_t k, int) { mine += k >> 21 == bin; });
-      if (mine) {
-        int at = atomicAdd(&n_cand, mine);
-        each(c0, own, [&](uint32_t k, int) { if (k >> 21 == bin) cand[at++] = k; });
-      }
-    });
+    int mine = 0;
+    each_own(keys, 0, own, n, [&](uint32_t k, int) { mine += k >> 21 == bin; });
+    if (mine) {
+      int at = atomicAdd(&n_cand, mine);
+      each_own(keys, 0, own, n, [&](uint32_t k, int) { if (k >> 21 == bin) cand[at++] = k; });
+    }
     __syncthreads();
   }
   if (ties <= kRanked) {
@@ -273,51 +303,195 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e, 
       if (picked) {
         for (int i = tid; i < picked; i += kSelThreads) count(cand[i]);
       } else {
-        chunks([&](int c0, int own) { each(c0, own, [&](uint32_t k, int) { count(k); }); });
+        each_own(keys, 0, own, n, [&](uint32_t k, int) { count(k); });
       }
       __syncthreads();
-      find_bin(want);
+      find_bin_of<kSelThreads>(hist, want, xch, chosen);
       last |= (uint32_t)chosen[0] << shift;
       want = chosen[1];
       ties = chosen[2];
     }
   }
   // Of the keys equal to the last one kept, the first `want` stay.
-  int32_t* moves = e.moves + (int64_t)pair * a.cap;
-  int tied = 0, holes = 0, movers = 0;                       // in the chunks before
-  chunks([&](int c0, int own) {
-    int spare = 0x7fffffff;                                  // equal keys that stay, from the thread's first on
-    if (want < ties) {
-      int mine = 0;
-      each(c0, own, [&](uint32_t k, int) { mine += k == last; });
-      const int4 s = threads_before(mine, 0, xch);
-      spare = want - tied - s.x;
-      tied += s.z;
+  const int2 s = list_moves<kSelThreads>(keys, 0, n, left, last, want < ties, want, 0, 0, e.moves + (int64_t)pair * a.cap, a.cap, xch);
+  if (tid == 0) e.counts[pair] = s.x;
+}
+
+// Longer caches: a workgroup per chunk of 4096 slots, cut so that a chunk lies before the budget or behind it, in three launches.
+//   1  the keys into the scratch, and the chunk's counts by their 11 leading bits
+//   2  the bits of the key looked for from all chunks' counts; the slots whose keys share them into one list
+//   3  that key from the list (by the next 11 bits, then the last 10), every workgroup by itself, and from the list and the chunks' counts
+//      how many slots before the chunk are freed or move: then its own part of the lists
+// (One workgroup per pair for these as well, the whole call: two caches of 20 and 32k tokens x 8 cut to 4096 52.5 us, one of 128k to
+// 16384 214; in three launches 46 and 82.)
+struct EvictChunk { int b, h, n, base, begin, len, chunks, c; };   // chunks: of the pair; len 0: none; base: begin, or the multiple of 16 before it
+__device__ __forceinline__ EvictChunk evict_chunk(const EvictArgs& e) {
+  const PagedArgs& a = e.a;
+  EvictChunk k;
+  const int pair = blockIdx.x / e.chunks;
+  k.c = blockIdx.x % e.chunks;
+  k.h = pair % a.h_kv;
+  k.b = pair / a.h_kv;
+  k.n = paged_len(a, k.b);
+  const int front = (min(k.n, e.budget) + kChunk - 1) / kChunk;
+  const int from = e.budget & ~15;                           // where the chunks behind the budget are counted from
+  k.chunks = k.n <= e.budget ? 0 : front + (k.n - from + kChunk - 1) / kChunk;
+  k.base = k.c < front ? k.c * kChunk : from + (k.c - front) * kChunk;
+  k.begin = k.c < front ? k.base : max(k.base, e.budget);
+  k.len = k.c >= k.chunks ? 0 : min(k.base + kChunk, k.c < front ? e.budget : k.n) - k.begin;
+  return k;
+}
+
+__global__ __launch_bounds__(kChunkThreads) void paged_long_keys_kernel(EvictArgs e) {
+  const PagedArgs& a = e.a;
+  __shared__ int hist[kBins];
+  const EvictChunk k = evict_chunk(e);
+  const int pair = blockIdx.x / e.chunks, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (k.c == 0) {
+    if (tid == 0) {
+      e.heads[4 * pair + 3] = 0;
+      if (k.chunks == 0) e.counts[pair] = 0;
     }
-    uint64_t stay = 0;                                       // of the thread's 33 slots at most
-    int freed = 0, moved = 0, same = 0;
-    each(c0, own, [&](uint32_t k, int i) {
-      const bool kept = k > last || (k == last && same++ < spare);
-      stay |= (uint64_t)kept << (i - c0 - tid * own);
-      freed += !kept && i < left;
-      moved += kept && i >= left;
-    });
-    const int4 s = threads_before(freed, moved, xch);        // (every thread has read its keys by then)
-    // the lists take the keys' place, each slot of the chunk once at most, before they are written out in whole lines
-    const int end = min((tid + 1) * own, min(room, n - c0));
-    int at = s.x, am = s.z + s.y;
-    for (int i = tid * own; i < end; i++) {
-      const bool kept = (stay >> (i - tid * own)) & 1;
-      if (!kept && c0 + i < left) keys[at++] = (uint32_t)(c0 + i);
-      if (kept && c0 + i >= left) keys[am++] = (uint32_t)(c0 + i);
-    }
-    __syncthreads();
-    for (int i = tid; i < s.z; i += kSelThreads) moves[holes + i] = (int)keys[i];
-    for (int i = tid; i < s.w; i += kSelThreads) moves[a.cap - 1 - movers - i] = (int)keys[s.z + i];
-    holes += s.z;
-    movers += s.w;
+    if (e.src)
+      for (int i = tid; i < e.budget; i += kChunkThreads) e.src[(int64_t)pair * e.budget + i] = i < k.n ? i : -1;   // the moves change theirs
+  }
+  if (k.len == 0) return;
+  for (int i = tid; i < kBins; i += kChunkThreads) hist[i] = 0;
+  __syncthreads();
+  uint32_t* keys = e.keys + (int64_t)pair * a.cap;
+  evict_keys16(e, k.b, k.h, a.seen[k.b] - e.recent, k.base + wave * (kChunk / 4), 16, k.begin + k.len, [&](uint32_t x, int i) {
+    if (i < k.begin) return;
+    keys[i] = x;
+    atomicAdd(&hist[x >> 21], 1);
   });
-  if (tid == 0) e.counts[pair] = holes;
+  __syncthreads();
+  int32_t* out = e.hists + ((int64_t)pair * e.chunks + k.c) * kBins;
+  for (int i = tid; i < kBins; i += kChunkThreads) out[i] = hist[i];
+}
+
+// the counts of all chunks of a pair, a thread's bins from the largest, and of chunk `c` alone
+__device__ __forceinline__ void sum_hists(const int32_t* hists, int chunks, int c, int (&all)[kBins / kChunkThreads], int (&own)[kBins / kChunkThreads]) {
+  constexpr int OWN = kBins / kChunkThreads;
+  const int4* p = reinterpret_cast<const int4*>(hists + kBins - OWN * ((int)threadIdx.x + 1));
+#pragma unroll
+  for (int q = 0; q < OWN; q++) all[q] = own[q] = 0;
+#pragma unroll 4
+  for (int i = 0; i < chunks; i++) {
+    const int4 x = p[(int64_t)i * (kBins / 4)], y = p[(int64_t)i * (kBins / 4) + 1];
+    const int v[OWN] = {y.w, y.z, y.y, y.x, x.w, x.z, x.y, x.x};
+#pragma unroll
+    for (int q = 0; q < OWN; q++) {
+      all[q] += v[q];
+      own[q] = i == c ? v[q] : own[q];
+    }
+  }
+}
+
+__global__ __launch_bounds__(kChunkThreads) void paged_long_pick_kernel(EvictArgs e) {
+  const PagedArgs& a = e.a;
+  constexpr int OWN = kBins / kChunkThreads;
+  __shared__ int2 xch[kChunkThreads / 64];
+  __shared__ int chosen[3], place;
+  const EvictChunk k = evict_chunk(e);
+  if (k.len == 0) return;
+  const int pair = blockIdx.x / e.chunks, tid = threadIdx.x;
+  const uint32_t* far = e.keys + (int64_t)pair * a.cap + k.begin;
+  uint32_t key[kChunk / kChunkThreads];
+#pragma unroll
+  for (int j = 0; j < kChunk / kChunkThreads; j++) key[j] = far[min(j * kChunkThreads + tid, k.len - 1)];
+  int all[OWN], mine[OWN];
+  sum_hists(e.hists + (int64_t)pair * e.chunks * kBins, k.chunks, k.c, all, mine);
+  find_bin<kChunkThreads>(all, e.budget, xch, chosen);
+  const int bin = chosen[0];
+  int more = 0, hits = 0;
+#pragma unroll
+  for (int q = 0; q < OWN; q++) more += kBins - 1 - OWN * tid - q > bin ? mine[q] : 0;
+#pragma unroll
+  for (int j = 0; j < kChunk / kChunkThreads; j++) hits += j * kChunkThreads + tid < k.len && (int)(key[j] >> 21) == bin;
+  if (k.c == 0 && tid < 3) e.heads[4 * pair + tid] = chosen[tid];
+  const int4 s = threads_before<kChunkThreads>(hits, more, xch);
+  if (tid == 0) {
+    e.above[(int64_t)pair * e.chunks + k.c] = s.w;
+    place = s.z ? atomicAdd(&e.heads[4 * pair + 3], s.z) : 0;
+  }
+  __syncthreads();
+  int32_t* to = e.cand + (int64_t)pair * a.cap + place + s.x;
+#pragma unroll
+  for (int j = 0; j < kChunk / kChunkThreads; j++)
+    if (j * kChunkThreads + tid < k.len && (int)(key[j] >> 21) == bin) *to++ = k.begin + j * kChunkThreads + tid;
+}
+
+__global__ __launch_bounds__(kChunkThreads) void paged_long_list_kernel(EvictArgs e) {
+  const PagedArgs& a = e.a;
+  __shared__ uint32_t keys[kChunk];
+  __shared__ int2 cand[kCands];                              // key, slot
+  __shared__ int hist[kBins];
+  __shared__ int2 xch[kChunkThreads / 64];
+  __shared__ int chosen[3];
+  const EvictChunk k = evict_chunk(e);
+  if (k.len == 0) return;
+  const int pair = blockIdx.x / e.chunks, tid = threadIdx.x, front = (e.budget + kChunk - 1) / kChunk;
+  const uint32_t* far = e.keys + (int64_t)pair * a.cap;
+  const int32_t* slots = e.cand + (int64_t)pair * a.cap;
+  uint32_t last = (uint32_t)e.heads[4 * pair] << 21;         // the smallest key that stays, from its leading bits on
+  int want = e.heads[4 * pair + 1], ties = e.heads[4 * pair + 2];   // of the keys that share them, those that stay, and all
+  const int n_cand = ties;
+#pragma unroll
+  for (int j = 0; j < kChunk / kChunkThreads; j++) {
+    const int i = j * kChunkThreads + tid;
+    if (i < k.len) keys[i] = far[k.begin + i];
+  }
+#pragma unroll 4
+  for (int i = tid; i < min(n_cand, kCands); i += kChunkThreads) {
+    const int at = slots[i];
+    cand[i] = make_int2((int)far[at], at);
+  }
+  // f(key, slot) of those picked out, a thread's share; the first 2048 from LDS
+  auto picked = [&](auto&& f) {
+    for (int i = tid; i < min(n_cand, kCands); i += kChunkThreads) {
+      const int2 x = cand[i];
+      f((uint32_t)x.x, x.y);
+    }
+#pragma unroll 4
+    for (int i = kCands + tid; i < n_cand; i += kChunkThreads) {
+      const int at = slots[i];
+      f(far[at], at);
+    }
+  };
+#pragma unroll 1
+  for (int step = 0; step < 2; step++) {
+    const int shift = step ? 0 : 10, known = step ? 10 : 21, bits = step ? 1023 : 2047;
+    __syncthreads();
+    for (int i = tid; i < kBins; i += kChunkThreads) hist[i] = 0;
+    __syncthreads();
+    picked([&](uint32_t x, int) {
+      if (x >> known == last >> known) atomicAdd(&hist[(x >> shift) & bits], 1);
+    });
+    __syncthreads();
+    find_bin_of<kChunkThreads>(hist, want, xch, chosen);
+    last |= (uint32_t)chosen[0] << shift;
+    want = chosen[1];
+    ties = chosen[2];
+  }
+  // Before the chunk: keys of its side (before the budget, behind it) above `last`; equal ones of its side and of the side before it.  Of all equal
+  // ones the first `want` stay.
+  const bool back = k.c >= front;
+  const int side = back ? e.budget : 0;
+  int more = 0, same = 0, same_front = 0;
+  for (int i = (back ? front : 0) + tid; i < k.c; i += kChunkThreads) more += e.above[(int64_t)pair * e.chunks + i];
+  picked([&](uint32_t x, int at) {
+    const bool in = at >= side && at < k.begin;
+    more += in && x > last;
+    same += in && x == last;
+    same_front += at < side && x == last;
+  });
+  const int4 s = threads_before<kChunkThreads>(more, same, xch);
+  const int front_ties = threads_before<kChunkThreads>(same_front, 0, xch).z;
+  const int kept = s.z + min(s.w, max(want - front_ties, 0));
+  const int holes = back ? 0 : k.begin - kept, movers = back ? kept : 0;
+  const int2 own = list_moves<kChunkThreads>(keys, k.begin, k.len, e.budget, last, want < ties, want - front_ties - s.w, holes, movers,
+                                             e.moves + (int64_t)pair * a.cap, a.cap, xch);
+  if (k.c == front - 1 && tid == 0) e.counts[pair] = holes + own.x;
 }
 
 // A wave moves eight tokens at a time: their places first, a lane each, then all their rows at once.
@@ -368,23 +542,46 @@ __global__ __launch_bounds__(256) void paged_move_kernel(EvictArgs e, int wgs) {
 }
 
 static size_t evict_align(size_t x) { return (x + 255) & ~(size_t)255; }
-size_t paged_evict_ws(const PagedArgs& a) {
+// the scratch, dealt from `ws` on; returns its bytes
+static size_t evict_scratch(EvictArgs& e, const PagedArgs& a, char* ws) {
   const size_t pairs = (size_t)a.batch * a.h_kv;
-  return evict_align(pairs * 4) + evict_align(pairs * a.cap * 4) * (a.cap > kSelKeys ? 2 : 1);
+  size_t at = 0;
+  const auto take = [&](size_t numbers) {
+    char* p = ws ? ws + at : nullptr;
+    at += evict_align(numbers * 4);
+    return (int32_t*)p;
+  };
+  e.counts = take(pairs);
+  e.moves = take(pairs * a.cap);
+  if (a.cap > kSelKeys) {
+    e.chunks = (a.cap + kChunk - 1) / kChunk + 1;
+    e.keys = (uint32_t*)take(pairs * a.cap);
+    e.cand = take(pairs * a.cap);
+    e.hists = take(pairs * e.chunks * kBins);
+    e.above = take(pairs * e.chunks);
+    e.heads = take(pairs * 4);
+  }
+  return at;
+}
+size_t paged_evict_ws(const PagedArgs& a) {
+  EvictArgs e;
+  return evict_scratch(e, a, nullptr);
 }
 
 hipError_t launch_paged_evict(const PagedArgs& a, int elem, int d, int32_t* lens, int budget, int sinks, int recent, int32_t* src,
                               char* ws, hipStream_t st) {
   EvictArgs e;
   e.a = a; e.budget = budget; e.sinks = sinks; e.recent = recent; e.lens = lens; e.src = src;
+  evict_scratch(e, a, ws);
   const size_t pairs = (size_t)a.batch * a.h_kv;
-  e.counts = (int32_t*)ws;
-  e.moves = (int32_t*)(ws + evict_align(pairs * 4));
-  e.keys = (uint32_t*)(ws + evict_align(pairs * 4) + evict_align(pairs * a.cap * 4));   // of caches that LDS may have no room for
-  const int room = a.cap < kSelKeys ? a.cap : kSelKeys;
-  static LdsOptIn opt_in;
-  if (hipError_t r = allow_dyn_lds((const void*)paged_select_kernel, (size_t)room * 4, opt_in); r != hipSuccess) return r;
-  hipLaunchKernelGGL(paged_select_kernel, dim3((unsigned)pairs), dim3(kSelThreads), (size_t)room * 4, st, e, room);
+  if (a.cap <= kSelKeys) {
+    hipLaunchKernelGGL(paged_select_kernel, dim3((unsigned)pairs), dim3(kSelThreads), (size_t)a.cap * 4, st, e);
+  } else {
+    const dim3 grid((unsigned)(pairs * e.chunks)), blk(kChunkThreads);
+    hipLaunchKernelGGL(paged_long_keys_kernel, grid, blk, 0, st, e);
+    hipLaunchKernelGGL(paged_long_pick_kernel, grid, blk, 0, st, e);
+    hipLaunchKernelGGL(paged_long_list_kernel, grid, blk, 0, st, e);
+  }
   if (hipError_t r = hipGetLastError(); r != hipSuccess) return r;
   // eight workgroups per CU are resident at once; how many tokens move is not known here
   const int wgs = pairs < 2048 ? (int)(2048 / pairs < 64 ? 2048 / pairs : 64) : 1;

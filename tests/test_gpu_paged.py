@@ -402,16 +402,17 @@ def test_evict_without_src_and_with_everything_protected():
     evict_both(s, 200, 1, 0, w, pos, s.ref.lens.clone(), with_src=False)
 
 
-@pytest.mark.parametrize("budget", [32768, 500, 69000])
+@pytest.mark.parametrize("budget", [32768, 500, 69000, 4111, 4096, 1])
 @pytest.mark.parametrize("ties", [False, True])
-def test_evict_long_sequences(budget, ties):
-    s = Setup([70000, 33000, 32768], [1, 1, 1], h_kv=1, g=1, d=64, page=64, seed=46)
+@pytest.mark.parametrize("page", [16, 64])
+def test_evict_long_sequences(budget, ties, page):
+    s = Setup([70000, 33000, 32768, 0, 4112], [1, 1, 1, 1, 1], h_kv=1, g=1, d=64, page=page, seed=46)
     gen = torch.Generator().manual_seed(47)
     w = torch.randn(s.ref.k.shape[:3], generator=gen).exp()
     if ties:
         w = (w > 1.5).float()
     pos, seen = positions(s, gen)
-    evict_both(s, budget, 4, 100, w, pos, seen)
+    evict_both(s, budget, min(4, budget), min(100, budget - min(4, budget)), w, pos, seen)
 
 
 # ---- together --------------------------------------------------------------------------------------------------------

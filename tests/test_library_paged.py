@@ -7,6 +7,7 @@ import pytest
 import torch
 
 import paged_ref as R
+from test_library_host import kernel_scratch
 from paper_2605_18753_amd import binding as B
 
 
@@ -88,10 +89,10 @@ def test_workspaces():
     for name, need in (("attend", n), ("weigh", B.paged_workspace_bytes(params())), ("evict", e)):
         assert call(name, params(), ws=None) == -3 and call(name, params(), ws=4097) == -3
     assert call("attend", params(), n=0) == -3 and call("evict", params(), n=e - 1) == -3 and call("weigh", params(), n=0) == -3
-    # the eviction's lists: a number a slot, two where the keys do not fit in LDS
+    # the eviction's lists: a number a slot; of long caches also the keys and those picked out, and counts of every 4096
     assert 4 * 2 * 20 * 64 * 4 <= e <= 4 * 2 * 20 * 64 * 4 + 4096
     big = B.paged_workspace_bytes(params(max_pages=513), evict=True)
-    assert 4 * 2 * 513 * 64 * 8 <= big <= 4 * 2 * 513 * 64 * 8 + 4096
+    assert 4 * 2 * 513 * 64 * 12 + 4 * 2 * 10 * 2048 * 4 <= big <= 4 * 2 * 513 * 64 * 12 + 4 * 2 * 10 * 2049 * 4 + 4096
     # one workspace serves every number of rows
     assert all(B.paged_workspace_bytes(params(n_rows=r)) == n for r in (1, 64, 5000, 1 << 20))
 
@@ -150,3 +151,8 @@ def test_the_plain_forms_agree_with_torch():
         assert (ref.transpose(0, 1) - o[r0:r1]).abs().max() < 1e-12
         total += 4 * m
     assert abs(float(w.sum()) - total) < 1e-9 and (tol > 0).all()
+
+
+def test_the_kernels_use_no_scratch_memory():
+    scratch = {n: b for n, b in kernel_scratch(B.LIB_PATH).items() if "dash" in n and "paged_" in n}
+    assert len(scratch) >= 20 and not {n: b for n, b in scratch.items() if b}
