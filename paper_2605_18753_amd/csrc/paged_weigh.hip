@@ -5,7 +5,9 @@
 // registers and walks the rows that see them, 16 at a time; a lane adds up its own pairs, and the 16 lanes of a key are added at the
 // end.  Each sum is one wave's (or, for rows cut into parts, one thread's over the parts), so results do not depend on timing.
 // A single token: K is read once, HBM bounds it.  Many: an exponential, an FMA and an addition per pair, 24 clocks of a SIMD for 64
-// pairs, against 16 (head dimension 128; 64: 8) of matrix work.
+// pairs, against 16 (head dimension 128; 64: 8) of matrix work: two sequences of 6000 and 16000 tokens, 1999 new ones, 16 heads of 64
+// on 4: 157 us, 145 of them the main kernel, where the vector units alone take 147 at the highest clock and the matrix products 45.  One
+// of 32768, 2048 new, 32 heads of 128 on 8: 517 us, 1.03 PFLOP/s of matrix work.
 //
 // (block of keys, row tile) pairs of all sequences are dealt evenly to a fixed number of workgroups; blocks cut between two of them
 // are added up by a second launch, in a fixed order.
@@ -25,6 +27,10 @@ template <int D> struct WeighTile<uint16_t, D> {
 #pragma unroll
     for (int s = 0; s < D / 32; s++) v[s] = *reinterpret_cast<const bf16x8*>(row + 32 * s + 8 * kq);
   }
+  __device__ __forceinline__ void read(const uint32_t (&at)[D / 32], uint32_t by) {   // LDS
+#pragma unroll
+    for (int s = 0; s < D / 32; s++) v[s] = lds_read_b128(at[s] + by);
+  }
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int s = 0; s < D / 32; s++) v[s] = bf16x8{};
@@ -41,9 +47,9 @@ template <int D> struct WeighTile<float, D> {
   static constexpr int SUBS = 2;
   f32x4 v[D / 16];
   __device__ __forceinline__ void load(const float* row, int kq) { load_row<D>(row, kq, v); }
-  __device__ __forceinline__ void clear() {
+  __device__ __forceinline__ void read(const uint32_t (&at)[D / 16], uint32_t by) {
 #pragma unroll
-    for (int s = 0; s < D / 16; s++) v[s] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < D / 16; s++) v[s] = __builtin_bit_cast(f32x4, lds_read_b128(at[s] + by));
   }
   __device__ __forceinline__ f32x4 dot(const WeighTile& b) const { return mma_dot<D>(v, b.v); }
 };
@@ -113,7 +119,7 @@ template <int KEYS> __device__ __forceinline__ void weigh_find(const PagedArgs& 
   }
 }
 template <typename T, int D>
-__global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : D == 128 ? 3 : 4) void paged_weigh_kernel(PagedArgs a) {
+__global__ __launch_bounds__(256, (D == 128 ? 3 : 4) - (sizeof(T) == 4)) void paged_weigh_kernel(PagedArgs a) {
   constexpr int SUBS = WeighTile<T, D>::SUBS;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv;
@@ -124,9 +130,23 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : D == 128 ? 3 : 4) void pa
   if (todo <= 0) return;
   const int Tt = 16 / a.g, n = lane & 15, kq = lane >> 4, pm = (1 << a.page_log) - 1;
   const int tl = n / a.g;
-  const uint32_t q_lane = (uint32_t)(tl * (int)a.q_t + n % a.g * (int)a.q_h) * (uint32_t)sizeof(T) + kq * 16;
-  const uint32_t l_lane = (uint32_t)(tl * a.h_q + n % a.g) * 4u;
+  // Row tiles come through LDS, four at a time and two such stages: wave w copies tile w of a stage, all four waves read it.  A row's
+  // 16-byte pieces are permuted by its number, so that the 16 rows of a piece lie in different banks.
+  constexpr int ROW = D * (int)sizeof(T), PIECES = ROW / 16, TILE = 16 * ROW, COPIES = TILE / 1024;
+  auto swizzle = [](int row) { return ROW == 128 ? row >> 1 : row; };
+  __shared__ __attribute__((aligned(1024))) char ring[2][4 * TILE];
+  __shared__ float offs[2][4][16];                           // -lse in base 2 of the rows
+  const uint32_t ring0 = lds_addr_of(ring);
+  uint32_t q_lane[COPIES], rd[ROW / 64];
+#pragma unroll
+  for (int c = 0; c < COPIES; c++) {
+    const int row = (64 * c + lane) / PIECES;
+    q_lane[c] = (uint32_t)(row / a.g * (int)a.q_t + row % a.g * (int)a.q_h) * (uint32_t)sizeof(T) + (((lane % PIECES) ^ swizzle(row)) << 4);
+  }
+#pragma unroll
+  for (int s = 0; s < ROW / 64; s++) rd[s] = ring0 + n * ROW + (((4 * s + kq) ^ swizzle(n)) << 4);
   WeighItem it;
+  int slot = 0;                                              // the stage to fill next
   weigh_find<kWeighKeys<T>>(a, f0, it);
   while (true) {
     const int key0 = it.block * kWeighKeys<T> + wave * SUBS * 16;
@@ -141,56 +161,77 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 2 : D == 128 ? 3 : 4) void pa
       kf[s].load((const T*)a.k + (int64_t)paged_clamp(a, page[s]) * a.kp_p + r * a.kp_h + (int64_t)(key & pm) * a.kp_t, kq);
       acc[s] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    // this run's row tiles of the item, those before the first that sees one of the wave's keys left out
+    // this run's row tiles of the item, those before the first that sees one of the block's, or the wave's, keys left out
     const int take = (int)min((int64_t)(it.s.tiles - it.x), todo), back = it.n - it.m;
     const int first = a.last > 0 ? max(it.m - a.last, 0) : 0;
     int x = it.s.x0 + it.x;
     const int xe = x + take;
-    if (a.causal) x = min(max(x, (key0 - back) / Tt), xe);     // its token sees keys up to back + t
-    if (key0 >= it.n) x = xe;
-    // A tile's rows lie at constant offsets of a lane from its first row's address, a scalar; lanes behind the last row repeat it.
-    WeighTile<T, D> qf;
+    int xw = key0 < it.n ? x : xe;
+    if (a.causal) {                                            // a token sees keys up to back + t
+      xw = max(xw, (key0 - back) / Tt);
+      x = min(max(x, (it.block * kWeighKeys<T> - back) / Tt), xe);
+    }
     float l = 0.f;
-    const char* q_at = (const char*)((const T*)a.q + (int64_t)(it.r0 + x * Tt) * a.q_t + (int64_t)(r * a.g) * a.q_h);
-    const char* l_at = (const char*)(a.lse_in + (int64_t)(it.r0 + x * Tt) * a.h_q + r * a.g);
-    auto ask = [&](int y) {
-      uint32_t q_off = q_lane, l_off = l_lane;
-      if (__builtin_expect((y + 1) * Tt > it.m, 0)) {
-        const int back_rows = max(tl - (it.m - 1 - y * Tt), 0);
-        q_off -= (uint32_t)back_rows * (uint32_t)a.q_t * (uint32_t)sizeof(T);
-        l_off -= (uint32_t)(back_rows * a.h_q) * 4u;
-      }
-      qf.load((const T*)(q_at + q_off), 0);
-      l = *(const float*)(l_at + l_off);
-      q_at += (int64_t)Tt * a.q_t * sizeof(T);
-      l_at += (int64_t)Tt * a.h_q * 4;
-    };
-    if (x < xe) ask(x);
-    for (; x < xe; x++) {
-      const int t = x * Tt + tl;
-      float off = l == -INFINITY ? -INFINITY : -l * kLog2e;
-      if (__builtin_expect(x * Tt < first || (x + 1) * Tt > it.m, 0)) {        // rows that do not weigh, whatever they hold
-        if (t < first || t >= it.m) {
-          qf.clear();
-          off = -INFINITY;
-        }
-        asm volatile("" : "+v"(off));
-      }
-      f32x4 s[SUBS];
+    auto ask = [&](int y) {                                    // the wave's tile of a stage; rows behind the last repeat it
+      if (y >= xe) return;
+      const int up = it.m - 1 - y * Tt;
+      const u32x4 rows = make_rsrc((const T*)a.q + (int64_t)(it.r0 + y * Tt) * a.q_t + (int64_t)(r * a.g) * a.q_h, 0xffffffff);
+      const uint32_t to = ring0 + (uint32_t)((slot * 4 + wave) * TILE);
+      l = a.lse_in[(int64_t)(it.r0 + y * Tt + min(tl, up)) * a.h_q + r * a.g + n % a.g];
 #pragma unroll
-      for (int j = 0; j < SUBS; j++) s[j] = kf[j].dot(qf);
-      if (x + 1 < xe) ask(x + 1);
-      if (key0 + SUBS * 16 - 1 > (a.causal ? back + x * Tt : it.n - 1)) {       // the tile's first token sees keys up to there
-        const int lim = (a.causal ? min(back + t, it.n - 1) : it.n - 1) - key0 - 4 * kq;
+      for (int c = 0; c < COPIES; c++) {
+        const int t = (64 * c + lane) / PIECES / a.g;
+        const uint32_t at = __builtin_expect(up < Tt - 1, 0) ? q_lane[c] - (uint32_t)max(t - up, 0) * (uint32_t)a.q_t * (uint32_t)sizeof(T) : q_lane[c];
+        copy16_to_lds(rows, to + 1024 * c, at, 0);
+      }
+    };
+    if (x < xe) ask(x + wave);
+    for (; x < xe; x += 4) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      const int y = x + wave;
+      if (y < xe) {
+        const int t = y * Tt + tl;
+        const bool weighs = t >= first && t < it.m;            // one that does not: whatever it holds
+        const float off = !weighs || l == -INFINITY ? -INFINITY : -l * kLog2e;
+        if (kq == 0) offs[slot][wave][n] = off;
+        if (!weighs) {
+#pragma unroll
+          for (int s = 0; s < ROW / 64; s++)
+            *reinterpret_cast<__attribute__((address_space(3))) f32x4*>(rd[s] + (uint32_t)((slot * 4 + wave) * TILE)) = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+      }
+      __syncthreads();
+      const int had = slot;
+      slot ^= 1;
+      if (x + 4 < xe) ask(x + 4 + wave);
+      const int i1 = min(xe - x, 4);
+      WeighTile<T, D> qf;
+      float off = 0.f;
+      auto read = [&](int i) {
+        qf.read(rd, (uint32_t)((had * 4 + i) * TILE));
+        off = offs[had][i][n];
+      };
+      int i = max(xw - x, 0);
+      if (i < i1) read(i);
+      for (; i < i1; i++) {
+        const int y = x + i;
+        const float o = off;
+        f32x4 s[SUBS];
+#pragma unroll
+        for (int j = 0; j < SUBS; j++) s[j] = kf[j].dot(qf);
+        if (i + 1 < i1) read(i + 1);
+        if (key0 + SUBS * 16 - 1 > (a.causal ? back + y * Tt : it.n - 1)) {     // the tile's first token sees keys up to there
+          const int lim = (a.causal ? min(back + y * Tt + tl, it.n - 1) : it.n - 1) - key0 - 4 * kq;
+#pragma unroll
+          for (int j = 0; j < SUBS; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) s[j][e] = 16 * j + e > lim ? -INFINITY : s[j][e];
+        }
 #pragma unroll
         for (int j = 0; j < SUBS; j++)
 #pragma unroll
-          for (int e = 0; e < 4; e++) s[j][e] = 16 * j + e > lim ? -INFINITY : s[j][e];
+          for (int e = 0; e < 4; e++) acc[j][e] += __builtin_amdgcn_exp2f(fmaf(s[j][e], a.c1, o));
       }
-#pragma unroll
-      for (int j = 0; j < SUBS; j++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) acc[j][e] += __builtin_amdgcn_exp2f(fmaf(s[j][e], a.c1, off));
     }
     // over the 16 rows of a key; lane (n, kq), n < 4, takes key 4 kq + n
     const bool whole = take == it.s.tiles;
@@ -340,14 +381,14 @@ __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a)
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
-// resident workgroups of a kv-head: three per CU at head dimension 128, four at 64
-static int weigh_wgs(const PagedArgs& a, int d) { return max((d == 128 ? 768 : 1024) / a.h_kv, 1); }
+// resident workgroups of a kv-head, by the registers of a wave: three per CU at head dimension 128, four at 64; fp32 two and three
+static int weigh_wgs(const PagedArgs& a, int dtype, int d) { return max(256 * ((d == 128 ? 3 : 4) - (dtype != DASH_BF16)) / a.h_kv, 1); }
 
 // K is streamed where the sequences bring no more than 16 rows each on the average
 static bool weigh_stream(const PagedArgs& a) { return (int64_t)a.n_rows * a.g <= (int64_t)a.batch * 16; }
 
 size_t paged_weigh_ws(const PagedArgs& a, int dtype, int d) {
-  return (size_t)weigh_wgs(a, d) * a.h_kv * 2 * (dtype == DASH_BF16 ? kWeighKeys<uint16_t> : kWeighKeys<float>) * 4;
+  return (size_t)weigh_wgs(a, dtype, d) * a.h_kv * 2 * (dtype == DASH_BF16 ? kWeighKeys<uint16_t> : kWeighKeys<float>) * 4;
 }
 
 template <typename T, int D>
@@ -360,7 +401,7 @@ static hipError_t launch_weigh_t(PagedArgs a, char* ws, hipStream_t st) {
     }
   }
   a.part_o = (float*)ws;
-  a.wgs = weigh_wgs(a, D);
+  a.wgs = weigh_wgs(a, sizeof(T) == 2 ? DASH_BF16 : DASH_F32, D);
   hipLaunchKernelGGL((paged_weigh_kernel<T, D>), dim3((unsigned)(a.wgs * a.h_kv)), dim3(256), 0, st, a);
   hipError_t e = hipGetLastError();
   // a single tile of rows is not cut
