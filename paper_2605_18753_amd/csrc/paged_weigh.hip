@@ -6,7 +6,7 @@
 // end.  Each sum is one wave's (or, for rows cut into parts, one thread's over the parts), so results do not depend on timing.
 // A single token: K is read once, HBM bounds it.  Many: an exponential, an FMA and an addition per pair, 24 clocks of a SIMD for 64
 // pairs, against 16 (head dimension 128; 64: 8) of matrix work: two sequences of 6000 and 16000 tokens, 1999 new ones, 16 heads of 64
-// on 4: 157 us, 145 of them the main kernel, where the vector units alone take 147 at the highest clock and the matrix products 45.  One
+// on 4: 155 us, 144 of them the main kernel, where the vector units alone take 147 at the highest clock and the matrix products 45.  One
 // of 32768, 2048 new, 32 heads of 128 on 8: 517 us, 1.03 PFLOP/s of matrix work.
 //
 // (block of keys, row tile) pairs of all sequences are dealt evenly to a fixed number of workgroups; blocks cut between two of them
@@ -220,6 +220,10 @@ __global__ __launch_bounds__(256, (D == 128 ? 3 : 4) - (sizeof(T) == 4)) void pa
 #pragma unroll
         for (int j = 0; j < SUBS; j++) s[j] = kf[j].dot(qf);
         if (i + 1 < i1) read(i + 1);
+#pragma unroll
+        for (int j = 0; j < SUBS; j++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) s[j][e] = fmaf(s[j][e], a.c1, o);         // a pair's logarithm; what is not seen weighs nothing, whatever the row holds
         if (key0 + SUBS * 16 - 1 > (a.causal ? back + y * Tt : it.n - 1)) {     // the tile's first token sees keys up to there
           const int lim = (a.causal ? min(back + y * Tt + tl, it.n - 1) : it.n - 1) - key0 - 4 * kq;
 #pragma unroll
@@ -230,7 +234,7 @@ __global__ __launch_bounds__(256, (D == 128 ? 3 : 4) - (sizeof(T) == 4)) void pa
 #pragma unroll
         for (int j = 0; j < SUBS; j++)
 #pragma unroll
-          for (int e = 0; e < 4; e++) acc[j][e] += __builtin_amdgcn_exp2f(fmaf(s[j][e], a.c1, o));
+          for (int e = 0; e < 4; e++) acc[j][e] += __builtin_amdgcn_exp2f(s[j][e]);
       }
     }
     // over the 16 rows of a key; lane (n, kq), n < 4, takes key 4 kq + n
@@ -337,6 +341,10 @@ __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a)
       f32x4 s[SUBS];
 #pragma unroll
       for (int j = 0; j < SUBS; j++) s[j] = kf[j].dot(qf);
+#pragma unroll
+      for (int j = 0; j < SUBS; j++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) s[j][e] = fmaf(s[j][e], a.c1, off);
       if (key0 + SUBS * 16 - 1 > (a.causal ? back + y * Tt : x.n - 1)) {
         const int lim = (a.causal ? min(back + y * Tt + tl, x.n - 1) : x.n - 1) - key0 - 4 * kq;
 #pragma unroll
@@ -347,7 +355,7 @@ __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a)
 #pragma unroll
       for (int j = 0; j < SUBS; j++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) acc[j][e] += __builtin_amdgcn_exp2f(fmaf(s[j][e], a.c1, off));
+        for (int e = 0; e < 4; e++) acc[j][e] += __builtin_amdgcn_exp2f(s[j][e]);
     }
 #pragma unroll
     for (int j = 0; j < SUBS; j++) {

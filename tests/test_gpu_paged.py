@@ -292,6 +292,26 @@ def test_the_rows_outside_the_window_weigh_nothing_whatever_they_hold(dtype):
     assert torch.equal(s.gpu.weights.cpu(), want)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("m,bad", [(2, 0), (30, 5), (130, 77)])
+def test_weights_a_row_that_is_nan_reaches_only_the_tokens_it_sees(dtype, m, bad):
+    s = Setup([200], [m], dtype=dtype, seed=31)
+    lse = R.attend(s.ref, s.q, s.row_start, 2)[1].float()
+    s.ref.weights = torch.zeros(s.ref.k.shape[:3])
+    q, l = s.q.clone(), lse.clone()
+    q[bad], l[bad] = 0.0, math.inf                              # the row left out
+    want, tol = R.weigh(s.ref, q, s.row_start, l, 2)
+    s.q[bad], lse[bad] = math.nan, math.nan
+    s.gpu.weights = s.ref.weights.to(DEV)
+    p = s.params()
+    B.dash_paged_weigh(p, s.gpu, s.q.to(DEV), s.start_gpu, lse.to(DEV), B.alloc_paged_workspace(p, DEV))
+    page, off = s.ref.where(0, 200)
+    got, want, tol = (x[page, :, off] for x in (s.gpu.weights.cpu(), want, tol))
+    seen = 200 - m + bad + 1
+    assert got[:seen].isnan().all()
+    assert ((got[seen:].double() - want[seen:]).abs() <= tol[seen:]).all()
+
+
 def test_weights_of_pages_that_sequences_share():
     s = Setup([300, 280], [1, 2], page=16, seed=28)
     s.ref.table[1, :17] = s.ref.table[0, :17]                   # 272 tokens in common
