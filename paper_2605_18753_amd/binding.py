@@ -43,6 +43,7 @@ class dash_paged_params(ctypes.Structure):
     _fields_ += [("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
     _fields_ += [(n, ctypes.c_int64 * k) for n, k in (("q_stride", 2), ("o_stride", 2), ("k_new_stride", 2), ("v_new_stride", 2),
                                                       ("k_stride", 3), ("v_stride", 3))]
+    layout = None        # of the cache that make_paged_params was given
 
 
 _lib = None
@@ -332,9 +333,14 @@ class PagedCache:
         return c
 
 
+def _layout(c: PagedCache):
+    k, v, t, n = c.k, c.v, c.table, c.lens
+    return (k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype, t.shape, t.stride(), t.dtype, n.shape, n.stride(), n.dtype)
+
+
 def make_paged_params(cache: PagedCache, n_rows: int, h_q: int, causal: bool = True, scale: float = 0.0) -> dash_paged_params:
-    """Checks the cache's tensors once; the calls below look at their own arguments only.  The strides of q, o, k_new and
-    v_new are those of the tensors each call is given."""
+    """Checks the cache's tensors once; the calls below take a cache of the same sizes, strides and types, and look at their own
+    arguments.  The strides of q, o, k_new and v_new are those of the tensors each call is given."""
     k, v, t, n = cache.k, cache.v, cache.table, cache.lens
     if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in (torch.bfloat16, torch.float32):
         raise DashError("k and v pages: two tensors [n_pages, h_kv, page_size, d] of one type, bf16 or fp32")
@@ -351,11 +357,15 @@ def make_paged_params(cache: PagedCache, n_rows: int, h_q: int, causal: bool = T
     p.v_stride[:] = v.stride()[:3]
     if v.device != k.device:
         raise DashError("the tensors of a call lie on one device")
+    p.layout = _layout(cache)
     return p
 
 
-def _paged_call(p: dash_paged_params, cache: PagedCache, row_start, rows, extra=(), ws=None) -> dash_paged_params:
-    """The call's own copy of p, with the strides of its packed tensors; rows: (tensor, heads, field of its strides)."""
+def _paged_call(p: dash_paged_params, cache: PagedCache, row_start, rows, extra=(), ws=None):
+    """The call's own copy of p, with the strides of its packed tensors, and the current stream; rows: (tensor, heads, field of
+    its strides)."""
+    if _layout(cache) != p.layout:
+        raise DashError("the parameters are those of a cache of other sizes, strides or types (make_paged_params)")
     p = dash_paged_params.from_buffer_copy(p)
     n_rows, head_dim, dtype, dev = p.n_rows, p.head_dim, cache.k.dtype, cache.k.get_device()
     if row_start is not None and (row_start.dtype is not torch.int32 or row_start.numel() != p.batch + 1 or not row_start.is_contiguous()
@@ -370,13 +380,15 @@ def _paged_call(p: dash_paged_params, cache: PagedCache, row_start, rows, extra=
     for t, want, shape in extra:
         if t is not None and (t.dtype is not want or t.shape != shape or not t.is_contiguous() or t.get_device() != dev):
             raise DashError(f"expected a contiguous {want} tensor of shape {tuple(shape)} on the cache's device")
-    if cache.table.get_device() != dev or cache.lens.get_device() != dev:
+    if cache.table.get_device() != dev or cache.lens.get_device() != dev or cache.v.get_device() != dev:
         raise DashError("the cache's tensors lie on one device")
     if dev < 0 or (ws is not None and ws.get_device() != dev):
         raise DashError("the cache and the workspace lie on one GPU")
-    if _device is not None and dev != _device():
+    if _device is None or _raw_stream is None or not torch.cuda.is_initialized():
+        return p, _stream()
+    if dev != _device():
         raise DashError(f"the cache lies on cuda:{dev}, which is not the current device")
-    return p
+    return p, _raw_stream(dev)
 
 
 def paged_workspace_bytes(p: dash_paged_params, evict: bool = False) -> int:
@@ -394,30 +406,32 @@ def alloc_paged_workspace(p: dash_paged_params, device, evict: bool = False) -> 
 def dash_paged_append(p: dash_paged_params, cache: PagedCache, k_new, v_new, row_start) -> None:
     """k_new, v_new [n_rows, h_kv, d]; cache.weights, pos and seen as far as they are there."""
     tok = cache.k.shape[:3]
-    p = _paged_call(p, cache, row_start, ((k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride")),
-                ((cache.weights, torch.float32, tok), (cache.pos, torch.int32, tok), (cache.seen, torch.int32, cache.lens.shape)))
-    _check(load_library().dash_paged_append(p, _ptr(k_new), _ptr(v_new), _ptr(cache.k), _ptr(cache.v), _ptr(row_start), _ptr(cache.lens),
-                                            _ptr(cache.table), _ptr(cache.weights), _ptr(cache.pos), _ptr(cache.seen), _stream()),
-           "dash_paged_append")
+    p, stream = _paged_call(p, cache, row_start, ((k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride")),
+                            ((cache.weights, torch.float32, tok), (cache.pos, torch.int32, tok), (cache.seen, torch.int32, cache.lens.shape)))
+    _check(load_library().dash_paged_append(p, k_new.data_ptr(), v_new.data_ptr(), cache.k.data_ptr(), cache.v.data_ptr(),
+                                            row_start.data_ptr(), cache.lens.data_ptr(), cache.table.data_ptr(), _ptr(cache.weights),
+                                            _ptr(cache.pos), _ptr(cache.seen), stream), "dash_paged_append")
 
 
 def dash_paged_attend(p: dash_paged_params, cache: PagedCache, q, row_start, o, ws: torch.Tensor, lse=None) -> None:
     """q, o [n_rows, h_q, d]; lse fp32 [n_rows, h_q] or None."""
-    p = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"), (o, p.h_q, "o_stride")), ((lse, torch.float32, (p.n_rows, p.h_q)),), ws)
+    p, stream = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"), (o, p.h_q, "o_stride")),
+                            ((lse, torch.float32, (p.n_rows, p.h_q)),), ws)
     wp, wn = _ws_ptr(ws)
-    _check(load_library().dash_paged_attend(p, _ptr(q), _ptr(cache.k), _ptr(cache.v), _ptr(row_start), _ptr(cache.lens), _ptr(cache.table),
-                                            _ptr(o), _ptr(lse), wp, wn, _stream()), "dash_paged_attend")
+    _check(load_library().dash_paged_attend(p, q.data_ptr(), cache.k.data_ptr(), cache.v.data_ptr(), row_start.data_ptr(),
+                                            cache.lens.data_ptr(), cache.table.data_ptr(), o.data_ptr(), _ptr(lse), wp, wn, stream),
+           "dash_paged_attend")
 
 
 def dash_paged_weigh(p: dash_paged_params, cache: PagedCache, q, row_start, lse, ws: torch.Tensor, last: int = 0) -> None:
     """Adds to cache.weights; lse as dash_paged_attend wrote it."""
     if cache.weights is None or lse is None:
         raise DashError("dash_paged_weigh needs the cache's weights and the rows' lse")
-    p = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"),),
-                ((lse, torch.float32, (p.n_rows, p.h_q)), (cache.weights, torch.float32, cache.k.shape[:3])), ws)
+    p, stream = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"),),
+                            ((lse, torch.float32, (p.n_rows, p.h_q)), (cache.weights, torch.float32, cache.k.shape[:3])), ws)
     wp, wn = _ws_ptr(ws)
-    _check(load_library().dash_paged_weigh(p, _ptr(q), _ptr(cache.k), _ptr(row_start), _ptr(cache.lens), _ptr(cache.table), _ptr(lse), last,
-                                           _ptr(cache.weights), wp, wn, _stream()), "dash_paged_weigh")
+    _check(load_library().dash_paged_weigh(p, q.data_ptr(), cache.k.data_ptr(), row_start.data_ptr(), cache.lens.data_ptr(),
+                                           cache.table.data_ptr(), _ptr(lse), last, _ptr(cache.weights), wp, wn, stream), "dash_paged_weigh")
 
 
 def dash_paged_evict(p: dash_paged_params, cache: PagedCache, budget: int, ws: torch.Tensor, sinks: int = 0, recent: int = 0, src=None) -> None:
@@ -425,9 +439,9 @@ def dash_paged_evict(p: dash_paged_params, cache: PagedCache, budget: int, ws: t
     if cache.weights is None or cache.pos is None or cache.seen is None:
         raise DashError("dash_paged_evict needs the cache's weights, pos and seen")
     tok = cache.k.shape[:3]
-    p = _paged_call(p, cache, None, (), ((cache.weights, torch.float32, tok), (cache.pos, torch.int32, tok),
-                                     (cache.seen, torch.int32, cache.lens.shape), (src, torch.int32, (p.batch, p.h_kv, budget))), ws)
+    p, stream = _paged_call(p, cache, None, (), ((cache.weights, torch.float32, tok), (cache.pos, torch.int32, tok),
+                                                 (cache.seen, torch.int32, cache.lens.shape), (src, torch.int32, (p.batch, p.h_kv, budget))), ws)
     wp, wn = _ws_ptr(ws)
-    _check(load_library().dash_paged_evict(p, _ptr(cache.k), _ptr(cache.v), _ptr(cache.lens), _ptr(cache.seen), _ptr(cache.table),
-                                           _ptr(cache.weights), _ptr(cache.pos), budget, sinks, recent, _ptr(src), wp, wn, _stream()),
+    _check(load_library().dash_paged_evict(p, cache.k.data_ptr(), cache.v.data_ptr(), cache.lens.data_ptr(), _ptr(cache.seen), cache.table.data_ptr(),
+                                           _ptr(cache.weights), _ptr(cache.pos), budget, sinks, recent, _ptr(src), wp, wn, stream),
            "dash_paged_evict")

@@ -167,6 +167,14 @@ def test_a_batch_of_more_sequences_than_a_wave_has_lanes():
     s.check_attend()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_chunks_of_more_sequences_than_a_wave_has_lanes(dtype):
+    lens = [(53 * i) % 300 + 30 for i in range(100)]
+    s = Setup(lens, [(7 * i) % 30 if i % 5 else 0 for i in range(100)], h_kv=1, g=4, d=64, page=16, dtype=dtype, seed=32)
+    s.check_attend()
+    check_weigh(s)
+
+
 def test_a_given_scale():
     s = Setup([200], [4], seed=10)
     s.check_attend(scale=0.3)
@@ -265,6 +273,22 @@ def test_weights_of_chunks(dtype, causal, last):
 @pytest.mark.parametrize("h_kv,g", [(1, 1), (3, 2), (1, 16), (8, 1)])
 def test_weights_of_head_layouts(dtype, h_kv, g):
     check_weigh(Setup([300, 41, 1000], [1, 3, 90], h_kv=h_kv, g=g, d=64, dtype=dtype, page=32, layout="token", seed=22))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("new", [1, 100])
+def test_weights_of_strided_queries(dtype, new):
+    s = Setup([300, 41], [new, min(new, 20)], dtype=dtype, page=32, layout="token", seed=33)
+    lse = R.attend(s.ref, s.q, s.row_start, 2)[1].float()
+    want = check_weigh(s, lse=lse)
+    p = s.params()
+    fused = torch.full((s.rows, 12, 128 + 8), math.nan, dtype=dtype, device=DEV)
+    by_head = torch.full((8, s.rows, 128), math.nan, dtype=dtype, device=DEV)
+    for q in (fused[:, 4:, 8:], by_head.transpose(0, 1)):
+        q.copy_(s.q)
+        s.gpu.weights = s.ref.weights.to(DEV)
+        B.dash_paged_weigh(p, s.gpu, q, s.start_gpu, lse.to(DEV), B.alloc_paged_workspace(p, DEV))
+        assert torch.equal(s.gpu.weights.cpu(), want)
 
 
 def test_weights_of_a_long_cache_and_a_large_batch():
@@ -433,6 +457,13 @@ def test_evict_long_sequences(budget, ties, page):
         w = (w > 1.5).float()
     pos, seen = positions(s, gen)
     evict_both(s, budget, min(4, budget), min(100, budget - min(4, budget)), w, pos, seen)
+
+
+def test_evict_more_caches_than_workgroups_fit():
+    s = Setup([(11 * i) % 60 for i in range(300)], [1] * 300, h_kv=8, g=1, d=64, page=16, seed=48)
+    gen = torch.Generator().manual_seed(49)
+    pos, seen = positions(s, gen)
+    evict_both(s, 32, 2, 8, torch.rand(s.ref.k.shape[:3], generator=gen), pos, seen)
 
 
 # ---- together --------------------------------------------------------------------------------------------------------

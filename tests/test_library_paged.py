@@ -133,6 +133,23 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
     assert list(p.q_stride) == [0, 0]                           # a call leaves the caller's parameters alone
 
 
+def test_the_binding_refuses_the_parameters_of_another_cache():
+    c = B.PagedCache.allocate(2, 2, 8, 16, 64, 4, "cpu", evicting=True)
+    p = B.make_paged_params(c, 3, 4)
+    q, start = torch.zeros((3, 4, 64), dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    ws = torch.empty(1 << 20, dtype=torch.uint8)
+    fewer = {"k": c.k[:4], "v": c.v[:4], "table": c.table[:, :2].contiguous(), "lens": c.lens.long()}
+    token = torch.zeros((8, 16, 2, 64), dtype=torch.bfloat16).transpose(1, 2)
+    for field, x in (*fewer.items(), ("table", c.table[:1]), ("k", token), ("v", token), ("k", c.k.float())):
+        other = B.PagedCache(**{**vars(c), field: x})
+        for f in (lambda: B.dash_paged_attend(p, other, q, start, q.clone(), ws), lambda: B.dash_paged_evict(p, other, 8, ws),
+                  lambda: B.dash_paged_append(p, other, q[:, :2], q[:, 2:], start)):
+            with pytest.raises(B.DashError, match="another|other sizes"):
+                f()
+    with pytest.raises(B.DashError, match="GPU"):               # other tensors, alike
+        B.dash_paged_attend(p, B.PagedCache(c.k.clone(), c.v.clone(), c.table.clone(), c.lens.clone()), q, start, q.clone(), ws)
+
+
 def test_the_plain_forms_agree_with_torch():
     gen = torch.Generator().manual_seed(1)
     k, v = (torch.randn((6, 2, 16, 64), generator=gen, dtype=torch.float32) for _ in range(2))
