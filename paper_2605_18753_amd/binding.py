@@ -10,7 +10,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
-from dataclasses import dataclass
+from dataclasses import dataclass, field
 from typing import Optional
 
 import torch
@@ -311,7 +311,8 @@ def kbar_shape(p: dash_params):
 class PagedCache:
     """Keys and values of several sequences in pages of a pool (see the header's section on the paged cache).
     k, v [n_pages, h_kv, page_size, d]; table int32 [batch, max_pages]; lens int32 [batch]; for evicting callers
-    weights (fp32) and pos (int32), both [n_pages, h_kv, page_size], and seen int32 [batch]."""
+    weights (fp32) and pos (int32), both [n_pages, h_kv, page_size], and seen int32 [batch].
+    The tensors are checked by the first call after another one is assigned, not by every call."""
     k: torch.Tensor
     v: torch.Tensor
     table: torch.Tensor
@@ -319,6 +320,12 @@ class PagedCache:
     weights: Optional[torch.Tensor] = None
     pos: Optional[torch.Tensor] = None
     seen: Optional[torch.Tensor] = None
+    layout: Optional[tuple] = field(default=None, init=False, repr=False, compare=False)   # None: not checked
+
+    def __setattr__(self, name, value):
+        own = self.__dict__
+        if own.get(name, own) is not value:
+            own[name], own["layout"] = value, None
 
     @staticmethod
     def allocate(batch: int, h_kv: int, n_pages: int, page_size: int, head_dim: int, max_pages: int, device,
@@ -333,55 +340,62 @@ class PagedCache:
         return c
 
 
-def _layout(c: PagedCache):
+def _paged_layout(c: PagedCache) -> tuple:
+    """Device, type, sizes and strides of a cache whose tensors fit each other."""
+    if c.layout is not None:
+        return c.layout
     k, v, t, n = c.k, c.v, c.table, c.lens
-    return (k.shape, k.stride(), k.dtype, v.shape, v.stride(), v.dtype, t.shape, t.stride(), t.dtype, n.shape, n.stride(), n.dtype)
-
-
-def make_paged_params(cache: PagedCache, n_rows: int, h_q: int, causal: bool = True, scale: float = 0.0) -> dash_paged_params:
-    """Checks the cache's tensors once; the calls below take a cache of the same sizes, strides and types, and look at their own
-    arguments.  The strides of q, o, k_new and v_new are those of the tensors each call is given."""
-    k, v, t, n = cache.k, cache.v, cache.table, cache.lens
     if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in (torch.bfloat16, torch.float32):
         raise DashError("k and v pages: two tensors [n_pages, h_kv, page_size, d] of one type, bf16 or fp32")
     if k.stride(3) != 1 or v.stride(3) != 1:
         raise DashError("k and v pages: head_dim must be contiguous")
     if t.dim() != 2 or n.shape != t.shape[:1] or t.dtype != torch.int32 or n.dtype != torch.int32 or not (t.is_contiguous() and n.is_contiguous()):
         raise DashError("table [batch, max_pages] and lens [batch]: contiguous int32 tensors")
+    for x, dtype, shape in ((c.weights, torch.float32, k.shape[:3]), (c.pos, torch.int32, k.shape[:3]), (c.seen, torch.int32, n.shape)):
+        if x is not None and (x.dtype != dtype or x.shape != shape or not x.is_contiguous()):
+            raise DashError("weights (fp32) and pos (int32) [n_pages, h_kv, page_size], seen int32 [batch]: contiguous")
+    if any(x is not None and x.device != k.device for x in (v, t, n, c.weights, c.pos, c.seen)):
+        raise DashError("the cache's tensors lie on one device")
+    c.__dict__["layout"] = layout = (k.get_device(), k.dtype, k.shape, k.stride(), v.stride(), t.shape)
+    return layout
+
+
+def make_paged_params(cache: PagedCache, n_rows: int, h_q: int, causal: bool = True, scale: float = 0.0) -> dash_paged_params:
+    """The parameters of calls on this cache, or on others of the same sizes, strides and type.  The strides of q, o, k_new and
+    v_new are those of the tensors each call is given."""
+    layout = _paged_layout(cache)
     p = dash_paged_params()
-    p.batch, p.max_pages = t.shape
-    p.n_pages, p.h_kv, p.page_size, p.head_dim = k.shape
+    p.batch, p.max_pages = cache.table.shape
+    p.n_pages, p.h_kv, p.page_size, p.head_dim = cache.k.shape
     p.h_q, p.n_rows, p.causal, p.scale = h_q, n_rows, int(causal), scale
-    p.dtype = DASH_BF16 if k.dtype == torch.bfloat16 else DASH_F32
-    p.k_stride[:] = k.stride()[:3]
-    p.v_stride[:] = v.stride()[:3]
-    if v.device != k.device:
-        raise DashError("the tensors of a call lie on one device")
-    p.layout = _layout(cache)
+    p.dtype = DASH_BF16 if cache.k.dtype == torch.bfloat16 else DASH_F32
+    p.k_stride[:] = cache.k.stride()[:3]
+    p.v_stride[:] = cache.v.stride()[:3]
+    p.layout = layout
     return p
 
 
-def _paged_call(p: dash_paged_params, cache: PagedCache, row_start, rows, extra=(), ws=None):
-    """The call's own copy of p, with the strides of its packed tensors, and the current stream; rows: (tensor, heads, field of
-    its strides)."""
-    if _layout(cache) != p.layout:
-        raise DashError("the parameters are those of a cache of other sizes, strides or types (make_paged_params)")
+def _paged_call(p: dash_paged_params, cache: PagedCache, row_start, rows, extra=None, ws=None):
+    """The call's own copy of p, with the strides of its packed tensors, and the current stream.  rows: (tensor, heads, field of
+    its strides); extra: (tensor, type, shape)."""
+    layout = _paged_layout(cache)
+    if layout is not p.layout and layout != p.layout:
+        raise DashError("the parameters are those of a cache of other sizes, strides or type (make_paged_params)")
     p = dash_paged_params.from_buffer_copy(p)
-    n_rows, head_dim, dtype, dev = p.n_rows, p.head_dim, cache.k.dtype, cache.k.get_device()
+    dev, dtype = layout[:2]
     if row_start is not None and (row_start.dtype is not torch.int32 or row_start.numel() != p.batch + 1 or not row_start.is_contiguous()
                                   or row_start.get_device() != dev):
         raise DashError("row_start: a contiguous int32 tensor of batch + 1 elements on the cache's device")
-    for t, heads, field in rows:
+    for t, heads, name in rows:
         s = t.stride()
-        if t.dtype is not dtype or t.shape != (n_rows, heads, head_dim) or s[2] != 1 or t.get_device() != dev:
-            raise DashError(f"packed rows: [{n_rows}, {heads}, {head_dim}] of the cache's type and device, head_dim contiguous")
-        f = getattr(p, field)
+        if t.dtype is not dtype or t.shape != (p.n_rows, heads, p.head_dim) or s[2] != 1 or t.get_device() != dev:
+            raise DashError(f"packed rows: [{p.n_rows}, {heads}, {p.head_dim}] of the cache's type and device, head_dim contiguous")
+        f = getattr(p, name)
         f[0], f[1] = s[0], s[1]
-    for t, want, shape in extra:
-        if t is not None and (t.dtype is not want or t.shape != shape or not t.is_contiguous() or t.get_device() != dev):
+    if extra is not None and extra[0] is not None:
+        t, want, shape = extra
+        if t.dtype is not want or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
             raise DashError(f"expected a contiguous {want} tensor of shape {tuple(shape)} on the cache's device")
-    if cache.table.get_device() != dev or cache.lens.get_device() != dev or cache.v.get_device() != dev:
-        raise DashError("the cache's tensors lie on one device")
     if dev < 0 or (ws is not None and ws.get_device() != dev):
         raise DashError("the cache and the workspace lie on one GPU")
     if _device is None or _raw_stream is None or not torch.cuda.is_initialized():
@@ -405,9 +419,7 @@ def alloc_paged_workspace(p: dash_paged_params, device, evict: bool = False) -> 
 
 def dash_paged_append(p: dash_paged_params, cache: PagedCache, k_new, v_new, row_start) -> None:
     """k_new, v_new [n_rows, h_kv, d]; cache.weights, pos and seen as far as they are there."""
-    tok = cache.k.shape[:3]
-    p, stream = _paged_call(p, cache, row_start, ((k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride")),
-                            ((cache.weights, torch.float32, tok), (cache.pos, torch.int32, tok), (cache.seen, torch.int32, cache.lens.shape)))
+    p, stream = _paged_call(p, cache, row_start, ((k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride")))
     _check(load_library().dash_paged_append(p, k_new.data_ptr(), v_new.data_ptr(), cache.k.data_ptr(), cache.v.data_ptr(),
                                             row_start.data_ptr(), cache.lens.data_ptr(), cache.table.data_ptr(), _ptr(cache.weights),
                                             _ptr(cache.pos), _ptr(cache.seen), stream), "dash_paged_append")
@@ -416,7 +428,7 @@ def dash_paged_append(p: dash_paged_params, cache: PagedCache, k_new, v_new, row
 def dash_paged_attend(p: dash_paged_params, cache: PagedCache, q, row_start, o, ws: torch.Tensor, lse=None) -> None:
     """q, o [n_rows, h_q, d]; lse fp32 [n_rows, h_q] or None."""
     p, stream = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"), (o, p.h_q, "o_stride")),
-                            ((lse, torch.float32, (p.n_rows, p.h_q)),), ws)
+                            (lse, torch.float32, (p.n_rows, p.h_q)), ws)
     wp, wn = _ws_ptr(ws)
     _check(load_library().dash_paged_attend(p, q.data_ptr(), cache.k.data_ptr(), cache.v.data_ptr(), row_start.data_ptr(),
                                             cache.lens.data_ptr(), cache.table.data_ptr(), o.data_ptr(), _ptr(lse), wp, wn, stream),
@@ -427,8 +439,7 @@ def dash_paged_weigh(p: dash_paged_params, cache: PagedCache, q, row_start, lse,
     """Adds to cache.weights; lse as dash_paged_attend wrote it."""
     if cache.weights is None or lse is None:
         raise DashError("dash_paged_weigh needs the cache's weights and the rows' lse")
-    p, stream = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"),),
-                            ((lse, torch.float32, (p.n_rows, p.h_q)), (cache.weights, torch.float32, cache.k.shape[:3])), ws)
+    p, stream = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"),), (lse, torch.float32, (p.n_rows, p.h_q)), ws)
     wp, wn = _ws_ptr(ws)
     _check(load_library().dash_paged_weigh(p, q.data_ptr(), cache.k.data_ptr(), row_start.data_ptr(), cache.lens.data_ptr(),
                                            cache.table.data_ptr(), _ptr(lse), last, _ptr(cache.weights), wp, wn, stream), "dash_paged_weigh")
@@ -438,9 +449,7 @@ def dash_paged_evict(p: dash_paged_params, cache: PagedCache, budget: int, ws: t
     """ws from alloc_paged_workspace(p, device, evict=True); src int32 [batch, h_kv, budget] or None."""
     if cache.weights is None or cache.pos is None or cache.seen is None:
         raise DashError("dash_paged_evict needs the cache's weights, pos and seen")
-    tok = cache.k.shape[:3]
-    p, stream = _paged_call(p, cache, None, (), ((cache.weights, torch.float32, tok), (cache.pos, torch.int32, tok),
-                                                 (cache.seen, torch.int32, cache.lens.shape), (src, torch.int32, (p.batch, p.h_kv, budget))), ws)
+    p, stream = _paged_call(p, cache, None, (), (src, torch.int32, (p.batch, p.h_kv, budget)), ws)
     wp, wn = _ws_ptr(ws)
     _check(load_library().dash_paged_evict(p, cache.k.data_ptr(), cache.v.data_ptr(), cache.lens.data_ptr(), _ptr(cache.seen), cache.table.data_ptr(),
                                            _ptr(cache.weights), _ptr(cache.pos), budget, sinks, recent, _ptr(src), wp, wn, stream),

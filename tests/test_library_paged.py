@@ -1,6 +1,7 @@
 """CPU-side tests of the paged cache's entry points: sizes, refusals before any launch, the binding's checks, and the plain
 forms of the GPU tests against torch."""
 import ctypes
+import dataclasses
 import math
 
 import pytest
@@ -141,10 +142,10 @@ def test_the_binding_refuses_the_parameters_of_another_cache():
     fewer = {"k": c.k[:4], "v": c.v[:4], "table": c.table[:, :2].contiguous(), "lens": c.lens.long()}
     token = torch.zeros((8, 16, 2, 64), dtype=torch.bfloat16).transpose(1, 2)
     for field, x in (*fewer.items(), ("table", c.table[:1]), ("k", token), ("v", token), ("k", c.k.float())):
-        other = B.PagedCache(**{**vars(c), field: x})
+        other = dataclasses.replace(c, **{field: x})
         for f in (lambda: B.dash_paged_attend(p, other, q, start, q.clone(), ws), lambda: B.dash_paged_evict(p, other, 8, ws),
                   lambda: B.dash_paged_append(p, other, q[:, :2], q[:, 2:], start)):
-            with pytest.raises(B.DashError, match="another|other sizes"):
+            with pytest.raises(B.DashError, match="other sizes|fit each other|int32|pages"):
                 f()
     with pytest.raises(B.DashError, match="GPU"):               # other tensors, alike
         B.dash_paged_attend(p, B.PagedCache(c.k.clone(), c.v.clone(), c.table.clone(), c.lens.clone()), q, start, q.clone(), ws)
@@ -173,3 +174,19 @@ def test_the_plain_forms_agree_with_torch():
 def test_the_kernels_use_no_scratch_memory():
     scratch = {n: b for n, b in kernel_scratch(B.LIB_PATH).items() if "dash" in n and "paged_" in n}
     assert len(scratch) >= 20 and not {n: b for n, b in scratch.items() if b}
+
+
+def test_the_binding_looks_at_a_tensor_that_is_assigned():
+    c = B.PagedCache.allocate(2, 2, 8, 16, 64, 4, "cpu", evicting=True)
+    p = B.make_paged_params(c, 3, 4)
+    ws = torch.empty(1 << 20, dtype=torch.uint8)
+    for field, bad in (("weights", c.weights.double()), ("weights", c.weights[:4]), ("pos", c.pos.long()), ("pos", c.pos.transpose(1, 2)),
+                       ("seen", c.seen[:1]), ("lens", c.lens.long()), ("v", c.v.float()), ("table", c.table.t())):
+        good = getattr(c, field)
+        setattr(c, field, bad)
+        with pytest.raises(B.DashError, match="contiguous|pages"):
+            B.dash_paged_evict(p, c, 8, ws)
+        setattr(c, field, good)
+    c.weights = c.weights.clone()
+    with pytest.raises(B.DashError, match="GPU"):
+        B.dash_paged_evict(p, c, 8, ws)
