@@ -6,8 +6,8 @@
 // end.  Each sum is one wave's (or, for rows cut into parts, one thread's over the parts), so results do not depend on timing.
 // A single token: K is read once, HBM bounds it.  Many: an exponential, an FMA and an addition per pair, 24 clocks of a SIMD for 64
 // pairs, against 16 (head dimension 128; 64: 8) of matrix work: two sequences of 6000 and 16000 tokens, 1999 new ones, 16 heads of 64
-// on 4: 155 us, 144 of them the main kernel, where the vector units alone take 147 at the highest clock and the matrix products 45.  One
-// of 32768, 2048 new, 32 heads of 128 on 8: 517 us, 1.03 PFLOP/s of matrix work.
+// on 4: 155 us the call, which the vector units alone would take 147 for at the highest clock and the matrix products 80 at a large
+// one's rate.  One of 32768, 2048 new, 32 heads of 128 on 8: 518 us, 1.03 PFLOP/s of matrix work.
 //
 // (block of keys, row tile) pairs of all sequences are dealt evenly to a fixed number of workgroups; blocks cut between two of them
 // are added up by a second launch, in a fixed order.
