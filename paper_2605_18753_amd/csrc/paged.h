@@ -11,7 +11,8 @@
 //   piece of an item, and most are cut.  1501 tokens beside seven decoding sequences of up to 12k 305 -> 309 us and the records to add
 //   up, 2048 tokens against 32k 995 -> 1088.)
 // Cut items leave records.  Of parts a second launch adds them up; of runs the workgroup whose record of an item is complete last, which
-// sees the flags of all (stored past the caches, as in decode_body.h; who merges clears them, so a captured launch can be replayed).
+// sees the flags of all (stored past the caches, as in decode_body.h; who merges clears them, so a captured launch can be replayed), or where
+// there are many in two levels.
 #pragma once
 #include "common.h"
 #include "dash_internal.h"
@@ -29,7 +30,7 @@ struct PagedArgs {
   float c1;                              // scale * log2(e)
   int wgs;                               // runs of a kv-head; 0: an item a workgroup.  Tiles of 128 rows: parts of a kv-head at most; 0: none is cut
   float* part_o; float* part_ml;         // records of cut items: two of each run (the item it begins in, the one it ends in), one of each part
-  uint64_t* flags; uint64_t nonce;       // runs: of each record, and the number that says that it is complete
+  uint64_t* flags; uint64_t nonce;       // runs: two of each record, and the number that says that it is complete
 };
 
 __device__ __forceinline__ int paged_len(const PagedArgs& a, int b) { return min(max(a.lens[b], 0), a.cap); }

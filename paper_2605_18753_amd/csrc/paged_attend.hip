@@ -4,7 +4,8 @@
 //
 // Few rows (decode, drafted tokens): a tile is 16 (token, head) rows, the heads of a kv-head's group for 16 / g tokens.  The
 // cache is read once for 4 g flops a byte, so HBM bounds it; a workgroup's four waves take 32-key tiles in turn, each through a ring of
-// its own in LDS (two tiles deep, global -> LDS copies), without a barrier until the four add up at the end.
+// its own in LDS (two tiles deep, global -> LDS copies), without a barrier until the four add up at the end.  A token of each of 32 sequences of
+// 4096 to 32768, 32 / 8 heads of 128: 415 us, 5.9 TB/s; one sequence of 1000: 9.3 us, a chain of round trips.
 #include <math.h>
 
 #include <type_traits>
@@ -113,7 +114,13 @@ struct PagedSum {
 // Behind a piece of an item that is cut between runs: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p, by the workgroup that sees the flags
 // of all its pieces.  They are those of runs w1, w1 + 1, ..; the first left its run's second record, the others their runs' first.  D / 4 threads
 // a row, 4 values each, and where the item has few rows several groups of threads that take every so manieth piece.  (A launch of its
-// own for this: one sequence of 1000 tokens, 32 / 8 heads, 11.1 us a step instead of 9.7.)
+// own for this: one sequence of 1000 tokens, 32 / 8 heads, 11.1 us a step instead of 9.3.)
+// Where a thread would have more than kChain records to add one after the other, two levels: groups of 8 or 16 pieces, each added up by a workgroup
+// that sees its flags into a record that nobody uses (the second of a run in the middle of the item), then the groups.  More than one workgroup
+// may see all flags; they write the same.  A second flag says that a piece's workgroup is done with its group: who sees all of these adds
+// up the groups and clears the flags, none of which is set after that.  (16 heads on one, one sequence of 16000 tokens, 125 pieces: 92 us in one
+// level, 20 in two; 32 on 8, 1000 tokens, 8 pieces: 11 in two, 9.3 in one.)
+constexpr int kChain = 24;
 template <typename T, int D, int THREADS>
 __device__ __forceinline__ void paged_few_join(const PagedArgs& a, const PagedRun& run, int r, int wg, char* lds) {
   constexpr int TPR = D / 4, UNITS = THREADS / TPR;        // threads of a row; rows at a time
@@ -137,48 +144,87 @@ __device__ __forceinline__ void paged_few_join(const PagedArgs& a, const PagedRu
   }
   const int64_t rec0 = ((int64_t)r * a.wgs + w1) * 2;
   auto record = [&](int p) { return p == 0 ? rec0 + 1 : rec0 + 2 * p; };
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // the record is in memory ...
-  __syncthreads();
-  if (threadIdx.x < 64) {
-    if (lane == 0) __hip_atomic_store(a.flags + record(wg - w1), a.nonce, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // ... before its flag, and that before the flags are read
-    bool seen = true;
-    for (int p = lane; p < pieces; p += 64) seen &= agent_load(a.flags + record(p)) == a.nonce;
-    const bool ok = __all(seen);
-    if (lane == 0) *all = ok;
-  }
-  __syncthreads();
-  if (!*all) return;
+  uint64_t* done = a.flags + (int64_t)a.wgs * a.h_kv * 2;
+  // sets the flag of this piece, behind all that the workgroup has stored, and tells whether those of pieces p0 .. p1 - 1 are set
+  auto complete = [&](uint64_t* flags, int p0, int p1) -> bool {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the record is in memory ...
+    __syncthreads();
+    if (threadIdx.x < 64) {
+      if (lane == 0) __hip_atomic_store(flags + record(wg - w1), a.nonce, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");     // ... before its flag, and that before the flags are read
+      bool seen = true;
+      for (int p = p0 + lane; p < p1; p += 64) seen &= agent_load(flags + record(p)) == a.nonce;
+      const bool ok = __all(seen);
+      if (lane == 0) *all = ok;
+    }
+    __syncthreads();
+    return *all;
+  };
   const int rows = min(run.deal.T, it.m - it.tile * run.deal.T) * a.g;
   const int slices = rows * 4 <= UNITS ? 4 : rows * 2 <= UNITS ? 2 : 1, per = UNITS / slices;
   const int c = threadIdx.x % TPR, unit = threadIdx.x / TPR, slice = unit / per;
-  for (int i0 = 0; i0 < rows; i0 += per) {
-    const int in = min(i0 + unit % per, rows - 1);
-    const float* ml = a.part_ml + in * 2;
-    PagedSum sum;
-    const float* po = a.part_o + in * D + c * 4;
-#pragma unroll 4
-    for (int p = slice; p < pieces; p += slices) {
-      const uint64_t y = agent_load(ml + record(p) * 32), v0 = agent_load(po + record(p) * (16 * D)), v1 = agent_load(po + record(p) * (16 * D) + 2);
-      sum.add(__uint_as_float((uint32_t)y), __uint_as_float((uint32_t)(y >> 32)),
-              f32x4{__uint_as_float((uint32_t)v0), __uint_as_float((uint32_t)(v0 >> 32)), __uint_as_float((uint32_t)v1), __uint_as_float((uint32_t)(v1 >> 32))});
+  // adds up `count` records, place(i) the i-th; write(row, sum) by the threads that hold a row's sum
+  auto add_up = [&](int count, auto&& place, auto&& write) {
+    for (int i0 = 0; i0 < rows; i0 += per) {
+      const int in = min(i0 + unit % per, rows - 1);
+      const float* ml = a.part_ml + in * 2;
+      PagedSum sum;
+      const float* po = a.part_o + in * D + c * 4;
+      for (int p0 = slice; p0 < count; p0 += 4 * slices) {
+        uint64_t y[4], v0[4], v1[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) {                        // asked for together; behind the last one it again
+          const int64_t at = place(min(p0 + k * slices, count - 1));
+          y[k] = agent_load(ml + at * 32);
+          v0[k] = agent_load(po + at * (16 * D));
+          v1[k] = agent_load(po + at * (16 * D) + 2);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; k++)
+          if (p0 + k * slices < count)
+            sum.add(__uint_as_float((uint32_t)y[k]), __uint_as_float((uint32_t)(y[k] >> 32)),
+                    f32x4{__uint_as_float((uint32_t)v0[k]), __uint_as_float((uint32_t)(v0[k] >> 32)), __uint_as_float((uint32_t)v1[k]), __uint_as_float((uint32_t)(v1[k] >> 32))});
+      }
+      if (slices > 1) {
+        __syncthreads();
+        xo[threadIdx.x] = sum.o;
+        if (c == 0) { xd[2 * unit] = sum.m; xd[2 * unit + 1] = sum.den; }
+        __syncthreads();
+        for (int k = 1; k < slices && slice == 0; k++) sum.add(xd[2 * (unit + k * per)], xd[2 * (unit + k * per) + 1], xo[threadIdx.x + k * per * TPR]);
+      }
+      if (slice == 0 && i0 + unit < rows) write(in, sum);
     }
-    if (slices > 1) {
-      __syncthreads();
-      xo[threadIdx.x] = sum.o;
-      if (c == 0) { xd[2 * unit] = sum.m; xd[2 * unit + 1] = sum.den; }
-      __syncthreads();
-      for (int k = 1; k < slices && slice == 0; k++) sum.add(xd[2 * (unit + k * per)], xd[2 * (unit + k * per) + 1], xo[threadIdx.x + k * per * TPR]);
-    }
-    const float M = sum.m, den = sum.den;
-    const f32x4 o = sum.o;
-    if (slice > 0 || i0 + unit >= rows) continue;
-    const float inv = den > 0.f ? 1.f / den : den == 0.f ? 0.f : den;
+  };
+  auto output = [&](int in, const PagedSum& sum) {
+    const float inv = sum.den > 0.f ? 1.f / sum.den : sum.den == 0.f ? 0.f : sum.den;
     const int row = it.r0 + it.tile * run.deal.T + in / a.g, head = r * a.g + in % a.g;
-    put_row4((T*)a.o + row * a.o_t + head * a.o_h + c * 4, o, inv);
-    if (a.lse && c == 0) a.lse[(int64_t)row * a.h_q + head] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
+    put_row4((T*)a.o + row * a.o_t + head * a.o_h + c * 4, sum.o, inv);
+    if (a.lse && c == 0) a.lse[(int64_t)row * a.h_q + head] = sum.den == 0.f ? -INFINITY : (sum.m + log2f(sum.den)) * kLn2;
+  };
+  const bool levels = ((rows + per - 1) / per) * pieces > kChain * slices && pieces > 8;
+  if (levels) {
+    const int size = pieces > 128 ? 16 : 8, me = wg - w1, first = me / size * size, members = min(size, pieces - first);
+    // group's record: a last piece on its own is one already
+    auto group = [&](int i) { return i * size == pieces - 1 ? record(i * size) : rec0 + 2 * max(i * size, 1) + 1; };
+    if (complete(a.flags, first, first + members) && members > 1) {
+      const int64_t to = group(first / size);
+      add_up(members, [&](int p) { return record(first + p); }, [&](int in, const PagedSum& sum) {
+        float* po = a.part_o + (to * 16 + in) * D + c * 4;
+        agent_store(po, sum.o[0], sum.o[1]);
+        agent_store(po + 2, sum.o[2], sum.o[3]);
+        if (c == 0) agent_store(a.part_ml + (to * 16 + in) * 2, sum.m, sum.den);
+      });
+    }
+    if (!complete(done, 0, pieces)) return;
+    add_up((pieces + size - 1) / size, group, output);
+  } else {
+    if (!complete(a.flags, 0, pieces)) return;
+    add_up(pieces, record, output);
   }
-  for (int p = threadIdx.x; p < pieces; p += THREADS) __hip_atomic_store(a.flags + record(p), (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  for (int p = threadIdx.x; p < pieces; p += THREADS) {
+    __hip_atomic_store(a.flags + record(p), (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (levels) __hip_atomic_store(done + record(p), (uint64_t)0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
 }
 
 template <int D>
@@ -437,7 +483,8 @@ __global__ __launch_bounds__(512) void paged_few_f32_kernel(PagedArgs args) {
 // transposing reads, B = P): in the 32x32 accumulator layout lane (n = lane % 32, h = lane / 32) holds, for row n, keys 8 q + 4 h + i,
 // which are its slots of operand B once the contraction runs in that order, so nothing moves between the products.
 // A wave pipelines its tiles: the first product of tile i runs with the exponentials of tile i - 1, the second product of
-// tile i - 1 with the row maxima of tile i.
+// tile i - 1 with the row maxima of tile i.  Bound by the matrix units at the power limit: 2048 tokens at the end of 32768, 32 / 8 heads of 128,
+// 980 to 1080 us from card to card, 1.0 to 1.09 PFLOP/s.
 template <int D> struct RowsCfg {
   static constexpr int NCH = D / 8, ROW_BYTES = D * 2;
   static constexpr int TILE_BYTES = 64 * ROW_BYTES;
@@ -800,11 +847,16 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
-// The kernel for a call: tiles of 128 rows where the sequences bring more than 16 rows each on the average, tiles of 16 otherwise.
-static bool use_rows(const PagedArgs& a, int dtype) { return dtype == DASH_BF16 && (int64_t)a.n_rows * a.g > (int64_t)a.batch * 16; }
 static int64_t most_items(const PagedArgs& a, int rows) {   // of a kv-head
   const int T = rows / a.g;
   return min((int64_t)a.n_rows / T + min(a.batch, a.n_rows), (int64_t)a.n_rows);
+}
+// The kernel for a call: tiles of 128 rows where the sequences bring more than 16 rows each on the average, tiles of 16 otherwise.  (32 / 8 heads, tiles of 128
+// and of 16.  16 rows each: 64 sequences of 2000 tokens 99.6 and 97.7 us, one of 1000 14.7 and 11.0; 20 rows: 101 and 167, 8 of 16000 104 and 103; 48
+// rows: 108 and 281.)  Short caches are read from the last-level cache again and again at no cost: tiles of 16 as long as each has a CU (one
+// of 1000 tokens, 64 rows 15.9 and 12.4 us, 128 17.3 and 11.8).
+static bool use_rows(const PagedArgs& a, int dtype) {
+  return dtype == DASH_BF16 && (int64_t)a.n_rows * a.g > (int64_t)a.batch * 16 && !(a.cap <= 8 * kStep && most_items(a, 16) * a.h_kv <= 256);
 }
 // Workgroups of a kv-head that are resident at once: one a CU for the 128 KB ring of 16-row tiles and the fp32 kernel, two otherwise.
 static int runs_of(const PagedArgs& a, int dtype, int d, bool big) { return max((!big && (dtype == DASH_F32 || d == 128) ? 256 : 512) / a.h_kv, 1); }
@@ -813,7 +865,7 @@ static size_t ws_align(size_t x) { return (x + 255) & ~(size_t)255; }
 size_t paged_attend_ws(const PagedArgs& a, int dtype, int d) {
   const size_t few = (size_t)runs_of(a, dtype, d, false) * a.h_kv * 2 * 16;    // rows of records
   const size_t rows = dtype == DASH_BF16 ? (size_t)runs_of(a, dtype, d, true) * a.h_kv * 128 : 0, recs = few > rows ? few : rows;
-  return ws_align(recs * 8) + recs * d * 4 + few / 16 * 8;
+  return ws_align(recs * 8) + recs * d * 4 + few / 16 * 16;   // two flags a record of 16 rows
 }
 
 template <int D>
@@ -821,9 +873,12 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
   const bool big = use_rows(a, dtype);
   const int runs = runs_of(a, dtype, D, big);
   const int64_t items = most_items(a, big ? 128 : 16);
-  // Runs of small tiles cost little (a record is 16 rows) and even out the lengths of a batch; with many items a workgroup each evens them out as well.
+  // Runs of small tiles cost little (a record is 16 rows) and even out the lengths of a batch; with many items a workgroup each evens them out as well.  (A
+  // token of 64 sequences of 1000 to 4000 tokens, 32 / 8 heads, 119 us in runs, 122 without; of 256, 8 items a run, 454 both ways.  Tiles of 128: 700
+  // tokens against 32k 435 in parts, 641 without; two of 700 against 4k 115 and 113.)
   a.wgs = items < (big ? 1 : 8) * (int64_t)runs ? runs : 0;
-  // Items of up to eight steps are not worth a launch that adds them up, if there is one for every other CU.
+  // Items of up to eight steps are not cut if there is one for every other CU.  (16 sequences of 200 to 1000 tokens, 32 / 8 heads: 13 us, in runs 19; fewer
+  // items: one of 1000 tokens 11.7, in runs 9.3.)
   if (!big && a.cap <= 8 * kStep && items * a.h_kv >= 128) a.wgs = 0;
   const size_t recs = (size_t)a.wgs * a.h_kv * (big ? 128 : 2 * 16);
   a.part_ml = (float*)ws;
@@ -847,10 +902,10 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.wgs <= 1 || !big) return e;
-  // few rows leave the chip idle unless several groups of threads share a row's parts
+  // few rows leave the chip idle unless several groups of threads share a row's parts (1280 rows, the call: 32.8 us shared, 34.0 not; 2048 59.4 and 58.0)
   const int64_t out = (int64_t)a.n_rows * a.h_q;
   constexpr int units = 256 / (D / 4);
-  if (out <= 8192) hipLaunchKernelGGL((paged_merge_kernel<D, 4>), dim3((unsigned)((out + units / 4 - 1) / (units / 4))), blk, 0, st, a);
+  if (out <= 1536) hipLaunchKernelGGL((paged_merge_kernel<D, 4>), dim3((unsigned)((out + units / 4 - 1) / (units / 4))), blk, 0, st, a);
   else hipLaunchKernelGGL((paged_merge_kernel<D, 1>), dim3(1024), blk, 0, st, a);
   return hipGetLastError();
 }

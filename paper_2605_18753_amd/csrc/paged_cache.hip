@@ -8,7 +8,8 @@ namespace dash {
 // ---- append ----------------------------------------------------------------------------------------------------------
 // A wave writes a packed row: its keys and values of all kv-heads, 16 bytes a lane at a time.  Bound by HBM where there are many rows (each
 // byte is read once and written once), by the chain of dependent loads where there are few: what a row holds, and the starts,
-// lengths and positions of 64 sequences, are asked for together; only the page waits for them.
+// lengths and positions of 64 sequences, are asked for together; only the page waits for them.  (2047 tokens of each of four sequences, 8 heads
+// of 128: 12.3 us, 5.5 TB/s; a token of 64: 4.4 us.)
 template <int ES, int D>   // bytes of an element
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedArgs a) {
   constexpr int CHUNKS = D * ES / 16, AHEAD = 4;             // 16-byte pieces of a row; pieces of a lane in flight
@@ -101,7 +102,8 @@ __device__ __forceinline__ uint32_t evict_key(float w, int pos, int sinks, int f
 }
 
 constexpr int kBins = 2048;                                // 11 bits of a key
-constexpr int kSelThreads = 1024, kSelKeys = 8192;         // caches of up to so many slots: a workgroup per pair, keys in LDS
+// caches of up to so many slots: a workgroup per pair, keys in LDS (two of 8000 tokens x 8 30 us, in three launches 38; sixteen 71 and 82)
+constexpr int kSelThreads = 1024, kSelKeys = 8192;
 constexpr int kCands = 2048, kRanked = 256;                // keys that are picked out; that are ranked against each other
 constexpr int kChunk = 4096, kChunkThreads = 256;          // longer ones: slots and threads of a workgroup
 
@@ -494,7 +496,8 @@ __global__ __launch_bounds__(kChunkThreads) void paged_long_list_kernel(EvictArg
   if (k.c == front - 1 && tid == 0) e.counts[pair] = holes + own.x;
 }
 
-// A wave moves eight tokens at a time: their places first, a lane each, then all their rows at once.
+// A wave moves eight tokens at a time: their places first, a lane each, then all their rows at once.  Bound by HBM: 65536 tokens of 128, 67 MB
+// read and written, 15 us.
 template <int ES, int D>
 __global__ __launch_bounds__(256) void paged_move_kernel(EvictArgs e, int wgs) {   // wgs: workgroups of a pair
   const PagedArgs& a = e.a;

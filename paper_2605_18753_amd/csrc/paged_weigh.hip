@@ -392,7 +392,8 @@ __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a)
 // resident workgroups of a kv-head, by the registers of a wave: three per CU at head dimension 128, four at 64; fp32 two and three
 static int weigh_wgs(const PagedArgs& a, int dtype, int d) { return max(256 * ((d == 128 ? 3 : 4) - (dtype != DASH_BF16)) / a.h_kv, 1); }
 
-// K is streamed where the sequences bring no more than 16 rows each on the average
+// K is streamed where the sequences bring no more than 16 rows each on the average (16 sequences of 2048 to 16384 tokens, 32 / 8 heads: 16 rows
+// 73 us streamed, 84 not; 20 rows 118 and 93)
 static bool weigh_stream(const PagedArgs& a) { return (int64_t)a.n_rows * a.g <= (int64_t)a.batch * 16; }
 
 size_t paged_weigh_ws(const PagedArgs& a, int dtype, int d) {

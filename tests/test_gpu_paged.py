@@ -130,6 +130,34 @@ def test_long_caches_are_cut_and_joined(dtype, n, news):
     s.check_attend()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("h_kv,g,lens,news", [(1, 16, [17000, 30], [1, 1]), (1, 8, [8200, 9000, 50], [2, 1, 0]), (2, 16, [4100], [1]), (1, 1, [40000], [3]),
+                                              (4, 4, [2177], [4])])
+@pytest.mark.parametrize("d", [64, 128])
+def test_long_caches_of_few_heads_are_joined_in_levels(dtype, h_kv, g, lens, news, d):
+    Setup(lens, news, h_kv=h_kv, g=g, d=d, dtype=dtype, page=64, seed=34).check_attend()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_join_in_levels_in_a_captured_graph(dtype):
+    s = Setup([17000], [1], h_kv=1, g=16, d=64, dtype=dtype, page=64, seed=35)
+    p, q = s.params(), s.q.to(DEV)
+    o, lse, ws = torch.empty_like(q), torch.empty((1, 16), device=DEV), B.alloc_paged_workspace(p, DEV)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        B.dash_paged_attend(p, s.gpu, q, s.start_gpu, o, ws, lse=lse)
+    for n in (17000, 900, 16500, 8191, 3, 17000):               # as many pieces as there are runs, some, one
+        s.gpu.lens[0] = n
+        s.ref.lens[0] = n
+        want, wl = s.attend()
+        for _ in range(3):
+            o.fill_(77.0)
+            lse.fill_(77.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(o.cpu(), want) and torch.equal(lse.cpu(), wl)
+
+
 def test_peaked_and_falling_logits():
     # logits of several hundred in rising and in falling order: the running maximum moves all the way, or never
     for sign in (1.0, -1.0):
