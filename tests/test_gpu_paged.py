@@ -115,6 +115,25 @@ def test_whole_prompts(dtype, d):
     s.check_attend()
 
 
+# tables wide enough for tiles of 128 rows, whatever the lengths
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d,page,h_kv,g", [(128, 16, 2, 4), (64, 16, 3, 2), (128, 64, 1, 16), (64, 256, 2, 8), (128, 32, 4, 1)])
+@pytest.mark.parametrize("news", [[7, 0, 33, 1, 130, 64, 9], [40, 20, 0, 1, 0, 3, 0], [0, 0, 0, 0, 700, 0, 0]])
+def test_chunks_in_wide_tables(causal, d, page, h_kv, g, news):
+    s = Setup([500, 20, 33, 1, max(131, news[4]), 64, 0], news, h_kv=h_kv, g=g, d=d, page=page, spare=3, behind=math.inf, seed=36, width=4096 // page)
+    s.check_attend(causal)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [16, 128])
+def test_whole_prompts_in_wide_tables(d, page):
+    s = Setup(EDGE, EDGE, h_kv=2, g=4, d=d, page=page, behind=math.nan, seed=37, width=4096 // page)
+    s.check_attend()
+    s = Setup([5, 0, 20, 1], [90, 64, 300, 33], d=d, page=page, behind=math.nan, seed=38, width=4096 // page)
+    lse = s.check_attend()
+    assert torch.isneginf(lse).sum() == (85 + 64 + 280 + 32) * 8
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_rows_that_see_nothing(dtype):
     # more new tokens than the cache holds: the first of them lie before slot 0
@@ -174,7 +193,11 @@ def test_peaked_and_falling_logits():
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_strided_queries_outputs_and_pages(dtype):
-    s = Setup([100, 333], [5, 80], dtype=dtype, page=32, layout="token", seed=8)
+    check_strides(Setup([100, 333], [5, 80], dtype=dtype, page=32, layout="token", seed=8), dtype)
+    check_strides(Setup([100, 333], [5, 80], dtype=dtype, page=32, layout="token", seed=8, width=64), dtype)
+
+
+def check_strides(s, dtype):
     s.check_attend()
     big = torch.full((s.rows, 2 * 8, 128 + 8), 5.0, dtype=dtype, device=DEV)
     q = big[:, 8:, 8:]
@@ -224,12 +247,13 @@ def test_pages_past_four_gigabytes():
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_a_bad_page_spoils_its_own_sequence_only(dtype):
-    s = Setup([100, 90], [2, 2], dtype=dtype, seed=12)
-    good, _ = s.attend()
-    for bad in (1 << 30, -5, s.gpu.k.shape[0]):
-        s.gpu.table[0, 2] = bad
-        o, _ = s.attend()
-        assert torch.equal(o[2:4], good[2:4])
+    for m, width in ((2, None), (40, 128)):
+        s = Setup([100, 90], [m, m], dtype=dtype, seed=12, width=width)
+        good, _ = s.attend()
+        for bad in (1 << 30, -5, s.gpu.k.shape[0]):
+            s.gpu.table[0, 2] = bad
+            o, _ = s.attend()
+            assert torch.equal(o[m:2 * m], good[m:2 * m])
 
 
 def test_lengths_and_row_starts_out_of_range_are_clamped():
