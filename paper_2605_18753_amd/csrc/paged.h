@@ -7,7 +7,9 @@
 //   Tiles of 16 rows: the steps of all items of a kv-head lie one behind the other, and G workgroups take equal runs
 //   [w F / G, (w + 1) F / G) of them: whatever the lengths, every CU streams as many keys.
 //   Tiles of 128 rows: one item a workgroup; items that leave the chip idle are cut into parts.  With n items of costs c_i and W > n
-//   workgroups, parts of S = ceil(sum c_i / (W - n)) give sum ceil(c_i / S) <= W of them.  (Equal runs for these as well: a run begins anew for every
+//   workgroups, parts of S = ceil(sum c_i / (W - n)) give sum ceil(c_i / S) <= W of them.  W is what is resident at once, or n and one and a
+//   half times that where the items' lengths would leave much of the chip idle.  (40 tokens of 40 sequences of 300 to 8000, 32 / 2 heads: 196 us with
+//   the first, 157 with the second; 700 of one of 30000 384 and 360; where the first is kept, 1501 tokens beside decoding ones, 305 and 326.)  (Equal runs for these as well: a run begins anew for every
 //   piece of an item, and most are cut.  1501 tokens beside seven decoding sequences of up to 12k 305 -> 309 us and the records to add
 //   up, 2048 tokens against 32k 995 -> 1088.)
 // Cut items leave records.  Of parts a second launch adds them up; of runs the workgroup whose record of an item is complete last, which
@@ -29,6 +31,7 @@ struct PagedArgs {
   int64_t q_t, q_h, o_t, o_h, kn_t, kn_h, vn_t, vn_h, kp_p, kp_h, kp_t, vp_p, vp_h, vp_t;
   float c1;                              // scale * log2(e)
   int wgs;                               // runs of a kv-head; 0: an item a workgroup.  Tiles of 128 rows: parts of a kv-head at most; 0: none is cut
+  int slots; float gain;                 // tiles of 128 rows: workgroups of a kv-head that are resident at once; what finer parts must come to
   float* part_o; float* part_ml;         // records of cut items: two of each run (the item it begins in, the one it ends in), one of each part
   uint64_t* flags; uint64_t nonce;       // runs: two of each record, and the number that says that it is complete
 };
@@ -81,7 +84,16 @@ template <typename F> __device__ __forceinline__ int paged_part_size(const Paged
     most = fmaxf(most, wave_max(s.x > 0 ? (float)s.y : 0.f));
   }
   if (items >= a.wgs) return kUncut;
-  const int S = max((int)fminf(cost * 1.0001f / (float)(a.wgs - items), 1e9f) + 1, kMinPart);   // the factor covers the sum's rounding
+  const auto size = [&](int w) { return max((int)fminf(cost * 1.0001f / (float)(w - items), 1e9f) + 1, kMinPart); };   // the factor covers the sum's rounding
+  // The time, in steps, of parts that are all resident (or of items, where more are not), and of finer ones that follow each other: what everybody
+  // has on the average, half a part until the last is done, and 4 steps for what a part costs besides
+  const float even = cost / (float)a.slots;
+  int S = items < a.slots ? size(a.slots) : kUncut;
+  const float time = items <= a.slots ? fminf((float)S, most) : even + 0.5f * most;
+  if (a.wgs > a.slots) {
+    const int fine = size(a.wgs);
+    if (even + 0.5f * (float)fine + 4.f < a.gain * time) S = fine;
+  }
   return (float)S >= most ? kUncut : S;
 }
 

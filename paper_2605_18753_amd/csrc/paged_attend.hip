@@ -860,11 +860,12 @@ static bool use_rows(const PagedArgs& a, int dtype) {
 }
 // Workgroups of a kv-head that are resident at once: one a CU for the 128 KB ring of 16-row tiles and the fp32 kernel, two otherwise.
 static int runs_of(const PagedArgs& a, int dtype, int d, bool big) { return max((!big && (dtype == DASH_F32 || d == 128) ? 256 : 512) / a.h_kv, 1); }
+static int most_parts(int runs) { return runs * 7 / 2; }   // of a kv-head: fewer than two items a resident workgroup, and one and a half
 static size_t ws_align(size_t x) { return (x + 255) & ~(size_t)255; }
 
 size_t paged_attend_ws(const PagedArgs& a, int dtype, int d) {
   const size_t few = (size_t)runs_of(a, dtype, d, false) * a.h_kv * 2 * 16;    // rows of records
-  const size_t rows = dtype == DASH_BF16 ? (size_t)runs_of(a, dtype, d, true) * a.h_kv * 128 : 0, recs = few > rows ? few : rows;
+  const size_t rows = dtype == DASH_BF16 ? (size_t)most_parts(runs_of(a, dtype, d, true)) * a.h_kv * 128 : 0, recs = few > rows ? few : rows;
   return ws_align(recs * 8) + recs * d * 4 + few / 16 * 16;   // two flags a record of 16 rows
 }
 
@@ -876,7 +877,12 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
   // Runs of small tiles cost little (a record is 16 rows) and even out the lengths of a batch; with many items a workgroup each evens them out as well.  (A
   // token of 64 sequences of 1000 to 4000 tokens, 32 / 8 heads, 119 us in runs, 122 without; of 256, 8 items a run, 454 both ways.  Tiles of 128: 700
   // tokens against 32k 435 in parts, 641 without; two of 700 against 4k 115 and 113.)
-  a.wgs = items < (big ? 1 : 8) * (int64_t)runs ? runs : 0;
+  a.wgs = items < (big ? 2 : 8) * (int64_t)runs ? runs : 0;
+  // Fine parts, if the lengths ask for them (paged_part_size).  Tiles of less than 64 rows on the average are bound by HBM, which idle workgroups hardly
+  // slow down: only if they are much faster (5 tokens of 64 sequences of 300 to 4000: 122 us, in fine parts 130).
+  if (big && a.wgs && items * 4 >= runs) a.wgs = (int)items + runs * 3 / 2;
+  a.slots = runs;
+  a.gain = (int64_t)a.n_rows * a.g < 64 * items ? 0.65f : 0.9f;
   // Items of up to eight steps are not cut if there is one for every other CU.  (16 sequences of 200 to 1000 tokens, 32 / 8 heads: 13 us, in runs 19; fewer
   // items: one of 1000 tokens 11.7, in runs 9.3.)
   if (!big && a.cap <= 8 * kStep && items * a.h_kv >= 128) a.wgs = 0;

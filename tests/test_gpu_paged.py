@@ -124,6 +124,12 @@ def test_chunks_in_wide_tables(causal, d, page, h_kv, g, news):
     s.check_attend(causal)
 
 
+@pytest.mark.parametrize("h_kv,g,d,batch,new", [(8, 1, 64, 30, 130), (16, 4, 128, 14, 30), (8, 2, 64, 70, 20), (32, 1, 64, 6, 140)])
+def test_items_of_unequal_lengths_are_cut_finely(h_kv, g, d, batch, new):
+    lens = [max(new, 2600 if i % 7 == 3 else (97 * i) % 200) for i in range(batch)]
+    Setup(lens, [new] * batch, h_kv=h_kv, g=g, d=d, page=64, seed=39).check_attend()
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("page", [16, 128])
 def test_whole_prompts_in_wide_tables(d, page):
