@@ -258,22 +258,37 @@ __global__ __launch_bounds__(256, (D == 128 ? 3 : 4) - (sizeof(T) == 4)) void pa
 }
 
 // Items cut between runs.  The end of run wg - 1 lies inside an item whose first piece is that run's: its last record.  Of the runs
-// behind it that begin inside the item, the first records follow.  A thread per key.
+// behind it that begin inside the item, the first records follow.  A thread per key; 16 records are asked for
+// together.  (One after the other: 700 tokens of 2000, 8 heads on one, 95 records, the call 44 us instead of 23.)
 template <typename T>
 __global__ __launch_bounds__(kWeighKeys<T>) void paged_weigh_sum_kernel(PagedArgs a) {
-  const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv + 1;
-  const int64_t total = weigh_total<kWeighKeys<T>>(a);
+  constexpr int KEYS = kWeighKeys<T>, AHEAD = 16;
+  const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv + 1, lane = threadIdx.x & 63;
+  const int64_t total = weigh_total<KEYS>(a);
   const PagedBounds<int64_t> bounds(a, total);
   const int64_t f = bounds.at(wg);
   if (f >= total) return;
   WeighItem it;
-  weigh_find<kWeighKeys<T>>(a, f, it);
+  weigh_find<KEYS>(a, f, it);
   const int64_t begin = f - it.x, end = begin + it.s.tiles;
   if (it.x == 0 || bounds.at(wg - 1) > begin) return;              // not cut here, or not for the first time
-  const float* p = a.part_o + ((int64_t)r * a.wgs + wg - 1) * 2 * kWeighKeys<T> + threadIdx.x;
-  float w = p[kWeighKeys<T>];
-  for (int k = wg; k < bounds.runs && bounds.at(k) < end; k++) w += *(p += 2 * kWeighKeys<T>);
-  const int key = it.block * kWeighKeys<T> + threadIdx.x;
+  int pieces = 1;                                                  // records of the item
+  for (int k0 = wg; k0 < bounds.runs; k0 += 64) {
+    const int more = __popcll(__ballot(k0 + lane < bounds.runs && bounds.at(k0 + lane) < end));
+    pieces += more;
+    if (more < 64) break;
+  }
+  const float* p = a.part_o + ((int64_t)r * a.wgs + wg) * 2 * KEYS + threadIdx.x;   // of run wg; the run's before it ends in the item
+  auto at = [&](int i) { return i == 0 ? p - KEYS : p + (int64_t)(i - 1) * 2 * KEYS; };
+  float w = 0.f;
+  for (int i0 = 0; i0 < pieces; i0 += AHEAD) {
+    float x[AHEAD];
+#pragma unroll
+    for (int k = 0; k < AHEAD; k++) x[k] = *at(min(i0 + k, pieces - 1));
+#pragma unroll
+    for (int k = 0; k < AHEAD; k++) w += i0 + k < pieces ? x[k] : 0.f;
+  }
+  const int key = it.block * KEYS + threadIdx.x;
   if (key >= it.n) return;
   const uint32_t page = (uint32_t)a.table[(int64_t)it.b * a.max_pages + (key >> a.page_log)];
   if (page < (uint32_t)a.n_pages) unsafeAtomicAdd(a.weights + ((((int64_t)page * a.h_kv + r) << a.page_log) + (key & ((1 << a.page_log) - 1))), w);
