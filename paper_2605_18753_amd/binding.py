@@ -320,12 +320,18 @@ class PagedCache:
     weights: Optional[torch.Tensor] = None
     pos: Optional[torch.Tensor] = None
     seen: Optional[torch.Tensor] = None
-    layout: Optional[tuple] = field(default=None, init=False, repr=False, compare=False)   # None: not checked
+    layout: Optional[tuple] = field(default=None, init=False, repr=False, compare=False)   # of k, v and table; None: not checked
+    fresh: tuple = field(default=(), init=False, repr=False, compare=False)                # others that are not checked
 
     def __setattr__(self, name, value):
         own = self.__dict__
-        if own.get(name, own) is not value:
-            own[name], own["layout"] = value, None
+        if own.get(name, own) is value:
+            return
+        own[name] = value
+        if name in ("k", "v", "table"):
+            own["layout"] = None
+        else:
+            own["fresh"] = self.fresh + (name,)
 
     @staticmethod
     def allocate(batch: int, h_kv: int, n_pages: int, page_size: int, head_dim: int, max_pages: int, device,
@@ -342,21 +348,30 @@ class PagedCache:
 
 def _paged_layout(c: PagedCache) -> tuple:
     """Device, type, sizes and strides of a cache whose tensors fit each other."""
-    if c.layout is not None:
-        return c.layout
-    k, v, t, n = c.k, c.v, c.table, c.lens
-    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in (torch.bfloat16, torch.float32):
-        raise DashError("k and v pages: two tensors [n_pages, h_kv, page_size, d] of one type, bf16 or fp32")
-    if k.stride(3) != 1 or v.stride(3) != 1:
-        raise DashError("k and v pages: head_dim must be contiguous")
-    if t.dim() != 2 or n.shape != t.shape[:1] or t.dtype != torch.int32 or n.dtype != torch.int32 or not (t.is_contiguous() and n.is_contiguous()):
-        raise DashError("table [batch, max_pages] and lens [batch]: contiguous int32 tensors")
-    for x, dtype, shape in ((c.weights, torch.float32, k.shape[:3]), (c.pos, torch.int32, k.shape[:3]), (c.seen, torch.int32, n.shape)):
-        if x is not None and (x.dtype != dtype or x.shape != shape or not x.is_contiguous()):
-            raise DashError("weights (fp32) and pos (int32) [n_pages, h_kv, page_size], seen int32 [batch]: contiguous")
-    if any(x is not None and x.device != k.device for x in (v, t, n, c.weights, c.pos, c.seen)):
-        raise DashError("the cache's tensors lie on one device")
-    c.__dict__["layout"] = layout = (k.get_device(), k.dtype, k.shape, k.stride(), v.stride(), t.shape)
+    layout = c.layout
+    if layout is None:
+        k, v, t = c.k, c.v, c.table
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in (torch.bfloat16, torch.float32):
+            raise DashError("k and v pages: two tensors [n_pages, h_kv, page_size, d] of one type, bf16 or fp32")
+        if k.stride(3) != 1 or v.stride(3) != 1:
+            raise DashError("k and v pages: head_dim must be contiguous")
+        if t.dim() != 2 or t.dtype != torch.int32 or not t.is_contiguous():
+            raise DashError("table [batch, max_pages]: a contiguous int32 tensor")
+        if v.device != k.device or t.device != k.device:
+            raise DashError("the cache's tensors lie on one device")
+        layout = (k.get_device(), k.dtype, k.shape, k.stride(), v.stride(), t.shape)
+        c.__dict__["fresh"] = ("lens", "weights", "pos", "seen")
+    if c.fresh:
+        for name in c.fresh:
+            x = getattr(c, name)
+            if x is None and name != "lens":
+                continue
+            if x.dtype is not (torch.float32 if name == "weights" else torch.int32) or not x.is_contiguous() or \
+                    x.shape != (layout[2][:3] if name in ("weights", "pos") else layout[5][:1]):
+                raise DashError("lens and seen int32 [batch], weights (fp32) and pos (int32) [n_pages, h_kv, page_size]: contiguous tensors")
+            if x.get_device() != layout[0]:
+                raise DashError("the cache's tensors lie on one device")
+        c.__dict__["layout"], c.__dict__["fresh"] = layout, ()
     return layout
 
 

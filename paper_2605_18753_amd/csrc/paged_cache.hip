@@ -88,7 +88,7 @@ struct EvictArgs {
   // long caches only
   int chunks;          // chunks of a pair at most
   uint32_t* keys;      // [pair][cap]
-  int32_t* cand;       // [pair][cap]: slots of the keys that share their leading bits with the one looked for
+  int2* cand;          // [pair][cap]: the keys that share their leading bits with the one looked for, and their slots
   int32_t* hists;      // [pair][chunk][kBins]
   int32_t* above;      // [pair][chunk]: keys with larger leading bits
   int32_t* heads;      // [pair][4]: the leading bits looked for, how many keys that share them stay, and all; slots picked out so far
@@ -106,6 +106,7 @@ constexpr int kBins = 2048;                                // 11 bits of a key
 constexpr int kSelThreads = 1024, kSelKeys = 8192;
 constexpr int kCands = 2048, kRanked = 256;                // keys that are picked out; that are ranked against each other
 constexpr int kChunk = 4096, kChunkThreads = 256;          // longer ones: slots and threads of a workgroup
+constexpr int kLongCands = 4096;                           // of those picked out, in LDS
 
 // For two counts of a thread: their sums over the threads before it (x, y) and over all (z, w).
 template <int THREADS> __device__ __forceinline__ int4 threads_before(int u, int v, int2* xch) {
@@ -417,16 +418,16 @@ __global__ __launch_bounds__(kChunkThreads) void paged_long_pick_kernel(EvictArg
     place = s.z ? atomicAdd(&e.heads[4 * pair + 3], s.z) : 0;
   }
   __syncthreads();
-  int32_t* to = e.cand + (int64_t)pair * a.cap + place + s.x;
+  int2* to = e.cand + (int64_t)pair * a.cap + place + s.x;
 #pragma unroll
   for (int j = 0; j < kChunk / kChunkThreads; j++)
-    if (j * kChunkThreads + tid < k.len && (int)(key[j] >> 21) == bin) *to++ = k.begin + j * kChunkThreads + tid;
+    if (j * kChunkThreads + tid < k.len && (int)(key[j] >> 21) == bin) *to++ = make_int2((int)key[j], k.begin + j * kChunkThreads + tid);
 }
 
 __global__ __launch_bounds__(kChunkThreads) void paged_long_list_kernel(EvictArgs e) {
   const PagedArgs& a = e.a;
   __shared__ uint32_t keys[kChunk];
-  __shared__ int2 cand[kCands];                              // key, slot
+  __shared__ int2 cand[kLongCands];
   __shared__ int hist[kBins];
   __shared__ int2 xch[kChunkThreads / 64];
   __shared__ int chosen[3];
@@ -434,7 +435,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_long_list_kernel(EvictArg
   if (k.len == 0) return;
   const int pair = blockIdx.x / e.chunks, tid = threadIdx.x, front = (e.budget + kChunk - 1) / kChunk;
   const uint32_t* far = e.keys + (int64_t)pair * a.cap;
-  const int32_t* slots = e.cand + (int64_t)pair * a.cap;
+  const int2* far_cand = e.cand + (int64_t)pair * a.cap;
   uint32_t last = (uint32_t)e.heads[4 * pair] << 21;         // the smallest key that stays, from its leading bits on
   int want = e.heads[4 * pair + 1], ties = e.heads[4 * pair + 2];   // of the keys that share them, those that stay, and all
   const int n_cand = ties;
@@ -443,21 +444,15 @@ __global__ __launch_bounds__(kChunkThreads) void paged_long_list_kernel(EvictArg
     const int i = j * kChunkThreads + tid;
     if (i < k.len) keys[i] = far[k.begin + i];
   }
-#pragma unroll 4
-  for (int i = tid; i < min(n_cand, kCands); i += kChunkThreads) {
-    const int at = slots[i];
-    cand[i] = make_int2((int)far[at], at);
-  }
-  // f(key, slot) of those picked out, a thread's share; the first 2048 from LDS
+#pragma unroll 8
+  for (int i = tid; i < min(n_cand, kLongCands); i += kChunkThreads) cand[i] = far_cand[i];
+  // f(key, slot) of those picked out, a thread's share; the first 4096 from LDS
   auto picked = [&](auto&& f) {
-    for (int i = tid; i < min(n_cand, kCands); i += kChunkThreads) {
-      const int2 x = cand[i];
+    for (int i = tid; i < min(n_cand, kLongCands); i += kChunkThreads) f((uint32_t)cand[i].x, cand[i].y);
+#pragma unroll 8
+    for (int i = kLongCands + tid; i < n_cand; i += kChunkThreads) {
+      const int2 x = far_cand[i];
       f((uint32_t)x.x, x.y);
-    }
-#pragma unroll 4
-    for (int i = kCands + tid; i < n_cand; i += kChunkThreads) {
-      const int at = slots[i];
-      f(far[at], at);
     }
   };
 #pragma unroll 1
@@ -559,7 +554,7 @@ static size_t evict_scratch(EvictArgs& e, const PagedArgs& a, char* ws) {
   if (a.cap > kSelKeys) {
     e.chunks = (a.cap + kChunk - 1) / kChunk + 1;
     e.keys = (uint32_t*)take(pairs * a.cap);
-    e.cand = take(pairs * a.cap);
+    e.cand = (int2*)take(2 * pairs * a.cap);
     e.hists = take(pairs * e.chunks * kBins);
     e.above = take(pairs * e.chunks);
     e.heads = take(pairs * 4);

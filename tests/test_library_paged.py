@@ -90,10 +90,10 @@ def test_workspaces():
     for name, need in (("attend", n), ("weigh", B.paged_workspace_bytes(params())), ("evict", e)):
         assert call(name, params(), ws=None) == -3 and call(name, params(), ws=4097) == -3
     assert call("attend", params(), n=0) == -3 and call("evict", params(), n=e - 1) == -3 and call("weigh", params(), n=0) == -3
-    # the eviction's lists: a number a slot; of long caches also the keys and those picked out, and counts of every 4096
+    # the eviction's lists: a number a slot; of long caches also the keys, those picked out with their slots, and counts of every 4096
     assert 4 * 2 * 20 * 64 * 4 <= e <= 4 * 2 * 20 * 64 * 4 + 4096
     big = B.paged_workspace_bytes(params(max_pages=513), evict=True)
-    assert 4 * 2 * 513 * 64 * 12 + 4 * 2 * 10 * 2048 * 4 <= big <= 4 * 2 * 513 * 64 * 12 + 4 * 2 * 10 * 2049 * 4 + 4096
+    assert 4 * 2 * 513 * 64 * 16 + 4 * 2 * 10 * 2048 * 4 <= big <= 4 * 2 * 513 * 64 * 16 + 4 * 2 * 10 * 2049 * 4 + 4096
     # one workspace serves every number of rows
     assert all(B.paged_workspace_bytes(params(n_rows=r)) == n for r in (1, 64, 5000, 1 << 20))
 
