@@ -31,6 +31,7 @@ struct PagedArgs {
   int64_t q_t, q_h, o_t, o_h, kn_t, kn_h, vn_t, vn_h, kp_p, kp_h, kp_t, vp_p, vp_h, vp_t;
   float c1;                              // scale * log2(e)
   int wgs;                               // runs of a kv-head; 0: an item a workgroup.  Tiles of 128 rows: parts of a kv-head at most; 0: none is cut
+  int whole;                             // runs: items may be left uncut
   int slots; float gain;                 // tiles of 128 rows: workgroups of a kv-head that are resident at once; what finer parts must come to
   float* part_o; float* part_ml;         // records of cut items: two of each run (the item it begins in, the one it ends in), one of each part
   uint64_t* flags; uint64_t nonce;       // runs: two of each record, and the number that says that it is complete
@@ -134,6 +135,10 @@ template <typename F> __device__ __forceinline__ bool paged_find_part(const Page
 // ceil((u + t + 1) / k) steps, u = ceil(old / T), k = 128 / T, and the tiles before it H(u + t) - H(u), H(x) = sum of ceil(y / k) over
 // y = 1 .. x.  Runs are used for fewer than 4096 items, of at most 2^17 steps each: 32 bits (H may wrap, its differences do not).
 constexpr int kStep = 128;
+// Adding up the pieces of an item takes as long as so many steps: items that are no longer than the runs would be by more than that are not cut, if there
+// is a workgroup for each.  (One token of sequences of 200 to 1000, 32 / 8 heads, 16 of them: 13.6 us, cut 19.1; 32: 17.7 and 23.3; one of
+// 1000: 12.2 and 9.0.)
+constexpr int kJoin = 6;
 struct PagedSeq { int tiles, u, flat; };                   // flat > 0: steps of every tile (no causal mask)
 struct PagedItem { int b, tile, r0, m, n; PagedSeq s; };
 struct PagedDeal {
@@ -148,13 +153,17 @@ struct PagedDeal {
   }
   __device__ __forceinline__ int before(const PagedSeq& s, int t) const { return s.flat ? s.flat * t : (int)(h(s.u + t) - h(s.u)); }
   __device__ __forceinline__ int steps(const PagedSeq& s, int t) const { return s.flat ? s.flat : ((s.u + t) >> k_log) + 1; }
-  // the steps of all items of a kv-head; a wave's lanes together; l0: the first 64 sequences
-  __device__ __forceinline__ int total(const PagedArgs& a, const PagedLane& l0) const {
+  // the steps of all items of a kv-head, and if they may be left uncut how many there are, and the steps of the longest; a wave's lanes together; l0: the first 64 sequences
+  __device__ __forceinline__ int total(const PagedArgs& a, const PagedLane& l0, int& items, int& most) const {
     int f = 0;
+    items = most = 0;
     for (int i0 = 0; i0 < a.batch; i0 += 64) {
       const PagedLane l = i0 ? paged_lane(a, i0 + lane_id()) : l0;
       const PagedSeq s = seq(a, l.rm.y, l.n);
       f += __builtin_amdgcn_readlane(wave_scan(before(s, s.tiles)), 63);
+      if (!a.whole) continue;
+      items += __builtin_amdgcn_readlane(wave_scan(s.tiles), 63);
+      most = max(most, (int)wave_max(s.tiles > 0 ? (float)steps(s, s.tiles - 1) : 0.f));
     }
     return f;
   }
@@ -232,13 +241,18 @@ struct PagedRun {
   __device__ __forceinline__ PagedRun(const PagedArgs& a) : deal(a) {}
   __device__ __forceinline__ bool begin(const PagedArgs& a, int wg) {
     const PagedLane l0 = paged_lane(a, lane_id());
-    if (a.wgs == 0) {
+    bool cut = a.wgs > 0;
+    if (cut) {
+      int items, most;
+      total = deal.total(a, l0, items, most);
+      cut = !a.whole || items > a.wgs || (most - kJoin) * a.wgs > total;
+    }
+    if (!cut) {
       if (deal.find(a, l0, wg, false, it) < 0) return false;
       x0 = next = end = 0;
       x1 = cost = deal.steps(it.s, it.tile);
       return true;
     }
-    total = deal.total(a, l0);
     const PagedBounds<int> b(a, total);
     next = __builtin_amdgcn_readfirstlane(b.at(wg));
     end = __builtin_amdgcn_readfirstlane(b.at(wg + 1));

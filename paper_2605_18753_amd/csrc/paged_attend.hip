@@ -883,8 +883,8 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
   if (big && a.wgs && items * 4 >= runs) a.wgs = (int)items + runs * 3 / 2;
   a.slots = runs;
   a.gain = (int64_t)a.n_rows * a.g < 64 * items ? 0.65f : 0.9f;
-  // Items of up to eight steps are not cut if there is one for every other CU.  (16 sequences of 200 to 1000 tokens, 32 / 8 heads: 13 us, in runs 19; fewer
-  // items: one of 1000 tokens 11.7, in runs 9.3.)
+  a.whole = items * 2 >= runs;                               // fewer items: not looked into
+  // Items of up to eight steps are not cut if there is one for every other CU.  (333 tokens of 1024 in fp32, 32 / 8 heads of 128: 86 us, in runs 90.)
   if (!big && a.cap <= 8 * kStep && items * a.h_kv >= 128) a.wgs = 0;
   const size_t recs = (size_t)a.wgs * a.h_kv * (big ? 128 : 2 * 16);
   a.part_ml = (float*)ws;

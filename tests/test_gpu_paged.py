@@ -124,6 +124,14 @@ def test_chunks_in_wide_tables(causal, d, page, h_kv, g, news):
     s.check_attend(causal)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("h_kv,g,d,longest,causal", [(8, 4, 64, 900, True), (8, 2, 128, 1500, False), (16, 1, 64, 3000, True)])
+def test_single_tokens_in_wide_tables(dtype, h_kv, g, d, longest, causal):
+    lens = [longest if i == 11 else (61 * i) % 900 for i in range(32)]
+    s = Setup(lens, [min(1 + i % 2, 2) for i in range(32)], h_kv=h_kv, g=g, d=d, page=64, dtype=dtype, behind=math.nan, seed=40, width=128)
+    s.check_attend(causal)
+
+
 @pytest.mark.parametrize("h_kv,g,d,batch,new", [(8, 1, 64, 30, 130), (16, 4, 128, 14, 30), (8, 2, 64, 70, 20), (32, 1, 64, 6, 140)])
 def test_items_of_unequal_lengths_are_cut_finely(h_kv, g, d, batch, new):
     lens = [max(new, 2600 if i % 7 == 3 else (97 * i) % 200) for i in range(batch)]
