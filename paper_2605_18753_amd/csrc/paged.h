@@ -72,30 +72,40 @@ constexpr int kMinPart = 4;                                // steps a part has a
 // The size S of a part, no item costing more: none is cut; a wave's lanes together.  shape(m, n) gives a sequence's tiles and the cost
 // of one (at least 1); l0: the first 64 sequences.
 constexpr int kUncut = 0x3fffffff;
-template <typename F> __device__ __forceinline__ int paged_part_size(const PagedArgs& a, const PagedLane& l0, F&& shape) {
-  if (a.wgs <= 0) return kUncut;
-  const int lane = lane_id();
+struct PagedCut { int size, whole; };                      // of the items behind the first `whole`
+// of sequence tiles, those among the first `whole` items; before: items before the sequence's
+__device__ __forceinline__ int paged_whole(const PagedCut& cut, int before, int tiles) { return min(max(cut.whole - before, 0), tiles); }
+template <typename F> __device__ __forceinline__ PagedCut paged_part_size(const PagedArgs& a, const PagedLane& l0, F&& shape) {
+  if (a.wgs <= 0) return {kUncut, 0};
+  const int lane = lane_id(), half = a.slots / 2;
   int items = 0;
-  float cost = 0.f, most = 0.f;
+  float cost = 0.f, most = 0.f, rest = 0.f;                // rest: of the items behind the first `half`
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
     const PagedLane l = i0 ? paged_lane(a, i0 + lane) : l0;
     const int2 s = shape(l.rm.y, l.n);
-    items += __builtin_amdgcn_readlane(wave_scan(s.x), 63);
+    const int incl = items + wave_scan(s.x);
+    rest += wave_sum((float)(s.x - min(max(half - (incl - s.x), 0), s.x)) * (float)s.y);
+    items = __builtin_amdgcn_readlane(incl, 63);
     cost += wave_sum((float)s.x * (float)s.y);
     most = fmaxf(most, wave_max(s.x > 0 ? (float)s.y : 0.f));
   }
-  if (items >= a.wgs) return kUncut;
-  const auto size = [&](int w) { return max((int)fminf(cost * 1.0001f / (float)(w - items), 1e9f) + 1, kMinPart); };   // the factor covers the sum's rounding
+  if (items >= a.wgs) return {kUncut, 0};
+  const auto size = [&](float c, int w) { return max((int)fminf(c * 1.0001f / (float)(w - items), 1e9f) + 1, kMinPart); };   // the factor covers the sum's rounding
   // The time, in steps, of parts that are all resident (or of items, where more are not), and of finer ones that follow each other: what everybody
   // has on the average, half a part until the last is done, and 4 steps for what a part costs besides
   const float even = cost / (float)a.slots;
-  int S = items < a.slots ? size(a.slots) : kUncut;
-  const float time = items <= a.slots ? fminf((float)S, most) : even + 0.5f * most;
+  PagedCut cut = {items < a.slots ? size(cost, a.slots) : kUncut, 0};
+  float time = items <= a.slots ? fminf((float)cut.size, most) : fminf((float)((items + a.slots - 1) / a.slots) * most, even + 0.5f * most);
   if (a.wgs > a.slots) {
-    const int fine = size(a.wgs);
-    if (even + 0.5f * (float)fine + 4.f < a.gain * time) S = fine;
+    const int fine = size(cost, a.wgs);
+    if (even + 0.5f * (float)fine + 4.f < a.gain * time) cut = {fine, 0};
+    else if (items > half && most < 1.4f * even) {         // one item a CU stays whole, the others fill up what these leave
+      const int fill = max(size(rest, a.wgs), (int)(0.5f * even));
+      if (even + 0.25f * (float)fill + 4.f < (a.gain + 0.05f) * time) cut = {fill, half};
+    }
   }
-  return (float)S >= most ? kUncut : S;
+  if ((float)cut.size >= most) cut = {kUncut, 0};
+  return cut;
 }
 
 struct PagedPart { int b, tile, part, parts, rec0, r0, m, n; };   // rec0: the item's first part among those of the kv-head
@@ -103,28 +113,31 @@ struct PagedPart { int b, tile, part, parts, rec0, r0, m, n; };   // rec0: the i
 template <typename F> __device__ __forceinline__ bool paged_find_part(const PagedArgs& a, int idx, F&& shape, PagedPart& it) {
   const int lane = lane_id();
   const PagedLane l0 = paged_lane(a, lane);
-  const int S = paged_part_size(a, l0, shape);
-  int base = 0;
+  const PagedCut cut = paged_part_size(a, l0, shape);
+  const bool whole = idx < cut.whole;
+  int items = 0, base = whole ? 0 : cut.whole;
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
     const PagedLane p = i0 ? paged_lane(a, i0 + lane) : l0;
     const int2 s = shape(p.rm.y, p.n);
-    const int parts = (s.y + S - 1) / S;
-    const int incl = wave_scan(s.x * parts);
+    const int upto = items + wave_scan(s.x), uncut = paged_whole(cut, upto - s.x, s.x);
+    const int parts = whole ? 1 : (s.y + cut.size - 1) / cut.size, skip = whole ? 0 : uncut, count = (s.x - skip) * parts;
+    const int incl = wave_scan(count);
     const uint64_t hit = __ballot(base + incl > idx);
     if (hit) {
       const int l = __builtin_ctzll(hit);
       it.b = i0 + l;
       it.parts = __builtin_amdgcn_readlane(parts, l);
-      const int first = base + __builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(s.x, l) * it.parts;
+      const int in = idx - (base + __builtin_amdgcn_readlane(incl, l) - __builtin_amdgcn_readlane(count, l));
       // the last tiles first: of a causal prompt they are the longest
-      it.tile = __builtin_amdgcn_readlane(s.x, l) - 1 - (idx - first) / it.parts;
-      it.part = (idx - first) % it.parts;
+      it.tile = __builtin_amdgcn_readlane(s.x, l) - 1 - __builtin_amdgcn_readlane(skip, l) - in / it.parts;
+      it.part = in % it.parts;
       it.rec0 = idx - it.part;
       it.r0 = __builtin_amdgcn_readlane(p.rm.x, l);
       it.m = __builtin_amdgcn_readlane(p.rm.y, l);
       it.n = __builtin_amdgcn_readlane(p.n, l);
       return true;
     }
+    items = __builtin_amdgcn_readlane(upto, 63);
     base += __builtin_amdgcn_readlane(incl, 63);
   }
   return false;

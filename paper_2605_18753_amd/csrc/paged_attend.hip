@@ -786,36 +786,38 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
   const int lane = threadIdx.x & 63, c = threadIdx.x % TPR, unit = threadIdx.x / TPR, slice = unit / PER;
   const auto shape = [&](int m, int n) { return rows_shape(a, m, n); };
   const PagedLane l0 = paged_lane(a, lane);
-  const int S = paged_part_size(a, l0, shape);
-  if (S == kUncut) return;
+  const PagedCut cut = paged_part_size(a, l0, shape);
+  if (cut.size == kUncut) return;
   // rows in the order kv-head, token, head of the group: neighbours lie side by side in the records
   const int64_t per = (int64_t)a.n_rows * a.g, all = per * a.h_kv;
   for (int64_t g0 = (int64_t)blockIdx.x * PER; g0 < all; g0 += (int64_t)gridDim.x * PER) {
     const int64_t gr = min(g0 + unit % PER, all - 1);
     const int r = (int)(gr / per), row = (int)(gr % per) / a.g, hg = (int)(gr % per) % a.g;
     // the dealing of the launch before, for a given row
-    int first = 0, parts = 0, tiles = 0, r0 = 0, base = 0;
+    int first = 0, parts = 0, tiles = 0, r0 = 0, items = 0, base = cut.whole;   // tiles: those that are cut
     for (int i0 = 0; i0 < a.batch; i0 += 64) {
       const PagedLane p = i0 ? paged_lane(a, i0 + lane) : l0;
       const int2 rm = p.rm, s = shape(rm.y, p.n);
-      const int np = (s.y + S - 1) / S, incl = wave_scan(s.x * np);
+      const int upto = items + wave_scan(s.x), nt = s.x - paged_whole(cut, upto - s.x, s.x);
+      const int np = (s.y + cut.size - 1) / cut.size, incl = wave_scan(nt * np);
 #pragma unroll
       for (int k = 0; k < 64 / TPR; k++) {
         const int want = __builtin_amdgcn_readlane(row, k * TPR);
         const uint64_t hit = __ballot(want >= rm.x && want < rm.x + rm.y);
         if (hit) {
           const int l = __builtin_ctzll(hit);
-          const int np_l = __builtin_amdgcn_readlane(np, l), tiles_l = __builtin_amdgcn_readlane(s.x, l);
+          const int np_l = __builtin_amdgcn_readlane(np, l), tiles_l = __builtin_amdgcn_readlane(nt, l);
           const int first_l = base + __builtin_amdgcn_readlane(incl, l) - tiles_l * np_l, r0_l = __builtin_amdgcn_readlane(rm.x, l);
           if (lane / TPR == k) { parts = np_l; tiles = tiles_l; first = first_l; r0 = r0_l; }
         }
       }
+      items = __builtin_amdgcn_readlane(upto, 63);
       base += __builtin_amdgcn_readlane(incl, 63);
     }
-    const bool mine = parts > 1 && g0 + unit % PER < all;
+    const int Tt = 128 / a.g, t = row - r0, tile = t / Tt, in = (t % Tt) * a.g + hg;
+    const bool mine = parts > 1 && tile < tiles && g0 + unit % PER < all;
     PagedSum sum;
     if (mine) {
-      const int Tt = 128 / a.g, t = row - r0, tile = t / Tt, in = (t % Tt) * a.g + hg;
       const int64_t rec = (int64_t)r * a.wgs + first + (tiles - 1 - tile) * parts;
       const float2* ml = reinterpret_cast<const float2*>(a.part_ml) + rec * 128 + in;
       const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o) + (rec * 128 + in) * (D / 4) + c;
