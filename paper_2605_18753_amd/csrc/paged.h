@@ -8,10 +8,11 @@
 //   [w F / G, (w + 1) F / G) of them: whatever the lengths, every CU streams as many keys.
 //   Tiles of 128 rows: one item a workgroup; items that leave the chip idle are cut into parts.  With n items of costs c_i and W > n
 //   workgroups, parts of S = ceil(sum c_i / (W - n)) give sum ceil(c_i / S) <= W of them.  W is what is resident at once, or n and one and a
-//   half times that where the items' lengths would leave much of the chip idle.  (40 tokens of 40 sequences of 300 to 8000, 32 / 2 heads: 196 us with
-//   the first, 157 with the second; 700 of one of 30000 384 and 360; where the first is kept, 1501 tokens beside decoding ones, 305 and 326.)  (Equal runs for these as well: a run begins anew for every
-//   piece of an item, and most are cut.  1501 tokens beside seven decoding sequences of up to 12k 305 -> 309 us and the records to add
-//   up, 2048 tokens against 32k 995 -> 1088.)
+//   half times that where the items' lengths would leave much of the chip idle; or one item a CU stays whole and the others are cut to fill up what
+//   these leave (paged_part_size).  (Finer parts: 40 tokens of 40 sequences of 300 to 8000, 32 / 2 heads, 196 -> 157 us; 700 of one of 30000
+//   384 -> 360; 1501 tokens beside decoding ones, where they are not taken, 305 and 326.)
+//   (Equal runs for these as well: a run begins anew for every piece of an item, and most are cut.  1501 tokens beside seven decoding
+//   sequences of up to 12k 305 -> 309 us and the records to add up, 2048 tokens against 32k 995 -> 1088.)
 // Cut items leave records.  Of parts a second launch adds them up; of runs the workgroup whose record of an item is complete last, which
 // sees the flags of all (stored past the caches, as in decode_body.h; who merges clears them, so a captured launch can be replayed), or where
 // there are many in two levels.
@@ -92,16 +93,18 @@ template <typename F> __device__ __forceinline__ PagedCut paged_part_size(const 
   if (items >= a.wgs) return {kUncut, 0};
   const auto size = [&](float c, int w) { return max((int)fminf(c * 1.0001f / (float)(w - items), 1e9f) + 1, kMinPart); };   // the factor covers the sum's rounding
   // The time, in steps, of parts that are all resident (or of items, where more are not), and of finer ones that follow each other: what everybody
-  // has on the average, half a part until the last is done, and 4 steps for what a part costs besides
+  // has on the average, half a part until the last is done (a quarter beside whole items, which run faster alone), and what a part costs besides: 4
+  // steps, or 10 where it is one more than a workgroup would have.  (One item a CU whole, the others filling up: 2200 tokens against 32k, 32 / 8
+  // heads, 69 items for 64 places, 1418 -> 1197 us; 1500, 47 items, 865 -> 785; against 2000, where it is not done, 54 and 64.)
   const float even = cost / (float)a.slots;
   PagedCut cut = {items < a.slots ? size(cost, a.slots) : kUncut, 0};
   float time = items <= a.slots ? fminf((float)cut.size, most) : fminf((float)((items + a.slots - 1) / a.slots) * most, even + 0.5f * most);
   if (a.wgs > a.slots) {
     const int fine = size(cost, a.wgs);
     if (even + 0.5f * (float)fine + 4.f < a.gain * time) cut = {fine, 0};
-    else if (items > half && most < 1.4f * even) {         // one item a CU stays whole, the others fill up what these leave
+    else if (items > half && most * (float)items < 1.2f * cost) {   // of like lengths: one item a CU stays whole, the others fill up what these leave
       const int fill = max(size(rest, a.wgs), (int)(0.5f * even));
-      if (even + 0.25f * (float)fill + 4.f < (a.gain + 0.05f) * time) cut = {fill, half};
+      if (even + 0.25f * (float)fill + 10.f < (a.gain + 0.05f) * time) cut = {fill, half};
     }
   }
   if ((float)cut.size >= most) cut = {kUncut, 0};

@@ -124,6 +124,11 @@ def test_chunks_in_wide_tables(causal, d, page, h_kv, g, news):
     s.check_attend(causal)
 
 
+@pytest.mark.parametrize("lens,news", [([6400], [380]), ([6300], [600]), ([6400, 70, 6000], [250, 1, 129])])
+def test_items_that_stay_whole_beside_cut_ones(lens, news):
+    Setup(lens, news, h_kv=128, g=1, d=64, page=128, seed=41).check_attend()
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("h_kv,g,d,longest,causal", [(8, 4, 64, 900, True), (8, 2, 128, 1500, False), (16, 1, 64, 3000, True)])
 def test_single_tokens_in_wide_tables(dtype, h_kv, g, d, longest, causal):
