@@ -789,10 +789,10 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
   const PagedCut cut = paged_part_size(a, l0, shape);
   if (cut.size == kUncut) return;
   // rows in the order kv-head, token, head of the group: neighbours lie side by side in the records
-  const int64_t per = (int64_t)a.n_rows * a.g, all = per * a.h_kv;
-  for (int64_t g0 = (int64_t)blockIdx.x * PER; g0 < all; g0 += (int64_t)gridDim.x * PER) {
-    const int64_t gr = min(g0 + unit % PER, all - 1);
-    const int r = (int)(gr / per), row = (int)(gr % per) / a.g, hg = (int)(gr % per) % a.g;
+  const uint32_t per = (uint32_t)a.n_rows * (uint32_t)a.g, all = per * (uint32_t)a.h_kv, g_log = 31 - __builtin_clz(a.g);   // 2^28 at most
+  for (uint32_t g0 = blockIdx.x * PER; g0 < all; g0 += gridDim.x * PER) {
+    const uint32_t gr = min(g0 + unit % PER, all - 1), kv = gr / per;
+    const int r = (int)kv, row = (int)((gr - kv * per) >> g_log), hg = (int)(gr - kv * per) & (a.g - 1);
     // the dealing of the launch before, for a given row
     int first = 0, parts = 0, tiles = 0, r0 = 0, items = 0, base = cut.whole;   // tiles: those that are cut
     for (int i0 = 0; i0 < a.batch; i0 += 64) {
@@ -814,7 +814,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
       items = __builtin_amdgcn_readlane(upto, 63);
       base += __builtin_amdgcn_readlane(incl, 63);
     }
-    const int Tt = 128 / a.g, t = row - r0, tile = t / Tt, in = (t % Tt) * a.g + hg;
+    const int t = row - r0, tile = t >> (7 - g_log), in = ((t << g_log) & 127) + hg;   // 128 / g tokens a tile
     const bool mine = parts > 1 && tile < tiles && g0 + unit % PER < all;
     PagedSum sum;
     if (mine) {
