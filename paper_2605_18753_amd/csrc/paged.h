@@ -76,7 +76,9 @@ constexpr int kUncut = 0x3fffffff;
 struct PagedCut { int size, whole; };                      // of the items behind the first `whole`
 // of sequence tiles, those among the first `whole` items; before: items before the sequence's
 __device__ __forceinline__ int paged_whole(const PagedCut& cut, int before, int tiles) { return min(max(cut.whole - before, 0), tiles); }
+// The launch that adds the parts up has to come to the same: no products are fused with sums here.
 template <typename F> __device__ __forceinline__ PagedCut paged_part_size(const PagedArgs& a, const PagedLane& l0, F&& shape) {
+#pragma clang fp contract(off)
   if (a.wgs <= 0) return {kUncut, 0};
   const int lane = lane_id(), half = a.slots / 2;
   int items = 0;
