@@ -32,7 +32,7 @@ struct PagedArgs {
   int64_t q_t, q_h, o_t, o_h, kn_t, kn_h, vn_t, vn_h, kp_p, kp_h, kp_t, vp_p, vp_h, vp_t;
   float c1;                              // scale * log2(e)
   int wgs;                               // runs of a kv-head; 0: an item a workgroup.  Tiles of 128 rows: parts of a kv-head at most; 0: none is cut
-  int whole;                             // runs: items may be left uncut
+  int whole;                             // runs: items may be left uncut; weights: two kernels share the sequences
   int slots; float gain;                 // tiles of 128 rows: workgroups of a kv-head that are resident at once; what finer parts must come to
   float* part_o; float* part_ml;         // records of cut items: two of each run (the item it begins in, the one it ends in), one of each part
   uint64_t* flags; uint64_t nonce;       // runs: two of each record, and the number that says that it is complete

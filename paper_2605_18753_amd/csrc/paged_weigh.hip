@@ -59,9 +59,13 @@ template <typename T> constexpr int kWeighKeys = sizeof(T) == 2 ? 256 : 128;   /
 // The work of a kv-head: items (blocks of keys) times the row tiles of their sequence, one after the other, dealt in equal runs
 // [w F / G, (w + 1) F / G) to G workgroups.
 struct WeighSeq { int items, tiles, x0; };                 // blocks of keys, row tiles each, the first of these
-template <int KEYS> __device__ __forceinline__ WeighSeq weigh_seq(const PagedArgs& a, int m, int n) {
-  const int Tt = 16 / a.g, x0 = (a.last > 0 ? max(m - a.last, 0) : 0) / Tt;
-  return {m > 0 ? (n + KEYS - 1) / KEYS : 0, (m + Tt - 1) / Tt - x0, x0};
+constexpr int kStreamTiles = 2;                            // row tiles of a sequence for which K is streamed
+// Where the kernel that streams K and the other one both run (a.whole), each has its own sequences.
+enum WeighOwn { kOwnLong, kOwnShort, kOwnAll };
+template <int KEYS> __device__ __forceinline__ WeighSeq weigh_seq(const PagedArgs& a, int m, int n, WeighOwn own) {
+  const int Tt = 16 / a.g, x0 = (a.last > 0 ? max(m - a.last, 0) : 0) / Tt, tiles = (m + Tt - 1) / Tt - x0;
+  const bool mine = own == kOwnAll || !a.whole || (tiles <= kStreamTiles) == (own == kOwnShort);
+  return {m > 0 && mine ? (n + KEYS - 1) / KEYS : 0, tiles, x0};
 }
 __device__ __forceinline__ int64_t scan64(int64_t v) {     // inclusive, over the lanes up to one's own
 #pragma unroll
@@ -75,13 +79,13 @@ __device__ __forceinline__ int64_t lane64(int64_t v, int l) {   // lane l's, as 
   return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)((uint64_t)v >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, l));
 }
 // whole: places are items, which are not cut
-template <int KEYS> __device__ __forceinline__ int64_t weigh_total(const PagedArgs& a, bool whole = false) {
+template <int KEYS> __device__ __forceinline__ int64_t weigh_total(const PagedArgs& a, bool whole = false, WeighOwn own = kOwnLong) {
   const int lane = lane_id();
   int64_t total = 0;
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
     int64_t v = 0;
     if (i0 + lane < a.batch) {
-      const WeighSeq s = weigh_seq<KEYS>(a, paged_rows(a, i0 + lane).y, paged_len(a, i0 + lane));
+      const WeighSeq s = weigh_seq<KEYS>(a, paged_rows(a, i0 + lane).y, paged_len(a, i0 + lane), own);
       v = whole ? s.items : (int64_t)s.items * s.tiles;
     }
     total += lane64(scan64(v), 63);
@@ -90,7 +94,7 @@ template <int KEYS> __device__ __forceinline__ int64_t weigh_total(const PagedAr
 }
 struct WeighItem { int b, block, x, r0, m, n; WeighSeq s; };   // x: row tiles of the item before the place
 // the item at place f < weigh_total
-template <int KEYS> __device__ __forceinline__ void weigh_find(const PagedArgs& a, int64_t f, WeighItem& it, bool whole = false) {
+template <int KEYS> __device__ __forceinline__ void weigh_find(const PagedArgs& a, int64_t f, WeighItem& it, bool whole = false, WeighOwn own = kOwnLong) {
   const int lane = lane_id();
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
     int2 rm = make_int2(0, 0);
@@ -99,7 +103,7 @@ template <int KEYS> __device__ __forceinline__ void weigh_find(const PagedArgs& 
     if (i0 + lane < a.batch) {
       rm = paged_rows(a, i0 + lane);
       n = paged_len(a, i0 + lane);
-      s = weigh_seq<KEYS>(a, rm.y, n);
+      s = weigh_seq<KEYS>(a, rm.y, n, own);
     }
     const int64_t v = whole ? s.items : (int64_t)s.items * s.tiles, incl = scan64(v);
     const uint64_t hit = __ballot(incl > f);
@@ -123,7 +127,8 @@ __global__ __launch_bounds__(256, (D == 128 ? 3 : 4) - (sizeof(T) == 4)) void pa
   constexpr int SUBS = WeighTile<T, D>::SUBS;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv;
-  const int64_t total = weigh_total<kWeighKeys<T>>(a);
+  const bool uncut = a.whole;                                // beside the streaming kernel: no launch adds pieces up
+  const int64_t total = weigh_total<kWeighKeys<T>>(a, uncut);
   const PagedBounds<int64_t> bounds(a, total);
   const int64_t f0 = bounds.at(wg), f1 = bounds.at(wg + 1);
   int64_t todo = f1 - f0;
@@ -147,7 +152,7 @@ __global__ __launch_bounds__(256, (D == 128 ? 3 : 4) - (sizeof(T) == 4)) void pa
   for (int s = 0; s < ROW / 64; s++) rd[s] = ring0 + n * ROW + (((4 * s + kq) ^ swizzle(n)) << 4);
   WeighItem it;
   int slot = 0;                                              // the stage to fill next
-  weigh_find<kWeighKeys<T>>(a, f0, it);
+  weigh_find<kWeighKeys<T>>(a, f0, it, uncut);
   while (true) {
     const int key0 = it.block * kWeighKeys<T> + wave * SUBS * 16;
     WeighTile<T, D> kf[SUBS];
@@ -162,7 +167,7 @@ __global__ __launch_bounds__(256, (D == 128 ? 3 : 4) - (sizeof(T) == 4)) void pa
       acc[s] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     // this run's row tiles of the item, those before the first that sees one of the block's, or the wave's, keys left out
-    const int take = (int)min((int64_t)(it.s.tiles - it.x), todo), back = it.n - it.m;
+    const int take = uncut ? it.s.tiles : (int)min((int64_t)(it.s.tiles - it.x), todo), back = it.n - it.m;
     const int first = a.last > 0 ? max(it.m - a.last, 0) : 0;
     int x = it.s.x0 + it.x;
     const int xe = x + take;
@@ -251,9 +256,9 @@ __global__ __launch_bounds__(256, (D == 128 ? 3 : 4) - (sizeof(T) == 4)) void pa
         else if (key < it.n && (uint32_t)page[j] < (uint32_t)a.n_pages) unsafeAtomicAdd(a.weights + ((((int64_t)page[j] * a.h_kv + r) << a.page_log) + (key & pm)), w);
       }
     }
-    if ((todo -= take) <= 0) return;
+    if ((todo -= uncut ? 1 : take) <= 0) return;
     it.x = 0;
-    if (++it.block >= it.s.items) weigh_find<kWeighKeys<T>>(a, f1 - todo, it);
+    if (++it.block >= it.s.items) weigh_find<kWeighKeys<T>>(a, f1 - todo, it, uncut);
   }
 }
 
@@ -296,28 +301,30 @@ __global__ __launch_bounds__(kWeighKeys<T>) void paged_weigh_sum_kernel(PagedArg
 
 // Few rows a sequence (decode): K is streamed once, the next block's keys asked for before the present one's are used.  Whole blocks
 // only, in equal runs.
-constexpr int kStreamSubs = 1;
-template <int D>
+constexpr int kStreamSubs = 1;                             // 16-key tiles of a wave
+// TILES: row tiles of a sequence that stay in registers from block to block
+template <int D, int TILES>
 __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a) {
   using T = uint16_t;
   using Tile = WeighTile<T, D>;
   constexpr int SUBS = kStreamSubs, KEYS = 64 * SUBS;
+  constexpr WeighOwn OWN = TILES > 1 ? kOwnShort : kOwnAll;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = blockIdx.x % a.h_kv, wg = blockIdx.x / a.h_kv;
   const int Tt = 16 / a.g, n = lane & 15, kq = lane >> 4, pm = (1 << a.page_log) - 1, tl = n / a.g;
   const uint32_t q_lane = (uint32_t)(tl * (int)a.q_t + n % a.g * (int)a.q_h) * 2u + kq * 16;
   const uint32_t l_lane = (uint32_t)(tl * a.h_q + n % a.g) * 4u;
   // blocks of all sequences, and the run's
-  const int64_t total = weigh_total<KEYS>(a, true);
+  const int64_t total = weigh_total<KEYS>(a, true, OWN);
   const PagedBounds<int64_t> bounds(a, total);
   int64_t f = bounds.at(wg);
   int todo = (int)(bounds.at(wg + 1) - f);
   if (todo <= 0) return;
   WeighItem it, next;
-  weigh_find<KEYS>(a, f, it, true);
+  weigh_find<KEYS>(a, f, it, true, OWN);
   auto advance = [&](WeighItem& x) {
     f++;
-    if (++x.block >= x.s.items) weigh_find<KEYS>(a, f, x, true);
+    if (++x.block >= x.s.items) weigh_find<KEYS>(a, f, x, true, OWN);
   };
   auto load_keys = [&](const WeighItem& x, Tile (&kf)[SUBS], int (&page)[SUBS]) {
     const int key0 = x.block * KEYS + wave * SUBS * 16;
@@ -329,10 +336,10 @@ __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a)
       kf[s].load((const T*)a.k + (int64_t)paged_clamp(a, page[s]) * a.kp_p + r * a.kp_h + (int64_t)(key & pm) * a.kp_t, kq);
     }
   };
-  Tile qf;
-  float off = 0.f;
-  int q_of = -1;                                             // the sequence whose only row tile qf and off hold
-  auto load_rows = [&](const WeighItem& x, int y) {
+  Tile rows[TILES];
+  float offs[TILES];
+  int q_of = -1;                                             // the sequence whose row tiles these hold
+  auto load_rows = [&](const WeighItem& x, int y, Tile& qf, float& off) {
     const int t = y * Tt + tl, up = max(t - (x.m - 1), 0);   // a lane behind the last row repeats it
     const int first = a.last > 0 ? max(x.m - a.last, 0) : 0;
     const char* q_at = (const char*)((const T*)a.q + (int64_t)(x.r0 + y * Tt) * a.q_t + (int64_t)(r * a.g) * a.q_h);
@@ -350,27 +357,37 @@ __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a)
     f32x4 acc[SUBS];
 #pragma unroll
     for (int j = 0; j < SUBS; j++) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int y = x.s.x0; y < x.s.x0 + x.s.tiles; y++) {
-      if (q_of != x.b) load_rows(x, y);
-      q_of = x.s.tiles == 1 ? x.b : -1;
-      f32x4 s[SUBS];
+    for (int y0 = x.s.x0; y0 < x.s.x0 + x.s.tiles; y0 += TILES) {
+      const int left = x.s.x0 + x.s.tiles - y0;
+      if (q_of != x.b) {
 #pragma unroll
-      for (int j = 0; j < SUBS; j++) s[j] = kf[j].dot(qf);
+        for (int u = 0; u < TILES; u++)
+          if (u < left) load_rows(x, y0 + u, rows[u], offs[u]);
+      }
+      q_of = x.s.tiles <= TILES ? x.b : -1;
 #pragma unroll
-      for (int j = 0; j < SUBS; j++)
+      for (int u = 0; u < TILES; u++) {
+        if (u >= left) break;
+        const int y = y0 + u;
+        f32x4 s[SUBS];
 #pragma unroll
-        for (int e = 0; e < 4; e++) s[j][e] = fmaf(s[j][e], a.c1, off);
-      if (key0 + SUBS * 16 - 1 > (a.causal ? back + y * Tt : x.n - 1)) {
-        const int lim = (a.causal ? min(back + y * Tt + tl, x.n - 1) : x.n - 1) - key0 - 4 * kq;
+        for (int j = 0; j < SUBS; j++) s[j] = kf[j].dot(rows[u]);
 #pragma unroll
         for (int j = 0; j < SUBS; j++)
 #pragma unroll
-          for (int e = 0; e < 4; e++) s[j][e] = 16 * j + e > lim ? -INFINITY : s[j][e];
+          for (int e = 0; e < 4; e++) s[j][e] = fmaf(s[j][e], a.c1, offs[u]);
+        if (key0 + SUBS * 16 - 1 > (a.causal ? back + y * Tt : x.n - 1)) {
+          const int lim = (a.causal ? min(back + y * Tt + tl, x.n - 1) : x.n - 1) - key0 - 4 * kq;
+#pragma unroll
+          for (int j = 0; j < SUBS; j++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) s[j][e] = 16 * j + e > lim ? -INFINITY : s[j][e];
+        }
+#pragma unroll
+        for (int j = 0; j < SUBS; j++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) acc[j][e] += __builtin_amdgcn_exp2f(s[j][e]);
       }
-#pragma unroll
-      for (int j = 0; j < SUBS; j++)
-#pragma unroll
-        for (int e = 0; e < 4; e++) acc[j][e] += __builtin_amdgcn_exp2f(s[j][e]);
     }
 #pragma unroll
     for (int j = 0; j < SUBS; j++) {
@@ -407,9 +424,16 @@ __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a)
 // resident workgroups of a kv-head, by the registers of a wave: three per CU at head dimension 128, four at 64; fp32 two and three
 static int weigh_wgs(const PagedArgs& a, int dtype, int d) { return max(256 * ((d == 128 ? 3 : 4) - (dtype != DASH_BF16)) / a.h_kv, 1); }
 
-// K is streamed where the sequences bring no more than 16 rows each on the average (16 sequences of 2048 to 16384 tokens, 32 / 8 heads: 16 rows
-// 73 us streamed, 84 not; 20 rows 118 and 93)
-static bool weigh_stream(const PagedArgs& a) { return (int64_t)a.n_rows * a.g <= (int64_t)a.batch * 16; }
+// K is streamed for sequences of up to 32 rows.  Which have more is known on the device only: calls that may have some, and bring no more than that on
+// the average, launch both kernels; a call of no more tokens than sequences launches the streaming one alone, which takes whatever there is.  (16
+// sequences of 2048 to 16384 tokens, 32 / 8 heads: 20 rows 78 us with both, not streamed 93; one of 400 new tokens beside 63 of one 190, not streamed
+// 230, only streamed 1984; three tokens of 8 sequences of 1000, where the second launch finds nothing, 18, only streamed 13.5.)
+enum class Weigh { kStream, kBoth, kNone };
+static Weigh weigh_how(const PagedArgs& a) {
+  const int64_t rows = (int64_t)a.n_rows * a.g;
+  if (a.n_rows <= a.batch || rows <= 16 * kStreamTiles) return Weigh::kStream;
+  return rows <= (int64_t)a.batch * 16 * kStreamTiles ? Weigh::kBoth : Weigh::kNone;
+}
 
 size_t paged_weigh_ws(const PagedArgs& a, int dtype, int d) {
   return (size_t)weigh_wgs(a, dtype, d) * a.h_kv * 2 * (dtype == DASH_BF16 ? kWeighKeys<uint16_t> : kWeighKeys<float>) * 4;
@@ -418,18 +442,22 @@ size_t paged_weigh_ws(const PagedArgs& a, int dtype, int d) {
 template <typename T, int D>
 static hipError_t launch_weigh_t(PagedArgs a, char* ws, hipStream_t st) {
   if constexpr (sizeof(T) == 2) {
-    if (weigh_stream(a)) {
+    const Weigh how = weigh_how(a);
+    if (how != Weigh::kNone) {
+      a.whole = how == Weigh::kBoth;
       a.wgs = max(1024 / a.h_kv, 1);
-      hipLaunchKernelGGL(paged_weigh_stream_kernel<D>, dim3((unsigned)(a.wgs * a.h_kv)), dim3(256), 0, st, a);
-      return hipGetLastError();
+      const dim3 grid((unsigned)(a.wgs * a.h_kv)), blk(256);
+      if (a.n_rows <= a.batch) hipLaunchKernelGGL((paged_weigh_stream_kernel<D, 1>), grid, blk, 0, st, a);
+      else hipLaunchKernelGGL((paged_weigh_stream_kernel<D, kStreamTiles>), grid, blk, 0, st, a);
+      if (hipError_t e = hipGetLastError(); e != hipSuccess || how == Weigh::kStream) return e;
     }
   }
   a.part_o = (float*)ws;
   a.wgs = weigh_wgs(a, sizeof(T) == 2 ? DASH_BF16 : DASH_F32, D);
   hipLaunchKernelGGL((paged_weigh_kernel<T, D>), dim3((unsigned)(a.wgs * a.h_kv)), dim3(256), 0, st, a);
   hipError_t e = hipGetLastError();
-  // a single tile of rows is not cut
-  if (e != hipSuccess || a.n_rows * (int64_t)a.g <= 16 || a.wgs == 1) return e;
+  // nothing is cut beside the streaming kernel, nor a single tile of rows
+  if (e != hipSuccess || a.whole || a.n_rows * (int64_t)a.g <= 16 || a.wgs == 1) return e;
   hipLaunchKernelGGL(paged_weigh_sum_kernel<T>, dim3((unsigned)((a.wgs - 1) * a.h_kv)), dim3(kWeighKeys<T>), 0, st, a);
   return hipGetLastError();
 }

@@ -407,6 +407,13 @@ def test_weights_a_row_that_is_nan_reaches_only_the_tokens_it_sees(dtype, m, bad
     assert ((got[seen:].double() - want[seen:]).abs() <= tol[seen:]).all()
 
 
+@pytest.mark.parametrize("last", [0, 2])
+@pytest.mark.parametrize("d,g", [(128, 4), (64, 8), (128, 1)])
+@pytest.mark.parametrize("news", [[70] + [1] * 30, [1, 2, 0, 33] + [3] * 36, [0] * 20 + [25] + [0] * 9, [5] * 12])
+def test_weights_of_long_and_short_pieces_in_one_call(last, d, g, news):
+    check_weigh(Setup([(83 * i) % 500 + news[i] for i in range(len(news))], news, h_kv=2, g=g, d=d, page=16, behind=math.nan, seed=42), last=last)
+
+
 def test_weights_of_pages_that_sequences_share():
     s = Setup([300, 280], [1, 2], page=16, seed=28)
     s.ref.table[1, :17] = s.ref.table[0, :17]                   # 272 tokens in common
