@@ -8,9 +8,10 @@ or a call fails, an exception is raised.
 from __future__ import annotations
 
 import ctypes
-import math
+import operator
 import os
-from dataclasses import dataclass, field
+import struct
+from dataclasses import dataclass
 from typing import Optional
 
 import torch
@@ -43,7 +44,6 @@ class dash_paged_params(ctypes.Structure):
     _fields_ += [("scale", ctypes.c_float), ("reserved", ctypes.c_int32)]
     _fields_ += [(n, ctypes.c_int64 * k) for n, k in (("q_stride", 2), ("o_stride", 2), ("k_new_stride", 2), ("v_new_stride", 2),
                                                       ("k_stride", 3), ("v_stride", 3))]
-    layout = None        # of the cache that make_paged_params was given
 
 
 _lib = None
@@ -312,7 +312,7 @@ class PagedCache:
     """Keys and values of several sequences in pages of a pool (see the header's section on the paged cache).
     k, v [n_pages, h_kv, page_size, d]; table int32 [batch, max_pages]; lens int32 [batch]; for evicting callers
     weights (fp32) and pos (int32), both [n_pages, h_kv, page_size], and seen int32 [batch].
-    The tensors are checked by the first call after another one is assigned, not by every call."""
+    Every call checks those that it uses."""
     k: torch.Tensor
     v: torch.Tensor
     table: torch.Tensor
@@ -320,18 +320,6 @@ class PagedCache:
     weights: Optional[torch.Tensor] = None
     pos: Optional[torch.Tensor] = None
     seen: Optional[torch.Tensor] = None
-    layout: Optional[tuple] = field(default=None, init=False, repr=False, compare=False)   # of k, v and table; None: not checked
-    fresh: tuple = field(default=(), init=False, repr=False, compare=False)                # others that are not checked
-
-    def __setattr__(self, name, value):
-        own = self.__dict__
-        if own.get(name, own) is value:
-            return
-        own[name] = value
-        if name in ("k", "v", "table"):
-            own["layout"] = None
-        else:
-            own["fresh"] = self.fresh + (name,)
 
     @staticmethod
     def allocate(batch: int, h_kv: int, n_pages: int, page_size: int, head_dim: int, max_pages: int, device,
@@ -346,39 +334,49 @@ class PagedCache:
         return c
 
 
-def _paged_layout(c: PagedCache) -> tuple:
-    """Device, type, sizes and strides of a cache whose tensors fit each other."""
-    layout = c.layout
-    if layout is None:
-        k, v, t = c.k, c.v, c.table
-        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype or k.dtype not in (torch.bfloat16, torch.float32):
-            raise DashError("k and v pages: two tensors [n_pages, h_kv, page_size, d] of one type, bf16 or fp32")
-        if k.stride(3) != 1 or v.stride(3) != 1:
-            raise DashError("k and v pages: head_dim must be contiguous")
-        if t.dim() != 2 or t.dtype != torch.int32 or not t.is_contiguous():
-            raise DashError("table [batch, max_pages]: a contiguous int32 tensor")
-        if v.device != k.device or t.device != k.device:
-            raise DashError("the cache's tensors lie on one device")
-        layout = (k.get_device(), k.dtype, k.shape, k.stride(), v.stride(), t.shape)
-        c.__dict__["fresh"] = ("lens", "weights", "pos", "seen")
-    if c.fresh:
-        for name in c.fresh:
-            x = getattr(c, name)
-            if x is None and name != "lens":
-                continue
-            if x.dtype is not (torch.float32 if name == "weights" else torch.int32) or not x.is_contiguous() or \
-                    x.shape != (layout[2][:3] if name in ("weights", "pos") else layout[5][:1]):
-                raise DashError("lens and seen int32 [batch], weights (fp32) and pos (int32) [n_pages, h_kv, page_size]: contiguous tensors")
-            if x.get_device() != layout[0]:
-                raise DashError("the cache's tensors lie on one device")
-        c.__dict__["layout"], c.__dict__["fresh"] = layout, ()
-    return layout
+_PAGED_PARAMS = struct.Struct("10ifi14q")                  # dash_paged_params ...
+_paged_sizes = operator.itemgetter(0, 2, 3, 4, 6, 7, 8, *range(20, 26))   # ... and its batch, h_kv, head_dim, dtype, page_size, n_pages, max_pages, k_stride, v_stride
+_INT, _FLOAT = torch.int32, torch.float32
+_PAGED_TYPES = {torch.bfloat16: DASH_BF16, _FLOAT: DASH_F32}
+
+
+def _paged_layout(c: PagedCache, weights=None, pos=None, seen=None) -> tuple:
+    """Device, type, and sizes and strides (as _paged_sizes has them) of a cache whose tensors fit each other, those of the optional
+    ones among them that are given.  Every call looks at them anew, for a tensor can change in place."""
+    k, v, t, lens = c.k, c.v, c.table, c.lens
+    shape, dtype, dev = tuple(k.shape), k.dtype, k.get_device()
+    if len(shape) != 4 or v.shape != shape or v.dtype is not dtype or dtype not in _PAGED_TYPES:
+        raise DashError("k and v pages: two tensors [n_pages, h_kv, page_size, d] of one type, bf16 or fp32")
+    n_pages, h_kv, page_size, d = shape
+    kp, kh, kt, k1 = k.stride()
+    vp, vh, vt, v1 = v.stride()
+    if k1 != 1 or v1 != 1:
+        raise DashError("k and v pages: head_dim must be contiguous")
+    if t.dtype is not _INT or t.dim() != 2 or not t.is_contiguous():
+        raise DashError("table [batch, max_pages]: a contiguous int32 tensor")
+    batch, max_pages = t.shape
+    ok = lens is not None and lens.dtype is _INT and lens.shape == (batch,) and lens.is_contiguous()
+    same = v.get_device() == dev == t.get_device()
+    if weights is not None:
+        ok = ok and weights.dtype is _FLOAT and weights.shape == shape[:3] and weights.is_contiguous()
+        same = same and weights.get_device() == dev
+    if pos is not None:
+        ok = ok and pos.dtype is _INT and pos.shape == shape[:3] and pos.is_contiguous()
+        same = same and pos.get_device() == dev
+    if seen is not None:
+        ok = ok and seen.dtype is _INT and seen.shape == (batch,) and seen.is_contiguous()
+        same = same and seen.get_device() == dev
+    if not ok:
+        raise DashError("lens and seen int32 [batch], weights (fp32) and pos (int32) [n_pages, h_kv, page_size]: contiguous tensors")
+    if not same or lens.get_device() != dev:
+        raise DashError("the cache's tensors lie on one device")
+    return dev, dtype, (batch, h_kv, d, _PAGED_TYPES[dtype], page_size, n_pages, max_pages, kp, kh, kt, vp, vh, vt)
 
 
 def make_paged_params(cache: PagedCache, n_rows: int, h_q: int, causal: bool = True, scale: float = 0.0) -> dash_paged_params:
     """The parameters of calls on this cache, or on others of the same sizes, strides and type.  The strides of q, o, k_new and
     v_new are those of the tensors each call is given."""
-    layout = _paged_layout(cache)
+    _paged_layout(cache, cache.weights, cache.pos, cache.seen)
     p = dash_paged_params()
     p.batch, p.max_pages = cache.table.shape
     p.n_pages, p.h_kv, p.page_size, p.head_dim = cache.k.shape
@@ -386,27 +384,27 @@ def make_paged_params(cache: PagedCache, n_rows: int, h_q: int, causal: bool = T
     p.dtype = DASH_BF16 if cache.k.dtype == torch.bfloat16 else DASH_F32
     p.k_stride[:] = cache.k.stride()[:3]
     p.v_stride[:] = cache.v.stride()[:3]
-    p.layout = layout
     return p
 
 
-def _paged_call(p: dash_paged_params, cache: PagedCache, row_start, rows, extra=None, ws=None):
-    """The call's own copy of p, with the strides of its packed tensors, and the current stream.  rows: (tensor, heads, field of
-    its strides); extra: (tensor, type, shape)."""
-    layout = _paged_layout(cache)
-    if layout is not p.layout and layout != p.layout:
+def _paged_call(p: dash_paged_params, layout, row_start, rows, extra=None, ws=None):
+    """The call's own copy of p, with the strides of its packed tensors, and the current stream.  layout: of the call's cache; rows: (tensor,
+    heads, field of its strides); extra: (tensor, type, shape)."""
+    dev, dtype, sizes = layout
+    f = _PAGED_PARAMS.unpack_from(p)
+    if _paged_sizes(f) != sizes:
         raise DashError("the parameters are those of a cache of other sizes, strides or type (make_paged_params)")
     p = dash_paged_params.from_buffer_copy(p)
-    dev, dtype = layout[:2]
-    if row_start is not None and (row_start.dtype is not torch.int32 or row_start.numel() != p.batch + 1 or not row_start.is_contiguous()
+    d, n_rows = f[3], f[9]
+    if row_start is not None and (row_start.dtype is not _INT or row_start.numel() != f[0] + 1 or not row_start.is_contiguous()
                                   or row_start.get_device() != dev):
         raise DashError("row_start: a contiguous int32 tensor of batch + 1 elements on the cache's device")
     for t, heads, name in rows:
         s = t.stride()
-        if t.dtype is not dtype or t.shape != (p.n_rows, heads, p.head_dim) or s[2] != 1 or t.get_device() != dev:
-            raise DashError(f"packed rows: [{p.n_rows}, {heads}, {p.head_dim}] of the cache's type and device, head_dim contiguous")
-        f = getattr(p, name)
-        f[0], f[1] = s[0], s[1]
+        if t.dtype is not dtype or t.shape != (n_rows, heads, d) or s[2] != 1 or t.get_device() != dev:
+            raise DashError(f"packed rows: [{n_rows}, {heads}, {d}] of the cache's type and device, head_dim contiguous")
+        strides = getattr(p, name)
+        strides[0], strides[1] = s[0], s[1]
     if extra is not None and extra[0] is not None:
         t, want, shape = extra
         if t.dtype is not want or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
@@ -434,7 +432,8 @@ def alloc_paged_workspace(p: dash_paged_params, device, evict: bool = False) -> 
 
 def dash_paged_append(p: dash_paged_params, cache: PagedCache, k_new, v_new, row_start) -> None:
     """k_new, v_new [n_rows, h_kv, d]; cache.weights, pos and seen as far as they are there."""
-    p, stream = _paged_call(p, cache, row_start, ((k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride")))
+    layout = _paged_layout(cache, cache.weights, cache.pos, cache.seen)
+    p, stream = _paged_call(p, layout, row_start, ((k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride")))
     _check(load_library().dash_paged_append(p, k_new.data_ptr(), v_new.data_ptr(), cache.k.data_ptr(), cache.v.data_ptr(),
                                             row_start.data_ptr(), cache.lens.data_ptr(), cache.table.data_ptr(), _ptr(cache.weights),
                                             _ptr(cache.pos), _ptr(cache.seen), stream), "dash_paged_append")
@@ -442,8 +441,8 @@ def dash_paged_append(p: dash_paged_params, cache: PagedCache, k_new, v_new, row
 
 def dash_paged_attend(p: dash_paged_params, cache: PagedCache, q, row_start, o, ws: torch.Tensor, lse=None) -> None:
     """q, o [n_rows, h_q, d]; lse fp32 [n_rows, h_q] or None."""
-    p, stream = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"), (o, p.h_q, "o_stride")),
-                            (lse, torch.float32, (p.n_rows, p.h_q)), ws)
+    p, stream = _paged_call(p, _paged_layout(cache), row_start, ((q, p.h_q, "q_stride"), (o, p.h_q, "o_stride")),
+                            (lse, _FLOAT, (p.n_rows, p.h_q)), ws)
     wp, wn = _ws_ptr(ws)
     _check(load_library().dash_paged_attend(p, q.data_ptr(), cache.k.data_ptr(), cache.v.data_ptr(), row_start.data_ptr(),
                                             cache.lens.data_ptr(), cache.table.data_ptr(), o.data_ptr(), _ptr(lse), wp, wn, stream),
@@ -454,7 +453,7 @@ def dash_paged_weigh(p: dash_paged_params, cache: PagedCache, q, row_start, lse,
     """Adds to cache.weights; lse as dash_paged_attend wrote it."""
     if cache.weights is None or lse is None:
         raise DashError("dash_paged_weigh needs the cache's weights and the rows' lse")
-    p, stream = _paged_call(p, cache, row_start, ((q, p.h_q, "q_stride"),), (lse, torch.float32, (p.n_rows, p.h_q)), ws)
+    p, stream = _paged_call(p, _paged_layout(cache, cache.weights), row_start, ((q, p.h_q, "q_stride"),), (lse, _FLOAT, (p.n_rows, p.h_q)), ws)
     wp, wn = _ws_ptr(ws)
     _check(load_library().dash_paged_weigh(p, q.data_ptr(), cache.k.data_ptr(), row_start.data_ptr(), cache.lens.data_ptr(),
                                            cache.table.data_ptr(), _ptr(lse), last, _ptr(cache.weights), wp, wn, stream), "dash_paged_weigh")
@@ -464,7 +463,8 @@ def dash_paged_evict(p: dash_paged_params, cache: PagedCache, budget: int, ws: t
     """ws from alloc_paged_workspace(p, device, evict=True); src int32 [batch, h_kv, budget] or None."""
     if cache.weights is None or cache.pos is None or cache.seen is None:
         raise DashError("dash_paged_evict needs the cache's weights, pos and seen")
-    p, stream = _paged_call(p, cache, None, (), (src, torch.int32, (p.batch, p.h_kv, budget)), ws)
+    layout = _paged_layout(cache, cache.weights, cache.pos, cache.seen)
+    p, stream = _paged_call(p, layout, None, (), (src, _INT, (p.batch, p.h_kv, budget)), ws)
     wp, wn = _ws_ptr(ws)
     _check(load_library().dash_paged_evict(p, cache.k.data_ptr(), cache.v.data_ptr(), cache.lens.data_ptr(), _ptr(cache.seen), cache.table.data_ptr(),
                                            _ptr(cache.weights), _ptr(cache.pos), budget, sinks, recent, _ptr(src), wp, wn, stream),

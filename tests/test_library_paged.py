@@ -190,3 +190,37 @@ def test_the_binding_looks_at_a_tensor_that_is_assigned():
     c.weights = c.weights.clone()
     with pytest.raises(B.DashError, match="GPU"):
         B.dash_paged_evict(p, c, 8, ws)
+
+
+def test_the_binding_looks_at_the_tensors_of_every_call():
+    """A tensor changed in place behind the first call (the same object, other sizes) is refused before anything reads by the old ones."""
+    def fresh():
+        c = B.PagedCache.allocate(2, 2, 8, 16, 64, 4, "cpu", evicting=True)
+        p = B.make_paged_params(c, 3, 4)
+        call = lambda: B.dash_paged_evict(p, c, 8, torch.empty(1 << 20, dtype=torch.uint8))  # noqa: E731
+        with pytest.raises(B.DashError, match="GPU"):            # nothing wrong but where the tensors lie
+            call()
+        return c, p, call
+    changes = {
+        "k pages fewer": lambda c: setattr(c.k, "data", c.k[:4]), "v pages fewer": lambda c: c.v.resize_(4, 2, 16, 64),
+        "k of another type": lambda c: setattr(c.k, "data", c.k.float()), "v strides": lambda c: setattr(c.v, "data", c.v.transpose(1, 2).contiguous().transpose(1, 2)),
+        "lens": lambda c: c.lens.resize_(1), "table": lambda c: c.table.resize_(2, 2), "table of another order": lambda c: c.table.t_(),
+        "weights": lambda c: c.weights.resize_(4, 2, 16), "weights of another type": lambda c: setattr(c.weights, "data", c.weights.double()),
+        "pos": lambda c: setattr(c.pos, "data", c.pos.transpose(1, 2)), "seen": lambda c: setattr(c.seen, "data", c.seen.long()),
+    }
+    for name, change in changes.items():
+        c, _, call = fresh()
+        change(c)
+        with pytest.raises(B.DashError, match="contiguous|pages|other sizes"):
+            call()
+    # and parameters whose sizes or strides are no longer the cache's
+    for field, value in (("batch", 3), ("n_pages", 9), ("max_pages", 5), ("page_size", 32), ("h_kv", 4), ("head_dim", 128), ("dtype", B.DASH_F32)):
+        _, p, call = fresh()
+        setattr(p, field, value)
+        with pytest.raises(B.DashError, match="other sizes"):
+            call()
+    for field in ("k_stride", "v_stride"):
+        _, p, call = fresh()
+        getattr(p, field)[2] = 128
+        with pytest.raises(B.DashError, match="other sizes"):
+            call()
