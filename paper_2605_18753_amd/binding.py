@@ -373,10 +373,18 @@ def _paged_layout(c: PagedCache, weights=None, pos=None, seen=None) -> tuple:
     return dev, dtype, (batch, h_kv, d, _PAGED_TYPES[dtype], page_size, n_pages, max_pages, kp, kh, kt, vp, vh, vt)
 
 
+def _int32(**numbers):
+    # ctypes takes the low 32 bits of a number without a word
+    for name, x in numbers.items():
+        if not -1 << 31 <= x < 1 << 31:
+            raise DashError(f"{name}: {x} does not fit 32 bits")
+
+
 def make_paged_params(cache: PagedCache, n_rows: int, h_q: int, causal: bool = True, scale: float = 0.0) -> dash_paged_params:
     """The parameters of calls on this cache, or on others of the same sizes, strides and type.  The strides of q, o, k_new and
     v_new are those of the tensors each call is given."""
     _paged_layout(cache, cache.weights, cache.pos, cache.seen)
+    _int32(n_rows=n_rows, h_q=h_q)
     p = dash_paged_params()
     p.batch, p.max_pages = cache.table.shape
     p.n_pages, p.h_kv, p.page_size, p.head_dim = cache.k.shape
@@ -453,6 +461,7 @@ def dash_paged_weigh(p: dash_paged_params, cache: PagedCache, q, row_start, lse,
     """Adds to cache.weights; lse as dash_paged_attend wrote it."""
     if cache.weights is None or lse is None:
         raise DashError("dash_paged_weigh needs the cache's weights and the rows' lse")
+    _int32(last=last)
     p, stream = _paged_call(p, _paged_layout(cache, cache.weights), row_start, ((q, p.h_q, "q_stride"),), (lse, _FLOAT, (p.n_rows, p.h_q)), ws)
     wp, wn = _ws_ptr(ws)
     _check(load_library().dash_paged_weigh(p, q.data_ptr(), cache.k.data_ptr(), row_start.data_ptr(), cache.lens.data_ptr(),
@@ -463,6 +472,7 @@ def dash_paged_evict(p: dash_paged_params, cache: PagedCache, budget: int, ws: t
     """ws from alloc_paged_workspace(p, device, evict=True); src int32 [batch, h_kv, budget] or None."""
     if cache.weights is None or cache.pos is None or cache.seen is None:
         raise DashError("dash_paged_evict needs the cache's weights, pos and seen")
+    _int32(budget=budget, sinks=sinks, recent=recent)
     layout = _paged_layout(cache, cache.weights, cache.pos, cache.seen)
     p, stream = _paged_call(p, layout, None, (), (src, _INT, (p.batch, p.h_kv, budget)), ws)
     wp, wn = _ws_ptr(ws)

@@ -224,3 +224,16 @@ def test_the_binding_looks_at_the_tensors_of_every_call():
         getattr(p, field)[2] = 128
         with pytest.raises(B.DashError, match="other sizes"):
             call()
+
+
+@pytest.mark.parametrize("far", [(1 << 32) + 8, 1 << 31, -(1 << 32) + 8])
+def test_the_binding_refuses_numbers_that_do_not_fit_32_bits(far):
+    """They would be cut to their low 32 bits on the way: a budget of 2^32 + 8 tokens to one of 8."""
+    c = B.PagedCache.allocate(2, 2, 8, 16, 64, 4, "cpu", evicting=True)
+    p = B.make_paged_params(c, 8, 4)
+    ws, start = torch.empty(1 << 20, dtype=torch.uint8), torch.zeros(3, dtype=torch.int32)
+    q, lse = torch.zeros((8, 4, 64), dtype=torch.bfloat16), torch.zeros((8, 4))
+    for f in (lambda: B.dash_paged_evict(p, c, far, ws), lambda: B.dash_paged_evict(p, c, 8, ws, sinks=far), lambda: B.dash_paged_evict(p, c, 8, ws, recent=far),
+              lambda: B.dash_paged_weigh(p, c, q, start, lse, ws, last=far), lambda: B.make_paged_params(c, far, 4), lambda: B.make_paged_params(c, 8, far)):
+        with pytest.raises(B.DashError, match="32 bits"):
+            f()
