@@ -161,6 +161,8 @@ def alloc_workspace(p: dash_params, device) -> torch.Tensor:
 
 
 def _ws_ptr(ws: torch.Tensor):
+    if not ws.is_contiguous():
+        raise DashError("a workspace is contiguous")
     base = ws.data_ptr()
     aligned = (base + 255) & ~255
     return aligned, ws.numel() - (aligned - base)

@@ -237,3 +237,12 @@ def test_the_binding_refuses_numbers_that_do_not_fit_32_bits(far):
               lambda: B.dash_paged_weigh(p, c, q, start, lse, ws, last=far), lambda: B.make_paged_params(c, far, 4), lambda: B.make_paged_params(c, 8, far)):
         with pytest.raises(B.DashError, match="32 bits"):
             f()
+
+
+def test_the_binding_refuses_a_workspace_whose_elements_do_not_lie_in_a_row():
+    """Its number of elements is not the bytes behind its address."""
+    one = torch.empty(1, dtype=torch.uint8)
+    for ws in (one.expand(1 << 30), torch.empty(1 << 12, dtype=torch.uint8)[::2]):
+        with pytest.raises(B.DashError, match="contiguous"):
+            B._ws_ptr(ws)
+    assert B._ws_ptr(torch.empty(1 << 12, dtype=torch.uint8))[1] > (1 << 12) - 256
