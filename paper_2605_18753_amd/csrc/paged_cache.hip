@@ -13,7 +13,7 @@ namespace dash {
 template <int ES, int D>   // bytes of an element
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedArgs a) {
   constexpr int CHUNKS = D * ES / 16, AHEAD = 4;             // 16-byte pieces of a row; pieces of a lane in flight
-  const int lane = threadIdx.x & 63, row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, row = paged_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (row >= a.n_rows) return;
   const int pieces = 2 * a.h_kv * CHUNKS;
   const char* kn = (const char*)a.k_new + row * a.kn_t * ES;
@@ -67,7 +67,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedArgs a) {
 }
 
 hipError_t launch_paged_append(const PagedArgs& a, int elem, int d, hipStream_t st) {
-  const dim3 grid((unsigned)(((int64_t)a.n_rows + 3) / 4)), blk(256);
+  const dim3 grid = paged_grid(((int64_t)a.n_rows + 3) / 4), blk(256);
   if (elem == 2 && d == 128) hipLaunchKernelGGL((paged_append_kernel<2, 128>), grid, blk, 0, st, a);
   else if (elem == 2) hipLaunchKernelGGL((paged_append_kernel<2, 64>), grid, blk, 0, st, a);
   else if (d == 128) hipLaunchKernelGGL((paged_append_kernel<4, 128>), grid, blk, 0, st, a);

@@ -454,6 +454,20 @@ def test_append(dtype, d, page, layout, h_kv, evicting):
         assert torch.equal(s.gpu.weights.cpu(), s.ref.weights) and torch.equal(s.gpu.pos.cpu(), s.ref.pos)
 
 
+def test_append_of_more_rows_than_a_launch_has_threads_for():
+    # a wave a row: 64 (2^26 + 5) threads.  The rows share one row of memory; the second sequence is shorter than its rows, so its last three are written.
+    n, c = (1 << 26) + 5, B.PagedCache.allocate(2, 1, 2, 16, 64, 1, DEV)
+    c.table.copy_(torch.tensor([[1], [0]]))
+    c.lens.copy_(torch.tensor([5, 3]))
+    row = torch.randn((2, 1, 1, 64), dtype=BF, device=DEV)
+    start = torch.tensor([0, 5, n], dtype=torch.int32, device=DEV)
+    B.dash_paged_append(B.make_paged_params(c, n, 1), c, row[0].expand(n, 1, 64), row[1].expand(n, 1, 64), start)
+    for x, y in ((c.k, row[0]), (c.v, row[1])):
+        want = torch.zeros_like(x)
+        want[1, 0, :5] = want[0, 0, :3] = y[0, 0]
+        assert torch.equal(x, want)
+
+
 def test_append_positions_without_seen_and_a_large_batch():
     lens = [1 + (37 * i) % 90 for i in range(150)]
     s = Setup(lens, [min(n, i % 4) for i, n in enumerate(lens)], h_kv=1, g=1, d=64, page=16, seed=32)
