@@ -320,7 +320,8 @@ int dash_kbar_summarize_backward(const dash_params* p, const void* k, const floa
  * serves any lengths that fit its n_rows, batch and max_pages.  A table entry outside [0, n_pages) is never
  * followed: reads take some page of the pool, writes leave the token out.
  * Limits: head_dim 64 or 128; h_q / h_kv in {1, 2, 4, 8, 16}; page_size a power of two from 16 to 1024;
- * max_pages * page_size <= 2^24; a page's slice of one head below 2 GiB; strides of q and o up to 2^25 elements
+ * max_pages * page_size <= 2^24; a page's slice of one head below 2 GiB; strides of q and o up to 2^25 elements;
+ * batch * h_kv <= 2^20; n_rows and n_rows * h_q <= 2^28, fp32 attention n_rows * h_q / 16 + batch * h_kv < 2^23
  * (DASH_EUNSUPPORTED beyond them).
  * NaN and infinities: as above, and what the pages hold behind a sequence's last token reaches nothing. */
 typedef struct dash_paged_params {

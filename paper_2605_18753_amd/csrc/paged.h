@@ -237,15 +237,6 @@ template <typename I> struct PagedBounds {
   }
 };
 
-// A launch of 2^32 threads or more in a dimension loses some without an error.  Kernels with a workgroup per row or item, which can be so many,
-// have them in rows of 2^22; those behind the last one find nothing to do.
-constexpr int kGridLog = 22;
-inline dim3 paged_grid(int64_t wgs) {
-  const int64_t row = (int64_t)1 << kGridLog;
-  return dim3((unsigned)(wgs < row ? wgs : row), (unsigned)((wgs + row - 1) / row));
-}
-__device__ __forceinline__ int paged_block() { return (int)(blockIdx.y << kGridLog | blockIdx.x); }
-
 // The kernel's arguments (its first and only parameter) and thread index, asked for anew: what follows from them is not kept in registers
 // from piece to piece, for which the walks have none left.
 __device__ __forceinline__ PagedArgs paged_reload() {
@@ -308,6 +299,7 @@ hipError_t launch_paged_attend(const PagedArgs& a, int dtype, int d, char* ws, h
 hipError_t launch_paged_weigh(const PagedArgs& a, int dtype, int d, char* ws, hipStream_t st);
 hipError_t launch_paged_evict(const PagedArgs& a, int elem, int d, int32_t* lens, int budget, int sinks, int recent, int32_t* src,
                               char* ws, hipStream_t st);
+bool paged_attend_fits(const PagedArgs& a, int dtype);
 size_t paged_attend_ws(const PagedArgs& a, int dtype, int d);
 size_t paged_weigh_ws(const PagedArgs& a, int dtype, int d);
 size_t paged_evict_ws(const PagedArgs& a);

@@ -96,6 +96,7 @@ int dash_paged_attend(const dash_paged_params* p, const void* q, const void* k_p
   if (const int rc = paged_args(p, &a, true, false); rc != DASH_OK) return rc;
   if (!q || !k_pages || !v_pages || !row_start || !lens || !table || !o) return DASH_EINVAL;
   if (misaligned(q) || misaligned(k_pages) || misaligned(v_pages) || misaligned(o)) return DASH_EINVAL;
+  if (!paged_attend_fits(a, p->dtype)) return DASH_EUNSUPPORTED;
   if (const int rc = check_scratch(paged_attend_ws(a, p->dtype, p->head_dim), workspace, workspace_bytes); rc != DASH_OK) return rc;
   a.q = q; a.k = (void*)k_pages; a.v = (void*)v_pages; a.o = o; a.lse = lse;
   a.row_start = row_start; a.lens = lens; a.table = table;

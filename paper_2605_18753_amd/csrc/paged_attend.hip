@@ -853,6 +853,9 @@ static int64_t most_items(const PagedArgs& a, int rows) {   // of a kv-head
   const int T = rows / a.g;
   return min((int64_t)a.n_rows / T + min(a.batch, a.n_rows), (int64_t)a.n_rows);
 }
+// A launch of 2^32 threads or more loses some without an error.  fp32: 512 for an item (bf16: 256, and fewer than 2^22 items whatever the limits of
+// n_rows h_q and batch h_kv allow).
+bool paged_attend_fits(const PagedArgs& a, int dtype) { return dtype != DASH_F32 || most_items(a, 16) * a.h_kv < (1 << 23); }
 // The kernel for a call: tiles of 128 rows where the sequences bring more than 16 rows each on the average, tiles of 16 otherwise.  (32 / 8 heads, tiles of 128
 // and of 16.  16 rows each: 64 sequences of 2000 tokens 99.6 and 97.7 us, one of 1000 14.7 and 11.0; 20 rows: 101 and 167, 8 of 16000 104 and 103; 48
 // rows: 108 and 281.)  Short caches are read from the last-level cache again and again at no cost: tiles of 16 as long as each has a CU (one

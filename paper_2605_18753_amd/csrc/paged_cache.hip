@@ -10,10 +10,12 @@ namespace dash {
 // byte is read once and written once), by the chain of dependent loads where there are few: what a row holds, and the starts,
 // lengths and positions of 64 sequences, are asked for together; only the page waits for them.  (2047 tokens of each of four sequences, 8 heads
 // of 128: 12.3 us, 5.5 TB/s; a token of 64: 4.4 us.)
+// A launch of 2^32 threads or more in a dimension loses some without an error: the workgroups lie in rows of 2^22.
+constexpr int kGridLog = 22;
 template <int ES, int D>   // bytes of an element
 __global__ __launch_bounds__(256) void paged_append_kernel(PagedArgs a) {
   constexpr int CHUNKS = D * ES / 16, AHEAD = 4;             // 16-byte pieces of a row; pieces of a lane in flight
-  const int lane = threadIdx.x & 63, row = paged_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, row = (int)(blockIdx.y << kGridLog | blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (row >= a.n_rows) return;
   const int pieces = 2 * a.h_kv * CHUNKS;
   const char* kn = (const char*)a.k_new + row * a.kn_t * ES;
@@ -67,7 +69,8 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedArgs a) {
 }
 
 hipError_t launch_paged_append(const PagedArgs& a, int elem, int d, hipStream_t st) {
-  const dim3 grid = paged_grid(((int64_t)a.n_rows + 3) / 4), blk(256);
+  const int64_t wgs = ((int64_t)a.n_rows + 3) / 4, most = (int64_t)1 << kGridLog;
+  const dim3 grid((unsigned)(wgs < most ? wgs : most), (unsigned)((wgs + most - 1) / most)), blk(256);
   if (elem == 2 && d == 128) hipLaunchKernelGGL((paged_append_kernel<2, 128>), grid, blk, 0, st, a);
   else if (elem == 2) hipLaunchKernelGGL((paged_append_kernel<2, 64>), grid, blk, 0, st, a);
   else if (d == 128) hipLaunchKernelGGL((paged_append_kernel<4, 128>), grid, blk, 0, st, a);

@@ -246,3 +246,16 @@ def test_the_binding_refuses_a_workspace_whose_elements_do_not_lie_in_a_row():
         with pytest.raises(B.DashError, match="contiguous"):
             B._ws_ptr(ws)
     assert B._ws_ptr(torch.empty(1 << 12, dtype=torch.uint8))[1] > (1 << 12) - 256
+
+
+def test_fp32_attention_refuses_more_rows_than_a_launch_has_threads_for():
+    """512 threads for 16 rows of a kv-head's group; threads behind 2^32 would be left out without an error."""
+    def rc(n_rows, batch, h_q, h_kv, dtype=B.DASH_F32, name="attend"):
+        p = params(n_rows=n_rows, batch=batch, h_q=h_q, h_kv=h_kv, head_dim=64, dtype=dtype)
+        return call(name, p, ws=4096, n=0 if name == "attend" else 1 << 40, k=264 if name == "weigh" else 256)
+    for case in (((1 << 24), 1, 16, 16), ((1 << 28), 1, 1, 1), ((1 << 23) - 1 << 4, 1, 1, 1), ((1 << 22), 1, 64, 4), ((1 << 23) - (1 << 20) << 4, 1 << 20, 1, 1)):
+        assert rc(*case) == -2, case
+    # the next smaller ones, and others of as many rows, come to the next check (the workspace's, the pages' alignment)
+    for case in (((1 << 23) - 1 << 4) - 1, 1, 1, 1), (1 << 22, 1 << 20, 1, 1):
+        assert rc(*case) == -3, case
+    assert rc(1 << 24, 1, 16, 16, dtype=B.DASH_BF16) == -3 and rc(1 << 24, 1, 16, 16, name="weigh") == -1
