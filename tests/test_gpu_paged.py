@@ -129,6 +129,15 @@ def test_items_that_stay_whole_beside_cut_ones(lens, news):
     Setup(lens, news, h_kv=128, g=1, d=64, page=128, seed=41).check_attend()
 
 
+# A workgroup that walks more than 64 pages asks for the next 64 entries of the table on the way.  Whole items of 400 and 200 pages beside parts of 136 and 68;
+# parts of 24 and of 46 tiles, 96 and 184 pages of 16, most of which begin inside the sequence.
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens,news,h_kv,g,d,page", [([6400], [380], 128, 1, 64, 16), ([6400], [380], 128, 1, 64, 32), ([9000, 70], [300, 1], 8, 4, 128, 16),
+                                                     ([17600, 40], [20, 5], 64, 8, 64, 16)])
+def test_items_of_many_pages(lens, news, h_kv, g, d, page, causal):
+    Setup(lens, news, h_kv=h_kv, g=g, d=d, page=page, behind=math.inf, seed=44).check_attend(causal)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("h_kv,g,d,longest,causal", [(8, 4, 64, 900, True), (8, 2, 128, 1500, False), (16, 1, 64, 3000, True)])
 def test_single_tokens_in_wide_tables(dtype, h_kv, g, d, longest, causal):
@@ -528,6 +537,44 @@ def test_evict_ties_and_special_weights(kind):
          "near": 1.0 + torch.randint(0, 3, shape, generator=gen) * 2.0 ** -23}[kind]
     pos, seen = positions(s, gen)
     evict_both(s, 600, 3, 50, w, pos, seen)
+
+
+# more than 2048 keys that share their leading bits with the one looked for, and others
+@pytest.mark.parametrize("budget", [600, 3000, 4999, 8000])
+@pytest.mark.parametrize("kind", ["all equal", "zeros and ones", "near", "any"])
+def test_evict_ties_of_thousands(kind, budget):
+    s = Setup([8192, 5000, 2100], [1] * 3, h_kv=2, g=1, d=64, page=16, seed=50)
+    gen = torch.Generator().manual_seed(51)
+    shape = s.ref.k.shape[:3]
+    w = {"all equal": torch.full(shape, 0.25), "zeros and ones": (torch.rand(shape, generator=gen) < 0.4).float(),
+         "near": 1.0 + torch.randint(0, 2048, shape, generator=gen) * 2.0 ** -23, "any": torch.randn(shape, generator=gen).exp()}[kind]
+    pos, seen = positions(s, gen)
+    evict_both(s, budget, 3, 50, w, pos, seen)
+
+
+@pytest.mark.parametrize("longest", [700, 9000])                # both ways to select
+@pytest.mark.parametrize("bad", [-1, 1 << 30, None])
+def test_evict_with_a_bad_page_leaves_the_others_alone(longest, bad):
+    s = Setup([600, 500, longest], [1] * 3, h_kv=2, g=1, d=64, page=16, seed=52)
+    gen = torch.Generator().manual_seed(53)
+    w = torch.randn(s.ref.k.shape[:3], generator=gen).exp()
+    pos, seen = positions(s, gen)
+    mine = s.ref.table[0][s.ref.table[0] >= 0].long()
+    s.ref.weights, s.ref.pos, s.ref.seen = w, pos, seen
+    s.gpu.weights, s.gpu.pos, s.gpu.seen = w.to(DEV), pos.to(DEV), seen.to(DEV)
+    for i in (1, 7, 30, 37):                                    # before the budget, behind it, the last one
+        s.gpu.table[0, i] = s.ref.k.shape[0] if bad is None else bad
+    p = s.params()
+    ws = B.alloc_paged_workspace(p, DEV, evict=True)
+    ws.fill_(255)
+    B.dash_paged_evict(p, s.gpu, 300, ws, sinks=2, recent=20)
+    s.ref.lens[0] = 0                                           # the others by themselves
+    R.evict(s.ref, 300, 2, 20)
+    others = torch.ones(s.ref.k.shape[0], dtype=torch.bool)
+    others[mine] = False
+    assert s.gpu.lens.tolist() == [300, 300, 300]
+    for x, y in ((s.gpu.k, s.ref.k), (s.gpu.v, s.ref.v), (s.gpu.pos, s.ref.pos), (s.gpu.weights, s.ref.weights)):
+        assert torch.equal(x.cpu()[others], y[others])
 
 
 def test_evict_without_src_and_with_everything_protected():
