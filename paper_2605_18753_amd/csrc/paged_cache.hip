@@ -84,7 +84,8 @@ hipError_t launch_paged_append(const PagedArgs& a, int elem, int d, hipStream_t 
 // slots before it that were freed, both in ascending order: only those rows are read and written, and no source is a target.
 struct EvictArgs {
   PagedArgs a;
-  int budget, sinks, recent;
+  int budget, sinks, recent;   // the budget is at most cap
+  uint32_t src_len;    // slots of a pair in src: the caller's budget, which may be any
   int32_t* lens; int32_t* src;
   int32_t* moves;      // [pair][cap]: the targets from the front, the sources from the back
   int32_t* counts;     // [pair]
@@ -240,9 +241,9 @@ __global__ __launch_bounds__(kSelThreads) void paged_select_kernel(EvictArgs e) 
   for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
   if (tid < kRanked) rank[tid] = make_int2(0, 0);
   if (tid == 0) n_cand = 0;
-  int32_t* src = e.src ? e.src + (int64_t)pair * e.budget : nullptr;
+  int32_t* src = e.src ? e.src + (int64_t)pair * e.src_len : nullptr;
   if (src)
-    for (int i = tid; i < e.budget; i += kSelThreads) src[i] = i < left ? i : -1;   // the moves change theirs
+    for (uint32_t i = tid; i < e.src_len; i += kSelThreads) src[i] = i < (uint32_t)left ? (int)i : -1;   // the moves change theirs
   if (n <= e.budget) {
     if (tid == 0) e.counts[pair] = 0;
     return;
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(kChunkThreads) void paged_long_keys_kernel(EvictArg
       if (k.chunks == 0) e.counts[pair] = 0;
     }
     if (e.src)
-      for (int i = tid; i < e.budget; i += kChunkThreads) e.src[(int64_t)pair * e.budget + i] = i < k.n ? i : -1;   // the moves change theirs
+      for (uint32_t i = tid; i < e.src_len; i += kChunkThreads) e.src[(int64_t)pair * e.src_len + i] = i < (uint32_t)k.n ? (int)i : -1;   // the moves change theirs
   }
   if (k.len == 0) return;
   for (int i = tid; i < kBins; i += kChunkThreads) hist[i] = 0;
@@ -514,7 +515,7 @@ __global__ __launch_bounds__(256) void paged_move_kernel(EvictArgs e, int wgs) {
     const int pt = a.table[(int64_t)b * a.max_pages + (to >> a.page_log)], pf = paged_page_lane(a, b, from >> a.page_log);
     const bool ok = (uint32_t)pt < (uint32_t)a.n_pages && j0 + (lane & (MOVES - 1)) < n_moves;
     if (lane < MOVES && j0 + lane < n_moves) {
-      if (e.src) e.src[(int64_t)pair * e.budget + to] = from;
+      if (e.src) e.src[(int64_t)pair * e.src_len + to] = from;
       if (ok) {
         const int64_t x = (((int64_t)pt * a.h_kv + h) << a.page_log) + (to & pm), y = (((int64_t)pf * a.h_kv + h) << a.page_log) + (from & pm);
         const float w = a.weights[y];
@@ -572,7 +573,7 @@ size_t paged_evict_ws(const PagedArgs& a) {
 hipError_t launch_paged_evict(const PagedArgs& a, int elem, int d, int32_t* lens, int budget, int sinks, int recent, int32_t* src,
                               char* ws, hipStream_t st) {
   EvictArgs e;
-  e.a = a; e.budget = budget; e.sinks = sinks; e.recent = recent; e.lens = lens; e.src = src;
+  e.a = a; e.budget = budget < a.cap ? budget : a.cap; e.src_len = (uint32_t)budget; e.sinks = sinks; e.recent = recent; e.lens = lens; e.src = src;
   evict_scratch(e, a, ws);
   const size_t pairs = (size_t)a.batch * a.h_kv;
   if (a.cap <= kSelKeys) {

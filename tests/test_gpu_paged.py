@@ -577,6 +577,21 @@ def test_evict_with_a_bad_page_leaves_the_others_alone(longest, bad):
         assert torch.equal(x.cpu()[others], y[others])
 
 
+@pytest.mark.parametrize("n", [100, 9000])                      # both ways to select
+def test_evict_a_budget_near_the_largest_number(n):
+    # src has a slot for every token of the budget: 2^31 - 1 of them
+    s = Setup([n], [1], h_kv=1, g=1, d=64, page=16, seed=54)
+    s.gpu.weights, s.gpu.pos, s.gpu.seen = (torch.zeros(s.ref.k.shape[:3], dtype=t, device=DEV) for t in (F32, torch.int32, torch.int32))
+    s.gpu.seen = s.gpu.lens.clone()
+    p = s.params()
+    budget = (1 << 31) - 1
+    src = torch.full((1, 1, budget), 5, dtype=torch.int32, device=DEV)
+    B.dash_paged_evict(p, s.gpu, budget, B.alloc_paged_workspace(p, DEV, evict=True), src=src)
+    assert s.gpu.lens.item() == n and torch.equal(src[0, 0, :n].cpu(), torch.arange(n, dtype=torch.int32))
+    assert all(bool((x == -1).all()) for x in src[0, 0, n:].split(1 << 28))
+    assert torch.equal(s.gpu.k.cpu(), s.ref.k) and torch.equal(s.gpu.v.cpu(), s.ref.v)
+
+
 def test_evict_without_src_and_with_everything_protected():
     s = Setup([500], [1], h_kv=2, g=1, d=64, page=16, seed=44)
     gen = torch.Generator().manual_seed(45)
