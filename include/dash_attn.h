@@ -25,7 +25,8 @@
  *     Entry points may be called from several threads.  A workspace belongs to one call at a time: calls that are in
  *     flight together (several streams) need one each, or must not use it.  dash_stage2_attend of a bf16 prefill uses
  *     it for lists that are not given, and for parts where few rows meet a long cache.
- *     A call repeated on the same inputs gives the same bits, with two exceptions: fp32 gradients are added up in no fixed order, and
+ *     A call repeated on the same inputs gives the same bits, with three exceptions: fp32 gradients and the weights of pages that
+ *     sequences of a dash_paged_weigh call share are added up in no fixed order, and
  *     while more than 64 large bf16 prefills are in flight on a GPU, one may be given the bits of the other Stage-2 kernel.  Which of the two
  *     such a prefill takes depends on the lists of all its sequences and heads: the last bits of a sequence may change with those beside it.
  *   - Tensors are [batch, head, token, head_dim] with head_dim contiguous; the
@@ -313,7 +314,7 @@ int dash_kbar_summarize_backward(const dash_params* p, const void* k, const floa
  *             [0, max_pages*page_size] by the kernels
  *   row_start int32 [batch+1], ascending: the new tokens of sequence b are the packed rows row_start[b] ..
  *             row_start[b+1]-1 of q, o, k_new, v_new, in order, and its last tokens: the t-th of m sits at slot
- *             lens[b]-m+t.  A sequence may have none.  Rows of no sequence are neither read nor written.
+ *             lens[b]-m+t.  A sequence may have none.  Rows of no sequence are not written, and what they hold reaches nothing.
  *   weights   fp32, pos int32, both [n_pages, h_kv, page_size] contiguous: the attention weight every token
  *             has received and its position in the sequence.  Only evicting callers need them.
  * All of these are device pointers; nothing about the lengths is known to the host, so a captured graph

@@ -483,8 +483,8 @@ __global__ __launch_bounds__(512) void paged_few_f32_kernel(PagedArgs args) {
 // transposing reads, B = P): in the 32x32 accumulator layout lane (n = lane % 32, h = lane / 32) holds, for row n, keys 8 q + 4 h + i,
 // which are its slots of operand B once the contraction runs in that order, so nothing moves between the products.
 // A wave pipelines its tiles: the first product of tile i runs with the exponentials of tile i - 1, the second product of
-// tile i - 1 with the row maxima of tile i.  Bound by the matrix units at the power limit: 2048 tokens at the end of 32768, 32 / 8 heads of 128,
-// 980 to 1080 us from card to card, 1.0 to 1.09 PFLOP/s.
+// tile i - 1 with the row maxima of tile i.  Bound by the matrix units and the card's power: 2048 tokens at the end of 32768, 32 / 8 heads of 128,
+// 980 to 1080 us from card to card, 1.0 to 1.09 PFLOP/s, the matrix pipe busy for 0.58 of the clocks at 1.7 GHz.
 template <int D> struct RowsCfg {
   static constexpr int NCH = D / 8, ROW_BYTES = D * 2;
   static constexpr int TILE_BYTES = 64 * ROW_BYTES;
@@ -857,9 +857,10 @@ static int64_t most_items(const PagedArgs& a, int rows) {   // of a kv-head
 // n_rows h_q and batch h_kv allow).
 bool paged_attend_fits(const PagedArgs& a, int dtype) { return dtype != DASH_F32 || most_items(a, 16) * a.h_kv < (1 << 23); }
 // The kernel for a call: tiles of 128 rows where the sequences bring more than 16 rows each on the average, tiles of 16 otherwise.  (32 / 8 heads, tiles of 128
-// and of 16.  16 rows each: 64 sequences of 2000 tokens 99.6 and 97.7 us, one of 1000 14.7 and 11.0; 20 rows: 101 and 167, 8 of 16000 104 and 103; 48
+// and of 16, sequences with like numbers of rows.  16 rows each: 64 sequences of 2000 tokens 99.6 and 97.7 us, one of 1000 14.7 and 11.0; 20 rows: 101 and 167, 8 of 16000 104 and 103; 48
 // rows: 108 and 281.)  Short caches are read from the last-level cache again and again at no cost: tiles of 16 as long as each has a CU (one
-// of 1000 tokens, 64 rows 15.9 and 12.4 us, 128 17.3 and 11.8).
+// of 1000 tokens, 64 rows 15.9 and 12.4 us, 128 17.3 and 11.8).  The average hides a long piece beside many single tokens: 380 tokens of a sequence of 8000
+// beside 127 sequences of 200 with one each, 507 in all, take tiles of 16 and 458 us, 400 of them tiles of 128 and 147.
 static bool use_rows(const PagedArgs& a, int dtype) {
   return dtype == DASH_BF16 && (int64_t)a.n_rows * a.g > (int64_t)a.batch * 16 && !(a.cap <= 8 * kStep && most_items(a, 16) * a.h_kv <= 256);
 }

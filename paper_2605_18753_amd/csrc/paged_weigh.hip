@@ -425,9 +425,11 @@ __global__ __launch_bounds__(256, 4) void paged_weigh_stream_kernel(PagedArgs a)
 static int weigh_wgs(const PagedArgs& a, int dtype, int d) { return max(256 * ((d == 128 ? 3 : 4) - (dtype != DASH_BF16)) / a.h_kv, 1); }
 
 // K is streamed for sequences of up to 32 rows.  Which have more is known on the device only: calls that may have some, and bring no more than that on
-// the average, launch both kernels; a call of no more tokens than sequences launches the streaming one alone, which takes whatever there is.  (16
-// sequences of 2048 to 16384 tokens, 32 / 8 heads: 20 rows 78 us with both, not streamed 93; one of 400 new tokens beside 63 of one 190, not streamed
-// 230, only streamed 1984; three tokens of 8 sequences of 1000, where the second launch finds nothing, 18, only streamed 13.5.)
+// the average, launch both kernels; a call of no more tokens than sequences launches the streaming one alone, which takes whatever there is.  (32 / 8
+// heads of 128.  16 sequences of 2048 to 16384 tokens, 20 rows each: 76 us with both, not streamed 86, only streamed 73.  64 sequences of 2000 to 8000,
+// one with 400 new tokens, the others with one: 188, not streamed 228, only streamed 1969.  Three tokens of 8 sequences of 1000, where the second launch
+// finds nothing: 17, only streamed 13.  Nobody but one of the sequences with new tokens, and fewer of them than sequences, is what the rule does not see:
+// 64 of one of 64 sequences, 8000 long, 37, not streamed 22; 400 of one of 512, 195 and 56.)
 enum class Weigh { kStream, kBoth, kNone };
 static Weigh weigh_how(const PagedArgs& a) {
   const int64_t rows = (int64_t)a.n_rows * a.g;
