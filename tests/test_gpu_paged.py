@@ -254,6 +254,85 @@ def test_chunks_of_more_sequences_than_a_wave_has_lanes(dtype):
     check_weigh(s)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("page,d", [(512, 128), (1024, 64)])
+def test_large_pages(dtype, page, d):
+    for news in ([1, 1, 1, 1], [3, 70, 600, 0]):
+        s = Setup([page, 2 * page + 1, 1500, page - 1], news, d=d, page=page, dtype=dtype, behind=math.nan, seed=45)
+        s.check_attend()
+        check_weigh(s)
+    gen = torch.Generator().manual_seed(46)
+    pos, seen = positions(s, gen)
+    s = Setup([page, 2 * page + 1, 1500, page - 1], [1] * 4, d=d, page=page, g=1, dtype=dtype, seed=45)
+    evict_both(s, 700, 4, 30, torch.randn(s.ref.k.shape[:3], generator=gen).exp(), pos, seen)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("news,width", [([2, 1, 0], None), ([40, 17, 3], 128), ([100, 1, 2], 128)])
+def test_rows_before_the_first_sequence(dtype, news, width):
+    s = Setup([300, 41, 90], news, h_kv=2, g=4, dtype=dtype, page=32, spare=5, seed=47, width=width)
+    s.row_start += 5
+    s.start_gpu = s.row_start.to(DEV)
+    o, lse = s.attend()
+    want, wl, tol, ltol = R.attend(s.ref, s.q, s.row_start, 2)
+    assert (o[:5].float() == 77).all() and (lse[:5] == 77).all()
+    assert ((o[5:].double() - want[5:]).abs() <= tol[5:]).all() and ((lse[5:].double() - wl[5:]).abs() <= ltol[5:]).all()
+    lse[:5] = math.nan
+    s.q[:5] = math.nan
+    check_weigh(s, lse=lse)
+    new = torch.randn((2, s.rows, 2, 128)).to(dtype)
+    B.dash_paged_append(s.params(), s.gpu, new[0].to(DEV), new[1].to(DEV), s.start_gpu)
+    R.append(s.ref, new[0], new[1], s.row_start)
+    assert torch.equal(s.gpu.k.cpu(), s.ref.k) and torch.equal(s.gpu.v.cpu(), s.ref.v)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("width", [None, 128])
+def test_keys_and_values_in_layouts_of_their_own(dtype, width):
+    s = Setup([300, 41], [5, 30], h_kv=3, g=2, dtype=dtype, page=16, seed=48, width=width)
+    # keys token by token with a gap behind each, values head by head with gaps between the pages
+    k = torch.full((s.ref.k.shape[0], 16, 3, 128 + 8), math.nan, dtype=dtype, device=DEV)[..., :128].transpose(1, 2)
+    v = torch.full((s.ref.k.shape[0], 4, 16, 128), math.nan, dtype=dtype, device=DEV)[:, :3]
+    k.copy_(s.ref.k)
+    v.copy_(s.ref.v)
+    s.gpu.k, s.gpu.v = k, v
+    s.check_attend()
+    check_weigh(s)
+    new = torch.randn((2, s.rows, 3, 128)).to(dtype)
+    B.dash_paged_append(s.params(), s.gpu, new[0].to(DEV), new[1].to(DEV), s.start_gpu)
+    R.append(s.ref, new[0], new[1], s.row_start)
+    gen = torch.Generator().manual_seed(49)
+    pos, seen = positions(s, gen)
+    s.g = 1
+    evict_both(s, 100, 2, 10, torch.rand(s.ref.k.shape[:3], generator=gen), pos, seen)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("h_kv,lens,news", [(600, [70, 200], [1, 1]), (1030, [40], [33]), (300, [150, 20], [60, 3])])
+def test_more_heads_than_the_chip_has_places(dtype, h_kv, lens, news):
+    s = Setup(lens, news, h_kv=h_kv, g=1, d=64, dtype=dtype, page=16, seed=55)
+    s.check_attend()
+    check_weigh(s)
+    gen = torch.Generator().manual_seed(56)
+    pos, seen = positions(s, gen)
+    evict_both(s, 32, 2, 10, torch.rand(s.ref.k.shape[:3], generator=gen), pos, seen)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_thousands_of_sequences(dtype):
+    lens = [(29 * i) % 50 for i in range(3000)]
+    s = Setup(lens, [i % 3 if i % 11 else 0 for i in range(3000)], h_kv=1, g=2, d=64, dtype=dtype, page=16, seed=57)
+    s.check_attend()
+    check_weigh(s)
+    new = torch.randn((2, s.rows, 1, 64)).to(dtype)
+    B.dash_paged_append(s.params(), s.gpu, new[0].to(DEV), new[1].to(DEV), s.start_gpu)
+    R.append(s.ref, new[0], new[1], s.row_start)
+    gen = torch.Generator().manual_seed(58)
+    pos, seen = positions(s, gen)
+    s.g = 1
+    evict_both(s, 20, 2, 5, torch.rand(s.ref.k.shape[:3], generator=gen), pos, seen)
+
+
 def test_a_given_scale():
     s = Setup([200], [4], seed=10)
     s.check_attend(scale=0.3)
