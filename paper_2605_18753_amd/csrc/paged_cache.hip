@@ -9,7 +9,7 @@ namespace dash {
 // A wave writes a packed row: its keys and values of all kv-heads, 16 bytes a lane at a time.  Bound by HBM where there are many rows (each
 // byte is read once and written once), by the chain of dependent loads where there are few: what a row holds, and the starts,
 // lengths and positions of 64 sequences, are asked for together; only the page waits for them.  (2047 tokens of each of four sequences, 8 heads
-// of 128: 12.3 us, 5.5 TB/s; a token of 64: 4.4 us.)
+// of 128: 12.3 us, 5.5 TB/s; a token of 64: 4.1 us.)
 // A launch of 2^32 threads or more in a dimension loses some without an error: the workgroups lie in rows of 2^22.
 constexpr int kGridLog = 22;
 template <int ES, int D>   // bytes of an element
