@@ -10,7 +10,8 @@
  *   Stage 2  block-sparse softmax attention over the kept  (Sec. 3.3, Eq. 5-6 in the
  *            chunks with the bias added to the logits       bias form of Prop. 1; Alg. 3)
  *   plus a split-KV decode variant of Stage 2 (Sec. 3.5) and a dense reference
- *   attention (Eq. 1); and the calls of a paged cache for dense layers (dash_paged_*).
+ *   attention (Eq. 1); the calls of a paged cache for dense layers (dash_paged_*, in 4 bits
+ *   dash_paged4_*), and rotary positions (dash_rotary_*).
  *
  * Conventions shared by every entry point
  *   - Every tensor pointer is a DEVICE pointer owned by the caller.  The library
@@ -385,6 +386,103 @@ int dash_paged_weigh(const dash_paged_params* p, const void* q, const void* k_pa
 int dash_paged_evict(const dash_paged_params* p, void* k_pages, void* v_pages, int32_t* lens, const int32_t* seen,
                      const int32_t* table, float* weights, int32_t* pos, int32_t budget, int32_t sinks, int32_t recent,
                      int32_t* src, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- Rotary positions ---------------------------------------------------------------------
+ *
+ * The calls above take queries and keys as they are; in most models these carry their token's position as a rotation.
+ * Pair i of the first rot_dim elements of a head, (x, y), becomes mscale (x cos a - y sin a, x sin a + y cos a) with a = position * theta_i; the
+ * other elements stay.  A theta is held as the 64-bit fraction of a whole turn that it makes; position times that, modulo 2^64, is the angle's own
+ * fraction, off by at most |position| 2^-65 of a turn (4e-10 radians at 2^31).  cos and sin are evaluated in 64 bits.
+ * Limits (DASH_EUNSUPPORTED beyond them): head_dim 64 or 128; rot_dim a multiple of 16 up to head_dim. */
+enum { DASH_ROT_HALVES = 0,     /* pair i: elements i and i + rot_dim / 2 */
+       DASH_ROT_ADJACENT = 1 }; /* pair i: elements 2 i and 2 i + 1       */
+
+typedef struct dash_rotary {
+  int32_t rot_dim;         /* leading elements of a head that turn                           */
+  int32_t layout;          /* DASH_ROT_HALVES or DASH_ROT_ADJACENT                           */
+  float mscale;            /* factor on the elements that turn, > 0 (1: none)                */
+  int32_t reserved;        /* 0                                                              */
+  const uint64_t* turns;   /* DEVICE pointer to rot_dim / 2 numbers from dash_rotary_turns   */
+} dash_rotary;
+
+/* How the angles grow in contexts longer than those trained on. */
+enum { DASH_ROT_PLAIN = 0,   /* theta_i = base^(-2 i / rot_dim)                                                                     */
+       DASH_ROT_LINEAR = 1,  /* theta_i / factor                                                                                    */
+       DASH_ROT_BASE = 2,    /* base * factor^(rot_dim / (rot_dim - 2)) in place of base: the slowest pair is divided by factor, the fastest stays */
+       DASH_ROT_PARTS = 3 }; /* theta_i (c + (1 - c) / factor), c = (r - low) / (high - low) within 0 .. 1, r = original theta_i / (2 pi): turns
+                                that the pair makes over the context trained on.  Fast pairs stay, slow ones are divided by factor.   */
+
+/* Fills turns (HOST memory, rot_dim / 2 numbers, for the caller to copy to the device): round(theta_i / (2 pi) 2^64) modulo 2^64.
+ *   freq  HOST pointer to the thetas themselves, radians a token (finite, of any sign), where the caller has them: base and what follows are not
+ *         used then.  NULL: from base (> 0) and scaling; factor > 0 for all but DASH_ROT_PLAIN, original > 0 and low < high for DASH_ROT_PARTS.
+ * Host computation only; rot_dim a multiple of 16, 16 .. 128. */
+int dash_rotary_turns(int32_t rot_dim, const double* freq, int32_t scaling, double base, double factor, double original,
+                      double low, double high, uint64_t* turns);
+
+typedef struct dash_rotary_params {
+  int32_t batch;           /* >= 1                                                                              */
+  int32_t h_q, h_kv;       /* heads of q and of k (where one of them is NULL, its heads and tokens are not used) */
+  int32_t n_q, n_kv;       /* tokens of q and of k; query t has the position of token n_kv - n_q + t, as in the calls above (n_q > n_kv is
+                              refused); without k the position of token t                                        */
+  int32_t head_dim;        /* 64 or 128                                                                         */
+  int32_t dtype;           /* DASH_F32 or DASH_BF16                                                             */
+  int32_t inverse;         /* 1: turned by -a instead, times mscale: the gradient of the turned tensor becomes that of the tensor */
+  int32_t start;           /* added to every position                                                           */
+  int32_t reserved;        /* 0                                                                                 */
+  int64_t pos_stride;      /* of pos between sequences, in elements; 0: one row for all                         */
+  int64_t q_stride[3], q_out_stride[3];   /* batch, head, token strides, in elements; multiples of 16 bytes      */
+  int64_t k_stride[3], k_out_stride[3];
+} dash_rotary_params;
+
+/* Turns q, k or both.
+ *   q, q_out  [batch, h_q, n_q, d]; q_out may be q itself (with its strides), or must not overlap it
+ *   k, k_out  [batch, h_kv, n_kv, d], likewise
+ *   pos       int32 [batch, tokens] (tokens: n_kv, or n_q without k), device; NULL: token t has position t
+ * Positions (start added, modulo 2^32) are taken as signed 32-bit numbers.  batch * tokens below 2^31, heads of both together up to 2^16
+ * (DASH_EUNSUPPORTED). */
+int dash_rotary_apply(const dash_rotary_params* p, const dash_rotary* r, const int32_t* pos, const void* q, void* q_out,
+                      const void* k, void* k_out, void* stream);
+
+/* dash_paged_append with the new tokens' keys turned by their positions on the way, seen[b]-m+t or the slot (what goes into pos) as rotary positions.
+ *   q, q_out  optional (both or none) [n_rows, h_q, d]: the new tokens' queries, turned as well; strides q_stride and
+ *             o_stride of p.  q_out may be q.  Rows of no sequence, and of tokens without a slot (more new ones than lens), are not
+ *             written; those of tokens without a page are. */
+int dash_paged_append_rotary(const dash_paged_params* p, const dash_rotary* r, const void* q, void* q_out,
+                             const void* k_new, const void* v_new, void* k_pages, void* v_pages, const int32_t* row_start,
+                             const int32_t* lens, const int32_t* table, float* weights, int32_t* pos, const int32_t* seen, void* stream);
+
+/* ---- Paged cache in 4 bits -----------------------------------------------------------------
+ *
+ * The same cache in a little more than a quarter of the memory (68 bytes for a row of 128 numbers instead of 256), and of the time to read it.
+ * 32 numbers of a row share a power of two; each is a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 times it (E2M1 with E8M0 scales, as the
+ * hardware converts them).
+ *   k_codes, v_codes    uint8 [n_pages, h_kv, page_size, d / 2]: element 2 i in the low half of byte i; d / 2 contiguous, the other strides, in BYTES,
+ *                       are k_stride and v_stride of dash_paged_params (multiples of 16)
+ *   k_scales, v_scales  uint8 [n_pages, h_kv, page_size, d / 32] contiguous: e + 127; 255: the 32 numbers are NaN
+ * A row is held so: e = floor(log2 max|x|) - 2, one more where max|x| > 7.25 * 2^e (up to there the largest is held as 6, which costs less than the coarser
+ * steps would: root mean square 0.112 of normal numbers instead of 0.117 with a border of 6, 0.116 of 8), within -120 .. 125; then each
+ * number at the nearest level, the even code of two as near.  32 numbers among which one is NaN or infinite are held as NaN.
+ * Tables, lengths, row starts, limits and dtype (that of q, o and the new tokens) are those of dash_paged_params.  Attention gives what
+ * dash_paged_attend gives over pages of the same values; a NaN in the cache reaches the rows that see its token and no other.
+ * Scale bytes that an append does not write (0 .. 6 and 253, 254; 0 beside codes of 0 is a row of zeros) stand for what the hardware makes of them. */
+
+int dash_paged4_workspace_bytes(const dash_paged_params* p, size_t* out_bytes);
+
+/* As dash_paged_append and (r not NULL) dash_paged_append_rotary; keys are rounded once, to 4 bits, from their turned values.
+ * seen (optional) int32 [batch]: positions as there.  q, q_out: only with r. */
+int dash_paged4_append(const dash_paged_params* p, const dash_rotary* r, const void* q, void* q_out, const void* k_new,
+                       const void* v_new, void* k_codes, void* k_scales, void* v_codes, void* v_scales, const int32_t* row_start,
+                       const int32_t* lens, const int32_t* table, const int32_t* seen, void* stream);
+
+/* As dash_paged_attend. */
+int dash_paged4_attend(const dash_paged_params* p, const void* q, const void* k_codes, const void* k_scales, const void* v_codes,
+                       const void* v_scales, const int32_t* row_start, const int32_t* lens, const int32_t* table, void* o, float* lse,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* The cache's values as pages of the run dtype, for calls that read those: k_pages, v_pages [n_pages, h_kv, page_size, d] contiguous.  Every token of every
+ * page is written (rows that were never appended as their bytes say). */
+int dash_paged4_unpack(const dash_paged_params* p, const void* k_codes, const void* k_scales, const void* v_codes,
+                       const void* v_scales, void* k_pages, void* v_pages, void* stream);
 
 /* Static, NUL-terminated description of a dash_status. */
 const char* dash_strerror(int code);

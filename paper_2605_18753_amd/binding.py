@@ -46,10 +46,23 @@ class dash_paged_params(ctypes.Structure):
                                                       ("k_stride", 3), ("v_stride", 3))]
 
 
+class dash_rotary_plan(ctypes.Structure):                  # dash_rotary of the header
+    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("mscale", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("turns", ctypes.c_void_p)]
+
+
+class dash_rotary_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "h_q", "h_kv", "n_q", "n_kv", "head_dim", "dtype", "inverse", "start", "reserved")]
+    _fields_ += [("pos_stride", ctypes.c_int64)]
+    _fields_ += [(n, ctypes.c_int64 * 3) for n in ("q_stride", "q_out_stride", "k_stride", "k_out_stride")]
+
+
 _lib = None
 _P = ctypes.POINTER(dash_params)
 _PP = ctypes.POINTER(dash_paged_params)
+_PR = ctypes.POINTER(dash_rotary_plan)
 _V = ctypes.c_void_p
+_D = ctypes.c_double
 _I = ctypes.c_int32
 _SIGNATURES = {
     "dash_list_stride": (ctypes.c_int32, [_P]),
@@ -75,6 +88,13 @@ _SIGNATURES = {
     "dash_paged_attend": (ctypes.c_int, [_PP] + [_V] * 9 + [ctypes.c_size_t, _V]),
     "dash_paged_weigh": (ctypes.c_int, [_PP] + [_V] * 6 + [_I, _V, _V, ctypes.c_size_t, _V]),
     "dash_paged_evict": (ctypes.c_int, [_PP] + [_V] * 7 + [_I, _I, _I, _V, _V, ctypes.c_size_t, _V]),
+    "dash_rotary_turns": (ctypes.c_int, [_I, _V, _I, _D, _D, _D, _D, _D, _V]),
+    "dash_rotary_apply": (ctypes.c_int, [ctypes.POINTER(dash_rotary_params), _PR] + [_V] * 6),
+    "dash_paged_append_rotary": (ctypes.c_int, [_PP, _PR] + [_V] * 13),
+    "dash_paged4_workspace_bytes": (ctypes.c_int, [_PP, ctypes.POINTER(ctypes.c_size_t)]),
+    "dash_paged4_append": (ctypes.c_int, [_PP, _PR] + [_V] * 13),
+    "dash_paged4_attend": (ctypes.c_int, [_PP] + [_V] * 11 + [ctypes.c_size_t, _V]),
+    "dash_paged4_unpack": (ctypes.c_int, [_PP] + [_V] * 7),
     "dash_strerror": (ctypes.c_char_p, [ctypes.c_int]),
 }
 
@@ -481,3 +501,249 @@ def dash_paged_evict(p: dash_paged_params, cache: PagedCache, budget: int, ws: t
     _check(load_library().dash_paged_evict(p, cache.k.data_ptr(), cache.v.data_ptr(), cache.lens.data_ptr(), _ptr(cache.seen), cache.table.data_ptr(),
                                            _ptr(cache.weights), _ptr(cache.pos), budget, sinks, recent, _ptr(src), wp, wn, stream),
            "dash_paged_evict")
+
+
+# ---- rotary positions ------------------------------------------------------------------------------------------------
+_LAYOUTS = {"halves": 0, "adjacent": 1}
+_SCALINGS = {None: 0, "linear": 1, "base": 2, "parts": 3}
+
+
+class Rotary:
+    """How positions turn queries and keys (make_rotary): the plan that calls take, and the device's table that it points to."""
+
+    def __init__(self, plan: dash_rotary_plan, turns: torch.Tensor):
+        self.plan, self.turns = plan, turns
+
+
+def make_rotary(rot_dim: int, device, layout: str = "halves", base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                original: float = 0.0, low: float = 1.0, high: float = 4.0, mscale: float = 1.0, frequencies=None) -> Rotary:
+    """The first rot_dim elements of a head turn, pairs of elements half of them apart ("halves") or of neighbours ("adjacent").  scaling None, "linear",
+    "base" or "parts" with the numbers that the header's dash_rotary_turns takes; frequencies: rot_dim / 2 radians a token instead (a sequence or a
+    tensor), where the program has its own."""
+    if layout not in _LAYOUTS or scaling not in _SCALINGS:
+        raise DashError(f"layout: one of {list(_LAYOUTS)}; scaling: one of {list(_SCALINGS)}")
+    _int32(rot_dim=rot_dim)
+    if rot_dim < 1 or rot_dim > 128:
+        raise DashError("rot_dim: a multiple of 16, at most the head dimension")
+    freq = None
+    if frequencies is not None:
+        freq = torch.as_tensor(frequencies, dtype=torch.float64).cpu().contiguous()
+        if freq.shape != (rot_dim // 2,):
+            raise DashError(f"frequencies: {rot_dim // 2} numbers, one for each pair")
+    turns = torch.empty(rot_dim // 2, dtype=torch.int64)
+    _check(load_library().dash_rotary_turns(rot_dim, _ptr(freq), _SCALINGS[scaling], base, factor, original, low, high, turns.data_ptr()), "dash_rotary_turns")
+    turns = turns.to(device)
+    return Rotary(dash_rotary_plan(rot_dim, _LAYOUTS[layout], mscale, 0, turns.data_ptr()), turns)
+
+
+def _rotary_plan(r: Rotary, dev: int) -> dash_rotary_plan:
+    t, plan = r.turns, r.plan
+    if t.dtype is not torch.int64 or not t.is_contiguous() or t.numel() * 2 != plan.rot_dim or t.data_ptr() != plan.turns:
+        raise DashError("the plan's table is not the one it was made with (make_rotary)")
+    if t.get_device() != dev:
+        raise DashError("the rotary plan lies on the tensors' device")
+    return plan
+
+
+def _gpu_stream(dev: int):
+    if dev < 0:
+        raise DashError("the tensors lie on a GPU")
+    if _device is None or _raw_stream is None or not torch.cuda.is_initialized():
+        return _stream()
+    if dev != _device():
+        raise DashError(f"the tensors lie on cuda:{dev}, which is not the current device")
+    return _raw_stream(dev)
+
+
+def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
+    span = lambda t: (t.data_ptr(), t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))))  # noqa: E731
+    (a0, a1), (b0, b1) = span(a), span(b)
+    return a0 < b1 and b0 < a1
+
+
+def dash_rotary(r: Rotary, q, q_out, k=None, k_out=None, pos=None, start: int = 0, inverse: bool = False) -> None:
+    """q, q_out [batch, h_q, n_q, d] and k, k_out [batch, h_kv, n_kv, d], each pair None or given; an output may be its input.  pos int32 [tokens] or
+    [batch, tokens] (tokens: n_kv, or n_q without k; query t has the position of token n_kv - n_q + t), None: token t has position t.  inverse: turns
+    back, which takes the gradient of an output to that of its input."""
+    pairs = [(x, y, name) for x, y, name in ((q, q_out, "q"), (k, k_out, "k")) if x is not None or y is not None]
+    if not pairs:
+        raise DashError("dash_rotary: q, k or both")
+    lead = pairs[0][0]
+    p = dash_rotary_params()
+    for x, y, name in pairs:
+        if x is None or y is None or x.dim() != 4 or y.shape != x.shape or x.dtype is not lead.dtype or y.dtype is not x.dtype or x.dtype not in _PAGED_TYPES:
+            raise DashError("rotary tensors: input and output [batch, heads, tokens, head_dim] of one type, bf16 or fp32")
+        if x.shape[0] != lead.shape[0] or x.shape[3] != lead.shape[3] or 0 in x.shape:
+            raise DashError("q and k have the same batch and head dimension, and no size is 0")
+        if x.stride(3) != 1 or y.stride(3) != 1:
+            raise DashError("head_dim must be contiguous")
+        if x.get_device() != lead.get_device() or y.get_device() != lead.get_device():
+            raise DashError("the tensors lie on one device")
+        if any(n > 1 and s == 0 for n, s in zip(y.shape, y.stride())):
+            raise DashError("an output has an element for each of its own")
+        if not (x.data_ptr() == y.data_ptr() and x.stride() == y.stride()) and _overlap(x, y):
+            raise DashError("an output is its input or does not overlap it")
+        getattr(p, f"{name}_stride")[:], getattr(p, f"{name}_out_stride")[:] = x.stride()[:3], y.stride()[:3]
+    if len(pairs) == 2 and (_overlap(q_out, k_out) or _overlap(q_out, k) or _overlap(k_out, q)) and not _interleaved(pairs):
+        raise DashError("the outputs overlap neither each other nor the other's input")
+    _int32(start=start)
+    p.batch, p.head_dim = lead.shape[0], lead.shape[3]
+    p.dtype, p.inverse, p.start = _PAGED_TYPES[lead.dtype], int(inverse), start
+    if q is not None:
+        p.h_q, p.n_q = q.shape[1], q.shape[2]
+    if k is not None:
+        p.h_kv, p.n_kv = k.shape[1], k.shape[2]
+    dev = lead.get_device()
+    if pos is not None:
+        tokens = (k if k is not None else q).shape[2]
+        if pos.dtype is not _INT or tuple(pos.shape) not in ((tokens,), (p.batch, tokens)) or (tokens > 1 and pos.stride(-1) != 1) or pos.get_device() != dev:
+            raise DashError("pos: int32 [tokens] or [batch, tokens], tokens contiguous, on the tensors' device")
+        p.pos_stride = pos.stride(0) if pos.dim() == 2 and p.batch > 1 else 0
+    plan, stream = _rotary_plan(r, dev), _gpu_stream(dev)
+    _check(load_library().dash_rotary_apply(p, plan, _ptr(pos), _ptr(q), _ptr(q_out), _ptr(k), _ptr(k_out), stream), "dash_rotary_apply")
+
+
+def _interleaved(pairs) -> bool:
+    """Whether q and k are heads of one tensor (their memory interleaved): the same strides, and starts within one token's row."""
+    (q, q_out, _), (k, k_out, _) = pairs
+    def apart(a, b):
+        if a.stride() != b.stride():
+            return False
+        first, then = (a, b) if a.data_ptr() <= b.data_ptr() else (b, a)
+        off = (then.data_ptr() - first.data_ptr()) // a.element_size()
+        s, heads = a.stride(), first.shape[1]
+        return (heads - 1) * s[1] + a.shape[3] <= off and off + (then.shape[1] - 1) * s[1] + a.shape[3] <= s[2]
+    return all(not _overlap(a, b) or apart(a, b) for a, b in ((q_out, k_out), (q_out, k), (k_out, q)))
+
+
+def dash_paged_append_rotary(p: dash_paged_params, cache: PagedCache, rotary: Rotary, k_new, v_new, row_start, q=None, q_out=None) -> None:
+    """dash_paged_append with the keys turned by their positions (cache.seen, or their slots); q, q_out [n_rows, h_q, d] (both or none): the tokens'
+    queries, turned as well; q_out may be q."""
+    layout = _paged_layout(cache, cache.weights, cache.pos, cache.seen)
+    plan = _rotary_plan(rotary, layout[0])
+    p, stream = _paged_call(p, layout, row_start, _fresh_rows(p, k_new, v_new, q, q_out))
+    _check(load_library().dash_paged_append_rotary(p, plan, _ptr(q), _ptr(q_out), k_new.data_ptr(), v_new.data_ptr(), cache.k.data_ptr(), cache.v.data_ptr(),
+                                                   row_start.data_ptr(), cache.lens.data_ptr(), cache.table.data_ptr(), _ptr(cache.weights),
+                                                   _ptr(cache.pos), _ptr(cache.seen), stream), "dash_paged_append_rotary")
+
+
+def _fresh_rows(p, k_new, v_new, q, q_out):
+    rows = ((k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride"))
+    if (q is None) != (q_out is None):
+        raise DashError("q and q_out: both or none")
+    if q is None:
+        return rows
+    if not (q.data_ptr() == q_out.data_ptr() and q.stride() == q_out.stride()) and _overlap(q, q_out):
+        raise DashError("q_out is q or does not overlap it")
+    return rows + ((q, p.h_q, "q_stride"), (q_out, p.h_q, "o_stride"))
+
+
+# ---- paged cache in 4 bits -------------------------------------------------------------------------------------------
+@dataclass
+class PagedCache4:
+    """A paged cache whose keys and values are held in 4 bits (see the header): codes uint8 [n_pages, h_kv, page_size, d / 2], scales uint8
+    [n_pages, h_kv, page_size, d / 32]; table, lens and seen as in PagedCache.  Every call checks those that it uses."""
+    k_codes: torch.Tensor
+    k_scales: torch.Tensor
+    v_codes: torch.Tensor
+    v_scales: torch.Tensor
+    table: torch.Tensor
+    lens: torch.Tensor
+    seen: Optional[torch.Tensor] = None
+
+    @staticmethod
+    def allocate(batch: int, h_kv: int, n_pages: int, page_size: int, head_dim: int, max_pages: int, device) -> "PagedCache4":
+        """An empty cache without pages (table entries -1)."""
+        whole = lambda *s: torch.zeros(s, dtype=torch.int32, device=device)  # noqa: E731
+        byte = lambda n: torch.zeros((n_pages, h_kv, page_size, n), dtype=torch.uint8, device=device)  # noqa: E731
+        return PagedCache4(byte(head_dim // 2), byte(head_dim // 32), byte(head_dim // 2), byte(head_dim // 32), whole(batch, max_pages).fill_(-1), whole(batch))
+
+
+def _paged4_layout(c: PagedCache4, dtype, seen=None) -> tuple:
+    """As _paged_layout; dtype: the packed rows'."""
+    k, v, ks, vs, t, lens = c.k_codes, c.v_codes, c.k_scales, c.v_scales, c.table, c.lens
+    shape, dev = tuple(k.shape), k.get_device()
+    if len(shape) != 4 or v.shape != shape or k.dtype is not torch.uint8 or v.dtype is not torch.uint8:
+        raise DashError("k and v codes: two uint8 tensors [n_pages, h_kv, page_size, d / 2]")
+    n_pages, h_kv, page_size, half = shape
+    kp, kh, kt, k1 = k.stride()
+    vp, vh, vt, v1 = v.stride()
+    if k1 != 1 or v1 != 1:
+        raise DashError("k and v codes: the last dimension must be contiguous")
+    scales = (n_pages, h_kv, page_size, half // 16)
+    for s in (ks, vs):
+        if s.dtype is not torch.uint8 or s.shape != scales or not s.is_contiguous():
+            raise DashError("k and v scales: contiguous uint8 tensors [n_pages, h_kv, page_size, d / 32]")
+    if t.dtype is not _INT or t.dim() != 2 or not t.is_contiguous():
+        raise DashError("table [batch, max_pages]: a contiguous int32 tensor")
+    batch, max_pages = t.shape
+    for x in (lens, seen):
+        if x is not None and (x.dtype is not _INT or x.shape != (batch,) or not x.is_contiguous()):
+            raise DashError("lens and seen: contiguous int32 tensors [batch]")
+    if lens is None or any(x is not None and x.get_device() != dev for x in (v, ks, vs, t, lens, seen)):
+        raise DashError("the cache's tensors lie on one device")
+    return dev, dtype, (batch, h_kv, 2 * half, _PAGED_TYPES[dtype], page_size, n_pages, max_pages, kp, kh, kt, vp, vh, vt)
+
+
+def make_paged4_params(cache: PagedCache4, n_rows: int, h_q: int, dtype=torch.bfloat16, causal: bool = True, scale: float = 0.0) -> dash_paged_params:
+    """As make_paged_params; dtype: that of q, o and the new tokens (bf16 or fp32)."""
+    if dtype not in _PAGED_TYPES:
+        raise DashError("dtype: bf16 or fp32")
+    _, _, (batch, h_kv, d, code, page_size, n_pages, max_pages, *strides) = _paged4_layout(cache, dtype, cache.seen)
+    _int32(n_rows=n_rows, h_q=h_q)
+    p = dash_paged_params()
+    p.batch, p.max_pages, p.n_pages, p.h_kv, p.page_size, p.head_dim = batch, max_pages, n_pages, h_kv, page_size, d
+    p.h_q, p.n_rows, p.causal, p.scale, p.dtype = h_q, n_rows, int(causal), scale, code
+    p.k_stride[:], p.v_stride[:] = strides[:3], strides[3:]
+    return p
+
+
+_ROW_TYPES = {code: t for t, code in _PAGED_TYPES.items()}
+
+
+def _row_type(p: dash_paged_params):
+    if p.dtype not in _ROW_TYPES:
+        raise DashError("the parameters' dtype: bf16 or fp32 (make_paged4_params)")
+    return _ROW_TYPES[p.dtype]
+
+
+def alloc_paged4_workspace(p: dash_paged_params, device) -> torch.Tensor:
+    """Scratch of dash_paged4_attend."""
+    n = ctypes.c_size_t(0)
+    _check(load_library().dash_paged4_workspace_bytes(ctypes.byref(p), ctypes.byref(n)), "dash_paged4_workspace_bytes")
+    return torch.empty(n.value + 256, dtype=torch.uint8, device=device)
+
+
+def dash_paged4_append(p: dash_paged_params, cache: PagedCache4, k_new, v_new, row_start, rotary: Optional[Rotary] = None, q=None, q_out=None) -> None:
+    """k_new, v_new [n_rows, h_kv, d]; with a rotary plan the keys are turned by their positions, and q into q_out (both or none; q_out may be q)."""
+    if rotary is None and (q is not None or q_out is not None):
+        raise DashError("q and q_out: only with a rotary plan")
+    layout = _paged4_layout(cache, _row_type(p), cache.seen)
+    plan = None if rotary is None else _rotary_plan(rotary, layout[0])
+    p, stream = _paged_call(p, layout, row_start, _fresh_rows(p, k_new, v_new, q, q_out))
+    _check(load_library().dash_paged4_append(p, plan, _ptr(q), _ptr(q_out), k_new.data_ptr(), v_new.data_ptr(), cache.k_codes.data_ptr(),
+                                             cache.k_scales.data_ptr(), cache.v_codes.data_ptr(), cache.v_scales.data_ptr(), row_start.data_ptr(),
+                                             cache.lens.data_ptr(), cache.table.data_ptr(), _ptr(cache.seen), stream), "dash_paged4_append")
+
+
+def dash_paged4_attend(p: dash_paged_params, cache: PagedCache4, q, row_start, o, ws: torch.Tensor, lse=None) -> None:
+    """q, o [n_rows, h_q, d]; lse fp32 [n_rows, h_q] or None."""
+    p, stream = _paged_call(p, _paged4_layout(cache, _row_type(p)), row_start, ((q, p.h_q, "q_stride"), (o, p.h_q, "o_stride")),
+                            (lse, _FLOAT, (p.n_rows, p.h_q)), ws)
+    wp, wn = _ws_ptr(ws)
+    _check(load_library().dash_paged4_attend(p, q.data_ptr(), cache.k_codes.data_ptr(), cache.k_scales.data_ptr(), cache.v_codes.data_ptr(),
+                                             cache.v_scales.data_ptr(), row_start.data_ptr(), cache.lens.data_ptr(), cache.table.data_ptr(),
+                                             o.data_ptr(), _ptr(lse), wp, wn, stream), "dash_paged4_attend")
+
+
+def dash_paged4_unpack(p: dash_paged_params, cache: PagedCache4, k_pages, v_pages) -> None:
+    """The cache's values as pages [n_pages, h_kv, page_size, d] of the parameters' type, contiguous."""
+    dtype = _row_type(p)
+    layout = _paged4_layout(cache, dtype)
+    shape = (p.n_pages, p.h_kv, p.page_size, p.head_dim)
+    for x in (k_pages, v_pages):
+        if x.dtype is not dtype or x.shape != shape or not x.is_contiguous() or x.get_device() != layout[0]:
+            raise DashError(f"pages: contiguous tensors {shape} of the parameters' type on the cache's device")
+    p, stream = _paged_call(p, layout, None, ())
+    _check(load_library().dash_paged4_unpack(p, cache.k_codes.data_ptr(), cache.k_scales.data_ptr(), cache.v_codes.data_ptr(), cache.v_scales.data_ptr(),
+                                             k_pages.data_ptr(), v_pages.data_ptr(), stream), "dash_paged4_unpack")

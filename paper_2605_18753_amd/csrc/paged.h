@@ -35,6 +35,7 @@ struct PagedArgs {
   int whole;                             // runs: items may be left uncut; weights: two kernels share the sequences
   int slots; float gain;                 // tiles of 128 rows: workgroups of a kv-head that are resident at once; what finer parts must come to
   float* part_o; float* part_ml;         // records of cut items: two of each run (the item it begins in, the one it ends in), one of each part
+  const uint8_t* k_sc; const uint8_t* v_sc;   // a cache in 4 bits: its scales (k and v its codes, their strides in bytes)
   uint64_t* flags; uint64_t nonce;       // runs: two of each record, and the number that says that it is complete
 };
 
@@ -66,6 +67,30 @@ __device__ __forceinline__ int paged_page(const PagedArgs& a, int b, int i) { re
 // the same for an index of the lane's own
 __device__ __forceinline__ int paged_page_lane(const PagedArgs& a, int b, int i) {
   return paged_clamp(a, a.table[(int64_t)b * a.max_pages + min(i, a.max_pages - 1)]);
+}
+
+// Where a packed row of a call that appends goes, for a wave's lanes together: sequence, slot and position (that of its
+// token in its sequence); false: nowhere.  Starts, lengths and positions of 64 sequences are asked for together.
+struct PagedPlace { int b, slot, position; };
+__device__ __forceinline__ bool paged_place(const PagedArgs& a, int row, PagedPlace& at) {
+  const int lane = lane_id();
+  int b = -1, end = 0, n = 0, seen = 0;
+  for (int i0 = 0; i0 < a.batch && b < 0; i0 += 64) {        // as many sequences end at or before the row
+    const int i = min(i0 + lane, a.batch - 1);
+    const int s0 = a.row_start[i], s1 = a.row_start[i + 1], len = a.lens[i], sn = a.seen ? a.seen[i] : 0;
+    const uint64_t on = __ballot(i0 + lane < a.batch && s1 > row);
+    if (on) {
+      const int l = __builtin_ctzll(on);
+      if (__builtin_amdgcn_readlane(s0, l) > row) return false;   // a row of no sequence
+      b = i0 + l;
+      end = min(__builtin_amdgcn_readlane(s1, l), a.n_rows);
+      n = min(max(__builtin_amdgcn_readlane(len, l), 0), a.cap);
+      seen = a.seen ? __builtin_amdgcn_readlane(sn, l) : n;
+    }
+  }
+  const int back = end - row;                                // 1 for the newest token
+  at = {b, n - back, seen - back};
+  return b >= 0 && n >= back;
 }
 
 // ---- parts (tiles of 128 rows) ----------------------------------------------------------------------------------------
@@ -299,6 +324,13 @@ hipError_t launch_paged_attend(const PagedArgs& a, int dtype, int d, char* ws, h
 hipError_t launch_paged_weigh(const PagedArgs& a, int dtype, int d, char* ws, hipStream_t st);
 hipError_t launch_paged_evict(const PagedArgs& a, int elem, int d, int32_t* lens, int budget, int sinks, int recent, int32_t* src,
                               char* ws, hipStream_t st);
+struct RotaryArgs;
+hipError_t launch_paged_append_rotary(const PagedArgs& a, const RotaryArgs& r, int elem, int d, hipStream_t st);
+hipError_t launch_paged4_append(const PagedArgs& a, const RotaryArgs* r, int elem, int d, hipStream_t st);   // r: null without rotation
+hipError_t launch_paged4_unpack(const PagedArgs& a, void* k_pages, void* v_pages, int elem, int d, hipStream_t st);
+hipError_t launch_paged4_attend(const PagedArgs& a, int dtype, int d, char* ws, hipStream_t st);
+bool paged4_attend_fits(const PagedArgs& a, int dtype);
+size_t paged4_attend_ws(const PagedArgs& a, int dtype, int d);
 bool paged_attend_fits(const PagedArgs& a, int dtype);
 size_t paged_attend_ws(const PagedArgs& a, int dtype, int d);
 size_t paged_weigh_ws(const PagedArgs& a, int dtype, int d);

@@ -30,23 +30,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedArgs a) {
     }
   };
   load(lane);
-  // the sequence that the row belongs to: as many as end at or before it
-  int b = -1, end = 0, n = 0, seen = 0;
-  for (int i0 = 0; i0 < a.batch && b < 0; i0 += 64) {
-    const int i = min(i0 + lane, a.batch - 1);
-    const int s0 = a.row_start[i], s1 = a.row_start[i + 1], len = a.lens[i], sn = a.seen ? a.seen[i] : 0;
-    const uint64_t on = __ballot(i0 + lane < a.batch && s1 > row);
-    if (on) {
-      const int l = __builtin_ctzll(on);
-      if (__builtin_amdgcn_readlane(s0, l) > row) return;    // a row of no sequence
-      b = i0 + l;
-      end = min(__builtin_amdgcn_readlane(s1, l), a.n_rows);
-      n = min(max(__builtin_amdgcn_readlane(len, l), 0), a.cap);
-      seen = a.seen ? __builtin_amdgcn_readlane(sn, l) : n;
-    }
-  }
-  const int back = end - row, slot = n - back;               // back: 1 for the newest token
-  if (b < 0 || slot < 0) return;
+  PagedPlace at_row;
+  if (!paged_place(a, row, at_row)) return;
+  const auto [b, slot, position] = at_row;
   const uint32_t page = (uint32_t)paged_entry(a, b, slot >> a.page_log);
   if (page >= (uint32_t)a.n_pages) return;                   // no page: nothing is written
   const int off = slot & ((1 << a.page_log) - 1);
@@ -64,7 +50,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(PagedArgs a) {
   for (int h = lane; h < a.h_kv; h += 64) {
     const int64_t at = (((int64_t)page * a.h_kv + h) << a.page_log) + off;
     if (a.weights) a.weights[at] = 0.f;
-    if (a.pos) a.pos[at] = seen - back;
+    if (a.pos) a.pos[at] = position;
   }
 }
 

@@ -1,0 +1,159 @@
+// Rotary positions of queries and keys, and their inverse for gradients.  C ABI: dash_rotary_turns, dash_rotary_apply.
+#include <math.h>
+
+#include "rotary.h"
+
+namespace dash {
+
+struct RotateArgs {
+  RotaryArgs r;
+  const void* x[2];  void* y[2];         // queries, keys
+  const int32_t* pos;
+  int64_t pos_b, x_b[2], x_h[2], x_t[2], y_b[2], y_h[2], y_t[2];
+  int heads[2], n[2];                    // n: tokens; those of tensor 0 are the last ones
+  int tokens, start, inverse;
+  uint32_t all;                          // batch * tokens, below 2^31
+};
+
+// HBM bounds it where there are many tokens: every byte is read once and written once.  A workgroup has TOK tokens of a sequence: cosines and sines of
+// their pairs are worked out once, into LDS; a thread keeps those of its unit (a token's 8 pairs) and walks heads.
+constexpr int kTok = 8;
+template <typename T, int D>
+__global__ __launch_bounds__(256) void rotary_kernel(RotateArgs a) {
+  constexpr int UNITS = D / 16, SLOTS = 256 / (UNITS * kTok);                  // heads at a time
+  __shared__ float2 cs[kTok][D / 2];
+  const int u = threadIdx.x % UNITS, t = threadIdx.x / UNITS % kTok, slot = threadIdx.x / (UNITS * kTok);
+  const bool turns = 8 * u < a.r.half;
+  const int2 at = rotary_unit(a.r, u);
+  // a.all tokens of all sequences, one after the other
+  for (uint32_t f0 = blockIdx.x * kTok; f0 < a.all; f0 += gridDim.x * kTok) {
+    for (int i = threadIdx.x; i < kTok * a.r.half; i += 256) {
+      const int ti = i / a.r.half, k = i - ti * a.r.half;
+      const uint32_t f = min(f0 + ti, a.all - 1), b = f / (uint32_t)a.tokens, j = f - b * a.tokens;
+      const double2 v = rotary_cos_sin(a.r, k, (int)((a.pos ? (uint32_t)a.pos[b * a.pos_b + j] : j) + (uint32_t)a.start));
+      cs[ti][k] = make_float2((float)v.x, (float)(a.inverse ? -v.y : v.y));
+    }
+    __syncthreads();
+    const uint32_t f = f0 + t, b = f / (uint32_t)a.tokens;
+    const int j = (int)(f - b * a.tokens);
+    float2 my[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) my[i] = turns ? cs[t][8 * u + i] : make_float2(1.f, 0.f);
+    __syncthreads();
+    if (f >= a.all) break;                                     // the last round: nobody waits any more
+    for (int x = 0; x < 2; x++) {
+      const int tok = j - (a.tokens - a.n[x]);
+      if (!a.x[x] || tok < 0 || (a.x[x] == a.y[x] && !turns)) continue;
+      const T* from = (const T*)a.x[x] + b * a.x_b[x] + tok * a.x_t[x];
+      T* to = (T*)a.y[x] + b * a.y_b[x] + tok * a.y_t[x];
+      for (int h = slot + (int)blockIdx.y * SLOTS; h < a.heads[x]; h += SLOTS * (int)gridDim.y) {
+        Eight p = load_eight(from + h * a.x_h[x] + at.x), q = load_eight(from + h * a.x_h[x] + at.y);
+        if (turns) turn_unit(p, q, my, a.r.adjacent);
+        store_eight(to + h * a.y_h[x] + at.x, p);
+        store_eight(to + h * a.y_h[x] + at.y, q);
+      }
+    }
+  }
+}
+
+template <typename T, int D> static hipError_t launch_rotary(const RotateArgs& a, hipStream_t st) {
+  constexpr int SLOTS = 256 / (D / 16 * kTok);
+  const int heads = a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1];
+  const uint32_t groups = (a.all + kTok - 1) / kTok, most = 1u << 20;
+  // few tokens: the heads of a token go to several workgroups, each of which works out the cosines and sines
+  const uint32_t split = groups >= 1024 ? 1 : (1024 + groups - 1) / groups, turns = (uint32_t)(heads + SLOTS - 1) / SLOTS;
+  hipLaunchKernelGGL((rotary_kernel<T, D>), dim3(groups < most ? groups : most, split < turns ? split : turns), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+int rotary_args(const dash_rotary* r, int head_dim, RotaryArgs* out) {
+  if (!r || !r->turns || r->reserved != 0 || ((uintptr_t)r->turns & 7) != 0) return DASH_EINVAL;
+  if (r->layout != DASH_ROT_HALVES && r->layout != DASH_ROT_ADJACENT) return DASH_EINVAL;
+  if (r->rot_dim < 1 || r->rot_dim > head_dim || !(r->mscale > 0.f) || !isfinite(r->mscale)) return DASH_EINVAL;
+  if (r->rot_dim % 16 != 0) return DASH_EUNSUPPORTED;
+  *out = {r->turns, r->rot_dim / 2, r->layout == DASH_ROT_ADJACENT, (double)r->mscale};
+  return DASH_OK;
+}
+
+}  // namespace dash
+
+using namespace dash;
+
+extern "C" {
+
+int dash_rotary_turns(int32_t rot_dim, const double* freq, int32_t scaling, double base, double factor, double original,
+                      double low, double high, uint64_t* turns) {
+  if (!turns || rot_dim < 16 || rot_dim > 128 || rot_dim % 16 != 0) return DASH_EINVAL;
+  const auto positive = [](double x) { return isfinite(x) && x > 0.0; };
+  if (!freq) {
+    if (scaling < DASH_ROT_PLAIN || scaling > DASH_ROT_PARTS || !positive(base)) return DASH_EINVAL;
+    if (scaling != DASH_ROT_PLAIN && !positive(factor)) return DASH_EINVAL;
+    if (scaling == DASH_ROT_PARTS && (!positive(original) || !isfinite(low) || !isfinite(high) || !(low < high))) return DASH_EINVAL;
+  } else {
+    for (int i = 0; i < rot_dim / 2; i++)
+      if (!isfinite(freq[i])) return DASH_EINVAL;
+  }
+  // long double: 64 bits of a theta, as many as the fraction has
+  const long double two_pi = 6.283185307179586476925286766559005768L;
+  uint64_t out[64];
+  for (int i = 0; i < rot_dim / 2; i++) {
+    long double theta;
+    if (freq) {
+      theta = freq[i];
+    } else {
+      long double b = base;
+      if (scaling == DASH_ROT_BASE) b *= powl((long double)factor, (long double)rot_dim / (rot_dim - 2));
+      theta = powl(b, -2.0L * i / rot_dim);
+      if (scaling == DASH_ROT_LINEAR) theta /= factor;
+      if (scaling == DASH_ROT_PARTS) {
+        const long double turned = original * theta / two_pi;
+        const long double c = fminl(fmaxl((turned - low) / ((long double)high - low), 0.0L), 1.0L);
+        theta *= c + (1.0L - c) / factor;
+      }
+      if (!isfinite(theta)) return DASH_EINVAL;
+    }
+    long double x = fabsl(theta) / two_pi;
+    x -= floorl(x);                                           // within 0 .. 1: whole turns do nothing
+    const long double y = roundl(x * 18446744073709551616.0L);
+    out[i] = y >= 18446744073709551616.0L ? 0 : (uint64_t)y;
+    if (theta < 0) out[i] = 0 - out[i];
+  }
+  for (int i = 0; i < rot_dim / 2; i++) turns[i] = out[i];
+  return DASH_OK;
+}
+
+int dash_rotary_apply(const dash_rotary_params* p, const dash_rotary* r, const int32_t* pos, const void* q, void* q_out,
+                      const void* k, void* k_out, void* stream) {
+  if (!p || (!q && !k) || !q != !q_out || !k != !k_out) return DASH_EINVAL;
+  if (p->batch < 1 || p->head_dim < 1 || (q && (p->h_q < 1 || p->n_q < 1)) || (k && (p->h_kv < 1 || p->n_kv < 1))) return DASH_EINVAL;
+  if (p->dtype != DASH_F32 && p->dtype != DASH_BF16) return DASH_EINVAL;
+  if ((p->inverse != 0 && p->inverse != 1) || p->reserved != 0 || p->pos_stride < 0 || (q && k && p->n_q > p->n_kv)) return DASH_EINVAL;
+  if (p->head_dim != 64 && p->head_dim != 128) return DASH_EUNSUPPORTED;
+  RotateArgs a = {};
+  if (const int rc = rotary_args(r, p->head_dim, &a.r); rc != DASH_OK) return rc;
+  a.x[0] = q; a.x[1] = k; a.y[0] = q_out; a.y[1] = k_out;
+  const int64_t* strides[2][2] = {{p->q_stride, p->q_out_stride}, {p->k_stride, p->k_out_stride}};
+  const int vec = p->dtype == DASH_BF16 ? 8 : 4;
+  for (int x = 0; x < 2; x++) {
+    if (!a.x[x]) continue;
+    if ((((uintptr_t)a.x[x] | (uintptr_t)a.y[x]) & 15) != 0) return DASH_EINVAL;
+    for (int i = 0; i < 3; i++)
+      if (strides[x][0][i] < 0 || strides[x][1][i] < 0 || strides[x][0][i] % vec != 0 || strides[x][1][i] % vec != 0 ||
+          (a.x[x] == a.y[x] && strides[x][0][i] != strides[x][1][i])) return DASH_EINVAL;
+    a.x_b[x] = strides[x][0][0]; a.x_h[x] = strides[x][0][1]; a.x_t[x] = strides[x][0][2];
+    a.y_b[x] = strides[x][1][0]; a.y_h[x] = strides[x][1][1]; a.y_t[x] = strides[x][1][2];
+    a.heads[x] = x ? p->h_kv : p->h_q;
+    a.n[x] = x ? p->n_kv : p->n_q;
+  }
+  a.tokens = k ? p->n_kv : p->n_q;
+  if ((int64_t)p->batch * a.tokens >= (int64_t)1 << 31 || (int64_t)a.heads[0] + a.heads[1] > 1 << 16) return DASH_EUNSUPPORTED;
+  a.pos = pos; a.pos_b = p->pos_stride; a.start = p->start; a.inverse = p->inverse;
+  a.all = (uint32_t)(p->batch * (int64_t)a.tokens);
+  const hipStream_t st = (hipStream_t)stream;
+  const bool bf = p->dtype == DASH_BF16;
+  const hipError_t e = p->head_dim == 128 ? (bf ? launch_rotary<uint16_t, 128>(a, st) : launch_rotary<float, 128>(a, st))
+                                          : (bf ? launch_rotary<uint16_t, 64>(a, st) : launch_rotary<float, 64>(a, st));
+  return e == hipSuccess ? DASH_OK : DASH_ELAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,333 @@
+"""Rotary positions against their definition in 64 bits (tests/paged4_ref.py, which derives the bounds)."""
+import math
+
+import pytest
+import torch
+
+import paged4_ref as R
+from paper_2605_18753_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, F32 = torch.bfloat16, torch.float32
+FAR = 2 ** 31
+
+
+def draws(seed):
+    gen = torch.Generator().manual_seed(seed)
+    return lambda *s: torch.randn(s, generator=gen)
+
+
+def check(got, x, pos, theta, layout, mscale=1.0, inverse=False):
+    want, tol = R.turn(x, pos, theta, layout, mscale, inverse)
+    tol = R.rounded(want, tol, x.dtype)
+    rot = 2 * len(theta)
+    err = (got.cpu().double() - want).abs()
+    assert (err <= tol).all(), float((err / tol).max())
+    assert torch.equal(got.cpu()[..., rot:], x[..., rot:])        # the rest of a head as it was
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d,rot", [(64, 64), (64, 16), (64, 48), (128, 128), (128, 96), (128, 32), (128, 16)])
+@pytest.mark.parametrize("layout", ["halves", "adjacent"])
+@pytest.mark.parametrize("batch,h_q,h_kv,n_q,n_kv", [(1, 1, 1, 1, 1), (2, 3, 1, 37, 37), (3, 16, 2, 1, 9), (1, 5, 5, 200, 203)])
+def test_queries_and_keys(dtype, d, rot, layout, batch, h_q, h_kv, n_q, n_kv):
+    rand = draws(1)
+    q, k = rand(batch, h_q, n_q, d).to(dtype), rand(batch, h_kv, n_kv, d).to(dtype)
+    r = B.make_rotary(rot, DEV, layout=layout, mscale=1.25)
+    qg, kg = q.to(DEV), k.to(DEV)
+    qo, ko = torch.full_like(qg, 77.0), torch.full_like(kg, 77.0)
+    B.dash_rotary(r, qg, qo, kg, ko)
+    theta, at = R.thetas(rot), torch.arange(n_kv)
+    check(qo, q, at[n_kv - n_q:], theta, layout, 1.25)
+    check(ko, k, at, theta, layout, 1.25)
+    assert torch.equal(qg.cpu(), q) and torch.equal(kg.cpu(), k)
+    for x, x_out, xg, n in ((q, qo, qg, n_q), (k, ko, kg, n_kv)):   # one at a time, in place: the same bits
+        y = xg.clone()
+        B.dash_rotary(r, y, y, start=n_kv - n)
+        assert torch.equal(y, x_out)
+        y = xg.clone()
+        B.dash_rotary(r, None, None, y, y, start=n_kv - n)
+        assert torch.equal(y, x_out)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("layout", ["halves", "adjacent"])
+def test_positions_of_any_size(dtype, layout):
+    """Angles in 64 bits: a product in fp32 would be off by radians."""
+    rand = draws(2)
+    at = torch.tensor([0, 1, 4095, 65537, 1000003, 16777217, 123456789, FAR - 1, -1, -FAR], dtype=torch.int64)
+    x = rand(2, 3, len(at), 64).to(dtype)
+    pos = torch.stack((at, at.flip(0))).to(torch.int32).to(DEV)
+    theta = R.thetas(64)
+    r = B.make_rotary(64, DEV, layout=layout)
+    y = torch.empty_like(x, device=DEV)
+    B.dash_rotary(r, x.to(DEV), y, pos=pos)
+    for b in range(2):
+        check(y[b], x[b], at if b == 0 else at.flip(0), theta, layout)
+    near = B.make_rotary(64, DEV, layout=layout)
+    B.dash_rotary(near, x.to(DEV), y, pos=pos[0, :4].repeat(3)[:len(at)].contiguous(), start=5)
+    check(y, x, at[:4].repeat(3)[:len(at)] + 5, theta, layout)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("batch,n,heads,h_kv", [(1, 1, 32, 8), (64, 1, 32, 8), (1, 3001, 4, 1), (5, 700, 1, 0), (300, 3, 2, 2), (1, 9001, 40, 8)])
+def test_sizes(dtype, batch, n, heads, h_kv):
+    rand = draws(3)
+    q = rand(batch, heads, n, 64).to(dtype)
+    k = rand(batch, h_kv, n, 64).to(dtype) if h_kv else None
+    gen = torch.Generator().manual_seed(5)
+    pos = torch.randint(0, 1 << 20, (batch, n), generator=gen, dtype=torch.int32)
+    r = B.make_rotary(64, DEV)
+    qo = torch.empty_like(q, device=DEV)
+    ko = torch.empty_like(k, device=DEV) if h_kv else None
+    B.dash_rotary(r, q.to(DEV), qo, k.to(DEV) if h_kv else None, ko, pos=pos.to(DEV))
+    theta = R.thetas(64)
+    check(qo, q, pos[:, None], theta, "halves")
+    if h_kv:
+        check(ko, k, pos[:, None], theta, "halves")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_strides(dtype):
+    """Tokens outside of heads, slices of one tensor of queries, keys and values turned in place, padded rows; a sequence's positions in a wider row."""
+    rand = draws(4)
+    batch, n, h_q, h_kv, d = 2, 21, 6, 2, 128
+    fused = torch.full((batch, n, h_q + 2 * h_kv, d + 16), 5.0).to(dtype)
+    fused[..., :d] = rand(batch, n, h_q + 2 * h_kv, d).to(dtype)
+    g = fused.to(DEV)
+    q, k = g[:, :, :h_q, :d].transpose(1, 2), g[:, :, h_q:h_q + h_kv, :d].transpose(1, 2)
+    pos = torch.randint(0, 1000, (batch, 50), generator=torch.Generator().manual_seed(1), dtype=torch.int32)
+    r = B.make_rotary(64, DEV, layout="adjacent")
+    q_out = torch.full((batch, h_q, n + 3, d), 77.0, dtype=dtype, device=DEV)
+    B.dash_rotary(r, q, q_out[:, :, 1:n + 1], pos=pos.to(DEV)[:, 7:7 + n])
+    B.dash_rotary(r, q, q, k, k, pos=pos.to(DEV)[:, 7:7 + n])
+    at = pos[:, None, 7:7 + n]
+    for got, x in ((q_out[:, :, 1:n + 1], fused[:, :, :h_q, :d]), (q, fused[:, :, :h_q, :d]), (k, fused[:, :, h_q:h_q + h_kv, :d])):
+        check(got, x.transpose(1, 2), at, R.thetas(64), "adjacent")
+    assert (q_out[:, :, 0] == 77).all() and (q_out[:, :, n + 1:] == 77).all()
+    assert torch.equal(g.cpu()[:, :, h_q + h_kv:], fused[:, :, h_q + h_kv:]) and (g.cpu()[..., d:] == 5).all()
+    # one row of positions for all sequences, and a batch of one seen as several
+    shared = fused[:1, :, :h_q, :d].transpose(1, 2).to(DEV).expand(3, -1, -1, -1)
+    out = torch.empty((3, h_q, n, d), dtype=dtype, device=DEV)
+    B.dash_rotary(r, shared, out, pos=pos[0, :n].to(DEV))
+    check(out, fused[:1, :, :h_q, :d].transpose(1, 2).expand(3, -1, -1, -1), pos[0, :n], R.thetas(64), "adjacent")
+
+
+@pytest.mark.parametrize("layout", ["halves", "adjacent"])
+@pytest.mark.parametrize("scaling,kw", [("linear", dict(factor=4.0)), ("base", dict(factor=8.0)), ("parts", dict(factor=8.0, original=4096.0, low=1.0, high=32.0)),
+                                        (None, dict(base=500000.0))])
+def test_scaled_frequencies(layout, scaling, kw):
+    rand = draws(6)
+    x = rand(1, 2, 50, 128)
+    r = B.make_rotary(96, DEV, layout=layout, scaling=scaling, **kw)
+    y = torch.empty_like(x, device=DEV)
+    B.dash_rotary(r, x.to(DEV), y, start=30000)
+    base, f = kw.get("base", 10000.0), kw.get("factor", 1.0)
+    if scaling == "base":
+        base *= f ** (96 / 94)
+    theta = R.thetas(96, base)
+    if scaling == "linear":
+        theta = [t / int(f) for t in theta]
+    if scaling == "parts":
+        theta = [float(t) for t in theta]
+        c = [min(max((4096.0 * t / (2 * math.pi) - 1.0) / 31.0, 0.0), 1.0) for t in theta]
+        assert min(c) == 0 and max(c) == 1 and any(0 < v < 1 for v in c)
+        theta = [t * (v + (1 - v) / f) for t, v in zip(theta, c)]
+    check(y, x, torch.arange(30000, 30050), theta, layout)
+    own = B.make_rotary(96, DEV, layout=layout, frequencies=theta)
+    z = torch.empty_like(y)
+    B.dash_rotary(own, x.to(DEV), z, start=30000)
+    check(z, x, torch.arange(30000, 30050), theta, layout)
+    back = B.make_rotary(96, DEV, layout=layout, frequencies=[-t for t in theta])      # turning the other way
+    B.dash_rotary(back, y, z, start=30000)
+    assert (z.cpu() - x).abs().max() <= 8 * R.U * x.abs().max() * 4
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("layout", ["halves", "adjacent"])
+def test_gradients(dtype, layout):
+    """inverse is the transposed map: against the formula, and against differences of the forward call."""
+    rand = draws(7)
+    q, gq = rand(2, 4, 19, 64).to(dtype), rand(2, 4, 19, 64).to(dtype)
+    k, gk = rand(2, 2, 19, 64).to(dtype), rand(2, 2, 19, 64).to(dtype)
+    r = B.make_rotary(32, DEV, layout=layout, mscale=1.5)
+    dq, dk = torch.empty_like(q, device=DEV), torch.empty_like(k, device=DEV)
+    B.dash_rotary(r, gq.to(DEV), dq, gk.to(DEV), dk, start=1000, inverse=True)
+    at, theta = torch.arange(1000, 1019), R.thetas(32)
+    check(dq, gq, at, theta, layout, 1.5, inverse=True)
+    check(dk, gk, at, theta, layout, 1.5, inverse=True)
+    if dtype == BF:
+        return
+    # the map is linear: (f(x + s e) - f(x - s e)) / 2 s has no error but rounding, of numbers up to 8 s or so
+    gen, s = torch.Generator().manual_seed(1), 64.0
+    y0, y1 = torch.empty_like(q, device=DEV), torch.empty_like(q, device=DEV)
+    for _ in range(20):
+        i = tuple(int(torch.randint(0, n, (1,), generator=gen)) for n in q.shape)
+        lo, hi = q.clone(), q.clone()
+        lo[i] -= s
+        hi[i] += s
+        B.dash_rotary(r, lo.to(DEV), y0, start=1000)
+        B.dash_rotary(r, hi.to(DEV), y1, start=1000)
+        diff = float(((y1.double() - y0.double()).cpu() * gq.double()).sum()) / (2 * s)
+        # two elements of y change; each is off by 5 u 1.5 (s + 5), times a gradient of at most 5, over s; d q itself by 5 u * 1.5 * 10
+        assert abs(diff - float(dq[i])) <= 2 * 2 * 5 * R.U * 1.5 * (s + 5) * 5 / (2 * s) + 75 * R.U
+
+
+def test_a_number_that_is_not_finite_reaches_its_pair_only():
+    for bad in (math.nan, math.inf):
+        for layout in ("halves", "adjacent"):
+            x = draws(8)(1, 2, 5, 64)
+            x[0, 1, 3, 9] = bad
+            r = B.make_rotary(32, DEV, layout=layout)
+            y = torch.empty_like(x, device=DEV)
+            B.dash_rotary(r, x.to(DEV), y, start=3)
+            lost = ~torch.isfinite(y.cpu())
+            pair = (9, 25) if layout == "halves" else (8, 9)
+            assert lost[0, 1, 3, list(pair)].all() and int(lost.sum()) == 2
+
+
+def test_in_a_graph_and_on_another_stream():
+    x = draws(9)(3, 8, 11, 128).to(BF)
+    xg = x.to(DEV)
+    pos = torch.arange(11, dtype=torch.int32, device=DEV)
+    r = B.make_rotary(128, DEV)
+    y = torch.zeros_like(xg)
+    want = []
+    for shift in (0, 5, 70000):
+        B.dash_rotary(r, xg, y, pos=pos + shift)
+        want.append(y.clone())
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        out = torch.zeros_like(xg)
+        B.dash_rotary(r, xg, out, pos=pos)
+    s.synchronize()
+    assert torch.equal(out, want[0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.dash_rotary(r, xg, y, pos=pos)
+    for i in (0, 1, 2, 1, 0):
+        pos.copy_(torch.arange(11) + (0, 5, 70000)[i])
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[i])
+
+
+# ---- appending on the way --------------------------------------------------------------------------------------------
+class Fresh:
+    """Sequences with new tokens, their cache's pages on the GPU, and what an append has to make of them."""
+
+    def __init__(self, lens, news, h_q=4, h_kv=2, d=64, page=16, dtype=BF, spare=0, seed=0, missing=(), seen=None):
+        rand = draws(seed)
+        self.lens, self.news = lens, news
+        per = [-(-n // page) for n in lens]
+        n_pages = sum(per) + 2
+        ids = torch.randperm(n_pages, generator=torch.Generator().manual_seed(seed))[:sum(per)].tolist()
+        self.table = torch.full((len(lens), max(max(per), 1)), -1, dtype=torch.int32)
+        at = 0
+        for b, k in enumerate(per):
+            self.table[b, :k] = torch.tensor(ids[at:at + k], dtype=torch.int32)
+            at += k
+        for b, i, entry in missing:
+            self.table[b, i] = entry
+        starts = [0]
+        for m in news:
+            starts.append(starts[-1] + m)
+        self.row_start = torch.tensor(starts, dtype=torch.int32)
+        self.rows = starts[-1] + spare
+        self.q, self.k_new, self.v_new = rand(self.rows, h_q, d).to(dtype), rand(self.rows, h_kv, d).to(dtype), rand(self.rows, h_kv, d).to(dtype)
+        self.seen = None if seen is None else torch.tensor(seen, dtype=torch.int32)
+        self.n_pages, self.page, self.h_kv, self.d, self.rand = n_pages, page, h_kv, d, rand
+        self.places = R.positions(lens, self.row_start, self.seen)
+
+    def gpu(self, x):
+        return None if x is None else x.to(DEV)
+
+    def written(self):
+        """(row, sequence, slot, position, page, offset) of the rows that have a page."""
+        for r, b, slot, pos in self.places:
+            page = int(self.table[b, slot // self.page])
+            if 0 <= page < self.n_pages:
+                yield r, b, slot, pos, page, slot % self.page
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("layout", ["halves", "adjacent"])
+@pytest.mark.parametrize("d,rot,h_q,h_kv,page", [(64, 64, 4, 2, 16), (128, 128, 32, 8, 64), (128, 48, 3, 3, 32), (64, 16, 16, 1, 16), (128, 128, 5, 5, 16)])
+@pytest.mark.parametrize("seen", [None, [1000, 7, 70001, 2 ** 30, 5]])
+def test_append(dtype, layout, d, rot, h_q, h_kv, page, seen):
+    s = Fresh([40, 5, 1, 33, 0], [9, 5, 1, 33, 0], h_q, h_kv, d, page, dtype, spare=2, seed=11, missing=((3, 0, 999), (0, 1 if page < 40 else 0, -1)), seen=seen)
+    k, v = s.rand(s.n_pages, h_kv, page, d).to(dtype), s.rand(s.n_pages, h_kv, page, d).to(dtype)
+    w, pos = s.rand(s.n_pages, h_kv, page), torch.full((s.n_pages, h_kv, page), -5, dtype=torch.int32)
+    c = B.PagedCache(k.to(DEV), v.to(DEV), s.table.to(DEV), torch.tensor(s.lens, dtype=torch.int32, device=DEV), w.to(DEV), pos.to(DEV), s.gpu(s.seen))
+    p = B.make_paged_params(c, s.rows, h_q)
+    r = B.make_rotary(rot, DEV, layout=layout, mscale=0.75)
+    q_out = torch.full_like(s.q, 77.0, device=DEV)
+    B.dash_paged_append_rotary(p, c, r, s.k_new.to(DEV), s.v_new.to(DEV), s.row_start.to(DEV), q=s.q.to(DEV), q_out=q_out)
+    theta = R.thetas(rot)
+    rows = [x[0] for x in s.places]
+    at = torch.tensor([x[3] for x in s.places])
+    check(q_out.cpu()[rows], s.q[rows], at[:, None], theta, layout, 0.75)
+    rest = [i for i in range(s.rows) if i not in set(rows)]
+    assert (q_out[rest] == 77).all()
+    got, want_v, want_w, want_pos = c.k.cpu(), v.clone(), w.clone(), pos.clone()
+    done = list(s.written())
+    assert len(done) < len(rows)
+    for row, b, slot, position, pg, off in done:
+        check(got[pg, :, off], s.k_new[row], torch.tensor(position), theta, layout, 0.75)
+        want_v[pg, :, off], want_w[pg, :, off], want_pos[pg, :, off] = s.v_new[row], 0, position
+        got[pg, :, off] = k[pg, :, off]
+    assert torch.equal(got, k)                                   # nothing else is touched
+    assert torch.equal(c.v.cpu(), want_v) and torch.equal(c.weights.cpu(), want_w) and torch.equal(c.pos.cpu(), want_pos)
+    # without queries, and with queries in place: the same
+    c2 = B.PagedCache(k.to(DEV), v.to(DEV), c.table, c.lens, None, None, c.seen)
+    B.dash_paged_append_rotary(p, c2, r, s.k_new.to(DEV), s.v_new.to(DEV), s.row_start.to(DEV))
+    assert torch.equal(c2.k, c.k) and torch.equal(c2.v, c.v)
+    qg = s.q.to(DEV)
+    B.dash_paged_append_rotary(p, c2, r, s.k_new.to(DEV), s.v_new.to(DEV), s.row_start.to(DEV), q=qg, q_out=qg)
+    assert torch.equal(qg.cpu()[rows], q_out.cpu()[rows]) and torch.equal(qg.cpu()[rest], s.q[rest])
+
+
+def test_append_turns_by_the_positions_that_rotary_turns_by():
+    """A prompt turned at once and one that comes in pieces: the same keys."""
+    x = draws(12)(1, 2, 50, 128).to(BF).to(DEV)
+    r = B.make_rotary(128, DEV)
+    y = torch.empty_like(x)
+    B.dash_rotary(r, x, y)
+    c = B.PagedCache.allocate(1, 2, 5, 16, 128, 4, DEV)
+    c.table.copy_(torch.tensor([[3, 0, 4, 1]]))
+    at = 0
+    for m in (17, 1, 32):
+        c.lens += m
+        new = x[0, :, at:at + m].transpose(0, 1)                 # strided rows
+        B.dash_paged_append_rotary(B.make_paged_params(c, m, 4), c, r, new, new, torch.tensor([0, m], dtype=torch.int32, device=DEV))
+        at += m
+    got = c.k[c.table[0].long()].transpose(0, 1).reshape(2, 64, 128)[:, :50]
+    assert torch.equal(got, y[0])
+
+
+@pytest.mark.parametrize("four", [False, True])
+def test_appends_of_many_sequences(four):
+    n = 200
+    lens = [(7 * i) % 50 + 1 for i in range(n)]
+    s = Fresh(lens, [min(1 + (i % 3), lens[i]) for i in range(n)], d=64, seed=13)
+    r = B.make_rotary(64, DEV)
+    lens_g = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    if four:
+        c = B.PagedCache4.allocate(n, 2, s.n_pages, 16, 64, s.table.shape[1], DEV)
+        c.table.copy_(s.table)
+        c.lens.copy_(lens_g)
+        B.dash_paged4_append(B.make_paged4_params(c, s.rows, 4), c, s.k_new.to(DEV), s.v_new.to(DEV), s.row_start.to(DEV), rotary=r)
+        got = R.values(c.k_codes.cpu(), c.k_scales.cpu())
+    else:
+        c = B.PagedCache(torch.zeros((s.n_pages, 2, 16, 64), dtype=BF, device=DEV), torch.zeros((s.n_pages, 2, 16, 64), dtype=BF, device=DEV), s.table.to(DEV), lens_g)
+        B.dash_paged_append_rotary(B.make_paged_params(c, s.rows, 4), c, r, s.k_new.to(DEV), s.v_new.to(DEV), s.row_start.to(DEV))
+        got = c.k.cpu()
+    for row, b, slot, position, pg, off in s.written():
+        if four:
+            want = R.values(*R.quantise(R.turn(s.k_new[row], torch.tensor(position), R.thetas(64), "halves")[0]))
+            assert torch.equal(got[pg, :, off], want)
+        else:
+            check(got[pg, :, off], s.k_new[row], torch.tensor(position), R.thetas(64), "halves")
