@@ -458,7 +458,7 @@ int dash_paged_append_rotary(const dash_paged_params* p, const dash_rotary* r, c
  * hardware converts them).
  *   k_codes, v_codes    uint8 [n_pages, h_kv, page_size, d / 2]: element 2 i in the low half of byte i; d / 2 contiguous, the other strides, in BYTES,
  *                       are k_stride and v_stride of dash_paged_params (multiples of 16)
- *   k_scales, v_scales  uint8 [n_pages, h_kv, page_size, d / 32] contiguous: e + 127; 255: the 32 numbers are NaN
+ *   k_scales, v_scales  uint8 [n_pages, h_kv, page_size, d / 32] contiguous, 16-byte aligned: e + 127; 255: the 32 numbers are NaN
  * A row is held so: e = floor(log2 max|x|) - 2, one more where max|x| > 7.25 * 2^e (up to there the largest is held as 6, which costs less than the coarser
  * steps would: root mean square 0.112 of normal numbers instead of 0.117 with a border of 6, 0.116 of 8), within -120 .. 125; then each
  * number at the nearest level, the even code of two as near.  32 numbers among which one is NaN or infinite are held as NaN.

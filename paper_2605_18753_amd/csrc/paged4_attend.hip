@@ -35,14 +35,39 @@ template <int CW> __device__ __forceinline__ Codes<CW> load_codes(__amdgpu_buffe
 }
 // bytes [0, bytes) behind p; loads past them give 0
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, int bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, bytes, 0x00020000);
+  const uint64_t at = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));   // ints: not to be widened
+  return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+// Scale bytes come as the word that they lie in (bytes would be widened as soon as they arrive, which waits for them).  Block b of a row among 16 that begin
+// at a multiple of 4 bytes: offset of its word, and its byte's place there.
+template <int D> __device__ __forceinline__ uint32_t scale_word(int row) { return D == 128 ? row * 4 : (row >> 1) * 4; }
+template <int D> __device__ __forceinline__ int scale_span(int rows) { return D == 128 ? rows * 4 : ((rows + 1) >> 1) * 4; }   // whole words
+template <int D> __device__ __forceinline__ uint32_t scale_byte(uint32_t w, int row, int b) { return __builtin_amdgcn_ubfe(w, D == 128 ? 8 * b : 16 * (row & 1) + 8 * b, 8); }
+// A uniform number kept within 0 .. 16.  (The compiler makes min and max a vector instruction, what follows from it too, and waits for loads whose registers it takes.)
+__device__ __forceinline__ int within_16(int x) {
+  int y;
+  asm("s_max_i32 %0, %1, 0\n\ts_min_i32 %0, %0, 16" : "=s"(y) : "s"(x) : "scc");
+  return y;
+}
+// Bytes of `rows` rows of codes, 0 .. 16 of them, from the first one's start.
+template <int D> __device__ __forceinline__ int rows_span(int rows, uint32_t stride) {
+  return max((int)((uint32_t)rows * stride - (stride - D / 2)), 0);
 }
 __device__ __forceinline__ void lds_write_b128(uint32_t addr, bf16x8 x) {
   *reinterpret_cast<__attribute__((address_space(3))) bf16x8*>(addr) = x;
 }
 
+// An address with bits flipped, worked out where it is used: the registers have no room for one a chunk.
+__device__ __forceinline__ uint32_t flipped(uint32_t addr, int bits) {
+  uint32_t x;
+  if (bits == 0) return addr;
+  asm volatile("v_xor_b32 %0, %2, %1" : "=v"(x) : "v"(addr), "i"(bits));
+  return x;
+}
+
 template <int D>
-__global__ __launch_bounds__(256, 3) void paged_few4_kernel(PagedArgs args) {
+__global__ __launch_bounds__(256, D == 128 ? 3 : 4) void paged_few4_kernel(PagedArgs args) {
   using C = Few4Cfg<D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int r = blockIdx.x % args.h_kv, wg = blockIdx.x / args.h_kv;
@@ -66,70 +91,67 @@ __global__ __launch_bounds__(256, 3) void paged_few4_kernel(PagedArgs args) {
   const int first_last = paged_last_key(a, it, t0);                              // of the tile's first token
   const int end = max(paged_last_key(a, it, min(t0 + T, it.m) - 1) + 1, 0);      // keys that a row of the tile sees
   // the wave's 32-key tiles of the piece's 128-key steps
-  const int j1 = min(run.x1 * 4, (end + 31) >> 5);
-  int j = run.x0 * 4 + wave;
+  const int j1 = __builtin_amdgcn_readfirstlane(min(run.x1 * 4, (end + 31) >> 5)), keys = __builtin_amdgcn_readfirstlane(it.n);
+  int j = __builtin_amdgcn_readfirstlane(run.x0 * 4) + wave;
 
   const uint32_t buf = lds_addr_of(lds) + wave * C::TILE_BYTES;
   const uint32_t kt = (uint32_t)a.kp_t, vt = (uint32_t)a.vp_t;
   // K: row n, quarter kq; V: row lane / 4, quarter lane % 4
   const uint32_t k_off = (uint32_t)n * kt + kq * (D / 8), v_off = (uint32_t)(lane >> 2) * vt + (lane & 3) * (D / 8);
-  const uint32_t ks_off = (uint32_t)(n * (D / 32) + kq * (D / 4) / 32), vs_off = (uint32_t)((lane >> 2) * (D / 32) + (lane & 3) * (D / 4) / 32);
+  const uint32_t ks_off = scale_word<D>(n), vs_off = scale_word<D>(lane >> 2);
   const char* kb = (const char*)a.k + r * a.kp_h;
   const char* vb = (const char*)a.v + r * a.vp_h;
   const int pm = (1 << a.page_log) - 1;
-  // the pages of a tile: one, or two of 16 tokens
-  auto pages_of = [&](int tile) {
-    return make_int2(paged_page(a, it.b, (tile * 32) >> a.page_log), paged_page(a, it.b, (tile * 32 + 16) >> a.page_log));
+  // the table's entries for a tile: of one page, or of two of 16 tokens; looked at a tile later, when they have arrived
+  auto entries_of = [&](int tile) {
+    return make_int2(paged_entry(a, it.b, (tile * 32) >> a.page_log), paged_entry(a, it.b, (tile * 32 + 16) >> a.page_log));
   };
   struct Raw { Codes<C::CW> k[2], v[2]; uint32_t ks[2], vs[2]; };
   // A resource ends with the sequence's last token: rows behind it read as zeros, whatever their page holds.
-  auto load = [&](int tile, int2 pg, Raw& x) {
+  auto load = [&](int tile, int2 entries, Raw& x) {
 #pragma unroll
     for (int half = 0; half < 2; half++) {
-      const int key = tile * 32 + half * 16, id = half ? pg.y : pg.x, rows = min(max(it.n - key, 0), 16);
-      const int64_t at = ((((int64_t)id * a.h_kv + r) << a.page_log) + (key & pm)) * (D / 32);
-      x.k[half] = load_codes<C::CW>(rsrc_of(kb + (int64_t)id * a.kp_p + (int64_t)(key & pm) * a.kp_t, rows ? (rows - 1) * (int)kt + D / 2 : 0), k_off);
-      x.v[half] = load_codes<C::CW>(rsrc_of(vb + (int64_t)id * a.vp_p + (int64_t)(key & pm) * a.vp_t, rows ? (rows - 1) * (int)vt + D / 2 : 0), v_off);
-      x.ks[half] = __builtin_amdgcn_raw_buffer_load_b8(rsrc_of(a.k_sc + at, rows * (D / 32)), ks_off, 0, 0);
-      x.vs[half] = __builtin_amdgcn_raw_buffer_load_b8(rsrc_of(a.v_sc + at, rows * (D / 32)), vs_off, 0, 0);
+      const int key = tile * 32 + half * 16;
+      const uint32_t id = paged_clamp(a, half ? entries.y : entries.x), off = key & pm;
+      const int rows = within_16(min(keys - key, (j1 - tile) * 32));                // behind the piece's last tile: nothing is read
+      const uint64_t at = ((((uint64_t)id * (uint32_t)a.h_kv + r) << a.page_log) + off) * (D / 32);
+      x.k[half] = load_codes<C::CW>(rsrc_of(kb + (uint64_t)id * (uint64_t)a.kp_p + off * kt, rows_span<D>(rows, kt)), k_off);
+      x.v[half] = load_codes<C::CW>(rsrc_of(vb + (uint64_t)id * (uint64_t)a.vp_p + off * vt, rows_span<D>(rows, vt)), v_off);
+      x.ks[half] = __builtin_amdgcn_raw_buffer_load_b32(rsrc_of(a.k_sc + at, scale_span<D>(rows)), ks_off, 0, 0);
+      x.vs[half] = __builtin_amdgcn_raw_buffer_load_b32(rsrc_of(a.v_sc + at, scale_span<D>(rows)), vs_off, 0, 0);
     }
   };
-  uint32_t v_wr[C::CW];
-#pragma unroll
-  for (int i = 0; i < C::CW; i++) v_wr[i] = buf + (uint32_t)((lane >> 2) * C::ROW_BYTES + ((C::CW * (lane & 3) + i) ^ v4_swz<D>(lane >> 2)) * 16);
+  // of a lane's first chunk; chunk i, and d-tile i of the reads, lie at those addresses with bits 4 .. and 5 .. flipped by i
+  const uint32_t v_wr = buf + (uint32_t)((lane >> 2) * C::ROW_BYTES + ((C::CW * (lane & 3)) ^ v4_swz<D>(lane >> 2)) * 16);
   // transposing read of V: lane s of a group of 16 points at row 4 kq + s / 4 (+ 16), d 4 (s % 4) of the 16-wide d-tile
-  uint32_t v_rd[D / 16];
-#pragma unroll
-  for (int dt = 0; dt < D / 16; dt++)
-    v_rd[dt] = buf + (uint32_t)((4 * kq + (n >> 2)) * C::ROW_BYTES + (((2 * dt + ((n & 3) >> 1)) ^ v4_swz<D>(n >> 2)) << 4) + ((n & 1) << 3));
+  const uint32_t v_rd = buf + (uint32_t)((4 * kq + (n >> 2)) * C::ROW_BYTES + ((((n & 3) >> 1) ^ v4_swz<D>(n >> 2)) << 4) + ((n & 1) << 3));
 
   float m_run = -INFINITY, l_run = 0.f;
   f32x4 oacc[D / 16];
 #pragma unroll
   for (int dt = 0; dt < D / 16; dt++) oacc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  Raw next;
-  int2 pg = make_int2(0, 0);
+  // Two sets of registers in turn: the next tile's loads are asked for before the present ones are waited for.
+  Raw even, odd;
+  int2 entries = make_int2(0, 0);
   if (j < j1) {
-    load(j, pages_of(j), next);
-    pg = pages_of(j + 4);
+    load(j, entries_of(j), even);
+    entries = entries_of(j + 4);
   }
-  for (; j < j1; j += 4) {
-    const Raw x = next;
-    if (j + 4 < j1) {
-      load(j + 4, pg, next);
-      pg = pages_of(j + 8);
-    }
-    // values of a block that is NaN go in as zeros; the rows that see its token get NaN below
+  auto tile = [&](const Raw& x, Raw& next) __attribute__((always_inline)) {
+    load(j + 4, entries, next);
+    entries = entries_of(j + 8);
+    // a block that is NaN goes in as numbers next to 0 (the scale's exponent 0): the rows that see its token get NaN below
+    uint32_t vs[2];
 #pragma unroll
     for (int half = 0; half < 2; half++) {
-      const float sc = x.vs[half] == 255u ? 0.f : __uint_as_float(x.vs[half] << 23);
+      vs[half] = scale_byte<D>(x.vs[half], lane >> 2, (lane & 3) * (D / 4) / 32);
+      const float sc = __uint_as_float(vs[half] == 255u ? 0u : vs[half] << 23);
 #pragma unroll
-      for (int i = 0; i < C::CW; i++)
-        lds_write_b128(v_wr[i] + half * 16 * C::ROW_BYTES, fp4_to_bf16(x.vs[half] == 255u ? 0u : x.v[half].w[i], sc));
+      for (int i = 0; i < C::CW; i++) lds_write_b128(flipped(v_wr, i << 4) + half * 16 * C::ROW_BYTES, fp4_to_bf16(x.v[half].w[i], sc));
     }
     f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;                                    // lane (row n, kq): keys 4 kq + i, 16 + 4 kq + i
-    const float k0 = fp4_scale(x.ks[0]), k1 = fp4_scale(x.ks[1]);
+    const float k0 = fp4_scale(scale_byte<D>(x.ks[0], n, kq * (D / 4) / 32)), k1 = fp4_scale(scale_byte<D>(x.ks[1], n, kq * (D / 4) / 32));
 #pragma unroll
     for (int s = 0; s < D / 32; s++) {
       s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp4_to_bf16(x.k[0].w[s], k0), qf[s], s0, 0, 0, 0);
@@ -166,13 +188,15 @@ __global__ __launch_bounds__(256, 3) void paged_few4_kernel(PagedArgs args) {
     const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
     asm volatile("" ::: "memory");                                               // a wave's LDS operations complete in order
 #pragma unroll
-    for (int dt = 0; dt < D / 16; dt++)
-      oacc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_read_tr_pair(v_rd[dt], v_rd[dt] + 16 * C::ROW_BYTES), pb, oacc[dt], 0, 0, 0);
+    for (int dt = 0; dt < D / 16; dt++) {
+      const uint32_t at = flipped(v_rd, dt << 5);
+      oacc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_read_tr_pair(at, at + 16 * C::ROW_BYTES), pb, oacc[dt], 0, 0, 0);
+    }
     asm volatile("" ::: "memory");
-    if (__builtin_expect(__any(x.vs[0] == 255u || x.vs[1] == 255u), 0)) {
+    if (__builtin_expect(__any(vs[0] == 255u || vs[1] == 255u), 0)) {
 #pragma unroll
       for (int half = 0; half < 2; half++)
-        for (uint64_t bad = __ballot(x.vs[half] == 255u); bad; bad &= bad - 1) {
+        for (uint64_t bad = __ballot(vs[half] == 255u); bad; bad &= bad - 1) {
           const int l = __builtin_ctzll(bad), block = (l & 3) * (D / 4) / 32;
           const bool seen = j * 32 + half * 16 + (l >> 2) <= last;
 #pragma unroll
@@ -180,6 +204,12 @@ __global__ __launch_bounds__(256, 3) void paged_few4_kernel(PagedArgs args) {
             if (dt >> 1 == block && seen) oacc[dt] = f32x4{NAN, NAN, NAN, NAN};
         }
     }
+  };
+  while (j < j1) {
+    tile(even, odd);
+    if ((j += 4) >= j1) break;
+    tile(odd, even);
+    j += 4;
   }
   const float l_tot = quad_rows_sum(l_run);
   __syncthreads();
@@ -199,36 +229,355 @@ __global__ __launch_bounds__(256, 3) void paged_few4_kernel(PagedArgs args) {
   } while (run.advance(args));
 }
 
-// ---- host ------------------------------------------------------------------------------------------------------------
-static int64_t most_items(const PagedArgs& a, int rows) {   // of a kv-head
-  const int T = rows / a.g;
-  return min((int64_t)a.n_rows / T + min(a.batch, a.n_rows), (int64_t)a.n_rows);
+// Many rows: a tile is 128 (token, head) rows, as in paged_rows_kernel, whose walk this is: the two products, the exponentials and the maxima
+// between their MFMAs, the order of operands.  64-key tiles of K and V are converted on their way into LDS, each by the whole workgroup once.
+template <int D> struct Rows4Cfg {
+  static constexpr int CW = D / 32, ROW_BYTES = D * 2;
+  static constexpr int TILE_BYTES = 64 * ROW_BYTES;
+  static constexpr int OUT_BYTES = 128 * (D + 4) * 4;      // a tile's rows in fp32, behind the walk
+  static constexpr int LDS_BYTES = 4 * TILE_BYTES + 64 > OUT_BYTES ? 4 * TILE_BYTES + 64 : OUT_BYTES;   // K ring [2], V ring [2], blocks that are NaN
+};
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void paged_rows4_kernel(PagedArgs a) {
+  using C = Rows4Cfg<D>;
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 31, h = lane >> 5;
+  // kv-heads are the fast index: with 8 of them each XCD's L2 sees the pages of one
+  const int r = blockIdx.x % a.h_kv;
+  PagedPart it;
+  if (!paged_find_part(a, blockIdx.x / a.h_kv, [&](int m, int n) { return rows_shape(a, m, n); }, it)) return;
+  const int T = 128 / a.g, t0 = it.tile * T, Tw = 32 / a.g, tw0 = t0 + wave * Tw;
+  const int t = tw0 + n / a.g;
+  bf16x8 qf[D / 16];
+  {
+    const uint16_t* qp = (const uint16_t*)a.q + (it.r0 + min(t, it.m - 1)) * a.q_t + (r * a.g + n % a.g) * a.q_h + h * 8;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ks++) qf[ks] = *reinterpret_cast<const bf16x8*>(qp + ks * 16);
+  }
+  // of the lane's row, worked out where it is used
+  auto last_key = [&]() { return paged_last_key(a, it, min(tw0 + ((paged_thread() & 31) >> (31 - __builtin_clz(a.g))), it.m - 1)); };
+  // keys that the tile, and the wave, sees; up to where the wave's first token does
+  const int end = max(paged_last_key(a, it, min(t0 + T, it.m) - 1) + 1, 0);
+  const int wave_end = tw0 < it.m ? paged_last_key(a, it, min(tw0 + Tw, it.m) - 1) + 1 : 0;
+  const int low = paged_last_key(a, it, min(tw0, it.m - 1));
+  const int kt = (end + 63) >> 6, per = (kt + it.parts - 1) / it.parts;
+  const int first = min(it.part * per, kt), n_it = min(per, kt - first);       // the part's tiles
+
+  // ---- pages: 64 entries of the table a lane each, the next 64 behind them ----------------------------------
+  const int32_t* table = a.table + (int64_t)it.b * a.max_pages;
+  auto window = [&](int i) { return paged_clamp(a, table[min(i + (paged_thread() & 63), a.max_pages - 1)]); };
+  int wbase = (first * 64) >> a.page_log;
+  int win = window(wbase), win_next = window(wbase + 64);
+
+  // ---- pages -> registers -> LDS --------------------------------------------------------------------------------
+  // A wave has 16 rows of a tile, which lie in one page: one resource, which ends with the sequence's last token (rows behind it read as
+  // zeros, whatever the page holds).  A lane has a quarter of row lane / 4.
+  const uint32_t k_t = (uint32_t)a.kp_t, v_t = (uint32_t)a.vp_t;
+  const char* kb = (const char*)a.k + r * a.kp_h;
+  const char* vb = (const char*)a.v + r * a.vp_h;
+  const int pm = (1 << a.page_log) - 1, row0 = wave * 16;
+  const uint32_t lds0 = lds_addr_of(lds);
+  const int part_end = first + n_it;
+  struct Raw { Codes<C::CW> c; uint32_t s; };
+  auto scale_of = [&](const Raw& x) {
+    const int l = paged_thread() & 63;
+    return scale_byte<D>(x.s, l >> 2, (l & 3) * (D / 4) / 32);
+  };
+  auto ask = [&](Raw& x, const char* base, int64_t page_stride, uint32_t row_stride, const uint8_t* scales, int id, int tile) {
+    const int l = paged_thread() & 63;
+    const int key = tile * 64 + row0, rows = tile < part_end ? within_16(it.n - key) : 0;   // behind the part's last tile: nothing is read
+    const uint32_t off = key & pm;
+    x.c = load_codes<C::CW>(rsrc_of(base + (uint64_t)(uint32_t)id * (uint64_t)page_stride + off * row_stride, rows_span<D>(rows, row_stride)),
+                           (uint32_t)(l >> 2) * row_stride + (l & 3) * (D / 8));
+    x.s = __builtin_amdgcn_raw_buffer_load_b32(rsrc_of(scales + ((((uint64_t)(uint32_t)id * (uint32_t)a.h_kv + r) << a.page_log) + off) * (D / 32), scale_span<D>(rows)), scale_word<D>(l >> 2), 0, 0);
+  };
+  int id_v = 0, id_k = 0;                                     // pages of tile i + 1 (its V is asked for) and of tile i + 2 (its K)
+  auto id_of = [&](int tile) { return __builtin_amdgcn_readlane(win, (((tile * 64 + row0) >> a.page_log) - wbase) & 63); };
+  // of a lane's first chunk; chunk i lies at that address with bits 4 and 5 flipped by i (the ring begins at a multiple of 1024)
+  uint32_t k_wr, v_wr;
+  {
+    const int row = row0 + (lane >> 2), c = C::CW * (lane & 3);
+    k_wr = lds0 + (uint32_t)(row * C::ROW_BYTES + ((c ^ pk_swz<D>(row)) << 4));
+    v_wr = lds0 + (uint32_t)(2 * C::TILE_BYTES + row * C::ROW_BYTES + ((c ^ v4_swz<D>(row)) << 4));
+  }
+  uint64_t* nan_blocks = reinterpret_cast<uint64_t*>(lds + 4 * C::TILE_BYTES);   // [slot][wave]: lanes whose block of V is NaN
+  Raw kr, vr;
+  float k_sc = 0.f, v_sc = 0.f;
+  auto conv = [&](uint32_t to, const Raw& x, float scale, int c, int slot) {
+    lds_write_b128(flipped(to, c << 4) + slot * C::TILE_BYTES, fp4_to_bf16(x.c.w[c], scale));
+  };
+  auto conv_k = [&](int c, int slot) { conv(k_wr, kr, k_sc, c, slot); };
+  auto conv_v = [&](int c, int slot) { conv(v_wr, vr, v_sc, c, slot); };
+  // ---- operand addresses in LDS, of slot 0 --------------------------------------------------------------------
+  const uint32_t k_rd0 = lds0 + (uint32_t)(n * C::ROW_BYTES + ((h ^ pk_swz<D>(n)) << 4));   // d slice ks: bits 5 .. flipped by ks
+  const int s16 = lane & 15, a16 = (lane >> 4) & 1;
+  const uint32_t v_rd0 = lds0 + (uint32_t)((4 * h + (s16 >> 2)) * C::ROW_BYTES + (((2 * a16 + ((s16 & 3) >> 1)) ^ v4_swz<D>(s16 >> 2)) << 4) + ((s16 & 1) << 3));
+
+  float m_run = -INFINITY, l_run = 0.f;
+  constexpr int NDT = D / 32;
+  f32x16 oacc[NDT];
+#pragma unroll
+  for (int dt = 0; dt < NDT; dt++)
+#pragma unroll
+    for (int j = 0; j < 16; j++) oacc[dt][j] = 0.f;
+  id_k = id_of(first);
+  ask(kr, kb, a.kp_p, k_t, a.k_sc, id_k, first);
+  ask(vr, vb, a.vp_p, v_t, a.v_sc, id_k, first);
+  k_sc = fp4_scale(scale_of(kr));
+#pragma unroll
+  for (int c = 0; c < C::CW; c++) conv_k(c, 0);
+  id_v = id_k = id_of(first + 1);
+  ask(kr, kb, a.kp_p, k_t, a.k_sc, id_k, first + 1);
+  // Iteration i, LDS: tile i lives in slot i & 1 of both rings, V one iteration behind K.  The barrier at its top makes everybody's tiles visible (K of
+  // tile i, V of tile i - 1) and retires the reads of iteration i - 1, whose slots this iteration writes over with what it converts: K of tile
+  // i + 1 and V of tile i, a word of codes at a time between the MFMAs.  Their registers then take K of tile i + 2 and V of tile i + 1.
+  int pend = 0;
+  float tmax_old = 0.f;
+  auto iteration = [&](auto p_tag, int i, f32x16 (&s)[2], f32x16 (&so)[2]) __attribute__((always_inline)) {
+    constexpr int P = decltype(p_tag)::value;
+    constexpr int NS = D / 8, KAHEAD = 4, VAHEAD = 2, EQ = 12, E0 = 2;
+    const bool cur = i < n_it;
+    const int tile = first + i;
+    const bool on = cur && tile * 64 < wave_end;
+    if (((tile + 2) * 64 >> a.page_log) - wbase >= 64) {
+      wbase += 64;
+      win = win_next;
+      win_next = window(wbase + 64);
+    }
+    id_v = id_k;
+    id_k = id_of(tile + 2);
+    if (pend && __builtin_expect(__any(tmax_old > m_run + kPagedLazy), 0)) {
+      const float m_new = fmaxf(m_run, fmaxf(tmax_old, __shfl_xor(tmax_old, 32)));
+      const float use = m_new == -INFINITY ? 0.f : m_new;
+      const float corr = __builtin_amdgcn_exp2f(m_run - use);
+      m_run = m_new;
+      l_run *= corr;
+#pragma unroll
+      for (int dt = 0; dt < NDT; dt++)
+#pragma unroll
+        for (int j = 0; j < 16; j++) oacc[dt][j] *= corr;
+    }
+    const float off = m_run == -INFINITY ? 0.f : -m_run;
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    k_sc = fp4_scale(scale_of(kr));
+    const uint32_t vs = scale_of(vr);
+    v_sc = __uint_as_float(vs == 255u ? 0u : vs << 23);        // a block that is NaN goes in as numbers next to 0: the rows that see it get NaN below
+    if (lane == 0) nan_blocks[P * 4 + wave] = 0;
+    if (const uint64_t bad = __ballot(vs == 255u); __builtin_expect(bad != 0, 0)) {
+      if (lane == 0) nan_blocks[P * 4 + wave] = bad;
+    }
+    auto k_read = [&](int x) -> bf16x8 {   // slot x: d slice x / 2, key half x % 2
+      return lds_read_b128(flipped(k_rd0, (x >> 1) << 5) + (uint32_t)(P * C::TILE_BYTES + (x & 1) * 32 * C::ROW_BYTES));
+    };
+    auto v_read = [&](int x) -> bf16x8 {   // slot x: contraction step x / NDT, d-tile x % NDT
+      const uint32_t at = flipped(v_rd0, (x % NDT) << 6) + (uint32_t)((2 + (P ^ 1)) * C::TILE_BYTES + 16 * (x / NDT) * C::ROW_BYTES);
+      return lds_read_tr_pair(at, at + 8 * C::ROW_BYTES);
+    };
+    u32x4 pb[4];
+    float l_tile = 0.f;
+    // Pair k of tile i - 1: P^T slots 2 (k % 4), + 1 of contraction step k / 4.  P in bf16, the matrix cores' operand type; the row sum takes the
+    // unrounded values.
+    auto e_pair = [&](int k) {
+      const int g = k >> 2, x = g >> 1, j = 8 * (g & 1) + 2 * (k & 3);
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(so[x][j], a.c1, off));
+      const float p1 = __builtin_amdgcn_exp2f(fmaf(so[x][j + 1], a.c1, off));
+      l_tile += p0 + p1;
+      uint32_t w = cvt_bf16x2(p0, p1);
+      asm volatile("" : "+v"(l_tile), "+v"(w));
+      pb[g][k & 3] = w;
+    };
+    auto next_k = [&]() { ask(kr, kb, a.kp_p, k_t, a.k_sc, id_k, tile + 2); };
+    auto next_v = [&]() { ask(vr, vb, a.vp_p, v_t, a.v_sc, id_v, tile + 1); };
+    bf16x8 vf[NS];
+    auto first_product = [&](auto e_tag) {
+      constexpr bool EXPS = decltype(e_tag)::value;
+      bf16x8 kf[NS];
+#pragma unroll
+      for (int x = 0; x < KAHEAD; x++) kf[x] = k_read(x);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (EXPS) {
+#pragma unroll
+        for (int k = 0; k < E0; k++) e_pair(k);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int x = 0; x < NS; x++) {
+        if (x + KAHEAD < NS) kf[x + KAHEAD] = k_read(x + KAHEAD);
+        if (x % 3 == 0 && x / 3 < C::CW) conv_k(x / 3, P ^ 1);
+        if (x == 3 * C::CW - 2) next_k();
+        const f32x16 z = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        s[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x], qf[x >> 1], x < 2 ? z : s[x & 1], 0, 0, 0);
+        if constexpr (EXPS) {
+#pragma unroll
+          for (int k = E0 + x * (EQ - E0) / NS; k < E0 + (x + 1) * (EQ - E0) / NS; k++) e_pair(k);
+          if (x >= NS - VAHEAD) vf[x - (NS - VAHEAD)] = v_read(x - (NS - VAHEAD));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    auto mask_keys = [&]() {
+      if (__builtin_expect(tile * 64 + 63 > low, 0)) {
+        int lim = last_key() - (tile * 64 + ((paged_thread() & 32) >> 3));
+        asm volatile("" : "+v"(lim));
+#pragma unroll
+        for (int x = 0; x < 2; x++)
+#pragma unroll
+          for (int j = 0; j < 16; j++) s[x][j] = x * 32 + (j >> 2) * 8 + (j & 3) > lim ? -INFINITY : s[x][j];
+      }
+    };
+    float mloc = -INFINITY;
+    auto max_quad = [&](int q) {
+      const int x = q >> 2, j = 4 * (q & 3);
+      mloc = fmaxf(fmaxf(mloc, s[x][j]), s[x][j + 1]);
+      mloc = fmaxf(fmaxf(mloc, s[x][j + 2]), s[x][j + 3]);
+    };
+    auto second_product = [&]() {
+#pragma unroll
+      for (int x = 0; x < NS; x++) {
+        if (x + VAHEAD < NS) vf[x + VAHEAD] = v_read(x + VAHEAD);
+        oacc[x % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x], __builtin_bit_cast(bf16x8, pb[x / NDT]), oacc[x % NDT], 0, 0, 0);
+        if (EQ + x < 16) e_pair(EQ + x);
+        if (x % 3 == 1 && x / 3 < C::CW) conv_v(x / 3, P);
+        if constexpr (NS == 16) { if (x >= 4 && x < 12) max_quad(x - 4); }
+        else if (x >= 4) { max_quad(2 * (x - 4)); max_quad(2 * (x - 4) + 1); }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      l_run += l_tile;
+      const uint64_t bad = nan_blocks[(P ^ 1) * 4 + (lane & 3)];
+      if (__builtin_expect(__any(bad != 0), 0)) {              // of tile i - 1
+        const int last = last_key();
+        for (int w = 0; w < 4; w++)
+          for (uint64_t left = nan_blocks[(P ^ 1) * 4 + w]; left; left &= left - 1) {
+            const int l = __builtin_ctzll(left), block = (l & 3) * (D / 4) / 32;
+            const bool sees = (tile - 1) * 64 + 16 * w + (l >> 2) <= last;
+#pragma unroll
+            for (int dt = 0; dt < NDT; dt++)
+#pragma unroll
+              for (int j = 0; j < 16; j++) oacc[dt][j] = dt == block && sees ? NAN : oacc[dt][j];
+          }
+      }
+    };
+    if (on) {
+      if (pend) first_product(std::true_type{});
+      else first_product(std::false_type{});
+      mask_keys();
+    } else {
+      asm volatile("" : "=v"(s[0]), "=v"(s[1]));               // nobody reads them
+      if (cur) {
+#pragma unroll
+        for (int c = 0; c < C::CW; c++) conv_k(c, P ^ 1);
+        next_k();
+      }
+      if (pend) {
+#pragma unroll
+        for (int x = 0; x < VAHEAD; x++) vf[x] = v_read(x);
+#pragma unroll
+        for (int k = 0; k < EQ; k++) e_pair(k);
+      }
+    }
+    if (pend) {
+      __builtin_amdgcn_sched_barrier(0);
+      second_product();
+    } else if (cur) {
+#pragma unroll
+      for (int c = 0; c < C::CW; c++) conv_v(c, P);
+    }
+    if (cur) next_v();
+    if (!pend && on) {
+#pragma unroll
+      for (int q = 0; q < 8; q++) max_quad(q);
+    }
+    tmax_old = mloc * a.c1;                                    // this lane half's; a.c1 > 0
+    pend = on;
+  };
+  if (n_it > 0) {
+    f32x16 sa[2], sb[2];
+    for (int i = 0;;) {
+      iteration(std::integral_constant<int, 0>{}, i, sa, sb);
+      if (++i > n_it) break;
+      iteration(std::integral_constant<int, 1>{}, i, sb, sa);
+      if (++i > n_it) break;
+    }
+  }
+  const float l_tot = l_run + __shfl_xor(l_run, 32);
+  {
+  const int lane = paged_thread() & 63, n = lane & 31, h = lane >> 5, t = tw0 + n / a.g, head = r * a.g + n % a.g;   // not kept through the walk
+  const bool row_ok = t < it.m;
+  // The rows go through LDS, each wave's on its own, so that they are written in whole lines: as the output, or unnormalised as a
+  // record of the part.
+  constexpr int LD = D + 4;
+  const bool cut = it.parts > 1;
+  const int64_t rec = (int64_t)r * a.wgs + it.rec0 + it.part;
+  const float inv = l_tot > 0.f ? 1.f / l_tot : l_tot == 0.f ? 0.f : l_tot;    // NaN stays
+  __syncthreads();                                             // nobody reads the tiles any more
+  float* x = reinterpret_cast<float*>(lds) + wave * 32 * LD;
+#pragma unroll
+  for (int dt = 0; dt < NDT; dt++)
+#pragma unroll
+    for (int q4 = 0; q4 < 4; q4++)
+      *reinterpret_cast<f32x4*>(x + n * LD + dt * 32 + q4 * 8 + h * 4) =
+          f32x4{oacc[dt][q4 * 4], oacc[dt][q4 * 4 + 1], oacc[dt][q4 * 4 + 2], oacc[dt][q4 * 4 + 3]};
+  if (h == 0) {
+    x[n * LD + D] = inv;
+    if (row_ok) {
+      if (cut) reinterpret_cast<float2*>(a.part_ml)[rec * 128 + wave * 32 + n] = make_float2(m_run, l_tot);
+      else if (a.lse) a.lse[(int64_t)(it.r0 + t) * a.h_q + head] = l_tot == 0.f ? -INFINITY : (m_run + log2f(l_tot)) * kLn2;
+    }
+  }
+  asm volatile("" ::: "memory");                               // a wave's LDS operations complete in order
+  constexpr int TPR = D / 4;
+  const int c = lane % TPR, rows = min(max(it.m - tw0, 0), Tw) * a.g;
+  for (int i = lane / TPR; i < rows; i += 64 / TPR) {
+    const f32x4 y = *reinterpret_cast<const f32x4*>(x + i * LD + c * 4);
+    if (cut) *reinterpret_cast<f32x4*>(a.part_o + (rec * 128 + wave * 32 + i) * D + c * 4) = y;
+    else put_row4((uint16_t*)a.o + (it.r0 + tw0 + i / a.g) * a.o_t + (r * a.g + i % a.g) * a.o_h + c * 4, y, x[i * LD + D]);
+  }
+  }
 }
+
+// ---- host ------------------------------------------------------------------------------------------------------------
 // fp32: 512 threads for an item, fewer than 2^32 in all, as paged_attend_fits
-bool paged4_attend_fits(const PagedArgs& a, int dtype) { return dtype != DASH_F32 || most_items(a, 16) * a.h_kv < (1 << 23); }
+bool paged4_attend_fits(const PagedArgs& a, int dtype) { return dtype != DASH_F32 || paged_most_items(a, 16) * a.h_kv < (1 << 23); }
+// The kernel for a call, as for pages of bf16.
+static bool use_rows(const PagedArgs& a, int dtype) {
+  return dtype == DASH_BF16 && (int64_t)a.n_rows * a.g > (int64_t)a.batch * 16 && !(a.cap <= 8 * kStep && paged_most_items(a, 16) * a.h_kv <= 256);
+}
 // Workgroups of a kv-head that are resident at once.
-static int runs_of(const PagedArgs& a, int dtype) { return max((dtype == DASH_F32 ? 256 : 768) / a.h_kv, 1); }
+static int runs_of(const PagedArgs& a, int dtype, bool big) { return max((dtype == DASH_F32 ? 256 : big ? 512 : 768) / a.h_kv, 1); }
 static size_t ws_align(size_t x) { return (x + 255) & ~(size_t)255; }
 
 size_t paged4_attend_ws(const PagedArgs& a, int dtype, int d) {
-  const size_t recs = (size_t)runs_of(a, dtype) * a.h_kv * 2 * 16;               // rows of records
-  return ws_align(recs * 8) + recs * d * 4 + recs / 16 * 16;                     // two flags a record of 16 rows
+  const size_t few = (size_t)runs_of(a, dtype, false) * a.h_kv * 2 * 16;         // rows of records
+  const size_t rows = dtype == DASH_BF16 ? (size_t)paged_most_parts(runs_of(a, dtype, true)) * a.h_kv * 128 : 0, recs = few > rows ? few : rows;
+  return ws_align(recs * 8) + recs * d * 4 + few / 16 * 16;                      // two flags a record of 16 rows
 }
 
 template <int D>
 static hipError_t launch_attend4(PagedArgs a, int dtype, char* ws, hipStream_t st) {
-  const int runs = runs_of(a, dtype);
-  const int64_t items = most_items(a, 16);
-  a.wgs = items < 8 * (int64_t)runs ? runs : 0;
+  const bool big = use_rows(a, dtype);
+  const int runs = runs_of(a, dtype, big);
+  const int64_t items = paged_most_items(a, big ? 128 : 16);
+  a.wgs = items < (big ? 2 : 8) * (int64_t)runs ? runs : 0;
+  if (big && a.wgs && items * 4 >= runs) a.wgs = (int)items + runs * 3 / 2;
   a.slots = runs;
+  a.gain = (int64_t)a.n_rows * a.g < 64 * items ? 0.65f : 0.9f;
   a.whole = items * 2 >= runs;                               // fewer items: not looked into
-  if (a.cap <= 8 * kStep && items * a.h_kv >= 128) a.wgs = 0;
-  const size_t recs = (size_t)a.wgs * a.h_kv * 2 * 16;
+  if (!big && a.cap <= 8 * kStep && items * a.h_kv >= 128) a.wgs = 0;
+  const size_t recs = (size_t)a.wgs * a.h_kv * (big ? 128 : 2 * 16);
   a.part_ml = (float*)ws;
   a.part_o = (float*)(ws + ws_align(recs * 8));
-  a.flags = (uint64_t*)((char*)a.part_o + recs * D * 4);
-  a.nonce = next_nonce();
+  a.flags = (uint64_t*)((char*)a.part_o + recs * D * 4);     // runs only
+  a.nonce = big ? 0 : next_nonce();
   const dim3 grid((unsigned)((a.wgs ? a.wgs : items) * a.h_kv));
+  if (big) {
+    static LdsOptIn opt_in;
+    if (hipError_t e = allow_dyn_lds((const void*)paged_rows4_kernel<D>, Rows4Cfg<D>::LDS_BYTES, opt_in); e != hipSuccess) return e;
+    hipLaunchKernelGGL(paged_rows4_kernel<D>, grid, dim3(256), Rows4Cfg<D>::LDS_BYTES, st, a);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || a.wgs <= 1 ? e : launch_paged_merge(a, D, st);
+  }
   if (dtype == DASH_BF16) {
     static LdsOptIn opt_in;
     if (hipError_t e = allow_dyn_lds((const void*)paged_few4_kernel<D>, Few4Cfg<D>::LDS_BYTES, opt_in); e != hipSuccess) return e;

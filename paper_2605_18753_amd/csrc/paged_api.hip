@@ -164,7 +164,8 @@ int dash_paged4_append(const dash_paged_params* p, const dash_rotary* r, const v
   if (r)
     if (const int rc = rotary_args(r, p->head_dim, &turn); rc != DASH_OK) return rc;
   if (!q != !q_out || (q && !r) || !k_new || !v_new || !k_codes || !k_scales || !v_codes || !v_scales || !row_start || !lens || !table) return DASH_EINVAL;
-  if (misaligned(q) || misaligned(q_out) || misaligned(k_new) || misaligned(v_new) || misaligned(k_codes) || misaligned(v_codes)) return DASH_EINVAL;
+  if (misaligned(q) || misaligned(q_out) || misaligned(k_new) || misaligned(v_new) || misaligned(k_codes) || misaligned(v_codes) ||
+      misaligned(k_scales) || misaligned(v_scales)) return DASH_EINVAL;
   if (q && q == q_out && (a.q_t != a.o_t || a.q_h != a.o_h)) return DASH_EINVAL;
   a.q = q; a.o = q_out; a.k_new = k_new; a.v_new = v_new; a.k = k_codes; a.v = v_codes; a.k_sc = (const uint8_t*)k_scales; a.v_sc = (const uint8_t*)v_scales;
   a.row_start = row_start; a.lens = lens; a.table = table; a.seen = seen;
@@ -177,7 +178,7 @@ int dash_paged4_attend(const dash_paged_params* p, const void* q, const void* k_
   PagedArgs a;
   if (const int rc = paged_args(p, &a, true, false, true); rc != DASH_OK) return rc;
   if (!q || !k_codes || !k_scales || !v_codes || !v_scales || !row_start || !lens || !table || !o) return DASH_EINVAL;
-  if (misaligned(q) || misaligned(k_codes) || misaligned(v_codes) || misaligned(o)) return DASH_EINVAL;
+  if (misaligned(q) || misaligned(k_codes) || misaligned(v_codes) || misaligned(k_scales) || misaligned(v_scales) || misaligned(o)) return DASH_EINVAL;
   if (!paged4_attend_fits(a, p->dtype)) return DASH_EUNSUPPORTED;
   if (const int rc = check_scratch(paged4_attend_ws(a, p->dtype, p->head_dim), workspace, workspace_bytes); rc != DASH_OK) return rc;
   a.q = q; a.k = (void*)k_codes; a.v = (void*)v_codes; a.k_sc = (const uint8_t*)k_scales; a.v_sc = (const uint8_t*)v_scales; a.o = o; a.lse = lse;
@@ -190,7 +191,7 @@ int dash_paged4_unpack(const dash_paged_params* p, const void* k_codes, const vo
   PagedArgs a;
   if (const int rc = paged_args(p, &a, false, false, true); rc != DASH_OK) return rc;
   if (!k_codes || !k_scales || !v_codes || !v_scales || !k_pages || !v_pages) return DASH_EINVAL;
-  if (misaligned(k_codes) || misaligned(v_codes) || misaligned(k_pages) || misaligned(v_pages)) return DASH_EINVAL;
+  if (misaligned(k_codes) || misaligned(v_codes) || misaligned(k_scales) || misaligned(v_scales) || misaligned(k_pages) || misaligned(v_pages)) return DASH_EINVAL;
   a.k = (void*)k_codes; a.v = (void*)v_codes; a.k_sc = (const uint8_t*)k_scales; a.v_sc = (const uint8_t*)v_scales;
   return launch_paged4_unpack(a, k_pages, v_pages, p->dtype == DASH_BF16 ? 2 : 4, p->head_dim, (hipStream_t)stream) == hipSuccess ? DASH_OK : DASH_ELAUNCH;
 }

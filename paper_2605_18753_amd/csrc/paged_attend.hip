@@ -193,12 +193,6 @@ template <int D> struct RowsCfg {
   static constexpr int LDS_BYTES = 4 * TILE_BYTES > OUT_BYTES ? 4 * TILE_BYTES : OUT_BYTES;   // K ring [2], V ring [2]
 };
 
-// tiles of 128 rows of a sequence; cost: their steps of 64 keys
-__device__ __forceinline__ int2 rows_shape(const PagedArgs& a, int m, int n) {
-  const int T = 128 / a.g;
-  return make_int2((m + T - 1) / T, max((n + 63) >> 6, 1));
-}
-
 template <int D>
 __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
   using C = RowsCfg<D>;
@@ -548,37 +542,42 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
-static int64_t most_items(const PagedArgs& a, int rows) {   // of a kv-head
-  const int T = rows / a.g;
-  return min((int64_t)a.n_rows / T + min(a.batch, a.n_rows), (int64_t)a.n_rows);
-}
 // A launch of 2^32 threads or more loses some without an error.  fp32: 512 for an item (bf16: 256, and fewer than 2^22 items whatever the limits of
 // n_rows h_q and batch h_kv allow).
-bool paged_attend_fits(const PagedArgs& a, int dtype) { return dtype != DASH_F32 || most_items(a, 16) * a.h_kv < (1 << 23); }
+bool paged_attend_fits(const PagedArgs& a, int dtype) { return dtype != DASH_F32 || paged_most_items(a, 16) * a.h_kv < (1 << 23); }
 // The kernel for a call: tiles of 128 rows where the sequences bring more than 16 rows each on the average, tiles of 16 otherwise.  (32 / 8 heads, tiles of 128
 // and of 16, sequences with like numbers of rows.  16 rows each: 64 sequences of 2000 tokens 99.6 and 97.7 us, one of 1000 14.7 and 11.0; 20 rows: 101 and 167, 8 of 16000 104 and 103; 48
 // rows: 108 and 281.)  Short caches are read from the last-level cache again and again at no cost: tiles of 16 as long as each has a CU (one
 // of 1000 tokens, 64 rows 15.9 and 12.4 us, 128 17.3 and 11.8).  The average hides a long piece beside many single tokens: 380 tokens of a sequence of 8000
 // beside 127 sequences of 200 with one each, 507 in all, take tiles of 16 and 458 us, 400 of them tiles of 128 and 147.
 static bool use_rows(const PagedArgs& a, int dtype) {
-  return dtype == DASH_BF16 && (int64_t)a.n_rows * a.g > (int64_t)a.batch * 16 && !(a.cap <= 8 * kStep && most_items(a, 16) * a.h_kv <= 256);
+  return dtype == DASH_BF16 && (int64_t)a.n_rows * a.g > (int64_t)a.batch * 16 && !(a.cap <= 8 * kStep && paged_most_items(a, 16) * a.h_kv <= 256);
 }
 // Workgroups of a kv-head that are resident at once: one a CU for the 128 KB ring of 16-row tiles and the fp32 kernel, two otherwise.
 static int runs_of(const PagedArgs& a, int dtype, int d, bool big) { return max((!big && (dtype == DASH_F32 || d == 128) ? 256 : 512) / a.h_kv, 1); }
-static int most_parts(int runs) { return runs * 7 / 2; }   // of a kv-head: fewer than two items a resident workgroup, and one and a half
 static size_t ws_align(size_t x) { return (x + 255) & ~(size_t)255; }
 
 size_t paged_attend_ws(const PagedArgs& a, int dtype, int d) {
   const size_t few = (size_t)runs_of(a, dtype, d, false) * a.h_kv * 2 * 16;    // rows of records
-  const size_t rows = dtype == DASH_BF16 ? (size_t)most_parts(runs_of(a, dtype, d, true)) * a.h_kv * 128 : 0, recs = few > rows ? few : rows;
+  const size_t rows = dtype == DASH_BF16 ? (size_t)paged_most_parts(runs_of(a, dtype, d, true)) * a.h_kv * 128 : 0, recs = few > rows ? few : rows;
   return ws_align(recs * 8) + recs * d * 4 + few / 16 * 16;   // two flags a record of 16 rows
 }
+
+template <int D> static hipError_t launch_merge(const PagedArgs& a, hipStream_t st) {
+  // few rows leave the chip idle unless several groups of threads share a row's parts (1280 rows, the call: 32.8 us shared, 34.0 not; 2048 59.4 and 58.0)
+  const int64_t out = (int64_t)a.n_rows * a.h_q;
+  constexpr int units = 256 / (D / 4);
+  if (out <= 1536) hipLaunchKernelGGL((paged_merge_kernel<D, 4>), dim3((unsigned)((out + units / 4 - 1) / (units / 4))), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((paged_merge_kernel<D, 1>), dim3(1024), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+hipError_t launch_paged_merge(const PagedArgs& a, int d, hipStream_t st) { return d == 128 ? launch_merge<128>(a, st) : launch_merge<64>(a, st); }
 
 template <int D>
 static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st) {
   const bool big = use_rows(a, dtype);
   const int runs = runs_of(a, dtype, D, big);
-  const int64_t items = most_items(a, big ? 128 : 16);
+  const int64_t items = paged_most_items(a, big ? 128 : 16);
   // Runs of small tiles cost little (a record is 16 rows) and even out the lengths of a batch; with many items a workgroup each evens them out as well.  (A
   // token of 64 sequences of 1000 to 4000 tokens, 32 / 8 heads, 119 us in runs, 122 without; of 256, 8 items a run, 454 both ways.  Tiles of 128: 700
   // tokens against 32k 435 in parts, 641 without; two of 700 against 4k 115 and 113.)
@@ -611,14 +610,8 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
     if (hipError_t e = allow_dyn_lds((const void*)(paged_few_f32_kernel<D, false>), lds, opt_in); e != hipSuccess) return e;
     hipLaunchKernelGGL((paged_few_f32_kernel<D, false>), grid, dim3(512), lds, st, a);
   }
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.wgs <= 1 || !big) return e;
-  // few rows leave the chip idle unless several groups of threads share a row's parts (1280 rows, the call: 32.8 us shared, 34.0 not; 2048 59.4 and 58.0)
-  const int64_t out = (int64_t)a.n_rows * a.h_q;
-  constexpr int units = 256 / (D / 4);
-  if (out <= 1536) hipLaunchKernelGGL((paged_merge_kernel<D, 4>), dim3((unsigned)((out + units / 4 - 1) / (units / 4))), blk, 0, st, a);
-  else hipLaunchKernelGGL((paged_merge_kernel<D, 1>), dim3(1024), blk, 0, st, a);
-  return hipGetLastError();
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || a.wgs <= 1 || !big ? e : launch_paged_merge(a, D, st);
 }
 
 hipError_t launch_paged_attend(const PagedArgs& a, int dtype, int d, char* ws, hipStream_t st) {

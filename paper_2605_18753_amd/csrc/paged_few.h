@@ -318,4 +318,17 @@ __global__ __launch_bounds__(512) void paged_few_f32_kernel(PagedArgs args) {
   } while (run.advance(args));
 }
 
+// tiles of 128 rows of a sequence; cost: their steps of 64 keys
+__device__ __forceinline__ int2 rows_shape(const PagedArgs& a, int m, int n) {
+  const int T = 128 / a.g;
+  return make_int2((m + T - 1) / T, max((n + 63) >> 6, 1));
+}
+
+inline int64_t paged_most_items(const PagedArgs& a, int rows) {   // of a kv-head
+  const int T = rows / a.g;
+  return min((int64_t)a.n_rows / T + min(a.batch, a.n_rows), (int64_t)a.n_rows);
+}
+inline int paged_most_parts(int runs) { return runs * 7 / 2; }   // of a kv-head: fewer than two items a resident workgroup, and one and a half
+hipError_t launch_paged_merge(const PagedArgs& a, int d, hipStream_t st);
+
 }  // namespace dash

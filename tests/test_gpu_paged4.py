@@ -395,18 +395,18 @@ def test_two_captured_graphs_and_eager_calls_between_them(dtype):
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             B.dash_paged4_attend(p, s.gpu, q, s.start_gpu, o, ws, lse=lse)
-        runs.append((graph, o, lse))
+        runs.append((graph, o, lse, ws))                         # a graph's workspace lives as long as it
     for lens in ([3000, 700, 40], [2999, 1, 0], [5, 700, 33], [3000, 700, 40]):
         s.gpu.lens.copy_(torch.tensor(lens))
         want = s.attend()
         streams = [torch.cuda.Stream() for _ in runs]
-        for st, (graph, o, lse) in zip(streams, runs):
+        for st, (graph, o, lse, _) in zip(streams, runs):
             st.wait_stream(torch.cuda.current_stream())
             with torch.cuda.stream(st):
                 o.zero_()
                 graph.replay()
         torch.cuda.synchronize()
-        for _, o, lse in runs:
+        for _, o, lse, _ in runs:
             assert torch.equal(o.cpu(), want[0]) and torch.equal(lse.cpu(), want[1])
 
 

@@ -189,7 +189,7 @@ def test_null_and_misaligned_pointers(name, needed):
     p = params() if name == "rotary" else params4()
     for x in needed:
         assert call4(name, p, plan(), **{x: None}) == -1, x
-    for x in set(needed) & {"k_new", "v_new", "q", "k", "v", "o", "k_out", "v_out"}:
+    for x in set(needed) & {"k_new", "v_new", "q", "k", "v", "ks", "vs", "o", "k_out", "v_out"}:
         assert call4(name, p, plan(), **{x: 264}) == -1, x
 
 
