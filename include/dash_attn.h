@@ -480,7 +480,7 @@ int dash_paged4_attend(const dash_paged_params* p, const void* q, const void* k_
                        void* workspace, size_t workspace_bytes, void* stream);
 
 /* The cache's values as pages of the run dtype, for calls that read those: k_pages, v_pages [n_pages, h_kv, page_size, d] contiguous.  Every token of every
- * page is written (rows that were never appended as their bytes say). */
+ * page is written (rows that were never appended as their bytes say).  n_pages * h_kv up to 2^30 (DASH_EUNSUPPORTED). */
 int dash_paged4_unpack(const dash_paged_params* p, const void* k_codes, const void* k_scales, const void* v_codes,
                        const void* v_scales, void* k_pages, void* v_pages, void* stream);
 

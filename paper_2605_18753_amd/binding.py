@@ -555,65 +555,100 @@ def _gpu_stream(dev: int):
     return _raw_stream(dev)
 
 
-def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
-    span = lambda t: (t.data_ptr(), t.data_ptr() + t.element_size() * (1 + sum((n - 1) * s for n, s in zip(t.shape, t.stride()))))  # noqa: E731
-    (a0, a1), (b0, b1) = span(a), span(b)
+def _span(ptr, shape, strides, size):
+    """The bytes that a tensor's elements lie in: the first, and the one behind the last."""
+    last = 0
+    for n, s in zip(shape, strides):
+        last += (n - 1) * s
+    return ptr, ptr + (last + 1) * size
+
+
+def _lies_on(x, x_ptr, x_strides, y, y_ptr, y_strides) -> bool:
+    """Whether an output overlaps its input without being it."""
+    if x_ptr == y_ptr and x_strides == y_strides:
+        return False
+    size = x.element_size()
+    (a0, a1), (b0, b1) = _span(x_ptr, x.shape, x_strides, size), _span(y_ptr, y.shape, y_strides, size)
     return a0 < b1 and b0 < a1
+
+
+_ROTARY_PARAMS = struct.Struct("10i13q")                   # dash_rotary_params
+_NO_STRIDES = (0, 0, 0)
+
+
+def _rotary_pair(x, y):
+    """Checks an input and its output; their shape, and the strides, first byte and byte behind the last of each."""
+    if x is None or y is None or x.dtype is not y.dtype or x.dtype not in _PAGED_TYPES:
+        raise DashError("rotary tensors: input and output of one type, bf16 or fp32")
+    shape = tuple(x.shape)
+    if len(shape) != 4 or shape != y.shape or 0 in shape:
+        raise DashError("rotary tensors: input and output [batch, heads, tokens, head_dim], no size 0")
+    b, h, n, d = shape
+    xs, ys, xp, yp, size = x.stride(), y.stride(), x.data_ptr(), y.data_ptr(), x.element_size()
+    if xs[3] != 1 or ys[3] != 1:
+        raise DashError("head_dim must be contiguous")
+    if 0 in ys and any(m > 1 and s == 0 for m, s in zip(shape, ys)):
+        raise DashError("an output has an element for each of its own")
+    x_end = xp + ((b - 1) * xs[0] + (h - 1) * xs[1] + (n - 1) * xs[2] + d) * size
+    y_end = yp + ((b - 1) * ys[0] + (h - 1) * ys[1] + (n - 1) * ys[2] + d) * size
+    if xp < y_end and yp < x_end and (xp != yp or xs != ys):
+        raise DashError("an output is its input or does not overlap it")
+    return shape, (xs, xp, x_end), (ys, yp, y_end)
 
 
 def dash_rotary(r: Rotary, q, q_out, k=None, k_out=None, pos=None, start: int = 0, inverse: bool = False) -> None:
     """q, q_out [batch, h_q, n_q, d] and k, k_out [batch, h_kv, n_kv, d], each pair None or given; an output may be its input.  pos int32 [tokens] or
     [batch, tokens] (tokens: n_kv, or n_q without k; query t has the position of token n_kv - n_q + t), None: token t has position t.  inverse: turns
     back, which takes the gradient of an output to that of its input."""
-    pairs = [(x, y, name) for x, y, name in ((q, q_out, "q"), (k, k_out, "k")) if x is not None or y is not None]
-    if not pairs:
-        raise DashError("dash_rotary: q, k or both")
-    lead = pairs[0][0]
-    p = dash_rotary_params()
-    for x, y, name in pairs:
-        if x is None or y is None or x.dim() != 4 or y.shape != x.shape or x.dtype is not lead.dtype or y.dtype is not x.dtype or x.dtype not in _PAGED_TYPES:
-            raise DashError("rotary tensors: input and output [batch, heads, tokens, head_dim] of one type, bf16 or fp32")
-        if x.shape[0] != lead.shape[0] or x.shape[3] != lead.shape[3] or 0 in x.shape:
-            raise DashError("q and k have the same batch and head dimension, and no size is 0")
-        if x.stride(3) != 1 or y.stride(3) != 1:
-            raise DashError("head_dim must be contiguous")
-        if x.get_device() != lead.get_device() or y.get_device() != lead.get_device():
+    batch = h_q = n_q = h_kv = n_kv = 0
+    qs = qos = ks = kos = _NO_STRIDES
+    qp = qop = kp = kop = None
+    if q is not None or q_out is not None:
+        (batch, h_q, n_q, d), q_in, q_to = _rotary_pair(q, q_out)
+        (qs, qp, _), (qos, qop, _) = q_in, q_to
+        dtype, dev = q.dtype, q.get_device()
+        if q_out.get_device() != dev:
             raise DashError("the tensors lie on one device")
-        if any(n > 1 and s == 0 for n, s in zip(y.shape, y.stride())):
-            raise DashError("an output has an element for each of its own")
-        if not (x.data_ptr() == y.data_ptr() and x.stride() == y.stride()) and _overlap(x, y):
-            raise DashError("an output is its input or does not overlap it")
-        getattr(p, f"{name}_stride")[:], getattr(p, f"{name}_out_stride")[:] = x.stride()[:3], y.stride()[:3]
-    if len(pairs) == 2 and (_overlap(q_out, k_out) or _overlap(q_out, k) or _overlap(k_out, q)) and not _interleaved(pairs):
-        raise DashError("the outputs overlap neither each other nor the other's input")
-    _int32(start=start)
-    p.batch, p.head_dim = lead.shape[0], lead.shape[3]
-    p.dtype, p.inverse, p.start = _PAGED_TYPES[lead.dtype], int(inverse), start
-    if q is not None:
-        p.h_q, p.n_q = q.shape[1], q.shape[2]
-    if k is not None:
-        p.h_kv, p.n_kv = k.shape[1], k.shape[2]
-    dev = lead.get_device()
+    if k is not None or k_out is not None:
+        (k_batch, h_kv, n_kv, k_d), k_in, k_to = _rotary_pair(k, k_out)
+        (ks, kp, _), (kos, kop, _) = k_in, k_to
+        if batch == 0:
+            batch, d, dtype, dev = k_batch, k_d, k.dtype, k.get_device()
+        elif k_batch != batch or k_d != d or k.dtype is not dtype:
+            raise DashError("q and k have the same batch, head dimension and type")
+        else:
+            # an output overlaps neither the other output nor the other's input
+            size = q.element_size()
+            for x, hx, y, hy in ((q_to, h_q, k_to, h_kv), (q_to, h_q, k_in, h_kv), (k_to, h_kv, q_in, h_q)):
+                if x[1] < y[2] and y[1] < x[2] and not _apart(x, hx, y, hy, d, size):
+                    raise DashError("the outputs overlap neither each other nor the other's input")
+        if k.get_device() != dev or k_out.get_device() != dev:
+            raise DashError("the tensors lie on one device")
+    if batch == 0:
+        raise DashError("dash_rotary: q, k or both")
+    pos_stride = 0
     if pos is not None:
-        tokens = (k if k is not None else q).shape[2]
-        if pos.dtype is not _INT or tuple(pos.shape) not in ((tokens,), (p.batch, tokens)) or (tokens > 1 and pos.stride(-1) != 1) or pos.get_device() != dev:
+        tokens, shape = n_kv or n_q, tuple(pos.shape)
+        if pos.dtype is not _INT or shape not in ((tokens,), (batch, tokens)) or (tokens > 1 and pos.stride(-1) != 1) or pos.get_device() != dev:
             raise DashError("pos: int32 [tokens] or [batch, tokens], tokens contiguous, on the tensors' device")
-        p.pos_stride = pos.stride(0) if pos.dim() == 2 and p.batch > 1 else 0
+        if len(shape) == 2 and batch > 1:
+            pos_stride = pos.stride(0)
+    try:
+        p = dash_rotary_params.from_buffer_copy(_ROTARY_PARAMS.pack(batch, h_q, h_kv, n_q, n_kv, d, _PAGED_TYPES[dtype], 1 if inverse else 0, start, 0, pos_stride,
+                                                                    *qs[:3], *qos[:3], *ks[:3], *kos[:3]))
+    except struct.error:
+        raise DashError("sizes and start: numbers that fit 32 bits") from None
     plan, stream = _rotary_plan(r, dev), _gpu_stream(dev)
-    _check(load_library().dash_rotary_apply(p, plan, _ptr(pos), _ptr(q), _ptr(q_out), _ptr(k), _ptr(k_out), stream), "dash_rotary_apply")
+    _check(load_library().dash_rotary_apply(p, plan, _ptr(pos), qp, qop, kp, kop, stream), "dash_rotary_apply")
 
 
-def _interleaved(pairs) -> bool:
-    """Whether q and k are heads of one tensor (their memory interleaved): the same strides, and starts within one token's row."""
-    (q, q_out, _), (k, k_out, _) = pairs
-    def apart(a, b):
-        if a.stride() != b.stride():
-            return False
-        first, then = (a, b) if a.data_ptr() <= b.data_ptr() else (b, a)
-        off = (then.data_ptr() - first.data_ptr()) // a.element_size()
-        s, heads = a.stride(), first.shape[1]
-        return (heads - 1) * s[1] + a.shape[3] <= off and off + (then.shape[1] - 1) * s[1] + a.shape[3] <= s[2]
-    return all(not _overlap(a, b) or apart(a, b) for a, b in ((q_out, k_out), (q_out, k), (k_out, q)))
+def _apart(x, x_heads, y, y_heads, d, size) -> bool:
+    """Whether tensors in each other's span are heads of one tensor (queries and keys of a fused projection): the same strides, and starts within one token's
+    row that keep their heads apart."""
+    (s, x_ptr, _), (t, y_ptr, _) = x, y
+    first, off = (x_heads, y_ptr - x_ptr) if x_ptr <= y_ptr else (y_heads, x_ptr - y_ptr)
+    then = x_heads + y_heads - first
+    return s == t and (first - 1) * s[1] + d <= off // size and off // size + (then - 1) * s[1] + d <= s[2]
 
 
 def dash_paged_append_rotary(p: dash_paged_params, cache: PagedCache, rotary: Rotary, k_new, v_new, row_start, q=None, q_out=None) -> None:
@@ -628,14 +663,13 @@ def dash_paged_append_rotary(p: dash_paged_params, cache: PagedCache, rotary: Ro
 
 
 def _fresh_rows(p, k_new, v_new, q, q_out):
-    rows = ((k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride"))
-    if (q is None) != (q_out is None):
+    if q is None and q_out is None:
+        return (k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride")
+    if q is None or q_out is None:
         raise DashError("q and q_out: both or none")
-    if q is None:
-        return rows
-    if not (q.data_ptr() == q_out.data_ptr() and q.stride() == q_out.stride()) and _overlap(q, q_out):
+    if _lies_on(q, q.data_ptr(), q.stride(), q_out, q_out.data_ptr(), q_out.stride()):
         raise DashError("q_out is q or does not overlap it")
-    return rows + ((q, p.h_q, "q_stride"), (q_out, p.h_q, "o_stride"))
+    return (k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride"), (q, p.h_q, "q_stride"), (q_out, p.h_q, "o_stride")
 
 
 # ---- paged cache in 4 bits -------------------------------------------------------------------------------------------

@@ -67,7 +67,7 @@ __device__ __forceinline__ uint32_t flipped(uint32_t addr, int bits) {
 }
 
 template <int D>
-__global__ __launch_bounds__(256, D == 128 ? 3 : 4) void paged_few4_kernel(PagedArgs args) {
+__global__ __launch_bounds__(256, D == 128 ? 2 : 4) void paged_few4_kernel(PagedArgs args) {
   using C = Few4Cfg<D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int r = blockIdx.x % args.h_kv, wg = blockIdx.x / args.h_kv;
@@ -187,11 +187,15 @@ __global__ __launch_bounds__(256, D == 128 ? 3 : 4) void paged_few4_kernel(Paged
     const u32x4 pw = {cvt_bf16x2(p[0], p[1]), cvt_bf16x2(p[2], p[3]), cvt_bf16x2(p[4], p[5]), cvt_bf16x2(p[6], p[7])};
     const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
     asm volatile("" ::: "memory");                                               // a wave's LDS operations complete in order
+    bf16x8 vf[D / 16];
 #pragma unroll
     for (int dt = 0; dt < D / 16; dt++) {
       const uint32_t at = flipped(v_rd, dt << 5);
-      oacc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lds_read_tr_pair(at, at + 16 * C::ROW_BYTES), pb, oacc[dt], 0, 0, 0);
+      vf[dt] = lds_read_tr_pair(at, at + 16 * C::ROW_BYTES);
     }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int dt = 0; dt < D / 16; dt++) oacc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[dt], pb, oacc[dt], 0, 0, 0);
     asm volatile("" ::: "memory");
     if (__builtin_expect(__any(vs[0] == 255u || vs[1] == 255u), 0)) {
 #pragma unroll
@@ -544,20 +548,20 @@ bool paged4_attend_fits(const PagedArgs& a, int dtype) { return dtype != DASH_F3
 static bool use_rows(const PagedArgs& a, int dtype) {
   return dtype == DASH_BF16 && (int64_t)a.n_rows * a.g > (int64_t)a.batch * 16 && !(a.cap <= 8 * kStep && paged_most_items(a, 16) * a.h_kv <= 256);
 }
-// Workgroups of a kv-head that are resident at once.
-static int runs_of(const PagedArgs& a, int dtype, bool big) { return max((dtype == DASH_F32 ? 256 : big ? 512 : 768) / a.h_kv, 1); }
+// Workgroups of a kv-head that are resident at once (16-row tiles at head dimension 64: three of four).
+static int runs_of(const PagedArgs& a, int dtype, int d, bool big) { return max((dtype == DASH_F32 ? 256 : big || d == 128 ? 512 : 768) / a.h_kv, 1); }
 static size_t ws_align(size_t x) { return (x + 255) & ~(size_t)255; }
 
 size_t paged4_attend_ws(const PagedArgs& a, int dtype, int d) {
-  const size_t few = (size_t)runs_of(a, dtype, false) * a.h_kv * 2 * 16;         // rows of records
-  const size_t rows = dtype == DASH_BF16 ? (size_t)paged_most_parts(runs_of(a, dtype, true)) * a.h_kv * 128 : 0, recs = few > rows ? few : rows;
+  const size_t few = (size_t)runs_of(a, dtype, d, false) * a.h_kv * 2 * 16;         // rows of records
+  const size_t rows = dtype == DASH_BF16 ? (size_t)paged_most_parts(runs_of(a, dtype, d, true)) * a.h_kv * 128 : 0, recs = few > rows ? few : rows;
   return ws_align(recs * 8) + recs * d * 4 + few / 16 * 16;                      // two flags a record of 16 rows
 }
 
 template <int D>
 static hipError_t launch_attend4(PagedArgs a, int dtype, char* ws, hipStream_t st) {
   const bool big = use_rows(a, dtype);
-  const int runs = runs_of(a, dtype, big);
+  const int runs = runs_of(a, dtype, D, big);
   const int64_t items = paged_most_items(a, big ? 128 : 16);
   a.wgs = items < (big ? 2 : 8) * (int64_t)runs ? runs : 0;
   if (big && a.wgs && items * 4 >= runs) a.wgs = (int)items + runs * 3 / 2;

@@ -191,6 +191,7 @@ int dash_paged4_unpack(const dash_paged_params* p, const void* k_codes, const vo
   PagedArgs a;
   if (const int rc = paged_args(p, &a, false, false, true); rc != DASH_OK) return rc;
   if (!k_codes || !k_scales || !v_codes || !v_scales || !k_pages || !v_pages) return DASH_EINVAL;
+  if ((int64_t)p->n_pages * p->h_kv > 1 << 30) return DASH_EUNSUPPORTED;   // heads of pages are counted in 32 bits
   if (misaligned(k_codes) || misaligned(v_codes) || misaligned(k_scales) || misaligned(v_scales) || misaligned(k_pages) || misaligned(v_pages)) return DASH_EINVAL;
   a.k = (void*)k_codes; a.v = (void*)v_codes; a.k_sc = (const uint8_t*)k_scales; a.v_sc = (const uint8_t*)v_scales;
   return launch_paged4_unpack(a, k_pages, v_pages, p->dtype == DASH_BF16 ? 2 : 4, p->head_dim, (hipStream_t)stream) == hipSuccess ? DASH_OK : DASH_ELAUNCH;

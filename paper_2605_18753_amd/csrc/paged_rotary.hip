@@ -11,49 +11,75 @@ static dim3 rows_grid(int n_rows) {
   return dim3((unsigned)(wgs < most ? wgs : most), (unsigned)((wgs + most - 1) / most));
 }
 
-// Turns the row's heads h0, h0 + step, .. (units of 16 elements, rotary_unit), from and to rows of heads.
-template <typename T>
-__device__ __forceinline__ void turn_heads(const RotaryArgs& r, const float2 (&cs)[8], int u, const T* from, int64_t from_h, T* to, int64_t to_h,
-                                           int h0, int step, int heads) {
-  const int2 at = rotary_unit(r, u);
-  const bool turns = 8 * u < r.half;
-  for (int h = h0; h < heads; h += step) {
-    Eight p = load_eight(from + h * from_h + at.x), q = load_eight(from + h * from_h + at.y);
-    if (turns) turn_unit(p, q, cs, r.adjacent);
-    store_eight(to + h * to_h + at.x, p);
-    store_eight(to + h * to_h + at.y, q);
+// A row's heads h0, h0 + step, .., turned: the first N asked for before anything is known about the row.
+template <typename T, int D, int N> struct Heads {
+  using U = Unit<T, D>;
+  typename U::Data x[N];
+  __device__ __forceinline__ void ask(const U& unit, const T* row, int64_t stride, int h0, int step, int heads) {
+#pragma unroll
+    for (int i = 0; i < N; i++)
+      if (h0 + i * step < heads) x[i] = unit.load(row + (h0 + i * step) * stride);
   }
-}
+  __device__ __forceinline__ void turn(const U& unit, const typename U::Pairs& cs, bool adjacent, const T* row, int64_t stride, int h0, int step, int heads,
+                                       T* to, int64_t to_stride) {
+    for (int h = h0; h < heads; h += N * step) {
+      if (h != h0) ask(unit, row, stride, h, step, heads);
+#pragma unroll
+      for (int i = 0; i < N; i++)
+        if (h + i * step < heads) unit.store(to + (h + i * step) * to_stride, x[i], cs, adjacent);
+    }
+  }
+};
 
-// A wave has a packed row: a lane works out the cosine and sine of a pair, into LDS, and takes those of its unit's eight pairs from there.
+// A wave has a packed row.  What the row holds is asked for first, with the turns; then the row's place is found, a lane works out the cosine and sine of a
+// pair, into LDS, and takes those of its unit's eight pairs from there.
+// (2047 tokens of each of four sequences, 32 / 8 heads of 128, two heads asked for ahead 44.8 us, four, which costs registers and waves, 47.8.)
 template <typename T, int D>
-__global__ __launch_bounds__(256) void paged_append_rotary_kernel(PagedArgs a, RotaryArgs r) {
-  constexpr int UNITS = D / 16, HEADS = 64 / UNITS, CHUNK = 16 / sizeof(T), CHUNKS = D / CHUNK;
+__global__ __launch_bounds__(256, 4) void paged_append_rotary_kernel(PagedArgs a, RotaryArgs r) {
+  using U = Unit<T, D>;
+  constexpr int HEADS = 64 / U::COUNT, CHUNK = 16 / sizeof(T), CHUNKS = D / CHUNK, NV = 2;
   __shared__ float2 table[4][D / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = (int)(blockIdx.y << kGridLog | blockIdx.x) * 4 + wave;
   if (row >= a.n_rows) return;
+  const int h0 = lane / U::COUNT;
+  const U unit(r, lane % U::COUNT);
+  const T* kn = (const T*)a.k_new + row * a.kn_t;
+  const T* vn = (const T*)a.v_new + row * a.vn_t;
+  const T* qn = (const T*)a.q + row * a.q_t;
+  const uint64_t turns = r.turns[min(lane, r.half - 1)];
+  Heads<T, D, 1> k;
+  Heads<T, D, 2> q;
+  u32x4 v[NV];
+  k.ask(unit, kn, a.kn_h, h0, HEADS, a.h_kv);
+  auto ask_v = [&](int x0) {
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int x = x0 + 64 * i;
+      if (x < a.h_kv * CHUNKS) v[i] = *reinterpret_cast<const u32x4*>(vn + x / CHUNKS * a.vn_h + x % CHUNKS * CHUNK);
+    }
+  };
+  ask_v(lane);
+  if (a.q) q.ask(unit, qn, a.q_h, h0, HEADS, a.h_q);
   PagedPlace at;
   if (!paged_place(a, row, at)) return;
   const uint32_t page = (uint32_t)paged_entry(a, at.b, at.slot >> a.page_log);
-  if (lane < r.half) {
-    const double2 t = rotary_cos_sin(r, lane, at.position);
-    table[wave][lane] = make_float2((float)t.x, (float)t.y);
-  }
+  const double2 t = rotary_cos_sin(r, turns, at.position);
+  table[wave][min(lane, D / 2 - 1)] = make_float2((float)t.x, (float)t.y);       // lanes behind the last pair: no one's
   asm volatile("" ::: "memory");                             // a wave's LDS operations complete in order
-  const int u = lane % UNITS, h0 = lane / UNITS;
-  float2 cs[8];
-#pragma unroll
-  for (int i = 0; i < 8; i++) cs[i] = table[wave][min(8 * u, r.half - 8) + i];
-  if (a.q) turn_heads(r, cs, u, (const T*)a.q + row * a.q_t, a.q_h, (T*)a.o + row * a.o_t, a.o_h, h0, HEADS, a.h_q);
+  const typename U::Pairs cs = unit.pairs(table[wave]);
+  if (a.q) q.turn(unit, cs, r.adjacent, qn, a.q_h, h0, HEADS, a.h_q, (T*)a.o + row * a.o_t, a.o_h);
   if (page >= (uint32_t)a.n_pages) return;                   // no page: nothing is written
   const int off = at.slot & ((1 << a.page_log) - 1);
-  turn_heads(r, cs, u, (const T*)a.k_new + row * a.kn_t, a.kn_h, (T*)a.k + (int64_t)page * a.kp_p + off * a.kp_t, a.kp_h, h0, HEADS, a.h_kv);
-  const T* vn = (const T*)a.v_new + row * a.vn_t;
+  k.turn(unit, cs, r.adjacent, kn, a.kn_h, h0, HEADS, a.h_kv, (T*)a.k + (int64_t)page * a.kp_p + off * a.kp_t, a.kp_h);
   T* vp = (T*)a.v + (int64_t)page * a.vp_p + off * a.vp_t;
-  for (int x = lane; x < a.h_kv * CHUNKS; x += 64) {
-    const int h = x / CHUNKS, c = x % CHUNKS * CHUNK;
-    *reinterpret_cast<u32x4*>(vp + h * a.vp_h + c) = *reinterpret_cast<const u32x4*>(vn + h * a.vn_h + c);
+  for (int x0 = lane; x0 < a.h_kv * CHUNKS; x0 += 64 * NV) {
+    if (x0 != lane) ask_v(x0);
+#pragma unroll
+    for (int i = 0; i < NV; i++) {
+      const int x = x0 + 64 * i;
+      if (x < a.h_kv * CHUNKS) *reinterpret_cast<u32x4*>(vp + x / CHUNKS * a.vp_h + x % CHUNKS * CHUNK) = v[i];
+    }
   }
   for (int h = lane; h < a.h_kv; h += 64) {
     const int64_t x = (((int64_t)page * a.h_kv + h) << a.page_log) + off;
@@ -66,91 +92,119 @@ __global__ __launch_bounds__(256) void paged_append_rotary_kernel(PagedArgs a, R
 // so that a number next to the border between two codes falls on the side that it lies on.
 template <typename T, int D, bool ROTARY>
 __global__ __launch_bounds__(256) void paged4_append_kernel(PagedArgs a, RotaryArgs r) {
-  constexpr int UNITS = D / 16, HEADS = 64 / UNITS, LANES = D / 8;
+  using U = Unit<T, D>;
+  constexpr int HEADS = 64 / U::COUNT, LANES = D / 8, STEP = 64 / LANES, NK = 2;
   __shared__ double2 table[ROTARY ? 4 : 1][D / 2];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = (int)(blockIdx.y << kGridLog | blockIdx.x) * 4 + wave;
   if (row >= a.n_rows) return;
+  const int h0 = lane / U::COUNT, c = lane % LANES, k0 = lane / LANES;
+  const T* kn = (const T*)a.k_new + row * a.kn_t;
+  const T* vn = (const T*)a.v_new + row * a.vn_t;
+  const T* qn = (const T*)a.q + row * a.q_t;
+  // the piece of 8 that holds the other elements of this one's pairs, and the first pair
+  const bool turned = ROTARY && 8 * c < 2 * r.half, second = ROTARY && !r.adjacent && 8 * c >= r.half;
+  const int other = !ROTARY || r.adjacent || !turned ? c : second ? c - r.half / 8 : c + r.half / 8, pair = ROTARY && r.adjacent ? 4 * c : 8 * min(c, other);
+  uint64_t turns = 0;
+  if constexpr (ROTARY) turns = r.turns[min(lane, r.half - 1)];
+  Piece<T> k[NK], ko[NK], v[NK];
+  auto ask = [&](int h) {
+#pragma unroll
+    for (int i = 0; i < NK; i++)
+      if (h + i * STEP < a.h_kv) {
+        k[i] = load_piece(kn + (h + i * STEP) * a.kn_h + 8 * c);
+        if constexpr (ROTARY) ko[i] = load_piece(kn + (h + i * STEP) * a.kn_h + 8 * other);
+        v[i] = load_piece(vn + (h + i * STEP) * a.vn_h + 8 * c);
+      }
+  };
+  ask(k0);
+  const U unit(r, lane % U::COUNT);
+  Heads<T, D, 4> q;
+  if constexpr (ROTARY) {
+    if (a.q) q.ask(unit, qn, a.q_h, h0, HEADS, a.h_q);
+  }
   PagedPlace at;
   if (!paged_place(a, row, at)) return;
   const uint32_t page = (uint32_t)paged_entry(a, at.b, at.slot >> a.page_log);
   if constexpr (ROTARY) {
-    if (lane < r.half) table[wave][lane] = rotary_cos_sin(r, lane, at.position);
+    table[wave][min(lane, D / 2 - 1)] = rotary_cos_sin(r, turns, at.position);   // lanes behind the last pair: no one's
     asm volatile("" ::: "memory");                           // a wave's LDS operations complete in order
-    if (a.q) {
-      const int u = lane % UNITS;
-      float2 cs[8];
-#pragma unroll
-      for (int i = 0; i < 8; i++) {
-        const double2 t = table[wave][min(8 * u, r.half - 8) + i];
-        cs[i] = make_float2((float)t.x, (float)t.y);
-      }
-      turn_heads(r, cs, u, (const T*)a.q + row * a.q_t, a.q_h, (T*)a.o + row * a.o_t, a.o_h, lane / UNITS, HEADS, a.h_q);
-    }
+    if (a.q) q.turn(unit, unit.pairs(table[wave]), r.adjacent, qn, a.q_h, h0, HEADS, a.h_q, (T*)a.o + row * a.o_t, a.o_h);
   }
   if (page >= (uint32_t)a.n_pages) return;                   // no page: nothing is written
-  const int off = at.slot & ((1 << a.page_log) - 1), c = lane % LANES;
-  auto put = [&](const float (&v)[8], int h, char* codes, int64_t codes_h, uint8_t* scales) {
+  const int off = at.slot & ((1 << a.page_log) - 1);
+  auto put = [&](const Eight& e, int h, char* codes, int64_t codes_h, uint8_t* scales) {
     uint32_t scale;
-    const uint32_t w = fp4_of_eight(v, scale);
+    const uint32_t w = fp4_of_eight(e.x, scale);
     *reinterpret_cast<uint32_t*>(codes + h * codes_h + c * 4) = w;
     if ((lane & 3) == 0) scales[((((int64_t)page * a.h_kv + h) << a.page_log) + off) * (D / 32) + c / 4] = (uint8_t)scale;
   };
-  const T* kn = (const T*)a.k_new + row * a.kn_t;
-  const T* vn = (const T*)a.v_new + row * a.vn_t;
   char* kp = (char*)a.k + (int64_t)page * a.kp_p + off * a.kp_t;
   char* vp = (char*)a.v + (int64_t)page * a.vp_p + off * a.vp_t;
-  const bool turns = ROTARY && 8 * c < 2 * r.half;
-  // the pieces of 8 that hold the other elements of this one's pairs, and its first pair
-  const bool second = !r.adjacent && 8 * c >= r.half;
-  const int other = r.adjacent ? c : second ? c - r.half / 8 : c + r.half / 8, pair = r.adjacent ? 4 * c : 8 * min(c, other);
-  for (int h = lane / LANES; h < a.h_kv; h += 64 / LANES) {
-    Eight x = load_eight(kn + h * a.kn_h + 8 * c);
-    if constexpr (ROTARY) {
-      if (turns) {
-        const Eight y = r.adjacent ? x : load_eight(kn + h * a.kn_h + 8 * other);
-        if (r.adjacent) {
+  for (int hb = k0; hb < a.h_kv; hb += NK * STEP) {
+    if (hb != k0) ask(hb);
 #pragma unroll
-          for (int i = 0; i < 4; i++) {
-            const double2 t = table[wave][pair + i];
-            const double p = x.x[2 * i], q = x.x[2 * i + 1];
-            x.x[2 * i] = sticky_float(__builtin_fma(p, t.x, -(q * t.y)));
-            x.x[2 * i + 1] = sticky_float(__builtin_fma(p, t.y, q * t.x));
+    for (int i = 0; i < NK; i++) {
+      const int h = hb + i * STEP;
+      if (h >= a.h_kv) break;
+      Eight x = eight_of(k[i]);
+      if constexpr (ROTARY) {
+        if (turned && r.adjacent) {
+#pragma unroll
+          for (int e = 0; e < 4; e++) {
+            const double2 t = table[wave][pair + e];
+            const double p = x.x[2 * e], y = x.x[2 * e + 1];
+            x.x[2 * e] = sticky_float(__builtin_fma(p, t.x, -(y * t.y)));
+            x.x[2 * e + 1] = sticky_float(__builtin_fma(p, t.y, y * t.x));
           }
-        } else {
+        } else if (turned) {
+          const Eight y = eight_of(ko[i]);
 #pragma unroll
-          for (int i = 0; i < 8; i++) {
-            const double2 t = table[wave][pair + i];
-            const double q = (double)y.x[i] * t.y;
-            x.x[i] = sticky_float(__builtin_fma((double)x.x[i], t.x, second ? q : -q));
+          for (int e = 0; e < 8; e++) {
+            const double2 t = table[wave][pair + e];
+            const double z = (double)y.x[e] * t.y;
+            x.x[e] = sticky_float(__builtin_fma((double)x.x[e], t.x, second ? z : -z));
           }
         }
       }
+      put(x, h, kp, a.kp_h, const_cast<uint8_t*>(a.k_sc));
+      put(eight_of(v[i]), h, vp, a.vp_h, const_cast<uint8_t*>(a.v_sc));
     }
-    put(x.x, h, kp, a.kp_h, const_cast<uint8_t*>(a.k_sc));
-    put(load_eight(vn + h * a.vn_h + 8 * c).x, h, vp, a.vp_h, const_cast<uint8_t*>(a.v_sc));
   }
 }
 
-// A thread has a word of codes, the eight values of which it writes; rows of the pool one after the other, those of V behind those of K.
+// A thread has words of eight codes and writes what they stand for; the rows of K of a head of a page, and those of V, are a workgroup's at a time.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void paged4_unpack_kernel(PagedArgs a, T* k_pages, T* v_pages) {
-  constexpr int LANES = D / 8, ROWS = 256 / LANES;
-  const int64_t rows = ((int64_t)a.n_pages * a.h_kv) << a.page_log;
-  const int c = threadIdx.x % LANES;
-  for (int64_t i = (int64_t)blockIdx.x * ROWS + threadIdx.x / LANES; i < 2 * rows; i += (int64_t)gridDim.x * ROWS) {
-    const bool v = i >= rows;
-    const int64_t row = v ? i - rows : i, head = row >> a.page_log;
-    const int64_t page = head / a.h_kv, h = head - page * a.h_kv, off = row & ((1 << a.page_log) - 1);
-    const char* codes = v ? (const char*)a.v + page * a.vp_p + h * a.vp_h + off * a.vp_t : (const char*)a.k + page * a.kp_p + h * a.kp_h + off * a.kp_t;
-    const uint32_t w = reinterpret_cast<const uint32_t*>(codes)[c];
-    const float s = fp4_scale((v ? a.v_sc : a.k_sc)[row * (D / 32) + c / 4]);
-    T* to = (v ? v_pages : k_pages) + row * D + 8 * c;
-    if constexpr (sizeof(T) == 2) {
-      *reinterpret_cast<bf16x8*>(to) = fp4_to_bf16(w, s);
-    } else {
-      reinterpret_cast<f32x4*>(to)[0] = fp4_to_f32<0>(w, s);
-      reinterpret_cast<f32x4*>(to)[1] = fp4_to_f32<1>(w, s);
+  constexpr int BLOCKS = D / 32, AHEAD = 4;
+  const int heads = a.n_pages * a.h_kv, P = 1 << a.page_log;
+  for (int head = blockIdx.x; head < heads; head += gridDim.x) {
+    const int page = head / a.h_kv, h = head - page * a.h_kv;
+    const int64_t first = (int64_t)head << a.page_log;
+    // words of codes: neighbours write side by side; several are asked for together
+    const int words = 2 * P * BLOCKS * 4;
+    for (int x0 = threadIdx.x; x0 < words; x0 += 256 * AHEAD) {
+      uint32_t word[AHEAD], scale[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; i++) {
+        const int x = min(x0 + 256 * i, words - 1), row = x / (BLOCKS * 4), in = x % (BLOCKS * 4), off = row & (P - 1);
+        const char* codes = row >= P ? (const char*)a.v + page * a.vp_p + h * a.vp_h + off * a.vp_t : (const char*)a.k + page * a.kp_p + h * a.kp_h + off * a.kp_t;
+        word[i] = reinterpret_cast<const uint32_t*>(codes)[in];
+        scale[i] = (row >= P ? a.v_sc : a.k_sc)[(first + off) * BLOCKS + in / 4];
+      }
+#pragma unroll
+      for (int i = 0; i < AHEAD; i++) {
+        const int x = x0 + 256 * i, row = x / (BLOCKS * 4), in = x % (BLOCKS * 4);
+        if (x >= words) break;
+        T* to = (row >= P ? v_pages : k_pages) + (first + (row & (P - 1))) * D + in * 8;
+        const float s = fp4_scale(scale[i]);
+        if constexpr (sizeof(T) == 2) {
+          *reinterpret_cast<bf16x8*>(to) = fp4_to_bf16(word[i], s);
+        } else {
+          reinterpret_cast<f32x4*>(to)[0] = fp4_to_f32<0>(word[i], s);
+          reinterpret_cast<f32x4*>(to)[1] = fp4_to_f32<1>(word[i], s);
+        }
+      }
     }
   }
 }
@@ -177,8 +231,8 @@ hipError_t launch_paged4_append(const PagedArgs& a, const RotaryArgs* r, int ele
 }
 
 hipError_t launch_paged4_unpack(const PagedArgs& a, void* k_pages, void* v_pages, int elem, int d, hipStream_t st) {
-  const int64_t wgs = ((((int64_t)a.n_pages * a.h_kv) << a.page_log) * 2 + 2048 / d - 1) / (2048 / d);
-  const dim3 grid((unsigned)(wgs < 1 << 16 ? wgs : 1 << 16)), blk(256);
+  const int64_t heads = (int64_t)a.n_pages * a.h_kv;
+  const dim3 grid((unsigned)(heads < 1 << 20 ? heads : 1 << 20)), blk(256);
   if (elem == 2 && d == 128) hipLaunchKernelGGL((paged4_unpack_kernel<uint16_t, 128>), grid, blk, 0, st, a, (uint16_t*)k_pages, (uint16_t*)v_pages);
   else if (elem == 2) hipLaunchKernelGGL((paged4_unpack_kernel<uint16_t, 64>), grid, blk, 0, st, a, (uint16_t*)k_pages, (uint16_t*)v_pages);
   else if (d == 128) hipLaunchKernelGGL((paged4_unpack_kernel<float, 128>), grid, blk, 0, st, a, (float*)k_pages, (float*)v_pages);

@@ -42,62 +42,114 @@ __device__ __forceinline__ double2 cos_sin_of_turn(uint64_t x) {
   return make_double2(quarter == 1 || quarter == 2 ? -a : a, quarter >= 2 ? -b : b);
 }
 
-// of pair i at a position, times mscale
-__device__ __forceinline__ double2 rotary_cos_sin(const RotaryArgs& r, int i, int position) {
-  const double2 t = cos_sin_of_turn((uint64_t)(int64_t)position * r.turns[i]);
+// of a pair's turns at a position, times mscale
+__device__ __forceinline__ double2 rotary_cos_sin(const RotaryArgs& r, uint64_t turns, int position) {
+  const double2 t = cos_sin_of_turn((uint64_t)(int64_t)position * turns);
   return make_double2(t.x * r.mscale, t.y * r.mscale);
 }
 
-// A unit is 16 elements of a head, two pieces of 8 that hold the pairs 8 u .. 8 u + 7 (or, behind the rotated part, none): their offsets.
-__device__ __forceinline__ int2 rotary_unit(const RotaryArgs& r, int u) {
-  return r.adjacent || 8 * u >= r.half ? make_int2(16 * u, 16 * u + 8) : make_int2(8 * u, r.half + 8 * u);
+// Eight elements of a tensor as they lie in memory: asked for early, made floats when they are used.
+template <typename T> struct Piece { u32x4 w[sizeof(T) / 2]; };
+template <typename T> __device__ __forceinline__ Piece<T> load_piece(const T* p) {
+  Piece<T> x;
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; i++) x.w[i] = reinterpret_cast<const u32x4*>(p)[i];
+  return x;
 }
-
-// 8 elements of a tensor as floats, and back (rounded to nearest)
+template <typename T> __device__ __forceinline__ void store_piece(T* p, const Piece<T>& x) {
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; i++) reinterpret_cast<u32x4*>(p)[i] = x.w[i];
+}
 struct Eight { float x[8]; };
-template <typename T> __device__ __forceinline__ Eight load_eight(const T* p);
-template <> __device__ __forceinline__ Eight load_eight<uint16_t>(const uint16_t* p) {
-  const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+__device__ __forceinline__ Eight eight_of(const Piece<uint16_t>& p) {
   Eight e;
 #pragma unroll
-  for (int i = 0; i < 4; i++) { e.x[2 * i] = bf16_lo(w[i]); e.x[2 * i + 1] = bf16_hi(w[i]); }
+  for (int i = 0; i < 4; i++) { e.x[2 * i] = bf16_lo(p.w[0][i]); e.x[2 * i + 1] = bf16_hi(p.w[0][i]); }
   return e;
 }
-template <> __device__ __forceinline__ Eight load_eight<float>(const float* p) {
-  const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
-  return {{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}};
-}
-__device__ __forceinline__ void store_eight(uint16_t* p, const Eight& e) {
-  typedef __bf16 pair __attribute__((ext_vector_type(2)));
-  u32x4 w;
+__device__ __forceinline__ Eight eight_of(const Piece<float>& p) {
+  Eight e;
 #pragma unroll
-  for (int i = 0; i < 4; i++) w[i] = __builtin_bit_cast(uint32_t, pair{(__bf16)e.x[2 * i], (__bf16)e.x[2 * i + 1]});
-  *reinterpret_cast<u32x4*>(p) = w;
-}
-__device__ __forceinline__ void store_eight(float* p, const Eight& e) {
-  reinterpret_cast<f32x4*>(p)[0] = f32x4{e.x[0], e.x[1], e.x[2], e.x[3]};
-  reinterpret_cast<f32x4*>(p)[1] = f32x4{e.x[4], e.x[5], e.x[6], e.x[7]};
+  for (int i = 0; i < 8; i++) e.x[i] = __uint_as_float(p.w[i >> 2][i & 3]);
+  return e;
 }
 
-// Turns the pairs of a unit's two pieces; cs: (cos, sin) of its eight pairs.  Products and sums in fp32, of which each result has two roundings.
-__device__ __forceinline__ void turn_unit(Eight& a, Eight& b, const float2 (&cs)[8], bool adjacent) {
-  if (adjacent) {
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      Eight& e = i < 4 ? a : b;
-      const float x = e.x[2 * (i & 3)], y = e.x[2 * (i & 3) + 1];
-      e.x[2 * (i & 3)] = fmaf(x, cs[i].x, -(y * cs[i].y));
-      e.x[2 * (i & 3) + 1] = fmaf(x, cs[i].y, y * cs[i].x);
+// A unit is two 16-byte pieces of a head, of V elements each, and V pairs (or none, behind the rotated part): of pairs that lie apart, piece a has
+// the first elements and b the second ones; neighbours lie in a piece, V / 2 pairs, and b is half a head behind a.  Neighbouring units are neighbours in memory
+// (pieces one behind the other in a thread instead: 2 x 20 heads of 64 x 3001 tokens in fp32 17.2 us instead of FP32_NEW).
+template <typename T, int D> struct Unit {
+  static constexpr int V = 16 / sizeof(T), COUNT = D / (2 * V);                // units of a head
+  int a, b, pa, pb;              // elements where the pieces begin; first pairs of the lower and the upper half of cs
+  bool ta, tb;                   // whether they turn
+  __device__ __forceinline__ Unit(const RotaryArgs& r, int u) {
+    if (r.adjacent) {
+      a = V * u; b = V * (u + COUNT);
+      ta = a < 2 * r.half; tb = b < 2 * r.half;
+      pa = a / 2; pb = b / 2;
+    } else {
+      ta = tb = V * u < r.half;
+      a = ta ? V * u : 2 * V * u; b = ta ? r.half + V * u : 2 * V * u + V;
+      pa = V * u; pb = pa + V / 2;
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      const float x = a.x[i], y = b.x[i];
-      a.x[i] = fmaf(x, cs[i].x, -(y * cs[i].y));
-      b.x[i] = fmaf(x, cs[i].y, y * cs[i].x);
-    }
+    pa = min(pa, r.half - V / 2);                            // that no one uses
+    pb = min(pb, r.half - V / 2);
   }
-}
+  struct Pairs { float2 cs[V]; };
+  template <typename C> __device__ __forceinline__ Pairs pairs(const C* cs) const {
+    Pairs p;
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+      const C c = cs[i < V / 2 ? pa + i : pb + i - V / 2];
+      p.cs[i] = make_float2((float)c.x, (float)c.y);
+    }
+    return p;
+  }
+  struct Data { u32x4 a, b; };
+  __device__ __forceinline__ Data load(const T* head) const { return {*reinterpret_cast<const u32x4*>(head + a), *reinterpret_cast<const u32x4*>(head + b)}; }
+  __device__ __forceinline__ static float get(const u32x4& w, int i) {
+    if constexpr (V == 4) return __uint_as_float(w[i]);
+    else return i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
+  }
+  __device__ __forceinline__ static u32x4 put(const float (&x)[V]) {           // rounded to nearest
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      if constexpr (V == 4) w[i] = __float_as_uint(x[i]);
+      else w[i] = __builtin_bit_cast(uint32_t, pair{(__bf16)x[2 * i], (__bf16)x[2 * i + 1]});
+    }
+    return w;
+  }
+  // Products and sums in fp32, of which each result has two roundings.
+  __device__ __forceinline__ static u32x4 neighbours(const u32x4& w, const float2* cs) {
+    float y[V];
+#pragma unroll
+    for (int i = 0; i < V / 2; i++) {
+      const float p = get(w, 2 * i), q = get(w, 2 * i + 1);
+      y[2 * i] = fmaf(p, cs[i].x, -(q * cs[i].y));
+      y[2 * i + 1] = fmaf(p, cs[i].y, q * cs[i].x);
+    }
+    return put(y);
+  }
+  __device__ __forceinline__ void store(T* head, Data x, const Pairs& p, bool adjacent) const {
+    if (adjacent) {
+      if (ta) x.a = neighbours(x.a, p.cs);
+      if (tb) x.b = neighbours(x.b, p.cs + V / 2);
+    } else if (ta) {
+      float y[V], z[V];
+#pragma unroll
+      for (int i = 0; i < V; i++) {
+        const float m = get(x.a, i), n = get(x.b, i);
+        y[i] = fmaf(m, p.cs[i].x, -(n * p.cs[i].y));
+        z[i] = fmaf(m, p.cs[i].y, n * p.cs[i].x);
+      }
+      x.a = put(y);
+      x.b = put(z);
+    }
+    *reinterpret_cast<u32x4*>(head + a) = x.a;
+    *reinterpret_cast<u32x4*>(head + b) = x.b;
+  }
+};
 
 // Validates r for heads of head_dim and fills out: a dash_status.
 int rotary_args(const dash_rotary* r, int head_dim, RotaryArgs* out);
