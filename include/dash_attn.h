@@ -474,7 +474,7 @@ int dash_paged4_append(const dash_paged_params* p, const dash_rotary* r, const v
                        const void* v_new, void* k_codes, void* k_scales, void* v_codes, void* v_scales, const int32_t* row_start,
                        const int32_t* lens, const int32_t* table, const int32_t* seen, void* stream);
 
-/* As dash_paged_attend. */
+/* As dash_paged_attend; the last bits of a row may also depend on n_rows (which kernel is taken follows from the rows a sequence has on the average). */
 int dash_paged4_attend(const dash_paged_params* p, const void* q, const void* k_codes, const void* k_scales, const void* v_codes,
                        const void* v_scales, const int32_t* row_start, const int32_t* lens, const int32_t* table, void* o, float* lse,
                        void* workspace, size_t workspace_bytes, void* stream);

@@ -358,6 +358,9 @@ class PagedCache:
 
 _PAGED_PARAMS = struct.Struct("10ifi14q")                  # dash_paged_params ...
 _paged_sizes = operator.itemgetter(0, 2, 3, 4, 6, 7, 8, *range(20, 26))   # ... and its batch, h_kv, head_dim, dtype, page_size, n_pages, max_pages, k_stride, v_stride
+_BYTE = torch.uint8
+_put_strides = struct.Struct("2q").pack_into
+_ROW_STRIDES = {n: getattr(dash_paged_params, n).offset for n in ("q_stride", "o_stride", "k_new_stride", "v_new_stride")}
 _INT, _FLOAT = torch.int32, torch.float32
 _PAGED_TYPES = {torch.bfloat16: DASH_BF16, _FLOAT: DASH_F32}
 
@@ -433,8 +436,7 @@ def _paged_call(p: dash_paged_params, layout, row_start, rows, extra=None, ws=No
         s = t.stride()
         if t.dtype is not dtype or t.shape != (n_rows, heads, d) or s[2] != 1 or t.get_device() != dev:
             raise DashError(f"packed rows: [{n_rows}, {heads}, {d}] of the cache's type and device, head_dim contiguous")
-        strides = getattr(p, name)
-        strides[0], strides[1] = s[0], s[1]
+        _put_strides(p, _ROW_STRIDES[name], s[0], s[1])
     if extra is not None and extra[0] is not None:
         t, want, shape = extra
         if t.dtype is not want or t.shape != shape or not t.is_contiguous() or t.get_device() != dev:
@@ -555,23 +557,6 @@ def _gpu_stream(dev: int):
     return _raw_stream(dev)
 
 
-def _span(ptr, shape, strides, size):
-    """The bytes that a tensor's elements lie in: the first, and the one behind the last."""
-    last = 0
-    for n, s in zip(shape, strides):
-        last += (n - 1) * s
-    return ptr, ptr + (last + 1) * size
-
-
-def _lies_on(x, x_ptr, x_strides, y, y_ptr, y_strides) -> bool:
-    """Whether an output overlaps its input without being it."""
-    if x_ptr == y_ptr and x_strides == y_strides:
-        return False
-    size = x.element_size()
-    (a0, a1), (b0, b1) = _span(x_ptr, x.shape, x_strides, size), _span(y_ptr, y.shape, y_strides, size)
-    return a0 < b1 and b0 < a1
-
-
 _ROTARY_PARAMS = struct.Struct("10i13q")                   # dash_rotary_params
 _NO_STRIDES = (0, 0, 0)
 
@@ -667,8 +652,11 @@ def _fresh_rows(p, k_new, v_new, q, q_out):
         return (k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride")
     if q is None or q_out is None:
         raise DashError("q and q_out: both or none")
-    if _lies_on(q, q.data_ptr(), q.stride(), q_out, q_out.data_ptr(), q_out.stride()):
-        raise DashError("q_out is q or does not overlap it")
+    qs, os, qp, op = q.stride(), q_out.stride(), q.data_ptr(), q_out.data_ptr()
+    if (qp != op or qs != os) and len(qs) == len(os) == 3:       # other shapes are refused with the packed rows'
+        n, h, size = p.n_rows - 1, p.h_q - 1, q.element_size()
+        if qp < op + (n * os[0] + h * os[1] + p.head_dim) * size and op < qp + (n * qs[0] + h * qs[1] + p.head_dim) * size:
+            raise DashError("q_out is q or does not overlap it")
     return (k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride"), (q, p.h_q, "q_stride"), (q_out, p.h_q, "o_stride")
 
 
@@ -697,7 +685,7 @@ def _paged4_layout(c: PagedCache4, dtype, seen=None) -> tuple:
     """As _paged_layout; dtype: the packed rows'."""
     k, v, ks, vs, t, lens = c.k_codes, c.v_codes, c.k_scales, c.v_scales, c.table, c.lens
     shape, dev = tuple(k.shape), k.get_device()
-    if len(shape) != 4 or v.shape != shape or k.dtype is not torch.uint8 or v.dtype is not torch.uint8:
+    if len(shape) != 4 or v.shape != shape or k.dtype is not _BYTE or v.dtype is not _BYTE:
         raise DashError("k and v codes: two uint8 tensors [n_pages, h_kv, page_size, d / 2]")
     n_pages, h_kv, page_size, half = shape
     kp, kh, kt, k1 = k.stride()
@@ -705,16 +693,19 @@ def _paged4_layout(c: PagedCache4, dtype, seen=None) -> tuple:
     if k1 != 1 or v1 != 1:
         raise DashError("k and v codes: the last dimension must be contiguous")
     scales = (n_pages, h_kv, page_size, half // 16)
-    for s in (ks, vs):
-        if s.dtype is not torch.uint8 or s.shape != scales or not s.is_contiguous():
-            raise DashError("k and v scales: contiguous uint8 tensors [n_pages, h_kv, page_size, d / 32]")
+    if ks.dtype is not _BYTE or ks.shape != scales or not ks.is_contiguous() or vs.dtype is not _BYTE or vs.shape != scales or not vs.is_contiguous():
+        raise DashError("k and v scales: contiguous uint8 tensors [n_pages, h_kv, page_size, d / 32]")
     if t.dtype is not _INT or t.dim() != 2 or not t.is_contiguous():
         raise DashError("table [batch, max_pages]: a contiguous int32 tensor")
     batch, max_pages = t.shape
-    for x in (lens, seen):
-        if x is not None and (x.dtype is not _INT or x.shape != (batch,) or not x.is_contiguous()):
-            raise DashError("lens and seen: contiguous int32 tensors [batch]")
-    if lens is None or any(x is not None and x.get_device() != dev for x in (v, ks, vs, t, lens, seen)):
+    ok = lens is not None and lens.dtype is _INT and lens.shape == (batch,) and lens.is_contiguous()
+    same = v.get_device() == dev == ks.get_device() == vs.get_device() == t.get_device()
+    if seen is not None:
+        ok = ok and seen.dtype is _INT and seen.shape == (batch,) and seen.is_contiguous()
+        same = same and seen.get_device() == dev
+    if not ok:
+        raise DashError("lens and seen: contiguous int32 tensors [batch]")
+    if not same or lens.get_device() != dev:
         raise DashError("the cache's tensors lie on one device")
     return dev, dtype, (batch, h_kv, 2 * half, _PAGED_TYPES[dtype], page_size, n_pages, max_pages, kp, kh, kt, vp, vh, vt)
 

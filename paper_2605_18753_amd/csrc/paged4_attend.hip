@@ -66,6 +66,69 @@ __device__ __forceinline__ uint32_t flipped(uint32_t addr, int bits) {
   return x;
 }
 
+// What the walks over 32-key tiles share: where a lane's codes lie, loads and conversions.
+template <int D> struct Walk4 {
+  using C = Few4Cfg<D>;
+  struct Raw { Codes<C::CW> k[2], v[2]; uint32_t ks[2], vs[2]; };
+  const PagedArgs& a;
+  int b, r, keys, j1, lane;                                // sequence, kv-head, tokens; behind the piece's last tile; all but lane uniform
+  uint32_t kt, vt, k_off, v_off, ks_off, vs_off, v_wr;
+  const char *kb, *vb;
+  __device__ __forceinline__ Walk4(const PagedArgs& a, int b, int r, int keys, int j1, int lane, uint32_t buf) : a(a), b(b), r(r), keys(keys), j1(j1), lane(lane) {
+    const int n = lane & 15, kq = lane >> 4;
+    kt = (uint32_t)a.kp_t; vt = (uint32_t)a.vp_t;
+    // K: row n, quarter kq; V: row lane / 4, quarter lane % 4
+    k_off = (uint32_t)n * kt + kq * (D / 8); v_off = (uint32_t)(lane >> 2) * vt + (lane & 3) * (D / 8);
+    ks_off = scale_word<D>(n); vs_off = scale_word<D>(lane >> 2);
+    kb = (const char*)a.k + r * a.kp_h;
+    vb = (const char*)a.v + r * a.vp_h;
+    // of a lane's first chunk of V; chunk i lies at that address with bits 4 .. flipped by i
+    v_wr = buf + (uint32_t)((lane >> 2) * C::ROW_BYTES + ((C::CW * (lane & 3)) ^ v4_swz<D>(lane >> 2)) * 16);
+  }
+  // the table's entries for a tile: of one page, or of two of 16 tokens; looked at a tile later, when they have arrived
+  __device__ __forceinline__ int2 entries_of(int tile) const {
+    return make_int2(paged_entry(a, b, (tile * 32) >> a.page_log), paged_entry(a, b, (tile * 32 + 16) >> a.page_log));
+  }
+  // A resource ends with the sequence's last token: rows behind it read as zeros, whatever their page holds.
+  __device__ __forceinline__ void load(int tile, int2 entries, Raw& x) const {
+#pragma unroll
+    for (int half = 0; half < 2; half++) {
+      const int key = tile * 32 + half * 16;
+      const uint32_t id = paged_clamp(a, half ? entries.y : entries.x), off = key & ((1 << a.page_log) - 1);
+      const int rows = within_16(min(keys - key, (j1 - tile) * 32));             // behind the piece's last tile: nothing is read
+      const uint64_t at = ((((uint64_t)id * (uint32_t)a.h_kv + r) << a.page_log) + off) * (D / 32);
+      x.k[half] = load_codes<C::CW>(rsrc_of(kb + (uint64_t)id * (uint64_t)a.kp_p + off * kt, rows_span<D>(rows, kt)), k_off);
+      x.v[half] = load_codes<C::CW>(rsrc_of(vb + (uint64_t)id * (uint64_t)a.vp_p + off * vt, rows_span<D>(rows, vt)), v_off);
+      x.ks[half] = __builtin_amdgcn_raw_buffer_load_b32(rsrc_of(a.k_sc + at, scale_span<D>(rows)), ks_off, 0, 0);
+      x.vs[half] = __builtin_amdgcn_raw_buffer_load_b32(rsrc_of(a.v_sc + at, scale_span<D>(rows)), vs_off, 0, 0);
+    }
+  }
+  __device__ __forceinline__ uint32_t k_scale(const Raw& x, int half) const { return scale_byte<D>(x.ks[half], lane & 15, (lane >> 4) * (D / 4) / 32); }
+  __device__ __forceinline__ uint32_t v_scale(const Raw& x, int half) const { return scale_byte<D>(x.vs[half], lane >> 2, (lane & 3) * (D / 4) / 32); }
+  // V of a tile into LDS, in bf16.  A block that is NaN goes in as numbers next to 0 (the scale's exponent 0).
+  __device__ __forceinline__ void put_v(const Raw& x, const uint32_t (&vs)[2], int at) const {
+#pragma unroll
+    for (int half = 0; half < 2; half++) {
+      const float sc = __uint_as_float(vs[half] == 255u ? 0u : vs[half] << 23);
+#pragma unroll
+      for (int i = 0; i < C::CW; i++) lds_write_b128(flipped(v_wr, i << 4) + at + half * 16 * C::ROW_BYTES, fp4_to_bf16(x.v[half].w[i], sc));
+    }
+  }
+  // The rows that see the token of a block of V that is NaN: NaN there.  last: the lane's row's last key.
+  __device__ __forceinline__ void spoil(const uint32_t (&vs)[2], int tile, int last, f32x4 (&oacc)[D / 16]) const {
+    if (__builtin_expect(!__any(vs[0] == 255u || vs[1] == 255u), 1)) return;
+#pragma unroll
+    for (int half = 0; half < 2; half++)
+      for (uint64_t bad = __ballot(vs[half] == 255u); bad; bad &= bad - 1) {
+        const int l = __builtin_ctzll(bad), block = (l & 3) * (D / 4) / 32;
+        const bool seen = tile * 32 + half * 16 + (l >> 2) <= last;
+#pragma unroll
+        for (int dt = 0; dt < D / 16; dt++)
+          if (dt >> 1 == block && seen) oacc[dt] = f32x4{NAN, NAN, NAN, NAN};
+      }
+  }
+};
+
 template <int D>
 __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void paged_few4_kernel(PagedArgs args) {
   using C = Few4Cfg<D>;
@@ -95,34 +158,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void paged_few4_kernel(Paged
   int j = __builtin_amdgcn_readfirstlane(run.x0 * 4) + wave;
 
   const uint32_t buf = lds_addr_of(lds) + wave * C::TILE_BYTES;
-  const uint32_t kt = (uint32_t)a.kp_t, vt = (uint32_t)a.vp_t;
-  // K: row n, quarter kq; V: row lane / 4, quarter lane % 4
-  const uint32_t k_off = (uint32_t)n * kt + kq * (D / 8), v_off = (uint32_t)(lane >> 2) * vt + (lane & 3) * (D / 8);
-  const uint32_t ks_off = scale_word<D>(n), vs_off = scale_word<D>(lane >> 2);
-  const char* kb = (const char*)a.k + r * a.kp_h;
-  const char* vb = (const char*)a.v + r * a.vp_h;
-  const int pm = (1 << a.page_log) - 1;
-  // the table's entries for a tile: of one page, or of two of 16 tokens; looked at a tile later, when they have arrived
-  auto entries_of = [&](int tile) {
-    return make_int2(paged_entry(a, it.b, (tile * 32) >> a.page_log), paged_entry(a, it.b, (tile * 32 + 16) >> a.page_log));
-  };
-  struct Raw { Codes<C::CW> k[2], v[2]; uint32_t ks[2], vs[2]; };
-  // A resource ends with the sequence's last token: rows behind it read as zeros, whatever their page holds.
-  auto load = [&](int tile, int2 entries, Raw& x) {
-#pragma unroll
-    for (int half = 0; half < 2; half++) {
-      const int key = tile * 32 + half * 16;
-      const uint32_t id = paged_clamp(a, half ? entries.y : entries.x), off = key & pm;
-      const int rows = within_16(min(keys - key, (j1 - tile) * 32));                // behind the piece's last tile: nothing is read
-      const uint64_t at = ((((uint64_t)id * (uint32_t)a.h_kv + r) << a.page_log) + off) * (D / 32);
-      x.k[half] = load_codes<C::CW>(rsrc_of(kb + (uint64_t)id * (uint64_t)a.kp_p + off * kt, rows_span<D>(rows, kt)), k_off);
-      x.v[half] = load_codes<C::CW>(rsrc_of(vb + (uint64_t)id * (uint64_t)a.vp_p + off * vt, rows_span<D>(rows, vt)), v_off);
-      x.ks[half] = __builtin_amdgcn_raw_buffer_load_b32(rsrc_of(a.k_sc + at, scale_span<D>(rows)), ks_off, 0, 0);
-      x.vs[half] = __builtin_amdgcn_raw_buffer_load_b32(rsrc_of(a.v_sc + at, scale_span<D>(rows)), vs_off, 0, 0);
-    }
-  };
-  // of a lane's first chunk; chunk i, and d-tile i of the reads, lie at those addresses with bits 4 .. and 5 .. flipped by i
-  const uint32_t v_wr = buf + (uint32_t)((lane >> 2) * C::ROW_BYTES + ((C::CW * (lane & 3)) ^ v4_swz<D>(lane >> 2)) * 16);
+  const Walk4<D> walk(a, it.b, r, keys, j1, lane, buf);
   // transposing read of V: lane s of a group of 16 points at row 4 kq + s / 4 (+ 16), d 4 (s % 4) of the 16-wide d-tile
   const uint32_t v_rd = buf + (uint32_t)((4 * kq + (n >> 2)) * C::ROW_BYTES + ((((n & 3) >> 1) ^ v4_swz<D>(n >> 2)) << 4) + ((n & 1) << 3));
 
@@ -132,26 +168,19 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void paged_few4_kernel(Paged
   for (int dt = 0; dt < D / 16; dt++) oacc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   // Two sets of registers in turn: the next tile's loads are asked for before the present ones are waited for.
-  Raw even, odd;
+  typename Walk4<D>::Raw even, odd;
   int2 entries = make_int2(0, 0);
   if (j < j1) {
-    load(j, entries_of(j), even);
-    entries = entries_of(j + 4);
+    walk.load(j, walk.entries_of(j), even);
+    entries = walk.entries_of(j + 4);
   }
-  auto tile = [&](const Raw& x, Raw& next) __attribute__((always_inline)) {
-    load(j + 4, entries, next);
-    entries = entries_of(j + 8);
-    // a block that is NaN goes in as numbers next to 0 (the scale's exponent 0): the rows that see its token get NaN below
-    uint32_t vs[2];
-#pragma unroll
-    for (int half = 0; half < 2; half++) {
-      vs[half] = scale_byte<D>(x.vs[half], lane >> 2, (lane & 3) * (D / 4) / 32);
-      const float sc = __uint_as_float(vs[half] == 255u ? 0u : vs[half] << 23);
-#pragma unroll
-      for (int i = 0; i < C::CW; i++) lds_write_b128(flipped(v_wr, i << 4) + half * 16 * C::ROW_BYTES, fp4_to_bf16(x.v[half].w[i], sc));
-    }
+  auto tile = [&](const typename Walk4<D>::Raw& x, typename Walk4<D>::Raw& next) __attribute__((always_inline)) {
+    walk.load(j + 4, entries, next);
+    entries = walk.entries_of(j + 8);
+    const uint32_t vs[2] = {walk.v_scale(x, 0), walk.v_scale(x, 1)};
+    walk.put_v(x, vs, 0);
     f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;                                    // lane (row n, kq): keys 4 kq + i, 16 + 4 kq + i
-    const float k0 = fp4_scale(scale_byte<D>(x.ks[0], n, kq * (D / 4) / 32)), k1 = fp4_scale(scale_byte<D>(x.ks[1], n, kq * (D / 4) / 32));
+    const float k0 = fp4_scale(walk.k_scale(x, 0)), k1 = fp4_scale(walk.k_scale(x, 1));
 #pragma unroll
     for (int s = 0; s < D / 32; s++) {
       s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp4_to_bf16(x.k[0].w[s], k0), qf[s], s0, 0, 0, 0);
@@ -197,17 +226,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void paged_few4_kernel(Paged
 #pragma unroll
     for (int dt = 0; dt < D / 16; dt++) oacc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[dt], pb, oacc[dt], 0, 0, 0);
     asm volatile("" ::: "memory");
-    if (__builtin_expect(__any(vs[0] == 255u || vs[1] == 255u), 0)) {
-#pragma unroll
-      for (int half = 0; half < 2; half++)
-        for (uint64_t bad = __ballot(vs[half] == 255u); bad; bad &= bad - 1) {
-          const int l = __builtin_ctzll(bad), block = (l & 3) * (D / 4) / 32;
-          const bool seen = j * 32 + half * 16 + (l >> 2) <= last;
-#pragma unroll
-          for (int dt = 0; dt < D / 16; dt++)
-            if (dt >> 1 == block && seen) oacc[dt] = f32x4{NAN, NAN, NAN, NAN};
-        }
-    }
+    walk.spoil(vs, j, last, oacc);
   };
   while (j < j1) {
     tile(even, odd);
@@ -232,6 +251,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void paged_few4_kernel(Paged
   __syncthreads();
   } while (run.advance(args));
 }
+
 
 // Many rows: a tile is 128 (token, head) rows, as in paged_rows_kernel, whose walk this is: the two products, the exponentials and the maxima
 // between their MFMAs, the order of operands.  64-key tiles of K and V are converted on their way into LDS, each by the whole workgroup once.
@@ -409,8 +429,6 @@ __global__ __launch_bounds__(256, 2) void paged_rows4_kernel(PagedArgs a) {
 #pragma unroll
       for (int x = 0; x < NS; x++) {
         if (x + KAHEAD < NS) kf[x + KAHEAD] = k_read(x + KAHEAD);
-        if (x % 3 == 0 && x / 3 < C::CW) conv_k(x / 3, P ^ 1);
-        if (x == 3 * C::CW - 2) next_k();
         const f32x16 z = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         s[x & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[x], qf[x >> 1], x < 2 ? z : s[x & 1], 0, 0, 0);
         if constexpr (EXPS) {
@@ -443,7 +461,8 @@ __global__ __launch_bounds__(256, 2) void paged_rows4_kernel(PagedArgs a) {
         if (x + VAHEAD < NS) vf[x + VAHEAD] = v_read(x + VAHEAD);
         oacc[x % NDT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[x], __builtin_bit_cast(bf16x8, pb[x / NDT]), oacc[x % NDT], 0, 0, 0);
         if (EQ + x < 16) e_pair(EQ + x);
-        if (x % 3 == 1 && x / 3 < C::CW) conv_v(x / 3, P);
+        if (x % 4 == 0 && x / 4 < C::CW) conv_k(x / 4, P ^ 1);
+        if (x % 4 == 2 && x / 4 < C::CW) conv_v(x / 4, P);
         if constexpr (NS == 16) { if (x >= 4 && x < 12) max_quad(x - 4); }
         else if (x >= 4) { max_quad(2 * (x - 4)); max_quad(2 * (x - 4) + 1); }
         __builtin_amdgcn_sched_barrier(0);
@@ -469,11 +488,6 @@ __global__ __launch_bounds__(256, 2) void paged_rows4_kernel(PagedArgs a) {
       mask_keys();
     } else {
       asm volatile("" : "=v"(s[0]), "=v"(s[1]));               // nobody reads them
-      if (cur) {
-#pragma unroll
-        for (int c = 0; c < C::CW; c++) conv_k(c, P ^ 1);
-        next_k();
-      }
       if (pend) {
 #pragma unroll
         for (int x = 0; x < VAHEAD; x++) vf[x] = v_read(x);
@@ -486,9 +500,9 @@ __global__ __launch_bounds__(256, 2) void paged_rows4_kernel(PagedArgs a) {
       second_product();
     } else if (cur) {
 #pragma unroll
-      for (int c = 0; c < C::CW; c++) conv_v(c, P);
+      for (int c = 0; c < C::CW; c++) { conv_k(c, P ^ 1); conv_v(c, P); }
     }
-    if (cur) next_v();
+    if (cur) { next_k(); next_v(); }
     if (!pend && on) {
 #pragma unroll
       for (int q = 0; q < 8; q++) max_quad(q);
@@ -544,9 +558,12 @@ __global__ __launch_bounds__(256, 2) void paged_rows4_kernel(PagedArgs a) {
 // ---- host ------------------------------------------------------------------------------------------------------------
 // fp32: 512 threads for an item, fewer than 2^32 in all, as paged_attend_fits
 bool paged4_attend_fits(const PagedArgs& a, int dtype) { return dtype != DASH_F32 || paged_most_items(a, 16) * a.h_kv < (1 << 23); }
-// The kernel for a call, as for pages of bf16.
+// The kernel for a call: tiles of 128 rows where the sequences bring more than 48 rows each on the average, tiles of 16 otherwise, and for short caches as for pages
+// of bf16.  (Tiles of 128 and of 16.  32 / 8 heads of 128, 8 sequences of 3000 to 16000: 32 rows each 55.7 and 41.0 us, 48 63.4 and 53.0, 80 66.6 and 77.5; 64 of
+// 2000: 74.8, 82.9, 85.9 and 50.7, 72.4, 117; head dimension 64, 8 sequences: 32 rows 43.5 and 32.0, 80 50.4 and 55.4.  Heads in a group of 16, two kv-heads: 48 rows
+// 28.8 and 30.0, 80 30.9 and 32.8.)
 static bool use_rows(const PagedArgs& a, int dtype) {
-  return dtype == DASH_BF16 && (int64_t)a.n_rows * a.g > (int64_t)a.batch * 16 && !(a.cap <= 8 * kStep && paged_most_items(a, 16) * a.h_kv <= 256);
+  return dtype == DASH_BF16 && (int64_t)a.n_rows * a.g > (int64_t)a.batch * 48 && !(a.cap <= 8 * kStep && paged_most_items(a, 16) * a.h_kv <= 256);
 }
 // Workgroups of a kv-head that are resident at once (16-row tiles at head dimension 64: three of four).
 static int runs_of(const PagedArgs& a, int dtype, int d, bool big) { return max((dtype == DASH_F32 ? 256 : big || d == 128 ? 512 : 768) / a.h_kv, 1); }
