@@ -254,7 +254,10 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void paged_few4_kernel(Paged
 
 
 // Many rows: a tile is 128 (token, head) rows, as in paged_rows_kernel, whose walk this is: the two products, the exponentials and the maxima
-// between their MFMAs, the order of operands.  64-key tiles of K and V are converted on their way into LDS, each by the whole workgroup once.
+// between their MFMAs, the order of operands.  64-key tiles of K and V are converted on their way into LDS, each by the whole workgroup once: 32 conversions a thread
+// and tile, beside some 150 vector instructions and 32 MFMAs of each wave.  Bound by the vector and the matrix units.  2048 tokens at the end of 32768, 32 / 8 heads of 128,
+// 1072 us (1.0 PFLOP/s; pages of bf16 967 to 1080 by card).  Head dimension 64: three workgroups a CU (all exponentials between the first product's MFMAs, which
+// spares the registers that a third one needs): the same 656 us, two 741; 1501 tokens beside seven decoding sequences 215 and 238.
 template <int D> struct Rows4Cfg {
   static constexpr int CW = D / 32, ROW_BYTES = D * 2;
   static constexpr int TILE_BYTES = 64 * ROW_BYTES;
@@ -263,7 +266,7 @@ template <int D> struct Rows4Cfg {
 };
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void paged_rows4_kernel(PagedArgs a) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_rows4_kernel(PagedArgs a) {
   using C = Rows4Cfg<D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -361,7 +364,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows4_kernel(PagedArgs a) {
   float tmax_old = 0.f;
   auto iteration = [&](auto p_tag, int i, f32x16 (&s)[2], f32x16 (&so)[2]) __attribute__((always_inline)) {
     constexpr int P = decltype(p_tag)::value;
-    constexpr int NS = D / 8, KAHEAD = 4, VAHEAD = 2, EQ = 12, E0 = 2;
+    constexpr int NS = D / 8, KAHEAD = D == 64 ? 3 : 4, VAHEAD = 2, EQ = D == 64 ? 16 : 12, E0 = D == 64 ? 0 : 2;
     const bool cur = i < n_it;
     const int tile = first + i;
     const bool on = cur && tile * 64 < wave_end;
@@ -565,8 +568,9 @@ bool paged4_attend_fits(const PagedArgs& a, int dtype) { return dtype != DASH_F3
 static bool use_rows(const PagedArgs& a, int dtype) {
   return dtype == DASH_BF16 && (int64_t)a.n_rows * a.g > (int64_t)a.batch * 48 && !(a.cap <= 8 * kStep && paged_most_items(a, 16) * a.h_kv <= 256);
 }
-// Workgroups of a kv-head that are resident at once (16-row tiles at head dimension 64: three of four).
-static int runs_of(const PagedArgs& a, int dtype, int d, bool big) { return max((dtype == DASH_F32 ? 256 : big || d == 128 ? 512 : 768) / a.h_kv, 1); }
+// Workgroups of a kv-head that are resident at once: two a CU at head dimension 128, three at 64 (of 16-row tiles, of which four are, three runs a CU are as fast:
+// 32 sequences of 4096 to 32768 75.7 us, four 76.3).
+static int runs_of(const PagedArgs& a, int dtype, int d, bool big) { return max((dtype == DASH_F32 ? 256 : d == 128 ? 512 : 768) / a.h_kv, 1); }
 static size_t ws_align(size_t x) { return (x + 255) & ~(size_t)255; }
 
 size_t paged4_attend_ws(const PagedArgs& a, int dtype, int d) {
