@@ -14,9 +14,8 @@ template <int D> struct Few4Cfg {
   static constexpr int OUT_BYTES = 4 * 16 * (D + 6) * 4;   // the waves' results, behind the walk
   static constexpr int LDS_BYTES = 4 * TILE_BYTES > OUT_BYTES ? 4 * TILE_BYTES : OUT_BYTES;
 };
-// Position of 16-byte chunk c of V's row: 4 rows x 2 chunks (transposing reads) and 2 rows x 4 chunks a quarter of a row apart (writes) spread over
-// all banks.
-template <int D> __device__ __forceinline__ int v4_swz(int row) { return D == 128 ? ((row & 3) << 2) | (row & 1) : ((row >> 1) & 1) << 2; }
+// Position of 16-byte chunk c of V's row: 4 rows x 2 chunks (transposing reads) and 4 rows x 4 chunks a quarter of a row apart (writes) spread over all banks.
+template <int D> __device__ __forceinline__ int v4_swz(int row) { return D == 128 ? (row & 3) * 5 : ((row >> 1) & 1) * 5; }
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32v4 __attribute__((ext_vector_type(4)));

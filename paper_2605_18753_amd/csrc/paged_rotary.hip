@@ -38,7 +38,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(256, 4) void paged_append_rotary_kernel(PagedArgs a, RotaryArgs r) {
   using U = Unit<T, D>;
   constexpr int HEADS = 64 / U::COUNT, CHUNK = 16 / sizeof(T), CHUNKS = D / CHUNK, NV = 2;
-  __shared__ float2 table[4][D / 2];
+  __shared__ float2 table[4][rotary_place(D / 2)];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = (int)(blockIdx.y << kGridLog | blockIdx.x) * 4 + wave;
   if (row >= a.n_rows) return;
@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256, 4) void paged_append_rotary_kernel(PagedArgs a
   if (!paged_place(a, row, at)) return;
   const uint32_t page = (uint32_t)paged_entry(a, at.b, at.slot >> a.page_log);
   const double2 t = rotary_cos_sin(r, turns, at.position);
-  table[wave][min(lane, D / 2 - 1)] = make_float2((float)t.x, (float)t.y);       // lanes behind the last pair: no one's
+  table[wave][rotary_place(min(lane, D / 2 - 1))] = make_float2((float)t.x, (float)t.y);       // lanes behind the last pair: no one's
   asm volatile("" ::: "memory");                             // a wave's LDS operations complete in order
   const typename U::Pairs cs = unit.pairs(table[wave]);
   if (a.q) q.turn(unit, cs, r.adjacent, qn, a.q_h, h0, HEADS, a.h_q, (T*)a.o + row * a.o_t, a.o_h);
@@ -94,7 +94,7 @@ template <typename T, int D, bool ROTARY>
 __global__ __launch_bounds__(256) void paged4_append_kernel(PagedArgs a, RotaryArgs r) {
   using U = Unit<T, D>;
   constexpr int HEADS = 64 / U::COUNT, LANES = D / 8, STEP = 64 / LANES, NK = 2;
-  __shared__ double2 table[ROTARY ? 4 : 1][D / 2];
+  __shared__ double2 table[ROTARY ? 4 : 1][rotary_place(D / 2)];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = (int)(blockIdx.y << kGridLog | blockIdx.x) * 4 + wave;
   if (row >= a.n_rows) return;
@@ -127,7 +127,7 @@ __global__ __launch_bounds__(256) void paged4_append_kernel(PagedArgs a, RotaryA
   if (!paged_place(a, row, at)) return;
   const uint32_t page = (uint32_t)paged_entry(a, at.b, at.slot >> a.page_log);
   if constexpr (ROTARY) {
-    table[wave][min(lane, D / 2 - 1)] = rotary_cos_sin(r, turns, at.position);   // lanes behind the last pair: no one's
+    table[wave][rotary_place(min(lane, D / 2 - 1))] = rotary_cos_sin(r, turns, at.position);   // lanes behind the last pair: no one's
     asm volatile("" ::: "memory");                           // a wave's LDS operations complete in order
     if (a.q) q.turn(unit, unit.pairs(table[wave]), r.adjacent, qn, a.q_h, h0, HEADS, a.h_q, (T*)a.o + row * a.o_t, a.o_h);
   }
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(256) void paged4_append_kernel(PagedArgs a, RotaryA
         if (turned && r.adjacent) {
 #pragma unroll
           for (int e = 0; e < 4; e++) {
-            const double2 t = table[wave][pair + e];
+            const double2 t = table[wave][rotary_place(pair) + e];
             const double p = x.x[2 * e], y = x.x[2 * e + 1];
             x.x[2 * e] = sticky_float(__builtin_fma(p, t.x, -(y * t.y)));
             x.x[2 * e + 1] = sticky_float(__builtin_fma(p, t.y, y * t.x));
@@ -161,7 +161,7 @@ __global__ __launch_bounds__(256) void paged4_append_kernel(PagedArgs a, RotaryA
           const Eight y = eight_of(ko[i]);
 #pragma unroll
           for (int e = 0; e < 8; e++) {
-            const double2 t = table[wave][pair + e];
+            const double2 t = table[wave][rotary_place(pair) + e];
             const double z = (double)y.x[e] * t.y;
             x.x[e] = sticky_float(__builtin_fma((double)x.x[e], t.x, second ? z : -z));
           }
@@ -173,36 +173,39 @@ __global__ __launch_bounds__(256) void paged4_append_kernel(PagedArgs a, RotaryA
   }
 }
 
-// A thread has words of eight codes and writes what they stand for; the rows of K of a head of a page, and those of V, are a workgroup's at a time.
+// A thread has words of eight codes, one of every so many rows, and writes what they stand for; the rows of K of a head of a page, and those of V, are a
+// workgroup's at a time.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void paged4_unpack_kernel(PagedArgs a, T* k_pages, T* v_pages) {
-  constexpr int BLOCKS = D / 32, AHEAD = 4;
-  const int heads = a.n_pages * a.h_kv, P = 1 << a.page_log;
+  constexpr int WORDS = D / 8, ROWS = 256 / WORDS, AHEAD = 4;                  // rows at a time
+  const int heads = a.n_pages * a.h_kv, P = 1 << a.page_log, w = threadIdx.x % WORDS, row0 = threadIdx.x / WORDS;
   for (int head = blockIdx.x; head < heads; head += gridDim.x) {
     const int page = head / a.h_kv, h = head - page * a.h_kv;
-    const int64_t first = (int64_t)head << a.page_log;
-    // words of codes: neighbours write side by side; several are asked for together
-    const int words = 2 * P * BLOCKS * 4;
-    for (int x0 = threadIdx.x; x0 < words; x0 += 256 * AHEAD) {
-      uint32_t word[AHEAD], scale[AHEAD];
 #pragma unroll
-      for (int i = 0; i < AHEAD; i++) {
-        const int x = min(x0 + 256 * i, words - 1), row = x / (BLOCKS * 4), in = x % (BLOCKS * 4), off = row & (P - 1);
-        const char* codes = row >= P ? (const char*)a.v + page * a.vp_p + h * a.vp_h + off * a.vp_t : (const char*)a.k + page * a.kp_p + h * a.kp_h + off * a.kp_t;
-        word[i] = reinterpret_cast<const uint32_t*>(codes)[in];
-        scale[i] = (row >= P ? a.v_sc : a.k_sc)[(first + off) * BLOCKS + in / 4];
-      }
+    for (int x = 0; x < 2; x++) {
+      const char* codes = (x ? (const char*)a.v + page * a.vp_p + h * a.vp_h : (const char*)a.k + page * a.kp_p + h * a.kp_h) + w * 4;
+      const uint32_t stride = x ? (uint32_t)a.vp_t : (uint32_t)a.kp_t;         // a page's rows span less than 2 GiB
+      const uint8_t* scales = (x ? a.v_sc : a.k_sc) + ((int64_t)head << a.page_log) * (D / 32) + w / 4;
+      T* to = (x ? v_pages : k_pages) + ((int64_t)head << a.page_log) * D + w * 8;
+      for (int r0 = row0; r0 < P; r0 += ROWS * AHEAD) {
+        uint32_t word[AHEAD], scale[AHEAD];                                    // asked for together
 #pragma unroll
-      for (int i = 0; i < AHEAD; i++) {
-        const int x = x0 + 256 * i, row = x / (BLOCKS * 4), in = x % (BLOCKS * 4);
-        if (x >= words) break;
-        T* to = (row >= P ? v_pages : k_pages) + (first + (row & (P - 1))) * D + in * 8;
-        const float s = fp4_scale(scale[i]);
-        if constexpr (sizeof(T) == 2) {
-          *reinterpret_cast<bf16x8*>(to) = fp4_to_bf16(word[i], s);
-        } else {
-          reinterpret_cast<f32x4*>(to)[0] = fp4_to_f32<0>(word[i], s);
-          reinterpret_cast<f32x4*>(to)[1] = fp4_to_f32<1>(word[i], s);
+        for (int i = 0; i < AHEAD; i++) {
+          const int r = min(r0 + i * ROWS, P - 1);
+          word[i] = *reinterpret_cast<const uint32_t*>(codes + r * stride);
+          scale[i] = scales[r * (D / 32)];
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; i++) {
+          const int r = r0 + i * ROWS;
+          if (r >= P) break;
+          const float s = fp4_scale(scale[i]);
+          if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<bf16x8*>(to + r * D) = fp4_to_bf16(word[i], s);
+          } else {
+            reinterpret_cast<f32x4*>(to + r * D)[0] = fp4_to_f32<0>(word[i], s);
+            reinterpret_cast<f32x4*>(to + r * D)[1] = fp4_to_f32<1>(word[i], s);
+          }
         }
       }
     }

@@ -48,6 +48,10 @@ __device__ __forceinline__ double2 rotary_cos_sin(const RotaryArgs& r, uint64_t 
   return make_double2(t.x * r.mscale, t.y * r.mscale);
 }
 
+// Where a pair's cosine and sine lie in LDS: a gap behind every eight, so that lanes that read eight each do not meet in the banks.  Four pairs that begin at a
+// multiple of 4 lie together.
+__host__ __device__ constexpr int rotary_place(int pair) { return pair + pair / 8; }
+
 // Eight elements of a tensor as they lie in memory: asked for early, made floats when they are used.
 template <typename T> struct Piece { u32x4 w[sizeof(T) / 2]; };
 template <typename T> __device__ __forceinline__ Piece<T> load_piece(const T* p) {
@@ -95,11 +99,11 @@ template <typename T, int D> struct Unit {
     pb = min(pb, r.half - V / 2);
   }
   struct Pairs { float2 cs[V]; };
-  template <typename C> __device__ __forceinline__ Pairs pairs(const C* cs) const {
+  template <typename C> __device__ __forceinline__ Pairs pairs(const C* cs) const {   // cs as rotary_place has them
     Pairs p;
 #pragma unroll
     for (int i = 0; i < V; i++) {
-      const C c = cs[i < V / 2 ? pa + i : pb + i - V / 2];
+      const C c = cs[i < V / 2 ? rotary_place(pa) + i : rotary_place(pb) + i - V / 2];
       p.cs[i] = make_float2((float)c.x, (float)c.y);
     }
     return p;

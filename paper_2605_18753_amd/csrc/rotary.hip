@@ -23,7 +23,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(256, 4) void rotary_kernel(RotateArgs a) {
   using U = Unit<T, D>;
   constexpr int SLOTS = 256 / (U::COUNT * kTok);             // heads at a time
-  __shared__ float2 cs[kTok][D / 2 + 1];
+  __shared__ float2 cs[kTok][rotary_place(D / 2)];
   const int t = threadIdx.x / U::COUNT % kTok, slot = threadIdx.x / (U::COUNT * kTok) + (int)blockIdx.y * SLOTS, step = SLOTS * (int)gridDim.y;
   const U unit(a.r, threadIdx.x % U::COUNT);
   // a.all tokens of all sequences, one after the other
@@ -33,7 +33,7 @@ __global__ __launch_bounds__(256, 4) void rotary_kernel(RotateArgs a) {
       const int position = (int)((a.pos ? (uint32_t)a.pos[b * a.pos_b + j] : j) + (uint32_t)a.start);
       for (int k = threadIdx.x / kTok; k < a.r.half; k += 256 / kTok) {
         const double2 v = rotary_cos_sin(a.r, a.r.turns[k], position);
-        cs[threadIdx.x & (kTok - 1)][k] = make_float2((float)v.x, (float)(a.inverse ? -v.y : v.y));
+        cs[threadIdx.x & (kTok - 1)][rotary_place(k)] = make_float2((float)v.x, (float)(a.inverse ? -v.y : v.y));
       }
     }
     __syncthreads();
