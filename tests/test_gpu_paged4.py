@@ -103,6 +103,36 @@ def test_unpack_every_code_and_scale(dtype, d):
         assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.nan_to_num(got), torch.nan_to_num(want))
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_append_and_unpack_of_codes_in_another_layout(dtype, d):
+    """Heads inside of tokens, with room behind each row of codes; K and V in layouts of their own; packed rows that are slices of one tensor.  Rows of several
+    workgroups lie side by side: every byte is its own row's."""
+    h_kv, page, n = 3, 32, 700
+    n_pages = -(-n // page) + 1
+    wide = torch.full((n_pages, page, h_kv, d // 2 + 16), 171, dtype=torch.uint8, device=DEV)
+    c = B.PagedCache4.allocate(1, h_kv, n_pages, page, d, n_pages, DEV)
+    c.k_codes = wide[..., :d // 2].transpose(1, 2)
+    c.table.copy_(torch.randperm(n_pages, generator=torch.Generator().manual_seed(1))[None])
+    c.lens.fill_(n)
+    fused = draws(30)(n, 4 * h_kv, d).to(dtype).to(DEV)
+    q, k, v = fused[:, :2 * h_kv], fused[:, 2 * h_kv:3 * h_kv], fused[:, 3 * h_kv:]
+    before = fused.cpu().clone()
+    p = B.make_paged4_params(c, n, 2 * h_kv, dtype=dtype)
+    r = B.make_rotary(d, DEV)
+    B.dash_paged4_append(p, c, k, v, torch.tensor([0, n], dtype=torch.int32, device=DEV), rotary=r, q=q, q_out=q)
+    kp, vp = (torch.full((n_pages, h_kv, page, d), 77.0, dtype=dtype, device=DEV) for _ in range(2))
+    B.dash_paged4_unpack(p, c, kp, vp)
+    assert (wide[..., d // 2:] == 171).all()
+    at = torch.arange(n)
+    where = c.table[0].cpu().long()[at // page], at % page
+    turned = R.turn(before[:, 2 * h_kv:3 * h_kv], at[:, None], R.thetas(d), "halves")[0]
+    assert torch.equal(kp.cpu().double()[where[0], :, where[1]], held(turned))
+    assert torch.equal(vp.cpu().double()[where[0], :, where[1]], held(before[:, 3 * h_kv:]))
+    check(q.cpu(), before[:, :2 * h_kv], at[:, None], R.thetas(d), "halves")
+    assert torch.equal(fused.cpu()[:, 2 * h_kv:], before[:, 2 * h_kv:])
+
+
 # ---- attention -------------------------------------------------------------------------------------------------------
 class Setup4:
     """A cache in 4 bits on the GPU and its values on the CPU.  behind: what the pages hold behind the sequences' ends (NaN: blocks that are NaN)."""
@@ -404,6 +434,13 @@ def test_pages_past_four_gigabytes():
     ref = P.Cache(*small, torch.tensor([[0, 1], [2, 3]], dtype=torch.int32), torch.tensor([1500, 1100], dtype=torch.int32))
     want, wl, tol, ltol = P.attend(ref, q, start, h_kv)
     assert ((o.cpu().double() - want).abs() <= tol).all() and ((lse.cpu().double() - wl).abs() <= ltol).all()
+    # the last token of the first sequence anew, with another scale
+    new = 100.0 * torch.randn((1, h_kv, d), generator=gen).to(BF)
+    c.table[1] = -1
+    B.dash_paged4_append(B.make_paged4_params(c, 1, h_kv), c, new.to(DEV), new.to(DEV), torch.tensor([0, 1, 1], dtype=torch.int32, device=DEV))
+    pg, off = int(pages[0, 1]), 1499 % page
+    for codes, scales in ((c.k_codes, c.k_scales), (c.v_codes, c.v_scales)):
+        assert torch.equal(R.values(codes[pg, :, off].cpu(), scales[pg, :, off].cpu()), held(new[0]))
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])

@@ -215,6 +215,18 @@ def test_in_a_graph_and_on_another_stream():
         assert torch.equal(y, want[i])
 
 
+def test_tensors_past_four_gigabytes():
+    n = (1 << 24) + 77
+    x = torch.zeros((1, 1, n, 128), dtype=BF, device=DEV)
+    rows = torch.tensor([0, 5, n // 2, (1 << 24) - 1, 1 << 24, n - 1])
+    values = draws(10)(len(rows), 128).to(BF)
+    x[0, 0, rows.to(DEV)] = values.to(DEV)
+    r = B.make_rotary(128, DEV)
+    B.dash_rotary(r, x, x)
+    check(x[0, 0, rows.to(DEV)], values, rows, R.thetas(128), "halves")
+    assert (x[0, 0, 1] == 0).all() and (x[0, 0, n - 2] == 0).all()
+
+
 # ---- appending on the way --------------------------------------------------------------------------------------------
 class Fresh:
     """Sequences with new tokens, their cache's pages on the GPU, and what an append has to make of them."""
