@@ -4,8 +4,10 @@
 // Dealing.  The host knows the number of packed rows and sequences, not their lengths, which lie on the device.  A launch has
 // a fixed grid; every workgroup finds its own work from row_start and lens (one pass over them, 64 sequences at a time).  An item of the
 // attention is a tile of a sequence's rows for one kv-head; its cost is the steps of keys that it walks.
-//   Tiles of 16 rows: the steps of all items of a kv-head lie one behind the other, and G workgroups take equal runs
+//   Tiles of 16 (or 32) rows: the steps of all items of a kv-head lie one behind the other, and G workgroups take equal runs
 //   [w F / G, (w + 1) F / G) of them: whatever the lengths, every CU streams as many keys.
+//   A run that goes on with another item has a second start and a second record to write: an item may count for `pad` steps more, in front of
+//   its first one, so that such a run has less to walk.
 //   Tiles of 128 rows: one item a workgroup; items that leave the chip idle are cut into parts.  With n items of costs c_i and W > n
 //   workgroups, parts of S = ceil(sum c_i / (W - n)) give sum ceil(c_i / S) <= W of them.  W is what is resident at once, or n and one and a
 //   half times that where the items' lengths would leave much of the chip idle; or one item a CU stays whole and the others are cut to fill up what
@@ -33,6 +35,7 @@ struct PagedArgs {
   float c1;                              // scale * log2(e)
   int wgs;                               // runs of a kv-head; 0: an item a workgroup.  Tiles of 128 rows: parts of a kv-head at most; 0: none is cut
   int whole;                             // runs: items may be left uncut; weights: two kernels share the sequences
+  int pad;                               // runs: steps that an item's start counts for
   int slots; float gain;                 // tiles of 128 rows: workgroups of a kv-head that are resident at once; what finer parts must come to
   float* part_o; float* part_ml;         // records of cut items: two of each run (the item it begins in, the one it ends in), one of each part
   const uint8_t* k_sc; const uint8_t* v_sc;   // a cache in 4 bits: its scales (k and v its codes, their strides in bytes)
@@ -173,10 +176,10 @@ template <typename F> __device__ __forceinline__ bool paged_find_part(const Page
   return false;
 }
 
-// ---- runs (tiles of 16 rows) ------------------------------------------------------------------------------------------
-// Steps are of 128 keys.  With m new tokens behind `old`, tile t of a causal call, T = 16 / g tokens, walks ceil((old + (t + 1) T) / 128) =
+// ---- runs (tiles of 16 or 32 rows) ------------------------------------------------------------------------------------------
+// Steps are of 128 keys.  With m new tokens behind `old`, tile t of a causal call, T = 16 / g (32 / g) tokens, walks ceil((old + (t + 1) T) / 128) =
 // ceil((u + t + 1) / k) steps, u = ceil(old / T), k = 128 / T, and the tiles before it H(u + t) - H(u), H(x) = sum of ceil(y / k) over
-// y = 1 .. x.  Runs are used for fewer than 4096 items, of at most 2^17 steps each: 32 bits (H may wrap, its differences do not).
+// y = 1 .. x.  Runs are used for fewer than 6144 items, of at most 2^17 steps each: 32 bits (H may wrap, its differences do not).
 constexpr int kStep = 128;
 // Adding up the pieces of an item takes as long as so many steps: items that are no longer than the runs would be by more than that are not cut, if there
 // is a workgroup for each.  (One token of sequences of 200 to 1000, 32 / 8 heads, 16 of them: 13.6 us, cut 19.1; 32: 17.7 and 23.3; one of
@@ -185,8 +188,8 @@ constexpr int kJoin = 6;
 struct PagedSeq { int tiles, u, flat; };                   // flat > 0: steps of every tile (no causal mask)
 struct PagedItem { int b, tile, r0, m, n; PagedSeq s; };
 struct PagedDeal {
-  int T, k_log;                                            // tokens of a tile, log2 of k
-  __device__ __forceinline__ PagedDeal(const PagedArgs& a) : T(16 / a.g), k_log(31 - __builtin_clz(kStep / (16 / a.g))) {}
+  int T, k_log, pad;                                       // tokens of a tile, log2 of k, steps before an item's first
+  __device__ __forceinline__ PagedDeal(const PagedArgs& a, int rows) : T(rows / a.g), k_log(31 - __builtin_clz(kStep / (rows / a.g))), pad(a.pad) {}
   __device__ __forceinline__ PagedSeq seq(const PagedArgs& a, int m, int n) const {
     return {(m + T - 1) / T, (max(n - m, 0) + T - 1) / T, a.causal ? 0 : max((n + kStep - 1) / kStep, 1)};
   }
@@ -194,7 +197,7 @@ struct PagedDeal {
     const uint32_t c = (uint32_t)x >> k_log, r = (uint32_t)x & ((1u << k_log) - 1u);
     return ((c & 1 ? c * ((c + 1) / 2) : (c / 2) * (c + 1)) << k_log) + (c + 1) * r;
   }
-  __device__ __forceinline__ int before(const PagedSeq& s, int t) const { return s.flat ? s.flat * t : (int)(h(s.u + t) - h(s.u)); }
+  __device__ __forceinline__ int before(const PagedSeq& s, int t) const { return (s.flat ? s.flat * t : (int)(h(s.u + t) - h(s.u))) + pad * t; }
   __device__ __forceinline__ int steps(const PagedSeq& s, int t) const { return s.flat ? s.flat : ((s.u + t) >> k_log) + 1; }
   // the steps of all items of a kv-head, and if they may be left uncut how many there are, and the steps of the longest; a wave's lanes together; l0: the first 64 sequences
   __device__ __forceinline__ int total(const PagedArgs& a, const PagedLane& l0, int& items, int& most) const {
@@ -248,17 +251,17 @@ struct PagedDeal {
 // Where run w of G = min(a.wgs, F) begins: floor(w F / G), the fraction's part in floats (a numerator below 2^20 and a half, whose
 // quotient is nearer than 2^-12 to exact and not nearer than 2^-11 to a whole number).  No run is empty.  I: type of a place.
 template <typename I> struct PagedBounds {
-  I q, total;
+  I q, total, pad;
   uint32_t rem;
   int runs;
   float inv;
-  __device__ __forceinline__ PagedBounds(const PagedArgs& a, I f) : total(f), runs((int)max(min((I)a.wgs, f), (I)1)) {
+  __device__ __forceinline__ PagedBounds(const PagedArgs& a, I f, I pad = 0) : total(f), pad(pad), runs((int)max(min((I)a.wgs, f), (I)1)) {
     q = f / runs;
     rem = (uint32_t)(f - q * runs);
     inv = 1.f / (float)runs;
   }
   __device__ __forceinline__ I at(int w) const {
-    return w >= runs ? total : q * w + (I)(uint32_t)(((float)(rem * (uint32_t)w) + 0.5f) * inv);
+    return pad + (w >= runs ? total : q * w + (I)(uint32_t)(((float)(rem * (uint32_t)w) + 0.5f) * inv));
   }
 };
 
@@ -281,13 +284,13 @@ struct PagedRun {
   PagedItem it;
   int x0, x1, cost;
   int next, end, total;                                    // the step behind this piece, the run's end, the steps of the kv-head
-  __device__ __forceinline__ PagedRun(const PagedArgs& a) : deal(a) {}
+  __device__ __forceinline__ PagedRun(const PagedArgs& a, int rows = 16) : deal(a, rows) {}
   __device__ __forceinline__ bool begin(const PagedArgs& a, int wg) {
     const PagedLane l0 = paged_lane(a, lane_id());
     bool cut = a.wgs > 0;
     if (cut) {
       int items, most;
-      total = deal.total(a, l0, items, most);
+      total = deal.total(a, l0, items, most) - deal.pad;
       cut = !a.whole || items > a.wgs || (most - kJoin) * a.wgs > total;
     }
     if (!cut) {
@@ -296,15 +299,18 @@ struct PagedRun {
       x1 = cost = deal.steps(it.s, it.tile);
       return true;
     }
-    const PagedBounds<int> b(a, total);
+    const PagedBounds<int> b(a, total, deal.pad);
     next = __builtin_amdgcn_readfirstlane(b.at(wg));
     end = __builtin_amdgcn_readfirstlane(b.at(wg + 1));
     if (next >= end) return false;
-    x0 = deal.find(a, l0, next, true, it);
+    const int in = deal.find(a, l0, next, true, it);
+    x0 = max(in - deal.pad, 0);
+    next += x0 + deal.pad - in;
     cost = deal.steps(it.s, it.tile);
     return piece();
   }
   __device__ __forceinline__ bool piece() {
+    if (next >= end) return false;                         // no more than an item's start
     x1 = min(cost, x0 + end - next);
     next += x1 - x0;
     return true;
@@ -313,6 +319,7 @@ struct PagedRun {
     if (next >= end) return false;
     x0 = 0;
     if (++it.tile >= it.s.tiles) deal.find(a, paged_lane(a, lane_id()), next, true, it);
+    next += deal.pad;
     cost = deal.steps(it.s, it.tile);
     return piece();
   }

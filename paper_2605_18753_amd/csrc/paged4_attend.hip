@@ -1,26 +1,25 @@
 // Attention of packed new tokens over a paged cache in 4 bits (fp4.h): the walks of paged_attend.hip, whose dealing and joining they use.
 //
-// Few rows: a tile is 16 (token, head) rows.  K goes from the pages into registers: the contraction over d runs in the order in which a lane's
+// Few rows: a tile is 16 (token, head) rows, or two groups of 16 that share what is read and converted.  K goes from the pages into registers: the contraction over d runs in the order in which a lane's
 // codes lie, d = D / 4 kq + .., so 16 bytes of a row are one load, one scale and, converted, the lane's operands of all steps.  V is converted into LDS, from
 // where transposing reads give its operands.  The next tile's loads are in flight while a tile is worked on.  Bound by HBM where the cache is long: 32 sequences
-// of 4096 to 32768 tokens, 32 / 8 heads of 128, 128 us, 660 MB at 5.2 TB/s, of which 10 us are the launch's start and end (the vector units issue in 0.42 of the
+// of 4096 to 32768 tokens, 32 / 8 heads of 128, 125 us, 660 MB at 5.3 TB/s, of which 8 us are the launch's start and end (the vector units issue in 0.42 of the
 // clocks); by latency where it is short: one sequence of 1000 tokens 9.2 us.
 #include "fp4.h"
 #include "paged_few.h"
 
 namespace dash {
 
-template <int D> struct Few4Cfg {
+template <int D, int ROWS = 16> struct Few4Cfg {
   static constexpr int CW = D / 32;                        // words of a lane's codes: a quarter of a row
   static constexpr int ROW_BYTES = D * 2, TILE_BYTES = 32 * ROW_BYTES;   // V of 32 keys in bf16
-  static constexpr int OUT_BYTES = 4 * 16 * (D + 6) * 4;   // the waves' results, behind the walk
+  static constexpr int OUT_BYTES = 4 * ROWS * (D + 6) * 4;   // the waves' results, behind the walk
   static constexpr int LDS_BYTES = 4 * TILE_BYTES > OUT_BYTES ? 4 * TILE_BYTES : OUT_BYTES;
 };
 // Position of 16-byte chunk c of V's row: 4 rows x 2 chunks (transposing reads) and 4 rows x 4 chunks a quarter of a row apart (writes) spread over all banks.
 template <int D> __device__ __forceinline__ int v4_swz(int row) { return D == 128 ? (row & 3) * 5 : ((row >> 1) & 1) * 5; }
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32v4 __attribute__((ext_vector_type(4)));
 template <int CW> struct Codes { uint32_t w[CW]; };
 template <int CW> __device__ __forceinline__ Codes<CW> load_codes(__amdgpu_buffer_rsrc_t rs, uint32_t off) {
   Codes<CW> c;
@@ -130,28 +129,32 @@ template <int D> struct Walk4 {
   }
 };
 
-template <int D>
-__global__ __launch_bounds__(256, D == 128 ? 2 : 4) void paged_few4_kernel(PagedArgs args) {
+template <int D, int G>
+__global__ __launch_bounds__(256, D == 128 ? 2 : 3) void paged_few4_kernel(PagedArgs args) {
   using C = Few4Cfg<D>;
+  constexpr int ROWS = 16 * G;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int r = blockIdx.x % args.h_kv, wg = blockIdx.x / args.h_kv;
-  PagedRun run(args);
+  PagedRun run(args, ROWS);
   if (!run.begin(args, wg)) return;
   const PagedItem& it = run.it;
   do {
   const PagedArgs a = paged_reload();
   const int tid = paged_thread(), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int T = 16 / a.g;
+  const int T = ROWS / a.g;
   const int t0 = it.tile * T;
   const int n = lane & 15, kq = lane >> 4;
-  const int t = t0 + n / a.g;
-  bf16x8 qf[D / 32];
-  {
-    const uint16_t* qp = (const uint16_t*)a.q + (it.r0 + min(t, it.m - 1)) * a.q_t + (r * a.g + n % a.g) * a.q_h + kq * (D / 4);
+  // group i of rows: 16 i + n
+  bf16x8 qf[G][D / 32];
+  int last[G];
 #pragma unroll
-    for (int s = 0; s < D / 32; s++) qf[s] = *reinterpret_cast<const bf16x8*>(qp + 8 * s);
+  for (int i = 0; i < G; i++) {
+    const int row = 16 * i + n, t = t0 + row / a.g;
+    const uint16_t* qp = (const uint16_t*)a.q + (it.r0 + min(t, it.m - 1)) * a.q_t + (r * a.g + row % a.g) * a.q_h + kq * (D / 4);
+#pragma unroll
+    for (int s = 0; s < D / 32; s++) qf[i][s] = *reinterpret_cast<const bf16x8*>(qp + 8 * s);
+    last[i] = t < it.m ? paged_last_key(a, it, t) : -1;
   }
-  const int last = t < it.m ? paged_last_key(a, it, t) : -1;
   const int first_last = paged_last_key(a, it, t0);                              // of the tile's first token
   const int end = max(paged_last_key(a, it, min(t0 + T, it.m) - 1) + 1, 0);      // keys that a row of the tile sees
   // the wave's 32-key tiles of the piece's 128-key steps
@@ -163,10 +166,14 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void paged_few4_kernel(Paged
   // transposing read of V: lane s of a group of 16 points at row 4 kq + s / 4 (+ 16), d 4 (s % 4) of the 16-wide d-tile
   const uint32_t v_rd = buf + (uint32_t)((4 * kq + (n >> 2)) * C::ROW_BYTES + ((((n & 3) >> 1) ^ v4_swz<D>(n >> 2)) << 4) + ((n & 1) << 3));
 
-  float m_run = -INFINITY, l_run = 0.f;
-  f32x4 oacc[D / 16];
+  float m_run[G], l_run[G];
+  f32x4 oacc[G][D / 16];
 #pragma unroll
-  for (int dt = 0; dt < D / 16; dt++) oacc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < G; i++) {
+    m_run[i] = -INFINITY; l_run[i] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; dt++) oacc[i][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
 
   // Two sets of registers in turn: the next tile's loads are asked for before the present ones are waited for.
   typename Walk4<D>::Raw even, odd;
@@ -180,42 +187,55 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void paged_few4_kernel(Paged
     entries = walk.entries_of(j + 8);
     const uint32_t vs[2] = {walk.v_scale(x, 0), walk.v_scale(x, 1)};
     walk.put_v(x, vs, 0);
-    f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = s0;                                    // lane (row n, kq): keys 4 kq + i, 16 + 4 kq + i
+    f32x4 s0[G], s1[G];                                                          // lane (row n, kq): keys 4 kq + i, 16 + 4 kq + i
     const float k0 = fp4_scale(walk.k_scale(x, 0)), k1 = fp4_scale(walk.k_scale(x, 1));
 #pragma unroll
-    for (int s = 0; s < D / 32; s++) {
-      s0 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp4_to_bf16(x.k[0].w[s], k0), qf[s], s0, 0, 0, 0);
-      s1 = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fp4_to_bf16(x.k[1].w[s], k1), qf[s], s1, 0, 0, 0);
-    }
-    if (j * 32 + 31 > first_last || t0 + T > it.m) {
-      const int lim = last - (j * 32 + 4 * kq);
+    for (int i = 0; i < G; i++) s0[i] = s1[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 4; i++) {
-        s0[i] = i > lim ? -INFINITY : s0[i];
-        s1[i] = 16 + i > lim ? -INFINITY : s1[i];
+    for (int s = 0; s < D / 32; s++) {
+      const bf16x8 x0 = fp4_to_bf16(x.k[0].w[s], k0), x1 = fp4_to_bf16(x.k[1].w[s], k1);
+#pragma unroll
+      for (int i = 0; i < G; i++) {
+        s0[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x0, qf[i][s], s0[i], 0, 0, 0);
+        s1[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x1, qf[i][s], s1[i], 0, 0, 0);
       }
     }
-    float mx = fmaxf(fmaxf(fmaxf(s0[0], s0[1]), fmaxf(s0[2], s0[3])), fmaxf(fmaxf(s1[0], s1[1]), fmaxf(s1[2], s1[3])));
-    mx = quad_rows_max(mx) * a.c1;
-    if (__any(mx > m_run + kPagedLazy)) {
-      const float m_new = fmaxf(m_run, mx), use = m_new == -INFINITY ? 0.f : m_new;
-      const float corr = __builtin_amdgcn_exp2f(m_run - use);
-      m_run = m_new;
-      l_run *= corr;
+    if (j * 32 + 31 > first_last || t0 + T > it.m) {
 #pragma unroll
-      for (int dt = 0; dt < D / 16; dt++) oacc[dt] *= corr;
-    }
-    const float off = m_run == -INFINITY ? 0.f : -m_run;
-    float p[8];
+      for (int g = 0; g < G; g++) {
+        const int lim = last[g] - (j * 32 + 4 * kq);
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      p[i] = __builtin_amdgcn_exp2f(fmaf(s0[i], a.c1, off));
-      p[4 + i] = __builtin_amdgcn_exp2f(fmaf(s1[i], a.c1, off));
+        for (int i = 0; i < 4; i++) {
+          s0[g][i] = i > lim ? -INFINITY : s0[g][i];
+          s1[g][i] = 16 + i > lim ? -INFINITY : s1[g][i];
+        }
+      }
     }
-    l_run += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-    // P in bf16, the operand type of the matrix cores (relative error 2^-9); the row sum takes the unrounded values
-    const u32x4 pw = {cvt_bf16x2(p[0], p[1]), cvt_bf16x2(p[2], p[3]), cvt_bf16x2(p[4], p[5]), cvt_bf16x2(p[6], p[7])};
-    const bf16x8 pb = __builtin_bit_cast(bf16x8, pw);
+    bf16x8 pb[G];
+#pragma unroll
+    for (int g = 0; g < G; g++) {
+      float mx = fmaxf(fmaxf(fmaxf(s0[g][0], s0[g][1]), fmaxf(s0[g][2], s0[g][3])), fmaxf(fmaxf(s1[g][0], s1[g][1]), fmaxf(s1[g][2], s1[g][3])));
+      mx = quad_rows_max(mx) * a.c1;
+      if (__any(mx > m_run[g] + kPagedLazy)) {
+        const float m_new = fmaxf(m_run[g], mx), use = m_new == -INFINITY ? 0.f : m_new;
+        const float corr = __builtin_amdgcn_exp2f(m_run[g] - use);
+        m_run[g] = m_new;
+        l_run[g] *= corr;
+#pragma unroll
+        for (int dt = 0; dt < D / 16; dt++) oacc[g][dt] *= corr;
+      }
+      const float off = m_run[g] == -INFINITY ? 0.f : -m_run[g];
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        p[i] = __builtin_amdgcn_exp2f(fmaf(s0[g][i], a.c1, off));
+        p[4 + i] = __builtin_amdgcn_exp2f(fmaf(s1[g][i], a.c1, off));
+      }
+      l_run[g] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      // P in bf16, the operand type of the matrix cores (relative error 2^-9); the row sum takes the unrounded values
+      const u32x4 pw = {cvt_bf16x2(p[0], p[1]), cvt_bf16x2(p[2], p[3]), cvt_bf16x2(p[4], p[5]), cvt_bf16x2(p[6], p[7])};
+      pb[g] = __builtin_bit_cast(bf16x8, pw);
+    }
     asm volatile("" ::: "memory");                                               // a wave's LDS operations complete in order
     bf16x8 vf[D / 16];
 #pragma unroll
@@ -225,9 +245,12 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void paged_few4_kernel(Paged
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int dt = 0; dt < D / 16; dt++) oacc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[dt], pb, oacc[dt], 0, 0, 0);
+    for (int dt = 0; dt < D / 16; dt++)
+#pragma unroll
+      for (int g = 0; g < G; g++) oacc[g][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[dt], pb[g], oacc[g][dt], 0, 0, 0);
     asm volatile("" ::: "memory");
-    walk.spoil(vs, j, last, oacc);
+#pragma unroll
+    for (int g = 0; g < G; g++) walk.spoil(vs, j, last[g], oacc[g]);
   };
   while (j < j1) {
     tile(even, odd);
@@ -235,20 +258,23 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 4) void paged_few4_kernel(Paged
     tile(odd, even);
     j += 4;
   }
-  const float l_tot = quad_rows_sum(l_run);
   __syncthreads();
-  float* x = reinterpret_cast<float*>(lds);                                      // [4][16][D + 4]
-  float* ml = x + 4 * 16 * (D + 4);
-  float* own = x + (wave * 16 + n) * (D + 4) + 4 * kq;
+  float* x = reinterpret_cast<float*>(lds);                                      // [4][ROWS][D + 4]
+  float* ml = x + 4 * ROWS * (D + 4);
 #pragma unroll
-  for (int dt = 0; dt < D / 16; dt++) *reinterpret_cast<f32x4*>(own + 16 * dt) = oacc[dt];
-  if (kq == 0) {
-    ml[(wave * 16 + n) * 2] = m_run;
-    ml[(wave * 16 + n) * 2 + 1] = l_tot;
+  for (int g = 0; g < G; g++) {
+    const float l_tot = quad_rows_sum(l_run[g]);
+    const int row = wave * ROWS + 16 * g + n;
+#pragma unroll
+    for (int dt = 0; dt < D / 16; dt++) *reinterpret_cast<f32x4*>(x + row * (D + 4) + 4 * kq + 16 * dt) = oacc[g][dt];
+    if (kq == 0) {
+      ml[row * 2] = m_run[g];
+      ml[row * 2 + 1] = l_tot;
+    }
   }
   __syncthreads();
-  paged_few_finish<uint16_t, D, 4>(a, run, r, ((int64_t)r * a.wgs + wg) * 2 + (run.x0 == 0), t0, x, ml);
-  if (!run.whole()) paged_few_join<uint16_t, D, 256>(a, run, r, wg, lds);
+  paged_few_finish<uint16_t, D, 4, ROWS>(a, run, r, ((int64_t)r * a.wgs + wg) * 2 + (run.x0 == 0), t0, x, ml);
+  if (!run.whole()) paged_few_join<uint16_t, D, 256, ROWS>(a, run, r, wg, lds);
   __syncthreads();
   } while (run.advance(args));
 }
@@ -562,36 +588,53 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_rows4_kernel(Paged
 // ---- host ------------------------------------------------------------------------------------------------------------
 // fp32: 512 threads for an item, fewer than 2^32 in all, as paged_attend_fits
 bool paged4_attend_fits(const PagedArgs& a, int dtype) { return dtype != DASH_F32 || paged_most_items(a, 16) * a.h_kv < (1 << 23); }
-// The kernel for a call: tiles of 128 rows where the sequences bring more than 48 rows each on the average, tiles of 16 otherwise, and for short caches as for pages
-// of bf16.  (Tiles of 128 and of 16.  32 / 8 heads of 128, 8 sequences of 3000 to 16000: 32 rows each 55.7 and 41.0 us, 48 63.4 and 53.0, 80 66.6 and 77.5; 64 of
-// 2000: 74.8, 82.9, 85.9 and 50.7, 72.4, 117; head dimension 64, 8 sequences: 32 rows 43.5 and 32.0, 80 50.4 and 55.4.  Heads in a group of 16, two kv-heads: 48 rows
-// 28.8 and 30.0, 80 30.9 and 32.8.)
-static bool use_rows(const PagedArgs& a, int dtype) {
-  return dtype == DASH_BF16 && (int64_t)a.n_rows * a.g > (int64_t)a.batch * 48 && !(a.cap <= 8 * kStep && paged_most_items(a, 16) * a.h_kv <= 256);
-}
 // Workgroups of a kv-head that are resident at once: two a CU at head dimension 128, three at 64 (of 16-row tiles, of which four are, three runs a CU are as fast:
 // 32 sequences of 4096 to 32768 75.7 us, four 76.3).
-static int runs_of(const PagedArgs& a, int dtype, int d, bool big) { return max((dtype == DASH_F32 ? 256 : d == 128 ? 512 : 768) / a.h_kv, 1); }
+static int runs_of(const PagedArgs& a, int dtype, int d) { return max((dtype == DASH_F32 ? 256 : d == 128 ? 512 : 768) / a.h_kv, 1); }
+// Rows of a call's tiles.  128 where the sequences bring more than 80 each on the average, but for short caches, as for pages of bf16; else 32 where they bring
+// more than 16 and there are tiles for every fourth run, so that few are cut into many pieces, whose records grow with a tile's rows; else 16.
+// (Tiles of 16, of 32 and of 128.  32 / 8 heads of 128, sequences of 3000 to 16000.  One of 20 rows: 18.4, 25.5, 22.3 us.  8 of 32 rows: 37.4, 38.8, 54.4; 64 rows: 62.0, 49.9,
+// 62.5; 80: 74.7, 65.6, 64.8.  24 of 20: 86.9, 66.4, 169; 48: 121, 111, 192; 64: 154, 114, 193.  16 of 80: 133, 114, 128.  64 of 2000 tokens, 48 rows: 72.0, 64.3, 79.9; 80: 117,
+// 93.1, 83.1.  Heads in a group of 16, two kv-heads, 8 sequences: 32 rows 23.1, 29.5, 25.6, 64 27.1, 31.6, 29.4, 96 32.4, 36.6, 31.6; 32 sequences, 64 rows: 61.2, 47.7, 58.9.  Head
+// dimension 64, 8 sequences: 48 rows 36.0, 37.9, 40.5, 64 44.2, 37.4, 40.8; 32 sequences, 64 rows: 131, 94.3, 132.)
+static int tile_rows(const PagedArgs& a, int dtype, int d) {
+  const int64_t rows = (int64_t)a.n_rows * a.g;
+  if (dtype != DASH_BF16) return 16;
+  if (rows > (int64_t)a.batch * 80 && !(a.cap <= 8 * kStep && paged_most_items(a, 16) * a.h_kv <= 256)) return 128;
+  return rows > (int64_t)a.batch * 16 && paged_most_items(a, 32) * 4 >= runs_of(a, dtype, d) ? 32 : 16;
+}
 static size_t ws_align(size_t x) { return (x + 255) & ~(size_t)255; }
 
 size_t paged4_attend_ws(const PagedArgs& a, int dtype, int d) {
-  const size_t few = (size_t)runs_of(a, dtype, d, false) * a.h_kv * 2 * 16;         // rows of records
-  const size_t rows = dtype == DASH_BF16 ? (size_t)paged_most_parts(runs_of(a, dtype, d, true)) * a.h_kv * 128 : 0, recs = few > rows ? few : rows;
+  const size_t few = (size_t)runs_of(a, dtype, d) * a.h_kv * 2 * 16;         // rows of records; with tiles of 32 twice as many, fewer than `rows`
+  const size_t rows = dtype == DASH_BF16 ? (size_t)paged_most_parts(runs_of(a, dtype, d)) * a.h_kv * 128 : 0, recs = few > rows ? few : rows;
   return ws_align(recs * 8) + recs * d * 4 + few / 16 * 16;                      // two flags a record of 16 rows
+}
+
+template <int D, int G> static hipError_t launch_few4(const PagedArgs& a, dim3 grid, hipStream_t st) {
+  constexpr int lds = Few4Cfg<D, 16 * G>::LDS_BYTES;
+  static LdsOptIn opt_in;
+  if (hipError_t e = allow_dyn_lds((const void*)(paged_few4_kernel<D, G>), lds, opt_in); e != hipSuccess) return e;
+  hipLaunchKernelGGL((paged_few4_kernel<D, G>), grid, dim3(256), lds, st, a);
+  return hipSuccess;
 }
 
 template <int D>
 static hipError_t launch_attend4(PagedArgs a, int dtype, char* ws, hipStream_t st) {
-  const bool big = use_rows(a, dtype);
-  const int runs = runs_of(a, dtype, D, big);
-  const int64_t items = paged_most_items(a, big ? 128 : 16);
+  const int tile = tile_rows(a, dtype, D);
+  const bool big = tile == 128;
+  const int runs = runs_of(a, dtype, D);
+  const int64_t items = paged_most_items(a, tile);
   a.wgs = items < (big ? 2 : 8) * (int64_t)runs ? runs : 0;
   if (big && a.wgs && items * 4 >= runs) a.wgs = (int)items + runs * 3 / 2;
   a.slots = runs;
   a.gain = (int64_t)a.n_rows * a.g < 64 * items ? 0.65f : 0.9f;
+  // An item's start (and the end of the piece before it) takes as long as so many steps.  (0, 3, 4, 5, 8 of them: one token of 32 sequences of 4096 to 32768 128.2, 125.7, 124.4,
+  // 126.6 and 127.9 us, of 8 of 384 to 16000 26.3, 24.0, 23.4, 23.5 and 24.7; of like lengths, where all runs begin with an item, 20.4, 20.8, 21.5, 21.5 and 21.5.)
+  a.pad = 4;
   a.whole = items * 2 >= runs;                               // fewer items: not looked into
   if (!big && a.cap <= 8 * kStep && items * a.h_kv >= 128) a.wgs = 0;
-  const size_t recs = (size_t)a.wgs * a.h_kv * (big ? 128 : 2 * 16);
+  const size_t recs = (size_t)a.wgs * a.h_kv * (big ? 128 : 2 * tile);
   a.part_ml = (float*)ws;
   a.part_o = (float*)(ws + ws_align(recs * 8));
   a.flags = (uint64_t*)((char*)a.part_o + recs * D * 4);     // runs only
@@ -605,9 +648,7 @@ static hipError_t launch_attend4(PagedArgs a, int dtype, char* ws, hipStream_t s
     return e != hipSuccess || a.wgs <= 1 ? e : launch_paged_merge(a, D, st);
   }
   if (dtype == DASH_BF16) {
-    static LdsOptIn opt_in;
-    if (hipError_t e = allow_dyn_lds((const void*)paged_few4_kernel<D>, Few4Cfg<D>::LDS_BYTES, opt_in); e != hipSuccess) return e;
-    hipLaunchKernelGGL(paged_few4_kernel<D>, grid, dim3(256), Few4Cfg<D>::LDS_BYTES, st, a);
+    if (hipError_t e = tile == 32 ? launch_few4<D, 2>(a, grid, st) : launch_few4<D, 1>(a, grid, st); e != hipSuccess) return e;
   } else {
     constexpr int lds = 8 * 16 * (D + 6) * 4;
     static LdsOptIn opt_in;

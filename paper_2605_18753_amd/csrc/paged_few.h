@@ -12,6 +12,7 @@
 
 namespace dash {
 
+typedef uint32_t u32v4 __attribute__((ext_vector_type(4)));
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kPagedLazy = 8.f;        // slack of the running maximum, in base-2 logit units: exponentials stay below 2^8
 
@@ -34,21 +35,34 @@ __device__ __forceinline__ void put_row4(uint16_t* p, f32x4 o, float inv) {
 }
 __device__ __forceinline__ void put_row4(float* p, f32x4 o, float inv) { *reinterpret_cast<f32x4*>(p) = o * inv; }
 
-// What the waves hold of a tile's 16 rows is added up in LDS, and written as the output or as a record of the piece.
-// x: [WAVES][16][D + 4] floats, ml: [WAVES][16][2].  Of the first 256 threads, 16 i .. + 15 hold row i.
-template <typename T, int D, int WAVES>
+// Records of a launch's pieces, ROWS rows of D floats each, past the caches as agent_store and agent_load, 16 bytes at a time.
+template <int D, int ROWS> struct PagedRecords {
+  static constexpr int AGENT = 16;                           // scope of the access: the device (sc1)
+  __amdgpu_buffer_rsrc_t rs;
+  __device__ __forceinline__ PagedRecords(const PagedArgs& a)
+      : rs(__builtin_amdgcn_make_buffer_rsrc(a.part_o, 0, a.wgs * a.h_kv * (2 * ROWS * D * 4), 0x00020000)) {}
+  __device__ __forceinline__ uint32_t place(int64_t rec, int row, int c) const { return (((uint32_t)rec * ROWS + row) * D + c) * 4; }
+  __device__ __forceinline__ void store(uint32_t at, f32x4 x) const { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32v4, x), rs, at, 0, AGENT); }
+  __device__ __forceinline__ f32x4 load(uint32_t at) const { return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rs, at, 0, AGENT)); }
+};
+
+// What the waves hold of a tile's ROWS rows is added up in LDS, and written as the output or as a record of the piece.
+// x: [WAVES][ROWS][D + 4] floats, ml: [WAVES][ROWS][2].  Of the first 256 threads, 16 i .. + 15 hold row i, row 16 + i ..
+template <typename T, int D, int WAVES, int ROWS = 16>
 __device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const PagedRun& run, int r, int64_t rec, int t0, const float* x, const float* ml) {
   const PagedItem& it = run.it;
-  const int row = threadIdx.x >> 4, c = threadIdx.x & 15;
-  if (WAVES > 4 && row >= 16) return;
+  const int c = threadIdx.x & 15;
+#pragma unroll
+  for (int row = threadIdx.x >> 4, rows = 0; rows < ROWS; row += 16, rows += 16) {
+  if (WAVES > 4 && row >= ROWS) return;
   float M = -INFINITY, den = 0.f, w[WAVES];
 #pragma unroll
-  for (int i = 0; i < WAVES; i++) M = fmaxf(M, ml[(i * 16 + row) * 2]);
+  for (int i = 0; i < WAVES; i++) M = fmaxf(M, ml[(i * ROWS + row) * 2]);
   const float use = M == -INFINITY ? 0.f : M;
 #pragma unroll
   for (int i = 0; i < WAVES; i++) {
-    w[i] = __builtin_amdgcn_exp2f(ml[(i * 16 + row) * 2] - use);
-    den = fmaf(w[i], ml[(i * 16 + row) * 2 + 1], den);
+    w[i] = __builtin_amdgcn_exp2f(ml[(i * ROWS + row) * 2] - use);
+    den = fmaf(w[i], ml[(i * ROWS + row) * 2 + 1], den);
   }
   float o[D / 16];
 #pragma unroll
@@ -56,7 +70,7 @@ __device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const Paged
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < WAVES; i++) {
-      const f32x4 y = *reinterpret_cast<const f32x4*>(x + (i * 16 + row) * (D + 4) + j * 64 + c * 4);
+      const f32x4 y = *reinterpret_cast<const f32x4*>(x + (i * ROWS + row) * (D + 4) + j * 64 + c * 4);
 #pragma unroll
       for (int e = 0; e < 4; e++) s[e] = fmaf(w[i], y[e], s[e]);
     }
@@ -66,14 +80,11 @@ __device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const Paged
   const int t = t0 + row / a.g, head = r * a.g + row % a.g;
   if (t >= it.m) return;
   if (!run.whole()) {
-    float* po = a.part_o + (rec * 16 + row) * D + c * 4;
+    const PagedRecords<D, ROWS> recs(a);
 #pragma unroll
-    for (int j = 0; j < D / 64; j++) {
-      agent_store(po + j * 64, o[j * 4], o[j * 4 + 1]);
-      agent_store(po + j * 64 + 2, o[j * 4 + 2], o[j * 4 + 3]);
-    }
-    if (c == 0) agent_store(a.part_ml + (rec * 16 + row) * 2, M, den);
-    return;
+    for (int j = 0; j < D / 64; j++) recs.store(recs.place(rec, row, j * 64 + c * 4), f32x4{o[j * 4], o[j * 4 + 1], o[j * 4 + 2], o[j * 4 + 3]});
+    if (c == 0) agent_store(a.part_ml + (rec * ROWS + row) * 2, M, den);
+    continue;
   }
   const float inv = den > 0.f ? 1.f / den : den == 0.f ? 0.f : den;     // NaN stays
   T* op = (T*)a.o + (it.r0 + t) * a.o_t + head * a.o_h;
@@ -81,6 +92,7 @@ __device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const Paged
   for (int j = 0; j < D / 64; j++)
     put_row4(op + j * 64 + c * 4, f32x4{o[j * 4], o[j * 4 + 1], o[j * 4 + 2], o[j * 4 + 3]}, inv);
   if (a.lse && c == 0) a.lse[(int64_t)(it.r0 + t) * a.h_q + head] = den == 0.f ? -INFINITY : (M + log2f(den)) * kLn2;
+  }
 }
 
 // Partial results of a row (maximum m of the base-2 logits, sum, 4 values of the product) added one by one: what has to be loaded of
@@ -108,7 +120,7 @@ struct PagedSum {
 // up the groups and clears the flags, none of which is set after that.  (16 heads on one, one sequence of 16000 tokens, 125 pieces: 92 us in one
 // level, 20 in two; 32 on 8, 1000 tokens, 8 pieces: 11 in two, 9.3 in one.)
 constexpr int kChain = 24;
-template <typename T, int D, int THREADS>
+template <typename T, int D, int THREADS, int ROWS = 16>
 __device__ __forceinline__ void paged_few_join(const PagedArgs& a, const PagedRun& run, int r, int wg, char* lds) {
   constexpr int TPR = D / 4, UNITS = THREADS / TPR;        // threads of a row; rows at a time
   const PagedItem& it = run.it;
@@ -116,7 +128,7 @@ __device__ __forceinline__ void paged_few_join(const PagedArgs& a, const PagedRu
   float* xd = reinterpret_cast<float*>(xo + THREADS);
   int* all = reinterpret_cast<int*>(xd + 2 * UNITS);
   const int lane = threadIdx.x & 63, begin = run.next - run.x1, end = begin + run.cost;
-  const PagedBounds<int> bounds(a, run.total);
+  const PagedBounds<int> bounds(a, run.total, run.deal.pad);
   int w1 = wg, pieces = 1;
   for (int k0 = wg; k0 > 0; k0 -= 64) {
     const int more = __popcll(__ballot(k0 - lane > 0 && bounds.at(max(k0 - lane, 0)) > begin));
@@ -150,36 +162,49 @@ __device__ __forceinline__ void paged_few_join(const PagedArgs& a, const PagedRu
   const int rows = min(run.deal.T, it.m - it.tile * run.deal.T) * a.g;
   const int slices = rows * 4 <= UNITS ? 4 : rows * 2 <= UNITS ? 2 : 1, per = UNITS / slices;
   const int c = threadIdx.x % TPR, unit = threadIdx.x / TPR, slice = unit / per;
+  const PagedRecords<D, ROWS> recs(a);
   // adds up `count` records, place(i) the i-th; write(row, sum) by the threads that hold a row's sum
   auto add_up = [&](int count, auto&& place, auto&& write) {
-    for (int i0 = 0; i0 < rows; i0 += per) {
-      const int in = min(i0 + unit % per, rows - 1);
-      const float* ml = a.part_ml + in * 2;
-      PagedSum sum;
-      const float* po = a.part_o + in * D + c * 4;
-      for (int p0 = slice; p0 < count; p0 += 4 * slices) {
-        uint64_t y[4], v0[4], v1[4];
+    constexpr int RG = D / 64, KP = 4;                        // rows of a thread, and records, asked for together; and as many records again where there are more
+    for (int i0 = 0; i0 < rows; i0 += per * RG) {
+      PagedSum sum[RG];
+      for (int p0 = 0; p0 < count; p0 += 2 * KP * slices) {
+        uint64_t y[RG][2 * KP];
+        f32x4 v[RG][2 * KP];
 #pragma unroll
-        for (int k = 0; k < 4; k++) {                        // asked for together; behind the last one it again
-          const int64_t at = place(min(p0 + k * slices, count - 1));
-          y[k] = agent_load(ml + at * 32);
-          v0[k] = agent_load(po + at * (16 * D));
-          v1[k] = agent_load(po + at * (16 * D) + 2);
+        for (int g = 0; g < RG; g++)
+#pragma unroll
+          for (int k0 = 0; k0 < 2 * KP; k0 += KP) {
+            if ((g && i0 + per >= rows) || (k0 && p0 + KP * slices >= count)) continue;
+            const int in = min(i0 + g * per + unit % per, rows - 1);
+            const float* ml = a.part_ml + in * 2;
+#pragma unroll
+            for (int k = k0; k < k0 + KP; k++) {             // behind the last one it again
+              const int64_t at = place(min(p0 + slice + k * slices, count - 1));
+              y[g][k] = agent_load(ml + at * (2 * ROWS));
+              v[g][k] = recs.load(recs.place(at, in, c * 4));
+            }
+          }
+#pragma unroll
+        for (int g = 0; g < RG; g++)
+#pragma unroll
+          for (int k = 0; k < 2 * KP; k++)
+            if (p0 + slice + k * slices < count && (g == 0 || i0 + per < rows))
+              sum[g].add(__uint_as_float((uint32_t)y[g][k]), __uint_as_float((uint32_t)(y[g][k] >> 32)), v[g][k]);
+      }
+#pragma unroll
+      for (int g = 0; g < RG; g++) {
+        if (g && i0 + per >= rows) break;
+        if (slices > 1) {
+          __syncthreads();
+          xo[threadIdx.x] = sum[g].o;
+          if (c == 0) { xd[2 * unit] = sum[g].m; xd[2 * unit + 1] = sum[g].den; }
+          __syncthreads();
+          for (int k = 1; k < slices && slice == 0; k++) sum[g].add(xd[2 * (unit + k * per)], xd[2 * (unit + k * per) + 1], xo[threadIdx.x + k * per * TPR]);
         }
-#pragma unroll
-        for (int k = 0; k < 4; k++)
-          if (p0 + k * slices < count)
-            sum.add(__uint_as_float((uint32_t)y[k]), __uint_as_float((uint32_t)(y[k] >> 32)),
-                    f32x4{__uint_as_float((uint32_t)v0[k]), __uint_as_float((uint32_t)(v0[k] >> 32)), __uint_as_float((uint32_t)v1[k]), __uint_as_float((uint32_t)(v1[k] >> 32))});
+        const int in = i0 + g * per + unit % per;
+        if (slice == 0 && in < rows) write(in, sum[g]);
       }
-      if (slices > 1) {
-        __syncthreads();
-        xo[threadIdx.x] = sum.o;
-        if (c == 0) { xd[2 * unit] = sum.m; xd[2 * unit + 1] = sum.den; }
-        __syncthreads();
-        for (int k = 1; k < slices && slice == 0; k++) sum.add(xd[2 * (unit + k * per)], xd[2 * (unit + k * per) + 1], xo[threadIdx.x + k * per * TPR]);
-      }
-      if (slice == 0 && i0 + unit < rows) write(in, sum);
     }
   };
   auto output = [&](int in, const PagedSum& sum) {
@@ -196,10 +221,8 @@ __device__ __forceinline__ void paged_few_join(const PagedArgs& a, const PagedRu
     if (complete(a.flags, first, first + members) && members > 1) {
       const int64_t to = group(first / size);
       add_up(members, [&](int p) { return record(first + p); }, [&](int in, const PagedSum& sum) {
-        float* po = a.part_o + (to * 16 + in) * D + c * 4;
-        agent_store(po, sum.o[0], sum.o[1]);
-        agent_store(po + 2, sum.o[2], sum.o[3]);
-        if (c == 0) agent_store(a.part_ml + (to * 16 + in) * 2, sum.m, sum.den);
+        recs.store(recs.place(to, in, c * 4), sum.o);
+        if (c == 0) agent_store(a.part_ml + (to * ROWS + in) * 2, sum.m, sum.den);
       });
     }
     if (!complete(done, 0, pieces)) return;

@@ -309,6 +309,67 @@ def test_tiles_of_few_rows_are_cut_and_joined(d, g, h_kv, lens, news):
     Setup4(lens, news, h_kv=h_kv, g=g, d=d, page=64, behind=math.nan, seed=25).check()
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("g,h_kv,m", [(1, 16, 33), (2, 8, 12), (4, 8, 9), (16, 8, 3)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("width,page", [(64, 16), (70, 64)])
+def test_tiles_of_32_rows(d, g, h_kv, m, causal, width, page):
+    """Between 16 and 80 rows a sequence on the average, in batches: tiles with one, one and a half and two groups of 16 rows; sequences without new tokens or shorter than
+    them; lengths on both sides of 32, 64 and 128 keys, in caches that hold more and no more than a thousand."""
+    around = [16, 700, 31, 33, 47, 64, 65, 5, 96, 97, 127, 129, 200, 1000, 0, 385]
+    lens = [around[i % len(around)] for i in range(26)]
+    news = [[m, m + 1, 0, 2 * m, 1, m // 2][i % 6] for i in range(26)]
+    Setup4(lens, news, h_kv=h_kv, g=g, d=d, page=page, width=max(width * 16 // page, 1000 // page + 1), behind=math.nan, spare=2, seed=31).check(causal)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("g,long,m", [(4, [9000, 1, 2500], 8), (4, [20000, 129, 128], 16), (8, [6001, 4097, 33], 5), (1, [12000, 7], 30)])
+def test_tiles_of_32_rows_are_cut_and_joined(d, g, long, m):
+    """A few long sequences beside short ones: some tiles are cut into many pieces, added up in one level and in two, and runs go over several tiles.  A block of V that is NaN
+    late in the first sequence, and one of K in the second, are lost where they are seen and nowhere else."""
+    h_kv, page = 8, 64
+    lens = long + [200 + 17 * i for i in range(22)]
+    news = [m, m - 1, 1][:len(long)] + [[m, m + 2, 0, 3][i % 4] for i in range(22)]
+    news = [min(x, n) for x, n in zip(news, lens)]
+    s = Setup4(lens, news, h_kv=h_kv, g=g, d=d, page=page, seed=32)
+    clean, clean_lse = s.check()
+    slots = [lens[0] - m // 2 - 1, max(lens[1] - 1, 0)]
+    for b, tensor, head in ((0, 3, 1), (1, 1, 2)):
+        s.codes[tensor][int(s.table[b, slots[b] // page]), head, slots[b] % page, d // 32 - 1] = 255
+    s.place()
+    o, lse = s.attend()
+    lost = torch.zeros(o.shape, dtype=torch.bool)
+    start = s.row_start.tolist()
+    for b, head, span in ((0, 1, slice(d - 32, d)), (1, 2, slice(0, d))):
+        for t in range(news[b]):
+            lost[start[b] + t, head * g:(head + 1) * g, span] = lens[b] - news[b] + t >= slots[b]
+    assert torch.equal(torch.isnan(o), lost)
+    assert torch.equal(torch.isnan(lse[:start[1]]), torch.zeros_like(lse[:start[1]], dtype=torch.bool))
+    assert torch.equal(torch.isnan(lse[start[1]:]), lost[start[1]:].any(-1))
+    assert torch.equal(o[~lost], clean[~lost])
+
+
+def test_tiles_of_32_rows_in_a_graph():
+    """Replayed with other lengths, eager calls between: the flags of cut tiles are clear each time."""
+    lens, news = [5000, 300, 2000] + [100] * 17, [8] * 20
+    s = Setup4(lens, news, h_kv=8, g=4, page=64, seed=33)
+    p, q = s.params(), s.q.to(DEV)
+    ws = B.alloc_paged4_workspace(p, DEV)
+    ws.zero_()
+    o, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.dash_paged4_attend(p, s.gpu, q, s.start_gpu, o, ws, lse=lse)
+    for other in (lens, [4999, 7, 0] + [33] * 17, [100] * 20, lens):
+        s.gpu.lens.copy_(torch.tensor(other))
+        want = s.attend()
+        for _ in range(2):
+            o.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(o.cpu(), want[0]) and torch.equal(lse.cpu(), want[1])
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_peaked_and_falling_logits(dtype):
     s = Setup4([700, 300], [3, 200], dtype=dtype, page=32, seed=11, qscale=30.0)
