@@ -628,12 +628,17 @@ def dash_rotary(r: Rotary, q, q_out, k=None, k_out=None, pos=None, start: int = 
 
 
 def _apart(x, x_heads, y, y_heads, d, size) -> bool:
-    """Whether tensors in each other's span are heads of one tensor (queries and keys of a fused projection): the same strides, and starts within one token's
-    row that keep their heads apart."""
+    """Whether tensors in each other's span are heads of one tensor (queries and keys of a fused projection): the same strides, and starts that keep their
+    heads apart within one token's row, or all of their heads apart modulo a stride that the others are multiples of."""
     (s, x_ptr, _), (t, y_ptr, _) = x, y
+    if s != t:
+        return False
     first, off = (x_heads, y_ptr - x_ptr) if x_ptr <= y_ptr else (y_heads, x_ptr - y_ptr)
-    then = x_heads + y_heads - first
-    return s == t and (first - 1) * s[1] + d <= off // size and off // size + (then - 1) * s[1] + d <= s[2]
+    then, off = x_heads + y_heads - first, off // size
+    if (first - 1) * s[1] + d <= off and off + (then - 1) * s[1] + d <= s[2]:
+        return True
+    step = min(s[:3])
+    return step > 0 and d <= off % step <= step - d and not any(x % step for x in s[:3])
 
 
 def dash_paged_append_rotary(p: dash_paged_params, cache: PagedCache, rotary: Rotary, k_new, v_new, row_start, q=None, q_out=None) -> None:

@@ -2,6 +2,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <utility>
+
 #include "paged.h"
 #include "rotary.h"
 
@@ -52,6 +54,27 @@ static int paged_args(const dash_paged_params* p, PagedArgs* a, bool rows, bool 
 }
 
 static bool misaligned(const void* x) { return ((uintptr_t)x & 15) != 0; }
+// Packed rows of heads (the call's rows; d elements of es bytes): whether x and y may share an element.  Those of one tensor do not where their strides are the
+// same and their heads lie apart within a row, or modulo the smaller stride where the other one is a multiple of it.
+struct Heads { const void* at; int64_t t, h; int heads; };
+static bool may_meet(Heads x, Heads y, const PagedArgs& a, int d, int es) {
+  if ((uintptr_t)x.at > (uintptr_t)y.at) std::swap(x, y);
+  const auto row = [&](const Heads& z) { return (z.heads - 1) * z.h + d; };
+  const int64_t off = (int64_t)(((uintptr_t)y.at - (uintptr_t)x.at) / es);     // both are aligned
+  if (a.n_rows == 0 || off >= (a.n_rows - 1) * x.t + row(x)) return false;
+  if (x.t != y.t) return true;
+  if (row(x) <= off && off + row(y) <= x.t) return false;
+  const int64_t step = x.t < x.h ? x.t : x.h, more = x.t < x.h ? x.h : x.t;
+  return !(x.h == y.h && step > 0 && more % step == 0 && off % step >= d && off % step <= step - d);
+}
+// The turned queries of a call that appends: q itself, or apart from q, and apart from the new keys and values.
+static bool queries_meet(const dash_paged_params* p, const PagedArgs& a) {
+  if (!a.q) return false;
+  const int es = p->dtype == DASH_BF16 ? 2 : 4, d = p->head_dim;
+  const Heads out = {a.o, a.o_t, a.o_h, p->h_q};
+  return (a.q == a.o ? a.q_t != a.o_t || a.q_h != a.o_h : may_meet({a.q, a.q_t, a.q_h, p->h_q}, out, a, d, es)) ||
+         may_meet({a.k_new, a.kn_t, a.kn_h, p->h_kv}, out, a, d, es) || may_meet({a.v_new, a.vn_t, a.vn_h, p->h_kv}, out, a, d, es);
+}
 static int check_scratch(size_t need, const void* ws, size_t bytes) {
   return (!ws || ((uintptr_t)ws & 255) != 0 || bytes < need) ? DASH_EWORKSPACE : DASH_OK;
 }
@@ -141,8 +164,8 @@ int dash_paged_append_rotary(const dash_paged_params* p, const dash_rotary* r, c
   if (const int rc = rotary_args(r, p->head_dim, &turn); rc != DASH_OK) return rc;
   if (!q != !q_out || !k_new || !v_new || !k_pages || !v_pages || !row_start || !lens || !table) return DASH_EINVAL;
   if (misaligned(q) || misaligned(q_out) || misaligned(k_new) || misaligned(v_new) || misaligned(k_pages) || misaligned(v_pages)) return DASH_EINVAL;
-  if (q && q == q_out && (a.q_t != a.o_t || a.q_h != a.o_h)) return DASH_EINVAL;
   a.q = q; a.o = q_out; a.k_new = k_new; a.v_new = v_new; a.k = k_pages; a.v = v_pages;
+  if (queries_meet(p, a)) return DASH_EINVAL;
   a.row_start = row_start; a.lens = lens; a.table = table; a.weights = weights; a.pos = pos; a.seen = seen;
   return launch_paged_append_rotary(a, turn, p->dtype == DASH_BF16 ? 2 : 4, p->head_dim, (hipStream_t)stream) == hipSuccess ? DASH_OK : DASH_ELAUNCH;
 }
@@ -166,8 +189,8 @@ int dash_paged4_append(const dash_paged_params* p, const dash_rotary* r, const v
   if (!q != !q_out || (q && !r) || !k_new || !v_new || !k_codes || !k_scales || !v_codes || !v_scales || !row_start || !lens || !table) return DASH_EINVAL;
   if (misaligned(q) || misaligned(q_out) || misaligned(k_new) || misaligned(v_new) || misaligned(k_codes) || misaligned(v_codes) ||
       misaligned(k_scales) || misaligned(v_scales)) return DASH_EINVAL;
-  if (q && q == q_out && (a.q_t != a.o_t || a.q_h != a.o_h)) return DASH_EINVAL;
   a.q = q; a.o = q_out; a.k_new = k_new; a.v_new = v_new; a.k = k_codes; a.v = v_codes; a.k_sc = (const uint8_t*)k_scales; a.v_sc = (const uint8_t*)v_scales;
+  if (queries_meet(p, a)) return DASH_EINVAL;
   a.row_start = row_start; a.lens = lens; a.table = table; a.seen = seen;
   return launch_paged4_append(a, r ? &turn : nullptr, p->dtype == DASH_BF16 ? 2 : 4, p->head_dim, (hipStream_t)stream) == hipSuccess ? DASH_OK : DASH_ELAUNCH;
 }

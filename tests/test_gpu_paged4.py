@@ -133,6 +133,42 @@ def test_append_and_unpack_of_codes_in_another_layout(dtype, d):
     assert torch.equal(fused.cpu()[:, 2 * h_kv:], before[:, 2 * h_kv:])
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_queries_keys_and_values_of_each_head_side_by_side(dtype):
+    """Slices [n, h, (q, k, v), d] of one projection, q turned in place, by an append into pages of either kind and by the call that turns alone."""
+    h, d, n, page = 4, 128, 150, 16
+    each = draws(34)(n, h, 3, d).to(dtype)
+    at, theta = torch.arange(n)[:, None], R.thetas(d)
+    turned = R.turn(each[:, :, 1], at, theta, "halves")[0]
+    r = B.make_rotary(d, DEV)
+    start = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    for four in (True, False):
+        g = each.to(DEV)
+        q, k, v = g.unbind(2)
+        c = B.PagedCache4.allocate(1, h, 10, page, d, 10, DEV) if four else B.PagedCache.allocate(1, h, 10, page, d, 10, DEV, dtype=dtype)
+        c.table.copy_(torch.arange(10)[None])
+        c.lens.fill_(n)
+        if four:
+            p = B.make_paged4_params(c, n, h, dtype=dtype)
+            B.dash_paged4_append(p, c, k, v, start, rotary=r, q=q, q_out=q)
+            kp, vp = (torch.zeros((10, h, page, d), dtype=dtype, device=DEV) for _ in range(2))
+            B.dash_paged4_unpack(p, c, kp, vp)
+            got = kp.cpu().double().transpose(0, 1).reshape(h, -1, d)[:, :n].transpose(0, 1)
+            assert torch.equal(got, held(turned))
+        else:
+            p = B.make_paged_params(c, n, h)
+            B.dash_paged_append_rotary(p, c, r, k, v, start, q=q, q_out=q)
+            check(c.k.cpu().transpose(0, 1).reshape(h, -1, d)[:, :n].transpose(0, 1), each[:, :, 1], at, theta, "halves")
+        check(q.cpu(), each[:, :, 0], at, theta, "halves")
+        assert torch.equal(g.cpu()[:, :, 1:], each[:, :, 1:])
+    g = each.to(DEV)[None]
+    q, k, _ = (x.transpose(1, 2) for x in g.unbind(3))
+    B.dash_rotary(r, q, q, k, k)
+    for i in (0, 1):
+        check(g[0, :, :, i].cpu(), each[:, :, i], at, theta, "halves")
+    assert torch.equal(g.cpu()[0, :, :, 2], each[:, :, 2])
+
+
 # ---- attention -------------------------------------------------------------------------------------------------------
 class Setup4:
     """A cache in 4 bits on the GPU and its values on the CPU.  behind: what the pages hold behind the sequences' ends (NaN: blocks that are NaN)."""

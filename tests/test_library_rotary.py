@@ -182,6 +182,31 @@ def test_parameters_of_the_packed_rows():
     assert call4("append", params4(), None, q=256, q_out=512) == -1                              # queries without a plan
 
 
+@pytest.mark.parametrize("name", ["rotary", "append"])
+def test_queries_are_not_written_over_what_is_read(name):
+    """16 rows of two heads of 128 in bf16 with strides of 256 and 128 elements: 8192 bytes.  Fused rows: 6 heads, q the first two."""
+    p = params(n_rows=16, h_q=2, h_kv=2) if name == "rotary" else params4(n_rows=16, h_q=2, h_kv=2)
+    far = 1 << 20
+    assert (p.q_stride[0], p.q_stride[1], p.k_new_stride[0]) == (256, 128, 256)
+    for kw in (dict(q=far, q_out=far + 16), dict(q=far + 8176, q_out=far), dict(q=far, q_out=4 * far, k_new=4 * far), dict(q=far, q_out=4 * far, v_new=4 * far + 8176),
+               dict(q=far, q_out=far, k_new=far + 256), dict(q=far, q_out=4 * far + 256, v_new=4 * far)):
+        a = dict(k_new=2 * far, v_new=3 * far)
+        a.update(kw)
+        assert call4(name, p, plan(), **a) == -1, kw
+    for x in (p.q_stride, p.o_stride, p.k_new_stride, p.v_new_stride):
+        x[0] = 768
+    for kw in (dict(k_new=far + 384), dict(v_new=far + 256), dict(q_out=far + 128), dict(k_new=far + 1536 - 256), dict(k_new=far + 1536 + 256)):
+        a = dict(q=far, q_out=far, k_new=far + 512, v_new=far + 1024)
+        a.update(kw)
+        assert call4(name, p, plan(), **a) == -1, kw
+    for x in (p.q_stride, p.o_stride, p.k_new_stride, p.v_new_stride):                           # rows of heads of (q, k, v)
+        x[1] = 384
+    for kw in (dict(k_new=far + 128), dict(v_new=far + 640), dict(k_new=far + 768 + 16)):
+        a = dict(q=far, q_out=far, k_new=far + 256, v_new=far + 512)
+        a.update(kw)
+        assert call4(name, p, plan(), **a) == -1, kw
+
+
 @pytest.mark.parametrize("name,needed", [
     ("rotary", ("k_new", "v_new", "k", "v", "row_start", "lens", "table")), ("append", ("k_new", "v_new", "k", "v", "ks", "vs", "row_start", "lens", "table")),
     ("attend", ("q", "k", "v", "ks", "vs", "row_start", "lens", "table", "o")), ("unpack", ("k", "v", "ks", "vs", "k_out", "v_out"))])
@@ -237,6 +262,12 @@ def test_rotary_binding_refuses_tensors_that_do_not_fit():
         assert "GPU" not in str(e.value), kw
     ok = [dict(), dict(q=None, q_out=None), dict(k=None, k_out=None), dict(q_out=q, k_out=k), dict(pos=None), dict(pos=torch.zeros(10, dtype=torch.int32)),
           dict(q=fused[:, :, :4].transpose(1, 2), q_out=fused[:, :, :4].transpose(1, 2), k=fused[:, :, 4:].transpose(1, 2), k_out=fused[:, :, 4:].transpose(1, 2))]
+    each = torch.zeros((2, 10, 4, 3, 64))                        # (q, k, v) of each head side by side
+    qe, ke = each[..., 0, :].transpose(1, 2), each[..., 1, :].transpose(1, 2)
+    ok.append(dict(q=qe, q_out=qe, k=ke, k_out=ke))
+    half = each.view(2, 10, 4, 192)[..., 32:96].transpose(1, 2)
+    with pytest.raises(B.DashError, match="overlap"):
+        run(q=qe, q_out=qe, k=half, k_out=half)
     for kw in ok:
         with pytest.raises(B.DashError, match="GPU"):            # nothing wrong but where the tensors lie
             run(**kw)
