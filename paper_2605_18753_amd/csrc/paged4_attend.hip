@@ -597,11 +597,14 @@ static int runs_of(const PagedArgs& a, int dtype, int d) { return max((dtype == 
 // 62.5; 80: 74.7, 65.6, 64.8.  24 of 20: 86.9, 66.4, 169; 48: 121, 111, 192; 64: 154, 114, 193.  16 of 80: 133, 114, 128.  64 of 2000 tokens, 48 rows: 72.0, 64.3, 79.9; 80: 117,
 // 93.1, 83.1.  Heads in a group of 16, two kv-heads, 8 sequences: 32 rows 23.1, 29.5, 25.6, 64 27.1, 31.6, 29.4, 96 32.4, 36.6, 31.6; 32 sequences, 64 rows: 61.2, 47.7, 58.9.  Head
 // dimension 64, 8 sequences: 48 rows 36.0, 37.9, 40.5, 64 44.2, 37.4, 40.8; 32 sequences, 64 rows: 131, 94.3, 132.)
+// Short caches: 16 while there are few tiles, each of which has a CU then.  (Caches of 1000 tokens.  12 of 20 rows, 192 tiles of 16, 11.5 and 15.4 us; 12 of 64, 384 of them, 15.3
+// and 14.9; 40 of 32, 640, 22.8 and 20.5.)
 static int tile_rows(const PagedArgs& a, int dtype, int d) {
   const int64_t rows = (int64_t)a.n_rows * a.g;
+  const int64_t few = a.cap <= 8 * kStep ? paged_most_items(a, 16) * a.h_kv : INT64_MAX;   // tiles of 16 rows of a short cache
   if (dtype != DASH_BF16) return 16;
-  if (rows > (int64_t)a.batch * 80 && !(a.cap <= 8 * kStep && paged_most_items(a, 16) * a.h_kv <= 256)) return 128;
-  return rows > (int64_t)a.batch * 16 && paged_most_items(a, 32) * 4 >= runs_of(a, dtype, d) ? 32 : 16;
+  if (rows > (int64_t)a.batch * 80 && few > 256) return 128;
+  return rows > (int64_t)a.batch * 16 && few > 384 && paged_most_items(a, 32) * 4 >= runs_of(a, dtype, d) ? 32 : 16;
 }
 static size_t ws_align(size_t x) { return (x + 255) & ~(size_t)255; }
 
