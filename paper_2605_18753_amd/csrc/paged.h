@@ -36,6 +36,7 @@ struct PagedArgs {
   int wgs;                               // runs of a kv-head; 0: an item a workgroup.  Tiles of 128 rows: parts of a kv-head at most; 0: none is cut
   int whole;                             // runs: items may be left uncut; weights: two kernels share the sequences
   int pad;                               // runs: steps that an item's start counts for
+  int few;                               // > 0: the launch has the sequences of up to so many rows; < 0: those of more than -few; 0: all
   int slots; float gain;                 // tiles of 128 rows: workgroups of a kv-head that are resident at once; what finer parts must come to
   float* part_o; float* part_ml;         // records of cut items: two of each run (the item it begins in, the one it ends in), one of each part
   const uint8_t* k_sc; const uint8_t* v_sc;   // a cache in 4 bits: its scales (k and v its codes, their strides in bytes)
@@ -54,6 +55,7 @@ __device__ __forceinline__ PagedLane paged_lane(const PagedArgs& a, int b) {
   PagedLane l = {make_int2(0, 0), 0};
   if (b < a.batch) {
     l.rm = paged_rows(a, b);
+    if (a.few > 0 ? l.rm.y > a.few : l.rm.y <= -a.few) l.rm.y = 0;
     l.n = paged_len(a, b);
   }
   return l;

@@ -406,6 +406,48 @@ def test_tiles_of_32_rows_in_a_graph():
             assert torch.equal(o.cpu(), want[0]) and torch.equal(lse.cpu(), want[1])
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("g,h_kv", [(1, 2), (4, 8), (16, 1)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("batch,page", [(5, 16), (70, 64)])
+def test_few_rows_beside_many(d, g, h_kv, causal, batch, page):
+    """Sequences of up to 48 rows and of more have launches of their own: some of 48 and of one token more, prompts, none, and shorter ones than their new rows."""
+    most = 48 // g
+    kinds = [(700, most), (900, most + 1), (2100, 1100 // g + 900), (33, 1), (5, 9), (0, 2), (640, 0), (1500, most - 1), (20, 20), (257, 2 * most + 3)]
+    seqs = [kinds[i % len(kinds)] for i in range(batch)]
+    if batch > 10:
+        seqs = [(n, min(m, 60)) for n, m in seqs[:-1]] + [(3000, 90 * batch // g)]
+    s = Setup4([n for n, _ in seqs], [m for _, m in seqs], h_kv=h_kv, g=g, d=d, page=page, behind=math.nan, spare=1, seed=35, width=3200 // page)
+    assert s.rows * g > 80 * batch
+    s.check(causal)
+
+
+def test_sequences_that_change_sides_in_a_graph():
+    """Captured once; row starts and lengths are those of each replay."""
+    s = Setup4([3000, 2000, 1000, 400], [200, 12, 13, 1], h_kv=8, g=4, page=64, seed=36)
+    p, q = s.params(), s.q.to(DEV)
+    ws = B.alloc_paged4_workspace(p, DEV)
+    ws.zero_()
+    o, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.dash_paged4_attend(p, s.gpu, q, s.start_gpu, o, ws, lse=lse)
+    for start, lens in (([0, 200, 212, 225, 226], [3000, 2000, 1000, 400]), ([0, 5, 218, 219, 226], [3000, 1999, 1000, 390]), ([0, 12, 24, 36, 48], [2999, 2000, 30, 400]),
+                        ([0, 56, 112, 168, 226], [3000, 2000, 1000, 57]), ([0, 226, 226, 226, 226], [3000, 1, 2, 3]), ([0, 200, 212, 225, 226], [3000, 2000, 1000, 400])):
+        s.start_gpu.copy_(torch.tensor(start))
+        s.gpu.lens.copy_(torch.tensor(lens))
+        s.row_start, s.lens = torch.tensor(start, dtype=torch.int32), torch.tensor(lens, dtype=torch.int32)
+        s.ref = P.Cache(s.ref.k, s.ref.v, s.table, s.lens)
+        s.check()
+        want = s.attend()
+        for _ in range(2):
+            o.fill_(77)
+            lse.fill_(77)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(o.cpu(), want[0]) and torch.equal(lse.cpu(), want[1])
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_peaked_and_falling_logits(dtype):
     s = Setup4([700, 300], [3, 200], dtype=dtype, page=32, seed=11, qscale=30.0)
