@@ -37,6 +37,7 @@ struct PagedArgs {
   int whole;                             // runs: items may be left uncut; weights: two kernels share the sequences
   int pad;                               // runs: steps that an item's start counts for
   int few;                               // > 0: the launch has the sequences of up to so many rows; < 0: those of more than -few; 0: all
+  int tight;                             // tiles of 128 rows: items of one length are cut into as many parts each as there are places for, or twice that
   int slots; float gain;                 // tiles of 128 rows: workgroups of a kv-head that are resident at once; what finer parts must come to
   float* part_o; float* part_ml;         // records of cut items: two of each run (the item it begins in, the one it ends in), one of each part
   const uint8_t* k_sc; const uint8_t* v_sc;   // a cache in 4 bits: its scales (k and v its codes, their strides in bytes)
@@ -131,13 +132,23 @@ template <typename F> __device__ __forceinline__ PagedCut paged_part_size(const 
   const float even = cost / (float)a.slots;
   PagedCut cut = {items < a.slots ? size(cost, a.slots) : kUncut, 0};
   float time = items <= a.slots ? fminf((float)cut.size, most) : fminf((float)((items + a.slots - 1) / a.slots) * most, even + 0.5f * most);
-  if (a.wgs > a.slots) {
+  // Items of one length (one sequence's): as many parts each as there are places for, once or twice.  (The sum over w - n leaves places unused: 512 tokens against 32k in 4 bits, 16
+  // items for 64 places, in three parts each 351 us, in four 291; 700, 22 items, in two 517, in five 438.)
+  bool finer = false;
+  if (a.tight && items <= a.slots && most * (float)items <= cost) {
+    const auto parts = [&](int k) { return max((int)ceilf(most / (float)max(k, 1)), kMinPart); };
+    const int once = parts(a.slots / max(items, 1)), twice = parts(min(2 * a.slots, a.wgs) / max(items, 1));
+    finer = 2 * twice + 6 < once;
+    cut = {finer ? twice : once, 0};
+    time = (float)once;
+  } else if (a.wgs > a.slots) {
     const int fine = size(cost, a.wgs);
-    if (even + 0.5f * (float)fine + 4.f < a.gain * time) cut = {fine, 0};
-    else if (items > half && most * (float)items < 1.2f * cost) {   // of like lengths: one item a CU stays whole, the others fill up what these leave
-      const int fill = max(size(rest, a.wgs), (int)(0.5f * even));
-      if (even + 0.25f * (float)fill + 10.f < (a.gain + 0.05f) * time) cut = {fill, half};
-    }
+    finer = even + 0.5f * (float)fine + 4.f < a.gain * time;
+    if (finer) cut = {fine, 0};
+  }
+  if (a.wgs > a.slots && !finer && items > half && most * (float)items < 1.2f * cost) {   // of like lengths: one item a CU stays whole, the others fill up what these leave
+    const int fill = max(size(rest, a.wgs), (int)(0.5f * even));
+    if (even + 0.25f * (float)fill + 10.f < (a.gain + 0.05f) * time) cut = {fill, half};
   }
   if ((float)cut.size >= most) cut = {kUncut, 0};
   return cut;

@@ -630,6 +630,7 @@ static hipError_t launch_tiles4(PagedArgs a, int dtype, int tile, int64_t items,
   a.wgs = items < (big ? 2 : 8) * (int64_t)runs ? runs : 0;
   if (big && a.wgs && items * 4 >= runs) a.wgs = (int)items + runs * 3 / 2;
   a.slots = runs;
+  a.tight = 1;
   a.gain = (int64_t)a.n_rows * a.g < 64 * items ? 0.65f : 0.9f;
   // An item's start (and the end of the piece before it) takes as long as so many steps.  (0, 3, 4, 5, 8 of them: one token of 32 sequences of 4096 to 32768 128.2, 125.7, 124.4,
   // 126.6 and 127.9 us, of 8 of 384 to 16000 26.3, 24.0, 23.4, 23.5 and 24.7; of like lengths, where all runs begin with an item, 20.4, 20.8, 21.5, 21.5 and 21.5.)
