@@ -100,17 +100,18 @@ __device__ __forceinline__ bool paged_place(const PagedArgs& a, int row, PagedPl
 }
 
 // ---- parts (tiles of 128 rows) ----------------------------------------------------------------------------------------
+constexpr int kCUs = 256;
 constexpr int kMinPart = 4;                                // steps a part has at least
 // The size S of a part, no item costing more: none is cut; a wave's lanes together.  shape(m, n) gives a sequence's tiles and the cost
 // of one (at least 1); l0: the first 64 sequences.
 constexpr int kUncut = 0x3fffffff;
-struct PagedCut { int size, whole; };                      // of the items behind the first `whole`
+struct PagedCut { int size, whole, items; };               // of the items behind the first `whole`
 // of sequence tiles, those among the first `whole` items; before: items before the sequence's
 __device__ __forceinline__ int paged_whole(const PagedCut& cut, int before, int tiles) { return min(max(cut.whole - before, 0), tiles); }
 // The launch that adds the parts up has to come to the same: no products are fused with sums here.
 template <typename F> __device__ __forceinline__ PagedCut paged_part_size(const PagedArgs& a, const PagedLane& l0, F&& shape) {
 #pragma clang fp contract(off)
-  if (a.wgs <= 0) return {kUncut, 0};
+  if (a.wgs <= 0) return {kUncut, 0, 0};
   const int lane = lane_id(), half = a.slots / 2;
   int items = 0;
   float cost = 0.f, most = 0.f, rest = 0.f;                // rest: of the items behind the first `half`
@@ -123,14 +124,14 @@ template <typename F> __device__ __forceinline__ PagedCut paged_part_size(const 
     cost += wave_sum((float)s.x * (float)s.y);
     most = fmaxf(most, wave_max(s.x > 0 ? (float)s.y : 0.f));
   }
-  if (items >= a.wgs) return {kUncut, 0};
+  if (items >= a.wgs) return {kUncut, 0, items};
   const auto size = [&](float c, int w) { return max((int)fminf(c * 1.0001f / (float)(w - items), 1e9f) + 1, kMinPart); };   // the factor covers the sum's rounding
   // The time, in steps, of parts that are all resident (or of items, where more are not), and of finer ones that follow each other: what everybody
   // has on the average, half a part until the last is done (a quarter beside whole items, which run faster alone), and what a part costs besides: 4
   // steps, or 10 where it is one more than a workgroup would have.  (One item a CU whole, the others filling up: 2200 tokens against 32k, 32 / 8
   // heads, 69 items for 64 places, 1418 -> 1197 us; 1500, 47 items, 865 -> 785; against 2000, where it is not done, 54 and 64.)
   const float even = cost / (float)a.slots;
-  PagedCut cut = {items < a.slots ? size(cost, a.slots) : kUncut, 0};
+  PagedCut cut = {items < a.slots ? size(cost, a.slots) : kUncut, 0, items};
   float time = items <= a.slots ? fminf((float)cut.size, most) : fminf((float)((items + a.slots - 1) / a.slots) * most, even + 0.5f * most);
   // Items of one length (one sequence's): as many parts each as there are places for, once or twice.  (The sum over w - n leaves places unused: 512 tokens against 32k in 4 bits, 16
   // items for 64 places, in three parts each 351 us, in four 291; 700, 22 items, in two 517, in five 438.)
@@ -139,18 +140,18 @@ template <typename F> __device__ __forceinline__ PagedCut paged_part_size(const 
     const auto parts = [&](int k) { return max((int)ceilf(most / (float)max(k, 1)), kMinPart); };
     const int once = parts(a.slots / max(items, 1)), twice = parts(min(2 * a.slots, a.wgs) / max(items, 1));
     finer = 2 * twice + 6 < once;
-    cut = {finer ? twice : once, 0};
+    cut.size = finer ? twice : once;
     time = (float)once;
   } else if (a.wgs > a.slots) {
     const int fine = size(cost, a.wgs);
     finer = even + 0.5f * (float)fine + 4.f < a.gain * time;
-    if (finer) cut = {fine, 0};
+    if (finer) cut.size = fine;
   }
   if (a.wgs > a.slots && !finer && items > half && most * (float)items < 1.2f * cost) {   // of like lengths: one item a CU stays whole, the others fill up what these leave
     const int fill = max(size(rest, a.wgs), (int)(0.5f * even));
-    if (even + 0.25f * (float)fill + 10.f < (a.gain + 0.05f) * time) cut = {fill, half};
+    if (even + 0.25f * (float)fill + 10.f < (a.gain + 0.05f) * time) cut = {fill, half, items};
   }
-  if ((float)cut.size >= most) cut = {kUncut, 0};
+  if ((float)cut.size >= most) cut = {kUncut, 0, items};
   return cut;
 }
 
@@ -160,6 +161,9 @@ template <typename F> __device__ __forceinline__ bool paged_find_part(const Page
   const int lane = lane_id();
   const PagedLane l0 = paged_lane(a, lane);
   const PagedCut cut = paged_part_size(a, l0, shape);
+  // None is cut, and all are resident: whoever comes second to a CU takes the tiles from the other end, so that a prompt's long ones stand beside its short ones.
+  // (In 4 bits, two prompts of 1000 tokens 51 and 44 us, 2000 tokens against 6000 188 and 181; 2000 of 2000 64 both ways.)
+  if (const int one = kCUs / a.h_kv; cut.size == kUncut && idx >= one && idx < cut.items && cut.items <= a.slots) idx = cut.items - 1 - (idx - one);
   const bool whole = idx < cut.whole;
   int items = 0, base = whole ? 0 : cut.whole;
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
