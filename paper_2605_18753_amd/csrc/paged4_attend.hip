@@ -175,7 +175,9 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void paged_few4_kernel(Paged
     for (int dt = 0; dt < D / 16; dt++) oacc[i][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // Two sets of registers in turn: the next tile's loads are asked for before the present ones are waited for.
+  // Two sets of registers in turn: the next tile's loads are asked for before the present ones are waited for.  A wave's priority rises through a tile: whoever is further on
+  // is served first, and the waves of a SIMD fall out of step, one's products beside another's conversions (24 sequences of 3000 to 16000 with 64 rows 109 -> 104 us, at
+  // head dimension 64 32 of them 94.8 -> 85.4, 80 rows of eight 31.0 -> 28.7).
   typename Walk4<D>::Raw even, odd;
   int2 entries = make_int2(0, 0);
   if (j < j1) {
@@ -188,6 +190,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void paged_few4_kernel(Paged
     const uint32_t vs[2] = {walk.v_scale(x, 0), walk.v_scale(x, 1)};
     walk.put_v(x, vs, 0);
     f32x4 s0[G], s1[G];                                                          // lane (row n, kq): keys 4 kq + i, 16 + 4 kq + i
+    __builtin_amdgcn_s_setprio(1);
     const float k0 = fp4_scale(walk.k_scale(x, 0)), k1 = fp4_scale(walk.k_scale(x, 1));
 #pragma unroll
     for (int i = 0; i < G; i++) s0[i] = s1[i] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -237,6 +240,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void paged_few4_kernel(Paged
       pb[g] = __builtin_bit_cast(bf16x8, pw);
     }
     asm volatile("" ::: "memory");                                               // a wave's LDS operations complete in order
+    __builtin_amdgcn_s_setprio(2);
     bf16x8 vf[D / 16];
 #pragma unroll
     for (int dt = 0; dt < D / 16; dt++) {
@@ -251,6 +255,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void paged_few4_kernel(Paged
     asm volatile("" ::: "memory");
 #pragma unroll
     for (int g = 0; g < G; g++) walk.spoil(vs, j, last[g], oacc[g]);
+    __builtin_amdgcn_s_setprio(0);
   };
   while (j < j1) {
     tile(even, odd);
@@ -388,6 +393,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_rows4_kernel(Paged
   // Iteration i, LDS: tile i lives in slot i & 1 of both rings, V one iteration behind K.  The barrier at its top makes everybody's tiles visible (K of
   // tile i, V of tile i - 1) and retires the reads of iteration i - 1, whose slots this iteration writes over with what it converts: K of tile
   // i + 1 and V of tile i, a word of codes at a time between the MFMAs.  Their registers then take K of tile i + 2 and V of tile i + 1.
+  // A wave's priority rises from the first product to the second: the waves of a SIMD, of several workgroups, fall out of step (2048 tokens against 32k 1060 -> 1000 us, at
+  // head dimension 64 655 -> 624; raised in the second alone 1002 and 646).
   int pend = 0;
   float tmax_old = 0.f;
   auto iteration = [&](auto p_tag, int i, f32x16 (&s)[2], f32x16 (&so)[2]) __attribute__((always_inline)) {
@@ -514,6 +521,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_rows4_kernel(Paged
       }
     };
     if (on) {
+      __builtin_amdgcn_s_setprio(1);
       if (pend) first_product(std::true_type{});
       else first_product(std::false_type{});
       mask_keys();
@@ -528,7 +536,9 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_rows4_kernel(Paged
     }
     if (pend) {
       __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_setprio(2);
       second_product();
+      __builtin_amdgcn_s_setprio(0);
     } else if (cur) {
 #pragma unroll
       for (int c = 0; c < C::CW; c++) { conv_k(c, P ^ 1); conv_v(c, P); }
