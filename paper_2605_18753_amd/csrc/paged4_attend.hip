@@ -288,8 +288,8 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void paged_few4_kernel(Paged
 // Many rows: a tile is 128 (token, head) rows, as in paged_rows_kernel, whose walk this is: the two products, the exponentials and the maxima
 // between their MFMAs, the order of operands.  64-key tiles of K and V are converted on their way into LDS, each by the whole workgroup once: 32 conversions a thread
 // and tile, beside some 250 vector instructions and 32 MFMAs of each wave.  Bound by the matrix units (0.44 of the clocks), the vector units (0.54) and LDS (K and V, 32 KB, go to each of
-// a CU's eight waves, 2050 clocks at 128 bytes a clock, and are written at 75, 850, of a step's 4400) by turns.  2048 tokens at the end of 32768, 32 / 8 heads of 128,
-// 1062 us (1.04 PFLOP/s; pages of bf16 967 to 1080 by card).  Head dimension 64: three workgroups a CU (all exponentials between the first product's MFMAs, which
+// a CU's eight waves, 2050 clocks at 128 bytes a clock, and are written at 75, 850, of a step's 4200) by turns.  2048 tokens at the end of 32768, 32 / 8 heads of 128,
+// 1000 us (1.1 PFLOP/s; pages of bf16 967 to 1080 by card).  Head dimension 64: three workgroups a CU (all exponentials between the first product's MFMAs, which
 // spares the registers that a third one needs): the same 656 us, two 741; 1501 tokens beside seven decoding sequences, in one launch, 215 and 238.
 template <int D> struct Rows4Cfg {
   static constexpr int CW = D / 32, ROW_BYTES = D * 2;
@@ -604,12 +604,12 @@ bool paged4_attend_fits(const PagedArgs& a, int dtype) { return dtype != DASH_F3
 static int runs_of(const PagedArgs& a, int dtype, int d) { return max((dtype == DASH_F32 ? 256 : d == 128 ? 512 : 768) / a.h_kv, 1); }
 // Rows of a call's tiles.  128 where the sequences bring more than 80 each on the average, but for short caches, as for pages of bf16; else 32 where they bring
 // more than 16 and there are tiles for every fourth run, so that few are cut into many pieces, whose records grow with a tile's rows; else 16.
-// (Tiles of 16, of 32 and of 128.  32 / 8 heads of 128, sequences of 3000 to 16000.  One of 20 rows: 18.4, 25.5, 22.3 us.  8 of 32 rows: 37.4, 38.8, 54.4; 64 rows: 62.0, 49.9,
-// 62.5; 80: 74.7, 65.6, 64.8.  24 of 20: 86.9, 66.4, 169; 48: 121, 111, 192; 64: 154, 114, 193.  16 of 80: 133, 114, 128.  64 of 2000 tokens, 48 rows: 72.0, 64.3, 79.9; 80: 117,
-// 93.1, 83.1.  Heads in a group of 16, two kv-heads, 8 sequences: 32 rows 23.1, 29.5, 25.6, 64 27.1, 31.6, 29.4, 96 32.4, 36.6, 31.6; 32 sequences, 64 rows: 61.2, 47.7, 58.9.  Head
-// dimension 64, 8 sequences: 48 rows 36.0, 37.9, 40.5, 64 44.2, 37.4, 40.8; 32 sequences, 64 rows: 131, 94.3, 132.)
-// Short caches: 16 while there are few tiles, each of which has a CU then.  (Caches of 1000 tokens.  12 of 20 rows, 192 tiles of 16, 11.5 and 15.4 us; 12 of 64, 384 of them, 15.3
-// and 14.9; 40 of 32, 640, 22.8 and 20.5.)
+// (Tiles of 16, of 32 and of 128.  32 / 8 heads of 128, sequences of 3000 to 16000.  One of 20 rows: 19.4, 25.2, 22.8 us.  8 of 32 rows: 35.7, 37.1, 55.2; 64 rows: 56.6, 47.0,
+// 59.0; 80: 68.4, 62.9, 62.6.  24 of 20: 84.8, 65.5, 173; 48: 118, 112, 182; 64: 150, 110, 183.  16 of 80: 127, 109, 121.  64 of 2000 tokens, 48 rows: 72.8, 62.4, 78.3; 80: 113,
+// 89.4, 83.0.  Heads in a group of 16, two kv-heads, 8 sequences: 32 rows 22.7, 29.1, 25.9, 64 26.0, 31.7, 29.2, 96 30.6, 35.2, 31.3.  Head
+// dimension 64, 8 sequences: 48 rows 34.2, 34.6, 39.8, 64 41.2, 34.6, 40.2; 32 sequences, 64 rows: 120, 88.7, 128.)
+// Short caches: 16 while there are few tiles, each of which has a CU then.  (Caches of 1000 tokens.  12 of 20 rows, 192 tiles of 16, 12.3 and 16.3 us; 40 of 32, 640 of them, 24.5
+// and 19.8.)
 static int tile_rows(const PagedArgs& a, int dtype, int d) {
   const int64_t rows = (int64_t)a.n_rows * a.g;
   const int64_t few = a.cap <= 8 * kStep ? paged_most_items(a, 16) * a.h_kv : INT64_MAX;   // tiles of 16 rows of a short cache
@@ -643,8 +643,8 @@ static hipError_t launch_tiles4(PagedArgs a, int dtype, int tile, int64_t items,
   a.slots = runs;
   a.tight = 1;
   a.gain = (int64_t)a.n_rows * a.g < 64 * items ? 0.65f : 0.9f;
-  // An item's start (and the end of the piece before it) takes as long as so many steps.  (0, 3, 4, 5, 8 of them: one token of 32 sequences of 4096 to 32768 128.2, 125.7, 124.4,
-  // 126.6 and 127.9 us, of 8 of 384 to 16000 26.3, 24.0, 23.4, 23.5 and 24.7; of like lengths, where all runs begin with an item, 20.4, 20.8, 21.5, 21.5 and 21.5.)
+  // An item's start (and the end of the piece before it) takes as long as so many steps.  (0, 3, 4, 8 of them: one token of 8 sequences of 384 to 16000 25.7, 23.1, 22.3 and
+  // 23.0 us, of 32 of 4096 to 32768 129.0, 127.6, 127.2 and 126.1; of 8 of one length, where all runs begin with an item, 20.3, 20.9, 21.2 and 21.2.)
   a.pad = 4;
   a.whole = items * 2 >= runs;                               // fewer items: not looked into
   if (!big && a.cap <= 8 * kStep && items * a.h_kv >= 128) a.wgs = 0;
@@ -673,9 +673,9 @@ static hipError_t launch_tiles4(PagedArgs a, int dtype, int tile, int64_t items,
 }
 
 // Tiles of 128 rows: in a batch, the sequences of up to 48 rows, of which such a tile would be mostly empty, have a launch of their own, of tiles of 16, in front of it.
-// (32 / 8 heads of 128, a piece of a prompt beside 31 sequences of 900 to 11777 with a token each: 1000 tokens 374 us in one launch, 272 in two, 1501 591 and 371;
-// beside seven: 300 114 and 102, 600 182 and 160, 1501 317 and 332, where the sequences of one token filled what the prompt's tiles leave, at head dimension 64 214 and
-// 206.  Where all bring more, a launch for nothing: 8 sequences of 24 tokens 66.7 and 70.3, 16 of 32 135 and 138.)
+// (32 / 8 heads of 128, a piece of a prompt beside 31 sequences of 900 to 11777 with a token each: 1000 tokens 343 us in one launch, 271 in two, 1501 578 and 393;
+// beside seven: 300 107 and 100, 600 179 and 159, 1501 349 and 361, where the sequences of one token filled what the prompt's tiles leave, at head dimension 64 219 and
+// 204.  Where all bring more, a launch for nothing: 8 sequences of 24 tokens 61.6 and 64.2, 16 of 32 130 and 132.)
 constexpr int kFewRows = 48;
 template <int D>
 static hipError_t launch_attend4(PagedArgs a, int dtype, char* ws, hipStream_t st) {

@@ -241,6 +241,8 @@ __device__ __forceinline__ void paged_few_join(const PagedArgs& a, const PagedRu
 // reaches the rows that see it and no other.  Eight waves, one of each step's eight tiles each: the matrix cores' fp32 rate
 // bounds a wave (1024 clocks a tile at head dimension 64), and items are few.  (Four waves, 333 tokens of two sequences of up to 1024, 4 / 2
 // heads of 64: 19.0 us; eight: 17.4.)
+// A wave's priority rises from the first product to the second: the two of a SIMD fall out of step (4 bits, 17.7 -> 17.0; 500 tokens of each of four sequences of 2000, 32 / 8
+// heads of 128, 682 -> 672).
 // FOUR: the cache holds 4 bits a number; the same values come out of their conversion.
 template <int D, bool FOUR>
 __global__ __launch_bounds__(512) void paged_few_f32_kernel(PagedArgs args) {
@@ -299,6 +301,7 @@ __global__ __launch_bounds__(512) void paged_few_f32_kernel(PagedArgs args) {
 #pragma unroll
       for (int e = 0; e < D / 64; e++) vv[0][i][e] = vn[i][e];
     if (j + 8 < j1) ask(j + 8);
+    __builtin_amdgcn_s_setprio(1);
     f32x4 s[1] = {mma_dot<D>(kv, qv)};                                           // lane (row n, kq): keys 4 kq + i
     const int lim = last - (j * 16 + 4 * kq);
     float mx = -INFINITY;
@@ -320,7 +323,9 @@ __global__ __launch_bounds__(512) void paged_few_f32_kernel(PagedArgs args) {
 #pragma unroll
     for (int i = 0; i < 4; i++) s[0][i] = __builtin_amdgcn_exp2f(fmaf(s[0][i], a.c1, off));
     l_run += (s[0][0] + s[0][1]) + (s[0][2] + s[0][3]);
+    __builtin_amdgcn_s_setprio(2);
     mma_outer_keys<D, 1>(vv, s, lim, min(T, it.m - t0), a.g, lane, acc);
+    __builtin_amdgcn_s_setprio(0);
   }
   const float l_tot = quad_rows_sum(l_run);
   float* ml = x + 8 * 16 * (D + 4);
