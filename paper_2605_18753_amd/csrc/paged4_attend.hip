@@ -287,10 +287,10 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void paged_few4_kernel(Paged
 
 // Many rows: a tile is 128 (token, head) rows, as in paged_rows_kernel, whose walk this is: the two products, the exponentials and the maxima
 // between their MFMAs, the order of operands.  64-key tiles of K and V are converted on their way into LDS, each by the whole workgroup once: 32 conversions a thread
-// and tile, beside some 250 vector instructions and 32 MFMAs of each wave.  Bound by the matrix units (0.44 of the clocks), the vector units (0.54) and LDS (K and V, 32 KB, go to each of
-// a CU's eight waves, 2050 clocks at 128 bytes a clock, and are written at 75, 850, of a step's 4200) by turns.  2048 tokens at the end of 32768, 32 / 8 heads of 128,
-// 1000 us (1.1 PFLOP/s; pages of bf16 967 to 1080 by card).  Head dimension 64: three workgroups a CU (all exponentials between the first product's MFMAs, which
-// spares the registers that a third one needs): the same 656 us, two 741; 1501 tokens beside seven decoding sequences, in one launch, 215 and 238.
+// and tile, beside some 250 vector instructions and 32 MFMAs of each wave.  Bound by the vector units (0.60 of the clocks), the matrix units (0.48) and LDS (K and V, 32 KB, go to each of
+// a CU's eight waves, 2050 clocks at 128 bytes a clock, and are written at 75, 850, of a step's 4000).  2048 tokens at the end of 32768, 32 / 8 heads of 128, 1000 to
+// 1060 us by card (1.1 PFLOP/s; pages of bf16 967 to 1080).  Head dimension 64: three workgroups a CU (all exponentials between the first product's MFMAs, which
+// spares the registers that a third one needs): the same 624 us (before waves had priorities 656, and with two workgroups a CU 741).
 template <int D> struct Rows4Cfg {
   static constexpr int CW = D / 32, ROW_BYTES = D * 2;
   static constexpr int TILE_BYTES = 64 * ROW_BYTES;
