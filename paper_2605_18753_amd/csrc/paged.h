@@ -35,14 +35,16 @@ struct PagedArgs {
   float c1;                              // scale * log2(e)
   int wgs;                               // runs of a kv-head; 0: an item a workgroup.  Tiles of 128 rows: parts of a kv-head at most; 0: none is cut
   int whole;                             // runs: items may be left uncut; weights: two kernels share the sequences
-  int pad;                               // runs: steps that an item's start counts for
-  int few;                               // > 0: the launch has the sequences of up to so many rows; < 0: those of more than -few; 0: all
-  int tight;                             // tiles of 128 rows: items of one length are cut into as many parts each as there are places for, or twice that
   int slots; float gain;                 // tiles of 128 rows: workgroups of a kv-head that are resident at once; what finer parts must come to
   float* part_o; float* part_ml;         // records of cut items: two of each run (the item it begins in, the one it ends in), one of each part
-  const uint8_t* k_sc; const uint8_t* v_sc;   // a cache in 4 bits: its scales (k and v its codes, their strides in bytes)
   uint64_t* flags; uint64_t nonce;       // runs: two of each record, and the number that says that it is complete
+  // a cache in 4 bits only (k and v its codes, their strides in bytes)
+  const uint8_t* k_sc; const uint8_t* v_sc;   // its scales
+  int pad;                               // runs: steps that an item's start counts for
+  int few;                               // > 0: the launch has the sequences of up to so many rows; < 0: those of more than -few; 0: all
 };
+// What these two ask for, and the dealing of items of one length (paged_part_size), is compiled for such a cache alone (FOUR): for pages of bf16, where they would
+// change nothing, they took a launch 0.3 to 1 us (one token of 16 sequences of 200 to 1000 12.65 -> 13.1, a prompt of 1000 28.9 -> 29.8).
 
 __device__ __forceinline__ int paged_len(const PagedArgs& a, int b) { return min(max(a.lens[b], 0), a.cap); }
 // first packed row of sequence b and how many it has
@@ -52,11 +54,11 @@ __device__ __forceinline__ int2 paged_rows(const PagedArgs& a, int b) {
 }
 // A lane's sequence of 64: its rows and length (none behind the batch).  The first 64 are loaded once and kept.
 struct PagedLane { int2 rm; int n; };
-__device__ __forceinline__ PagedLane paged_lane(const PagedArgs& a, int b) {
+template <bool FOUR> __device__ __forceinline__ PagedLane paged_lane(const PagedArgs& a, int b) {
   PagedLane l = {make_int2(0, 0), 0};
   if (b < a.batch) {
     l.rm = paged_rows(a, b);
-    if (a.few > 0 ? l.rm.y > a.few : l.rm.y <= -a.few) l.rm.y = 0;
+    if constexpr (FOUR) if (a.few > 0 ? l.rm.y > a.few : l.rm.y <= -a.few) l.rm.y = 0;
     l.n = paged_len(a, b);
   }
   return l;
@@ -109,14 +111,14 @@ struct PagedCut { int size, whole, items; };               // of the items behin
 // of sequence tiles, those among the first `whole` items; before: items before the sequence's
 __device__ __forceinline__ int paged_whole(const PagedCut& cut, int before, int tiles) { return min(max(cut.whole - before, 0), tiles); }
 // The launch that adds the parts up has to come to the same: no products are fused with sums here.
-template <typename F> __device__ __forceinline__ PagedCut paged_part_size(const PagedArgs& a, const PagedLane& l0, F&& shape) {
+template <bool FOUR, typename F> __device__ __forceinline__ PagedCut paged_part_size(const PagedArgs& a, const PagedLane& l0, F&& shape) {
 #pragma clang fp contract(off)
   if (a.wgs <= 0) return {kUncut, 0, 0};
   const int lane = lane_id(), half = a.slots / 2;
   int items = 0;
   float cost = 0.f, most = 0.f, rest = 0.f;                // rest: of the items behind the first `half`
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
-    const PagedLane l = i0 ? paged_lane(a, i0 + lane) : l0;
+    const PagedLane l = i0 ? paged_lane<FOUR>(a, i0 + lane) : l0;
     const int2 s = shape(l.rm.y, l.n);
     const int incl = items + wave_scan(s.x);
     rest += wave_sum((float)(s.x - min(max(half - (incl - s.x), 0), s.x)) * (float)s.y);
@@ -133,10 +135,10 @@ template <typename F> __device__ __forceinline__ PagedCut paged_part_size(const 
   const float even = cost / (float)a.slots;
   PagedCut cut = {items < a.slots ? size(cost, a.slots) : kUncut, 0, items};
   float time = items <= a.slots ? fminf((float)cut.size, most) : fminf((float)((items + a.slots - 1) / a.slots) * most, even + 0.5f * most);
-  // Items of one length (one sequence's): as many parts each as there are places for, once or twice.  (The sum over w - n leaves places unused: 512 tokens against 32k in 4 bits, 16
+  // A cache in 4 bits, items of one length (one sequence's): as many parts each as there are places for, once or twice.  (The sum over w - n leaves places unused: 512 tokens against 32k in 4 bits, 16
   // items for 64 places, in three parts each 330 us, in four 296; 700, 22 items: five parts take 0.85 of the time of two.)
   bool finer = false;
-  if (a.tight && items <= a.slots && most * (float)items <= cost) {
+  if (FOUR && items <= a.slots && most * (float)items <= cost) {
     const auto parts = [&](int k) { return max((int)ceilf(most / (float)max(k, 1)), kMinPart); };
     const int once = parts(a.slots / max(items, 1)), twice = parts(min(2 * a.slots, a.wgs) / max(items, 1));
     finer = 2 * twice + 6 < once;
@@ -157,17 +159,18 @@ template <typename F> __device__ __forceinline__ PagedCut paged_part_size(const 
 
 struct PagedPart { int b, tile, part, parts, rec0, r0, m, n; };   // rec0: the item's first part among those of the kv-head
 // Every lane of a wave: part `idx` of a kv-head.
-template <typename F> __device__ __forceinline__ bool paged_find_part(const PagedArgs& a, int idx, F&& shape, PagedPart& it) {
+template <bool FOUR, typename F> __device__ __forceinline__ bool paged_find_part(const PagedArgs& a, int idx, F&& shape, PagedPart& it) {
   const int lane = lane_id();
-  const PagedLane l0 = paged_lane(a, lane);
-  const PagedCut cut = paged_part_size(a, l0, shape);
+  const PagedLane l0 = paged_lane<FOUR>(a, lane);
+  const PagedCut cut = paged_part_size<FOUR>(a, l0, shape);
   // None is cut, and all are resident: whoever comes second to a CU takes the tiles from the other end, so that a prompt's long ones stand beside its short ones.
-  // (In 4 bits, two prompts of 1000 tokens 51 and 44 us, 2000 tokens against 6000 188 and 181; 2000 of 2000 64 both ways.)
+  // (In 4 bits, two prompts of 1000 tokens 51 and 44 us, 2000 tokens against 6000 188 and 181; 2000 of 2000 64 both ways.  Over pages of bf16 39.6 and 34.1, 174 and
+  // 169, 53 and 52; three prompts of 1000 49.9 and 50.1.)
   if (const int one = kCUs / a.h_kv; cut.size == kUncut && idx >= one && idx < cut.items && cut.items <= a.slots) idx = cut.items - 1 - (idx - one);
   const bool whole = idx < cut.whole;
   int items = 0, base = whole ? 0 : cut.whole;
   for (int i0 = 0; i0 < a.batch; i0 += 64) {
-    const PagedLane p = i0 ? paged_lane(a, i0 + lane) : l0;
+    const PagedLane p = i0 ? paged_lane<FOUR>(a, i0 + lane) : l0;
     const int2 s = shape(p.rm.y, p.n);
     const int upto = items + wave_scan(s.x), uncut = paged_whole(cut, upto - s.x, s.x);
     const int parts = whole ? 1 : (s.y + cut.size - 1) / cut.size, skip = whole ? 0 : uncut, count = (s.x - skip) * parts;
@@ -204,9 +207,9 @@ constexpr int kStep = 128;
 constexpr int kJoin = 6;
 struct PagedSeq { int tiles, u, flat; };                   // flat > 0: steps of every tile (no causal mask)
 struct PagedItem { int b, tile, r0, m, n; PagedSeq s; };
-struct PagedDeal {
+template <bool FOUR> struct PagedDeal {
   int T, k_log, pad;                                       // tokens of a tile, log2 of k, steps before an item's first
-  __device__ __forceinline__ PagedDeal(const PagedArgs& a, int rows) : T(rows / a.g), k_log(31 - __builtin_clz(kStep / (rows / a.g))), pad(a.pad) {}
+  __device__ __forceinline__ PagedDeal(const PagedArgs& a, int rows) : T(rows / a.g), k_log(31 - __builtin_clz(kStep / (rows / a.g))), pad(FOUR ? a.pad : 0) {}
   __device__ __forceinline__ PagedSeq seq(const PagedArgs& a, int m, int n) const {
     return {(m + T - 1) / T, (max(n - m, 0) + T - 1) / T, a.causal ? 0 : max((n + kStep - 1) / kStep, 1)};
   }
@@ -221,7 +224,7 @@ struct PagedDeal {
     int f = 0;
     items = most = 0;
     for (int i0 = 0; i0 < a.batch; i0 += 64) {
-      const PagedLane l = i0 ? paged_lane(a, i0 + lane_id()) : l0;
+      const PagedLane l = i0 ? paged_lane<FOUR>(a, i0 + lane_id()) : l0;
       const PagedSeq s = seq(a, l.rm.y, l.n);
       f += __builtin_amdgcn_readlane(wave_scan(before(s, s.tiles)), 63);
       if (!a.whole) continue;
@@ -234,7 +237,7 @@ struct PagedDeal {
   __device__ __forceinline__ int find(const PagedArgs& a, const PagedLane& l0, int f, bool by_steps, PagedItem& it) const {
     const int lane = lane_id();
     for (int i0 = 0; i0 < a.batch; i0 += 64) {
-      const PagedLane p = i0 ? paged_lane(a, i0 + lane) : l0;
+      const PagedLane p = i0 ? paged_lane<FOUR>(a, i0 + lane) : l0;
       const PagedSeq s = seq(a, p.rm.y, p.n);
       const int v = by_steps ? before(s, s.tiles) : s.tiles, incl = wave_scan(v);
       const uint64_t hit = __ballot(incl > f);
@@ -296,14 +299,14 @@ __device__ __forceinline__ int paged_thread() {
 }
 
 // A workgroup's pieces of items, one after the other: steps [x0, x1) of item `it`.
-struct PagedRun {
-  PagedDeal deal;
+template <bool FOUR> struct PagedRun {
+  PagedDeal<FOUR> deal;
   PagedItem it;
   int x0, x1, cost;
   int next, end, total;                                    // the step behind this piece, the run's end, the steps of the kv-head
   __device__ __forceinline__ PagedRun(const PagedArgs& a, int rows = 16) : deal(a, rows) {}
   __device__ __forceinline__ bool begin(const PagedArgs& a, int wg) {
-    const PagedLane l0 = paged_lane(a, lane_id());
+    const PagedLane l0 = paged_lane<FOUR>(a, lane_id());
     bool cut = a.wgs > 0;
     if (cut) {
       int items, most;
@@ -335,7 +338,7 @@ struct PagedRun {
   __device__ __forceinline__ bool advance(const PagedArgs& a) {
     if (next >= end) return false;
     x0 = 0;
-    if (++it.tile >= it.s.tiles) deal.find(a, paged_lane(a, lane_id()), next, true, it);
+    if (++it.tile >= it.s.tiles) deal.find(a, paged_lane<FOUR>(a, lane_id()), next, true, it);
     next += deal.pad;
     cost = deal.steps(it.s, it.tile);
     return piece();

@@ -135,7 +135,7 @@ __global__ __launch_bounds__(256, D == 128 ? 2 : 3) void paged_few4_kernel(Paged
   constexpr int ROWS = 16 * G;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int r = blockIdx.x % args.h_kv, wg = blockIdx.x / args.h_kv;
-  PagedRun run(args, ROWS);
+  PagedRun<true> run(args, ROWS);
   if (!run.begin(args, wg)) return;
   const PagedItem& it = run.it;
   do {
@@ -307,7 +307,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void paged_rows4_kernel(Paged
   // kv-heads are the fast index: with 8 of them each XCD's L2 sees the pages of one
   const int r = blockIdx.x % a.h_kv;
   PagedPart it;
-  if (!paged_find_part(a, blockIdx.x / a.h_kv, [&](int m, int n) { return rows_shape(a, m, n); }, it)) return;
+  if (!paged_find_part<true>(a, blockIdx.x / a.h_kv, [&](int m, int n) { return rows_shape(a, m, n); }, it)) return;
   const int T = 128 / a.g, t0 = it.tile * T, Tw = 32 / a.g, tw0 = t0 + wave * Tw;
   const int t = tw0 + n / a.g;
   bf16x8 qf[D / 16];
@@ -641,7 +641,6 @@ static hipError_t launch_tiles4(PagedArgs a, int dtype, int tile, int64_t items,
   a.wgs = items < (big ? 2 : 8) * (int64_t)runs ? runs : 0;
   if (big && a.wgs && items * 4 >= runs) a.wgs = (int)items + runs * 3 / 2;
   a.slots = runs;
-  a.tight = 1;
   a.gain = (int64_t)a.n_rows * a.g < 64 * items ? 0.65f : 0.9f;
   // An item's start (and the end of the piece before it) takes as long as so many steps.  (0, 3, 4, 8 of them: one token of 8 sequences of 384 to 16000 25.7, 23.1, 22.3 and
   // 23.0 us, of 32 of 4096 to 32768 129.0, 127.6, 127.2 and 126.1; of 8 of one length, where all runs begin with an item, 20.3, 20.9, 21.2 and 21.2.)
@@ -659,7 +658,7 @@ static hipError_t launch_tiles4(PagedArgs a, int dtype, int tile, int64_t items,
     if (hipError_t e = allow_dyn_lds((const void*)paged_rows4_kernel<D>, Rows4Cfg<D>::LDS_BYTES, opt_in); e != hipSuccess) return e;
     hipLaunchKernelGGL(paged_rows4_kernel<D>, grid, dim3(256), Rows4Cfg<D>::LDS_BYTES, st, a);
     const hipError_t e = hipGetLastError();
-    return e != hipSuccess || a.wgs <= 1 ? e : launch_paged_merge(a, D, st);
+    return e != hipSuccess || a.wgs <= 1 ? e : launch_paged4_merge(a, D, st);
   }
   if (dtype == DASH_BF16) {
     if (hipError_t e = tile == 32 ? launch_few4<D, 2>(a, grid, st) : launch_few4<D, 1>(a, grid, st); e != hipSuccess) return e;

@@ -24,7 +24,7 @@ __global__ __launch_bounds__(256, 2) void paged_few_kernel(PagedArgs args) {
   using C = FewCfg<D>;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int r = blockIdx.x % args.h_kv, wg = blockIdx.x / args.h_kv;
-  PagedRun run(args);
+  PagedRun<false> run(args);
   if (!run.begin(args, wg)) return;
   const PagedItem& it = run.it;
   do {
@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
   // kv-heads are the fast index: with 8 of them each XCD's L2 sees the pages of one
   const int r = blockIdx.x % a.h_kv;
   PagedPart it;
-  if (!paged_find_part(a, blockIdx.x / a.h_kv, [&](int m, int n) { return rows_shape(a, m, n); }, it)) return;
+  if (!paged_find_part<false>(a, blockIdx.x / a.h_kv, [&](int m, int n) { return rows_shape(a, m, n); }, it)) return;
   const int T = 128 / a.g, t0 = it.tile * T, Tw = 32 / a.g, tw0 = t0 + wave * Tw;
   const int t = tw0 + n / a.g, head = r * a.g + n % a.g;
   const bool row_ok = t < it.m;
@@ -471,15 +471,15 @@ __global__ __launch_bounds__(256, 2) void paged_rows_kernel(PagedArgs a) {
 
 // Adds up the parts of tiles of 128 rows: o = sum_p 2^(m_p - M) O_p / sum_p 2^(m_p - M) l_p.  A workgroup adds 256 / (D / 4) / SLICES (token, head) rows at a time, SLICES groups of threads
 // each taking every SLICES-th part.
-template <int D, int SLICES>
+template <int D, int SLICES, bool FOUR>
 __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
   constexpr int TPR = D / 4, PER = 256 / TPR / SLICES;     // threads of a row's slice, rows of a workgroup
   __shared__ f32x4 xo[SLICES > 1 ? 256 : 1];
   __shared__ float xd[SLICES > 1 ? 2 * (256 / TPR) : 1];
   const int lane = threadIdx.x & 63, c = threadIdx.x % TPR, unit = threadIdx.x / TPR, slice = unit / PER;
   const auto shape = [&](int m, int n) { return rows_shape(a, m, n); };
-  const PagedLane l0 = paged_lane(a, lane);
-  const PagedCut cut = paged_part_size(a, l0, shape);
+  const PagedLane l0 = paged_lane<FOUR>(a, lane);
+  const PagedCut cut = paged_part_size<FOUR>(a, l0, shape);
   if (cut.size == kUncut) return;
   // rows in the order kv-head, token, head of the group: neighbours lie side by side in the records
   const uint32_t per = (uint32_t)a.n_rows * (uint32_t)a.g, all = per * (uint32_t)a.h_kv, g_log = 31 - __builtin_clz(a.g);   // 2^28 at most
@@ -489,7 +489,7 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedArgs a) {
     // the dealing of the launch before, for a given row
     int first = 0, parts = 0, tiles = 0, r0 = 0, items = 0, base = cut.whole;   // tiles: those that are cut
     for (int i0 = 0; i0 < a.batch; i0 += 64) {
-      const PagedLane p = i0 ? paged_lane(a, i0 + lane) : l0;
+      const PagedLane p = i0 ? paged_lane<FOUR>(a, i0 + lane) : l0;
       const int2 rm = p.rm, s = shape(rm.y, p.n);
       const int upto = items + wave_scan(s.x), nt = s.x - paged_whole(cut, upto - s.x, s.x);
       const int np = (s.y + cut.size - 1) / cut.size, incl = wave_scan(nt * np);
@@ -563,15 +563,15 @@ size_t paged_attend_ws(const PagedArgs& a, int dtype, int d) {
   return ws_align(recs * 8) + recs * d * 4 + few / 16 * 16;   // two flags a record of 16 rows
 }
 
-template <int D> static hipError_t launch_merge(const PagedArgs& a, hipStream_t st) {
+template <int D, bool FOUR> static hipError_t launch_merge(const PagedArgs& a, hipStream_t st) {
   // few rows leave the chip idle unless several groups of threads share a row's parts (1280 rows, the call: 32.8 us shared, 34.0 not; 2048 59.4 and 58.0)
   const int64_t out = (int64_t)a.n_rows * a.h_q;
   constexpr int units = 256 / (D / 4);
-  if (out <= 1536) hipLaunchKernelGGL((paged_merge_kernel<D, 4>), dim3((unsigned)((out + units / 4 - 1) / (units / 4))), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((paged_merge_kernel<D, 1>), dim3(1024), dim3(256), 0, st, a);
+  if (out <= 1536) hipLaunchKernelGGL((paged_merge_kernel<D, 4, FOUR>), dim3((unsigned)((out + units / 4 - 1) / (units / 4))), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((paged_merge_kernel<D, 1, FOUR>), dim3(1024), dim3(256), 0, st, a);
   return hipGetLastError();
 }
-hipError_t launch_paged_merge(const PagedArgs& a, int d, hipStream_t st) { return d == 128 ? launch_merge<128>(a, st) : launch_merge<64>(a, st); }
+hipError_t launch_paged4_merge(const PagedArgs& a, int d, hipStream_t st) { return d == 128 ? launch_merge<128, true>(a, st) : launch_merge<64, true>(a, st); }
 
 template <int D>
 static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st) {
@@ -611,7 +611,7 @@ static hipError_t launch_attend(PagedArgs a, int dtype, char* ws, hipStream_t st
     hipLaunchKernelGGL((paged_few_f32_kernel<D, false>), grid, dim3(512), lds, st, a);
   }
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess || a.wgs <= 1 || !big ? e : launch_paged_merge(a, D, st);
+  return e != hipSuccess || a.wgs <= 1 || !big ? e : launch_merge<D, false>(a, st);
 }
 
 hipError_t launch_paged_attend(const PagedArgs& a, int dtype, int d, char* ws, hipStream_t st) {

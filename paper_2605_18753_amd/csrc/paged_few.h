@@ -48,8 +48,8 @@ template <int D, int ROWS> struct PagedRecords {
 
 // What the waves hold of a tile's ROWS rows is added up in LDS, and written as the output or as a record of the piece.
 // x: [WAVES][ROWS][D + 4] floats, ml: [WAVES][ROWS][2].  Of the first 256 threads, 16 i .. + 15 hold row i, row 16 + i ..
-template <typename T, int D, int WAVES, int ROWS = 16>
-__device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const PagedRun& run, int r, int64_t rec, int t0, const float* x, const float* ml) {
+template <typename T, int D, int WAVES, int ROWS = 16, bool FOUR>
+__device__ __forceinline__ void paged_few_finish(const PagedArgs& a, const PagedRun<FOUR>& run, int r, int64_t rec, int t0, const float* x, const float* ml) {
   const PagedItem& it = run.it;
   const int c = threadIdx.x & 15;
 #pragma unroll
@@ -120,8 +120,8 @@ struct PagedSum {
 // up the groups and clears the flags, none of which is set after that.  (16 heads on one, one sequence of 16000 tokens, 125 pieces: 92 us in one
 // level, 20 in two; 32 on 8, 1000 tokens, 8 pieces: 11 in two, 9.3 in one.)
 constexpr int kChain = 24;
-template <typename T, int D, int THREADS, int ROWS = 16>
-__device__ __forceinline__ void paged_few_join(const PagedArgs& a, const PagedRun& run, int r, int wg, char* lds) {
+template <typename T, int D, int THREADS, int ROWS = 16, bool FOUR>
+__device__ __forceinline__ void paged_few_join(const PagedArgs& a, const PagedRun<FOUR>& run, int r, int wg, char* lds) {
   constexpr int TPR = D / 4, UNITS = THREADS / TPR;        // threads of a row; rows at a time
   const PagedItem& it = run.it;
   f32x4* xo = reinterpret_cast<f32x4*>(lds);               // [THREADS], [UNITS][2], [1]
@@ -165,7 +165,8 @@ __device__ __forceinline__ void paged_few_join(const PagedArgs& a, const PagedRu
   const PagedRecords<D, ROWS> recs(a);
   // adds up `count` records, place(i) the i-th; write(row, sum) by the threads that hold a row's sum
   auto add_up = [&](int count, auto&& place, auto&& write) {
-    constexpr int RG = D / 64, KP = 4;                        // rows of a thread, and records, asked for together; and as many records again where there are more
+    // rows of a thread, and records, asked for together; and as many records again where there are more.  (Two rows: no faster over pages of bf16, in fp32 33.3 us for 32.9.)
+    constexpr int RG = FOUR ? D / 64 : 1, KP = 4;
     for (int i0 = 0; i0 < rows; i0 += per * RG) {
       PagedSum sum[RG];
       for (int p0 = 0; p0 < count; p0 += 2 * KP * slices) {
@@ -249,7 +250,7 @@ __global__ __launch_bounds__(512) void paged_few_f32_kernel(PagedArgs args) {
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   float* x = reinterpret_cast<float*>(lds);                                      // [8][16][D + 4], [8][16][2]
   const int r = blockIdx.x % args.h_kv, wg = blockIdx.x / args.h_kv;
-  PagedRun run(args);
+  PagedRun<FOUR> run(args);
   if (!run.begin(args, wg)) return;
   const PagedItem& it = run.it;
   do {
@@ -357,6 +358,6 @@ inline int64_t paged_most_items(const PagedArgs& a, int rows) {   // of a kv-hea
   return min((int64_t)a.n_rows / T + min(a.batch, a.n_rows), (int64_t)a.n_rows);
 }
 inline int paged_most_parts(int runs) { return runs * 7 / 2; }   // of a kv-head: fewer than two items a resident workgroup, and one and a half
-hipError_t launch_paged_merge(const PagedArgs& a, int d, hipStream_t st);
+hipError_t launch_paged4_merge(const PagedArgs& a, int d, hipStream_t st);
 
 }  // namespace dash
