@@ -603,9 +603,9 @@ def dash_rotary(r: Rotary, q, q_out, k=None, k_out=None, pos=None, start: int = 
             raise DashError("q and k have the same batch, head dimension and type")
         else:
             # an output overlaps neither the other output nor the other's input
-            size = q.element_size()
-            for x, hx, y, hy in ((q_to, h_q, k_to, h_kv), (q_to, h_q, k_in, h_kv), (k_to, h_kv, q_in, h_q)):
-                if x[1] < y[2] and y[1] < x[2] and not _apart(x, hx, y, hy, d, size):
+            q_shape, k_shape, size = (batch, h_q, n_q), (batch, h_kv, n_kv), q.element_size()
+            for x, x_shape, y, y_shape in ((q_to, q_shape, k_to, k_shape), (q_to, q_shape, k_in, k_shape), (k_to, k_shape, q_in, q_shape)):
+                if x[1] < y[2] and y[1] < x[2] and _meet(x, x_shape, y, y_shape, d, size):
                     raise DashError("the outputs overlap neither each other nor the other's input")
         if k.get_device() != dev or k_out.get_device() != dev:
             raise DashError("the tensors lie on one device")
@@ -627,18 +627,29 @@ def dash_rotary(r: Rotary, q, q_out, k=None, k_out=None, pos=None, start: int = 
     _check(load_library().dash_rotary_apply(p, plan, _ptr(pos), qp, qop, kp, kop, stream), "dash_rotary_apply")
 
 
-def _apart(x, x_heads, y, y_heads, d, size) -> bool:
-    """Whether tensors in each other's span are heads of one tensor (queries and keys of a fused projection): the same strides, and starts that keep their
-    heads apart within one token's row, or all of their heads apart modulo a stride that the others are multiples of."""
-    (s, x_ptr, _), (t, y_ptr, _) = x, y
-    if s != t:
-        return False
-    first, off = (x_heads, y_ptr - x_ptr) if x_ptr <= y_ptr else (y_heads, x_ptr - y_ptr)
-    then, off = x_heads + y_heads - first, off // size
-    if (first - 1) * s[1] + d <= off and off + (then - 1) * s[1] + d <= s[2]:
-        return True
-    step = min(s[:3])
-    return step > 0 and d <= off % step <= step - d and not any(x % step for x in s[:3])
+def _meet(x, x_shape, y, y_shape, d, size) -> bool:
+    """Whether two tensors (strides, first byte; shape without the d numbers of a row, which lie together) share an element.  Their differences of
+    indices are gone through by falling strides, those alone that the rest can make up for: one or two a stride where a tensor's dimensions lie
+    inside of each other.  Tensors for which that takes more than a thousand steps count as meeting."""
+    steps = []
+    for s, m, t, n in zip(x[0], x_shape, y[0], y_shape):
+        if s == t:
+            steps.append((s, 1 - m, n - 1))
+        else:
+            steps += [(s, 1 - m, 0), (t, 0, n - 1)]
+    steps = sorted((s for s in steps if s[0] and s[1] < s[2]), reverse=True)
+    tries = 1000
+
+    def near(i, off):
+        nonlocal tries
+        tries -= 1
+        if i == len(steps) or tries < 0:
+            return tries < 0 or -d < off < d
+        s, lo, hi = steps[i]
+        low = off + sum(t * m for t, m, _ in steps[i + 1:])
+        high = off + sum(t * m for t, _, m in steps[i + 1:])
+        return any(near(i + 1, off + a * s) for a in range(max(lo, -((high + d - 1) // s)), min(hi, (d - 1 - low) // s) + 1))
+    return near(0, (y[1] - x[1]) // size)                    # addresses are multiples of 16 bytes
 
 
 def dash_paged_append_rotary(p: dash_paged_params, cache: PagedCache, rotary: Rotary, k_new, v_new, row_start, q=None, q_out=None) -> None:

@@ -359,3 +359,57 @@ def test_the_plain_quantisation():
     unit = torch.exp2(scales.double() - 127)
     # no further off than half the step where it is: 0.25 below 2, 0.5 below 4, 1 below 6, and at the largest up to 1.25
     assert ((held - y).abs() <= torch.where(y.abs() < 2 * unit, 0.25, torch.where(y.abs() < 4 * unit, 0.5, 1.25)) * unit).all()
+
+
+# ---- tensors in each other's span ------------------------------------------------------------------------------------
+def elements(x):
+    """The elements' places in their storage."""
+    return torch.arange(x.untyped_storage().size() // x.element_size()).as_strided(x.shape, x.stride(), x.storage_offset())
+
+
+def share(x, y):
+    return x.untyped_storage().data_ptr() == y.untyped_storage().data_ptr() and bool(torch.isin(elements(x), elements(y)).any())
+
+
+def spans(batch, h_q, h_kv, n, d, seed):
+    """Queries and keys cut out of one tensor, its dimensions in any order, each at a place of its own."""
+    gen = torch.Generator().manual_seed(seed)
+    draw = lambda lo, hi: int(torch.randint(lo, hi + 1, (1,), generator=gen))  # noqa: E731
+    order = torch.randperm(3, generator=gen).tolist()            # which of batch, head and token lies outermost
+    sizes = [batch, h_q + h_kv, n]
+    room = [m + draw(0, 2) for m in sizes]
+    x = torch.zeros([room[i] for i in order] + [d + 16 * draw(0, 1)])
+    x = x.permute(*[order.index(i) for i in range(3)], 3)
+    def part(heads):
+        b, h, t = (draw(0, room[i] - m) for i, m in ((0, batch), (1, heads), (2, n)))
+        return x[b:b + batch, h:h + heads, t:t + n, :d]
+    return part(h_q), part(h_kv)
+
+
+def test_tensors_that_share_elements_are_told_from_those_that_do_not():
+    """In place on both: refused where they share elements, and nowhere else."""
+    r = B.make_rotary(64, "cpu")
+    said = {True: 0, False: 0}
+    for seed in range(300):
+        gen = torch.Generator().manual_seed(seed)
+        batch, h_q, h_kv, n = (int(torch.randint(1, m, (1,), generator=gen)) for m in (4, 5, 3, 6))
+        q, k = spans(batch, h_q, h_kv, n, 64, seed)
+        with pytest.raises(B.DashError) as e:
+            B.dash_rotary(r, q, q, k, k)
+        said[share(q, k)] += 1
+        assert ("overlap" if share(q, k) else "GPU") in str(e.value), (seed, q.shape, q.stride(), k.shape, k.stride(), k.storage_offset() - q.storage_offset())
+    assert min(said.values()) > 50
+
+
+def test_batches_inside_of_a_tokens_row():
+    """[tokens, sequences, heads, d]: the queries' second sequence is the keys' first; heads of one tensor, and sequences in both, are apart."""
+    r = B.make_rotary(64, "cpu")
+    x = torch.zeros((10, 5, 6, 64))
+    pairs = [(x[:, 0:4, :4].permute(1, 2, 0, 3), x[:, 1:5, :4].permute(1, 2, 0, 3), True), (x[:, 0:4, :4].permute(1, 2, 0, 3), x[:, 0:4, 4:].permute(1, 2, 0, 3), False),
+             (x[:, 0:4, :4].permute(1, 2, 0, 3), x[:, 1:5, 4:].permute(1, 2, 0, 3), False), (x[:, 0:2, :4].permute(1, 2, 0, 3), x[:, 2:4, :4].permute(1, 2, 0, 3), False)]
+    one = torch.zeros((10, 3, 64))
+    pairs.append((one[:, 0:2].transpose(0, 1).unsqueeze(1), one[:, 1:3].transpose(0, 1).unsqueeze(1), True))
+    for q, k, meet in pairs:
+        assert share(q, k) == meet
+        with pytest.raises(B.DashError, match="overlap" if meet else "GPU"):
+            B.dash_rotary(r, q, q, k, k)
