@@ -359,7 +359,7 @@ int dash_paged_append(const dash_paged_params* p, const void* k_new, const void*
                       const int32_t* seen, void* stream);
 
 /* Attention of the new tokens over the cache (Eq. 1), which holds their own keys and values already:
- *   o   out [n_rows, h_q, d]
+ *   o   out [n_rows, h_q, d]; strides that let elements of it fall together are refused (DASH_EINVAL)
  *   lse out, optional, fp32 [n_rows, h_q] contiguous: log of the sum of e^logit over what the row sees
  * A row that sees nothing gets o = 0 and lse = -inf.  The result of a row does not depend on what else is in flight, but
  * its last bits may on the lengths beside it (they decide how long caches are cut). */
@@ -435,7 +435,8 @@ typedef struct dash_rotary_params {
 } dash_rotary_params;
 
 /* Turns q, k or both.
- *   q, q_out  [batch, h_q, n_q, d]; q_out may be q itself (with its strides), or must not overlap it
+ *   q, q_out  [batch, h_q, n_q, d]; q_out may be q itself (with its strides), or must not overlap it; outputs whose strides let elements of their own
+ *             fall together are refused (DASH_EINVAL)
  *   k, k_out  [batch, h_kv, n_kv, d], likewise
  *   pos       int32 [batch, tokens] (tokens: n_kv, or n_q without k), device; NULL: token t has position t
  * Positions (start added, modulo 2^32) are taken as signed 32-bit numbers.  batch * tokens below 2^31, heads of both together up to 2^16
@@ -445,7 +446,7 @@ int dash_rotary_apply(const dash_rotary_params* p, const dash_rotary* r, const i
 
 /* dash_paged_append with the new tokens' keys turned by their positions on the way, seen[b]-m+t or the slot (what goes into pos) as rotary positions.
  *   q, q_out  optional (both or none) [n_rows, h_q, d]: the new tokens' queries, turned as well; strides q_stride and
- *             o_stride of p.  q_out may be q, and shares no element with k_new, v_new or, being another tensor, with q: where their
+ *             o_stride of p.  q_out has a place for each element, may be q, and shares no element with k_new, v_new or, being another tensor, with q: where their
  *             extents overlap, equal strides have to show it (heads of one tensor; DASH_EINVAL otherwise).  Rows of no sequence, and of
  *             tokens without a slot (more new ones than lens), are not written; those of tokens without a page are. */
 int dash_paged_append_rotary(const dash_paged_params* p, const dash_rotary* r, const void* q, void* q_out,

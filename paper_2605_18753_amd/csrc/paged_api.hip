@@ -6,6 +6,7 @@
 
 #include "paged.h"
 #include "rotary.h"
+#include "strided.h"
 
 namespace dash {
 
@@ -67,12 +68,16 @@ static bool may_meet(Heads x, Heads y, const PagedArgs& a, int d, int es) {
   const int64_t step = x.t < x.h ? x.t : x.h, more = x.t < x.h ? x.h : x.t;
   return !(x.h == y.h && step > 0 && more % step == 0 && off % step >= d && off % step <= step - d);
 }
-// The turned queries of a call that appends: q itself, or apart from q, and apart from the new keys and values.
+// Whether packed rows of heads that a call writes share elements among themselves.
+static bool rows_repeat(const dash_paged_params* p, const PagedArgs& a, const void* o) {
+  return strided_repeats({o, 2, {a.o_t, a.o_h}, {a.n_rows, a.h_q}}, p->head_dim);
+}
+// The turned queries of a call that appends: each in a place of its own, q's or apart from q, and apart from the new keys and values.
 static bool queries_meet(const dash_paged_params* p, const PagedArgs& a) {
   if (!a.q) return false;
   const int es = p->dtype == DASH_BF16 ? 2 : 4, d = p->head_dim;
   const Heads out = {a.o, a.o_t, a.o_h, p->h_q};
-  return (a.q == a.o ? a.q_t != a.o_t || a.q_h != a.o_h : may_meet({a.q, a.q_t, a.q_h, p->h_q}, out, a, d, es)) ||
+  return rows_repeat(p, a, a.o) || (a.q == a.o ? a.q_t != a.o_t || a.q_h != a.o_h : may_meet({a.q, a.q_t, a.q_h, p->h_q}, out, a, d, es)) ||
          may_meet({a.k_new, a.kn_t, a.kn_h, p->h_kv}, out, a, d, es) || may_meet({a.v_new, a.vn_t, a.vn_h, p->h_kv}, out, a, d, es);
 }
 static int check_scratch(size_t need, const void* ws, size_t bytes) {
@@ -122,6 +127,7 @@ int dash_paged_attend(const dash_paged_params* p, const void* q, const void* k_p
   if (!q || !k_pages || !v_pages || !row_start || !lens || !table || !o) return DASH_EINVAL;
   if (misaligned(q) || misaligned(k_pages) || misaligned(v_pages) || misaligned(o)) return DASH_EINVAL;
   if (!paged_attend_fits(a, p->dtype)) return DASH_EUNSUPPORTED;
+  if (rows_repeat(p, a, o)) return DASH_EINVAL;
   if (const int rc = check_scratch(paged_attend_ws(a, p->dtype, p->head_dim), workspace, workspace_bytes); rc != DASH_OK) return rc;
   a.q = q; a.k = (void*)k_pages; a.v = (void*)v_pages; a.o = o; a.lse = lse;
   a.row_start = row_start; a.lens = lens; a.table = table;
@@ -203,6 +209,7 @@ int dash_paged4_attend(const dash_paged_params* p, const void* q, const void* k_
   if (!q || !k_codes || !k_scales || !v_codes || !v_scales || !row_start || !lens || !table || !o) return DASH_EINVAL;
   if (misaligned(q) || misaligned(k_codes) || misaligned(v_codes) || misaligned(k_scales) || misaligned(v_scales) || misaligned(o)) return DASH_EINVAL;
   if (!paged4_attend_fits(a, p->dtype)) return DASH_EUNSUPPORTED;
+  if (rows_repeat(p, a, o)) return DASH_EINVAL;
   if (const int rc = check_scratch(paged4_attend_ws(a, p->dtype, p->head_dim), workspace, workspace_bytes); rc != DASH_OK) return rc;
   a.q = q; a.k = (void*)k_codes; a.v = (void*)v_codes; a.k_sc = (const uint8_t*)k_scales; a.v_sc = (const uint8_t*)v_scales; a.o = o; a.lse = lse;
   a.row_start = row_start; a.lens = lens; a.table = table;

@@ -2,6 +2,7 @@
 #include <math.h>
 
 #include "rotary.h"
+#include "strided.h"
 
 namespace dash {
 
@@ -144,6 +145,8 @@ int dash_rotary_apply(const dash_rotary_params* p, const dash_rotary* r, const i
   }
   a.tokens = k ? p->n_kv : p->n_q;
   if ((int64_t)p->batch * a.tokens >= (int64_t)1 << 31 || (int64_t)a.heads[0] + a.heads[1] > 1 << 16) return DASH_EUNSUPPORTED;
+  for (int x = 0; x < 2; x++)
+    if (a.x[x] && strided_repeats({a.y[x], 3, {a.y_b[x], a.y_h[x], a.y_t[x]}, {p->batch, a.heads[x], a.n[x]}}, p->head_dim)) return DASH_EINVAL;
   a.pos = pos; a.pos_b = p->pos_stride; a.start = p->start; a.inverse = p->inverse;
   a.all = (uint32_t)(p->batch * (int64_t)a.tokens);
   const hipStream_t st = (hipStream_t)stream;

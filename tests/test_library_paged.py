@@ -259,3 +259,10 @@ def test_fp32_attention_refuses_more_rows_than_a_launch_has_threads_for():
     for case in (((1 << 23) - 1 << 4) - 1, 1, 1, 1), (1 << 22, 1 << 20, 1, 1):
         assert rc(*case) == -3, case
     assert rc(1 << 24, 1, 16, 16, dtype=B.DASH_BF16) == -3 and rc(1 << 24, 1, 16, 16, name="weigh") == -1
+
+
+def test_outputs_that_share_elements_among_themselves_are_refused():
+    for s in ([0, 128], [1024, 0], [1024, 120], [1016, 128], [256, 128]):      # 7 rows of 8 heads
+        assert call("attend", params(o_stride=s)) == -1, s
+    assert call("attend", params(o_stride=[1024, 128]), n=0) == call("attend", params(o_stride=[128, 896]), n=0) == -3
+    assert call("attend", params(n_rows=1, o_stride=[0, 128]), n=0) == -3

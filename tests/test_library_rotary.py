@@ -4,6 +4,9 @@ import ctypes
 import dataclasses
 import decimal
 import math
+import os
+import shutil
+import subprocess
 
 import pytest
 import torch
@@ -413,3 +416,76 @@ def test_batches_inside_of_a_tokens_row():
         assert share(q, k) == meet
         with pytest.raises(B.DashError, match="overlap" if meet else "GPU"):
             B.dash_rotary(r, q, q, k, k)
+
+
+STRIDED = r"""
+#include <cstdio>
+#include <set>
+#include <vector>
+#include "strided.h"
+using namespace dash;
+static unsigned state = 1;
+static int pick(int n) { state = state * 1664525u + 1013904223u; return (state >> 8) % n; }
+template <typename F> static void each(const Strided& x, F f) {
+  long n[3] = {1, 1, 1}, s[3] = {0, 0, 0};
+  for (int i = 0; i < x.dims; i++) { n[i] = x.size[i]; s[i] = x.stride[i]; }
+  for (int a = 0; a < n[0]; a++) for (int b = 0; b < n[1]; b++) for (int c = 0; c < n[2]; c++) f(a * s[0] + b * s[1] + c * s[2]);
+}
+// small tensors against the set of their elements; strides that often lie next to where a dimension ends
+static Strided some(int d, int place) {
+  Strided x = {(const void*)(long)(16 * place), 1 + pick(3), {}, {}};
+  long inner = d;
+  for (int i = 0; i < x.dims; i++) {
+    x.size[i] = 1 + pick(4);
+    x.stride[i] = pick(3) ? inner + pick(3) - 1 + d * pick(2) : pick(40);
+    inner = x.stride[i] * (x.size[i] - 1) + inner;
+  }
+  if (pick(2) && x.dims > 1) { std::swap(x.size[0], x.size[1]); std::swap(x.stride[0], x.stride[1]); }
+  return x;
+}
+int main() {
+  int bad = 0, found[2] = {0, 0};
+  for (int t = 0; t < 20000; t++) {
+    const int d = 1 + pick(8);
+    const Strided x = some(d, 0);
+    std::set<long> on;
+    bool repeats = false;
+    each(x, [&](long at) { for (int e = 0; e < d; e++) repeats |= !on.insert(at + e).second; });
+    found[repeats]++;
+    bad += strided_repeats(x, d) != repeats;
+  }
+  // a torch layout of the largest sizes takes a few steps, whatever lies outermost
+  const Strided wide = {nullptr, 3, {128, 1l << 40, 1l << 33}, {1 << 20, 65536, 128}};
+  bad += strided_repeats(wide, 128) || strided_repeats({nullptr, 3, {1l << 62, 1l << 62, 128}, {2, 1, 5}}, 128);
+  std::printf("%d wrong, %d apart, %d not\n", bad, found[0], found[1]);
+  return bad != 0 || found[0] < 2000 || found[1] < 2000;
+}
+"""
+
+
+def compiled(tmp_path, source):
+    (tmp_path / "strided.cpp").write_text(source)
+    csrc = os.path.join(os.path.dirname(B.__file__), "csrc")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-I", csrc, str(tmp_path / "strided.cpp"), "-o", str(tmp_path / "strided")], check=True, timeout=120)
+    r = subprocess.run([str(tmp_path / "strided")], capture_output=True, text=True, timeout=60)
+    assert r.returncode == 0, r.stdout
+
+
+@pytest.mark.skipif(not shutil.which("g++"), reason="no host compiler")
+def test_rows_that_share_elements_among_themselves(tmp_path):
+    compiled(tmp_path, STRIDED)
+
+
+def test_outputs_that_share_elements_among_themselves_are_refused():
+    far = 1 << 30
+    for s in ([0, 1280, 128], [5120, 0, 128], [5120, 1280, 0], [5120, 1280, 120], [1280, 1280, 128], [5112, 1280, 128]):
+        p = rparams(q_out_stride=s, k_out_stride=s, h_kv=4)
+        assert apply(p, q_out=far, k=None, k_out=None) == -1 and apply(p, q=None, q_out=None, k_out=far) == -1, s
+    far = dict(q=far, q_out=2 * far, k_new=3 * far, v_new=4 * far)
+    for s in ([0, 128], [1024, 0], [1024, 120], [1016, 128], [256, 128]):      # 7 rows of 8 heads
+        assert call4("rotary", params(o_stride=s), plan(), **far) == -1, s
+        assert call4("append", params4(o_stride=s), plan(), **far) == -1, s
+        assert call4("attend", params4(o_stride=s)) == -1, s
+    n = dict(n=0)                                                # nothing else is wrong but the workspace
+    assert call4("attend", params4(o_stride=[1024, 128]), **n) == call4("attend", params4(o_stride=[128, 896]), **n) == -3
+    assert call4("attend", params4(n_rows=1, o_stride=[0, 128]), **n) == -3
