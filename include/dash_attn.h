@@ -435,9 +435,10 @@ typedef struct dash_rotary_params {
 } dash_rotary_params;
 
 /* Turns q, k or both.
- *   q, q_out  [batch, h_q, n_q, d]; q_out may be q itself (with its strides), or must not overlap it; outputs whose strides let elements of their own
- *             fall together are refused (DASH_EINVAL)
+ *   q, q_out  [batch, h_q, n_q, d]; q_out may be q itself (with its strides)
  *   k, k_out  [batch, h_kv, n_kv, d], likewise
+ *             Refused (DASH_EINVAL) as the strides say: an output whose elements fall together, that shares some with its input without being it, or with
+ *             the other tensor or its output.  (Slices of one tensor that lie apart are fine.)
  *   pos       int32 [batch, tokens] (tokens: n_kv, or n_q without k), device; NULL: token t has position t
  * Positions (start added, modulo 2^32) are taken as signed 32-bit numbers.  batch * tokens below 2^31, heads of both together up to 2^16
  * (DASH_EUNSUPPORTED). */

@@ -145,8 +145,13 @@ int dash_rotary_apply(const dash_rotary_params* p, const dash_rotary* r, const i
   }
   a.tokens = k ? p->n_kv : p->n_q;
   if ((int64_t)p->batch * a.tokens >= (int64_t)1 << 31 || (int64_t)a.heads[0] + a.heads[1] > 1 << 16) return DASH_EUNSUPPORTED;
+  // an output has a place for each element, is its input or apart from it, and apart from the other tensor's
+  const auto in = [&](int x) { return Strided{a.x[x], 3, {a.x_b[x], a.x_h[x], a.x_t[x]}, {p->batch, a.heads[x], a.n[x]}}; };
+  const auto out = [&](int x) { return Strided{a.y[x], 3, {a.y_b[x], a.y_h[x], a.y_t[x]}, {p->batch, a.heads[x], a.n[x]}}; };
+  const auto meet = [&](const Strided& x, const Strided& y) { return strided_meet(x, y, p->head_dim, 16 / vec); };
   for (int x = 0; x < 2; x++)
-    if (a.x[x] && strided_repeats({a.y[x], 3, {a.y_b[x], a.y_h[x], a.y_t[x]}, {p->batch, a.heads[x], a.n[x]}}, p->head_dim)) return DASH_EINVAL;
+    if (a.x[x] && (strided_repeats(out(x), p->head_dim) || (a.x[x] != a.y[x] && meet(in(x), out(x))))) return DASH_EINVAL;
+  if (q && k && (meet(out(0), out(1)) || meet(in(0), out(1)) || meet(out(0), in(1)))) return DASH_EINVAL;
   a.pos = pos; a.pos_b = p->pos_stride; a.start = p->start; a.inverse = p->inverse;
   a.all = (uint32_t)(p->batch * (int64_t)a.tokens);
   const hipStream_t st = (hipStream_t)stream;

@@ -53,4 +53,19 @@ inline bool strided_repeats(const Strided& x, int d) {
   return false;
 }
 
+// Whether two tensors of es bytes an element and as many dimensions share elements; their addresses are multiples of es.
+inline bool strided_meet(const Strided& x, const Strided& y, int d, int es) {
+  StridedSteps s(d);
+  for (int i = 0; i < x.dims; i++) {
+    if (x.stride[i] == y.stride[i]) {
+      s.add(x.stride[i], 1 - x.size[i], y.size[i] - 1);
+    } else {
+      s.add(x.stride[i], 1 - x.size[i], 0);
+      s.add(y.stride[i], 0, y.size[i] - 1);
+    }
+  }
+  s.sort();
+  return s.near(0, ((StridedSteps::Place)(uintptr_t)y.at - (StridedSteps::Place)(uintptr_t)x.at) / es);
+}
+
 }  // namespace dash

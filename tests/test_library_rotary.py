@@ -462,6 +462,28 @@ int main() {
 }
 """
 
+MEET = STRIDED[:STRIDED.index("int main")] + r"""
+int main() {
+  int bad = 0, found[2] = {0, 0};
+  for (int t = 0; t < 20000; t++) {
+    const int d = 1 + pick(8);
+    Strided x = some(d, 0), y = pick(2) ? some(d, 0) : x;
+    y.at = (const void*)(long)(2 * pick(60));
+    if (x.dims != y.dims) continue;
+    if (pick(2)) std::swap(x, y);
+    std::set<long> on;
+    bool meet = false;
+    const long off = ((long)y.at - (long)x.at) / 2;
+    each(x, [&](long at) { for (int e = 0; e < d; e++) on.insert(at + e); });
+    each(y, [&](long at) { for (int e = 0; e < d; e++) meet |= on.count(off + at + e) > 0; });
+    found[meet]++;
+    bad += strided_meet(x, y, d, 2) != meet;
+  }
+  std::printf("%d wrong, %d apart, %d not\n", bad, found[0], found[1]);
+  return bad != 0 || found[0] < 2000 || found[1] < 2000;
+}
+"""
+
 
 def compiled(tmp_path, source):
     (tmp_path / "strided.cpp").write_text(source)
@@ -489,3 +511,23 @@ def test_outputs_that_share_elements_among_themselves_are_refused():
     n = dict(n=0)                                                # nothing else is wrong but the workspace
     assert call4("attend", params4(o_stride=[1024, 128]), **n) == call4("attend", params4(o_stride=[128, 896]), **n) == -3
     assert call4("attend", params4(n_rows=1, o_stride=[0, 128]), **n) == -3
+
+
+@pytest.mark.skipif(not shutil.which("g++"), reason="no host compiler")
+def test_tensors_that_share_elements_are_told_by_the_library(tmp_path):
+    compiled(tmp_path, MEET)
+
+
+def test_rotary_outputs_over_what_is_read_are_refused_by_the_library():
+    """2 sequences of 4 and 2 heads of 128, 10 tokens, bf16; queries and keys as slices [tokens, heads, d] of one tensor of 8 heads, or of
+    sequences inside of a token's row."""
+    far, row = 1 << 30, 8 * 128
+    fused = [10 * row, 128, row]
+    st = dict(q_stride=fused, q_out_stride=fused, k_stride=fused, k_out_stride=fused)
+    at = lambda heads: far + heads * 256  # noqa: E731
+    for q, q_out, k, k_out in ((at(0), at(1), None, None), (at(0), at(0), at(3), at(3)), (at(0), 2 * far, at(4), 2 * far + 256), (at(0), at(4), at(6), 2 * far),
+                               (at(0), 2 * far, at(6), at(3)), (at(0), at(4), at(3), 2 * far), (None, None, at(4), at(5))):
+        assert apply(rparams(**st), q=q, q_out=q_out, k=k, k_out=k_out) == -1, (q, q_out, k, k_out)
+    inner = [4 * 128, 128, 5 * 4 * 128]                          # [tokens, 5 sequences, 4 heads, d]: the second sequence of q is the first of k
+    p = rparams(q_stride=inner, q_out_stride=inner, k_stride=inner, k_out_stride=inner)
+    assert apply(p, q=far, q_out=far, k=far + 4 * 256, k_out=far + 4 * 256) == -1
