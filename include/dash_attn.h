@@ -447,8 +447,8 @@ int dash_rotary_apply(const dash_rotary_params* p, const dash_rotary* r, const i
 
 /* dash_paged_append with the new tokens' keys turned by their positions on the way, seen[b]-m+t or the slot (what goes into pos) as rotary positions.
  *   q, q_out  optional (both or none) [n_rows, h_q, d]: the new tokens' queries, turned as well; strides q_stride and
- *             o_stride of p.  q_out has a place for each element, may be q, and shares no element with k_new, v_new or, being another tensor, with q: where their
- *             extents overlap, equal strides have to show it (heads of one tensor; DASH_EINVAL otherwise).  Rows of no sequence, and of
+ *             o_stride of p.  q_out has a place for each element, may be q, and shares no element with k_new, v_new or, being another tensor, with q
+ *             (DASH_EINVAL otherwise; slices of one tensor that lie apart are fine).  Rows of no sequence, and of
  *             tokens without a slot (more new ones than lens), are not written; those of tokens without a page are. */
 int dash_paged_append_rotary(const dash_paged_params* p, const dash_rotary* r, const void* q, void* q_out,
                              const void* k_new, const void* v_new, void* k_pages, void* v_pages, const int32_t* row_start,

@@ -576,7 +576,7 @@ def _rotary_pair(x, y):
         raise DashError("an output has an element for each of its own")
     x_end = xp + ((b - 1) * xs[0] + (h - 1) * xs[1] + (n - 1) * xs[2] + d) * size
     y_end = yp + ((b - 1) * ys[0] + (h - 1) * ys[1] + (n - 1) * ys[2] + d) * size
-    if xp < y_end and yp < x_end and (xp != yp or xs != ys):
+    if xp < y_end and yp < x_end and (xp != yp or xs != ys) and _meet((xs[:3], xp), shape[:3], (ys[:3], yp), shape[:3], d, size):
         raise DashError("an output is its input or does not overlap it")
     return shape, (xs, xp, x_end), (ys, yp, y_end)
 
@@ -671,7 +671,8 @@ def _fresh_rows(p, k_new, v_new, q, q_out):
     qs, os, qp, op = q.stride(), q_out.stride(), q.data_ptr(), q_out.data_ptr()
     if (qp != op or qs != os) and len(qs) == len(os) == 3:       # other shapes are refused with the packed rows'
         n, h, size = p.n_rows - 1, p.h_q - 1, q.element_size()
-        if qp < op + (n * os[0] + h * os[1] + p.head_dim) * size and op < qp + (n * qs[0] + h * qs[1] + p.head_dim) * size:
+        if (qp < op + (n * os[0] + h * os[1] + p.head_dim) * size and op < qp + (n * qs[0] + h * qs[1] + p.head_dim) * size
+                and _meet((qs[:2], qp), q.shape[:2], (os[:2], op), q_out.shape[:2], p.head_dim, size)):
             raise DashError("q_out is q or does not overlap it")
     return (k_new, p.h_kv, "k_new_stride"), (v_new, p.h_kv, "v_new_stride"), (q, p.h_q, "q_stride"), (q_out, p.h_q, "o_stride")
 

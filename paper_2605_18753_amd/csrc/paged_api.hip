@@ -2,8 +2,6 @@
 #include <math.h>
 #include <string.h>
 
-#include <utility>
-
 #include "paged.h"
 #include "rotary.h"
 #include "strided.h"
@@ -55,19 +53,6 @@ static int paged_args(const dash_paged_params* p, PagedArgs* a, bool rows, bool 
 }
 
 static bool misaligned(const void* x) { return ((uintptr_t)x & 15) != 0; }
-// Packed rows of heads (the call's rows; d elements of es bytes): whether x and y may share an element.  Those of one tensor do not where their strides are the
-// same and their heads lie apart within a row, or modulo the smaller stride where the other one is a multiple of it.
-struct Heads { const void* at; int64_t t, h; int heads; };
-static bool may_meet(Heads x, Heads y, const PagedArgs& a, int d, int es) {
-  if ((uintptr_t)x.at > (uintptr_t)y.at) std::swap(x, y);
-  const auto row = [&](const Heads& z) { return (z.heads - 1) * z.h + d; };
-  const int64_t off = (int64_t)(((uintptr_t)y.at - (uintptr_t)x.at) / es);     // both are aligned
-  if (a.n_rows == 0 || off >= (a.n_rows - 1) * x.t + row(x)) return false;
-  if (x.t != y.t) return true;
-  if (row(x) <= off && off + row(y) <= x.t) return false;
-  const int64_t step = x.t < x.h ? x.t : x.h, more = x.t < x.h ? x.h : x.t;
-  return !(x.h == y.h && step > 0 && more % step == 0 && off % step >= d && off % step <= step - d);
-}
 // Whether packed rows of heads that a call writes share elements among themselves.
 static bool rows_repeat(const dash_paged_params* p, const PagedArgs& a, const void* o) {
   return strided_repeats({o, 2, {a.o_t, a.o_h}, {a.n_rows, a.h_q}}, p->head_dim);
@@ -75,10 +60,12 @@ static bool rows_repeat(const dash_paged_params* p, const PagedArgs& a, const vo
 // The turned queries of a call that appends: each in a place of its own, q's or apart from q, and apart from the new keys and values.
 static bool queries_meet(const dash_paged_params* p, const PagedArgs& a) {
   if (!a.q) return false;
-  const int es = p->dtype == DASH_BF16 ? 2 : 4, d = p->head_dim;
-  const Heads out = {a.o, a.o_t, a.o_h, p->h_q};
-  return rows_repeat(p, a, a.o) || (a.q == a.o ? a.q_t != a.o_t || a.q_h != a.o_h : may_meet({a.q, a.q_t, a.q_h, p->h_q}, out, a, d, es)) ||
-         may_meet({a.k_new, a.kn_t, a.kn_h, p->h_kv}, out, a, d, es) || may_meet({a.v_new, a.vn_t, a.vn_h, p->h_kv}, out, a, d, es);
+  const int es = p->dtype == DASH_BF16 ? 2 : 4;
+  const auto rows = [&](const void* at, int64_t t, int64_t h, int heads) { return Strided{at, 2, {t, h}, {a.n_rows, heads}}; };
+  const Strided out = rows(a.o, a.o_t, a.o_h, p->h_q);
+  const auto meets = [&](const Strided& x) { return strided_meet(x, out, p->head_dim, es); };
+  return rows_repeat(p, a, a.o) || (a.q == a.o ? a.q_t != a.o_t || a.q_h != a.o_h : meets(rows(a.q, a.q_t, a.q_h, p->h_q))) ||
+         meets(rows(a.k_new, a.kn_t, a.kn_h, p->h_kv)) || meets(rows(a.v_new, a.vn_t, a.vn_h, p->h_kv));
 }
 static int check_scratch(size_t need, const void* ws, size_t bytes) {
   return (!ws || ((uintptr_t)ws & 255) != 0 || bytes < need) ? DASH_EWORKSPACE : DASH_OK;

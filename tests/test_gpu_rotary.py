@@ -343,3 +343,31 @@ def test_appends_of_many_sequences(four):
             assert torch.equal(got[pg, :, off], want)
         else:
             check(got[pg, :, off], s.k_new[row], torch.tensor(position), R.thetas(64), "halves")
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_outputs_in_other_slices_of_their_inputs_tensor(dtype):
+    """Queries and keys turned into the free heads of their own rows, with sequences inside of a token's row; appends' queries likewise."""
+    n, batch, d = 30, 2, 64
+    x = draws(40)(n, batch, 10, d).to(dtype)
+    g = x.to(DEV)
+    r = B.make_rotary(d, DEV)
+    cut = lambda t, a, b: t[:, :, a:b].permute(1, 2, 0, 3)  # noqa: E731
+    B.dash_rotary(r, cut(g, 0, 4), cut(g, 5, 9), cut(g, 4, 5), cut(g, 9, 10))
+    at, theta = torch.arange(n), R.thetas(d)
+    check(cut(g, 5, 9), cut(x, 0, 4), at, theta, "halves")
+    check(cut(g, 9, 10), cut(x, 4, 5), at, theta, "halves")
+    assert torch.equal(g.cpu()[:, :, :5], x[:, :, :5])
+    for four in (False, True):
+        g = x[:, 0].to(DEV)
+        c = B.PagedCache4.allocate(1, 1, 2, 16, d, 2, DEV) if four else B.PagedCache.allocate(1, 1, 2, 16, d, 2, DEV, dtype=dtype)
+        c.table.copy_(torch.arange(2)[None])
+        c.lens.fill_(n)
+        start = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+        if four:
+            B.dash_paged4_append(B.make_paged4_params(c, n, 4, dtype=dtype), c, g[:, 4:5], g[:, 9:], start, rotary=r, q=g[:, :4], q_out=g[:, 5:9])
+        else:
+            B.dash_paged_append_rotary(B.make_paged_params(c, n, 4), c, r, g[:, 4:5], g[:, 9:], start, q=g[:, :4], q_out=g[:, 5:9])
+            check(c.k.cpu().transpose(0, 1).reshape(1, 32, d)[:, :n].transpose(0, 1), x[:, 0, 4:5], at[:, None], theta, "halves")
+        check(g[:, 5:9], x[:, 0, :4], at[:, None], theta, "halves")
+        assert torch.equal(g.cpu()[:, :5], x[:, 0, :5]) and torch.equal(g.cpu()[:, 9:], x[:, 0, 9:])

@@ -531,3 +531,19 @@ def test_rotary_outputs_over_what_is_read_are_refused_by_the_library():
     inner = [4 * 128, 128, 5 * 4 * 128]                          # [tokens, 5 sequences, 4 heads, d]: the second sequence of q is the first of k
     p = rparams(q_stride=inner, q_out_stride=inner, k_stride=inner, k_out_stride=inner)
     assert apply(p, q=far, q_out=far, k=far + 4 * 256, k_out=far + 4 * 256) == -1
+
+
+def test_queries_turned_into_another_slice_of_their_tensor():
+    """Apart from the queries, though in their span: accepted by appends into pages of either kind."""
+    c, full, r = cache4(), B.PagedCache.allocate(2, 2, 8, 16, 64, 4, "cpu"), B.make_rotary(64, "cpu")
+    p, fp, start = B.make_paged4_params(c, 3, 4), B.make_paged_params(full, 3, 4), torch.zeros(3, dtype=torch.int32)
+    x = torch.zeros((3, 12, 64), dtype=torch.bfloat16)
+    each = torch.zeros((3, 4, 4, 64), dtype=torch.bfloat16)      # (q, k, v, turned q) of each head side by side
+    for q, q_out, meet in ((x[:, :4], x[:, 4:8], False), (x[:, 4:8], x[:, :4], False), (x[:, :4], x[:, 3:7], True), (x[:, 8:], x[:, 5:9], True),
+                           (each[:, :, 0], each[:, :, 3], False), (each.view(3, 4, 256)[..., 32:96], each[:, :, 1], True)):
+        for f in (lambda: B.dash_paged4_append(p, c, x[:, 8:10], x[:, 10:], start, rotary=r, q=q, q_out=q_out),
+                  lambda: B.dash_paged_append_rotary(fp, full, r, x[:, 8:10], x[:, 10:], start, q=q, q_out=q_out)):
+            with pytest.raises(B.DashError, match="overlap" if meet else "GPU"):
+                f()
+        with pytest.raises(B.DashError, match="overlap" if meet else "GPU"):
+            B.dash_rotary(r, q.transpose(0, 1)[None], q_out.transpose(0, 1)[None])
