@@ -400,7 +400,7 @@ enum { DASH_ROT_HALVES = 0,     /* pair i: elements i and i + rot_dim / 2 */
 typedef struct dash_rotary {
   int32_t rot_dim;         /* leading elements of a head that turn                           */
   int32_t layout;          /* DASH_ROT_HALVES or DASH_ROT_ADJACENT                           */
-  float mscale;            /* factor on the elements that turn, > 0 (1: none)                */
+  double mscale;           /* factor on the elements that turn, > 0 (1: none), in fp32's range */
   int32_t reserved;        /* 0                                                              */
   const uint64_t* turns;   /* DEVICE pointer to rot_dim / 2 numbers from dash_rotary_turns   */
 } dash_rotary;

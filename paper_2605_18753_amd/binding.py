@@ -47,7 +47,7 @@ class dash_paged_params(ctypes.Structure):
 
 
 class dash_rotary_plan(ctypes.Structure):                  # dash_rotary of the header
-    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("mscale", ctypes.c_float), ("reserved", ctypes.c_int32),
+    _fields_ = [("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32), ("mscale", ctypes.c_double), ("reserved", ctypes.c_int32),
                 ("turns", ctypes.c_void_p)]
 
 

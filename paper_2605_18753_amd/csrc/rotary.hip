@@ -67,9 +67,9 @@ template <typename T, int D> static hipError_t launch_rotary(const RotateArgs& a
 int rotary_args(const dash_rotary* r, int head_dim, RotaryArgs* out) {
   if (!r || !r->turns || r->reserved != 0 || ((uintptr_t)r->turns & 7) != 0) return DASH_EINVAL;
   if (r->layout != DASH_ROT_HALVES && r->layout != DASH_ROT_ADJACENT) return DASH_EINVAL;
-  if (r->rot_dim < 1 || r->rot_dim > head_dim || !(r->mscale > 0.f) || !isfinite(r->mscale)) return DASH_EINVAL;
+  if (r->rot_dim < 1 || r->rot_dim > head_dim || !((float)r->mscale > 0.f) || !isfinite((float)r->mscale)) return DASH_EINVAL;
   if (r->rot_dim % 16 != 0) return DASH_EUNSUPPORTED;
-  *out = {r->turns, r->rot_dim / 2, r->layout == DASH_ROT_ADJACENT, (double)r->mscale};
+  *out = {r->turns, r->rot_dim / 2, r->layout == DASH_ROT_ADJACENT, r->mscale};
   return DASH_OK;
 }
 

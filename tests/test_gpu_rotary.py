@@ -371,3 +371,32 @@ def test_outputs_in_other_slices_of_their_inputs_tensor(dtype):
             check(c.k.cpu().transpose(0, 1).reshape(1, 32, d)[:, :n].transpose(0, 1), x[:, 0, 4:5], at[:, None], theta, "halves")
         check(g[:, 5:9], x[:, 0, :4], at[:, None], theta, "halves")
         assert torch.equal(g.cpu()[:, :5], x[:, 0, :5]) and torch.equal(g.cpu()[:, 9:], x[:, 0, 9:])
+
+
+@pytest.mark.parametrize("layout", ["halves", "adjacent"])
+def test_scales_that_are_no_floats(layout):
+    """The factor is held in 64 bits: each number is as near as with a factor of 1, times it.  Cut to 24 bits 0.1 would be off by 0.25 u, 1.2 by 0.67 u of every number:
+    sums over many numbers show what each one's bound has room for."""
+    x, at, theta = draws(41)(1, 4, 500, 128), torch.arange(500), R.thetas(128)
+    for mscale in (1.2, 0.1):
+        r = B.make_rotary(128, DEV, layout=layout, mscale=mscale)
+        y = torch.empty_like(x, device=DEV)
+        for inverse in (False, True):
+            B.dash_rotary(r, x.to(DEV), y, inverse=inverse)
+            want, tol = R.turn(x, at, theta, layout, 1.0, inverse)
+            want, tol = mscale * want, mscale * tol + 2.0 ** -149
+            off = y.cpu().double() - want
+            assert (off.abs() <= tol).all()
+            # roundings, whose signs differ, up to tol each: their share of sum w y, w = want, is below 6 sqrt(sum (w tol)^2); a factor off by f gives f sum w^2
+            w, bound = want, 6 * float(((want * tol) ** 2).sum().sqrt())
+            assert bound < 0.1 * R.U * float((w ** 2).sum()) and abs(float((w * off).sum())) <= bound
+    # keys in 4 bits: as the definition in 64 bits says, number by number
+    for dtype in (BF, F32):
+        x = draws(42)(600, 2, 128).to(dtype)
+        c = B.PagedCache4.allocate(1, 2, 38, 16, 128, 38, DEV)
+        c.table.copy_(torch.arange(38)[None])
+        c.lens.fill_(600)
+        B.dash_paged4_append(B.make_paged4_params(c, 600, 2, dtype=dtype), c, x.to(DEV), x.to(DEV), torch.tensor([0, 600], dtype=torch.int32, device=DEV), rotary=r)
+        got = R.values(c.k_codes.cpu(), c.k_scales.cpu()).transpose(0, 1).reshape(2, 608, 128)[:, :600].transpose(0, 1)
+        want = 0.1 * R.turn(x, torch.arange(600)[:, None], theta, layout)[0]
+        assert torch.equal(got, R.values(*R.quantise(want)))

@@ -547,3 +547,10 @@ def test_queries_turned_into_another_slice_of_their_tensor():
                 f()
         with pytest.raises(B.DashError, match="overlap" if meet else "GPU"):
             B.dash_rotary(r, q.transpose(0, 1)[None], q_out.transpose(0, 1)[None])
+
+
+def test_a_plans_scale_is_held_in_64_bits():
+    for mscale in (1.2, 0.1, 1.0 + 2.0 ** -40):
+        assert B.make_rotary(64, "cpu", mscale=mscale).plan.mscale == mscale
+    for mscale in (1e39, 1e-50, -0.1):                           # no float
+        assert apply(r=plan(mscale=mscale)) == -1
