@@ -392,7 +392,7 @@ int dash_paged_evict(const dash_paged_params* p, void* k_pages, void* v_pages, i
  * The calls above take queries and keys as they are; in most models these carry their token's position as a rotation.
  * Pair i of the first rot_dim elements of a head, (x, y), becomes mscale (x cos a - y sin a, x sin a + y cos a) with a = position * theta_i; the
  * other elements stay.  A theta is held as the 64-bit fraction of a whole turn that it makes; position times that, modulo 2^64, is the angle's own
- * fraction, off by at most |position| 2^-65 of a turn (4e-10 radians at 2^31).  cos and sin are evaluated in 64 bits.
+ * fraction, off by at most |position| 2^-65 of a turn (4e-10 radians at 2^31; thetas of up to 2^30, larger ones by |theta| 2^-112 a position more).  cos and sin are evaluated in 64 bits.
  * Limits (DASH_EUNSUPPORTED beyond them): head_dim 64 or 128; rot_dim a multiple of 16 up to head_dim. */
 enum { DASH_ROT_HALVES = 0,     /* pair i: elements i and i + rot_dim / 2 */
        DASH_ROT_ADJACENT = 1 }; /* pair i: elements 2 i and 2 i + 1       */

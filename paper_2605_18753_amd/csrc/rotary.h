@@ -1,7 +1,7 @@
 // Rotary positions: what the kernels that turn queries and keys share.
 //
 // Pair i, (x, y), becomes mscale (x cos a - y sin a, x sin a + y cos a), a = position theta_i.  theta_i comes as the 64-bit fraction of a whole turn that
-// it makes, so position * fraction modulo 2^64 is the angle's own fraction: off by position * 2^-65 turns, 4e-13 radians at a million, where
+// it makes, so position * fraction modulo 2^64 is the angle's own fraction: off by position * 2^-65 turns, 1.7e-13 radians at a million, where
 // a product in fp32 is off by 0.06.  The nearest quarter turn is taken off in whole numbers, and the rest, at most pi / 4, goes into the Taylor series of
 // sine and cosine in 64 bits (terms up to y^17 and y^16: what follows is below 1e-17).
 #pragma once

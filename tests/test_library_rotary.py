@@ -554,3 +554,24 @@ def test_a_plans_scale_is_held_in_64_bits():
         assert B.make_rotary(64, "cpu", mscale=mscale).plan.mscale == mscale
     for mscale in (1e39, 1e-50, -0.1):                           # no float
         assert apply(r=plan(mscale=mscale)) == -1
+
+
+def test_turns_are_the_nearest_fractions():
+    """A table off by more than half of its last bit would be off by more than |position| 2^-65 turns.  113 bits leave a theta of 2^30 2^-19 units of that bit."""
+    D, most = decimal.Decimal, decimal.Decimal("0.50001")
+    near = lambda want, got: abs((want * TURN - got).remainder_near(TURN)) <= most  # noqa: E731
+    for rot in range(16, 144, 16):
+        for base in (10000.0, 500000.0, 1e6, 10.0, 0.5, 1.0, 123456.789):
+            rc, got = turns(rot, base=base)
+            assert rc == 0 and all(near(t / R.TWO_PI, g) for t, g in zip(R.thetas(rot, base), got)), (rot, base)
+        theta, f = R.thetas(rot), D(8)
+        for scaling, want in ((1, [t / f for t in theta]), (2, [((D(10000).ln() + f.ln() * rot / (rot - 2)) * -2 * i / rot).exp() for i in range(rot // 2)]),
+                              (3, [t * (c + (1 - c) / f) for t, c in ((t, min(max((D(8192) * t / R.TWO_PI - 1) / 31, D(0)), D(1))) for t in theta)])):
+            rc, got = turns(rot, scaling=scaling, factor=8.0, original=8192.0, low=1.0, high=32.0)
+            assert rc == 0 and all(near(t / R.TWO_PI, g) for t, g in zip(want, got)), (rot, scaling)
+    gen = torch.Generator().manual_seed(1)
+    freq = [1.0, 3.0, 100.0, -100.0, 0.1, 2.0 ** 30, -(2.0 ** 30 - 0.3), 1e-9, 5e-324, 0.0, 2 * math.pi] + (torch.randn(37, generator=gen, dtype=torch.float64) * 1000).tolist()
+    rc, got = turns(96, freq=freq)
+    assert rc == 0 and all(near(D(f) / R.TWO_PI % 1, g) for f, g in zip(freq, got))
+    for huge in (1e300, -1e22):                                  # finite: a fraction, whichever
+        assert turns(16, freq=[huge] * 8)[0] == 0
