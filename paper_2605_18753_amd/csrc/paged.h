@@ -11,7 +11,7 @@
 //   Tiles of 128 rows: one item a workgroup; items that leave the chip idle are cut into parts.  With n items of costs c_i and W > n
 //   workgroups, parts of S = ceil(sum c_i / (W - n)) give sum ceil(c_i / S) <= W of them.  W is what is resident at once, or n and one and a
 //   half times that where the items' lengths would leave much of the chip idle; or one item a CU stays whole and the others are cut to fill up what
-//   these leave (paged_part_size).  (Finer parts: 40 tokens of 40 sequences of 300 to 8000, 32 / 2 heads, 196 -> 157 us; 700 of one of 30000
+//   these leave (paged_cut.h).  (Finer parts: 40 tokens of 40 sequences of 300 to 8000, 32 / 2 heads, 196 -> 157 us; 700 of one of 30000
 //   384 -> 360; 1501 tokens beside decoding ones, where they are not taken, 305 and 326.)
 //   (Equal runs for these as well: a run begins anew for every piece of an item, and most are cut.  1501 tokens beside seven decoding
 //   sequences of up to 12k 305 -> 309 us and the records to add up, 2048 tokens against 32k 995 -> 1088.)
@@ -21,6 +21,7 @@
 #pragma once
 #include "common.h"
 #include "dash_internal.h"
+#include "paged_cut.h"
 
 namespace dash {
 
@@ -43,7 +44,7 @@ struct PagedArgs {
   int pad;                               // runs: steps that an item's start counts for
   int few;                               // > 0: the launch has the sequences of up to so many rows; < 0: those of more than -few; 0: all
 };
-// What these two ask for, and the dealing of items of one length (paged_part_size), is compiled for such a cache alone (FOUR): for pages of bf16, where they would
+// What these two ask for, and the dealing of items of one length (paged_cut.h), is compiled for such a cache alone (FOUR): for pages of bf16, where they would
 // change nothing, they took a launch 0.3 to 1 us (one token of 16 sequences of 200 to 1000 12.65 -> 13.1, a prompt of 1000 28.9 -> 29.8).
 
 __device__ __forceinline__ int paged_len(const PagedArgs& a, int b) { return min(max(a.lens[b], 0), a.cap); }
@@ -103,14 +104,10 @@ __device__ __forceinline__ bool paged_place(const PagedArgs& a, int row, PagedPl
 
 // ---- parts (tiles of 128 rows) ----------------------------------------------------------------------------------------
 constexpr int kCUs = 256;
-constexpr int kMinPart = 4;                                // steps a part has at least
-// The size S of a part, no item costing more: none is cut; a wave's lanes together.  shape(m, n) gives a sequence's tiles and the cost
-// of one (at least 1); l0: the first 64 sequences.
-constexpr int kUncut = 0x3fffffff;
-struct PagedCut { int size, whole, items; };               // of the items behind the first `whole`
 // of sequence tiles, those among the first `whole` items; before: items before the sequence's
 __device__ __forceinline__ int paged_whole(const PagedCut& cut, int before, int tiles) { return min(max(cut.whole - before, 0), tiles); }
-// The launch that adds the parts up has to come to the same: no products are fused with sums here.
+// How a launch's items are cut (paged_cut.h); a wave's lanes together.  shape(m, n) gives a sequence's tiles and the cost of one (at least 1); l0: the first 64
+// sequences.
 template <bool FOUR, typename F> __device__ __forceinline__ PagedCut paged_part_size(const PagedArgs& a, const PagedLane& l0, F&& shape) {
 #pragma clang fp contract(off)
   if (a.wgs <= 0) return {kUncut, 0, 0};
@@ -126,35 +123,7 @@ template <bool FOUR, typename F> __device__ __forceinline__ PagedCut paged_part_
     cost += wave_sum((float)s.x * (float)s.y);
     most = fmaxf(most, wave_max(s.x > 0 ? (float)s.y : 0.f));
   }
-  if (items >= a.wgs) return {kUncut, 0, items};
-  const auto size = [&](float c, int w) { return max((int)fminf(c * 1.0001f / (float)(w - items), 1e9f) + 1, kMinPart); };   // the factor covers the sum's rounding
-  // The time, in steps, of parts that are all resident (or of items, where more are not), and of finer ones that follow each other: what everybody
-  // has on the average, half a part until the last is done (a quarter beside whole items, which run faster alone), and what a part costs besides: 4
-  // steps, or 10 where it is one more than a workgroup would have.  (One item a CU whole, the others filling up: 2200 tokens against 32k, 32 / 8
-  // heads, 69 items for 64 places, 1418 -> 1197 us; 1500, 47 items, 865 -> 785; against 2000, where it is not done, 54 and 64.)
-  const float even = cost / (float)a.slots;
-  PagedCut cut = {items < a.slots ? size(cost, a.slots) : kUncut, 0, items};
-  float time = items <= a.slots ? fminf((float)cut.size, most) : fminf((float)((items + a.slots - 1) / a.slots) * most, even + 0.5f * most);
-  // A cache in 4 bits, items of one length (one sequence's): as many parts each as there are places for, once or twice.  (The sum over w - n leaves places unused: 512 tokens against 32k in 4 bits, 16
-  // items for 64 places, in three parts each 330 us, in four 296; 700, 22 items: five parts take 0.85 of the time of two.)
-  bool finer = false;
-  if (FOUR && items <= a.slots && most * (float)items <= cost) {
-    const auto parts = [&](int k) { return max((int)ceilf(most / (float)max(k, 1)), kMinPart); };
-    const int once = parts(a.slots / max(items, 1)), twice = parts(min(2 * a.slots, a.wgs) / max(items, 1));
-    finer = 2 * twice + 6 < once;
-    cut.size = finer ? twice : once;
-    time = (float)once;
-  } else if (a.wgs > a.slots) {
-    const int fine = size(cost, a.wgs);
-    finer = even + 0.5f * (float)fine + 4.f < a.gain * time;
-    if (finer) cut.size = fine;
-  }
-  if (a.wgs > a.slots && !finer && items > half && most * (float)items < 1.2f * cost) {   // of like lengths: one item a CU stays whole, the others fill up what these leave
-    const int fill = max(size(rest, a.wgs), (int)(0.5f * even));
-    if (even + 0.25f * (float)fill + 10.f < (a.gain + 0.05f) * time) cut = {fill, half, items};
-  }
-  if ((float)cut.size >= most) cut = {kUncut, 0, items};
-  return cut;
+  return paged_cut<FOUR>(a.wgs, a.slots, a.gain, items, cost, most, rest);
 }
 
 struct PagedPart { int b, tile, part, parts, rec0, r0, m, n; };   // rec0: the item's first part among those of the kv-head
