@@ -22,7 +22,8 @@ struct StridedSteps {
     if (stride != 0 && lo < hi) step[n++] = {stride, lo, hi};
   }
   void sort() {
-    std::sort(step, step + n, [](const Step& x, const Step& y) { return x.stride > y.stride; });
+    for (int i = 1; i < n; i++)
+      for (int k = i; k > 0 && step[k].stride > step[k - 1].stride; k--) std::swap(step[k], step[k - 1]);
   }
   static Place floor_div(Place x, Place y) { return x >= 0 ? x / y : -((y - 1 - x) / y); }
   bool near(int i, Place off) {
@@ -45,6 +46,11 @@ inline bool strided_repeats(const Strided& x, int d) {
   StridedSteps all(d);
   for (int i = 0; i < x.dims; i++) all.add(x.stride[i], 1 - x.size[i], x.size[i] - 1);
   all.sort();
+  // mostly each index goes through what one step of the next larger stride holds
+  StridedSteps::Place span = d;
+  int inside = all.n;
+  while (inside > 0 && all.step[inside - 1].stride >= span) span += all.step[inside - 1].stride * all.step[inside - 1].hi, inside--;
+  if (inside == 0) return false;
   for (int i = 0; i < all.n; i++) {
     StridedSteps s = all;
     s.step[i].lo = 1;
@@ -55,6 +61,12 @@ inline bool strided_repeats(const Strided& x, int d) {
 
 // Whether two tensors of es bytes an element and as many dimensions share elements; their addresses are multiples of es.
 inline bool strided_meet(const Strided& x, const Strided& y, int d, int es) {
+  const auto end = [&](const Strided& z) {
+    StridedSteps::Place e = d;
+    for (int i = 0; i < z.dims; i++) e += (StridedSteps::Place)z.stride[i] * (z.size[i] - 1);
+    return (StridedSteps::Place)(uintptr_t)z.at + e * es;
+  };
+  if (end(x) <= (StridedSteps::Place)(uintptr_t)y.at || end(y) <= (StridedSteps::Place)(uintptr_t)x.at) return false;
   StridedSteps s(d);
   for (int i = 0; i < x.dims; i++) {
     if (x.stride[i] == y.stride[i]) {
