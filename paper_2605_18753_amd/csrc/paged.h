@@ -36,15 +36,14 @@ struct PagedArgs {
   float c1;                              // scale * log2(e)
   int wgs;                               // runs of a kv-head; 0: an item a workgroup.  Tiles of 128 rows: parts of a kv-head at most; 0: none is cut
   int whole;                             // runs: items may be left uncut; weights: two kernels share the sequences
+  int pad;                               // a cache in 4 bits, runs: steps that an item's start counts for
+  int few;                               // a cache in 4 bits: > 0: the launch has the sequences of up to so many rows; < 0: those of more than -few; 0: all
   int slots; float gain;                 // tiles of 128 rows: workgroups of a kv-head that are resident at once; what finer parts must come to
   float* part_o; float* part_ml;         // records of cut items: two of each run (the item it begins in, the one it ends in), one of each part
+  const uint8_t* k_sc; const uint8_t* v_sc;   // a cache in 4 bits: its scales (k and v its codes, their strides in bytes)
   uint64_t* flags; uint64_t nonce;       // runs: two of each record, and the number that says that it is complete
-  // a cache in 4 bits only (k and v its codes, their strides in bytes)
-  const uint8_t* k_sc; const uint8_t* v_sc;   // its scales
-  int pad;                               // runs: steps that an item's start counts for
-  int few;                               // > 0: the launch has the sequences of up to so many rows; < 0: those of more than -few; 0: all
 };
-// What these two ask for, and the dealing of items of one length (paged_cut.h), is compiled for such a cache alone (FOUR): for pages of bf16, where they would
+// What `pad` and `few` ask for, and the dealing of items of one length (paged_cut.h), is compiled for such a cache alone (FOUR): for pages of bf16, where they would
 // change nothing, they took a launch 0.3 to 1 us (one token of 16 sequences of 200 to 1000 12.65 -> 13.1, a prompt of 1000 28.9 -> 29.8).
 
 __device__ __forceinline__ int paged_len(const PagedArgs& a, int b) { return min(max(a.lens[b], 0), a.cap); }
