@@ -3,7 +3,7 @@
 // Few rows: a tile is 16 (token, head) rows, or two groups of 16 that share what is read and converted.  K goes from the pages into registers: the contraction over d runs in the order in which a lane's
 // codes lie, d = D / 4 kq + .., so 16 bytes of a row are one load, one scale and, converted, the lane's operands of all steps.  V is converted into LDS, from
 // where transposing reads give its operands.  The next tile's loads are in flight while a tile is worked on.  Bound by HBM where the cache is long: 32 sequences
-// of 4096 to 32768 tokens, 32 / 8 heads of 128, 125 us, 660 MB at 5.3 TB/s, of which 8 us are the launch's start and end (the vector units issue in 0.42 of the
+// of 4096 to 32768 tokens, 32 / 8 heads of 128, 125 to 127 us, 660 MB at 5.2 TB/s, of which 8 us are the launch's start and end (the vector units issue in 0.44 of the
 // clocks); by latency where it is short: one sequence of 1000 tokens 9.2 us.
 #include "fp4.h"
 #include "paged_few.h"

@@ -33,7 +33,7 @@ template <typename T, int D, int N> struct Heads {
 
 // A wave has a packed row.  What the row holds is asked for first, with the turns; then the row's place is found, a lane works out the cosine and sine of a
 // pair, into LDS, and takes those of its unit's eight pairs from there.
-// Bound by HBM: 2047 tokens of each of four sequences, 32 / 8 heads of 128, 42.6 us, 101 MB in and 102 out at 4.8 TB/s; by latency where there are few: 32
+// Bound by HBM: 2047 tokens of each of four sequences, 32 / 8 heads of 128, 42.6 us, 101 MB in and 102 out at 4.8 TB/s; by latency where there are few: 64
 // tokens 5.3 us.  (Of that many, two heads asked for ahead; four, which costs registers and waves, 3 us more.)
 template <typename T, int D>
 __global__ __launch_bounds__(256, 4) void paged_append_rotary_kernel(PagedArgs a, RotaryArgs r) {

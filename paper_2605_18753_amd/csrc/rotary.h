@@ -80,7 +80,7 @@ __device__ __forceinline__ Eight eight_of(const Piece<float>& p) {
 
 // A unit is two 16-byte pieces of a head, of V elements each, and V pairs (or none, behind the rotated part): of pairs that lie apart, piece a has
 // the first elements and b the second ones; neighbours lie in a piece, V / 2 pairs, and b is half a head behind a.  Neighbouring units are neighbours in memory.
-// (Pieces one behind the other in a thread: 2 x 20 heads of 64 x 3001 tokens in fp32 17.2 us; as here 11.4.)
+// (Pieces one behind the other in a thread: 2 x 20 heads of 64 x 3001 tokens in fp32 17.2 us; as here 11.5 to 11.9 by card.)
 template <typename T, int D> struct Unit {
   static constexpr int V = 16 / sizeof(T), COUNT = D / (2 * V);                // units of a head
   int a, b, pa, pb;              // elements where the pieces begin; first pairs of the lower and the upper half of cs

@@ -58,7 +58,7 @@ template <typename T, int D> static hipError_t launch_rotary(const RotateArgs& a
   const int heads = a.heads[0] > a.heads[1] ? a.heads[0] : a.heads[1];
   const uint32_t groups = (a.all + kTok - 1) / kTok, most = 1u << 20;
   // Few tokens: the heads of a token go to several workgroups, each of which works out the cosines and sines.  (Up to 512 workgroups; without: 1000 tokens of 40
-  // heads of 128 8.7 us instead of 7.9; up to 1024: 2 x 20 heads of 64 x 3001 tokens in fp32 12.1 instead of 11.5.)
+  // heads of 128 8.7 us instead of 7.9; up to 1024: 2 x 20 heads of 64 x 3001 tokens in fp32 12.1 instead of 11.5, by card up to 11.9.)
   const uint32_t split = groups >= 512 ? 1 : (512 + groups - 1) / groups, turns = (uint32_t)(heads + SLOTS - 1) / SLOTS;
   hipLaunchKernelGGL((rotary_kernel<T, D>), dim3(groups < most ? groups : most, split < turns ? split : turns), dim3(256), 0, st, a);
   return hipGetLastError();
