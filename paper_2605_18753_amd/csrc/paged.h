@@ -292,13 +292,13 @@ template <bool FOUR> struct PagedRun {
     end = __builtin_amdgcn_readfirstlane(b.at(wg + 1));
     if (next >= end) return false;
     const int in = deal.find(a, l0, next, true, it);
-    x0 = max(in - deal.pad, 0);
-    next += x0 + deal.pad - in;
+    x0 = FOUR ? max(in - deal.pad, 0) : in;
+    if constexpr (FOUR) next += x0 + deal.pad - in;
     cost = deal.steps(it.s, it.tile);
     return piece();
   }
   __device__ __forceinline__ bool piece() {
-    if (next >= end) return false;                         // no more than an item's start
+    if (FOUR && next >= end) return false;                 // no more than an item's start
     x1 = min(cost, x0 + end - next);
     next += x1 - x0;
     return true;
